@@ -12,6 +12,13 @@
  *       autocorrelation / empirical Fisher of the method-family table);
  *   (3) exact top-k lookup of a query against the gradient store (section
  *       "Attribution Pipelines": every store supports exact top-k).
+ * Beside that core stand the training steps it attributes:
+ *   (4) token log-probabilities, the clipped policy loss with a KL term and
+ *       the paired log-ratio preference loss, with their gradients with
+ *       respect to the logits (the gradients whose per-example products (1)
+ *       projects);
+ *   (5) the AdamW step over a model's tensors, whose second moments are the
+ *       optimizer states that (1) divides gradients by.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -58,7 +65,9 @@ typedef enum {
   ATTR_ERR_DEVICE = 5        /* HIP launch / runtime error */
 } attr_status;
 
-typedef enum { ATTR_F32 = 0, ATTR_BF16 = 1, ATTR_F16 = 2 } attr_dtype;
+/* ATTR_E4M3 (8 bits: sign, 4 exponent and 3 mantissa bits, largest value 448)
+ * is a type of attr_adamw_step's states only. */
+typedef enum { ATTR_F32 = 0, ATTR_BF16 = 1, ATTR_F16 = 2, ATTR_E4M3 = 3 } attr_dtype;
 
 typedef enum {
   ATTR_PRECOND_NONE = 0,  /* identity */
@@ -274,6 +283,148 @@ attr_status attr_score_topk(const void* Q, int64_t n_q, int64_t ldq, const void*
                             int32_t k, int64_t index_base, int32_t merge,
                             float* top_score, int64_t* top_index,
                             void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* (4) Losses over token log-probabilities, and their gradients.            */
+/* ------------------------------------------------------------------------ */
+
+/* A batch's rows of logits and the token each row predicts.  Token t of
+ * example i is row (row_offset ? row_offset[i] : i * T) + t, as in
+ * attr_project.  A token COUNTS if t < length[i], its row lies in
+ * [0, n_rows), its target in [0, V) and its weight is not 0; the logits of
+ * tokens that do not count are never read (padding may hold any bits).
+ * With a row's largest logit z_max and s = logit_scale,
+ *     logp = s (z_target - z_max) - log sum_j exp(s (z_j - z_max)),
+ * differences, products and sums in fp32.  Logits of -inf are vocabulary
+ * entries of probability 0; a row that holds a NaN or +inf, or -inf only, has
+ * logp NaN.
+ * Outputs of rows that do not count: without row_offset every row i * T + t,
+ * t < T, is written (logp 0, dlogits zeros); with row_offset the rows of
+ * tokens t < length[i] (clamped to [0, T]), and no others, are written.  The
+ * ranges of two examples must not overlap.
+ * Read only during the call (host struct with device pointers). */
+typedef struct {
+  const void* logits;    /* [n_rows, V], row stride ldl >= V; any V, stride and element alignment */
+  attr_dtype dtype;      /* ATTR_F32, ATTR_BF16 or ATTR_F16 */
+  int64_t n_rows, V, ldl;  /* 1 <= V <= 2^28 */
+  float logit_scale;     /* s: one over the sampling temperature; > 0 */
+  const int64_t* target;   /* device [n_rows] */
+  const float* weight;     /* device [n_rows] or NULL (1 for every token) */
+  int64_t n_examples, T;   /* n_examples * T < 2^31; without row_offset n_rows >= n_examples * T */
+  const int64_t* row_offset;  /* device [n_examples] or NULL (then i * T) */
+  const int32_t* length;      /* device [n_examples] or NULL (then T); clamped to [0, T] */
+} attr_token_rows;
+
+/* logp of every token (see above) into logp, device fp32 [n_rows]: what a
+ * rollout records of the tokens it samples (T = 1: one decoding step), and
+ * what a reference model gives for whole sequences.
+ *   ws  attr_token_logp_workspace_size(rows) bytes, 256-byte aligned */
+size_t attr_token_logp_workspace_size(const attr_token_rows* rows);
+attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/* Clipped policy loss with a KL term (the GRPO losses whose gradients section
+ * "Attribution Pipelines" collects).  For a token that counts, with its
+ * weight w, its advantage A and ratio = exp(logp - logp_old):
+ *     l = max(-A ratio, -A clip(ratio, 1 - clip_low, 1 + clip_high))
+ *         + beta (exp(logp_ref - logp) - (logp_ref - logp) - 1)
+ *     loss[i] = sum_t w l          (0 for an example without such tokens)
+ *     c = dloss/dlogp = w ((-A ratio if that is the maximum, else 0)
+ *                          - beta (exp(logp_ref - logp) - 1))
+ *     dlogits[row, j] = s c ([j = target] - exp(logp_j))
+ * The weights carry the mask and the normalisation (1 / tokens for a mean over
+ * each example, one constant for a sum, a loss scale).  Each row of logits is
+ * read once and each row of dlogits written once where a row fits a
+ * workgroup's registers (256 KB); loss sums are formed in fp64 in a fixed order.
+ *   advantage  device fp32 [n_examples], or [n_rows] with per_token != 0
+ *   logp_old   device fp32 [n_rows], or NULL: the logits' own (ratio 1)
+ *   logp_ref   device fp32 [n_rows]; may be NULL if beta is 0
+ *   clip_low, clip_high  >= 0 (clip_high may be infinite); beta >= 0
+ *   loss       device fp32 [n_examples]
+ *   logp       device fp32 [n_rows] or NULL
+ *   dlogits    device [n_rows, V] of the logits' type, row stride ldd >= V, or
+ *              NULL (the loss alone); may be the logits themselves with
+ *              ldd = ldl, any other overlap is ATTR_ERR_INVALID_ARG
+ *   ws         attr_policy_loss_workspace_size(rows) bytes, 256-byte aligned */
+size_t attr_policy_loss_workspace_size(const attr_token_rows* rows);
+attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage, int32_t per_token,
+                             const float* logp_old, const float* logp_ref, float clip_low,
+                             float clip_high, float beta, float* loss, float* logp, void* dlogits,
+                             int64_t ldd, void* ws, size_t ws_bytes, void* stream);
+
+/* Preference loss over paired log ratios.  n_examples = 2 n_pairs: pair p's
+ * chosen sequence is example p, its rejected one example n_pairs + p.
+ *     log_ratio[i] = sum_t w (logp - logp_ref)      (over tokens that count)
+ *     h = beta (log_ratio[p] - log_ratio[n_pairs + p]) - margin
+ *     loss[p] = pw ((1 - e) softplus(-h) + e softplus(h)),  e = label_smoothing
+ *     c = dloss/dlogp = +-w pw beta (e sigma(h) - (1 - e) sigma(-h))
+ *                                  (+: chosen, -: rejected)
+ *     dlogits[row, j] = s c ([j = target] - exp(logp_j))
+ * Without logp_ref (NULL) the ratios are the log-probabilities themselves;
+ * weights of 1 / tokens make them means.  Sums over tokens are formed in fp64
+ * in a fixed order.  The gradient needs both sequences' sums first, so the
+ * logits are read twice.
+ *   logp_ref     device fp32 [n_rows] or NULL
+ *   pair_weight  device fp32 [n_pairs] or NULL (1)
+ *   beta, margin finite;  label_smoothing in [0, 1]
+ *   loss         device fp32 [n_pairs]
+ *   log_ratio    device fp32 [n_examples] or NULL
+ *   logp, dlogits, ldd  as attr_policy_loss
+ *   ws           attr_preference_loss_workspace_size(rows) bytes */
+size_t attr_preference_loss_workspace_size(const attr_token_rows* rows);
+attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_ref,
+                                 const float* pair_weight, float beta, float margin,
+                                 float label_smoothing, float* loss, float* log_ratio, float* logp,
+                                 void* dlogits, int64_t ldd, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* (5) attr_adamw_step: one AdamW step over many tensors.                    */
+/* ------------------------------------------------------------------------ */
+
+/* One tensor of n contiguous elements (host struct with device pointers; any
+ * element alignment).  With 8-bit states m and v hold E4M3 values in blocks of
+ * 256 elements, the last one as long as what is left: m_e = m_scale[b] m[e],
+ * and v holds the root of the second moment, v_e = (v_scale[b] v[e])^2; a
+ * block's scale is its largest magnitude over 448.  Zeroed states and scales
+ * are those of step 0. */
+typedef struct {
+  void* p;          /* weights, p_dtype; with a master: its rounding, written and never read */
+  const void* g;    /* gradients, g_dtype */
+  void* m;          /* first moment, state_dtype */
+  void* v;          /* second moment, or its root (8-bit), state_dtype */
+  float* master;    /* fp32 weights that the step updates, or NULL: p itself */
+  float* m_scale;   /* 8-bit states: fp32 [(n + 255) / 256]; else NULL */
+  float* v_scale;
+  int64_t n;        /* 0 <= n < 2^40 */
+  float lr_scale;   /* times lr for this tensor */
+  float weight_decay;
+} attr_adamw_tensor;
+
+/* For every element, with g' = grad_scale g (grad_scale a device scalar, so
+ * that clipping by the gradients' norm needs no host read; NULL: 1):
+ *     m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+ *     x = x - lr' wd x - lr' (m / (1 - beta1^step))
+ *                        / (sqrt(v / (1 - beta2^step) + eps_root) + eps)
+ * with lr' = lr lr_scale, x the weight (its master where there is one).  All
+ * in fp32 without contraction, so the result does not depend on how the work
+ * is split.  8-bit states are encoded after the update: m to the nearest E4M3
+ * value (ties to even), the root of v likewise but never to zero while v is
+ * positive (a second moment rounded to zero would make the next step huge).
+ * E4M3 keeps a root within 6.25%: between steps a stored second moment follows
+ * its block's scale exactly, and its place in the block only by changes of
+ * that size.  A NaN or infinity in a block's new states makes the block's
+ * scale NaN.
+ *   tensors    (host) [n_tensors], 0 <= n_tensors; their buffers must not
+ *              overlap
+ *   p_dtype    ATTR_F32, ATTR_BF16 or ATTR_F16 (the last two with or without
+ *              masters); g_dtype the same three; state_dtype ATTR_F32 or
+ *              ATTR_E4M3
+ *   step       >= 1 (the first step is 1)
+ *   beta1, beta2 in [0, 1);  eps, eps_root >= 0;  lr finite */
+attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors, attr_dtype p_dtype,
+                            attr_dtype g_dtype, attr_dtype state_dtype, int64_t step, double lr,
+                            double beta1, double beta2, double eps, double eps_root,
+                            const float* grad_scale, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Calibration (not part of the method): the rates this GPU sustains, used  */

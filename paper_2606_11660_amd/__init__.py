@@ -30,6 +30,9 @@ __all__ = [
     "attr_precond_apply", "attr_score_topk", "attr_project_workspace_size",
     "attr_precond_accumulate_workspace_size", "attr_precond_apply_workspace_size",
     "attr_score_topk_workspace_size", "Workspace", "attr_probe_read", "attr_probe_mfma",
+    "ATTR_E4M3", "TokenRows", "attr_token_logp", "attr_policy_loss", "attr_preference_loss",
+    "attr_token_logp_workspace_size", "attr_policy_loss_workspace_size",
+    "attr_preference_loss_workspace_size", "AdamTensors", "attr_adamw_step",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -37,7 +40,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 # build of the CPU tests); by default the in-tree libattr.so.
 _LIB_PATH = os.environ.get("ATTR_LIBRARY") or os.path.join(_PKG, "libattr.so")
 
-ATTR_F32, ATTR_BF16, ATTR_F16 = 0, 1, 2
+ATTR_F32, ATTR_BF16, ATTR_F16, ATTR_E4M3 = 0, 1, 2, 3
 PRECOND_NONE, PRECOND_DIAG, PRECOND_FULL = 0, 1, 2
 _STATUS = {0: "ATTR_OK", 1: "ATTR_ERR_INVALID_ARG", 2: "ATTR_ERR_UNSUPPORTED",
            3: "ATTR_ERR_ALIGNMENT", 4: "ATTR_ERR_WORKSPACE", 5: "ATTR_ERR_DEVICE"}
@@ -56,6 +59,20 @@ class _CModule(ctypes.Structure):
                 ("S", ctypes.c_void_p), ("lda", ctypes.c_int64), ("ldg", ctypes.c_int64),
                 ("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64), ("out_col", ctypes.c_int64),
                 ("v_out", ctypes.c_void_p), ("v_in", ctypes.c_void_p)]
+
+
+class _CTokenRows(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("dtype", ctypes.c_int), ("n_rows", ctypes.c_int64),
+                ("V", ctypes.c_int64), ("ldl", ctypes.c_int64), ("logit_scale", ctypes.c_float),
+                ("target", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("n_examples", ctypes.c_int64),
+                ("T", ctypes.c_int64), ("row_offset", ctypes.c_void_p), ("length", ctypes.c_void_p)]
+
+
+class _CAdamTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64), ("lr_scale", ctypes.c_float),
+                ("weight_decay", ctypes.c_float)]
 
 
 _lib = None
@@ -107,6 +124,19 @@ def lib() -> ctypes.CDLL:
     L.attr_score_topk.restype = ctypes.c_int
     L.attr_score_topk.argtypes = [vp, i64, i64, vp, i64, i64, ctypes.c_int, i64, i32, i64, i32, vp,
                                   vp, vp, sz, vp]
+    f32, f64, rows = ctypes.c_float, ctypes.c_double, ctypes.POINTER(_CTokenRows)
+    for name in ("attr_token_logp", "attr_policy_loss", "attr_preference_loss"):
+        query = getattr(L, name + "_workspace_size")
+        query.restype, query.argtypes = sz, [rows]
+    L.attr_token_logp.restype = ctypes.c_int
+    L.attr_token_logp.argtypes = [rows, vp, vp, sz, vp]
+    L.attr_policy_loss.restype = ctypes.c_int
+    L.attr_policy_loss.argtypes = [rows, vp, i32, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, sz, vp]
+    L.attr_preference_loss.restype = ctypes.c_int
+    L.attr_preference_loss.argtypes = [rows, vp, vp, f32, f32, f32, vp, vp, vp, vp, i64, vp, sz, vp]
+    L.attr_adamw_step.restype = ctypes.c_int
+    L.attr_adamw_step.argtypes = [ctypes.POINTER(_CAdamTensor), i32, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                  i64, f64, f64, f64, f64, f64, vp, vp]
     _lib = L
     return L
 
@@ -483,6 +513,211 @@ def attr_score_topk(Q: torch.Tensor, G: torch.Tensor, k: int, top_score: torch.T
                              index_base, 1 if merge else 0, top_score.data_ptr(),
                              top_index.data_ptr(), wsp, wsn, _stream(stream)))
     return top_score, top_index
+
+
+# ----------------------------------------------------------------------------
+# (4) losses over token log-probabilities
+# ----------------------------------------------------------------------------
+class TokenRows:
+    """A batch's rows of logits and the token each row predicts.
+
+    logits: [n_rows, V] (leading dims packed, last dim contiguous; fp32, bf16 or
+    fp16); target: int64 [n_rows]; token t of example i is row i*T + t, or
+    row_offset[i] + t.  length (int32 [n_examples]), weight (fp32 [n_rows], 0
+    masks a token) and targets outside [0, V) say which tokens count;
+    logit_scale is one over the sampling temperature.
+    """
+
+    def __init__(self, logits: torch.Tensor, target: torch.Tensor, n_examples: int, T: int,
+                 row_offset: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None,
+                 weight: Optional[torch.Tensor] = None, logit_scale: float = 1.0):
+        self.logits, self.target, self.weight = logits, target, weight
+        self.n_examples, self.T = int(n_examples), int(T)
+        self.row_offset, self.length, self.logit_scale = row_offset, length, float(logit_scale)
+
+    def c(self) -> _CTokenRows:
+        """The checked descriptor."""
+        n, V, ldl = _rows(self.logits)
+        if self.n_examples < 0 or self.T < 1:
+            raise ValueError("n_examples must be >= 0 and T >= 1")
+        if self.row_offset is None and n < self.n_examples * self.T:
+            raise ValueError(f"logits hold {n} rows, {self.n_examples} examples of {self.T} tokens need "
+                             f"{self.n_examples * self.T}")
+        _vector(self.target, n, torch.int64, "target")
+        _vector(self.weight, n, torch.float32, "weight")
+        _vector(self.row_offset, self.n_examples, torch.int64, "row_offset")
+        _vector(self.length, self.n_examples, torch.int32, "length")
+        _same_gpu(self.logits, self.target, self.weight, self.row_offset, self.length)
+        return _CTokenRows(self.logits.data_ptr(), _dtype(self.logits), n, V, ldl, self.logit_scale,
+                           self.target.data_ptr(), _ptr(self.weight), self.n_examples, self.T,
+                           _ptr(self.row_offset), _ptr(self.length))
+
+
+def attr_token_logp_workspace_size(rows: TokenRows) -> int:
+    return int(lib().attr_token_logp_workspace_size(rows.c()))
+
+
+def attr_policy_loss_workspace_size(rows: TokenRows) -> int:
+    return int(lib().attr_policy_loss_workspace_size(rows.c()))
+
+
+def attr_preference_loss_workspace_size(rows: TokenRows) -> int:
+    return int(lib().attr_preference_loss_workspace_size(rows.c()))
+
+
+def _check_dlogits(dlogits: Optional[torch.Tensor], rows: TokenRows) -> int:
+    """Row stride of the gradient's buffer (0 without one)."""
+    if dlogits is None:
+        return 0
+    n, V, ldd = _rows(dlogits)
+    if dlogits.dtype != rows.logits.dtype or (n, V) != _rows(rows.logits)[:2]:
+        raise ValueError("dlogits must have the logits' shape and type")
+    return ldd
+
+
+def attr_token_logp(rows: TokenRows, logp: torch.Tensor, ws: Optional[Workspace] = None,
+                    stream=None) -> torch.Tensor:
+    """Log-probability of every row's target into logp (fp32 [n_rows]; 0 for tokens that do not count)."""
+    c = rows.c()
+    _vector(logp, c.n_rows, torch.float32, "logp")
+    _same_gpu(rows.logits, logp)
+    L = lib()
+    stream = _call_stream(stream)
+    wsp, wsn = _ws(ws, logp.device, stream).get(L.attr_token_logp_workspace_size(c), stream)
+    _check(L.attr_token_logp(c, logp.data_ptr(), wsp, wsn, _stream(stream)))
+    return logp
+
+
+def attr_policy_loss(rows: TokenRows, advantage: torch.Tensor, loss: torch.Tensor,
+                     logp: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                     logp_old: Optional[torch.Tensor] = None, logp_ref: Optional[torch.Tensor] = None,
+                     per_token: bool = False, clip_low: float = 0.2, clip_high: float = 0.2,
+                     beta: float = 0.0, ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """Clipped policy loss with a KL term per example into loss (fp32 [n_examples]), and its gradient.
+
+    advantage: fp32 [n_examples], or [n_rows] with per_token; logp_old, logp_ref:
+    fp32 [n_rows] (logp_old None: on policy, ratio 1).  dlogits (the logits' shape
+    and type, may be the logits themselves) takes the gradient of loss.sum(); rows'
+    weights carry the mask and the normalisation."""
+    c = rows.c()
+    _vector(advantage, c.n_rows if per_token else c.n_examples, torch.float32, "advantage")
+    _vector(loss, c.n_examples, torch.float32, "loss")
+    for t, name in ((logp, "logp"), (logp_old, "logp_old"), (logp_ref, "logp_ref")):
+        _vector(t, c.n_rows, torch.float32, name)
+    ldd = _check_dlogits(dlogits, rows)
+    _same_gpu(rows.logits, advantage, loss, logp, dlogits, logp_old, logp_ref)
+    L = lib()
+    stream = _call_stream(stream)
+    wsp, wsn = _ws(ws, loss.device, stream).get(L.attr_policy_loss_workspace_size(c), stream)
+    _check(L.attr_policy_loss(c, advantage.data_ptr(), 1 if per_token else 0, _ptr(logp_old), _ptr(logp_ref),
+                              clip_low, clip_high, beta, loss.data_ptr(), _ptr(logp), _ptr(dlogits), ldd,
+                              wsp, wsn, _stream(stream)))
+    return loss
+
+
+def attr_preference_loss(rows: TokenRows, loss: torch.Tensor, log_ratio: Optional[torch.Tensor] = None,
+                         logp: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                         logp_ref: Optional[torch.Tensor] = None, pair_weight: Optional[torch.Tensor] = None,
+                         beta: float = 0.1, margin: float = 0.0, label_smoothing: float = 0.0,
+                         ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """Preference loss of n_examples / 2 pairs into loss (fp32 [n_pairs]), and its gradient.
+
+    Pair p: example p was chosen, example n_pairs + p rejected.  log_ratio: fp32
+    [n_examples], the weighted sums of logp - logp_ref; dlogits takes the gradient
+    of loss.sum(); pair_weight (fp32 [n_pairs]) scales each pair's loss."""
+    c = rows.c()
+    n_pairs = c.n_examples // 2
+    _vector(loss, n_pairs, torch.float32, "loss")
+    _vector(pair_weight, n_pairs, torch.float32, "pair_weight")
+    _vector(log_ratio, c.n_examples, torch.float32, "log_ratio")
+    for t, name in ((logp, "logp"), (logp_ref, "logp_ref")):
+        _vector(t, c.n_rows, torch.float32, name)
+    ldd = _check_dlogits(dlogits, rows)
+    _same_gpu(rows.logits, loss, log_ratio, logp, dlogits, logp_ref, pair_weight)
+    L = lib()
+    stream = _call_stream(stream)
+    wsp, wsn = _ws(ws, loss.device, stream).get(L.attr_preference_loss_workspace_size(c), stream)
+    _check(L.attr_preference_loss(c, _ptr(logp_ref), _ptr(pair_weight), beta, margin, label_smoothing,
+                                  loss.data_ptr(), _ptr(log_ratio), _ptr(logp), _ptr(dlogits), ldd, wsp, wsn,
+                                  _stream(stream)))
+    return loss
+
+
+# ----------------------------------------------------------------------------
+# (5) AdamW
+# ----------------------------------------------------------------------------
+class AdamTensors:
+    """A model's tensors for ``attr_adamw_step``, checked once.
+
+    p, g, m, v: lists of contiguous tensors, one of each per weight, with the same
+    number of elements; p and g fp32, bf16 or fp16, all of one type each; m and v
+    fp32, or torch.float8_e4m3fn with m_scale and v_scale (fp32, one element per
+    256 of the tensor's; v then holds the second moment's root).  master: fp32
+    weights that the step updates, p taking their rounded values.  weight_decay
+    and lr_scale: one number, or one for each tensor.
+
+    The object keeps the tensors and their addresses: give their storage new
+    contents, not a new place (a step with gradients elsewhere needs a new object).
+    """
+
+    def __init__(self, p: Sequence[torch.Tensor], g: Sequence[torch.Tensor], m: Sequence[torch.Tensor],
+                 v: Sequence[torch.Tensor], master: Optional[Sequence[torch.Tensor]] = None,
+                 m_scale: Optional[Sequence[torch.Tensor]] = None,
+                 v_scale: Optional[Sequence[torch.Tensor]] = None, weight_decay=0.0, lr_scale=1.0):
+        n = len(p)
+        if n == 0:
+            raise ValueError("need at least one tensor")
+        eight = m[0].dtype == torch.float8_e4m3fn if len(m) else False
+        if eight != (m_scale is not None) or eight != (v_scale is not None):
+            raise ValueError("m_scale and v_scale go with 8-bit states")
+        state = torch.float8_e4m3fn if eight else torch.float32
+        kinds = {"p": (p, p[0].dtype), "g": (g, g[0].dtype if len(g) else None), "m": (m, state), "v": (v, state),
+                 "master": (master, torch.float32), "m_scale": (m_scale, torch.float32),
+                 "v_scale": (v_scale, torch.float32)}
+        kinds = {k: x for k, x in kinds.items() if x[0] is not None}
+        decay, scale = ([float(x)] * n if isinstance(x, (int, float)) else [float(y) for y in x]
+                        for x in (weight_decay, lr_scale))
+        for name, ts in [(k, x[0]) for k, x in kinds.items()] + [("weight_decay", decay), ("lr_scale", scale)]:
+            if len(ts) != n:
+                raise ValueError(f"{name} has {len(ts)} entries, p has {n}")
+        self.p_dtype, self.g_dtype = _dtype(p[0]), _dtype(g[0])
+        self.state_dtype = ATTR_E4M3 if eight else ATTR_F32
+        self.tensors = {k: list(x[0]) for k, x in kinds.items()}
+        self.device = p[0].device
+        self.array = (_CAdamTensor * n)()
+        spans = []
+        for j in range(n):
+            size = p[j].numel()
+            for name, (ts, dtype) in kinds.items():
+                t = ts[j]
+                want = -(-size // 256) if name.endswith("_scale") else size
+                if t.dtype != dtype or not t.is_contiguous() or t.numel() != want:
+                    raise ValueError(f"tensor {j}: {name} must be a contiguous {dtype} tensor of {want} elements")
+                if not t.is_cuda or t.device != self.device:
+                    raise ValueError("every tensor must live on the same GPU device")
+                if want:
+                    spans.append((t.data_ptr(), t.data_ptr() + want * t.element_size(), name, j))
+            of = {k: x[0][j].data_ptr() for k, x in kinds.items()}
+            self.array[j] = _CAdamTensor(of["p"], of["g"], of["m"], of["v"], of.get("master"), of.get("m_scale"),
+                                         of.get("v_scale"), size, scale[j], decay[j])
+        spans.sort()
+        for a, b in zip(spans, spans[1:]):
+            if b[0] < a[1] and not (a[2] == b[2] == "g"):
+                raise ValueError(f"tensor {a[3]}'s {a[2]} and tensor {b[3]}'s {b[2]} overlap")
+
+
+def attr_adamw_step(tensors: AdamTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, eps_root: float = 0.0, grad_scale: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+    """AdamW step number `step` (from 1) over every tensor: updates p, m, v (and
+    master, scales) in place.  grad_scale: fp32 device scalar that multiplies the gradients."""
+    if grad_scale is not None:
+        _vector(grad_scale, 1, torch.float32, "grad_scale")
+        if grad_scale.device != tensors.device:
+            raise ValueError("every tensor must live on the same GPU device")
+    _check(lib().attr_adamw_step(tensors.array, len(tensors.array), tensors.p_dtype, tensors.g_dtype,
+                                 tensors.state_dtype, step, lr, beta1, beta2, eps, eps_root, _ptr(grad_scale),
+                                 _stream(stream)))
 
 
 # ----------------------------------------------------------------------------

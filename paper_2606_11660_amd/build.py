@@ -23,7 +23,7 @@ ARCH = "gfx950"
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 HIP_SOURCES = ["project.hip", "rowwise.hip", "syrk.hip", "apply_full.hip", "apply_few.hip",
-               "score.hip", "probe.hip"]
+               "score.hip", "token_loss.hip", "adamw.hip", "probe.hip"]
 CXX_SOURCES = ["api.cpp"]
 # the Python binding's native part (torch's and Python's headers, no device code)
 MARSHAL = os.path.join(PKG, "_marshal.so")

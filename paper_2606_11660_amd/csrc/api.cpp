@@ -5,6 +5,7 @@
 #include "attr.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -605,6 +606,330 @@ attr_status attr_score_topk(const void* Q, int64_t n_q, int64_t ldq, const void*
     return ATTR_OK;
   } catch (...) {
     return fail(ATTR_ERR_INVALID_ARG, "attr_score_topk: host exception");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// losses over token log-probabilities
+// ---------------------------------------------------------------------------
+namespace {
+
+static_assert(sizeof(attr_token_rows) == 96 && sizeof(attr_adamw_tensor) == 72, "layouts that the binding mirrors");
+
+bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+attr_status token_validate(const attr_token_rows* r, const char* who) {
+  if (!r) return fail(ATTR_ERR_INVALID_ARG, "%s: rows is NULL", who);
+  if (r->dtype != ATTR_F32 && r->dtype != ATTR_BF16 && r->dtype != ATTR_F16)
+    return fail(ATTR_ERR_UNSUPPORTED, "%s: logits must be ATTR_F32, ATTR_BF16 or ATTR_F16", who);
+  if (r->V < 1 || r->V > (1ll << 28))
+    return fail(ATTR_ERR_INVALID_ARG, "%s: V=%lld must be in [1, 2^28]", who, (long long)r->V);
+  if (r->n_rows < 0 || r->n_examples < 0 || r->T < 1)
+    return fail(ATTR_ERR_INVALID_ARG, "%s: n_rows and n_examples must be >= 0, T >= 1", who);
+  if (r->T >= (1ll << 31) || r->n_examples >= (1ll << 31) || r->n_examples * r->T >= (1ll << 31))
+    return fail(ATTR_ERR_UNSUPPORTED, "%s: n_examples * T must be below 2^31; split the batch", who);
+  if (r->ldl < r->V || r->ldl > (1ll << 40))
+    return fail(ATTR_ERR_INVALID_ARG, "%s: ldl=%lld must be in [V, 2^40]", who, (long long)r->ldl);
+  if (r->n_rows > (1ll << 40) / r->ldl * (1ll << 20))
+    return fail(ATTR_ERR_INVALID_ARG, "%s: n_rows=%lld is too large", who, (long long)r->n_rows);
+  if (!(r->logit_scale > 0.f) || r->logit_scale > 3.0e38f)
+    return fail(ATTR_ERR_INVALID_ARG, "%s: logit_scale must be positive and finite", who);
+  if (!r->row_offset && r->n_rows < r->n_examples * r->T)
+    return fail(ATTR_ERR_INVALID_ARG, "%s: %lld rows, %lld examples of %lld tokens need more", who,
+                (long long)r->n_rows, (long long)r->n_examples, (long long)r->T);
+  if (r->n_examples > 0 && r->n_rows > 0 && (!r->logits || !r->target))
+    return fail(ATTR_ERR_INVALID_ARG, "%s: logits or target is NULL", who);
+  if (!aligned_to(r->logits, (size_t)dtype_bytes(r->dtype)) || !aligned_to(r->target, 8) ||
+      !aligned_to(r->weight, 4) || !aligned_to(r->row_offset, 8) || !aligned_to(r->length, 4))
+    return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+  return ATTR_OK;
+}
+
+// Checks of the gradient's buffer: its stride, and no overlap with the logits
+// but the same rows.
+attr_status dlogits_validate(const attr_token_rows* r, void* dlogits, int64_t ldd, const char* who) {
+  if (!dlogits) return ATTR_OK;
+  const int eb = dtype_bytes(r->dtype);
+  if (ldd < r->V || ldd > (1ll << 40))
+    return fail(ATTR_ERR_INVALID_ARG, "%s: ldd=%lld must be in [V, 2^40]", who, (long long)ldd);
+  if (r->n_rows > (1ll << 40) / ldd * (1ll << 20))
+    return fail(ATTR_ERR_INVALID_ARG, "%s: n_rows=%lld is too large", who, (long long)r->n_rows);
+  if (!aligned_to(dlogits, (size_t)eb))
+    return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+  if (dlogits == r->logits && ldd == r->ldl) return ATTR_OK;
+  if (overlap(span_of(dlogits, r->n_rows, r->V, ldd, eb), span_of(r->logits, r->n_rows, r->V, r->ldl, eb)))
+    return fail(ATTR_ERR_INVALID_ARG, "%s: dlogits overlaps the logits", who);
+  return ATTR_OK;
+}
+
+attr::TokenArgs token_args(const attr_token_rows* r, float* logp, void* dlogits, int64_t ldd) {
+  attr::TokenArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.logits = r->logits;
+  a.target = r->target;
+  a.weight = r->weight;
+  a.row_offset = r->row_offset;
+  a.length = r->length;
+  a.logp = logp;
+  a.dlogits = dlogits;
+  a.n_rows = r->n_rows;
+  a.ldl = r->ldl;
+  a.ldd = ldd;
+  a.n_slots = (uint32_t)(r->n_examples * r->T);
+  a.T = (uint32_t)r->T;
+  a.V = (int32_t)r->V;
+  a.scale = r->logit_scale;
+  return a;
+}
+
+// Workspace of the three calls: what each keeps per token slot and per pair.
+struct TokenLayout {
+  size_t off_stats, off_logp, off_coef, total;
+};
+TokenLayout token_layout(const attr_token_rows* r, int mode) {
+  TokenLayout L{0, 0, 0, 0};
+  const size_t slots = (size_t)(r->n_examples * r->T);
+  if (mode == attr::kTokenPolicy) L.total = align_up(4 * slots);
+  if (mode == attr::kTokenPref) {
+    L.off_logp = align_up(8 * slots);
+    L.off_coef = L.off_logp + align_up(4 * slots);
+    L.total = L.off_coef + align_up(4 * (size_t)(r->n_examples / 2));
+  }
+  return L;
+}
+
+attr_status token_workspace(const TokenLayout& L, void* ws, size_t ws_bytes, const char* who) {
+  if (L.total > 0 && (!ws || ws_bytes < L.total))
+    return fail(ATTR_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", who, L.total,
+                ws ? ws_bytes : (size_t)0);
+  if (reinterpret_cast<uintptr_t>(ws) & 255u)
+    return fail(ATTR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+  return ATTR_OK;
+}
+
+size_t token_query(const attr_token_rows* r, int mode) {
+  if (!r || r->n_examples < 0 || r->T < 1 || r->T >= (1ll << 31) || r->n_examples >= (1ll << 31) ||
+      r->n_examples * r->T >= (1ll << 31))
+    return 0;
+  return token_layout(r, mode).total;
+}
+
+}  // namespace
+
+size_t attr_token_logp_workspace_size(const attr_token_rows* rows) { return token_query(rows, attr::kTokenLogp); }
+size_t attr_policy_loss_workspace_size(const attr_token_rows* rows) { return token_query(rows, attr::kTokenPolicy); }
+size_t attr_preference_loss_workspace_size(const attr_token_rows* rows) { return token_query(rows, attr::kTokenPref); }
+
+attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, size_t ws_bytes,
+                            void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_token_logp";
+    attr_status st = token_validate(rows, who);
+    if (st != ATTR_OK) return st;
+    if (rows->n_examples == 0 || rows->n_rows == 0) return ATTR_OK;
+    if (!logp) return fail(ATTR_ERR_INVALID_ARG, "%s: logp is NULL", who);
+    if (!aligned_to(logp, 4)) return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    const TokenLayout L = token_layout(rows, attr::kTokenLogp);
+    st = token_workspace(L, ws, ws_bytes, who);
+    if (st != ATTR_OK) return st;
+    const attr::TokenArgs a = token_args(rows, logp, nullptr, 0);
+    attr::PolicyArgs p;
+    std::memset(&p, 0, sizeof(p));
+    const hipError_t e = attr::launch_token_rows(attr::kTokenLogp, (int)rows->dtype, a, p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_token_logp launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_token_logp: host exception");
+  }
+}
+
+attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage, int32_t per_token,
+                             const float* logp_old, const float* logp_ref, float clip_low,
+                             float clip_high, float beta, float* loss, float* logp, void* dlogits,
+                             int64_t ldd, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_policy_loss";
+    attr_status st = token_validate(rows, who);
+    if (st == ATTR_OK) st = dlogits_validate(rows, dlogits, ldd, who);
+    if (st != ATTR_OK) return st;
+    if (!(clip_low >= 0.f) || !(clip_high >= 0.f))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: clip_low and clip_high must be >= 0", who);
+    if (!(beta >= 0.f) || beta > 3.0e38f)
+      return fail(ATTR_ERR_INVALID_ARG, "%s: beta must be finite and >= 0", who);
+    if (per_token != 0 && per_token != 1) return fail(ATTR_ERR_INVALID_ARG, "%s: per_token must be 0 or 1", who);
+    if (rows->n_examples == 0) return ATTR_OK;
+    if (!loss || !advantage) return fail(ATTR_ERR_INVALID_ARG, "%s: loss or advantage is NULL", who);
+    if (beta != 0.f && !logp_ref) return fail(ATTR_ERR_INVALID_ARG, "%s: a KL term needs logp_ref", who);
+    if (!aligned_to(advantage, 4) || !aligned_to(logp_old, 4) || !aligned_to(logp_ref, 4) || !aligned_to(loss, 4) ||
+        !aligned_to(logp, 4))
+      return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    const TokenLayout L = token_layout(rows, attr::kTokenPolicy);
+    st = token_workspace(L, ws, ws_bytes, who);
+    if (st != ATTR_OK) return st;
+    const attr::TokenArgs a = token_args(rows, logp, dlogits, ldd);
+    attr::PolicyArgs p;
+    std::memset(&p, 0, sizeof(p));
+    p.advantage = advantage;
+    p.per_token = per_token;
+    p.logp_old = logp_old;
+    p.logp_ref = logp_ref;
+    p.lo = 1.f - clip_low;
+    p.hi = 1.f + clip_high;
+    p.beta = beta;
+    p.token_loss = static_cast<float*>(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = attr::launch_token_rows(attr::kTokenPolicy, (int)rows->dtype, a, p, s);
+    if (e != hipSuccess) return device_fail(e, "attr_policy_loss launch");
+    e = attr::launch_example_sum(p.token_loss, a.T, (uint32_t)rows->n_examples, loss, s);
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_policy_loss sum launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_policy_loss: host exception");
+  }
+}
+
+attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_ref,
+                                 const float* pair_weight, float beta, float margin,
+                                 float label_smoothing, float* loss, float* log_ratio, float* logp,
+                                 void* dlogits, int64_t ldd, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_preference_loss";
+    attr_status st = token_validate(rows, who);
+    if (st == ATTR_OK) st = dlogits_validate(rows, dlogits, ldd, who);
+    if (st != ATTR_OK) return st;
+    if (rows->n_examples % 2)
+      return fail(ATTR_ERR_INVALID_ARG, "%s: n_examples=%lld must be even (chosen, then rejected)", who,
+                  (long long)rows->n_examples);
+    if (!(beta >= -3.0e38f && beta <= 3.0e38f) || !(margin >= -3.0e38f && margin <= 3.0e38f))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: beta and margin must be finite", who);
+    if (!(label_smoothing >= 0.f && label_smoothing <= 1.f))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: label_smoothing must be in [0, 1]", who);
+    if (rows->n_examples == 0) return ATTR_OK;
+    if (!loss) return fail(ATTR_ERR_INVALID_ARG, "%s: loss is NULL", who);
+    if (!aligned_to(logp_ref, 4) || !aligned_to(pair_weight, 4) || !aligned_to(loss, 4) ||
+        !aligned_to(log_ratio, 4) || !aligned_to(logp, 4))
+      return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    const TokenLayout L = token_layout(rows, attr::kTokenPref);
+    st = token_workspace(L, ws, ws_bytes, who);
+    if (st != ATTR_OK) return st;
+    char* base = static_cast<char*>(ws);
+    attr::TokenArgs a = token_args(rows, logp, dlogits, ldd);
+    a.stats = reinterpret_cast<float2*>(base + L.off_stats);
+    a.slot_logp = reinterpret_cast<float*>(base + L.off_logp);
+    attr::PolicyArgs none;
+    std::memset(&none, 0, sizeof(none));
+    attr::PrefArgs p;
+    std::memset(&p, 0, sizeof(p));
+    p.logp_ref = logp_ref;
+    p.pair_weight = pair_weight;
+    p.loss = loss;
+    p.log_ratio = log_ratio;
+    p.coef = reinterpret_cast<float*>(base + L.off_coef);
+    p.n_pairs = (uint32_t)(rows->n_examples / 2);
+    p.beta = beta;
+    p.margin = margin;
+    p.smoothing = label_smoothing;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = attr::launch_token_rows(attr::kTokenPref, (int)rows->dtype, a, none, s);
+    if (e != hipSuccess) return device_fail(e, "attr_preference_loss launch");
+    e = attr::launch_pairs(a, p, s);
+    if (e != hipSuccess) return device_fail(e, "attr_preference_loss pair launch");
+    if (!dlogits) return ATTR_OK;
+    e = attr::launch_pref_grad((int)rows->dtype, a, p, s);
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_preference_loss gradient launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_preference_loss: host exception");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// AdamW
+// ---------------------------------------------------------------------------
+attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors, attr_dtype p_dtype,
+                            attr_dtype g_dtype, attr_dtype state_dtype, int64_t step, double lr,
+                            double beta1, double beta2, double eps, double eps_root,
+                            const float* grad_scale, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_adamw_step";
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: n_tensors is negative or tensors NULL", who);
+    if (!valid_dtype(p_dtype) || !valid_dtype(g_dtype))
+      return fail(ATTR_ERR_UNSUPPORTED, "%s: weights and gradients must be ATTR_F32, ATTR_BF16 or ATTR_F16", who);
+    if (state_dtype != ATTR_F32 && state_dtype != ATTR_E4M3)
+      return fail(ATTR_ERR_UNSUPPORTED, "%s: states must be ATTR_F32 or ATTR_E4M3", who);
+    if (step < 1) return fail(ATTR_ERR_INVALID_ARG, "%s: step=%lld must be >= 1", who, (long long)step);
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: beta1 and beta2 must be in [0, 1)", who);
+    if (!(eps >= 0.0 && eps <= 3.0e38) || !(eps_root >= 0.0 && eps_root <= 3.0e38) || !(std::fabs(lr) <= 3.0e38))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: lr, eps and eps_root must be finite, eps and eps_root >= 0", who);
+    if (!aligned_to(grad_scale, 4)) return fail(ATTR_ERR_ALIGNMENT, "%s: grad_scale must be 4-byte aligned", who);
+    const bool eight = state_dtype == ATTR_E4M3;
+    const size_t pb = (size_t)dtype_bytes(p_dtype), gb = (size_t)dtype_bytes(g_dtype), sb = eight ? 1 : 4;
+    for (int32_t j = 0; j < n_tensors; ++j) {
+      const attr_adamw_tensor& t = tensors[j];
+      if (t.n < 0 || t.n >= (1ll << 40)) return fail(ATTR_ERR_INVALID_ARG, "%s: tensor %d: n=%lld", who, j, (long long)t.n);
+      if (!(std::fabs(t.lr_scale) <= 3.0e38f) || !(std::fabs(t.weight_decay) <= 3.0e38f))
+        return fail(ATTR_ERR_INVALID_ARG, "%s: tensor %d: lr_scale and weight_decay must be finite", who, j);
+      if (t.n == 0) continue;
+      if (!t.p || !t.g || !t.m || !t.v) return fail(ATTR_ERR_INVALID_ARG, "%s: tensor %d: NULL pointer", who, j);
+      if (eight != (t.m_scale != nullptr) || eight != (t.v_scale != nullptr))
+        return fail(ATTR_ERR_INVALID_ARG, "%s: tensor %d: m_scale and v_scale go with 8-bit states", who, j);
+      if (!aligned_to(t.p, pb) || !aligned_to(t.g, gb) || !aligned_to(t.m, sb) || !aligned_to(t.v, sb) ||
+          !aligned_to(t.master, 4) || !aligned_to(t.m_scale, 4) || !aligned_to(t.v_scale, 4))
+        return fail(ATTR_ERR_ALIGNMENT, "%s: tensor %d: pointers must be aligned to their elements", who, j);
+    }
+    attr::AdamwArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.grad_scale = grad_scale;
+    a.beta1 = (float)beta1;
+    a.one_beta1 = (float)(1.0 - beta1);
+    a.beta2 = (float)beta2;
+    a.one_beta2 = (float)(1.0 - beta2);
+    a.corr1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)step)));
+    a.corr2 = (float)(1.0 / (1.0 - std::pow(beta2, (double)step)));
+    a.eps = (float)eps;
+    a.eps_root = (float)eps_root;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint32_t blocks = 0;
+    auto flush = [&]() -> hipError_t {
+      if (a.n == 0) return hipSuccess;
+      const hipError_t e = attr::launch_adamw((int)p_dtype, (int)g_dtype, eight, blocks, a, s);
+      a.n = 0;
+      blocks = 0;
+      return e;
+    };
+    constexpr uint32_t kMostBlocks = 1u << 22;
+    for (int32_t j = 0; j < n_tensors; ++j) {
+      const attr_adamw_tensor& t = tensors[j];
+      // a tensor of more workgroups than a launch takes comes in pieces of whole blocks
+      for (int64_t at = 0; at < t.n; at += (int64_t)kMostBlocks * attr::kAdamwChunk) {
+        const int64_t n = std::min(t.n - at, (int64_t)kMostBlocks * attr::kAdamwChunk);
+        const uint32_t need = (uint32_t)((n + attr::kAdamwChunk - 1) / attr::kAdamwChunk);
+        if (a.n == attr::kAdamwMax || blocks + need > kMostBlocks) {
+          const hipError_t e = flush();
+          if (e != hipSuccess) return device_fail(e, "attr_adamw_step launch");
+        }
+        attr::AdamwEntry& x = a.e[a.n++];
+        x.p = static_cast<char*>(t.p) + (size_t)at * pb;
+        x.g = static_cast<const char*>(t.g) + (size_t)at * gb;
+        x.m = static_cast<char*>(t.m) + (size_t)at * sb;
+        x.v = static_cast<char*>(t.v) + (size_t)at * sb;
+        x.master = t.master ? t.master + at : nullptr;
+        x.m_scale = t.m_scale ? t.m_scale + at / 256 : nullptr;
+        x.v_scale = t.v_scale ? t.v_scale + at / 256 : nullptr;
+        x.n = n;
+        x.lr = (float)(lr * (double)t.lr_scale);
+        x.lr_wd = (float)(lr * (double)t.lr_scale * (double)t.weight_decay);
+        x.chunk0 = blocks;
+        blocks += need;
+      }
+    }
+    const hipError_t e = flush();
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_adamw_step launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_adamw_step: host exception");
   }
 }
 

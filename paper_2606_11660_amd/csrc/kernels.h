@@ -3,6 +3,7 @@
 #pragma once
 
 #include <hip/hip_runtime_api.h>
+#include <hip/hip_vector_types.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -187,6 +188,76 @@ ApplyFewPlan plan_apply_few(int64_t n_rows, int64_t D);
 hipError_t launch_apply_few(const ApplyFewPlan& P, const void* X, int64_t n_rows, int64_t ldx,
                             int64_t D, const float* M, int y_dtype, void* Y, int64_t ldy, int unit,
                             void* ws, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// losses over token log-probabilities
+// ---------------------------------------------------------------------------
+constexpr int kTokenLogp = 0, kTokenPolicy = 1, kTokenPref = 2;
+struct TokenArgs {
+  const void* logits;
+  const int64_t* target;
+  const float* weight;         // or null
+  const int64_t* row_offset;   // or null
+  const int32_t* length;       // or null
+  float* logp;                 // or null
+  void* dlogits;               // or null
+  float2* stats;               // per slot: row maximum and sum (preference loss)
+  float* slot_logp;            // per slot (preference loss)
+  int64_t n_rows, ldl, ldd;
+  uint32_t n_slots, T;         // slot = example * T + token
+  int32_t V;
+  float scale;
+};
+struct PolicyArgs {
+  const float* advantage;
+  const float* logp_old;       // or null
+  const float* logp_ref;       // null only with beta 0
+  float* token_loss;           // per slot
+  float lo, hi, beta;          // ratio bounds
+  int32_t per_token;
+};
+struct PrefArgs {
+  const float* logp_ref;       // or null
+  const float* pair_weight;    // or null
+  float* loss;
+  float* log_ratio;            // or null
+  float* coef;                 // per pair: dloss/dlogp of a chosen token of weight 1
+  uint32_t n_pairs;
+  float beta, margin, smoothing;
+};
+hipError_t launch_token_rows(int mode, int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s);
+hipError_t launch_example_sum(const float* token_loss, uint32_t T, uint32_t n, float* loss, hipStream_t s);
+hipError_t launch_pairs(const TokenArgs& a, const PrefArgs& p, hipStream_t s);
+hipError_t launch_pref_grad(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// AdamW
+// ---------------------------------------------------------------------------
+// One tensor of a launch; descriptors travel in kernel arguments (4096 bytes).
+struct AdamwEntry {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* master;
+  float* m_scale;
+  float* v_scale;
+  int64_t n;
+  float lr, lr_wd;
+  uint32_t chunk0;  // first workgroup
+  uint32_t pad;
+};
+constexpr int kAdamwMax = 48;
+constexpr int64_t kAdamwChunk = 4096;  // elements of a workgroup, a multiple of the 8-bit states' 256
+struct AdamwArgs {
+  AdamwEntry e[kAdamwMax];
+  const float* grad_scale;  // or null
+  float beta1, one_beta1, beta2, one_beta2, corr1, corr2, eps, eps_root;
+  int32_t n;
+};
+static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
+hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, uint32_t blocks, const AdamwArgs& a,
+                        hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // calibration

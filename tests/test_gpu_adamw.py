@@ -1,0 +1,219 @@
+"""AdamW over many tensors against the 64-bit oracle.
+
+Tolerances, u = 2^-24: a state is a sum of two rounded products (4 u of their
+magnitudes), the weight three rounded terms (its update's relative error below 16 u).
+8-bit states: the same error of a state before its encoding (6 u of its products'
+magnitudes: two more roundings decode the old state), so a scale has that error of its
+block's largest, and codes equal the oracle's encoding of the step's 64-bit states except
+where that error (and 16 u for the encoding's own arithmetic) reaches a rounding boundary;
+there the neighbour is allowed too.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_11660_amd as P
+from oracle import training as O
+from tests._util import host, say
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+ROUND = {torch.float32: 0.0, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}  # 8 and 11 significant bits
+SIZES = [1, 255, 256, 257, 3, 4096, 4097, 0, 12289, 7, 64 * 64, 100003]
+HYPER = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-8, eps_root=1e-6)
+
+
+class Model:
+    def __init__(self, seed, sizes, p=torch.float32, g=torch.float32, eight=False, master=False, shift=0):
+        r = np.random.default_rng(seed)
+        self.sizes, self.eight = sizes, eight
+
+        def put(x, dtype):
+            """On the device, `shift` elements into its buffer."""
+            buf = torch.zeros(len(x) + shift, dtype=torch.float32 if dtype == torch.float8_e4m3fn else dtype, device="cuda")
+            buf[shift:] = torch.from_numpy(np.asarray(x, np.float32)).to(buf.dtype).cuda()
+            return buf.to(dtype)[shift:]
+        self.x = [r.standard_normal(n) * 0.1 for n in sizes]
+        self.decay = [0.1 if j % 2 else 0.0 for j in range(len(sizes))]
+        self.lr_scale = [1.0 if j % 3 else 0.5 for j in range(len(sizes))]
+        loud = [np.exp(r.standard_normal(-(-n // 32))).repeat(32)[:n] for n in sizes]
+        self.gd = [put(r.standard_normal(n) * 0.02 * s, g) for n, s in zip(sizes, loud)]
+        m = [r.standard_normal(n) * 0.01 * s for n, s in zip(sizes, loud)]
+        v = [(r.standard_normal(n) ** 2 + 0.05) * 1e-4 * s * s for n, s in zip(sizes, loud)]
+        self.master = [put(x, torch.float32) for x in self.x] if master else None
+        self.p = [put(x, p) for x in self.x]
+        self.ms = self.vs = None
+        if eight:
+            qm, qv = [O.blocks(x) for x in m], [O.blocks(np.sqrt(x), root=True) for x in v]
+            self.m, self.v = ([put(q, torch.float8_e4m3fn) for q, _ in qs] for qs in (qm, qv))
+            self.ms, self.vs = ([put(s, torch.float32) for _, s in qs] for qs in (qm, qv))
+        else:
+            self.m, self.v = ([put(x, torch.float32) for x in xs] for xs in (m, v))
+
+    def tensors(self):
+        return P.AdamTensors(self.p, self.gd, self.m, self.v, master=self.master, m_scale=self.ms, v_scale=self.vs,
+                             weight_decay=self.decay, lr_scale=self.lr_scale)
+
+    def states(self, j):
+        m, v = (host(t.float()).astype(np.float64) for t in (self.m[j], self.v[j]))
+        if self.eight:
+            m *= host(self.ms[j]).astype(np.float64).repeat(256)[:len(m)]
+            v = (v * host(self.vs[j]).astype(np.float64).repeat(256)[:len(v)]) ** 2
+        return m, v
+
+
+def check_codes(got, scale, want, mag, root):
+    """8-bit values and scales of the 64-bit states `want`, whose products had the magnitudes `mag`."""
+    q, s = O.blocks(want, root)
+    per = s.repeat(256)[:len(want)]
+    err = 6 * U * mag
+    most = np.array([err[b:b + 256].max() for b in range(0, len(want), 256)]) / 448
+    assert (np.abs(scale - s) <= most + 16 * U * s).all()
+    rel = (most / s).repeat(256)[:len(want)] + 16 * U  # of the scale
+    lo, hi = want / per * (1 - np.sign(want) * rel) - err / per, want / per * (1 + np.sign(want) * rel) + err / per
+    lo, hi = (O.e4m3(np.clip(x, -448, 448)) for x in (lo, hi))
+    if root:
+        lo, hi = (np.where(want > 0, np.maximum(x, 2.0 ** -9), x) for x in (lo, hi))
+    ok = (got >= lo) & (got <= hi)
+    assert ok.all(), (got[~ok][:5], q[~ok][:5])
+    assert len(q) < 2000 or (got == q).mean() > 0.999
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["f32", "e4m3"])
+@pytest.mark.parametrize("p,g,master", [(torch.float32, torch.float32, False), (torch.float32, torch.bfloat16, False),
+                                        (torch.bfloat16, torch.bfloat16, True), (torch.bfloat16, torch.float16, False),
+                                        (torch.float16, torch.float16, True), (torch.float16, torch.float32, True)])
+def test_step(p, g, master, eight):
+    for shift in (0, 1, 5):
+        say(f"case: adamw p={p} g={g} master={master} eight={eight} shift={shift}")
+        M = Model(3 + shift, SIZES, p, g, eight, master, shift)
+        gs = torch.full((1,), 0.37, device="cuda") if shift != 1 else None
+        plan = M.tensors()
+        for step in (1, 2, 50):
+            before = [(host((M.master or M.p)[j].float()).astype(np.float64), host(M.gd[j].float()), *M.states(j))
+                      for j in range(len(SIZES))]
+            P.attr_adamw_step(plan, step, grad_scale=gs, **HYPER)
+            for j, n in enumerate(SIZES):
+                x, grad, m, v = before[j]
+                lr = HYPER["lr"] * M.lr_scale[j]
+                f = float(gs) if gs is not None else 1.0
+                nx, nm, nv = O.adamw(x, grad, m, v, step, **{**HYPER, "lr": lr}, weight_decay=M.decay[j], grad_scale=f)
+                got = host((M.master or M.p)[j].float()).astype(np.float64)
+                upd = np.abs(nx - x) + lr * 0.1 * np.abs(x)
+                # the update's error: that of m (cancelling terms included) over the root
+                mag = HYPER["beta1"] * np.abs(m) + (1 - HYPER["beta1"]) * np.abs(grad * f)
+                root = np.sqrt(nv / (1 - HYPER["beta2"] ** step) + HYPER["eps_root"]) + HYPER["eps"]
+                tol = 4 * U * np.abs(x) + 16 * U * (upd + lr * mag / (1 - HYPER["beta1"] ** step) / root)
+                if not M.master:
+                    tol = tol + ROUND[p] * (np.abs(nx) + tol) + (2.0 ** -25 if p == torch.float16 else 0.0)
+                assert (np.abs(got - nx) <= tol).all(), (j, n, step, np.abs(got - nx).max())
+                if M.master:
+                    assert torch.equal(M.p[j], M.master[j].to(p))
+                if eight:
+                    if n:
+                        check_codes(host(M.m[j].float()), host(M.ms[j]), nm, mag, False)
+                        check_codes(host(M.v[j].float()), host(M.vs[j]), np.sqrt(nv), np.sqrt(nv), True)
+                else:
+                    gm, gv = M.states(j)
+                    assert (np.abs(gm - nm) <= 4 * U * mag).all() and (np.abs(gv - nv) <= 6 * U * nv + 2.0 ** -140).all()
+
+
+def test_elements_do_not_depend_on_the_split():
+    """One tensor of n elements and the same elements in tensors of whole blocks give the same bits."""
+    for eight in (False, True):
+        n, cut = 256 * 77 + 13, 256 * 30
+        A, B = Model(9, [n], eight=eight), Model(9, [n], eight=eight)
+        P.attr_adamw_step(A.tensors(), 3, **HYPER)
+        k = cut // 256
+        two = lambda t: [t[:cut], t[cut:]]  # noqa: E731
+        sc = (lambda t: [t[:k], t[k:]]) if eight else (lambda t: None)
+        plan = P.AdamTensors(two(B.p[0]), two(B.gd[0]), two(B.m[0]), two(B.v[0]), m_scale=sc(B.ms[0] if eight else None),
+                             v_scale=sc(B.vs[0] if eight else None), weight_decay=0.0, lr_scale=0.5)
+        P.attr_adamw_step(plan, 3, **HYPER)
+        assert torch.equal(A.p[0], B.p[0]) and torch.equal(A.m[0].view(torch.uint8), B.m[0].view(torch.uint8))
+        assert torch.equal(A.v[0].view(torch.uint8), B.v[0].view(torch.uint8))
+
+
+def test_many_tensors():
+    """More tensors than one launch takes, empty ones among them."""
+    sizes = [(37 * j) % 701 for j in range(217)]
+    M = Model(21, sizes)
+    before = [host(p).copy() for p in M.p]
+    st = [M.states(j) for j in range(len(sizes))]
+    P.attr_adamw_step(M.tensors(), 4, **HYPER)
+    for j in range(len(sizes)):
+        nx, nm, nv = O.adamw(before[j], host(M.gd[j]), *st[j], 4, **{**HYPER, "lr": HYPER["lr"] * M.lr_scale[j]}, weight_decay=M.decay[j])
+        assert np.abs(host(M.p[j]) - nx).max(initial=0) <= 1e-6
+        assert np.abs(host(M.m[j]) - nm).max(initial=0) <= 1e-7
+
+
+def test_eight_bit_edges():
+    """Zero gradients and states, a second moment that underflows its block, infinities and NaN, a step of size zero."""
+    n = 256 * 6
+    p, g = torch.ones(n, device="cuda"), torch.zeros(n, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.float8_e4m3fn, device="cuda") for _ in range(2))
+    ms, vs = torch.zeros(6, device="cuda"), torch.zeros(6, device="cuda")
+    g[256:512] = 1e-30                       # its square is zero in fp32
+    g[512], g[513:768] = 1e6, 1e-9           # a root that would round to zero
+    g[768 + 5] = float("inf")
+    g[1024 + 7] = float("nan")
+    g[1280:] = 1.0
+    plan = P.AdamTensors([p], [g], [m], [v], m_scale=[ms], v_scale=[vs])
+    P.attr_adamw_step(plan, 1, 1e-3, 0.9, 0.95, 1e-8)
+    q, r, sm, sv = host(m.float()), host(v.float()), host(ms), host(vs)
+    x = host(p)
+    assert (x[:256] == 1).all() and (q[:256] == 0).all() and (r[:256] == 0).all()
+    assert np.isfinite(x[256:512]).all() and (q[256:512] > 0).all() and (r[256:512] == 0).all()
+    assert r[512] == 448 and (r[513:768] == 2.0 ** -9).all() and q[512] == 448
+    assert np.isnan(sm[3]) and np.isnan(sv[3]) and np.isnan(sm[4]) and np.isnan(sv[4])
+    assert np.isfinite(sm[[0, 1, 2, 5]]).all() and np.isfinite(sv[[0, 1, 2, 5]]).all()
+    bad = np.isnan(x)
+    assert bad[[773, 1031]].all() and bad.sum() == 2   # inf / inf, NaN; every other weight is finite
+    assert (q[1280:] == 448).all() and (r[1280:] == 448).all()
+    assert np.abs(x[1280:] - (1 - 1e-3)).max() <= 1e-7
+    q2 = P.AdamTensors([p[:256]], [g[:256]], [m[:256]], [v[:256]], m_scale=[ms[:1]], v_scale=[vs[:1]], weight_decay=0.5)
+    P.attr_adamw_step(q2, 2, 0.0)
+    assert (host(p[:256]) == 1).all()
+
+
+def test_eight_bit_states_train():
+    """A least-squares fit with 8-bit states ends near where 32-bit states end."""
+    torch.manual_seed(0)
+    A, want = torch.randn(512, 300, device="cuda"), torch.randn(300, device="cuda")
+    b = A @ want
+    ends = []
+    for eight in (False, True):
+        x, g = torch.zeros(300, device="cuda"), torch.zeros(300, device="cuda")
+        kind = torch.float8_e4m3fn if eight else torch.float32
+        m, v = (torch.zeros(300, dtype=kind, device="cuda") for _ in range(2))
+        sc = dict(m_scale=[torch.zeros(2, device="cuda")], v_scale=[torch.zeros(2, device="cuda")]) if eight else {}
+        plan = P.AdamTensors([x], [g], [m], [v], **sc)
+        for step in range(1, 401):
+            g.copy_(A.t() @ (A @ x - b) / 512)
+            P.attr_adamw_step(plan, step, 0.05 * (1 - step / 401), 0.9, 0.95, 1e-8)
+        ends.append(float((x - want).norm() / want.norm()))
+    say("fit errors", ends)
+    assert ends[0] < 1e-2 and ends[1] < 2e-2
+
+
+def test_plan_refusals():
+    t = lambda n, d=torch.float32: torch.zeros(n, dtype=d, device="cuda")  # noqa: E731
+    p, g, m, v = t(300), t(300), t(300), t(300)
+    with pytest.raises(ValueError, match="300 elements"):
+        P.AdamTensors([p], [t(299)], [m], [v])
+    with pytest.raises(ValueError, match="float32"):
+        P.AdamTensors([p], [g], [m], [t(300, torch.bfloat16)])
+    with pytest.raises(ValueError, match="go with 8-bit"):
+        P.AdamTensors([p], [g], [t(300, torch.float8_e4m3fn)], [t(300, torch.float8_e4m3fn)])
+    with pytest.raises(ValueError, match="overlap"):
+        P.AdamTensors([p], [g], [m], [m])
+    with pytest.raises(ValueError, match="entries"):
+        P.AdamTensors([p], [g], [m], [v], weight_decay=[0.1, 0.2])
+    with pytest.raises(ValueError, match="contiguous"):
+        P.AdamTensors([t(600)[::2]], [g], [m], [v])
+    plan = P.AdamTensors([p], [g], [m], [v])
+    for kw, text in ((dict(step=0, lr=1.0), "step"), (dict(step=1, lr=float("nan")), "finite"),
+                     (dict(step=1, lr=1.0, beta1=1.0), "beta1"), (dict(step=1, lr=1.0, eps=-1.0), "eps")):
+        with pytest.raises(P.AttrError, match=text):
+            P.attr_adamw_step(plan, **kw)
+    assert (p == 0).all()

@@ -1,0 +1,422 @@
+"""Token log-probabilities, the policy loss and the preference loss against the 64-bit oracle.
+
+Tolerances are derived, with u = 2^-24: a row's sum of exponentials is a chain of at most
+V / 64 fp32 additions per thread and a tree (relative error u (V / 64 + 128), the second
+term covering the exponentials' own error, whose arguments are weighted by the
+probabilities); a log-probability adds a few roundings of its two terms; a gradient
+s c (1[j = y] - p_j) has the relative error of c (that of exp(logp - old)) and of p_j, and
+one rounding to the logits' type.  The losses are sums of fp64-summed terms.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_11660_amd as P
+from oracle import training as O
+from tests._util import host, say
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+LEAST = {torch.float32: 2.0 ** -126, torch.bfloat16: 2.0 ** -126, torch.float16: 2.0 ** -24}
+NAMES = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float16: "f16"}
+
+
+def rel_sum(V):
+    return U * (V / 64 + 128)
+
+
+def logp_tol(lp, V):
+    return 4 * U * abs(lp) + rel_sum(V)
+
+
+class Batch:
+    """Seeded logits with a layout that the parameters choose, on the device and in 64 bits."""
+
+    def __init__(self, seed, dtype, V, n, T, packed=False, ragged=False, weighted=False, extra_ld=0, shift=0,
+                 scale=1.0, spread=3.0):
+        r = np.random.default_rng(seed)
+        self.dtype, self.V, self.n, self.T, self.scale = dtype, V, n, T, scale
+        lens = r.integers(0, T + 1, n) if ragged else np.full(n, T)
+        if ragged and n > 1:
+            lens[0], lens[-1] = T, 0
+        self.length = lens.astype(np.int32) if ragged else None
+        self.row_offset = None
+        self.rows = n * T
+        if packed:  # a row of nobody's in front of every example
+            self.row_offset = np.concatenate([[0], np.cumsum(lens)[:-1]]).astype(np.int64) + np.arange(1, n + 1)
+            self.rows = int(lens.sum()) + n + 1
+        self.ld = V + extra_ld
+        z = torch.from_numpy(r.standard_normal((self.rows, V)).astype(np.float32) * spread)
+        self.target = r.integers(0, V, self.rows)
+        z[torch.arange(self.rows), torch.from_numpy(self.target)] += 4.0
+        z = z.to(dtype)
+        self.weight = None
+        if weighted:
+            self.weight = r.uniform(0.1, 1.5, self.rows).astype(np.float32)
+            self.weight[r.random(self.rows) < 0.25] = 0.0
+            self.target = np.where((self.weight == 0) & (r.random(self.rows) < 0.5), -100, self.target)
+            self.target[r.random(self.rows) < 0.1] = -100
+        self.z = z
+        self.buf = torch.full((self.rows * self.ld + shift,), float("nan"), dtype=dtype, device="cuda")
+        self.logits = self.buf[shift:].view(self.rows, self.ld)[:, :V]
+        self.sync()
+        self.r = r
+
+    def sync(self):
+        self.logits.copy_(self.z)
+
+    def numpy(self):
+        return self.z.double().numpy()
+
+    def where(self):
+        return {"weight": self.weight, "row_offset": self.row_offset, "length": self.length}
+
+    def slots(self):
+        return O.slots(self.n, self.T, self.rows, self.V, self.target, **self.where())
+
+    def tokens(self):
+        def up(x):
+            return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+        return P.TokenRows(self.logits, up(self.target.astype(np.int64)), self.n, self.T, row_offset=up(self.row_offset),
+                           length=up(self.length), weight=up(self.weight), logit_scale=self.scale)
+
+    def dbuf(self, fill=7.0):
+        b = torch.full_like(self.buf, fill)
+        return b[len(b) - self.rows * self.ld:].view(self.rows, self.ld)[:, :self.V], b
+
+    def old_ref(self, ratio_clear=()):
+        """Earlier and reference log-probabilities near the present ones; ratios keep clear of the bounds."""
+        lp = O.token_logp(self.numpy(), self.target, self.n, self.T, self.scale, **self.where())
+        old, ref = np.zeros(self.rows, np.float32), np.zeros(self.rows, np.float32)
+        for row, v in lp.items():
+            d = self.r.normal() * 0.3
+            while any(abs(math.exp(d) - b) < 5e-3 for b in ratio_clear):
+                d = self.r.normal() * 0.3
+            if np.isfinite(v):
+                old[row], ref[row] = v - d, v + self.r.normal() * 0.5
+        return old, ref
+
+
+def check_logp(b, got, untouched):
+    want = O.token_logp(b.numpy(), b.target, b.n, b.T, b.scale, **b.where())
+    for row in range(b.rows):
+        if row not in want:
+            assert got[row] == untouched, (row, got[row])
+        elif np.isnan(want[row]):
+            assert np.isnan(got[row]), (row, got[row])
+        elif np.isinf(want[row]):
+            assert got[row] == want[row], (row, got[row])
+        else:
+            assert abs(got[row] - want[row]) <= logp_tol(want[row], b.V), (row, got[row], want[row])
+
+
+def check_dlogits(b, got, grad, logp, c_rel, c_abs, untouched=7.0):
+    """Every element within the row's derivative's error, the probability's and one rounding."""
+    counts = {row: c for _, _, row, c in b.slots()}
+    for row in range(b.rows):
+        if row not in grad:
+            assert (got[row] == untouched).all(), row
+            continue
+        if not counts[row]:
+            assert (got[row] == 0).all(), row
+            continue
+        y, want = b.target[row], grad[row]
+        lps = O.log_softmax(b.numpy()[row], b.scale)
+        p = np.exp(lps)
+        one = np.zeros(b.V)
+        one[y] = 1
+        cs = abs(want[y]) / max(1 - p[y], 1e-300) if p[y] < 1 else 0.0
+        x = np.where(p > 0, np.maximum(lps.max() - lps, 0), 0)
+        rel_p = rel_sum(b.V) + U * (8 + 4 * x)
+        tol = (cs * c_rel + c_abs[row]) * (p + one) + cs * (p * rel_p + one * 2 * U)
+        tol = tol + ROUND[b.dtype] * (np.abs(want) + tol) + LEAST[b.dtype]
+        bad = np.abs(got[row] - want) > tol
+        assert not bad.any(), (row, int(bad.argmax()), got[row][bad][:4], want[bad][:4], tol[bad][:4])
+
+
+SHAPES = [  # V, n, T: one entry, fewer than a wave, odd, a vector's length and one off it, several waves, large
+    (1, 2, 3), (2, 1, 1), (37, 3, 5), (64, 2, 2), (255, 2, 3), (1000, 4, 7), (1023, 1, 5), (2048, 2, 3), (4099, 3, 2),
+    (8192, 2, 2), (8193, 1, 3), (16384, 1, 2), (32003, 2, 3), (50257, 2, 2), (65536, 1, 2), (131072, 1, 2), (131079, 1, 1)]
+LAYOUTS = [dict(), dict(ragged=True), dict(packed=True, ragged=True, weighted=True, extra_ld=5, shift=3),
+           dict(weighted=True, ragged=True, extra_ld=8, scale=1.25)]
+
+
+@pytest.mark.parametrize("layout", range(len(LAYOUTS)))
+@pytest.mark.parametrize("dtype", list(NAMES), ids=NAMES.get)
+def test_token_logp(dtype, layout):
+    for V, n, T in SHAPES:
+        say(f"case: logp {NAMES[dtype]} V={V} n={n} T={T} layout={layout}")
+        b = Batch(V + n, dtype, V, n, T, **LAYOUTS[layout])
+        logp = torch.full((b.rows,), 7.0, device="cuda")
+        P.attr_token_logp(b.tokens(), logp)
+        check_logp(b, host(logp), 7.0)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 5, 63, 64, 200, 300, 1100])
+def test_token_logp_by_row_count(rows):
+    """The number of rows decides how a row is spread over workgroups; its value does not."""
+    for dtype, V in ((torch.bfloat16, 9001), (torch.float32, 20000)):
+        say(f"case: logp rows={rows} {NAMES[dtype]} V={V}")
+        b = Batch(rows, dtype, V, rows, 1, weighted=rows > 3)
+        logp = torch.full((b.rows,), 7.0, device="cuda")
+        P.attr_token_logp(b.tokens(), logp)
+        check_logp(b, host(logp), 7.0)
+
+
+def policy_tols(b, old, adv, ref, beta, per_token):
+    """Absolute error of c (weights included) and of the example losses."""
+    lp = O.token_logp(b.numpy(), b.target, b.n, b.T, b.scale, **b.where())
+    c_abs, loss_tol = np.zeros(b.rows), np.zeros(b.n)
+    for i, _, row, counts in b.slots():
+        if not counts:
+            continue
+        w = 1.0 if b.weight is None else float(b.weight[row])
+        a = abs(float(adv[row if per_token else i]))
+        ratio = math.exp(lp[row] - old[row]) if old is not None else 1.0
+        d = ref[row] - lp[row] if beta else 0.0
+        e = math.exp(d) * beta
+        delta = logp_tol(lp[row], b.V)
+        c_abs[row] = b.scale * w * ((a * ratio + e) * (delta + 8 * U) + 8 * U * beta)
+        loss_tol[i] += w * ((a * ratio + e + beta) * (delta + 8 * U) + 8 * U * beta * abs(d)) * 1.01 + 4 * U * w * a * 2
+    return c_abs, loss_tol
+
+
+@pytest.mark.parametrize("layout", range(len(LAYOUTS)))
+@pytest.mark.parametrize("dtype", list(NAMES), ids=NAMES.get)
+def test_policy_loss(dtype, layout):
+    for k, (V, n, T) in enumerate(SHAPES):
+        say(f"case: policy {NAMES[dtype]} V={V} n={n} T={T} layout={layout}")
+        b = Batch(V + 3 * n, dtype, V, n, T, **LAYOUTS[layout])
+        per_token, kl, has_old = k % 3 == 1, k % 4 != 3, k % 5 != 4
+        low, high, beta = 0.2, 0.28, 0.04 if kl else 0.0
+        old, ref = b.old_ref((1 - low, 1 + high))
+        adv = b.r.standard_normal(b.rows if per_token else b.n).astype(np.float32)
+        up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+        loss, logp = torch.full((n,), 7.0, device="cuda"), torch.full((b.rows,), 7.0, device="cuda")
+        dl, _ = b.dbuf()
+        P.attr_policy_loss(b.tokens(), up(adv), loss, logp=logp, dlogits=dl, logp_old=up(old) if has_old else None,
+                           logp_ref=up(ref) if kl else None, per_token=per_token, clip_low=low, clip_high=high, beta=beta)
+        wl, wlp, wg = O.policy_loss(b.numpy(), b.target, n, T, adv, b.scale, logp_old=old if has_old else None, logp_ref=ref,
+                                    per_token=per_token, clip_low=low, clip_high=high, beta=beta, **b.where())
+        check_logp(b, host(logp), 7.0)
+        c_abs, tol = policy_tols(b, old if has_old else None, adv, ref, beta, per_token)
+        assert (np.abs(host(loss) - wl) <= tol + U * np.abs(wl)).all(), (host(loss), wl, tol)
+        check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 0.0, c_abs)
+        again = torch.full((n,), 7.0, device="cuda")  # the loss alone
+        P.attr_policy_loss(b.tokens(), up(adv), again, logp_old=up(old) if has_old else None, logp_ref=up(ref) if kl else None,
+                           per_token=per_token, clip_low=low, clip_high=high, beta=beta)
+        assert (np.abs(host(again) - wl) <= tol + U * np.abs(wl)).all()
+
+
+@pytest.mark.parametrize("layout", range(len(LAYOUTS)))
+@pytest.mark.parametrize("dtype", list(NAMES), ids=NAMES.get)
+def test_preference_loss(dtype, layout):
+    for k, (V, n, T) in enumerate(SHAPES):
+        n += n % 2
+        say(f"case: preference {NAMES[dtype]} V={V} n={n} T={T} layout={layout}")
+        b = Batch(V + 5 * n, dtype, V, n, T, **LAYOUTS[layout])
+        _, ref = b.old_ref()
+        has_ref, has_pw = k % 3 != 2, k % 2 == 0
+        pw = b.r.uniform(0.2, 2.0, n // 2).astype(np.float32)
+        args = dict(beta=0.3, margin=0.25 if k % 4 == 0 else 0.0, label_smoothing=0.1 if k % 2 else 0.0)
+        up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+        loss, ratio = torch.full((n // 2,), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")
+        logp = torch.full((b.rows,), 7.0, device="cuda")
+        dl, _ = b.dbuf()
+        P.attr_preference_loss(b.tokens(), loss, log_ratio=ratio, logp=logp, dlogits=dl, logp_ref=up(ref) if has_ref else None,
+                               pair_weight=up(pw) if has_pw else None, **args)
+        wl, wr, wlp, wg = O.preference_loss(b.numpy(), b.target, n, T, b.scale, logp_ref=ref if has_ref else None,
+                                            pair_weight=pw if has_pw else None, **args, **b.where())
+        check_logp(b, host(logp), 7.0)
+        r_tol = np.zeros(n)
+        for i, _, row, counts in b.slots():
+            if counts:
+                r_tol[i] += (1.0 if b.weight is None else b.weight[row]) * logp_tol(wlp[row], V)
+        assert (np.abs(host(ratio) - wr) <= r_tol + 2 * U * np.abs(wr)).all(), (host(ratio), wr, r_tol)
+        weight = pw if has_pw else np.ones(n // 2)
+        h_tol = 0.3 * (r_tol[:n // 2] + r_tol[n // 2:])
+        assert (np.abs(host(loss) - wl) <= weight * h_tol + 2 * U * np.abs(wl)).all()
+        c_abs = np.zeros(b.rows)  # sigma' <= 1/4
+        for i, _, row, counts in b.slots():
+            if counts:
+                j = i % (n // 2)
+                c_abs[row] = b.scale * (1.0 if b.weight is None else b.weight[row]) * weight[j] * 0.3 * h_tol[j] / 4
+        check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 4 * U, c_abs)
+
+
+@pytest.mark.parametrize("V,rows", [(700, 600), (12000, 300), (5003, 40)])
+def test_gradients_in_place(V, rows):
+    """dlogits may be the logits: the same bits as apart from them."""
+    for dtype in NAMES:
+        say(f"case: in place {NAMES[dtype]} V={V} rows={rows}")
+        b = Batch(V, dtype, V, rows, 1, weighted=True)
+        old, ref = b.old_ref()
+        up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+        adv = up(b.r.standard_normal(rows).astype(np.float32))
+        loss = torch.zeros(rows, device="cuda")
+        apart, _ = b.dbuf()
+        for call in ("policy", "pref"):
+            for into in (apart, b.logits):
+                rows_ = b.tokens()
+                if call == "policy":
+                    P.attr_policy_loss(rows_, adv, loss, dlogits=into, logp_old=up(old), logp_ref=up(ref), beta=0.1)
+                else:
+                    P.attr_preference_loss(rows_, loss, dlogits=into, logp_ref=up(ref))
+            assert torch.equal(apart, b.logits), call
+            b.sync()
+
+
+def test_masked_vocabulary_and_odd_values():
+    """-inf entries, the types' lowest values, rows of nothing, NaN and +inf, a target that is masked."""
+    for dtype in NAMES:
+        V = 3001
+        say(f"case: odd values {NAMES[dtype]}")
+        low = torch.finfo(dtype).min
+        b = Batch(5, dtype, V, 9, 1)
+        b.z[0, 1::2] = -math.inf          # half masked, the target not
+        b.target[0] = 4
+        b.z[1] = low                      # lowest everywhere: uniform
+        b.z[2] = -math.inf                # nothing left
+        b.z[3, 7] = math.nan
+        b.z[4, 9] = math.inf
+        b.z[5, 11], b.target[5] = -math.inf, 11   # the target masked
+        b.z[6] = low
+        b.z[6, 100] = 1.0                 # one entry against the lowest value
+        b.target[6] = 100
+        b.z[7, :] = -math.inf
+        b.z[7, 2999] = -2.0               # one entry left, at the end
+        b.target[7] = 2999
+        b.sync()
+        logp = torch.zeros(9, device="cuda")
+        P.attr_token_logp(b.tokens(), logp)
+        got = host(logp)
+        check_logp(b, got, None)
+        assert abs(got[1] + math.log(V)) <= logp_tol(math.log(V), V) and got[6] == 0 and got[7] == 0
+        assert np.isnan(got[[2, 3, 4]]).all() and np.isneginf(got[5])
+        # the gradient: zeros at masked entries, NaN rows NaN, others the formula's
+        loss, (dl, _) = torch.zeros(9, device="cuda"), b.dbuf()
+        P.attr_policy_loss(b.tokens(), torch.ones(9, device="cuda"), loss, dlogits=dl)
+        d = dl.double().cpu().numpy()
+        assert (d[0, 1::2] == 0).all() and (d[6] == 0).all() and (d[7] == 0).all()
+        assert np.isnan(d[[2, 3]]).all() and np.isnan(d[4]).all()
+        assert np.isnan(host(loss)[[2, 3, 4]]).all() and np.isfinite(host(loss)[[0, 1, 6, 7, 8]]).all()
+        want = -(np.eye(V)[b.target[1]] - 1 / V)
+        assert (np.abs(d[1] - want) <= 2 * ROUND[dtype] * np.abs(want) + rel_sum(V) / V + LEAST[dtype]).all()
+
+
+def test_examples_without_tokens():
+    """Lengths of zero, weights of zero, targets out of range: losses of zero, gradients of zero, nothing NaN."""
+    b = Batch(3, torch.bfloat16, 513, 6, 4)
+    b.length = np.array([0, 4, -3, 4, 9, 1], np.int32)   # clamped to [0, 4]
+    b.weight = np.ones(24, np.float32)
+    b.weight[4:8] = 0
+    b.target[12:16] = [513, -1, -100, 2 ** 40]
+    b.z[:4], b.z[8:12] = math.nan, math.nan
+    b.sync()
+    adv, ref = torch.ones(6, device="cuda"), torch.full((24,), -1.0, device="cuda")
+    loss, logp, (dl, _) = torch.full((6,), 7.0, device="cuda"), torch.full((24,), 7.0, device="cuda"), b.dbuf()
+    P.attr_policy_loss(b.tokens(), adv, loss, logp=logp, dlogits=dl, logp_ref=ref, beta=0.1)
+    assert (host(loss)[:4] == 0).all() and (host(logp)[:16] == 0).all() and (host(dl.float())[:16] == 0).all()
+    assert np.isfinite(host(loss)).all() and (host(loss)[4:] != 0).all() and (host(dl.float())[21:] == 0).all()
+    pl, ratio, (dl, _) = torch.full((3,), 7.0, device="cuda"), torch.full((6,), 7.0, device="cuda"), b.dbuf()
+    P.attr_preference_loss(b.tokens(), pl, log_ratio=ratio, dlogits=dl)
+    assert (host(ratio)[:4] == 0).all() and (host(dl.float())[:16] == 0).all()
+    assert np.isfinite(host(pl)).all()
+    P.attr_policy_loss(P.TokenRows(b.logits, torch.zeros(24, dtype=torch.int64, device="cuda"), 0, 4), adv, loss[:0])
+
+
+def test_rows_past_32_bits():
+    """Row offsets beyond 2^32 elements, and rows outside the buffer."""
+    V, rows = 32768, 140000  # 4.6e9 elements
+    say("case: far rows")
+    big = torch.empty((rows, V), dtype=torch.bfloat16, device="cuda")
+    b = Batch(11, torch.bfloat16, V, 4, 2)
+    at = [0, 139998, 131071]
+    for i, r in enumerate(at):
+        big[r:r + 2] = b.logits[2 * i:2 * i + 2]
+    target = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    for i, r in enumerate(at):
+        target[r:r + 2] = torch.from_numpy(b.target[2 * i:2 * i + 2]).cuda()
+    dl = torch.empty_like(big)
+    logp = torch.full((rows,), 7.0, device="cuda")
+    offs = torch.tensor(at + [rows], dtype=torch.int64, device="cuda")  # the last one: no row is inside
+    tok = P.TokenRows(big, target, 4, 2, row_offset=offs)
+    loss = torch.full((4,), 7.0, device="cuda")
+    P.attr_policy_loss(tok, torch.ones(4, device="cuda"), loss, logp=logp, dlogits=dl)
+    _, wlp, wg = O.policy_loss(b.numpy(), b.target, 3, 2, np.ones(3))
+    got = host(logp)
+    for i, r in enumerate(at):
+        for t in range(2):
+            assert abs(got[r + t] - wlp[2 * i + t]) <= logp_tol(wlp[2 * i + t], V)
+            d = dl[r + t].double().cpu().numpy()
+            w = wg[2 * i + t]
+            assert np.linalg.norm(d - w) <= 2.0 ** -8 * np.linalg.norm(w)
+    assert (np.delete(got, [0, 1, 139998, 139999, 131071, 131072]) == 7).all() and host(loss)[3] == 0
+
+
+def test_gradient_against_differences():
+    """Along random directions, the oracle's loss changes by what the kernel's gradient says."""
+    b = Batch(17, torch.float32, 301, 4, 5, ragged=True, weighted=True, scale=1.25)
+    low, high = 0.2, 0.28
+    old, ref = b.old_ref((1 - low, 1 + high))
+    adv = b.r.standard_normal(4).astype(np.float32)
+    up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    z, h = b.numpy(), 1e-5
+    kw = dict(logp_old=old, logp_ref=ref, clip_low=low, clip_high=high, beta=0.1)
+    dl, _ = b.dbuf(0.0)
+    P.attr_policy_loss(b.tokens(), up(adv), torch.zeros(4, device="cuda"), dlogits=dl, **{**kw, "logp_old": up(old), "logp_ref": up(ref)})
+    pl, _ = b.dbuf(0.0)
+    P.attr_preference_loss(b.tokens(), torch.zeros(2, device="cuda"), dlogits=pl, logp_ref=up(ref), beta=0.3, margin=0.1, label_smoothing=0.05)
+    for k in range(6):
+        d = b.r.standard_normal(z.shape)
+        f = lambda s: O.policy_loss(z + s * d, b.target, 4, 5, adv, b.scale, **kw, **b.where())[0].sum()  # noqa: B023,E731
+        g = lambda s: O.preference_loss(z + s * d, b.target, 4, 5, b.scale, logp_ref=ref, beta=0.3, margin=0.1,  # noqa: B023,E731
+                                        label_smoothing=0.05, **b.where())[0].sum()
+        for fn, grad in ((f, dl), (g, pl)):
+            want = (fn(h) - fn(-h)) / (2 * h)
+            grad = grad.double().cpu().numpy()
+            # truncation h^2 x third derivative (O(1) a token), cancellation 1e-16 / h, fp32 gradients
+            tol = 1e-8 + rel_sum(301) * np.linalg.norm(grad) * np.linalg.norm(d)
+            assert abs((grad * d).sum() - want) <= tol, (k, (grad * d).sum(), want)
+
+
+def test_other_stream_and_workspace():
+    """A side stream with a workspace of its own gives the bits of the default stream."""
+    b = Batch(23, torch.bfloat16, 20011, 6, 8, ragged=True)
+    adv = torch.ones(6, device="cuda")
+    outs = []
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        loss, (dl, _) = torch.zeros(6, device="cuda"), b.dbuf()
+        tok = b.tokens()
+        torch.cuda.synchronize()
+        P.attr_policy_loss(tok, adv, loss, dlogits=dl, ws=P.Workspace(), stream=stream)
+        torch.cuda.synchronize()
+        outs.append((loss, dl))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+def test_refusals_on_the_device():
+    z = torch.zeros((8, 100), device="cuda")
+    y = torch.zeros(8, dtype=torch.int64, device="cuda")
+    loss, adv = torch.full((4,), 7.0, device="cuda"), torch.ones(4, device="cuda")
+    rows = P.TokenRows(z, y, 4, 2)
+    with pytest.raises(P.AttrError, match="needs logp_ref"):
+        P.attr_policy_loss(rows, adv, loss, beta=0.1)
+    with pytest.raises(P.AttrError, match="clip_low"):
+        P.attr_policy_loss(rows, adv, loss, clip_low=-0.1)
+    with pytest.raises(P.AttrError, match="label_smoothing"):
+        P.attr_preference_loss(rows, loss, label_smoothing=1.5)
+    with pytest.raises(P.AttrError, match="even"):
+        P.attr_preference_loss(P.TokenRows(z, y, 3, 2), loss)
+    with pytest.raises(P.AttrError, match="logit_scale"):
+        P.attr_token_logp(P.TokenRows(z, y, 4, 2, logit_scale=0.0), torch.zeros(8, device="cuda"))
+    with pytest.raises(P.AttrError, match="overlaps"):
+        buf = torch.zeros(2000, device="cuda")
+        P.attr_policy_loss(P.TokenRows(buf[:800].view(8, 100), y, 4, 2), adv, loss, dlogits=buf[50:850].view(8, 100))
+    with pytest.raises(ValueError, match="same GPU"):
+        P.attr_token_logp(P.TokenRows(z, y.cpu(), 4, 2), torch.zeros(8, device="cuda"))
+    assert (loss == 7).all()

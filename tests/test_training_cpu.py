@@ -1,0 +1,185 @@
+"""The post-training steps on the CPU: the oracle's gradients against differences, its
+8-bit format against torch's, and every refusal of the C entry points and the binding."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_11660_amd as P
+from oracle import training as O
+
+INVALID, UNSUPPORTED, ALIGN, WORKSPACE = 1, 2, 3, 4
+FAKE = 0x100000
+
+
+def test_oracle_gradients_against_differences():
+    r = np.random.default_rng(1)
+    z, y = r.standard_normal((12, 17)) * 2, r.integers(0, 17, 12)
+    y[3] = -100
+    w = r.uniform(0.2, 1.0, 12).astype(np.float32)
+    w[7] = 0
+    length = np.array([3, 0, 2, 3])
+    where = dict(weight=w, length=length)
+    old, ref = r.normal(-2, 0.5, 12).astype(np.float32), r.normal(-2, 0.5, 12).astype(np.float32)
+    adv = r.standard_normal(4).astype(np.float32)
+
+    def policy(x):
+        return O.policy_loss(x, y, 4, 3, adv, 1.25, logp_old=old, logp_ref=ref, beta=0.3, **where)
+
+    def pref(x):
+        loss, _, logp, grad = O.preference_loss(x, y, 4, 3, 1.25, logp_ref=ref, pair_weight=[0.5, 2.0], beta=0.4,
+                                                margin=0.2, label_smoothing=0.1, **where)
+        return loss, logp, grad
+    for f in (policy, pref):
+        grad, h = f(z)[2], 1e-6
+        assert sorted(grad) == list(range(12))
+        for row in range(12):
+            for j in range(17):
+                d = np.zeros_like(z)
+                d[row, j] = h
+                want = (f(z + d)[0].sum() - f(z - d)[0].sum()) / (2 * h)
+                assert abs(grad[row][j] - want) < 1e-8, (f.__name__, row, j)
+
+
+def test_oracle_e4m3_against_torch():
+    x = np.concatenate([np.random.default_rng(2).uniform(-448, 448, 20000), O.E4M3, -O.E4M3,
+                        (O.E4M3[1:] + O.E4M3[:-1]) / 2, 2.0 ** np.linspace(-14, 8.8, 999)]).astype(np.float32)
+    x = np.clip(x, -448, 448)
+    assert np.array_equal(O.e4m3(x), torch.from_numpy(x).to(torch.float8_e4m3fn).double().numpy())
+
+
+def _rows(**kw):
+    base = dict(logits=FAKE, dtype=P.ATTR_F32, n_rows=8, V=100, ldl=100, logit_scale=1.0, target=FAKE, weight=None,
+                n_examples=4, T=2, row_offset=None, length=None)
+    base.update(kw)
+    return P._CTokenRows(*base.values())
+
+
+def _calls(rows):
+    """Each entry point on these rows, with valid further arguments and no workspace."""
+    L = P.lib()
+    out = 0x900000
+    return [L.attr_token_logp(rows, out, None, 0, None),
+            L.attr_policy_loss(rows, FAKE, 0, None, None, 0.2, 0.2, 0.0, out, None, None, 0, None, 0, None),
+            L.attr_preference_loss(rows, None, None, 0.1, 0.0, 0.0, out, None, None, None, 0, None, 0, None)]
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(dtype=P.ATTR_E4M3), UNSUPPORTED), (dict(V=0), INVALID), (dict(V=2 ** 28 + 1, ldl=2 ** 29), INVALID),
+    (dict(ldl=99), INVALID), (dict(ldl=2 ** 41), INVALID), (dict(n_rows=-1), INVALID), (dict(n_rows=7), INVALID),
+    (dict(n_rows=2 ** 62), INVALID), (dict(n_examples=-2), INVALID), (dict(T=0), INVALID),
+    (dict(n_examples=2 ** 20, T=2 ** 11, n_rows=2 ** 31), UNSUPPORTED), (dict(n_examples=2 ** 62, T=4), UNSUPPORTED),
+    (dict(T=2 ** 62), UNSUPPORTED),
+    (dict(logit_scale=0.0), INVALID), (dict(logit_scale=-1.0), INVALID), (dict(logit_scale=float("nan")), INVALID),
+    (dict(logit_scale=float("inf")), INVALID), (dict(logits=None), INVALID), (dict(target=None), INVALID),
+    (dict(logits=FAKE + 2), ALIGN), (dict(target=FAKE + 4), ALIGN), (dict(weight=FAKE + 2), ALIGN),
+    (dict(row_offset=FAKE + 4), ALIGN), (dict(length=FAKE + 2), ALIGN)])
+def test_token_rows_refusals(bad, status):
+    assert _calls(_rows(**bad)) == [status] * 3, P.lib().attr_last_error()
+
+
+def test_token_calls_without_work():
+    """No examples: nothing is enqueued, nothing is needed."""
+    assert _calls(_rows(n_examples=0, n_rows=0, logits=None, target=None)) == [0, 0, 0]
+
+
+def test_policy_refusals():
+    L, rows = P.lib(), _rows()
+    ws = L.attr_policy_loss_workspace_size(rows)
+    assert ws >= 4 * 8
+
+    def call(adv=FAKE, per=0, old=None, ref=None, lo=0.2, hi=0.2, beta=0.0, loss=0x900000, logp=None, d=None, ldd=100,
+             w=0xa00000, wn=ws):
+        return L.attr_policy_loss(rows, adv, per, old, ref, lo, hi, beta, loss, logp, d, ldd, w, wn, None)
+    nan = float("nan")
+    assert call(adv=None) == INVALID and call(loss=None) == INVALID and call(per=2) == INVALID
+    assert call(lo=-0.1) == INVALID and call(lo=nan) == INVALID and call(hi=-1.0) == INVALID and call(hi=nan) == INVALID
+    assert call(beta=-0.1) == INVALID and call(beta=nan) == INVALID and call(beta=float("inf")) == INVALID
+    assert call(beta=0.1) == INVALID and b"logp_ref" in L.attr_last_error()
+    assert call(adv=FAKE + 2) == ALIGN and call(loss=0x900002) == ALIGN and call(old=FAKE + 1) == ALIGN
+    assert call(ref=FAKE + 2) == ALIGN and call(logp=FAKE + 2) == ALIGN
+    assert call(d=0x800000, ldd=99) == INVALID and call(d=0x800002) == ALIGN
+    assert call(d=FAKE + 400) == INVALID and b"overlap" in L.attr_last_error()
+    assert call(d=FAKE, ldd=101) == INVALID
+    assert call(w=None) == WORKSPACE and call(wn=ws - 1) == WORKSPACE and call(w=0xa00010) == ALIGN
+
+
+def test_preference_refusals():
+    L = P.lib()
+
+    def call(rows=None, ref=None, pw=None, beta=0.1, margin=0.0, e=0.0, loss=0x900000, ratio=None, logp=None, d=None,
+             ldd=100, w=0xa00000, wn=1 << 20):
+        return L.attr_preference_loss(rows or _rows(), ref, pw, beta, margin, e, loss, ratio, logp, d, ldd, w, wn, None)
+    nan, inf = float("nan"), float("inf")
+    assert call(_rows(n_examples=3)) == INVALID and b"even" in L.attr_last_error()
+    for kw in (dict(beta=nan), dict(beta=inf), dict(margin=nan), dict(margin=-inf), dict(e=-0.1), dict(e=1.1), dict(e=nan),
+               dict(loss=None), dict(d=0x800000, ldd=10), dict(d=FAKE + 400)):
+        assert call(**kw) == INVALID, kw
+    for kw in (dict(ref=FAKE + 2), dict(pw=FAKE + 2), dict(loss=0x900001), dict(ratio=FAKE + 2), dict(logp=FAKE + 2),
+               dict(d=0x800001), dict(w=0xa00004)):
+        assert call(**kw) == ALIGN, kw
+    need = L.attr_preference_loss_workspace_size(_rows())
+    assert call(wn=need - 1) == WORKSPACE and call(w=None) == WORKSPACE
+
+
+def test_workspace_queries_of_odd_batches():
+    L = P.lib()
+    for name in ("attr_token_logp", "attr_policy_loss", "attr_preference_loss"):
+        query = getattr(L, name + "_workspace_size")
+        assert query(None) == 0
+        assert query(_rows(n_examples=-1)) == 0 and query(_rows(T=0)) == 0 and query(_rows(n_examples=2 ** 40)) == 0
+        assert query(_rows(n_examples=2 ** 20, T=2 ** 10, n_rows=2 ** 30)) % 256 == 0
+
+
+def test_adamw_refusals():
+    L = P.lib()
+
+    def tensor(**kw):
+        base = dict(p=0x100000, g=0x200000, m=0x300000, v=0x400000, master=None, m_scale=None, v_scale=None, n=100,
+                    lr_scale=1.0, weight_decay=0.0)
+        base.update(kw)
+        return (P._CAdamTensor * 1)(P._CAdamTensor(*base.values()))
+
+    def call(t=None, n=1, p=P.ATTR_F32, g=P.ATTR_F32, s=P.ATTR_F32, step=1, lr=1e-3, b1=0.9, b2=0.95, eps=1e-8, root=0.0,
+             gs=None):
+        return L.attr_adamw_step(tensor() if t is None else t, n, p, g, s, step, lr, b1, b2, eps, root, gs, None)
+    nan, inf = float("nan"), float("inf")
+    assert call(n=0) == 0 and L.attr_adamw_step(None, 0, 0, 0, 0, 1, 0.1, 0.9, 0.9, 0.0, 0.0, None, None) == 0
+    assert call(tensor(n=0, p=None, g=None, m=None, v=None)) == 0
+    for kw in (dict(n=-1), dict(step=0), dict(b1=1.0), dict(b2=-0.1), dict(b1=nan), dict(eps=-1.0), dict(eps=nan),
+               dict(root=inf), dict(lr=nan), dict(lr=inf)):
+        assert call(**kw) == INVALID, kw
+    assert L.attr_adamw_step(None, 1, 0, 0, 0, 1, 0.1, 0.9, 0.9, 0.0, 0.0, None, None) == INVALID
+    for kw in (dict(p=P.ATTR_E4M3), dict(g=P.ATTR_E4M3), dict(s=P.ATTR_BF16), dict(s=7), dict(p=9)):
+        assert call(**kw) == UNSUPPORTED, kw
+    for kw in (dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(n=-5), dict(n=2 ** 40), dict(lr_scale=nan),
+               dict(weight_decay=inf), dict(m_scale=FAKE), dict(v_scale=FAKE)):
+        assert call(tensor(**kw)) == INVALID, kw
+    assert call(tensor(m_scale=FAKE), s=P.ATTR_E4M3) == INVALID and call(s=P.ATTR_E4M3) == INVALID
+    for kw in (dict(p=0x100002), dict(g=0x200002), dict(m=0x300001), dict(v=0x400002), dict(master=0x500002)):
+        assert call(tensor(**kw)) == ALIGN, kw
+    assert call(tensor(m_scale=0x500002, v_scale=0x600000), s=P.ATTR_E4M3) == ALIGN
+    assert call(gs=0x700002) == ALIGN
+
+
+def test_binding_refusals():
+    """The binding checks shapes, types and devices before it calls the library."""
+    z, y = torch.zeros((8, 100)), torch.zeros(8, dtype=torch.int64)
+    for kw, text in ((dict(n_examples=5, T=2), "hold 8 rows"), (dict(n_examples=4, T=0), "T >= 1"),
+                     (dict(n_examples=4, T=2, weight=torch.zeros(7)), "weight"),
+                     (dict(n_examples=4, T=2, length=torch.zeros(4)), "length"),
+                     (dict(n_examples=4, T=2, row_offset=torch.zeros(3, dtype=torch.int64)), "row_offset"),
+                     (dict(n_examples=4, T=2), "same GPU")):
+        with pytest.raises(ValueError, match=text):
+            P.TokenRows(z, y, **kw).c()
+    with pytest.raises(ValueError, match="contiguous last"):
+        P.TokenRows(z.t(), y, 4, 2).c()
+    with pytest.raises(ValueError, match="target"):
+        P.TokenRows(z, y.int(), 4, 2).c()
+    with pytest.raises(ValueError, match="at least one"):
+        P.AdamTensors([], [], [], [])
+    x = torch.zeros(10)
+    with pytest.raises(ValueError, match="same GPU"):
+        P.AdamTensors([x], [x], [x], [x])
+    assert ctypes.sizeof(P._CTokenRows) == 96 and ctypes.sizeof(P._CAdamTensor) == 72
