@@ -91,13 +91,13 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
       am = am < kAmaxLeast ? kAmaxLeast : am;
       av = av < kAmaxLeast ? kAmaxLeast : av;
       if (in) {
-        ((uint8_t*)t.m)[i] = e4m3_code(r.m * (kE4M3Max / am));
-        const float q = root * (kE4M3Max / av);
+        ((uint8_t*)t.m)[i] = e4m3_code(r.m * (1.f / am * kE4M3Max));
+        const float q = root * (1.f / av * kE4M3Max);
         ((uint8_t*)t.v)[i] = e4m3_code(q > 0.f && q < kE4M3Least ? kE4M3Least : q);
       }
       if (threadIdx.x == 0) {
-        t.m_scale[b / kQuantBlock] = am < INFINITY ? am / kE4M3Max : NAN;
-        t.v_scale[b / kQuantBlock] = av < INFINITY ? av / kE4M3Max : NAN;
+        t.m_scale[b / kQuantBlock] = am < INFINITY ? am * (1.f / kE4M3Max) : NAN;
+        t.v_scale[b / kQuantBlock] = av < INFINITY ? av * (1.f / kE4M3Max) : NAN;
       }
     } else if (in) {
       ((float*)t.m)[i] = r.m;

@@ -734,9 +734,7 @@ attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, 
     st = token_workspace(L, ws, ws_bytes, who);
     if (st != ATTR_OK) return st;
     const attr::TokenArgs a = token_args(rows, logp, nullptr, 0);
-    attr::PolicyArgs p;
-    std::memset(&p, 0, sizeof(p));
-    const hipError_t e = attr::launch_token_rows(attr::kTokenLogp, (int)rows->dtype, a, p, static_cast<hipStream_t>(stream));
+    const hipError_t e = attr::launch_token_logp((int)rows->dtype, false, a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_token_logp launch");
   } catch (...) {
     return fail(ATTR_ERR_INVALID_ARG, "attr_token_logp: host exception");
@@ -779,7 +777,7 @@ attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage
     p.beta = beta;
     p.token_loss = static_cast<float*>(ws);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = attr::launch_token_rows(attr::kTokenPolicy, (int)rows->dtype, a, p, s);
+    hipError_t e = attr::launch_policy_rows((int)rows->dtype, a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_policy_loss launch");
     e = attr::launch_example_sum(p.token_loss, a.T, (uint32_t)rows->n_examples, loss, s);
     return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_policy_loss sum launch");
@@ -817,8 +815,6 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
     attr::TokenArgs a = token_args(rows, logp, dlogits, ldd);
     a.stats = reinterpret_cast<float2*>(base + L.off_stats);
     a.slot_logp = reinterpret_cast<float*>(base + L.off_logp);
-    attr::PolicyArgs none;
-    std::memset(&none, 0, sizeof(none));
     attr::PrefArgs p;
     std::memset(&p, 0, sizeof(p));
     p.logp_ref = logp_ref;
@@ -831,7 +827,7 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
     p.margin = margin;
     p.smoothing = label_smoothing;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = attr::launch_token_rows(attr::kTokenPref, (int)rows->dtype, a, none, s);
+    hipError_t e = attr::launch_token_logp((int)rows->dtype, true, a, s);
     if (e != hipSuccess) return device_fail(e, "attr_preference_loss launch");
     e = attr::launch_pairs(a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_preference_loss pair launch");

@@ -192,7 +192,7 @@ hipError_t launch_apply_few(const ApplyFewPlan& P, const void* X, int64_t n_rows
 // ---------------------------------------------------------------------------
 // losses over token log-probabilities
 // ---------------------------------------------------------------------------
-constexpr int kTokenLogp = 0, kTokenPolicy = 1, kTokenPref = 2;
+constexpr int kTokenLogp = 0, kTokenPolicy = 1, kTokenPref = 2;  // the three calls
 struct TokenArgs {
   const void* logits;
   const int64_t* target;
@@ -201,7 +201,7 @@ struct TokenArgs {
   const int32_t* length;       // or null
   float* logp;                 // or null
   void* dlogits;               // or null
-  float2* stats;               // per slot: row maximum and sum (preference loss)
+  float2* stats;               // per slot: a row's offset and sum (preference loss)
   float* slot_logp;            // per slot (preference loss)
   int64_t n_rows, ldl, ldd;
   uint32_t n_slots, T;         // slot = example * T + token
@@ -225,7 +225,8 @@ struct PrefArgs {
   uint32_t n_pairs;
   float beta, margin, smoothing;
 };
-hipError_t launch_token_rows(int mode, int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s);
+hipError_t launch_token_logp(int dtype, bool pref, const TokenArgs& a, hipStream_t s);
+hipError_t launch_policy_rows(int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s);
 hipError_t launch_example_sum(const float* token_loss, uint32_t T, uint32_t n, float* loss, hipStream_t s);
 hipError_t launch_pairs(const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 hipError_t launch_pref_grad(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);

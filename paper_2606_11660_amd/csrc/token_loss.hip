@@ -2,11 +2,19 @@
 // the paired log-ratio preference loss, with their gradients with respect to
 // the logits.
 //
-// A row's log-probability is s (z_y - m) - log S with m = max_j z_j and
-// S = sum_j exp(s (z_j - m)); the differences are formed first, so large or
-// lowest-value logits neither overflow nor cancel.  The gradient of any loss
-// with derivative c by that log-probability is s c ([j = y] - e_j / S), e_j the
-// same exponentials.
+// With c = s log2 e, a row's largest m and e_j = exp2(c z_j - c m), S = sum e_j:
+//     logp = (c z_y - c m - log2 S) ln 2,   p_j = e_j / S,
+// and the gradient of a loss with derivative g by logp is s g ([j = y] - p_j).
+// c z_j - c m is one fused multiply-add with the rounded c m: its rounding is the
+// same factor in every e_j and cancels (up to |c m| = 2^20, see kMostMc; other
+// rows, those of infinities and of nothing but a mask's lowest value among them,
+// form the differences z_j - m first).  Sums are fp32 chains per thread, then
+// trees.
+//
+// All of it is bound by HBM: a row is read once, with 16-byte loads that need no
+// alignment beyond the element's (an odd vocabulary's rows start anywhere).  The
+// last vector of a row is moved back to end with it, and the sum leaves out what
+// it then holds twice.
 #include "common.h"
 #include "kernels.h"
 
@@ -14,6 +22,8 @@ namespace attr {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kMostMc = 1048576.f;  // 2^20: the residual of the fused form stays below 2^-4
 
 // What a workgroup does with one token's slot.
 struct Slot {
@@ -42,27 +52,269 @@ __device__ inline Slot slot_of(const TokenArgs& a, uint32_t slot) {
   return r;
 }
 
+// ---------------------------------------------------------------------------
+// 16-byte vectors of elements
+// ---------------------------------------------------------------------------
 template <typename T>
-__device__ inline float as_f32(T x) { return (float)x; }
+constexpr int kE = 16 / (int)sizeof(T);  // elements of a vector
 
-// A running maximum of logits and the sum of exp2(c (z - max)), c = s log2 e.
-struct MaxSum {
-  float m, s;
-};
-__device__ inline MaxSum join(MaxSum a, MaxSum b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  // a side that holds nothing (-inf) adds nothing; NaN stays NaN through its sum
-  const float sa = a.m == m ? a.s : a.s * __builtin_amdgcn_exp2f((a.m - m) * c);
-  const float sb = b.m == m ? b.s : b.s * __builtin_amdgcn_exp2f((b.m - m) * c);
-  return {m, sa + sb};
+// vectors at any element's address
+template <typename T>
+struct Loose;
+template <>
+struct Loose<float> { typedef i32x4 vec __attribute__((aligned(4))); };
+template <>
+struct Loose<__bf16> { typedef i32x4 vec __attribute__((aligned(2))); };
+template <>
+struct Loose<_Float16> { typedef i32x4 vec __attribute__((aligned(2))); };
+
+template <typename T>
+__device__ inline i32x4 load_vec(const T* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const typename Loose<T>::vec*>(p));
 }
-__device__ inline MaxSum wave_join(MaxSum v, float c) {
+template <typename T>
+__device__ inline void store_vec(T* p, i32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<typename Loose<T>::vec*>(p));
+}
+
+__device__ inline void unpack(i32x4 v, float, float (&x)[4]) {
+  const f32x4 f = __builtin_bit_cast(f32x4, v);
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1)
-    v = join(v, MaxSum{__shfl_xor(v.m, off, kWave), __shfl_xor(v.s, off, kWave)}, c);
-  return v;
+  for (int e = 0; e < 4; ++e) x[e] = f[e];
+}
+__device__ inline void unpack(i32x4 v, __bf16, float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __builtin_bit_cast(float, v[e] << 16);
+    x[2 * e + 1] = __builtin_bit_cast(float, v[e] & (int)0xffff0000);
+  }
+}
+__device__ inline void unpack(i32x4 v, _Float16, float (&x)[8]) {
+  const f16x8 h = __builtin_bit_cast(f16x8, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
 }
 
+__device__ inline i32x4 pack(const float (&x)[4], float) {
+  return __builtin_bit_cast(i32x4, f32x4{x[0], x[1], x[2], x[3]});
+}
+__device__ inline i32x4 pack(const float (&x)[8], __bf16) {
+  bf16x8 h;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] = (__bf16)x[e];
+  return __builtin_bit_cast(i32x4, h);
+}
+__device__ inline i32x4 pack(const float (&x)[8], _Float16) {
+  f16x8 h;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] = (_Float16)x[e];
+  return __builtin_bit_cast(i32x4, h);
+}
+
+// ---------------------------------------------------------------------------
+// reductions
+// ---------------------------------------------------------------------------
+// Lane shifts within rows of 16 and broadcasts across them, no LDS: the result
+// is in lane 63 and returned to all.
+template <int CTRL, int ROWS>
+__device__ inline float dpp(float old, float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, x),
+                                                               CTRL, ROWS, 0xf, false));
+}
+__device__ inline float lane63(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ inline float wave_max_dpp(float x) {
+  x = fmaxf(x, dpp<0x111, 0xf>(-INFINITY, x));
+  x = fmaxf(x, dpp<0x112, 0xf>(-INFINITY, x));
+  x = fmaxf(x, dpp<0x114, 0xf>(-INFINITY, x));
+  x = fmaxf(x, dpp<0x118, 0xf>(-INFINITY, x));
+  x = fmaxf(x, dpp<0x142, 0xa>(-INFINITY, x));
+  x = fmaxf(x, dpp<0x143, 0xc>(-INFINITY, x));
+  return lane63(x);
+}
+__device__ inline float wave_sum_dpp(float x) {
+  x += dpp<0x111, 0xf>(0.f, x);
+  x += dpp<0x112, 0xf>(0.f, x);
+  x += dpp<0x114, 0xf>(0.f, x);
+  x += dpp<0x118, 0xf>(0.f, x);
+  x += dpp<0x142, 0xa>(0.f, x);
+  x += dpp<0x143, 0xc>(0.f, x);
+  return lane63(x);
+}
+template <int NT>
+__device__ inline float block_max(float x, float* sh) {
+  x = wave_max_dpp(x);
+  if (NT == 64) return x;
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = sh[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) x = fmaxf(x, sh[w]);
+  return x;
+}
+template <int NT>
+__device__ inline float block_add(float x, float* sh) {
+  x = wave_sum_dpp(x);
+  if (NT == 64) return x;
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = sh[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) x += sh[w];
+  return x;
+}
+
+// Scratch of a workgroup: two sets, so that a reduction's reads need no barrier
+// before the next one's writes.
+struct Shared {
+  float max[16], sum[16], slow[16], zy;
+};
+
+// A row's maximum and sum in either form: offset is c m and x_j = fma(z_j, c,
+// -offset) in the fused form; in the other, x_j = (z_j - offset) c, offset = m.
+struct RowSum {
+  float offset, sum;
+  bool apart;
+};
+__device__ inline float exponent(float z, float c, const RowSum& r) {
+  return r.apart ? (z - r.offset) * c : fmaf(z, c, -r.offset);
+}
+__device__ inline float row_logp(float zy, float c, const RowSum& r) {
+  return (exponent(zy, c, r) - log2f(r.sum)) * kLn2;
+}
+
+// The sum with the differences formed first, one element at a time: rows whose
+// maximum m the fused form does not take.
+template <typename T, int NT>
+__device__ RowSum row_sum_apart(const T* z, int32_t V, float c, float m, float* sh) {
+  float s = 0.f;
+#pragma unroll 1
+  for (int32_t j = threadIdx.x; j < V; j += NT) s += __builtin_amdgcn_exp2f(((float)z[j] - m) * c);
+  return {m, block_add<NT>(s, sh), true};
+}
+template <typename T, int NT>
+__device__ void row_grad_apart(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
+                               float ce) {
+#pragma unroll 1
+  for (int32_t j = threadIdx.x; j < V; j += NT) {
+    float d = ce * __builtin_amdgcn_exp2f(exponent((float)z[j], c, r));
+    if (j == y) d += cs;
+    out[j] = (T)d;
+  }
+}
+
+template <typename T, int NT>
+__device__ inline void row_zero(T* out, int32_t V) {
+  if (V < kE<T>) {
+    if ((int32_t)threadIdx.x < V) out[threadIdx.x] = (T)0.f;
+    return;
+  }
+  for (int32_t j = threadIdx.x * kE<T>; j < V; j += NT * kE<T>)
+    store_vec(out + (j < V - kE<T> ? j : V - kE<T>), i32x4{0, 0, 0, 0});
+}
+
+// One vector's gradient, from its elements.
+template <typename T>
+__device__ inline i32x4 grad_vec(i32x4 v, float c, float offset, float cs, float ce, int32_t y_at) {
+  float x[kE<T>];
+  unpack(v, T{}, x);
+#pragma unroll
+  for (int e = 0; e < kE<T>; ++e) x[e] = ce * __builtin_amdgcn_exp2f(fmaf(x[e], c, -offset));
+  if ((uint32_t)y_at < (uint32_t)kE<T>) {
+#pragma unroll
+    for (int e = 0; e < kE<T>; ++e) x[e] += e == y_at ? cs : 0.f;
+  }
+  return pack(x, T{});
+}
+
+// A row's maximum and sum in one sweep: per thread a running maximum (not below
+// -2^20 / c, so that nothing but -inf needs no case of its own) and a sum that is
+// rescaled when it grows, U vectors at a time.
+template <typename T, int NT>
+__device__ RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& sh) {
+  constexpr int E = kE<T>, U = 4;
+  float top = -INFINITY, mc = -kMostMc, s = 0.f;
+  if (V >= E) {
+    for (int32_t j0 = threadIdx.x * E; j0 < V; j0 += NT * E * U) {
+      i32x4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int32_t j = j0 + u * NT * E;
+        if (j < V) v[u] = load_vec(z + (j < V - E ? j : V - E));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int32_t j = j0 + u * NT * E;
+        if (j >= V) continue;
+        float x[E];
+        unpack(v[u], T{}, x);
+        float m = x[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) m = fmaxf(m, x[e]);
+        top = fmaxf(top, m);
+        if (m * c > mc) {
+          s *= __builtin_amdgcn_exp2f(mc - m * c);
+          mc = m * c;
+        }
+        const int32_t twice = j - (V - E);
+        if (twice <= 0) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) s += e >= twice ? __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc)) : 0.f;
+        }
+      }
+    }
+  } else if ((int32_t)threadIdx.x < V) {
+    top = (float)z[threadIdx.x];
+    mc = fmaxf(top * c, mc);
+    s = __builtin_amdgcn_exp2f(fmaf(top, c, -mc));
+    if (top != top) s = top;
+  }
+  const float m = block_max<NT>(top, sh.max);
+  if (!(fabsf(m * c) <= kMostMc)) return row_sum_apart<T, NT>(z, V, c, m, sh.slow);
+  const float most = m * c;
+  s *= __builtin_amdgcn_exp2f(mc - most);
+  return {most, block_add<NT>(s, sh.sum), false};
+}
+
+// The gradient of one row, read a second time.  A thread reads and writes its own
+// elements only (the two may be one buffer), so the last vector, if it is not
+// whole, goes element by element.
+template <typename T, int NT>
+__device__ void row_grad_stream(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
+                                float ce) {
+  constexpr int E = kE<T>, U = 4;
+  if (r.apart) return row_grad_apart<T, NT>(z, out, V, y, c, r, cs, ce);
+  for (int32_t j0 = threadIdx.x * E; j0 < V; j0 += NT * E * U) {
+    i32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t j = j0 + u * NT * E;
+      if (j + E <= V) v[u] = load_vec(z + j);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int32_t j = j0 + u * NT * E;
+      if (j + E <= V) {
+        store_vec(out + j, grad_vec<T>(v[u], c, r.offset, cs, ce, y - j));
+      } else {
+#pragma unroll 1
+        for (int32_t k = j; k < V; ++k) {
+          float d = ce * __builtin_amdgcn_exp2f(fmaf((float)z[k], c, -r.offset));
+          if (k == y) d += cs;
+          out[k] = (T)d;
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// kernels
+// ---------------------------------------------------------------------------
 // Loss and derivative by logp of one token of the policy loss, weights included.
 struct TokenLoss {
   float loss, c;
@@ -84,54 +336,141 @@ __device__ inline TokenLoss policy_token(const PolicyArgs& p, const TokenArgs& a
   return {w * loss, w * c};
 }
 
-template <typename T, int MODE>
-__global__ __launch_bounds__(256) void token_kernel(TokenArgs a, PolicyArgs p) {
-  __shared__ MaxSum sh[4];
+// Outputs of a slot that does not count.
+template <typename T, int NT>
+__device__ inline void skip_slot(const TokenArgs& a, const Slot& sl) {
+  if (!sl.write) return;
+  if (threadIdx.x == 0 && a.logp) a.logp[sl.row] = 0.f;
+  if (a.dlogits) row_zero<T, NT>((T*)a.dlogits + sl.row * a.ldd, a.V);
+}
+
+// Log-probabilities (PREF: and what the gradient needs of each row), one sweep.
+template <typename T, int NT, bool PREF>
+__global__ __launch_bounds__(NT) void token_logp_kernel(TokenArgs a) {
+  __shared__ Shared sh;
   const float c = a.scale * kLog2e;
   for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
     const Slot sl = slot_of(a, slot);
-    T* out = a.dlogits ? (T*)a.dlogits + sl.row * a.ldd : nullptr;
     if (!sl.counts) {
-      if (threadIdx.x == 0) {
-        if (sl.write && a.logp) a.logp[sl.row] = 0.f;
-        if (MODE == kTokenPolicy) p.token_loss[slot] = 0.f;
-      }
-      if (sl.write && out)
-        for (int32_t j = threadIdx.x; j < a.V; j += 256) out[j] = (T)0.f;
+      if (threadIdx.x == 0 && sl.write && a.logp) a.logp[sl.row] = 0.f;
       continue;
     }
     const T* z = (const T*)a.logits + sl.row * a.ldl;
-    const float zy = as_f32(z[sl.target]);
-    MaxSum v{-INFINITY, 0.f};
-    for (int32_t j = threadIdx.x; j < a.V; j += 256) {
-      const float x = as_f32(z[j]);
-      v = join(v, MaxSum{x, x == -INFINITY ? 0.f : 1.f}, c);
-      if (x != x) v.s = x;
+    const float zy = (float)z[sl.target];
+    const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
+    if (threadIdx.x != 0) continue;
+    const float logp = row_logp(zy, c, r);
+    if (a.logp) a.logp[sl.row] = logp;
+    if (PREF) {
+      a.slot_logp[slot] = logp;
+      a.stats[slot] = float2{r.offset, r.apart ? -r.sum : r.sum};
     }
-    v = wave_join(v, c);
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = join(join(sh[0], sh[1], c), join(sh[2], sh[3], c), c);
-    __syncthreads();
-    if (v.m == INFINITY) v.s = NAN;
-    const float logp = (zy - v.m) * a.scale - logf(v.s);
-    if (MODE == kTokenPref) {
-      if (threadIdx.x == 0) {
-        a.stats[slot] = float2{v.m, v.s};
-        a.slot_logp[slot] = logp;
+  }
+}
+
+// Policy loss with the row in registers: NV vectors a thread, kE <= V <= NT NV kE.
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void policy_kernel(TokenArgs a, PolicyArgs p) {
+  constexpr int E = kE<T>;
+  __shared__ Shared sh;
+  const float c = a.scale * kLog2e;
+  const int32_t V = a.V;
+  for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
+    const Slot sl = slot_of(a, slot);
+    if (!sl.counts) {
+      skip_slot<T, NT>(a, sl);
+      if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
+      continue;
+    }
+    const T* z = (const T*)a.logits + sl.row * a.ldl;
+    const float zy = (float)z[sl.target];
+    i32x4 v[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int32_t j = (k * NT + (int32_t)threadIdx.x) * E;
+      if (k * NT * E < V) v[k] = load_vec(z + (j < V - E ? j : V - E));
+    }
+    float top = zy;  // an element of the row: read before anything of it is written
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      if (k * NT * E >= V) break;
+      float x[E];
+      unpack(v[k], T{}, x);
+#pragma unroll
+      for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
+    }
+    const float m = block_max<NT>(top, sh.max), mc = m * c;
+    RowSum r{mc, 0.f, false};
+    if (fabsf(mc) <= kMostMc) {
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        if (k * NT * E >= V) break;
+        float x[E];
+        unpack(v[k], T{}, x);
+        if ((k + 1) * NT * E <= V) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
+        } else {
+          const int32_t twice = (k * NT + (int32_t)threadIdx.x) * E - (V - E);
+#pragma unroll
+          for (int e = 0; e < E; ++e) s += e >= twice ? __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc)) : 0.f;
+        }
       }
+      r.sum = block_add<NT>(s, sh.sum);
+    } else {
+      r = row_sum_apart<T, NT>(z, V, c, m, sh.slow);
     }
-    if (threadIdx.x == 0 && a.logp) a.logp[sl.row] = logp;
-    if (MODE != kTokenPolicy) continue;
+    const float logp = row_logp(zy, c, r);
     const TokenLoss l = policy_token(p, a, slot, sl.row, logp);
-    if (threadIdx.x == 0) p.token_loss[slot] = l.loss;
-    if (!out) continue;
-    const float cs = l.c * a.scale, ce = -cs / v.s;
-    for (int32_t j = threadIdx.x; j < a.V; j += 256) {
-      float d = ce * __builtin_amdgcn_exp2f((as_f32(z[j]) - v.m) * c);
-      if (j == sl.target) d += cs;
-      out[j] = (T)d;
+    if (threadIdx.x == 0) {
+      p.token_loss[slot] = l.loss;
+      if (a.logp) a.logp[sl.row] = logp;
     }
+    if (!a.dlogits) continue;
+    T* out = (T*)a.dlogits + sl.row * a.ldd;
+    const float cs = l.c * a.scale, ce = -cs / r.sum;
+    if (r.apart) {
+      row_grad_apart<T, NT>(z, out, V, sl.target, c, r, cs, ce);
+      continue;
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int32_t j = (k * NT + (int32_t)threadIdx.x) * E;
+      if (j >= V) break;
+      const int32_t at = j < V - E ? j : V - E;
+      store_vec(out + at, grad_vec<T>(v[k], c, mc, cs, ce, sl.target - at));
+    }
+  }
+}
+
+// Policy loss of any row length, the row read twice.
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void policy_stream_kernel(TokenArgs a, PolicyArgs p) {
+  __shared__ Shared sh;
+  const float c = a.scale * kLog2e;
+  for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
+    const Slot sl = slot_of(a, slot);
+    if (!sl.counts) {
+      skip_slot<T, NT>(a, sl);
+      if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
+      continue;
+    }
+    const T* z = (const T*)a.logits + sl.row * a.ldl;
+    const float zy = (float)z[sl.target];
+    if (threadIdx.x == 0) sh.zy = zy;  // read before anything of the row is written
+    const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
+    if (NT == 64) __syncthreads();
+    const float logp = row_logp(sh.zy, c, r);
+    const TokenLoss l = policy_token(p, a, slot, sl.row, logp);
+    if (threadIdx.x == 0) {
+      p.token_loss[slot] = l.loss;
+      if (a.logp) a.logp[sl.row] = logp;
+    }
+    if (!a.dlogits) continue;
+    const float cs = l.c * a.scale, ce = -cs / r.sum;
+    row_grad_stream<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r, cs, ce);
+    __syncthreads();
   }
 }
 
@@ -188,51 +527,75 @@ __global__ __launch_bounds__(256) void pair_kernel(TokenArgs a, PrefArgs p) {
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void pref_grad_kernel(TokenArgs a, PrefArgs p) {
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void pref_grad_kernel(TokenArgs a, PrefArgs p) {
   const float c = a.scale * kLog2e;
   for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
     const Slot sl = slot_of(a, slot);
-    if (!sl.write) continue;
-    T* out = (T*)a.dlogits + sl.row * a.ldd;
     if (!sl.counts) {
-      for (int32_t j = threadIdx.x; j < a.V; j += 256) out[j] = (T)0.f;
+      if (sl.write) row_zero<T, NT>((T*)a.dlogits + sl.row * a.ldd, a.V);
       continue;
     }
-    const T* z = (const T*)a.logits + sl.row * a.ldl;
     const float2 st = a.stats[slot];
+    const RowSum r{st.x, fabsf(st.y), st.y < 0.f};
     const uint32_t i = slot / a.T;
     const float w = a.weight ? a.weight[sl.row] : 1.f;
-    const float cs = (i < p.n_pairs ? p.coef[i] : -p.coef[i - p.n_pairs]) * w * a.scale, ce = -cs / st.y;
-    for (int32_t j = threadIdx.x; j < a.V; j += 256) {
-      float d = ce * __builtin_amdgcn_exp2f((as_f32(z[j]) - st.x) * c);
-      if (j == sl.target) d += cs;
-      out[j] = (T)d;
-    }
+    const float cs = (i < p.n_pairs ? p.coef[i] : -p.coef[i - p.n_pairs]) * w * a.scale, ce = -cs / r.sum;
+    row_grad_stream<T, NT>((const T*)a.logits + sl.row * a.ldl, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r,
+                           cs, ce);
   }
 }
 
 uint32_t blocks_for(uint32_t n) { return n < (1u << 20) ? n : (1u << 20); }
 
+// Threads that sweep a row: a wave up to 4 KB of it, then 256, and 1024 from 64 KB.
+template <typename T, bool PREF>
+void launch_logp(const TokenArgs& a, hipStream_t s) {
+  const dim3 grid(blocks_for(a.n_slots));
+  const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
+  if (bytes <= 4096) hipLaunchKernelGGL((token_logp_kernel<T, 64, PREF>), grid, dim3(64), 0, s, a);
+  else if (bytes <= 65536) hipLaunchKernelGGL((token_logp_kernel<T, 256, PREF>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((token_logp_kernel<T, 1024, PREF>), grid, dim3(1024), 0, s, a);
+}
+
+template <typename T, int NT, int NV>
+void launch_policy_kernel(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL((policy_kernel<T, NT, NV>), dim3(blocks_for(a.n_slots)), dim3(NT), 0, s, a, p);
+}
+template <typename T>
+void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
+  const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
+  if (a.V < kE<T> || bytes > 262144)
+    hipLaunchKernelGGL((policy_stream_kernel<T, 1024>), dim3(blocks_for(a.n_slots)), dim3(1024), 0, s, a, p);
+  else if (bytes <= 2048) launch_policy_kernel<T, 64, 2>(a, p, s);
+  else if (bytes <= 8192) launch_policy_kernel<T, 64, 8>(a, p, s);
+  else if (bytes <= 32768) launch_policy_kernel<T, 256, 8>(a, p, s);
+  else if (bytes <= 65536) launch_policy_kernel<T, 512, 8>(a, p, s);
+  else if (bytes <= 131072) launch_policy_kernel<T, 512, 16>(a, p, s);
+  else launch_policy_kernel<T, 1024, 16>(a, p, s);
+}
+
+template <typename T>
+void launch_grad(const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
+  const dim3 grid(blocks_for(a.n_slots));
+  const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
+  if (bytes <= 4096) hipLaunchKernelGGL((pref_grad_kernel<T, 64>), grid, dim3(64), 0, s, a, p);
+  else hipLaunchKernelGGL((pref_grad_kernel<T, 256>), grid, dim3(256), 0, s, a, p);
+}
+
 }  // namespace
 
-hipError_t launch_token_rows(int mode, int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
-  const dim3 grid(blocks_for(a.n_slots)), block(256);
-#define ATTR_TOKEN(T, M) hipLaunchKernelGGL((token_kernel<T, M>), grid, block, 0, s, a, p)
-  if (dtype == 0) {
-    if (mode == kTokenLogp) ATTR_TOKEN(float, kTokenLogp);
-    else if (mode == kTokenPolicy) ATTR_TOKEN(float, kTokenPolicy);
-    else ATTR_TOKEN(float, kTokenPref);
-  } else if (dtype == 1) {
-    if (mode == kTokenLogp) ATTR_TOKEN(__bf16, kTokenLogp);
-    else if (mode == kTokenPolicy) ATTR_TOKEN(__bf16, kTokenPolicy);
-    else ATTR_TOKEN(__bf16, kTokenPref);
-  } else {
-    if (mode == kTokenLogp) ATTR_TOKEN(_Float16, kTokenLogp);
-    else if (mode == kTokenPolicy) ATTR_TOKEN(_Float16, kTokenPolicy);
-    else ATTR_TOKEN(_Float16, kTokenPref);
-  }
-#undef ATTR_TOKEN
+hipError_t launch_token_logp(int dtype, bool pref, const TokenArgs& a, hipStream_t s) {
+  if (dtype == 0) pref ? launch_logp<float, true>(a, s) : launch_logp<float, false>(a, s);
+  else if (dtype == 1) pref ? launch_logp<__bf16, true>(a, s) : launch_logp<__bf16, false>(a, s);
+  else pref ? launch_logp<_Float16, true>(a, s) : launch_logp<_Float16, false>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_policy_rows(int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
+  if (dtype == 0) launch_policy<float>(a, p, s);
+  else if (dtype == 1) launch_policy<__bf16>(a, p, s);
+  else launch_policy<_Float16>(a, p, s);
   return hipGetLastError();
 }
 
@@ -247,10 +610,9 @@ hipError_t launch_pairs(const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
 }
 
 hipError_t launch_pref_grad(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
-  const dim3 grid(blocks_for(a.n_slots)), block(256);
-  if (dtype == 0) hipLaunchKernelGGL(pref_grad_kernel<float>, grid, block, 0, s, a, p);
-  else if (dtype == 1) hipLaunchKernelGGL(pref_grad_kernel<__bf16>, grid, block, 0, s, a, p);
-  else hipLaunchKernelGGL(pref_grad_kernel<_Float16>, grid, block, 0, s, a, p);
+  if (dtype == 0) launch_grad<float>(a, p, s);
+  else if (dtype == 1) launch_grad<__bf16>(a, p, s);
+  else launch_grad<_Float16>(a, p, s);
   return hipGetLastError();
 }
 
