@@ -205,6 +205,7 @@ struct TokenArgs {
   float* slot_logp;            // per slot (preference loss)
   int64_t n_rows, ldl, ldd;
   uint32_t n_slots, T;         // slot = example * T + token
+  uint32_t slot0;              // of a launch
   int32_t V;
   float scale;
 };

@@ -12,9 +12,8 @@
 // trees.
 //
 // All of it is bound by HBM: a row is read once, with 16-byte loads that need no
-// alignment beyond the element's (an odd vocabulary's rows start anywhere).  The
-// last vector of a row is moved back to end with it, and the sum leaves out what
-// it then holds twice.
+// alignment beyond the element's (an odd vocabulary's rows start anywhere).  What
+// is left of a row after its whole vectors goes one element a thread.
 #include "common.h"
 #include "kernels.h"
 
@@ -68,6 +67,11 @@ struct Loose<__bf16> { typedef i32x4 vec __attribute__((aligned(2))); };
 template <>
 struct Loose<_Float16> { typedef i32x4 vec __attribute__((aligned(2))); };
 
+// a vector of -inf: it adds nothing to a maximum or a sum
+__device__ inline i32x4 no_vec(float) { return i32x4{(int)0xff800000, (int)0xff800000, (int)0xff800000, (int)0xff800000}; }
+__device__ inline i32x4 no_vec(__bf16) { return i32x4{(int)0xff80ff80, (int)0xff80ff80, (int)0xff80ff80, (int)0xff80ff80}; }
+__device__ inline i32x4 no_vec(_Float16) { return i32x4{(int)0xfc00fc00, (int)0xfc00fc00, (int)0xfc00fc00, (int)0xfc00fc00}; }
+
 template <typename T>
 __device__ inline i32x4 load_vec(const T* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const typename Loose<T>::vec*>(p));
@@ -93,6 +97,17 @@ __device__ inline void unpack(i32x4 v, _Float16, float (&x)[8]) {
   const f16x8 h = __builtin_bit_cast(f16x8, v);
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
+}
+
+// Makes the compiler forget what it knows of a value: without it the unpacked
+// elements of one stage are kept for the next (twice the registers for 16-bit
+// types), and the lane masks of the loads for the stores.
+__device__ inline void forget(i32x4& v) { asm volatile("" : "+v"(v)); }
+__device__ inline void forget(int32_t& v) { asm volatile("" : "+v"(v)); }
+template <int N>
+__device__ inline void forget(i32x4 (&v)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) forget(v[k]);
 }
 
 __device__ inline i32x4 pack(const float (&x)[4], float) {
@@ -206,12 +221,10 @@ __device__ void row_grad_apart(const T* z, T* out, int32_t V, int32_t y, float c
 
 template <typename T, int NT>
 __device__ inline void row_zero(T* out, int32_t V) {
-  if (V < kE<T>) {
-    if ((int32_t)threadIdx.x < V) out[threadIdx.x] = (T)0.f;
-    return;
-  }
-  for (int32_t j = threadIdx.x * kE<T>; j < V; j += NT * kE<T>)
-    store_vec(out + (j < V - kE<T> ? j : V - kE<T>), i32x4{0, 0, 0, 0});
+  constexpr int E = kE<T>;
+  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
+  for (int32_t j = threadIdx.x * E; j < whole; j += NT * E) store_vec(out + j, i32x4{0, 0, 0, 0});
+  if (at < V) out[at] = (T)0.f;
 }
 
 // One vector's gradient, from its elements.
@@ -228,50 +241,40 @@ __device__ inline i32x4 grad_vec(i32x4 v, float c, float offset, float cs, float
   return pack(x, T{});
 }
 
+template <typename T>
+__device__ inline T grad_one(T z, float c, float offset, float cs, float ce, bool y) {
+  const float d = ce * __builtin_amdgcn_exp2f(fmaf((float)z, c, -offset));
+  return (T)(y ? d + cs : d);
+}
+
 // A row's maximum and sum in one sweep: per thread a running maximum (not below
 // -2^20 / c, so that nothing but -inf needs no case of its own) and a sum that is
 // rescaled when it grows, U vectors at a time.
 template <typename T, int NT>
 __device__ RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& sh) {
   constexpr int E = kE<T>, U = 4;
-  float top = -INFINITY, mc = -kMostMc, s = 0.f;
-  if (V >= E) {
-    for (int32_t j0 = threadIdx.x * E; j0 < V; j0 += NT * E * U) {
-      i32x4 v[U];
+  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
+  float top = at < V ? (float)z[at] : -INFINITY;
+  float mc = fmaxf(top * c, -kMostMc), s = __builtin_amdgcn_exp2f(fmaf(top, c, -mc));
+  for (int32_t j0 = threadIdx.x * E; j0 < whole; j0 += NT * E * U) {
+    i32x4 v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int32_t j = j0 + u * NT * E;
-        if (j < V) v[u] = load_vec(z + (j < V - E ? j : V - E));
+    for (int u = 0; u < U; ++u) v[u] = j0 + u * NT * E < whole ? load_vec(z + j0 + u * NT * E) : no_vec(T{});
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[E];
+      unpack(v[u], T{}, x);
+      float m = x[0];
+#pragma unroll
+      for (int e = 1; e < E; ++e) m = fmaxf(m, x[e]);
+      top = fmaxf(top, m);
+      if (m * c > mc) {
+        s *= __builtin_amdgcn_exp2f(mc - m * c);
+        mc = m * c;
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int32_t j = j0 + u * NT * E;
-        if (j >= V) continue;
-        float x[E];
-        unpack(v[u], T{}, x);
-        float m = x[0];
-#pragma unroll
-        for (int e = 1; e < E; ++e) m = fmaxf(m, x[e]);
-        top = fmaxf(top, m);
-        if (m * c > mc) {
-          s *= __builtin_amdgcn_exp2f(mc - m * c);
-          mc = m * c;
-        }
-        const int32_t twice = j - (V - E);
-        if (twice <= 0) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e) s += e >= twice ? __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc)) : 0.f;
-        }
-      }
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
     }
-  } else if ((int32_t)threadIdx.x < V) {
-    top = (float)z[threadIdx.x];
-    mc = fmaxf(top * c, mc);
-    s = __builtin_amdgcn_exp2f(fmaf(top, c, -mc));
-    if (top != top) s = top;
   }
   const float m = block_max<NT>(top, sh.max);
   if (!(fabsf(m * c) <= kMostMc)) return row_sum_apart<T, NT>(z, V, c, m, sh.slow);
@@ -281,33 +284,23 @@ __device__ RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& sh) {
 }
 
 // The gradient of one row, read a second time.  A thread reads and writes its own
-// elements only (the two may be one buffer), so the last vector, if it is not
-// whole, goes element by element.
+// elements only: the two may be one buffer.
 template <typename T, int NT>
 __device__ void row_grad_stream(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
                                 float ce) {
   constexpr int E = kE<T>, U = 4;
   if (r.apart) return row_grad_apart<T, NT>(z, out, V, y, c, r, cs, ce);
-  for (int32_t j0 = threadIdx.x * E; j0 < V; j0 += NT * E * U) {
+  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
+  if (at < V) out[at] = grad_one(z[at], c, r.offset, cs, ce, at == y);
+  for (int32_t j0 = threadIdx.x * E; j0 < whole; j0 += NT * E * U) {
     i32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int32_t j = j0 + u * NT * E;
-      if (j + E <= V) v[u] = load_vec(z + j);
-    }
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * NT * E < whole) v[u] = load_vec(z + j0 + u * NT * E);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int32_t j = j0 + u * NT * E;
-      if (j + E <= V) {
-        store_vec(out + j, grad_vec<T>(v[u], c, r.offset, cs, ce, y - j));
-      } else {
-#pragma unroll 1
-        for (int32_t k = j; k < V; ++k) {
-          float d = ce * __builtin_amdgcn_exp2f(fmaf((float)z[k], c, -r.offset));
-          if (k == y) d += cs;
-          out[k] = (T)d;
-        }
-      }
+      if (j < whole) store_vec(out + j, grad_vec<T>(v[u], c, r.offset, cs, ce, y - j));
     }
   }
 }
@@ -336,6 +329,17 @@ __device__ inline TokenLoss policy_token(const PolicyArgs& p, const TokenArgs& a
   return {w * loss, w * c};
 }
 
+// Writes a token's loss and log-probability; returns the factor s c of its gradient.
+__device__ inline float policy_outputs(const TokenArgs& a, const PolicyArgs& p, uint32_t slot, int64_t row,
+                                       float logp) {
+  const TokenLoss l = policy_token(p, a, slot, row, logp);
+  if (threadIdx.x == 0) {
+    p.token_loss[slot] = l.loss;
+    if (a.logp) a.logp[row] = logp;
+  }
+  return l.c * a.scale;
+}
+
 // Outputs of a slot that does not count.
 template <typename T, int NT>
 __device__ inline void skip_slot(const TokenArgs& a, const Slot& sl) {
@@ -349,98 +353,85 @@ template <typename T, int NT, bool PREF>
 __global__ __launch_bounds__(NT) void token_logp_kernel(TokenArgs a) {
   __shared__ Shared sh;
   const float c = a.scale * kLog2e;
-  for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
-    const Slot sl = slot_of(a, slot);
-    if (!sl.counts) {
-      if (threadIdx.x == 0 && sl.write && a.logp) a.logp[sl.row] = 0.f;
-      continue;
-    }
-    const T* z = (const T*)a.logits + sl.row * a.ldl;
-    const float zy = (float)z[sl.target];
-    const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
-    if (threadIdx.x != 0) continue;
-    const float logp = row_logp(zy, c, r);
-    if (a.logp) a.logp[sl.row] = logp;
-    if (PREF) {
-      a.slot_logp[slot] = logp;
-      a.stats[slot] = float2{r.offset, r.apart ? -r.sum : r.sum};
-    }
+  const uint32_t slot = a.slot0 + blockIdx.x;
+  const Slot sl = slot_of(a, slot);
+  if (!sl.counts) {
+    if (threadIdx.x == 0 && sl.write && a.logp) a.logp[sl.row] = 0.f;
+    return;
+  }
+  const T* z = (const T*)a.logits + sl.row * a.ldl;
+  const float zy = (float)z[sl.target];
+  const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
+  if (threadIdx.x != 0) return;
+  const float logp = row_logp(zy, c, r);
+  if (a.logp) a.logp[sl.row] = logp;
+  if (PREF) {
+    a.slot_logp[slot] = logp;
+    a.stats[slot] = float2{r.offset, r.apart ? -r.sum : r.sum};
   }
 }
 
-// Policy loss with the row in registers: NV vectors a thread, kE <= V <= NT NV kE.
+// Policy loss with the row in registers: NV vectors a thread, V <= NT NV kE.
 template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) void policy_kernel(TokenArgs a, PolicyArgs p) {
+__global__ __launch_bounds__(NT, NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
   constexpr int E = kE<T>;
   __shared__ Shared sh;
   const float c = a.scale * kLog2e;
   const int32_t V = a.V;
-  for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
-    const Slot sl = slot_of(a, slot);
-    if (!sl.counts) {
-      skip_slot<T, NT>(a, sl);
-      if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
-      continue;
-    }
-    const T* z = (const T*)a.logits + sl.row * a.ldl;
-    const float zy = (float)z[sl.target];
-    i32x4 v[NV];
+  const uint32_t slot = a.slot0 + blockIdx.x;
+  const Slot sl = slot_of(a, slot);
+  if (!sl.counts) {
+    skip_slot<T, NT>(a, sl);
+    if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
+    return;
+  }
+  const T* z = (const T*)a.logits + sl.row * a.ldl;
+  const float zy = (float)z[sl.target];
+  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
+  const T rest = at < V ? z[at] : (T)-INFINITY;
+  i32x4 v[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int32_t j = (k * NT + (int32_t)threadIdx.x) * E;
-      if (k * NT * E < V) v[k] = load_vec(z + (j < V - E ? j : V - E));
-    }
-    float top = zy;  // an element of the row: read before anything of it is written
+  for (int k = 0; k < NV; ++k) {
+    const int32_t j = (k * NT + (int32_t)threadIdx.x) * E;
+    v[k] = j < whole ? load_vec(z + j) : no_vec(T{});
+  }
+  float top = fmaxf(zy, (float)rest);  // zy, an element of the row, is read before anything of it is written
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      if (k * NT * E >= V) break;
-      float x[E];
-      unpack(v[k], T{}, x);
+  for (int k = 0; k < NV; ++k) {
+    float x[E];
+    unpack(v[k], T{}, x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
-    }
-    const float m = block_max<NT>(top, sh.max), mc = m * c;
-    RowSum r{mc, 0.f, false};
-    if (fabsf(mc) <= kMostMc) {
-      float s = 0.f;
+    for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
+  }
+  const float m = block_max<NT>(top, sh.max), mc = m * c;
+  if (!(fabsf(mc) <= kMostMc)) {
+    const RowSum r = row_sum_apart<T, NT>(z, V, c, m, sh.slow);
+    const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r));
+    if (a.dlogits) row_grad_apart<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, V, sl.target, c, r, g, -g / r.sum);
+    return;
+  }
+  forget(v);
+  float s = __builtin_amdgcn_exp2f(fmaf((float)rest, c, -mc));
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        if (k * NT * E >= V) break;
-        float x[E];
-        unpack(v[k], T{}, x);
-        if ((k + 1) * NT * E <= V) {
+  for (int k = 0; k < NV; ++k) {
+    float x[E];
+    unpack(v[k], T{}, x);
 #pragma unroll
-          for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
-        } else {
-          const int32_t twice = (k * NT + (int32_t)threadIdx.x) * E - (V - E);
+    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
+  }
+  const RowSum r{mc, block_add<NT>(s, sh.sum), false};
+  const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r));
+  if (!a.dlogits) return;
+  T* out = (T*)a.dlogits + sl.row * a.ldd;
+  const float ce = -g / r.sum;
+  forget(v);
+  int32_t j0 = (int32_t)threadIdx.x * E;
+  forget(j0);
+  if (at < V) out[at] = grad_one(rest, c, mc, g, ce, at == sl.target);
 #pragma unroll
-          for (int e = 0; e < E; ++e) s += e >= twice ? __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc)) : 0.f;
-        }
-      }
-      r.sum = block_add<NT>(s, sh.sum);
-    } else {
-      r = row_sum_apart<T, NT>(z, V, c, m, sh.slow);
-    }
-    const float logp = row_logp(zy, c, r);
-    const TokenLoss l = policy_token(p, a, slot, sl.row, logp);
-    if (threadIdx.x == 0) {
-      p.token_loss[slot] = l.loss;
-      if (a.logp) a.logp[sl.row] = logp;
-    }
-    if (!a.dlogits) continue;
-    T* out = (T*)a.dlogits + sl.row * a.ldd;
-    const float cs = l.c * a.scale, ce = -cs / r.sum;
-    if (r.apart) {
-      row_grad_apart<T, NT>(z, out, V, sl.target, c, r, cs, ce);
-      continue;
-    }
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int32_t j = (k * NT + (int32_t)threadIdx.x) * E;
-      if (j >= V) break;
-      const int32_t at = j < V - E ? j : V - E;
-      store_vec(out + at, grad_vec<T>(v[k], c, mc, cs, ce, sl.target - at));
-    }
+  for (int k = 0; k < NV; ++k) {
+    const int32_t j = j0 + k * NT * E;
+    if (j < whole) store_vec(out + j, grad_vec<T>(v[k], c, mc, g, ce, sl.target - j));
   }
 }
 
@@ -449,29 +440,21 @@ template <typename T, int NT>
 __global__ __launch_bounds__(NT) void policy_stream_kernel(TokenArgs a, PolicyArgs p) {
   __shared__ Shared sh;
   const float c = a.scale * kLog2e;
-  for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
-    const Slot sl = slot_of(a, slot);
-    if (!sl.counts) {
-      skip_slot<T, NT>(a, sl);
-      if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
-      continue;
-    }
-    const T* z = (const T*)a.logits + sl.row * a.ldl;
-    const float zy = (float)z[sl.target];
-    if (threadIdx.x == 0) sh.zy = zy;  // read before anything of the row is written
-    const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
-    if (NT == 64) __syncthreads();
-    const float logp = row_logp(sh.zy, c, r);
-    const TokenLoss l = policy_token(p, a, slot, sl.row, logp);
-    if (threadIdx.x == 0) {
-      p.token_loss[slot] = l.loss;
-      if (a.logp) a.logp[sl.row] = logp;
-    }
-    if (!a.dlogits) continue;
-    const float cs = l.c * a.scale, ce = -cs / r.sum;
-    row_grad_stream<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r, cs, ce);
-    __syncthreads();
+  const uint32_t slot = a.slot0 + blockIdx.x;
+  const Slot sl = slot_of(a, slot);
+  if (!sl.counts) {
+    skip_slot<T, NT>(a, sl);
+    if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
+    return;
   }
+  const T* z = (const T*)a.logits + sl.row * a.ldl;
+  const float zy = (float)z[sl.target];
+  if (threadIdx.x == 0) sh.zy = zy;  // read before anything of the row is written
+  const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
+  if (NT == 64) __syncthreads();
+  const float g = policy_outputs(a, p, slot, sl.row, row_logp(sh.zy, c, r));
+  if (a.dlogits)
+    row_grad_stream<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r, g, -g / r.sum);
 }
 
 __device__ inline double block_sum(double v, double* sh) {
@@ -530,57 +513,59 @@ __global__ __launch_bounds__(256) void pair_kernel(TokenArgs a, PrefArgs p) {
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void pref_grad_kernel(TokenArgs a, PrefArgs p) {
   const float c = a.scale * kLog2e;
-  for (uint32_t slot = blockIdx.x; slot < a.n_slots; slot += gridDim.x) {
-    const Slot sl = slot_of(a, slot);
-    if (!sl.counts) {
-      if (sl.write) row_zero<T, NT>((T*)a.dlogits + sl.row * a.ldd, a.V);
-      continue;
-    }
-    const float2 st = a.stats[slot];
-    const RowSum r{st.x, fabsf(st.y), st.y < 0.f};
-    const uint32_t i = slot / a.T;
-    const float w = a.weight ? a.weight[sl.row] : 1.f;
-    const float cs = (i < p.n_pairs ? p.coef[i] : -p.coef[i - p.n_pairs]) * w * a.scale, ce = -cs / r.sum;
-    row_grad_stream<T, NT>((const T*)a.logits + sl.row * a.ldl, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r,
-                           cs, ce);
+  const uint32_t slot = a.slot0 + blockIdx.x;
+  const Slot sl = slot_of(a, slot);
+  if (!sl.counts) {
+    if (sl.write) row_zero<T, NT>((T*)a.dlogits + sl.row * a.ldd, a.V);
+    return;
   }
+  const float2 st = a.stats[slot];
+  const RowSum r{st.x, fabsf(st.y), st.y < 0.f};
+  const uint32_t i = slot / a.T;
+  const float w = a.weight ? a.weight[sl.row] : 1.f;
+  const float cs = (i < p.n_pairs ? p.coef[i] : -p.coef[i - p.n_pairs]) * w * a.scale, ce = -cs / r.sum;
+  row_grad_stream<T, NT>((const T*)a.logits + sl.row * a.ldl, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r,
+                         cs, ce);
 }
 
 uint32_t blocks_for(uint32_t n) { return n < (1u << 20) ? n : (1u << 20); }
 
+// One workgroup a slot, in launches of fewer than 2^32 threads.
+template <typename... K, typename... Args>
+void launch_slots(void (*kernel)(TokenArgs, K...), int threads, TokenArgs a, hipStream_t s, Args... args) {
+  constexpr uint32_t kMost = 1u << 21;
+  for (a.slot0 = 0; a.slot0 < a.n_slots; a.slot0 += kMost) {
+    const uint32_t n = a.n_slots - a.slot0;
+    hipLaunchKernelGGL(kernel, dim3(n < kMost ? n : kMost), dim3(threads), 0, s, a, args...);
+  }
+}
+
 // Threads that sweep a row: a wave up to 4 KB of it, then 256, and 1024 from 64 KB.
 template <typename T, bool PREF>
 void launch_logp(const TokenArgs& a, hipStream_t s) {
-  const dim3 grid(blocks_for(a.n_slots));
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (bytes <= 4096) hipLaunchKernelGGL((token_logp_kernel<T, 64, PREF>), grid, dim3(64), 0, s, a);
-  else if (bytes <= 65536) hipLaunchKernelGGL((token_logp_kernel<T, 256, PREF>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((token_logp_kernel<T, 1024, PREF>), grid, dim3(1024), 0, s, a);
+  if (bytes <= 4096) launch_slots(token_logp_kernel<T, 64, PREF>, 64, a, s);
+  else if (bytes <= 65536) launch_slots(token_logp_kernel<T, 256, PREF>, 256, a, s);
+  else launch_slots(token_logp_kernel<T, 1024, PREF>, 1024, a, s);
 }
 
-template <typename T, int NT, int NV>
-void launch_policy_kernel(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
-  hipLaunchKernelGGL((policy_kernel<T, NT, NV>), dim3(blocks_for(a.n_slots)), dim3(NT), 0, s, a, p);
-}
 template <typename T>
 void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (a.V < kE<T> || bytes > 262144)
-    hipLaunchKernelGGL((policy_stream_kernel<T, 1024>), dim3(blocks_for(a.n_slots)), dim3(1024), 0, s, a, p);
-  else if (bytes <= 2048) launch_policy_kernel<T, 64, 2>(a, p, s);
-  else if (bytes <= 8192) launch_policy_kernel<T, 64, 8>(a, p, s);
-  else if (bytes <= 32768) launch_policy_kernel<T, 256, 8>(a, p, s);
-  else if (bytes <= 65536) launch_policy_kernel<T, 512, 8>(a, p, s);
-  else if (bytes <= 131072) launch_policy_kernel<T, 512, 16>(a, p, s);
-  else launch_policy_kernel<T, 1024, 16>(a, p, s);
+  if (bytes <= 2048) launch_slots(policy_kernel<T, 64, 2>, 64, a, s, p);
+  else if (bytes <= 8192) launch_slots(policy_kernel<T, 64, 8>, 64, a, s, p);
+  else if (bytes <= 32768) launch_slots(policy_kernel<T, 256, 8>, 256, a, s, p);
+  else if (bytes <= 65536) launch_slots(policy_kernel<T, 512, 8>, 512, a, s, p);
+  else if (bytes <= 131072) launch_slots(policy_kernel<T, 512, 16>, 512, a, s, p);
+  else if (bytes <= 262144) launch_slots(policy_kernel<T, 1024, 16>, 1024, a, s, p);
+  else launch_slots(policy_stream_kernel<T, 1024>, 1024, a, s, p);
 }
 
 template <typename T>
 void launch_grad(const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
-  const dim3 grid(blocks_for(a.n_slots));
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (bytes <= 4096) hipLaunchKernelGGL((pref_grad_kernel<T, 64>), grid, dim3(64), 0, s, a, p);
-  else hipLaunchKernelGGL((pref_grad_kernel<T, 256>), grid, dim3(256), 0, s, a, p);
+  if (bytes <= 4096) launch_slots(pref_grad_kernel<T, 64>, 64, a, s, p);
+  else launch_slots(pref_grad_kernel<T, 256>, 256, a, s, p);
 }
 
 }  // namespace
