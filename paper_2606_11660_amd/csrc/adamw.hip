@@ -1,58 +1,109 @@
 // One AdamW step over many tensors (attr_adamw_step).
 //
-// The descriptors travel in kernel arguments; a workgroup finds its tensor by
-// its first chunk and takes one chunk of it.  Arithmetic is fp32 and never
-// contracted into fused multiply-adds: every element's result is the same
-// however the tensors are split over workgroups.
+// Every element is read once and written once: HBM-bound (26 to 28 bytes an
+// element with 32-bit states, 12 to 16 with 8-bit ones).  The descriptors travel in
+// kernel arguments; a workgroup finds its tensor by its first chunk and takes one
+// chunk of it, a wave U runs of 256 elements, four elements a lane, all loads in
+// flight before the first is used.  A run is a block of the 8-bit states: its
+// largest magnitude is one reduction over the wave's lanes, without LDS or barriers.
+// Loads and stores need no alignment beyond the element's.
+//
+// Arithmetic is fp32 and never contracted into fused multiply-adds: every
+// element's result is the same however the tensors are split over workgroups.
 #include "common.h"
 #include "kernels.h"
+
+#include <type_traits>
 
 #pragma clang fp contract(off)
 
 namespace attr {
 namespace {
 
-constexpr int kQuantBlock = 256;       // elements that share a scale of the 8-bit states
+constexpr int kQuantBlock = 256;       // elements that share a scale of the 8-bit states: a wave's run
 constexpr float kE4M3Max = 448.f;
 constexpr float kE4M3Least = 0.001953125f;  // 2^-9, the smallest positive value
 constexpr float kAmaxLeast = 0x1p-100f;     // below it 448 / amax nears fp32's range
+
+constexpr int kRuns = 4;               // runs of a wave
+static_assert(kAdamwChunk == 4 * kRuns * kQuantBlock, "a workgroup of four waves");
+
+// four elements at any element's address
+template <typename T>
+struct Four;
+template <>
+struct Four<float> { typedef f32x4 vec __attribute__((aligned(4))); };
+template <>
+struct Four<__bf16> {
+  typedef __bf16 plain __attribute__((ext_vector_type(4)));
+  typedef plain vec __attribute__((aligned(2)));
+};
+template <>
+struct Four<_Float16> { typedef f16x4 vec __attribute__((aligned(2))); };
+template <>
+struct Four<uint8_t> {
+  typedef uint8_t plain __attribute__((ext_vector_type(4)));
+  typedef plain vec __attribute__((aligned(1)));
+};
+
+// The first `in` of four elements (4: all of them, in one access); 0 for the rest.
+template <typename T>
+__device__ inline void load4(const T* p, int in, T (&x)[4]) {
+  if (in >= 4) {
+    const auto v = __builtin_nontemporal_load(reinterpret_cast<const typename Four<T>::vec*>(p));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = v[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = e < in ? p[e] : (T)0;
+  }
+}
+template <typename T>
+__device__ inline void store4(T* p, int in, const T (&x)[4]) {
+  if (in >= 4) {
+    typename Four<T>::vec v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = x[e];
+    __builtin_nontemporal_store(v, reinterpret_cast<typename Four<T>::vec*>(p));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < in) p[e] = x[e];
+  }
+}
+
+// largest of a wave's values: magnitudes as their bits, whose order keeps
+// infinities and NaN above every finite value
+template <int CTRL, int ROWS>
+__device__ inline uint32_t dpp_max(uint32_t x) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+  return o > x ? o : x;
+}
+__device__ inline float wave_amax(const float (&x)[4]) {
+  uint32_t b = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t o = __builtin_bit_cast(uint32_t, x[e]) & 0x7fffffffu;
+    b = o > b ? o : b;
+  }
+  b = dpp_max<0x111, 0xf>(b);
+  b = dpp_max<0x112, 0xf>(b);
+  b = dpp_max<0x114, 0xf>(b);
+  b = dpp_max<0x118, 0xf>(b);
+  b = dpp_max<0x142, 0xa>(b);
+  b = dpp_max<0x143, 0xc>(b);
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)b, 63));
+}
 
 __device__ inline float e4m3_value(uint8_t code) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0); }
 __device__ inline uint8_t e4m3_code(float x) {
   return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
 }
 
-struct Step {
-  float m, v, x;
-};
-__device__ inline Step adamw_element(const AdamwArgs& a, float lr, float lr_wd, float x, float g, float m,
-                                     float v) {
-  m = m * a.beta1 + g * a.one_beta1;
-  v = v * a.beta2 + (g * g) * a.one_beta2;
-  const float root = sqrtf(v * a.corr2 + a.eps_root) + a.eps;
-  x = x - x * lr_wd - (m * a.corr1) / root * lr;
-  return {m, v, x};
-}
-
-// largest magnitude of a 256-thread workgroup's values, as fp32 bits: integer
-// order keeps infinities and NaN above every finite value
-__device__ inline uint32_t block_amax(float x, uint32_t* sh) {
-  uint32_t b = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)b, off, kWave);
-    b = o > b ? o : b;
-  }
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = b;
-  __syncthreads();
-  const uint32_t p = sh[0] > sh[1] ? sh[0] : sh[1], q = sh[2] > sh[3] ? sh[2] : sh[3];
-  __syncthreads();
-  return p > q ? p : q;
-}
-
-template <typename P, typename G, bool EIGHT>
+template <typename P, typename G, bool EIGHT, bool MASTER>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
-  __shared__ uint32_t sh[4];
+  typedef typename std::conditional<EIGHT, uint8_t, float>::type S;
+  typedef typename std::conditional<MASTER, float, P>::type W;
   int lo = 0, hi = a.n - 1;  // the last tensor whose first chunk is not past this workgroup
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -62,69 +113,109 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
   const AdamwEntry& t = a.e[lo];
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const float lr = t.lr, lr_wd = t.lr_wd;
-  const int64_t i0 = (int64_t)(blockIdx.x - t.chunk0) * kAdamwChunk;
-  for (int64_t b = i0; b < t.n && b < i0 + kAdamwChunk; b += 256) {
-    const int64_t i = b + threadIdx.x;
-    const bool in = i < t.n;
-    float x = 0.f, g = 0.f, m = 0.f, v = 0.f;
-    if (in) {
-      x = t.master ? t.master[i] : (float)((const P*)t.p)[i];
-      g = (float)((const G*)t.g)[i] * gs;
-      if (EIGHT) {
-        m = e4m3_value(((const uint8_t*)t.m)[i]) * t.m_scale[b / kQuantBlock];
-        v = e4m3_value(((const uint8_t*)t.v)[i]) * t.v_scale[b / kQuantBlock];
-        v = v * v;
-      } else {
-        m = ((const float*)t.m)[i];
-        v = ((const float*)t.v)[i];
-      }
-    }
-    const Step r = adamw_element(a, lr, lr_wd, x, g, m, v);
-    if (in) {
-      if (t.master) t.master[i] = r.x;
-      ((P*)t.p)[i] = (P)r.x;
-    }
+  const int lane = threadIdx.x & 63;
+  const int64_t run0 = ((int64_t)(blockIdx.x - t.chunk0) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRuns;
+  W* const wt = MASTER ? (W*)t.master : (W*)t.p;
+  W x[kRuns][4];
+  G g[kRuns][4];
+  S m[kRuns][4], v[kRuns][4];
+  float ms[kRuns], vs[kRuns];
+#pragma unroll
+  for (int u = 0; u < kRuns; ++u) {
+    const int64_t b = (run0 + u) * kQuantBlock, i = b + lane * 4;
+    const int in = t.n - i >= 4 ? 4 : (int)(t.n - i);
+    if (b >= t.n) break;
+    load4(wt + i, in, x[u]);
+    load4((const G*)t.g + i, in, g[u]);
+    load4((const S*)t.m + i, in, m[u]);
+    load4((const S*)t.v + i, in, v[u]);
     if (EIGHT) {
-      const float root = sqrtf(r.v);
-      float am = __builtin_bit_cast(float, block_amax(in ? r.m : 0.f, sh));
-      float av = __builtin_bit_cast(float, block_amax(in ? root : 0.f, sh));
+      ms[u] = t.m_scale[run0 + u];
+      vs[u] = t.v_scale[run0 + u];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kRuns; ++u) {
+    const int64_t b = (run0 + u) * kQuantBlock, i = b + lane * 4;
+    const int in = t.n - i >= 4 ? 4 : (int)(t.n - i);
+    if (b >= t.n) break;
+    float nm[4], nv[4];
+    W nx[4];
+    P np[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float gr = (float)g[u][e] * gs, w = (float)x[u][e];
+      float om, ov;
+      if constexpr (EIGHT) {
+        om = e4m3_value(m[u][e]) * ms[u];
+        ov = e4m3_value(v[u][e]) * vs[u];
+        ov = ov * ov;
+      } else {
+        om = m[u][e];
+        ov = v[u][e];
+      }
+      nm[e] = om * a.beta1 + gr * a.one_beta1;
+      nv[e] = ov * a.beta2 + (gr * gr) * a.one_beta2;
+      const float root = sqrtf(nv[e] * a.corr2 + a.eps_root) + a.eps;
+      const float r = w - w * lr_wd - (nm[e] * a.corr1) / root * lr;
+      nx[e] = (W)r;
+      np[e] = (P)r;
+    }
+    store4(wt + i, in, nx);
+    if (MASTER) store4((P*)t.p + i, in, np);
+    if constexpr (EIGHT) {
+      float root[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        root[e] = e < in ? sqrtf(nv[e]) : 0.f;
+        nm[e] = e < in ? nm[e] : 0.f;
+      }
+      float am = wave_amax(nm), av = wave_amax(root);
       am = am < kAmaxLeast ? kAmaxLeast : am;
       av = av < kAmaxLeast ? kAmaxLeast : av;
-      if (in) {
-        ((uint8_t*)t.m)[i] = e4m3_code(r.m * (1.f / am * kE4M3Max));
-        const float q = root * (1.f / av * kE4M3Max);
-        ((uint8_t*)t.v)[i] = e4m3_code(q > 0.f && q < kE4M3Least ? kE4M3Least : q);
+      const float fm = 1.f / am * kE4M3Max, fv = 1.f / av * kE4M3Max;
+      uint8_t qm[4], qv[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        qm[e] = e4m3_code(nm[e] * fm);
+        const float q = root[e] * fv;
+        qv[e] = e4m3_code(q > 0.f && q < kE4M3Least ? kE4M3Least : q);
       }
-      if (threadIdx.x == 0) {
-        t.m_scale[b / kQuantBlock] = am < INFINITY ? am * (1.f / kE4M3Max) : NAN;
-        t.v_scale[b / kQuantBlock] = av < INFINITY ? av * (1.f / kE4M3Max) : NAN;
+      store4((S*)t.m + i, in, qm);
+      store4((S*)t.v + i, in, qv);
+      if (lane == 0) {
+        t.m_scale[run0 + u] = am < INFINITY ? am * (1.f / kE4M3Max) : NAN;
+        t.v_scale[run0 + u] = av < INFINITY ? av * (1.f / kE4M3Max) : NAN;
       }
-    } else if (in) {
-      ((float*)t.m)[i] = r.m;
-      ((float*)t.v)[i] = r.v;
+    } else {
+      store4((S*)t.m + i, in, nm);
+      store4((S*)t.v + i, in, nv);
     }
   }
 }
 
 template <typename P, typename G>
-void launch(bool eight, uint32_t blocks, const AdamwArgs& a, hipStream_t s) {
-  if (eight) hipLaunchKernelGGL((adamw_kernel<P, G, true>), dim3(blocks), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((adamw_kernel<P, G, false>), dim3(blocks), dim3(256), 0, s, a);
+void launch(bool eight, bool master, uint32_t blocks, const AdamwArgs& a, hipStream_t s) {
+  const dim3 grid(blocks), block(256);
+  if (eight && master) hipLaunchKernelGGL((adamw_kernel<P, G, true, true>), grid, block, 0, s, a);
+  else if (eight) hipLaunchKernelGGL((adamw_kernel<P, G, true, false>), grid, block, 0, s, a);
+  else if (master) hipLaunchKernelGGL((adamw_kernel<P, G, false, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((adamw_kernel<P, G, false, false>), grid, block, 0, s, a);
 }
 template <typename P>
-void launch_g(int g_dtype, bool eight, uint32_t blocks, const AdamwArgs& a, hipStream_t s) {
-  if (g_dtype == 0) launch<P, float>(eight, blocks, a, s);
-  else if (g_dtype == 1) launch<P, __bf16>(eight, blocks, a, s);
-  else launch<P, _Float16>(eight, blocks, a, s);
+void launch_g(int g_dtype, bool eight, bool master, uint32_t blocks, const AdamwArgs& a, hipStream_t s) {
+  if (g_dtype == 0) launch<P, float>(eight, master, blocks, a, s);
+  else if (g_dtype == 1) launch<P, __bf16>(eight, master, blocks, a, s);
+  else launch<P, _Float16>(eight, master, blocks, a, s);
 }
 
 }  // namespace
 
-hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, uint32_t blocks, const AdamwArgs& a,
+hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, bool master, uint32_t blocks, const AdamwArgs& a,
                         hipStream_t s) {
-  if (p_dtype == 0) launch_g<float>(g_dtype, eight, blocks, a, s);
-  else if (p_dtype == 1) launch_g<__bf16>(g_dtype, eight, blocks, a, s);
-  else launch_g<_Float16>(g_dtype, eight, blocks, a, s);
+  if (p_dtype == 0) launch_g<float>(g_dtype, eight, master, blocks, a, s);
+  else if (p_dtype == 1) launch_g<__bf16>(g_dtype, eight, master, blocks, a, s);
+  else launch_g<_Float16>(g_dtype, eight, master, blocks, a, s);
   return hipGetLastError();
 }
 

@@ -889,9 +889,10 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
     a.eps_root = (float)eps_root;
     hipStream_t s = static_cast<hipStream_t>(stream);
     uint32_t blocks = 0;
+    bool master = false;  // of the launch being filled
     auto flush = [&]() -> hipError_t {
       if (a.n == 0) return hipSuccess;
-      const hipError_t e = attr::launch_adamw((int)p_dtype, (int)g_dtype, eight, blocks, a, s);
+      const hipError_t e = attr::launch_adamw((int)p_dtype, (int)g_dtype, eight, master, blocks, a, s);
       a.n = 0;
       blocks = 0;
       return e;
@@ -903,10 +904,11 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
       for (int64_t at = 0; at < t.n; at += (int64_t)kMostBlocks * attr::kAdamwChunk) {
         const int64_t n = std::min(t.n - at, (int64_t)kMostBlocks * attr::kAdamwChunk);
         const uint32_t need = (uint32_t)((n + attr::kAdamwChunk - 1) / attr::kAdamwChunk);
-        if (a.n == attr::kAdamwMax || blocks + need > kMostBlocks) {
+        if (a.n == attr::kAdamwMax || blocks + need > kMostBlocks || master != (t.master != nullptr)) {
           const hipError_t e = flush();
           if (e != hipSuccess) return device_fail(e, "attr_adamw_step launch");
         }
+        master = t.master != nullptr;
         attr::AdamwEntry& x = a.e[a.n++];
         x.p = static_cast<char*>(t.p) + (size_t)at * pb;
         x.g = static_cast<const char*>(t.g) + (size_t)at * gb;

@@ -258,7 +258,8 @@ struct AdamwArgs {
   int32_t n;
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
-hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, uint32_t blocks, const AdamwArgs& a,
+// Every tensor of a launch has a master, or none has.
+hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, bool master, uint32_t blocks, const AdamwArgs& a,
                         hipStream_t s);
 
 // ---------------------------------------------------------------------------
