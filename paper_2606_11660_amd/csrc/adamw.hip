@@ -46,10 +46,10 @@ struct Four<uint8_t> {
   typedef plain vec __attribute__((aligned(1)));
 };
 
-// The first `in` of four elements (4: all of them, in one access); 0 for the rest.
-template <typename T>
+// Four elements in one access, or (not WHOLE) the first `in` of them and 0 for the rest.
+template <bool WHOLE, typename T>
 __device__ inline void load4(const T* p, int in, T (&x)[4]) {
-  if (in >= 4) {
+  if constexpr (WHOLE) {
     const auto v = __builtin_nontemporal_load(reinterpret_cast<const typename Four<T>::vec*>(p));
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = v[e];
@@ -58,9 +58,9 @@ __device__ inline void load4(const T* p, int in, T (&x)[4]) {
     for (int e = 0; e < 4; ++e) x[e] = e < in ? p[e] : (T)0;
   }
 }
-template <typename T>
+template <bool WHOLE, typename T>
 __device__ inline void store4(T* p, int in, const T (&x)[4]) {
-  if (in >= 4) {
+  if constexpr (WHOLE) {
     typename Four<T>::vec v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = x[e];
@@ -100,45 +100,41 @@ __device__ inline uint8_t e4m3_code(float x) {
   return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
 }
 
-template <typename P, typename G, bool EIGHT, bool MASTER>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
+// RUNS runs of a wave from run0 on; all of their elements are there (WHOLE), or some
+// are not.
+template <typename P, typename G, bool EIGHT, bool MASTER, bool WHOLE, int RUNS>
+__device__ inline void adamw_runs(const AdamwArgs& a, const AdamwEntry& t, float gs, int64_t run0) {
   typedef typename std::conditional<EIGHT, uint8_t, float>::type S;
   typedef typename std::conditional<MASTER, float, P>::type W;
-  int lo = 0, hi = a.n - 1;  // the last tensor whose first chunk is not past this workgroup
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.e[mid].chunk0 <= blockIdx.x) lo = mid;
-    else hi = mid - 1;
-  }
-  const AdamwEntry& t = a.e[lo];
-  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-  const float lr = t.lr, lr_wd = t.lr_wd;
   const int lane = threadIdx.x & 63;
-  const int64_t run0 = ((int64_t)(blockIdx.x - t.chunk0) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRuns;
-  W* const wt = MASTER ? (W*)t.master : (W*)t.p;
-  W x[kRuns][4];
-  G g[kRuns][4];
-  S m[kRuns][4], v[kRuns][4];
-  float ms[kRuns], vs[kRuns];
+  const float lr = t.lr, lr_wd = t.lr_wd;
+  const int64_t i0 = run0 * kQuantBlock + lane * 4;
+  W* const wt = (MASTER ? (W*)t.master : (W*)t.p) + i0;
+  P* const pt = (P*)t.p + i0;
+  const G* const gt = (const G*)t.g + i0;
+  S* const mt = (S*)t.m + i0;
+  S* const vt = (S*)t.v + i0;
+  W x[RUNS][4];
+  G g[RUNS][4];
+  S m[RUNS][4], v[RUNS][4];
+  float ms[RUNS], vs[RUNS];
 #pragma unroll
-  for (int u = 0; u < kRuns; ++u) {
-    const int64_t b = (run0 + u) * kQuantBlock, i = b + lane * 4;
-    const int in = t.n - i >= 4 ? 4 : (int)(t.n - i);
-    if (b >= t.n) break;
-    load4(wt + i, in, x[u]);
-    load4((const G*)t.g + i, in, g[u]);
-    load4((const S*)t.m + i, in, m[u]);
-    load4((const S*)t.v + i, in, v[u]);
+  for (int u = 0; u < RUNS; ++u) {
+    const int k = u * kQuantBlock;
+    const int in = t.n - i0 - k >= 4 ? 4 : (int)(t.n - i0 - k);
+    load4<WHOLE>(wt + k, in, x[u]);
+    load4<WHOLE>(gt + k, in, g[u]);
+    load4<WHOLE>(mt + k, in, m[u]);
+    load4<WHOLE>(vt + k, in, v[u]);
     if (EIGHT) {
       ms[u] = t.m_scale[run0 + u];
       vs[u] = t.v_scale[run0 + u];
     }
   }
 #pragma unroll
-  for (int u = 0; u < kRuns; ++u) {
-    const int64_t b = (run0 + u) * kQuantBlock, i = b + lane * 4;
-    const int in = t.n - i >= 4 ? 4 : (int)(t.n - i);
-    if (b >= t.n) break;
+  for (int u = 0; u < RUNS; ++u) {
+    const int k = u * kQuantBlock;
+    const int in = t.n - i0 - k >= 4 ? 4 : (int)(t.n - i0 - k);
     float nm[4], nv[4];
     W nx[4];
     P np[4];
@@ -161,14 +157,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
       nx[e] = (W)r;
       np[e] = (P)r;
     }
-    store4(wt + i, in, nx);
-    if (MASTER) store4((P*)t.p + i, in, np);
+    store4<WHOLE>(wt + k, in, nx);
+    if (MASTER) store4<WHOLE>(pt + k, in, np);
     if constexpr (EIGHT) {
       float root[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        root[e] = e < in ? sqrtf(nv[e]) : 0.f;
-        nm[e] = e < in ? nm[e] : 0.f;
+        root[e] = sqrtf(nv[e]);
+        if (!WHOLE && e >= in) root[e] = nm[e] = 0.f;
       }
       float am = wave_amax(nm), av = wave_amax(root);
       am = am < kAmaxLeast ? kAmaxLeast : am;
@@ -181,16 +177,36 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
         const float q = root[e] * fv;
         qv[e] = e4m3_code(q > 0.f && q < kE4M3Least ? kE4M3Least : q);
       }
-      store4((S*)t.m + i, in, qm);
-      store4((S*)t.v + i, in, qv);
+      store4<WHOLE>(mt + k, in, qm);
+      store4<WHOLE>(vt + k, in, qv);
       if (lane == 0) {
         t.m_scale[run0 + u] = am < INFINITY ? am * (1.f / kE4M3Max) : NAN;
         t.v_scale[run0 + u] = av < INFINITY ? av * (1.f / kE4M3Max) : NAN;
       }
     } else {
-      store4((S*)t.m + i, in, nm);
-      store4((S*)t.v + i, in, nv);
+      store4<WHOLE>(mt + k, in, nm);
+      store4<WHOLE>(vt + k, in, nv);
     }
+  }
+}
+
+template <typename P, typename G, bool EIGHT, bool MASTER>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
+  int lo = 0, hi = a.n - 1;  // the last tensor whose first chunk is not past this workgroup
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.e[mid].chunk0 <= blockIdx.x) lo = mid;
+    else hi = mid - 1;
+  }
+  const AdamwEntry& t = a.e[lo];
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
+  const int64_t run0 = ((int64_t)(blockIdx.x - t.chunk0) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRuns;
+  if ((run0 + kRuns) * kQuantBlock <= t.n) {
+    adamw_runs<P, G, EIGHT, MASTER, true, kRuns>(a, t, gs, run0);
+  } else {
+#pragma unroll 1
+    for (int64_t r = run0; r < run0 + kRuns && r * kQuantBlock < t.n; ++r)
+      adamw_runs<P, G, EIGHT, MASTER, false, 1>(a, t, gs, r);
   }
 }
 
