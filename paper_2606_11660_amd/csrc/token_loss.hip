@@ -11,9 +11,10 @@
 // form the differences z_j - m first).  Sums are fp32 chains per thread, then
 // trees.
 //
-// All of it is bound by HBM: a row is read once, with 16-byte loads that need no
-// alignment beyond the element's (an odd vocabulary's rows start anywhere).  What
-// is left of a row after its whole vectors goes one element a thread.
+// All of it is bound by HBM: rows are read with 16-byte loads.  An odd vocabulary's
+// rows start anywhere; the elements before a row's first 16-byte boundary and those
+// after its last whole vector go one a thread (vectors across the boundaries cost a
+// fifth of the rate).  Stores follow the loads' cut, wherever that falls in dlogits.
 #include "common.h"
 #include "kernels.h"
 
@@ -180,6 +181,33 @@ __device__ inline float block_add(float x, float* sh) {
   return x;
 }
 
+// A row is swept by NT threads: a whole workgroup, or (64) one of its four waves,
+// since a workgroup a short row would be bound by their dispatch (16384 rows of
+// 2 KB: 12.3 us).
+template <int NT>
+__device__ inline int32_t thread() { return NT == 64 ? threadIdx.x & 63 : threadIdx.x; }
+template <int NT>
+__device__ inline uint32_t first_slot() {
+  return NT == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
+}
+
+// A row of V elements: `head` before the first 16-byte boundary, `whole` in vectors
+// from there on, fewer than a vector's after them; `at`: this thread's element of the
+// first and last (V or more: none).
+struct Cut {
+  int32_t head, whole, at;
+};
+template <typename T, int NT>
+__device__ inline Cut cut_row(const T* z, int32_t V) {
+  constexpr int E = kE<T>;
+  const int32_t off = (int32_t)(-(reinterpret_cast<intptr_t>(z) / (int)sizeof(T)) & (E - 1));
+  Cut k;
+  k.head = off < V ? off : V;
+  k.whole = (V - k.head) / E * E;
+  k.at = thread<NT>() < k.head ? thread<NT>() : k.whole + thread<NT>();
+  return k;
+}
+
 // Scratch of a workgroup: two sets, so that a reduction's reads need no barrier
 // before the next one's writes.
 struct Shared {
@@ -205,14 +233,14 @@ template <typename T, int NT>
 __device__ RowSum row_sum_apart(const T* z, int32_t V, float c, float m, float* sh) {
   float s = 0.f;
 #pragma unroll 1
-  for (int32_t j = threadIdx.x; j < V; j += NT) s += __builtin_amdgcn_exp2f(((float)z[j] - m) * c);
+  for (int32_t j = thread<NT>(); j < V; j += NT) s += __builtin_amdgcn_exp2f(((float)z[j] - m) * c);
   return {m, block_add<NT>(s, sh), true};
 }
 template <typename T, int NT>
 __device__ void row_grad_apart(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
                                float ce) {
 #pragma unroll 1
-  for (int32_t j = threadIdx.x; j < V; j += NT) {
+  for (int32_t j = thread<NT>(); j < V; j += NT) {
     float d = ce * __builtin_amdgcn_exp2f(exponent((float)z[j], c, r));
     if (j == y) d += cs;
     out[j] = (T)d;
@@ -222,9 +250,9 @@ __device__ void row_grad_apart(const T* z, T* out, int32_t V, int32_t y, float c
 template <typename T, int NT>
 __device__ inline void row_zero(T* out, int32_t V) {
   constexpr int E = kE<T>;
-  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
-  for (int32_t j = threadIdx.x * E; j < whole; j += NT * E) store_vec(out + j, i32x4{0, 0, 0, 0});
-  if (at < V) out[at] = (T)0.f;
+  const Cut k = cut_row<T, NT>(out, V);
+  for (int32_t j = thread<NT>() * E; j < k.whole; j += NT * E) store_vec(out + k.head + j, i32x4{0, 0, 0, 0});
+  if (k.at < V) out[k.at] = (T)0.f;
 }
 
 // One vector's gradient, from its elements.
@@ -250,16 +278,17 @@ __device__ inline T grad_one(T z, float c, float offset, float cs, float ce, boo
 // A row's maximum and sum in one sweep: per thread a running maximum (not below
 // -2^20 / c, so that nothing but -inf needs no case of its own) and a sum that is
 // rescaled when it grows, U vectors at a time.
-template <typename T, int NT>
-__device__ RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& sh) {
-  constexpr int E = kE<T>, U = 4;
-  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
-  float top = at < V ? (float)z[at] : -INFINITY;
+template <typename T, int NT, int U>
+__device__ inline RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& sh) {
+  constexpr int E = kE<T>;
+  const Cut k = cut_row<T, NT>(z, V);
+  const T* zv = z + k.head;
+  float top = k.at < V ? (float)z[k.at] : -INFINITY;
   float mc = fmaxf(top * c, -kMostMc), s = __builtin_amdgcn_exp2f(fmaf(top, c, -mc));
-  for (int32_t j0 = threadIdx.x * E; j0 < whole; j0 += NT * E * U) {
+  for (int32_t j0 = thread<NT>() * E; j0 < k.whole; j0 += NT * E * U) {
     i32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = j0 + u * NT * E < whole ? load_vec(z + j0 + u * NT * E) : no_vec(T{});
+    for (int u = 0; u < U; ++u) v[u] = j0 + u * NT * E < k.whole ? load_vec(zv + j0 + u * NT * E) : no_vec(T{});
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float x[E];
@@ -285,22 +314,25 @@ __device__ RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& sh) {
 
 // The gradient of one row, read a second time.  A thread reads and writes its own
 // elements only: the two may be one buffer.
-template <typename T, int NT>
-__device__ void row_grad_stream(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
-                                float ce) {
-  constexpr int E = kE<T>, U = 4;
+template <typename T, int NT, int U>
+__device__ inline void row_grad_stream(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
+                                       float ce) {
+  constexpr int E = kE<T>;
   if (r.apart) return row_grad_apart<T, NT>(z, out, V, y, c, r, cs, ce);
-  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
-  if (at < V) out[at] = grad_one(z[at], c, r.offset, cs, ce, at == y);
-  for (int32_t j0 = threadIdx.x * E; j0 < whole; j0 += NT * E * U) {
+  const Cut k = cut_row<T, NT>(z, V);
+  if (k.at < V) out[k.at] = grad_one(z[k.at], c, r.offset, cs, ce, k.at == y);
+  z += k.head;
+  out += k.head;
+  y -= k.head;
+  for (int32_t j0 = thread<NT>() * E; j0 < k.whole; j0 += NT * E * U) {
     i32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (j0 + u * NT * E < whole) v[u] = load_vec(z + j0 + u * NT * E);
+      if (j0 + u * NT * E < k.whole) v[u] = load_vec(z + j0 + u * NT * E);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int32_t j = j0 + u * NT * E;
-      if (j < whole) store_vec(out + j, grad_vec<T>(v[u], c, r.offset, cs, ce, y - j));
+      if (j < k.whole) store_vec(out + j, grad_vec<T>(v[u], c, r.offset, cs, ce, y - j));
     }
   }
 }
@@ -329,11 +361,12 @@ __device__ inline TokenLoss policy_token(const PolicyArgs& p, const TokenArgs& a
   return {w * loss, w * c};
 }
 
-// Writes a token's loss and log-probability; returns the factor s c of its gradient.
+// Writes a token's loss and log-probability (one thread, `first`, does); returns the
+// factor s c of its gradient.
 __device__ inline float policy_outputs(const TokenArgs& a, const PolicyArgs& p, uint32_t slot, int64_t row,
-                                       float logp) {
+                                       float logp, bool first) {
   const TokenLoss l = policy_token(p, a, slot, row, logp);
-  if (threadIdx.x == 0) {
+  if (first) {
     p.token_loss[slot] = l.loss;
     if (a.logp) a.logp[row] = logp;
   }
@@ -344,25 +377,29 @@ __device__ inline float policy_outputs(const TokenArgs& a, const PolicyArgs& p, 
 template <typename T, int NT>
 __device__ inline void skip_slot(const TokenArgs& a, const Slot& sl) {
   if (!sl.write) return;
-  if (threadIdx.x == 0 && a.logp) a.logp[sl.row] = 0.f;
+  if (thread<NT>() == 0 && a.logp) a.logp[sl.row] = 0.f;
   if (a.dlogits) row_zero<T, NT>((T*)a.dlogits + sl.row * a.ldd, a.V);
 }
 
+// Threads of a workgroup whose rows are swept by NT threads each.
+constexpr int group_of(int nt) { return nt == 64 ? 256 : nt; }
+
 // Log-probabilities (PREF: and what the gradient needs of each row), one sweep.
-template <typename T, int NT, bool PREF>
-__global__ __launch_bounds__(NT) void token_logp_kernel(TokenArgs a) {
+template <typename T, int NT, int U, bool PREF>
+__global__ __launch_bounds__(group_of(NT)) void token_logp_kernel(TokenArgs a) {
   __shared__ Shared sh;
   const float c = a.scale * kLog2e;
-  const uint32_t slot = a.slot0 + blockIdx.x;
+  const uint32_t slot = a.slot0 + first_slot<NT>();
+  if (slot >= a.n_slots) return;
   const Slot sl = slot_of(a, slot);
   if (!sl.counts) {
-    if (threadIdx.x == 0 && sl.write && a.logp) a.logp[sl.row] = 0.f;
+    if (thread<NT>() == 0 && sl.write && a.logp) a.logp[sl.row] = 0.f;
     return;
   }
   const T* z = (const T*)a.logits + sl.row * a.ldl;
   const float zy = (float)z[sl.target];
-  const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
-  if (threadIdx.x != 0) return;
+  const RowSum r = row_sum_stream<T, NT, U>(z, a.V, c, sh);
+  if (thread<NT>() != 0) return;
   const float logp = row_logp(zy, c, r);
   if (a.logp) a.logp[sl.row] = logp;
   if (PREF) {
@@ -373,27 +410,29 @@ __global__ __launch_bounds__(NT) void token_logp_kernel(TokenArgs a) {
 
 // Policy loss with the row in registers: NV vectors a thread, V <= NT NV kE.
 template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT, NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
+__global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
   constexpr int E = kE<T>;
   __shared__ Shared sh;
   const float c = a.scale * kLog2e;
   const int32_t V = a.V;
-  const uint32_t slot = a.slot0 + blockIdx.x;
+  const uint32_t slot = a.slot0 + first_slot<NT>();
+  if (slot >= a.n_slots) return;
   const Slot sl = slot_of(a, slot);
+  const bool first = thread<NT>() == 0;
   if (!sl.counts) {
     skip_slot<T, NT>(a, sl);
-    if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
+    if (first) p.token_loss[slot] = 0.f;
     return;
   }
   const T* z = (const T*)a.logits + sl.row * a.ldl;
   const float zy = (float)z[sl.target];
-  const int32_t whole = V / E * E, at = whole + (int32_t)threadIdx.x;
-  const T rest = at < V ? z[at] : (T)-INFINITY;
+  const Cut cut = cut_row<T, NT>(z, V);
+  const T rest = cut.at < V ? z[cut.at] : (T)-INFINITY;
   i32x4 v[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int32_t j = (k * NT + (int32_t)threadIdx.x) * E;
-    v[k] = j < whole ? load_vec(z + j) : no_vec(T{});
+    const int32_t j = (k * NT + thread<NT>()) * E;
+    v[k] = j < cut.whole ? load_vec(z + cut.head + j) : no_vec(T{});
   }
   float top = fmaxf(zy, (float)rest);  // zy, an element of the row, is read before anything of it is written
 #pragma unroll
@@ -406,7 +445,7 @@ __global__ __launch_bounds__(NT, NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a,
   const float m = block_max<NT>(top, sh.max), mc = m * c;
   if (!(fabsf(mc) <= kMostMc)) {
     const RowSum r = row_sum_apart<T, NT>(z, V, c, m, sh.slow);
-    const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r));
+    const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r), first);
     if (a.dlogits) row_grad_apart<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, V, sl.target, c, r, g, -g / r.sum);
     return;
   }
@@ -420,18 +459,19 @@ __global__ __launch_bounds__(NT, NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a,
     for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
   }
   const RowSum r{mc, block_add<NT>(s, sh.sum), false};
-  const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r));
+  const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r), first);
   if (!a.dlogits) return;
   T* out = (T*)a.dlogits + sl.row * a.ldd;
   const float ce = -g / r.sum;
+  if (cut.at < V) out[cut.at] = grad_one(rest, c, mc, g, ce, cut.at == sl.target);
+  out += cut.head;
   forget(v);
-  int32_t j0 = (int32_t)threadIdx.x * E;
+  int32_t j0 = thread<NT>() * E;
   forget(j0);
-  if (at < V) out[at] = grad_one(rest, c, mc, g, ce, at == sl.target);
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int32_t j = j0 + k * NT * E;
-    if (j < whole) store_vec(out + j, grad_vec<T>(v[k], c, mc, g, ce, sl.target - j));
+    if (j < cut.whole) store_vec(out + j, grad_vec<T>(v[k], c, mc, g, ce, sl.target - cut.head - j));
   }
 }
 
@@ -440,21 +480,20 @@ template <typename T, int NT>
 __global__ __launch_bounds__(NT) void policy_stream_kernel(TokenArgs a, PolicyArgs p) {
   __shared__ Shared sh;
   const float c = a.scale * kLog2e;
-  const uint32_t slot = a.slot0 + blockIdx.x;
+  const uint32_t slot = a.slot0 + first_slot<NT>();
   const Slot sl = slot_of(a, slot);
+  const bool first = thread<NT>() == 0;
   if (!sl.counts) {
     skip_slot<T, NT>(a, sl);
-    if (threadIdx.x == 0) p.token_loss[slot] = 0.f;
+    if (first) p.token_loss[slot] = 0.f;
     return;
   }
   const T* z = (const T*)a.logits + sl.row * a.ldl;
-  const float zy = (float)z[sl.target];
-  if (threadIdx.x == 0) sh.zy = zy;  // read before anything of the row is written
-  const RowSum r = row_sum_stream<T, NT>(z, a.V, c, sh);
-  if (NT == 64) __syncthreads();
-  const float g = policy_outputs(a, p, slot, sl.row, row_logp(sh.zy, c, r));
+  if (first) sh.zy = (float)z[sl.target];  // read before anything of the row is written
+  const RowSum r = row_sum_stream<T, NT, 4>(z, a.V, c, sh);
+  const float g = policy_outputs(a, p, slot, sl.row, row_logp(sh.zy, c, r), first);
   if (a.dlogits)
-    row_grad_stream<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r, g, -g / r.sum);
+    row_grad_stream<T, NT, 4>(z, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r, g, -g / r.sum);
 }
 
 __device__ inline double block_sum(double v, double* sh) {
@@ -510,10 +549,11 @@ __global__ __launch_bounds__(256) void pair_kernel(TokenArgs a, PrefArgs p) {
   }
 }
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void pref_grad_kernel(TokenArgs a, PrefArgs p) {
+template <typename T, int NT, int U>
+__global__ __launch_bounds__(group_of(NT)) void pref_grad_kernel(TokenArgs a, PrefArgs p) {
   const float c = a.scale * kLog2e;
-  const uint32_t slot = a.slot0 + blockIdx.x;
+  const uint32_t slot = a.slot0 + first_slot<NT>();
+  if (slot >= a.n_slots) return;
   const Slot sl = slot_of(a, slot);
   if (!sl.counts) {
     if (sl.write) row_zero<T, NT>((T*)a.dlogits + sl.row * a.ldd, a.V);
@@ -524,48 +564,49 @@ __global__ __launch_bounds__(NT) void pref_grad_kernel(TokenArgs a, PrefArgs p) 
   const uint32_t i = slot / a.T;
   const float w = a.weight ? a.weight[sl.row] : 1.f;
   const float cs = (i < p.n_pairs ? p.coef[i] : -p.coef[i - p.n_pairs]) * w * a.scale, ce = -cs / r.sum;
-  row_grad_stream<T, NT>((const T*)a.logits + sl.row * a.ldl, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r,
-                         cs, ce);
+  row_grad_stream<T, NT, U>((const T*)a.logits + sl.row * a.ldl, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r,
+                            cs, ce);
 }
 
 uint32_t blocks_for(uint32_t n) { return n < (1u << 20) ? n : (1u << 20); }
 
-// One workgroup a slot, in launches of fewer than 2^32 threads.
-template <typename... K, typename... Args>
-void launch_slots(void (*kernel)(TokenArgs, K...), int threads, TokenArgs a, hipStream_t s, Args... args) {
-  constexpr uint32_t kMost = 1u << 21;
+// Every slot's row swept by NT threads, in launches of fewer than 2^32 threads.
+template <int NT, typename... K, typename... Args>
+void launch_slots(void (*kernel)(TokenArgs, K...), TokenArgs a, hipStream_t s, Args... args) {
+  constexpr uint32_t kMost = 1u << 21, kRows = group_of(NT) / NT;
   for (a.slot0 = 0; a.slot0 < a.n_slots; a.slot0 += kMost) {
-    const uint32_t n = a.n_slots - a.slot0;
-    hipLaunchKernelGGL(kernel, dim3(n < kMost ? n : kMost), dim3(threads), 0, s, a, args...);
+    const uint32_t n = a.n_slots - a.slot0 < kMost ? a.n_slots - a.slot0 : kMost;
+    hipLaunchKernelGGL(kernel, dim3((n + kRows - 1) / kRows), dim3(group_of(NT)), 0, s, a, args...);
   }
 }
 
-// Threads that sweep a row: a wave up to 4 KB of it, then 256, and 1024 from 64 KB.
 template <typename T, bool PREF>
 void launch_logp(const TokenArgs& a, hipStream_t s) {
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (bytes <= 4096) launch_slots(token_logp_kernel<T, 64, PREF>, 64, a, s);
-  else if (bytes <= 65536) launch_slots(token_logp_kernel<T, 256, PREF>, 256, a, s);
-  else launch_slots(token_logp_kernel<T, 1024, PREF>, 1024, a, s);
+  if (bytes <= 4096) launch_slots<64>(token_logp_kernel<T, 64, 4, PREF>, a, s);
+  else if (bytes <= 65536) launch_slots<256>(token_logp_kernel<T, 256, 4, PREF>, a, s);
+  else if (bytes <= 131072) launch_slots<512>(token_logp_kernel<T, 512, 2, PREF>, a, s);
+  else launch_slots<512>(token_logp_kernel<T, 512, 4, PREF>, a, s);
 }
 
 template <typename T>
 void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (bytes <= 2048) launch_slots(policy_kernel<T, 64, 2>, 64, a, s, p);
-  else if (bytes <= 8192) launch_slots(policy_kernel<T, 64, 8>, 64, a, s, p);
-  else if (bytes <= 32768) launch_slots(policy_kernel<T, 256, 8>, 256, a, s, p);
-  else if (bytes <= 65536) launch_slots(policy_kernel<T, 512, 8>, 512, a, s, p);
-  else if (bytes <= 131072) launch_slots(policy_kernel<T, 512, 16>, 512, a, s, p);
-  else if (bytes <= 262144) launch_slots(policy_kernel<T, 1024, 16>, 1024, a, s, p);
-  else launch_slots(policy_stream_kernel<T, 1024>, 1024, a, s, p);
+  if (bytes <= 2048) launch_slots<64>(policy_kernel<T, 64, 2>, a, s, p);
+  else if (bytes <= 8192) launch_slots<256>(policy_kernel<T, 256, 2>, a, s, p);
+  else if (bytes <= 32768) launch_slots<256>(policy_kernel<T, 256, 8>, a, s, p);
+  else if (bytes <= 65536) launch_slots<1024>(policy_kernel<T, 1024, 4>, a, s, p);
+  else if (bytes <= 131072) launch_slots<1024>(policy_kernel<T, 1024, 8>, a, s, p);
+  else if (bytes <= 262144) launch_slots<1024>(policy_kernel<T, 1024, 16>, a, s, p);
+  else launch_slots<1024>(policy_stream_kernel<T, 1024>, a, s, p);
 }
 
 template <typename T>
 void launch_grad(const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (bytes <= 4096) launch_slots(pref_grad_kernel<T, 64>, 64, a, s, p);
-  else launch_slots(pref_grad_kernel<T, 256>, 256, a, s, p);
+  if (bytes <= 4096) launch_slots<64>(pref_grad_kernel<T, 64, 4>, a, s, p);
+  else if (bytes <= 65536) launch_slots<256>(pref_grad_kernel<T, 256, 4>, a, s, p);
+  else launch_slots<1024>(pref_grad_kernel<T, 1024, 2>, a, s, p);
 }
 
 }  // namespace
