@@ -142,6 +142,23 @@ def lib() -> ctypes.CDLL:
 
 
 _native_modules = None
+_native_rows = None
+
+
+def _native_token_rows():
+    """The native gatherer of a token call's rows, loaded once, as _native()."""
+    global _native_rows
+    if _native_rows is None:
+        try:
+            from ._marshal import token_rows
+        except ImportError as e:
+            warnings.warn(f"_marshal is not available ({e}): token calls check their tensors in Python "
+                          "(build it with `python -m paper_2606_11660_amd.build`)", RuntimeWarning, stacklevel=2)
+
+            def token_rows(*args):
+                return None
+        _native_rows = token_rows
+    return _native_rows
 
 
 def _native():
@@ -180,6 +197,13 @@ def _stream(stream) -> Optional[int]:
 def _call_stream(stream):
     """The call's stream, looked up once."""
     return torch.cuda.current_stream() if stream is None else stream
+
+
+def _raw_stream(stream) -> int:
+    """The call's stream as a handle, without a Stream object (2.8 us) for the current one."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return _stream(stream)
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -565,26 +589,35 @@ def attr_preference_loss_workspace_size(rows: TokenRows) -> int:
     return int(lib().attr_preference_loss_workspace_size(rows.c()))
 
 
-def _check_dlogits(dlogits: Optional[torch.Tensor], rows: TokenRows) -> int:
-    """Row stride of the gradient's buffer (0 without one)."""
-    if dlogits is None:
-        return 0
-    n, V, ldd = _rows(dlogits)
-    if dlogits.dtype != rows.logits.dtype or (n, V) != _rows(rows.logits)[:2]:
-        raise ValueError("dlogits must have the logits' shape and type")
-    return ldd
+def _token_call(rows: TokenRows, per_row: tuple, per_example: tuple = (), per_pair: tuple = (),
+                dlogits: Optional[torch.Tensor] = None) -> Tuple[_CTokenRows, int]:
+    """(checked descriptor, row stride of dlogits) of a token call with these fp32 vectors
+    (or None), by the number of elements that each needs."""
+    got = _native_token_rows()(rows, TokenRows, per_row, per_example, per_pair, dlogits)
+    if got is not None:
+        return _CTokenRows.from_buffer(got[0]), got[1]
+    c = rows.c()
+    for ts, n, what in ((per_row, c.n_rows, "row"), (per_example, c.n_examples, "example"),
+                        (per_pair, c.n_examples // 2, "pair")):
+        for t in ts:
+            _vector(t, n, torch.float32, f"a vector with one value for each {what}")
+    ldd = 0
+    if dlogits is not None:
+        n, V, ldd = _rows(dlogits)
+        if dlogits.dtype != rows.logits.dtype or (n, V) != (c.n_rows, c.V):
+            raise ValueError("dlogits must have the logits' shape and type")
+    _same_gpu(rows.logits, dlogits, *per_row, *per_example, *per_pair)
+    return c, ldd
 
 
 def attr_token_logp(rows: TokenRows, logp: torch.Tensor, ws: Optional[Workspace] = None,
                     stream=None) -> torch.Tensor:
     """Log-probability of every row's target into logp (fp32 [n_rows]; 0 for tokens that do not count)."""
-    c = rows.c()
-    _vector(logp, c.n_rows, torch.float32, "logp")
-    _same_gpu(rows.logits, logp)
+    c, _ = _token_call(rows, (logp,))
     L = lib()
-    stream = _call_stream(stream)
-    wsp, wsn = _ws(ws, logp.device, stream).get(L.attr_token_logp_workspace_size(c), stream)
-    _check(L.attr_token_logp(c, logp.data_ptr(), wsp, wsn, _stream(stream)))
+    raw = _raw_stream(stream)
+    wsp, wsn = _ws(ws, logp.device, raw).get(L.attr_token_logp_workspace_size(c), raw)
+    _check(L.attr_token_logp(c, logp.data_ptr(), wsp, wsn, raw))
     return logp
 
 
@@ -599,19 +632,16 @@ def attr_policy_loss(rows: TokenRows, advantage: torch.Tensor, loss: torch.Tenso
     fp32 [n_rows] (logp_old None: on policy, ratio 1).  dlogits (the logits' shape
     and type, may be the logits themselves) takes the gradient of loss.sum(); rows'
     weights carry the mask and the normalisation."""
-    c = rows.c()
-    _vector(advantage, c.n_rows if per_token else c.n_examples, torch.float32, "advantage")
-    _vector(loss, c.n_examples, torch.float32, "loss")
-    for t, name in ((logp, "logp"), (logp_old, "logp_old"), (logp_ref, "logp_ref")):
-        _vector(t, c.n_rows, torch.float32, name)
-    ldd = _check_dlogits(dlogits, rows)
-    _same_gpu(rows.logits, advantage, loss, logp, dlogits, logp_old, logp_ref)
+    if per_token:
+        c, ldd = _token_call(rows, (advantage, logp, logp_old, logp_ref), (loss,), (), dlogits)
+    else:
+        c, ldd = _token_call(rows, (logp, logp_old, logp_ref), (loss, advantage), (), dlogits)
     L = lib()
-    stream = _call_stream(stream)
-    wsp, wsn = _ws(ws, loss.device, stream).get(L.attr_policy_loss_workspace_size(c), stream)
+    raw = _raw_stream(stream)
+    wsp, wsn = _ws(ws, loss.device, raw).get(L.attr_policy_loss_workspace_size(c), raw)
     _check(L.attr_policy_loss(c, advantage.data_ptr(), 1 if per_token else 0, _ptr(logp_old), _ptr(logp_ref),
                               clip_low, clip_high, beta, loss.data_ptr(), _ptr(logp), _ptr(dlogits), ldd,
-                              wsp, wsn, _stream(stream)))
+                              wsp, wsn, raw))
     return loss
 
 
@@ -625,21 +655,12 @@ def attr_preference_loss(rows: TokenRows, loss: torch.Tensor, log_ratio: Optiona
     Pair p: example p was chosen, example n_pairs + p rejected.  log_ratio: fp32
     [n_examples], the weighted sums of logp - logp_ref; dlogits takes the gradient
     of loss.sum(); pair_weight (fp32 [n_pairs]) scales each pair's loss."""
-    c = rows.c()
-    n_pairs = c.n_examples // 2
-    _vector(loss, n_pairs, torch.float32, "loss")
-    _vector(pair_weight, n_pairs, torch.float32, "pair_weight")
-    _vector(log_ratio, c.n_examples, torch.float32, "log_ratio")
-    for t, name in ((logp, "logp"), (logp_ref, "logp_ref")):
-        _vector(t, c.n_rows, torch.float32, name)
-    ldd = _check_dlogits(dlogits, rows)
-    _same_gpu(rows.logits, loss, log_ratio, logp, dlogits, logp_ref, pair_weight)
+    c, ldd = _token_call(rows, (logp, logp_ref), (log_ratio,), (loss, pair_weight), dlogits)
     L = lib()
-    stream = _call_stream(stream)
-    wsp, wsn = _ws(ws, loss.device, stream).get(L.attr_preference_loss_workspace_size(c), stream)
+    raw = _raw_stream(stream)
+    wsp, wsn = _ws(ws, loss.device, raw).get(L.attr_preference_loss_workspace_size(c), raw)
     _check(L.attr_preference_loss(c, _ptr(logp_ref), _ptr(pair_weight), beta, margin, label_smoothing,
-                                  loss.data_ptr(), _ptr(log_ratio), _ptr(logp), _ptr(dlogits), ldd, wsp, wsn,
-                                  _stream(stream)))
+                                  loss.data_ptr(), _ptr(log_ratio), _ptr(logp), _ptr(dlogits), ldd, wsp, wsn, raw))
     return loss
 
 
@@ -717,7 +738,7 @@ def attr_adamw_step(tensors: AdamTensors, step: int, lr: float, beta1: float = 0
             raise ValueError("every tensor must live on the same GPU device")
     _check(lib().attr_adamw_step(tensors.array, len(tensors.array), tensors.p_dtype, tensors.g_dtype,
                                  tensors.state_dtype, step, lr, beta1, beta2, eps, eps_root, _ptr(grad_scale),
-                                 _stream(stream)))
+                                 _raw_stream(stream)))
 
 
 # ----------------------------------------------------------------------------

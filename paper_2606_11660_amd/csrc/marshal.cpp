@@ -1,4 +1,5 @@
-// Module descriptors of a projection call, gathered from the Python objects.
+// Module descriptors of a projection call, and the rows of a token loss, gathered
+// from the Python objects.
 //
 // A call over a model's modules passes four tensors each: checking them and
 // reading their pointers, shapes and strides attribute by attribute from Python
@@ -6,7 +7,9 @@
 // take (here: 15 us).  modules() makes the binding's checks on exact torch
 // tensors and returns None as soon as one does not hold or anything is of
 // another kind (a subclass, a wrapper without storage, a CPU tensor): the
-// binding's own Python checks then run, and raise or accept.
+// binding's own Python checks then run, and raise or accept.  token_rows() does the
+// same for a batch of token rows and the fp32 vectors of its call (1 us of the 7 that
+// the Python checks take, where a small call's kernels take 4).
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -18,6 +21,7 @@ namespace {
 
 struct Names {
   PyObject *a, *g, *R, *S, *out_col, *v_out, *v_in;
+  PyObject *logits, *target, *weight, *n_examples, *T, *row_offset, *length, *logit_scale;
 } names;
 
 // a new reference, or NULL
@@ -153,21 +157,103 @@ PyObject* py_modules(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return buf ? Py_BuildValue("iN", dtype, buf) : nullptr;
 }
 
+// a size that products of two stay inside 64 bits with
+bool size_of(PyObject* o, int64_t& v) {
+  if (!o || !PyLong_CheckExact(o)) return false;
+  v = PyLong_AsLongLong(o);
+  return !PyErr_Occurred() && v >= 0 && v <= ((int64_t)1 << 31);
+}
+
+// None or a tuple of fp32 vectors (or None) of at least n elements on dev
+bool vectors_ok(PyObject* o, int64_t n, const at::Device& dev) {
+  if (!PyTuple_CheckExact(o)) return false;
+  for (Py_ssize_t j = 0; j < PyTuple_GET_SIZE(o); ++j)
+    if (!vector_ok(PyTuple_GET_ITEM(o, j), at::kFloat, n, dev)) return false;
+  return true;
+}
+
+bool gather_rows(PyObject* rows, PyObject* rows_type, PyObject* const* vecs, PyObject* dlogits, attr_token_rows& c,
+                 int64_t& ldd) {
+  if ((PyObject*)Py_TYPE(rows) != rows_type) return false;
+  const Ref logits(PyObject_GetAttr(rows, names.logits)), target(PyObject_GetAttr(rows, names.target)),
+      weight(PyObject_GetAttr(rows, names.weight)), n_ex(PyObject_GetAttr(rows, names.n_examples)),
+      T(PyObject_GetAttr(rows, names.T)), off(PyObject_GetAttr(rows, names.row_offset)),
+      len(PyObject_GetAttr(rows, names.length)), scale(PyObject_GetAttr(rows, names.logit_scale));
+  const at::Tensor *z = tensor_of(logits.p), *y = tensor_of(target.p);
+  if (!z || !y || !weight.p || !off.p || !len.p || !scale.p || !PyFloat_CheckExact(scale.p) || !z->is_cuda() ||
+      !size_of(n_ex.p, c.n_examples) || !size_of(T.p, c.T) || c.T < 1)
+    return false;
+  const at::Device dev = z->device();
+  const at::ScalarType type = z->scalar_type();
+  if (type != at::kFloat && type != at::kBFloat16 && type != at::kHalf) return false;
+  if (!rows_of(*z, c.n_rows, c.V, c.ldl) || (off.p == Py_None && c.n_rows < c.n_examples * c.T)) return false;
+  if (target.p == Py_None || !vector_ok(target.p, at::kLong, c.n_rows, dev) ||
+      !vector_ok(weight.p, at::kFloat, c.n_rows, dev) || !vector_ok(off.p, at::kLong, c.n_examples, dev) ||
+      !vector_ok(len.p, at::kInt, c.n_examples, dev) || !vectors_ok(vecs[0], c.n_rows, dev) ||
+      !vectors_ok(vecs[1], c.n_examples, dev) || !vectors_ok(vecs[2], c.n_examples / 2, dev))
+    return false;
+  ldd = 0;
+  if (dlogits != Py_None) {
+    const at::Tensor* d = tensor_of(dlogits);
+    int64_t n, V;
+    if (!d || !on(*d, dev) || d->scalar_type() != type || !rows_of(*d, n, V, ldd) || n != c.n_rows || V != c.V)
+      return false;
+  }
+  auto ptr = [](PyObject* o) -> void* { return o == Py_None ? nullptr : THPVariable_Unpack(o).mutable_data_ptr(); };
+  c.logits = z->mutable_data_ptr();
+  c.dtype = type == at::kFloat ? ATTR_F32 : type == at::kBFloat16 ? ATTR_BF16 : ATTR_F16;
+  c.logit_scale = (float)PyFloat_AS_DOUBLE(scale.p);
+  c.target = static_cast<const int64_t*>(y->mutable_data_ptr());
+  c.weight = static_cast<const float*>(ptr(weight.p));
+  c.row_offset = static_cast<const int64_t*>(ptr(off.p));
+  c.length = static_cast<const int32_t*>(ptr(len.p));
+  return true;
+}
+
+// token_rows(rows, TokenRows, per_row, per_example, per_pair, dlogits)
+// -> (bytearray of attr_token_rows, row stride of dlogits) or None; the three tuples:
+// the call's fp32 vectors by the number of their elements
+PyObject* py_token_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  if (nargs != 6) {
+    PyErr_SetString(PyExc_TypeError, "token_rows() takes 6 arguments");
+    return nullptr;
+  }
+  attr_token_rows c;
+  std::memset(&c, 0, sizeof(c));
+  int64_t ldd = 0;
+  bool ok = false;
+  try {
+    ok = gather_rows(args[0], args[1], args + 2, args[5], c, ldd);
+  } catch (...) {  // a tensor without storage, for one
+    ok = false;
+  }
+  if (!ok) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  PyObject* buf = PyByteArray_FromStringAndSize(reinterpret_cast<const char*>(&c), (Py_ssize_t)sizeof(c));
+  return buf ? Py_BuildValue("NL", buf, (long long)ldd) : nullptr;
+}
+
 PyMethodDef methods[] = {{"modules", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_modules)),
                           METH_FASTCALL, "module descriptors of a projection call, or None"},
+                         {"token_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_token_rows)),
+                          METH_FASTCALL, "descriptor of a token call's rows, or None"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__marshal(void) {
-  names.a = PyUnicode_InternFromString("a");
-  names.g = PyUnicode_InternFromString("g");
-  names.R = PyUnicode_InternFromString("R");
-  names.S = PyUnicode_InternFromString("S");
-  names.out_col = PyUnicode_InternFromString("out_col");
-  names.v_out = PyUnicode_InternFromString("v_out");
-  names.v_in = PyUnicode_InternFromString("v_in");
-  if (!names.a || !names.g || !names.R || !names.S || !names.out_col || !names.v_out || !names.v_in) return nullptr;
+  struct {
+    PyObject** at;
+    const char* name;
+  } const all[] = {{&names.a, "a"}, {&names.g, "g"}, {&names.R, "R"}, {&names.S, "S"}, {&names.out_col, "out_col"},
+                   {&names.v_out, "v_out"}, {&names.v_in, "v_in"}, {&names.logits, "logits"},
+                   {&names.target, "target"}, {&names.weight, "weight"}, {&names.n_examples, "n_examples"},
+                   {&names.T, "T"}, {&names.row_offset, "row_offset"}, {&names.length, "length"},
+                   {&names.logit_scale, "logit_scale"}};
+  for (const auto& n : all)
+    if (!(*n.at = PyUnicode_InternFromString(n.name))) return nullptr;
   return PyModule_Create(&module_def);
 }
