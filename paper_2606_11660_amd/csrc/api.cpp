@@ -662,7 +662,33 @@ attr_status dlogits_validate(const attr_token_rows* r, void* dlogits, int64_t ld
   return ATTR_OK;
 }
 
-attr::TokenArgs token_args(const attr_token_rows* r, float* logp, void* dlogits, int64_t ldd) {
+// Workspace of the three calls: what each keeps per token slot, per pair and per part
+// of a row.
+struct TokenLayout {
+  size_t off_stats, off_part, off_coef, off_parts, off_zy, total;
+  int n_parts;
+};
+TokenLayout token_layout(const attr_token_rows* r, int mode) {
+  TokenLayout L{0, 0, 0, 0, 0, 0, 1};
+  const int64_t n = r->n_examples * r->T;
+  const size_t slots = (size_t)n;
+  if (mode == attr::kTokenPolicy) L.total = align_up(4 * slots);
+  if (mode == attr::kTokenPref) {
+    L.off_part = align_up(8 * slots);
+    L.off_coef = L.off_part + align_up(8 * slots);
+    L.total = L.off_coef + align_up(4 * (size_t)(r->n_examples / 2));
+  }
+  L.n_parts = attr::token_parts(n, r->V * dtype_bytes(r->dtype));
+  if (L.n_parts > 1) {
+    L.off_parts = L.total;
+    L.off_zy = L.off_parts + align_up(8 * slots * (size_t)L.n_parts);
+    L.total = L.off_zy + align_up(4 * slots);
+  }
+  return L;
+}
+
+attr::TokenArgs token_args(const attr_token_rows* r, const TokenLayout& L, float* logp, void* dlogits, int64_t ldd,
+                           void* ws) {
   attr::TokenArgs a;
   std::memset(&a, 0, sizeof(a));
   a.logits = r->logits;
@@ -679,23 +705,14 @@ attr::TokenArgs token_args(const attr_token_rows* r, float* logp, void* dlogits,
   a.T = (uint32_t)r->T;
   a.V = (int32_t)r->V;
   a.scale = r->logit_scale;
-  return a;
-}
-
-// Workspace of the three calls: what each keeps per token slot and per pair.
-struct TokenLayout {
-  size_t off_stats, off_logp, off_coef, total;
-};
-TokenLayout token_layout(const attr_token_rows* r, int mode) {
-  TokenLayout L{0, 0, 0, 0};
-  const size_t slots = (size_t)(r->n_examples * r->T);
-  if (mode == attr::kTokenPolicy) L.total = align_up(4 * slots);
-  if (mode == attr::kTokenPref) {
-    L.off_logp = align_up(8 * slots);
-    L.off_coef = L.off_logp + align_up(4 * slots);
-    L.total = L.off_coef + align_up(4 * (size_t)(r->n_examples / 2));
+  // parts start at multiples of 64 elements, so that they cut no vector of an aligned row
+  a.part_len = (int32_t)(L.n_parts > 1 ? ((r->V + L.n_parts - 1) / L.n_parts + 63) & ~63ll : r->V);
+  a.n_parts = (int32_t)((r->V + a.part_len - 1) / a.part_len);
+  if (L.n_parts > 1) {
+    a.parts = reinterpret_cast<float2*>(static_cast<char*>(ws) + L.off_parts);
+    a.zy = reinterpret_cast<float*>(static_cast<char*>(ws) + L.off_zy);
   }
-  return L;
+  return a;
 }
 
 attr_status token_workspace(const TokenLayout& L, void* ws, size_t ws_bytes, const char* who) {
@@ -708,7 +725,7 @@ attr_status token_workspace(const TokenLayout& L, void* ws, size_t ws_bytes, con
 }
 
 size_t token_query(const attr_token_rows* r, int mode) {
-  if (!r || r->n_examples < 0 || r->T < 1 || r->T >= (1ll << 31) || r->n_examples >= (1ll << 31) ||
+  if (!r || !valid_dtype(r->dtype) || r->V < 1 || r->V > (1ll << 28) || r->n_examples < 0 || r->T < 1 || r->T >= (1ll << 31) || r->n_examples >= (1ll << 31) ||
       r->n_examples * r->T >= (1ll << 31))
     return 0;
   return token_layout(r, mode).total;
@@ -733,8 +750,8 @@ attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, 
     const TokenLayout L = token_layout(rows, attr::kTokenLogp);
     st = token_workspace(L, ws, ws_bytes, who);
     if (st != ATTR_OK) return st;
-    const attr::TokenArgs a = token_args(rows, logp, nullptr, 0);
-    const hipError_t e = attr::launch_token_logp((int)rows->dtype, false, a, static_cast<hipStream_t>(stream));
+    const attr::TokenArgs a = token_args(rows, L, logp, nullptr, 0, ws);
+    const hipError_t e = attr::launch_token_logp((int)rows->dtype, a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_token_logp launch");
   } catch (...) {
     return fail(ATTR_ERR_INVALID_ARG, "attr_token_logp: host exception");
@@ -765,7 +782,7 @@ attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage
     const TokenLayout L = token_layout(rows, attr::kTokenPolicy);
     st = token_workspace(L, ws, ws_bytes, who);
     if (st != ATTR_OK) return st;
-    const attr::TokenArgs a = token_args(rows, logp, dlogits, ldd);
+    const attr::TokenArgs a = token_args(rows, L, logp, dlogits, ldd, ws);
     attr::PolicyArgs p;
     std::memset(&p, 0, sizeof(p));
     p.advantage = advantage;
@@ -777,6 +794,11 @@ attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage
     p.beta = beta;
     p.token_loss = static_cast<float*>(ws);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (attr::policy_by_example(rows->V * dtype_bytes(rows->dtype), rows->T, rows->n_examples)) {
+      const hipError_t e =
+          attr::launch_policy_examples((int)rows->dtype, a, p, (uint32_t)rows->n_examples, loss, s);
+      return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_policy_loss launch");
+    }
     hipError_t e = attr::launch_policy_rows((int)rows->dtype, a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_policy_loss launch");
     e = attr::launch_example_sum(p.token_loss, a.T, (uint32_t)rows->n_examples, loss, s);
@@ -812,9 +834,9 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
     st = token_workspace(L, ws, ws_bytes, who);
     if (st != ATTR_OK) return st;
     char* base = static_cast<char*>(ws);
-    attr::TokenArgs a = token_args(rows, logp, dlogits, ldd);
+    attr::TokenArgs a = token_args(rows, L, logp, dlogits, ldd, ws);
     a.stats = reinterpret_cast<float2*>(base + L.off_stats);
-    a.slot_logp = reinterpret_cast<float*>(base + L.off_logp);
+    a.part = reinterpret_cast<double*>(base + L.off_part);
     attr::PrefArgs p;
     std::memset(&p, 0, sizeof(p));
     p.logp_ref = logp_ref;
@@ -827,12 +849,13 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
     p.margin = margin;
     p.smoothing = label_smoothing;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = attr::launch_token_logp((int)rows->dtype, true, a, s);
+    hipError_t e = attr::launch_pref_stats((int)rows->dtype, a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_preference_loss launch");
-    e = attr::launch_pairs(a, p, s);
+    const bool pair = dlogits && rows->T <= 1024 && a.n_slots <= 2048;
+    if (!pair) e = attr::launch_pairs(a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_preference_loss pair launch");
     if (!dlogits) return ATTR_OK;
-    e = attr::launch_pref_grad((int)rows->dtype, a, p, s);
+    e = attr::launch_pref_grad((int)rows->dtype, pair, a, p, s);
     return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_preference_loss gradient launch");
   } catch (...) {
     return fail(ATTR_ERR_INVALID_ARG, "attr_preference_loss: host exception");

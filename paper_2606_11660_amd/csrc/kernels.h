@@ -202,11 +202,14 @@ struct TokenArgs {
   float* logp;                 // or null
   void* dlogits;               // or null
   float2* stats;               // per slot: a row's offset and sum (preference loss)
-  float* slot_logp;            // per slot (preference loss)
+  double* part;                // per slot: its share of the log ratio (preference loss)
+  float2* parts;               // per slot and part of its row: maximum and sum (n_parts > 1)
+  float* zy;                   // per slot: the target's logit (n_parts > 1)
   int64_t n_rows, ldl, ldd;
   uint32_t n_slots, T;         // slot = example * T + token
   uint32_t slot0;              // of a launch
   int32_t V;
+  int32_t n_parts, part_len;   // a row's parts and their elements (1 and V: whole rows)
   float scale;
 };
 struct PolicyArgs {
@@ -226,11 +229,20 @@ struct PrefArgs {
   uint32_t n_pairs;
   float beta, margin, smoothing;
 };
-hipError_t launch_token_logp(int dtype, bool pref, const TokenArgs& a, hipStream_t s);
+int token_parts(int64_t n_slots, int64_t row_bytes);
+hipError_t launch_token_logp(int dtype, const TokenArgs& a, hipStream_t s);
+// Policy loss: token losses of every slot, then their sums; or both at once.
 hipError_t launch_policy_rows(int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s);
 hipError_t launch_example_sum(const float* token_loss, uint32_t T, uint32_t n, float* loss, hipStream_t s);
+constexpr uint32_t kPolicyExampleMost = 16;  // tokens of an example
+bool policy_by_example(int64_t row_bytes, int64_t T, int64_t n_examples);
+hipError_t launch_policy_examples(int dtype, const TokenArgs& a, const PolicyArgs& p, uint32_t n, float* loss,
+                                  hipStream_t s);
+// Preference loss: a row's sums and its share of the log ratio; the pairs; the
+// gradient, with the pairs (pair) or after them.
+hipError_t launch_pref_stats(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 hipError_t launch_pairs(const TokenArgs& a, const PrefArgs& p, hipStream_t s);
-hipError_t launch_pref_grad(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
+hipError_t launch_pref_grad(int dtype, bool pair, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // AdamW

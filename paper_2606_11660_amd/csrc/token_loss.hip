@@ -29,26 +29,25 @@ constexpr float kMostMc = 1048576.f;  // 2^20: the residual of the fused form st
 struct Slot {
   int64_t row;
   int32_t target;   // in [0, V) where counts
+  float weight;
   bool write;       // the row's outputs are written
   bool counts;      // its logits are read
 };
 
-// Token slot of a batch: example slot / T, token slot % T (attr_token_rows).
+// Token slot of a batch: example slot / T, token slot % T (attr_token_rows).  Loads
+// that do not depend on each other are issued together: their latency is what a call
+// of few rows consists of.
 __device__ inline Slot slot_of(const TokenArgs& a, uint32_t slot) {
   const uint32_t i = slot / a.T, t = slot - i * a.T;
   Slot r;
-  bool in = true;
-  if (a.length) in = (int64_t)t < (int64_t)a.length[i];
+  const int32_t len = a.length ? a.length[i] : (int32_t)a.T;
   r.row = a.row_offset ? a.row_offset[i] + t : (int64_t)slot;
-  const bool inside = r.row >= 0 && r.row < a.n_rows;
+  const bool inside = r.row >= 0 && r.row < a.n_rows, in = (int32_t)t < len;
+  const int64_t y = inside ? a.target[r.row] : -1;
+  r.weight = inside && a.weight ? a.weight[r.row] : 1.f;
   r.write = inside && (in || !a.row_offset);
-  r.counts = inside && in;
-  r.target = 0;
-  if (r.counts) {
-    const int64_t y = a.target[r.row];
-    r.counts = y >= 0 && y < a.V && !(a.weight && a.weight[r.row] == 0.f);
-    r.target = (int32_t)y;
-  }
+  r.counts = inside && in && y >= 0 && y < a.V && r.weight != 0.f;
+  r.target = (int32_t)y;
   return r;
 }
 
@@ -211,13 +210,13 @@ __device__ inline Cut cut_row(const T* z, int32_t V) {
 // Scratch of a workgroup: two sets, so that a reduction's reads need no barrier
 // before the next one's writes.
 struct Shared {
-  float max[16], sum[16], slow[16], zy;
+  float max[16], sum[16], slow[16], part[16], zy;
 };
 
 // A row's maximum and sum in either form: offset is c m and x_j = fma(z_j, c,
 // -offset) in the fused form; in the other, x_j = (z_j - offset) c, offset = m.
 struct RowSum {
-  float offset, sum;
+  float offset, sum, top;  // top: m
   bool apart;
 };
 __device__ inline float exponent(float z, float c, const RowSum& r) {
@@ -234,7 +233,7 @@ __device__ RowSum row_sum_apart(const T* z, int32_t V, float c, float m, float* 
   float s = 0.f;
 #pragma unroll 1
   for (int32_t j = thread<NT>(); j < V; j += NT) s += __builtin_amdgcn_exp2f(((float)z[j] - m) * c);
-  return {m, block_add<NT>(s, sh), true};
+  return {m, block_add<NT>(s, sh), m, true};
 }
 template <typename T, int NT>
 __device__ void row_grad_apart(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
@@ -309,7 +308,7 @@ __device__ inline RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& 
   if (!(fabsf(m * c) <= kMostMc)) return row_sum_apart<T, NT>(z, V, c, m, sh.slow);
   const float most = m * c;
   s *= __builtin_amdgcn_exp2f(mc - most);
-  return {most, block_add<NT>(s, sh.sum), false};
+  return {most, block_add<NT>(s, sh.sum), m, false};
 }
 
 // The gradient of one row, read a second time.  A thread reads and writes its own
@@ -340,37 +339,31 @@ __device__ inline void row_grad_stream(const T* z, T* out, int32_t V, int32_t y,
 // ---------------------------------------------------------------------------
 // kernels
 // ---------------------------------------------------------------------------
+// A token's part of the policy loss, loaded before its row.
+struct PolicyToken {
+  float weight, advantage, old, ref;
+};
+__device__ inline PolicyToken policy_inputs(const PolicyArgs& p, const TokenArgs& a, uint32_t slot, const Slot& sl) {
+  return {sl.weight, p.advantage[p.per_token ? sl.row : (int64_t)(slot / a.T)],
+          p.logp_old ? p.logp_old[sl.row] : 0.f, p.beta != 0.f ? p.logp_ref[sl.row] : 0.f};
+}
+
 // Loss and derivative by logp of one token of the policy loss, weights included.
 struct TokenLoss {
   float loss, c;
 };
-__device__ inline TokenLoss policy_token(const PolicyArgs& p, const TokenArgs& a, uint32_t slot,
-                                         int64_t row, float logp) {
-  const float w = a.weight ? a.weight[row] : 1.f;
-  const float adv = p.advantage[p.per_token ? row : (int64_t)(slot / a.T)];
-  const float ratio = p.logp_old ? expf(logp - p.logp_old[row]) : logp == logp ? 1.f : logp;
-  const float free_ = -adv * ratio;
-  const float held = -adv * fminf(fmaxf(ratio, p.lo), p.hi);
+__device__ inline TokenLoss policy_token(const PolicyArgs& p, const PolicyToken& k, float logp) {
+  const float ratio = p.logp_old ? expf(logp - k.old) : logp == logp ? 1.f : logp;
+  const float free_ = -k.advantage * ratio;
+  const float held = -k.advantage * fminf(fmaxf(ratio, p.lo), p.hi);
   float loss = free_ >= held ? free_ : held, c = free_ >= held ? free_ : 0.f;
   if (ratio != ratio) loss = c = ratio;  // a NaN stays
   if (p.beta != 0.f) {
-    const float d = p.logp_ref[row] - logp, less = expm1f(d);
+    const float d = k.ref - logp, less = expm1f(d);
     loss += p.beta * (less - d);
     c -= p.beta * less;
   }
-  return {w * loss, w * c};
-}
-
-// Writes a token's loss and log-probability (one thread, `first`, does); returns the
-// factor s c of its gradient.
-__device__ inline float policy_outputs(const TokenArgs& a, const PolicyArgs& p, uint32_t slot, int64_t row,
-                                       float logp, bool first) {
-  const TokenLoss l = policy_token(p, a, slot, row, logp);
-  if (first) {
-    p.token_loss[slot] = l.loss;
-    if (a.logp) a.logp[row] = logp;
-  }
-  return l.c * a.scale;
+  return {k.weight * loss, k.weight * c};
 }
 
 // Outputs of a slot that does not count.
@@ -384,46 +377,53 @@ __device__ inline void skip_slot(const TokenArgs& a, const Slot& sl) {
 // Threads of a workgroup whose rows are swept by NT threads each.
 constexpr int group_of(int nt) { return nt == 64 ? 256 : nt; }
 
+// A slot's log-probability, and (PREF) what the preference loss keeps of it.
+template <bool PREF>
+__device__ inline void write_logp(const TokenArgs& a, uint32_t slot, const Slot& sl, float logp, const RowSum& r,
+                                  const float* logp_ref) {
+  if (a.logp) a.logp[sl.row] = logp;
+  if (!PREF) return;
+  a.part[slot] = (double)sl.weight * ((double)logp - (logp_ref ? (double)logp_ref[sl.row] : 0.0));
+  a.stats[slot] = float2{r.offset, r.apart ? -r.sum : r.sum};
+}
+template <bool PREF>
+__device__ inline void skip_logp(const TokenArgs& a, uint32_t slot, const Slot& sl) {
+  if (sl.write && a.logp) a.logp[sl.row] = 0.f;
+  if (PREF) a.part[slot] = 0.0;
+}
+
 // Log-probabilities (PREF: and what the gradient needs of each row), one sweep.
 template <typename T, int NT, int U, bool PREF>
-__global__ __launch_bounds__(group_of(NT)) void token_logp_kernel(TokenArgs a) {
+__global__ __launch_bounds__(group_of(NT)) void token_logp_kernel(TokenArgs a, const float* logp_ref) {
   __shared__ Shared sh;
   const float c = a.scale * kLog2e;
   const uint32_t slot = a.slot0 + first_slot<NT>();
   if (slot >= a.n_slots) return;
   const Slot sl = slot_of(a, slot);
   if (!sl.counts) {
-    if (thread<NT>() == 0 && sl.write && a.logp) a.logp[sl.row] = 0.f;
+    if (thread<NT>() == 0) skip_logp<PREF>(a, slot, sl);
     return;
   }
   const T* z = (const T*)a.logits + sl.row * a.ldl;
   const float zy = (float)z[sl.target];
   const RowSum r = row_sum_stream<T, NT, U>(z, a.V, c, sh);
-  if (thread<NT>() != 0) return;
-  const float logp = row_logp(zy, c, r);
-  if (a.logp) a.logp[sl.row] = logp;
-  if (PREF) {
-    a.slot_logp[slot] = logp;
-    a.stats[slot] = float2{r.offset, r.apart ? -r.sum : r.sum};
-  }
+  if (thread<NT>() == 0) write_logp<PREF>(a, slot, sl, row_logp(zy, c, r), r, logp_ref);
 }
 
-// Policy loss with the row in registers: NV vectors a thread, V <= NT NV kE.
+// Policy loss of one slot with the row in registers: NV vectors a thread,
+// V <= NT NV kE.  Returns the token's loss.
 template <typename T, int NT, int NV>
-__global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
+__device__ inline float policy_slot(const TokenArgs& a, const PolicyArgs& p, uint32_t slot, Shared& sh) {
   constexpr int E = kE<T>;
-  __shared__ Shared sh;
   const float c = a.scale * kLog2e;
   const int32_t V = a.V;
-  const uint32_t slot = a.slot0 + first_slot<NT>();
-  if (slot >= a.n_slots) return;
   const Slot sl = slot_of(a, slot);
   const bool first = thread<NT>() == 0;
   if (!sl.counts) {
     skip_slot<T, NT>(a, sl);
-    if (first) p.token_loss[slot] = 0.f;
-    return;
+    return 0.f;
   }
+  const PolicyToken in = policy_inputs(p, a, slot, sl);
   const T* z = (const T*)a.logits + sl.row * a.ldl;
   const float zy = (float)z[sl.target];
   const Cut cut = cut_row<T, NT>(z, V);
@@ -445,9 +445,12 @@ __global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void po
   const float m = block_max<NT>(top, sh.max), mc = m * c;
   if (!(fabsf(mc) <= kMostMc)) {
     const RowSum r = row_sum_apart<T, NT>(z, V, c, m, sh.slow);
-    const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r), first);
+    const float logp = row_logp(zy, c, r);
+    const TokenLoss l = policy_token(p, in, logp);
+    if (first && a.logp) a.logp[sl.row] = logp;
+    const float g = l.c * a.scale;
     if (a.dlogits) row_grad_apart<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, V, sl.target, c, r, g, -g / r.sum);
-    return;
+    return l.loss;
   }
   forget(v);
   float s = __builtin_amdgcn_exp2f(fmaf((float)rest, c, -mc));
@@ -458,11 +461,13 @@ __global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void po
 #pragma unroll
     for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
   }
-  const RowSum r{mc, block_add<NT>(s, sh.sum), false};
-  const float g = policy_outputs(a, p, slot, sl.row, row_logp(zy, c, r), first);
-  if (!a.dlogits) return;
+  const RowSum r{mc, block_add<NT>(s, sh.sum), m, false};
+  const float logp = row_logp(zy, c, r);
+  const TokenLoss l = policy_token(p, in, logp);
+  if (first && a.logp) a.logp[sl.row] = logp;
+  if (!a.dlogits) return l.loss;
   T* out = (T*)a.dlogits + sl.row * a.ldd;
-  const float ce = -g / r.sum;
+  const float g = l.c * a.scale, ce = -g / r.sum;
   if (cut.at < V) out[cut.at] = grad_one(rest, c, mc, g, ce, cut.at == sl.target);
   out += cut.head;
   forget(v);
@@ -473,6 +478,33 @@ __global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void po
     const int32_t j = j0 + k * NT * E;
     if (j < cut.whole) store_vec(out + j, grad_vec<T>(v[k], c, mc, g, ce, sl.target - cut.head - j));
   }
+  return l.loss;
+}
+
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
+  __shared__ Shared sh;
+  const uint32_t slot = a.slot0 + first_slot<NT>();
+  if (slot >= a.n_slots) return;
+  const float loss = policy_slot<T, NT, NV>(a, p, slot, sh);
+  if (thread<NT>() == 0) p.token_loss[slot] = loss;
+}
+
+// Examples of up to 16 short rows in one launch: a workgroup an example, a wave a
+// token; the first adds the losses up, in fp64 in the order of the tokens.  256
+// examples of 16 rows of 4 KB take 7.4 us so, 11.9 with sums of their own; with two
+// tokens a wave (8 examples of 32) the sums' launch is the cheaper (5.3 against 8.3).
+template <typename T, int NV>
+__global__ __launch_bounds__(64 * kPolicyExampleMost) void policy_example_kernel(TokenArgs a, PolicyArgs p, float* loss) {
+  __shared__ Shared sh;
+  __shared__ float token[kPolicyExampleMost];
+  const uint32_t t = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float l = policy_slot<T, 64, NV>(a, p, blockIdx.x * a.T + t, sh);
+  if ((threadIdx.x & 63) == 0) token[t] = l;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const double v = wave_sum(threadIdx.x < a.T ? (double)token[threadIdx.x] : 0.0);
+  if (threadIdx.x == 0) loss[blockIdx.x] = (float)v;
 }
 
 // Policy loss of any row length, the row read twice.
@@ -488,12 +520,115 @@ __global__ __launch_bounds__(NT) void policy_stream_kernel(TokenArgs a, PolicyAr
     if (first) p.token_loss[slot] = 0.f;
     return;
   }
+  const PolicyToken in = policy_inputs(p, a, slot, sl);
   const T* z = (const T*)a.logits + sl.row * a.ldl;
   if (first) sh.zy = (float)z[sl.target];  // read before anything of the row is written
   const RowSum r = row_sum_stream<T, NT, 4>(z, a.V, c, sh);
-  const float g = policy_outputs(a, p, slot, sl.row, row_logp(sh.zy, c, r), first);
+  const float logp = row_logp(sh.zy, c, r);
+  const TokenLoss l = policy_token(p, in, logp);
+  if (first) p.token_loss[slot] = l.loss;
+  if (first && a.logp) a.logp[sl.row] = logp;
+  const float g = l.c * a.scale;
   if (a.dlogits)
     row_grad_stream<T, NT, 4>(z, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r, g, -g / r.sum);
+}
+
+// ---------------------------------------------------------------------------
+// few long rows: each in parts, joined
+// ---------------------------------------------------------------------------
+// One CU reads 50 GB/s: a row of 1 MB takes 20 us in one workgroup.  A part's result
+// is its largest element m and the sum of exp2(c (z - m)), without the rounding of
+// c m (0 where the part holds -inf only, so that it adds nothing).
+template <typename T, int NT, int U>
+__device__ inline float2 part_sum(const T* z, int32_t n, float c, Shared& sh) {
+  const RowSum r = row_sum_stream<T, NT, U>(z, n, c, sh);
+  if (!r.apart) return float2{r.top, r.sum * __builtin_amdgcn_exp2f(-fmaf(r.top, c, -r.offset))};
+  if (r.top != -INFINITY) return float2{r.top, r.sum};
+  float s = 0.f;
+#pragma unroll 1
+  for (int32_t j = thread<NT>(); j < n; j += NT) {
+    const float x = (float)z[j];
+    s += x == x ? 0.f : x;
+  }
+  return float2{r.top, block_add<NT>(s, sh.part)};
+}
+
+// A row's sum from its parts (at most 64), by every wave.
+__device__ inline RowSum join_parts(const float2* part, int32_t n, float c) {
+  const int lane = threadIdx.x & 63;
+  const float2 k = lane < n ? part[lane] : float2{-INFINITY, 0.f};
+  const float m = wave_max_dpp(k.x), mc = m * c;
+  const float s = wave_sum_dpp(k.y == 0.f ? 0.f : k.y * __builtin_amdgcn_exp2f((k.x - m) * c));
+  if (fabsf(mc) <= kMostMc) return {mc, s * __builtin_amdgcn_exp2f(fmaf(m, c, -mc)), m, false};
+  return {m, s, m, true};
+}
+
+// Part blockIdx.y of a row: elements [from, from + n).
+struct Range {
+  int32_t from, n;
+};
+__device__ inline Range part_of(const TokenArgs& a) {
+  const int32_t from = (int32_t)blockIdx.y * a.part_len;
+  return {from, a.V - from < a.part_len ? a.V - from : a.part_len};
+}
+
+template <typename T, int NT, int U>
+__global__ __launch_bounds__(NT) void split_sum_kernel(TokenArgs a) {
+  __shared__ Shared sh;
+  const uint32_t slot = blockIdx.x;
+  const Slot sl = slot_of(a, slot);
+  if (!sl.counts) return;
+  const T* z = (const T*)a.logits + sl.row * a.ldl;
+  const Range g = part_of(a);
+  const float zy = (float)z[sl.target];
+  const float2 v = part_sum<T, NT, U>(z + g.from, g.n, a.scale * kLog2e, sh);
+  if (threadIdx.x != 0) return;
+  a.parts[slot * gridDim.y + blockIdx.y] = v;
+  if (blockIdx.y == 0) a.zy[slot] = zy;
+}
+
+// The log-probabilities of rows summed in n_parts parts: a wave a slot.
+template <bool PREF>
+__global__ __launch_bounds__(256) void split_logp_kernel(TokenArgs a, int32_t n_parts, const float* logp_ref) {
+  const uint32_t slot = first_slot<64>();
+  if (slot >= a.n_slots) return;
+  const Slot sl = slot_of(a, slot);
+  const float c = a.scale * kLog2e;
+  if (!sl.counts) {
+    if (thread<64>() == 0) skip_logp<PREF>(a, slot, sl);
+    return;
+  }
+  const RowSum r = join_parts(a.parts + (size_t)slot * n_parts, n_parts, c);
+  if (thread<64>() == 0) write_logp<PREF>(a, slot, sl, row_logp(a.zy[slot], c, r), r, logp_ref);
+}
+
+template <typename T, int NT, int U>
+__global__ __launch_bounds__(NT) void split_policy_kernel(TokenArgs a, PolicyArgs p) {
+  const uint32_t slot = blockIdx.x;
+  const Slot sl = slot_of(a, slot);
+  const Range g = part_of(a);
+  const bool first = blockIdx.y == 0 && threadIdx.x == 0;
+  T* out = a.dlogits ? (T*)a.dlogits + sl.row * a.ldd + g.from : nullptr;
+  if (!sl.counts) {
+    if (first) p.token_loss[slot] = 0.f;
+    if (!sl.write) return;
+    if (first && a.logp) a.logp[sl.row] = 0.f;
+    if (out) row_zero<T, NT>(out, g.n);
+    return;
+  }
+  const PolicyToken in = policy_inputs(p, a, slot, sl);
+  const float c = a.scale * kLog2e;
+  const RowSum r = join_parts(a.parts + (size_t)slot * gridDim.y, gridDim.y, c);
+  const float logp = row_logp(a.zy[slot], c, r);
+  const TokenLoss l = policy_token(p, in, logp);
+  if (first) {
+    p.token_loss[slot] = l.loss;
+    if (a.logp) a.logp[sl.row] = logp;
+  }
+  const float cs = l.c * a.scale;
+  if (out)
+    row_grad_stream<T, NT, U>((const T*)a.logits + sl.row * a.ldl + g.from, out, g.n, sl.target - g.from, c, r, cs,
+                              -cs / r.sum);
 }
 
 __device__ inline double block_sum(double v, double* sh) {
@@ -519,52 +654,77 @@ __global__ __launch_bounds__(256) void example_sum_kernel(const float* __restric
 
 __device__ inline double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
 
-// A pair's log ratios, its loss and the derivative by its log-probabilities.
-__global__ __launch_bounds__(256) void pair_kernel(TokenArgs a, PrefArgs p) {
-  __shared__ double sh[4];
-  for (uint32_t pair = blockIdx.x; pair < p.n_pairs; pair += gridDim.x) {
-    double ratio[2];
+// Sum over NT threads, the result in all of them.
+template <int NT>
+__device__ inline double threads_sum(double v, double* sh) {
+  v = wave_sum(v);
+  if (NT == 64) return v;
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = sh[0];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      const uint32_t i = pair + side * p.n_pairs;
-      double v = 0.0;
-      for (uint32_t t = threadIdx.x; t < a.T; t += 256) {
-        const uint32_t slot = i * a.T + t;
-        const Slot sl = slot_of(a, slot);
-        if (!sl.counts) continue;
-        const double d = (double)a.slot_logp[slot] - (p.logp_ref ? (double)p.logp_ref[sl.row] : 0.0);
-        v += (a.weight ? (double)a.weight[sl.row] : 1.0) * d;
-      }
-      ratio[side] = block_sum(v, sh);
-    }
-    if (threadIdx.x != 0) continue;
-    const double h = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin, e = (double)p.smoothing;
-    const double pw = p.pair_weight ? (double)p.pair_weight[pair] : 1.0;
-    p.loss[pair] = (float)(pw * ((1.0 - e) * softplus(-h) + e * softplus(h)));
+  for (int w = 1; w < NT / 64; ++w) v += sh[w];
+  __syncthreads();
+  return v;
+}
+
+// h of a pair from its tokens' parts; one call writes its loss and log ratios.
+// Returns the derivative of its loss by the log-probability of a chosen token of
+// weight 1.
+template <int NT>
+__device__ inline float pair_coefficient(const TokenArgs& a, const PrefArgs& p, uint32_t pair, bool outputs, double* sh) {
+  double ratio[2];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const double* part = a.part + (size_t)(pair + side * p.n_pairs) * a.T;
+    double v = 0.0;
+    for (uint32_t t = thread<NT>(); t < a.T; t += NT) v += part[t];
+    ratio[side] = threads_sum<NT>(v, sh);
+  }
+  const double h = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin;
+  const float pw = p.pair_weight ? p.pair_weight[pair] : 1.f, e = p.smoothing;
+  if (outputs && thread<NT>() == 0) {
+    p.loss[pair] = (float)((double)pw * ((1.0 - (double)e) * softplus(-h) + (double)e * softplus(h)));
     if (p.log_ratio) {
       p.log_ratio[pair] = (float)ratio[0];
       p.log_ratio[pair + p.n_pairs] = (float)ratio[1];
     }
-    p.coef[pair] = (float)(pw * (double)p.beta * (e / (1.0 + exp(-h)) - (1.0 - e) / (1.0 + exp(h))));
+  }
+  return pw * p.beta * (e / (1.f + expf((float)-h)) - (1.f - e) / (1.f + expf((float)h)));
+}
+
+__global__ __launch_bounds__(256) void pair_kernel(TokenArgs a, PrefArgs p) {
+  __shared__ double sh[4];
+  for (uint32_t pair = blockIdx.x; pair < p.n_pairs; pair += gridDim.x) {
+    const float g = pair_coefficient<256>(a, p, pair, true, sh);
+    if (threadIdx.x == 0) p.coef[pair] = g;
   }
 }
 
-template <typename T, int NT, int U>
+// PAIR: every row forms its pair's sums itself, and the pair's first slot writes its
+// outputs; else they are there.  The grid's second dimension is a row's parts.
+template <typename T, int NT, int U, bool PAIR>
 __global__ __launch_bounds__(group_of(NT)) void pref_grad_kernel(TokenArgs a, PrefArgs p) {
+  __shared__ double sh[16];
   const float c = a.scale * kLog2e;
   const uint32_t slot = a.slot0 + first_slot<NT>();
   if (slot >= a.n_slots) return;
   const Slot sl = slot_of(a, slot);
+  const uint32_t i = slot / a.T, pair = i < p.n_pairs ? i : i - p.n_pairs;
+  const bool outputs = PAIR && slot == pair * a.T && blockIdx.y == 0;
+  const Range part = part_of(a);
+  T* const out = (T*)a.dlogits + sl.row * a.ldd + part.from;
+  float g = 0.f;
+  if (PAIR && (sl.counts || outputs)) g = pair_coefficient<NT>(a, p, pair, outputs, sh);
   if (!sl.counts) {
-    if (sl.write) row_zero<T, NT>((T*)a.dlogits + sl.row * a.ldd, a.V);
+    if (sl.write) row_zero<T, NT>(out, part.n);
     return;
   }
+  if (!PAIR) g = p.coef[pair];
   const float2 st = a.stats[slot];
-  const RowSum r{st.x, fabsf(st.y), st.y < 0.f};
-  const uint32_t i = slot / a.T;
-  const float w = a.weight ? a.weight[sl.row] : 1.f;
-  const float cs = (i < p.n_pairs ? p.coef[i] : -p.coef[i - p.n_pairs]) * w * a.scale, ce = -cs / r.sum;
-  row_grad_stream<T, NT, U>((const T*)a.logits + sl.row * a.ldl, (T*)a.dlogits + sl.row * a.ldd, a.V, sl.target, c, r,
+  const RowSum r{st.x, fabsf(st.y), 0.f, st.y < 0.f};
+  const float cs = (i < p.n_pairs ? g : -g) * sl.weight * a.scale, ce = -cs / r.sum;
+  row_grad_stream<T, NT, U>((const T*)a.logits + sl.row * a.ldl + part.from, out, part.n, sl.target - part.from, c, r,
                             cs, ce);
 }
 
@@ -576,22 +736,37 @@ void launch_slots(void (*kernel)(TokenArgs, K...), TokenArgs a, hipStream_t s, A
   constexpr uint32_t kMost = 1u << 21, kRows = group_of(NT) / NT;
   for (a.slot0 = 0; a.slot0 < a.n_slots; a.slot0 += kMost) {
     const uint32_t n = a.n_slots - a.slot0 < kMost ? a.n_slots - a.slot0 : kMost;
-    hipLaunchKernelGGL(kernel, dim3((n + kRows - 1) / kRows), dim3(group_of(NT)), 0, s, a, args...);
+    hipLaunchKernelGGL(kernel, dim3((n + kRows - 1) / kRows, a.n_parts), dim3(group_of(NT)), 0, s, a, args...);
   }
 }
 
+template <typename T>
+void launch_split_sum(const TokenArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((split_sum_kernel<T, 512, 4>), dim3(a.n_slots, a.n_parts), dim3(512), 0, s, a);
+}
+
 template <typename T, bool PREF>
-void launch_logp(const TokenArgs& a, hipStream_t s) {
+void launch_logp(TokenArgs a, const float* ref, hipStream_t s) {
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (bytes <= 4096) launch_slots<64>(token_logp_kernel<T, 64, 4, PREF>, a, s);
-  else if (bytes <= 65536) launch_slots<256>(token_logp_kernel<T, 256, 4, PREF>, a, s);
-  else if (bytes <= 131072) launch_slots<512>(token_logp_kernel<T, 512, 2, PREF>, a, s);
-  else launch_slots<512>(token_logp_kernel<T, 512, 4, PREF>, a, s);
+  if (a.n_parts > 1) {
+    launch_split_sum<T>(a, s);
+    hipLaunchKernelGGL((split_logp_kernel<PREF>), dim3((a.n_slots + 3) / 4), dim3(256), 0, s, a, (int32_t)a.n_parts, ref);
+    return;
+  }
+  if (bytes <= 4096) launch_slots<64>(token_logp_kernel<T, 64, 4, PREF>, a, s, ref);
+  else if (bytes <= 65536) launch_slots<256>(token_logp_kernel<T, 256, 4, PREF>, a, s, ref);
+  else if (bytes <= 131072) launch_slots<512>(token_logp_kernel<T, 512, 2, PREF>, a, s, ref);
+  else launch_slots<512>(token_logp_kernel<T, 512, 4, PREF>, a, s, ref);
 }
 
 template <typename T>
 void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
+  if (a.n_parts > 1) {
+    launch_split_sum<T>(a, s);
+    hipLaunchKernelGGL((split_policy_kernel<T, 512, 4>), dim3(a.n_slots, a.n_parts), dim3(512), 0, s, a, p);
+    return;
+  }
   if (bytes <= 2048) launch_slots<64>(policy_kernel<T, 64, 2>, a, s, p);
   else if (bytes <= 8192) launch_slots<256>(policy_kernel<T, 256, 2>, a, s, p);
   else if (bytes <= 32768) launch_slots<256>(policy_kernel<T, 256, 8>, a, s, p);
@@ -602,19 +777,56 @@ void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
 }
 
 template <typename T>
+void launch_examples(const TokenArgs& a, const PolicyArgs& p, uint32_t n, float* loss, hipStream_t s) {
+  if ((int64_t)a.V * (int64_t)sizeof(T) <= 2048)
+    hipLaunchKernelGGL((policy_example_kernel<T, 2>), dim3(n), dim3(64 * a.T), 0, s, a, p, loss);
+  else
+    hipLaunchKernelGGL((policy_example_kernel<T, 8>), dim3(n), dim3(64 * a.T), 0, s, a, p, loss);
+}
+
+template <typename T, bool PAIR>
 void launch_grad(const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
   const int64_t bytes = (int64_t)a.V * (int64_t)sizeof(T);
-  if (bytes <= 4096) launch_slots<64>(pref_grad_kernel<T, 64, 4>, a, s, p);
-  else if (bytes <= 65536) launch_slots<256>(pref_grad_kernel<T, 256, 4>, a, s, p);
-  else launch_slots<1024>(pref_grad_kernel<T, 1024, 2>, a, s, p);
+  if (bytes <= 4096) launch_slots<64>(pref_grad_kernel<T, 64, 4, PAIR>, a, s, p);
+  else if (bytes <= 65536) launch_slots<256>(pref_grad_kernel<T, 256, 4, PAIR>, a, s, p);
+  else if (a.n_parts > 1) launch_slots<512>(pref_grad_kernel<T, 512, 4, PAIR>, a, s, p);
+  else launch_slots<1024>(pref_grad_kernel<T, 1024, 2, PAIR>, a, s, p);
 }
 
 }  // namespace
 
-hipError_t launch_token_logp(int dtype, bool pref, const TokenArgs& a, hipStream_t s) {
-  if (dtype == 0) pref ? launch_logp<float, true>(a, s) : launch_logp<float, false>(a, s);
-  else if (dtype == 1) pref ? launch_logp<__bf16, true>(a, s) : launch_logp<__bf16, false>(a, s);
-  else pref ? launch_logp<_Float16, true>(a, s) : launch_logp<_Float16, false>(a, s);
+hipError_t launch_token_logp(int dtype, const TokenArgs& a, hipStream_t s) {
+  if (dtype == 0) launch_logp<float, false>(a, nullptr, s);
+  else if (dtype == 1) launch_logp<__bf16, false>(a, nullptr, s);
+  else launch_logp<_Float16, false>(a, nullptr, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_pref_stats(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
+  if (dtype == 0) launch_logp<float, true>(a, p.logp_ref, s);
+  else if (dtype == 1) launch_logp<__bf16, true>(a, p.logp_ref, s);
+  else launch_logp<_Float16, true>(a, p.logp_ref, s);
+  return hipGetLastError();
+}
+
+// Parts of a row where there are fewer rows than CUs: of 32 KB or more, a thousand in
+// all, from rows of more than 128 KB on (below, the launch that joins them takes as
+// long as it saves).
+int token_parts(int64_t n_slots, int64_t row_bytes) {
+  if (n_slots < 1 || n_slots >= 256 || row_bytes <= 131072) return 1;
+  const int64_t by_size = (row_bytes + 32767) / 32768, by_count = (1024 + n_slots - 1) / n_slots;
+  return (int)(by_size < by_count ? (by_size < 64 ? by_size : 64) : (by_count < 64 ? by_count : 64));
+}
+
+bool policy_by_example(int64_t row_bytes, int64_t T, int64_t n) {
+  return row_bytes <= 8192 && T <= kPolicyExampleMost && n <= 4096;
+}
+
+hipError_t launch_policy_examples(int dtype, const TokenArgs& a, const PolicyArgs& p, uint32_t n, float* loss,
+                                  hipStream_t s) {
+  if (dtype == 0) launch_examples<float>(a, p, n, loss, s);
+  else if (dtype == 1) launch_examples<__bf16>(a, p, n, loss, s);
+  else launch_examples<_Float16>(a, p, n, loss, s);
   return hipGetLastError();
 }
 
@@ -635,10 +847,10 @@ hipError_t launch_pairs(const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_pref_grad(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
-  if (dtype == 0) launch_grad<float>(a, p, s);
-  else if (dtype == 1) launch_grad<__bf16>(a, p, s);
-  else launch_grad<_Float16>(a, p, s);
+hipError_t launch_pref_grad(int dtype, bool pair, const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
+  if (dtype == 0) pair ? launch_grad<float, true>(a, p, s) : launch_grad<float, false>(a, p, s);
+  else if (dtype == 1) pair ? launch_grad<__bf16, true>(a, p, s) : launch_grad<__bf16, false>(a, p, s);
+  else pair ? launch_grad<_Float16, true>(a, p, s) : launch_grad<_Float16, false>(a, p, s);
   return hipGetLastError();
 }
 

@@ -420,3 +420,71 @@ def test_refusals_on_the_device():
     with pytest.raises(ValueError, match="same GPU"):
         P.attr_token_logp(P.TokenRows(z, y.cpu(), 4, 2), torch.zeros(8, device="cuda"))
     assert (loss == 7).all()
+
+
+@pytest.mark.parametrize("V,rows,dtype", [(66001, 260, torch.float32), (40000, 258, torch.float32), (70001, 256, torch.bfloat16),
+                                          (140000, 257, torch.float16), (40003, 100, torch.float32), (262144, 3, torch.float32),
+                                          (300007, 40, torch.bfloat16)])
+def test_long_rows(V, rows, dtype):
+    """Rows past what a workgroup holds, and few long ones in parts, against torch in 64 bits; in place too."""
+    say(f"case: long rows V={V} rows={rows} {NAMES[dtype]}")
+    torch.manual_seed(V)
+    z = (torch.randn(rows, V, device="cuda") * 3).to(dtype)
+    z[0, : V // 2] = -math.inf          # whole parts of nothing
+    z[1] = torch.finfo(dtype).min       # lowest everywhere
+    y = torch.randint(0, V, (rows,), device="cuda")
+    y[0] = V - 1
+    z[torch.arange(2, rows, device="cuda"), y[2:]] += 4
+    if rows > 2:
+        z[2, V - 1] = math.nan
+    w = torch.rand(rows, device="cuda") + 0.5
+    w[rows - 1] = 0
+    adv = torch.randn(rows, device="cuda")
+    lps = torch.log_softmax(z.double(), 1)
+    lp = lps[torch.arange(rows, device="cuda"), y]
+    tol = 4 * U * lp.abs() + rel_sum(V)
+    logp, loss, dl = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"), torch.empty_like(z)
+    tok = P.TokenRows(z, y, rows, 1, weight=w)
+    P.attr_token_logp(tok, logp)
+    live = torch.ones(rows, dtype=torch.bool, device="cuda")
+    live[rows - 1] = False
+    if rows > 3:
+        live[2] = False
+        assert torch.isnan(logp[2])
+    assert ((logp.double() - lp).abs() <= tol)[live].all() and logp[rows - 1] == 0
+    P.attr_policy_loss(tok, adv, loss, logp=logp, dlogits=dl)
+    assert ((logp.double() - lp).abs() <= tol)[live].all()
+    assert (loss[live] == (-adv * w)[live]).all() and loss[rows - 1] == 0  # on policy: ratio 1
+    c = (-adv * w).double()
+
+    def check(got, c):
+        want = -lps.exp() * c[:, None]
+        want[torch.arange(rows, device="cuda"), y] += c
+        err = (got.double() - want).abs()
+        x = (lps.max(1, keepdim=True)[0] - lps).clamp(max=200)
+        bound = want.abs() * ROUND[dtype] * 1.01 + c.abs()[:, None] * lps.exp() * (rel_sum(V) + U * (16 + 4 * x)) + LEAST[dtype]
+        bound[torch.arange(rows, device="cuda"), y] += c.abs() * 8 * U
+        assert (err <= bound)[live].all()
+        assert (got[rows - 1] == 0).all() and (rows <= 3 or torch.isnan(got[2]).all())
+
+    check(dl, c)
+    if rows % 2 == 0:
+        n = rows // 2
+        # NaN rows make their pair NaN: leave the third row out
+        w[2] = 0
+        pl, ratio, pd = torch.zeros(n, device="cuda"), torch.zeros(rows, device="cuda"), torch.empty_like(z)
+        P.attr_preference_loss(tok, pl, log_ratio=ratio, dlogits=pd, beta=0.05)
+        r = torch.where(w > 0, w.double() * lp, 0.0)
+        assert ((ratio.double() - r).abs() <= w.double() * tol + 2 * U * r.abs())[live].all()
+        h = 0.05 * (ratio[:n].double() - ratio[n:].double())
+        g = -0.05 * torch.sigmoid(-h)
+        cp = torch.cat([g, -g]) * w.double()
+        want = -lps.exp() * cp[:, None]
+        want[torch.arange(rows, device="cuda"), y] += cp
+        err = (pd.double() - want).abs()
+        bound = want.abs() * (ROUND[dtype] + 16 * U + rel_sum(V)) * 1.01 + cp.abs()[:, None] * lps.exp() * (rel_sum(V) + U * 900) + LEAST[dtype]
+        bound[torch.arange(rows, device="cuda"), y] += cp.abs() * 16 * U
+        assert (err <= bound)[live].all() and (pd[2] == 0).all()
+        w[2] = 1.0
+    P.attr_policy_loss(tok, adv, loss, dlogits=z)  # in place
+    assert torch.equal(z[live], dl[live])
