@@ -20,13 +20,10 @@
 namespace attr {
 namespace {
 
-constexpr int kQuantBlock = 256;       // elements that share a scale of the 8-bit states: a wave's run
+constexpr int kQuantBlock = kAdamwRun;  // elements that share a scale of the 8-bit states: a wave's run
 constexpr float kE4M3Max = 448.f;
 constexpr float kE4M3Least = 0.001953125f;  // 2^-9, the smallest positive value
 constexpr float kAmaxLeast = 0x1p-100f;     // below it 448 / amax nears fp32's range
-
-constexpr int kRuns = 4;               // runs of a wave
-static_assert(kAdamwChunk == 4 * kRuns * kQuantBlock, "a workgroup of four waves");
 
 // four elements at any element's address
 template <typename T>
@@ -103,13 +100,13 @@ __device__ inline uint8_t e4m3_code(float x) {
 // RUNS runs of a wave from run0 on; all of their elements are there (WHOLE), or some
 // are not.
 template <typename P, typename G, bool EIGHT, bool MASTER, bool WHOLE, int RUNS>
-__device__ inline void adamw_runs(const AdamwArgs& a, const AdamwEntry& t, float gs, int64_t run0) {
+__device__ inline void adamw_runs(const AdamwStep& a, const AdamwEntry& t, const AdamwExtra& ex, float gs, int64_t run0) {
   typedef typename std::conditional<EIGHT, uint8_t, float>::type S;
   typedef typename std::conditional<MASTER, float, P>::type W;
   const int lane = threadIdx.x & 63;
   const float lr = t.lr, lr_wd = t.lr_wd;
   const int64_t i0 = run0 * kQuantBlock + lane * 4;
-  W* const wt = (MASTER ? (W*)t.master : (W*)t.p) + i0;
+  W* const wt = (MASTER ? (W*)ex.master : (W*)t.p) + i0;
   P* const pt = (P*)t.p + i0;
   const G* const gt = (const G*)t.g + i0;
   S* const mt = (S*)t.m + i0;
@@ -121,20 +118,20 @@ __device__ inline void adamw_runs(const AdamwArgs& a, const AdamwEntry& t, float
 #pragma unroll
   for (int u = 0; u < RUNS; ++u) {
     const int k = u * kQuantBlock;
-    const int in = t.n - i0 - k >= 4 ? 4 : (int)(t.n - i0 - k);
+    const int in = (int64_t)t.n - i0 - k >= 4 ? 4 : (int)((int64_t)t.n - i0 - k);
     load4<WHOLE>(wt + k, in, x[u]);
     load4<WHOLE>(gt + k, in, g[u]);
     load4<WHOLE>(mt + k, in, m[u]);
     load4<WHOLE>(vt + k, in, v[u]);
     if (EIGHT) {
-      ms[u] = t.m_scale[run0 + u];
-      vs[u] = t.v_scale[run0 + u];
+      ms[u] = ex.m_scale[run0 + u];
+      vs[u] = ex.v_scale[run0 + u];
     }
   }
 #pragma unroll
   for (int u = 0; u < RUNS; ++u) {
     const int k = u * kQuantBlock;
-    const int in = t.n - i0 - k >= 4 ? 4 : (int)(t.n - i0 - k);
+    const int in = (int64_t)t.n - i0 - k >= 4 ? 4 : (int)((int64_t)t.n - i0 - k);
     float nm[4], nv[4];
     W nx[4];
     P np[4];
@@ -180,8 +177,8 @@ __device__ inline void adamw_runs(const AdamwArgs& a, const AdamwEntry& t, float
       store4<WHOLE>(mt + k, in, qm);
       store4<WHOLE>(vt + k, in, qv);
       if (lane == 0) {
-        t.m_scale[run0 + u] = am < INFINITY ? am * (1.f / kE4M3Max) : NAN;
-        t.v_scale[run0 + u] = av < INFINITY ? av * (1.f / kE4M3Max) : NAN;
+        ex.m_scale[run0 + u] = am < INFINITY ? am * (1.f / kE4M3Max) : NAN;
+        ex.v_scale[run0 + u] = av < INFINITY ? av * (1.f / kE4M3Max) : NAN;
       }
     } else {
       store4<WHOLE>(mt + k, in, nm);
@@ -190,49 +187,70 @@ __device__ inline void adamw_runs(const AdamwArgs& a, const AdamwEntry& t, float
   }
 }
 
-template <typename P, typename G, bool EIGHT, bool MASTER>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
-  int lo = 0, hi = a.n - 1;  // the last tensor whose first chunk is not past this workgroup
+template <typename P, typename G, bool EIGHT, bool MASTER, int RUNS, typename Args>
+__global__ __launch_bounds__(256) void adamw_kernel(Args a) {
+  int lo = 0, hi = a.step.n - 1;  // the last tensor whose first chunk is not past this workgroup
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.e[mid].chunk0 <= blockIdx.x) lo = mid;
     else hi = mid - 1;
   }
   const AdamwEntry& t = a.e[lo];
-  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
-  const int64_t run0 = ((int64_t)(blockIdx.x - t.chunk0) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kRuns;
-  if ((run0 + kRuns) * kQuantBlock <= t.n) {
-    adamw_runs<P, G, EIGHT, MASTER, true, kRuns>(a, t, gs, run0);
+  AdamwExtra ex{};
+  if constexpr (EIGHT || MASTER) ex = a.x[lo];
+  const float gs = a.step.grad_scale ? *a.step.grad_scale : 1.f;
+  const int64_t run0 = ((int64_t)(blockIdx.x - t.chunk0) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * RUNS;
+  if ((run0 + RUNS) * kQuantBlock <= t.n) {
+    adamw_runs<P, G, EIGHT, MASTER, true, RUNS>(a.step, t, ex, gs, run0);
   } else {
 #pragma unroll 1
-    for (int64_t r = run0; r < run0 + kRuns && r * kQuantBlock < t.n; ++r)
-      adamw_runs<P, G, EIGHT, MASTER, false, 1>(a, t, gs, r);
+    for (int64_t r = run0; r < run0 + RUNS && r * kQuantBlock < t.n; ++r)
+      adamw_runs<P, G, EIGHT, MASTER, false, 1>(a.step, t, ex, gs, r);
   }
 }
 
-template <typename P, typename G>
-void launch(bool eight, bool master, uint32_t blocks, const AdamwArgs& a, hipStream_t s) {
-  const dim3 grid(blocks), block(256);
-  if (eight && master) hipLaunchKernelGGL((adamw_kernel<P, G, true, true>), grid, block, 0, s, a);
-  else if (eight) hipLaunchKernelGGL((adamw_kernel<P, G, true, false>), grid, block, 0, s, a);
-  else if (master) hipLaunchKernelGGL((adamw_kernel<P, G, false, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((adamw_kernel<P, G, false, false>), grid, block, 0, s, a);
+template <typename P, typename G, bool EIGHT, bool MASTER, typename Args>
+void launch_runs(int runs, uint32_t blocks, const Args& a, hipStream_t s) {
+  if (runs == 1) hipLaunchKernelGGL((adamw_kernel<P, G, EIGHT, MASTER, 1, Args>), dim3(blocks), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((adamw_kernel<P, G, EIGHT, MASTER, 4, Args>), dim3(blocks), dim3(256), 0, s, a);
 }
-template <typename P>
-void launch_g(int g_dtype, bool eight, bool master, uint32_t blocks, const AdamwArgs& a, hipStream_t s) {
-  if (g_dtype == 0) launch<P, float>(eight, master, blocks, a, s);
-  else if (g_dtype == 1) launch<P, __bf16>(eight, master, blocks, a, s);
-  else launch<P, _Float16>(eight, master, blocks, a, s);
+template <typename P, typename G>
+void launch(bool, bool, int runs, uint32_t blocks, const AdamwPlain& a, hipStream_t s) {
+  launch_runs<P, G, false, false>(runs, blocks, a, s);
+}
+template <typename P, typename G>
+void launch(bool eight, bool master, int runs, uint32_t blocks, const AdamwFull& a, hipStream_t s) {
+  if (eight && master) launch_runs<P, G, true, true>(runs, blocks, a, s);
+  else if (eight) launch_runs<P, G, true, false>(runs, blocks, a, s);
+  else launch_runs<P, G, false, true>(runs, blocks, a, s);
+}
+template <typename P, typename Args>
+void launch_g(int g_dtype, bool eight, bool master, int runs, uint32_t blocks, const Args& a, hipStream_t s) {
+  if (g_dtype == 0) launch<P, float>(eight, master, runs, blocks, a, s);
+  else if (g_dtype == 1) launch<P, __bf16>(eight, master, runs, blocks, a, s);
+  else launch<P, _Float16>(eight, master, runs, blocks, a, s);
+}
+template <typename Args>
+hipError_t launch_p(int p_dtype, int g_dtype, bool eight, bool master, int runs, uint32_t blocks, const Args& a,
+                    hipStream_t s) {
+  if (p_dtype == 0) launch_g<float>(g_dtype, eight, master, runs, blocks, a, s);
+  else if (p_dtype == 1) launch_g<__bf16>(g_dtype, eight, master, runs, blocks, a, s);
+  else launch_g<_Float16>(g_dtype, eight, master, runs, blocks, a, s);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, bool master, uint32_t blocks, const AdamwArgs& a,
-                        hipStream_t s) {
-  if (p_dtype == 0) launch_g<float>(g_dtype, eight, master, blocks, a, s);
-  else if (p_dtype == 1) launch_g<__bf16>(g_dtype, eight, master, blocks, a, s);
-  else launch_g<_Float16>(g_dtype, eight, master, blocks, a, s);
-  return hipGetLastError();
+// Four runs keep 16 KB of each wave in flight; small models take one, for four times
+// the waves.
+int adamw_runs_per_wave(int64_t elements) { return elements < (8 << 20) ? 1 : 4; }
+
+hipError_t launch_adamw(int p_dtype, int g_dtype, int runs, uint32_t blocks, const AdamwPlain& a, hipStream_t s) {
+  return launch_p(p_dtype, g_dtype, false, false, runs, blocks, a, s);
+}
+hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, bool master, int runs, uint32_t blocks,
+                        const AdamwFull& a, hipStream_t s) {
+  return launch_p(p_dtype, g_dtype, eight, master, runs, blocks, a, s);
 }
 
 }  // namespace attr

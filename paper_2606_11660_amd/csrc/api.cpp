@@ -865,6 +865,58 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
 // ---------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------
+namespace {
+
+// Gathers tensors into launches.
+struct AdamwLaunch {
+  int p_dtype, g_dtype;
+  bool eight;
+  int runs;
+  attr::AdamwStep step;
+  hipStream_t stream;
+  bool master = false;  // of the launch being filled
+  uint32_t blocks = 0;
+  attr::AdamwPlain plain = {};
+  attr::AdamwFull full = {};
+
+  hipError_t add(attr::AdamwEntry e, const attr::AdamwExtra& x) {
+    const uint32_t chunk = 4 * (uint32_t)runs * attr::kAdamwRun, need = (uint32_t)(((uint64_t)e.n + chunk - 1) / chunk);
+    const int most = eight || x.master ? attr::kAdamwMostExtra : attr::kAdamwMost;
+    // below 2^32 threads a launch
+    if (step.n >= most || blocks + need > (1u << 23) || master != (x.master != nullptr)) {
+      const hipError_t r = flush();
+      if (r != hipSuccess) return r;
+    }
+    master = x.master != nullptr;
+    e.chunk0 = blocks;
+    if (eight || master) {
+      full.e[step.n] = e;
+      full.x[step.n] = x;
+    } else {
+      plain.e[step.n] = e;
+    }
+    ++step.n;
+    blocks += need;
+    return hipSuccess;
+  }
+  hipError_t flush() {
+    if (step.n == 0) return hipSuccess;
+    hipError_t r;
+    if (eight || master) {
+      full.step = step;
+      r = attr::launch_adamw(p_dtype, g_dtype, eight, master, runs, blocks, full, stream);
+    } else {
+      plain.step = step;
+      r = attr::launch_adamw(p_dtype, g_dtype, runs, blocks, plain, stream);
+    }
+    step.n = 0;
+    blocks = 0;
+    return r;
+  }
+};
+
+}  // namespace
+
 attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors, attr_dtype p_dtype,
                             attr_dtype g_dtype, attr_dtype state_dtype, int64_t step, double lr,
                             double beta1, double beta2, double eps, double eps_root,
@@ -899,56 +951,43 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
           !aligned_to(t.master, 4) || !aligned_to(t.m_scale, 4) || !aligned_to(t.v_scale, 4))
         return fail(ATTR_ERR_ALIGNMENT, "%s: tensor %d: pointers must be aligned to their elements", who, j);
     }
-    attr::AdamwArgs a;
-    std::memset(&a, 0, sizeof(a));
-    a.grad_scale = grad_scale;
-    a.beta1 = (float)beta1;
-    a.one_beta1 = (float)(1.0 - beta1);
-    a.beta2 = (float)beta2;
-    a.one_beta2 = (float)(1.0 - beta2);
-    a.corr1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)step)));
-    a.corr2 = (float)(1.0 / (1.0 - std::pow(beta2, (double)step)));
-    a.eps = (float)eps;
-    a.eps_root = (float)eps_root;
+    attr::AdamwStep h;
+    std::memset(&h, 0, sizeof(h));
+    h.grad_scale = grad_scale;
+    h.beta1 = (float)beta1;
+    h.one_beta1 = (float)(1.0 - beta1);
+    h.beta2 = (float)beta2;
+    h.one_beta2 = (float)(1.0 - beta2);
+    h.corr1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)step)));
+    h.corr2 = (float)(1.0 / (1.0 - std::pow(beta2, (double)step)));
+    h.eps = (float)eps;
+    h.eps_root = (float)eps_root;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    uint32_t blocks = 0;
-    bool master = false;  // of the launch being filled
-    auto flush = [&]() -> hipError_t {
-      if (a.n == 0) return hipSuccess;
-      const hipError_t e = attr::launch_adamw((int)p_dtype, (int)g_dtype, eight, master, blocks, a, s);
-      a.n = 0;
-      blocks = 0;
-      return e;
-    };
-    constexpr uint32_t kMostBlocks = 1u << 22;
+    int64_t total = 0;
+    for (int32_t j = 0; j < n_tensors; ++j) total = std::min(total + tensors[j].n, (int64_t)1 << 40);
+    AdamwLaunch L{(int)p_dtype, (int)g_dtype, eight, attr::adamw_runs_per_wave(total), h, s};
     for (int32_t j = 0; j < n_tensors; ++j) {
       const attr_adamw_tensor& t = tensors[j];
-      // a tensor of more workgroups than a launch takes comes in pieces of whole blocks
-      for (int64_t at = 0; at < t.n; at += (int64_t)kMostBlocks * attr::kAdamwChunk) {
-        const int64_t n = std::min(t.n - at, (int64_t)kMostBlocks * attr::kAdamwChunk);
-        const uint32_t need = (uint32_t)((n + attr::kAdamwChunk - 1) / attr::kAdamwChunk);
-        if (a.n == attr::kAdamwMax || blocks + need > kMostBlocks || master != (t.master != nullptr)) {
-          const hipError_t e = flush();
-          if (e != hipSuccess) return device_fail(e, "attr_adamw_step launch");
-        }
-        master = t.master != nullptr;
-        attr::AdamwEntry& x = a.e[a.n++];
-        x.p = static_cast<char*>(t.p) + (size_t)at * pb;
-        x.g = static_cast<const char*>(t.g) + (size_t)at * gb;
-        x.m = static_cast<char*>(t.m) + (size_t)at * sb;
-        x.v = static_cast<char*>(t.v) + (size_t)at * sb;
-        x.master = t.master ? t.master + at : nullptr;
-        x.m_scale = t.m_scale ? t.m_scale + at / 256 : nullptr;
-        x.v_scale = t.v_scale ? t.v_scale + at / 256 : nullptr;
-        x.n = n;
-        x.lr = (float)(lr * (double)t.lr_scale);
-        x.lr_wd = (float)(lr * (double)t.lr_scale * (double)t.weight_decay);
-        x.chunk0 = blocks;
-        blocks += need;
+      // pieces of whole blocks whose sizes fit 32 bits
+      constexpr int64_t kMost = 1ll << 31;
+      for (int64_t at = 0; at < t.n; at += kMost) {
+        attr::AdamwEntry e;
+        e.p = static_cast<char*>(t.p) + (size_t)at * pb;
+        e.g = static_cast<const char*>(t.g) + (size_t)at * gb;
+        e.m = static_cast<char*>(t.m) + (size_t)at * sb;
+        e.v = static_cast<char*>(t.v) + (size_t)at * sb;
+        e.lr = (float)(lr * (double)t.lr_scale);
+        e.lr_wd = (float)(lr * (double)t.lr_scale * (double)t.weight_decay);
+        e.n = (uint32_t)std::min(t.n - at, kMost);
+        e.chunk0 = 0;
+        const attr::AdamwExtra x{t.master ? t.master + at : nullptr, t.m_scale ? t.m_scale + at / 256 : nullptr,
+                                 t.v_scale ? t.v_scale + at / 256 : nullptr};
+        const hipError_t r = L.add(e, x);
+        if (r != hipSuccess) return device_fail(r, "attr_adamw_step launch");
       }
     }
-    const hipError_t e = flush();
-    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_adamw_step launch");
+    const hipError_t r = L.flush();
+    return r == hipSuccess ? ATTR_OK : device_fail(r, "attr_adamw_step launch");
   } catch (...) {
     return fail(ATTR_ERR_INVALID_ARG, "attr_adamw_step: host exception");
   }

@@ -247,32 +247,48 @@ hipError_t launch_pref_grad(int dtype, bool pair, const TokenArgs& a, const Pref
 // ---------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------
-// One tensor of a launch; descriptors travel in kernel arguments (4096 bytes).
+// One tensor, or a piece of one, of a launch; descriptors travel in kernel arguments
+// (4096 bytes).  What only masters and 8-bit states need is apart: 84 tensors a launch
+// without it, 55 with it.
 struct AdamwEntry {
   void* p;
   const void* g;
   void* m;
   void* v;
+  float lr, lr_wd;
+  uint32_t n;       // elements
+  uint32_t chunk0;  // first workgroup
+};
+struct AdamwExtra {
   float* master;
   float* m_scale;
   float* v_scale;
-  int64_t n;
-  float lr, lr_wd;
-  uint32_t chunk0;  // first workgroup
-  uint32_t pad;
 };
-constexpr int kAdamwMax = 48;
-constexpr int64_t kAdamwChunk = 4096;  // elements of a workgroup, a multiple of the 8-bit states' 256
-struct AdamwArgs {
-  AdamwEntry e[kAdamwMax];
+constexpr int kAdamwMost = 84, kAdamwMostExtra = 55;
+struct AdamwStep {
   const float* grad_scale;  // or null
   float beta1, one_beta1, beta2, one_beta2, corr1, corr2, eps, eps_root;
   int32_t n;
 };
-static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
-// Every tensor of a launch has a master, or none has.
-hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, bool master, uint32_t blocks, const AdamwArgs& a,
-                        hipStream_t s);
+struct AdamwPlain {
+  AdamwStep step;
+  AdamwEntry e[kAdamwMost];
+};
+struct AdamwFull {
+  AdamwStep step;
+  AdamwEntry e[kAdamwMostExtra];
+  AdamwExtra x[kAdamwMostExtra];
+};
+static_assert(sizeof(AdamwPlain) <= 4096 && sizeof(AdamwFull) <= 4096, "kernel arguments");
+// A wave takes runs of 256 elements (a block of the 8-bit states), a workgroup four
+// waves' chunk of them.
+constexpr int kAdamwRun = 256;
+int adamw_runs_per_wave(int64_t elements);
+// Every tensor of a launch has a master, or none has.  AdamwPlain: no masters, 32-bit
+// states.
+hipError_t launch_adamw(int p_dtype, int g_dtype, int runs, uint32_t blocks, const AdamwPlain& a, hipStream_t s);
+hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, bool master, int runs, uint32_t blocks,
+                        const AdamwFull& a, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // calibration
