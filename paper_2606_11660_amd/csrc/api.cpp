@@ -799,8 +799,10 @@ attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage
           attr::launch_policy_examples((int)rows->dtype, a, p, (uint32_t)rows->n_examples, loss, s);
       return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_policy_loss launch");
     }
+    if (rows->T == 1) p.token_loss = loss;  // an example is its token
     hipError_t e = attr::launch_policy_rows((int)rows->dtype, a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_policy_loss launch");
+    if (rows->T == 1) return ATTR_OK;
     e = attr::launch_example_sum(p.token_loss, a.T, (uint32_t)rows->n_examples, loss, s);
     return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_policy_loss sum launch");
   } catch (...) {
@@ -849,6 +851,10 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
     p.margin = margin;
     p.smoothing = label_smoothing;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (attr::pref_by_pair(rows->V * dtype_bytes(rows->dtype), rows->T, p.n_pairs)) {
+      const hipError_t e = attr::launch_pref_pairs((int)rows->dtype, a, p, s);
+      return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_preference_loss launch");
+    }
     hipError_t e = attr::launch_pref_stats((int)rows->dtype, a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_preference_loss launch");
     const bool pair = dlogits && rows->T <= 1024 && a.n_slots <= 2048;

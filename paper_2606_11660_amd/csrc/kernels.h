@@ -234,12 +234,15 @@ hipError_t launch_token_logp(int dtype, const TokenArgs& a, hipStream_t s);
 // Policy loss: token losses of every slot, then their sums; or both at once.
 hipError_t launch_policy_rows(int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s);
 hipError_t launch_example_sum(const float* token_loss, uint32_t T, uint32_t n, float* loss, hipStream_t s);
-constexpr uint32_t kPolicyExampleMost = 16;  // tokens of an example
+constexpr uint32_t kPolicyExampleMost = 32;  // tokens of an example
 bool policy_by_example(int64_t row_bytes, int64_t T, int64_t n_examples);
 hipError_t launch_policy_examples(int dtype, const TokenArgs& a, const PolicyArgs& p, uint32_t n, float* loss,
                                   hipStream_t s);
-// Preference loss: a row's sums and its share of the log ratio; the pairs; the
-// gradient, with the pairs (pair) or after them.
+// Preference loss: all of it at once; or a row's sums and its share of the log ratio,
+// the pairs, and the gradient, with the pairs (pair) or after them.
+constexpr uint32_t kPrefPairMost = 16;  // tokens of a sequence
+bool pref_by_pair(int64_t row_bytes, int64_t T, int64_t n_pairs);
+hipError_t launch_pref_pairs(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 hipError_t launch_pref_stats(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 hipError_t launch_pairs(const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 hipError_t launch_pref_grad(int dtype, bool pair, const TokenArgs& a, const PrefArgs& p, hipStream_t s);

@@ -230,6 +230,9 @@ __device__ inline float row_logp(float zy, float c, const RowSum& r) {
   return (exponent(zy, c, r) - log2f(r.sum)) * kLn2;
 }
 
+// Whether the fused form takes a row (part) with maximum m; not if it is NaN.
+__device__ inline bool fused(float m, float c) { return fabsf(m * c) <= kMostMc; }
+
 // The sum with the differences formed first, one element at a time: rows whose
 // maximum m the fused form does not take.
 template <typename T, int NT>
@@ -309,7 +312,7 @@ __device__ inline RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& 
     }
   }
   const float m = block_max<NT>(top, sh.max);
-  if (!(fabsf(m * c) <= kMostMc)) return row_sum_apart<T, NT>(z, V, c, m, sh.slow);
+  if (!fused(m, c)) return row_sum_apart<T, NT>(z, V, c, m, sh.slow);
   const float most = m * c;
   s *= __builtin_amdgcn_exp2f(mc - most);
   return {most, block_add<NT>(s, sh.sum), m, false};
@@ -381,9 +384,18 @@ __device__ inline void skip_slot(const TokenArgs& a, const Slot& sl) {
 // Threads of a workgroup whose rows are swept by NT threads each.
 constexpr int group_of(int nt) { return nt == 64 ? 256 : nt; }
 
-// A slot's log-probability, and (PREF) what the preference loss keeps of it.
-// The log ratios are small differences of sums: there the logarithm and its
-// differences are in fp64.
+// A counting token's share of its log ratio; one thread writes its log-probability.  The
+// ratios are small differences of sums: here the logarithm and its differences are in
+// fp64.
+__device__ inline double token_part(const TokenArgs& a, const Slot& sl, float zy, float c, const RowSum& r,
+                                    const float* logp_ref) {
+  const double x = r.apart ? ((double)zy - (double)r.offset) * (double)c : (double)zy * (double)c - (double)r.offset;
+  const double logp = (x - log2((double)r.sum)) * 0.6931471805599453;
+  if (thread<64>() == 0 && a.logp) a.logp[sl.row] = (float)logp;
+  return (double)sl.weight * (logp - (logp_ref ? (double)logp_ref[sl.row] : 0.0));
+}
+
+// A slot's log-probability, and (PREF) what the preference loss keeps of it: one thread.
 template <bool PREF>
 __device__ inline void write_logp(const TokenArgs& a, uint32_t slot, const Slot& sl, float zy, float c,
                                   const RowSum& r, const float* logp_ref) {
@@ -391,10 +403,7 @@ __device__ inline void write_logp(const TokenArgs& a, uint32_t slot, const Slot&
     a.logp[sl.row] = row_logp(zy, c, r);
     return;
   }
-  const double x = r.apart ? ((double)zy - (double)r.offset) * (double)c : (double)zy * (double)c - (double)r.offset;
-  const double logp = (x - log2((double)r.sum)) * 0.6931471805599453;
-  if (a.logp) a.logp[sl.row] = (float)logp;
-  a.part[slot] = (double)sl.weight * (logp - (logp_ref ? (double)logp_ref[sl.row] : 0.0));
+  a.part[slot] = token_part(a, sl, zy, c, r, logp_ref);
   a.stats[slot] = float2{r.offset, r.apart ? -r.sum : r.sum};
 }
 template <bool PREF>
@@ -423,97 +432,138 @@ __global__ __launch_bounds__(group_of(NT)) void token_logp_kernel(TokenArgs a, c
   if (thread<NT>() == 0) write_logp<PREF>(a, slot, sl, zy, c, r, logp_ref);
 }
 
-// Policy loss of one slot with the row in registers: NV vectors a thread,
-// V <= NT NV kE.  Returns the token's loss.
+// A row in the registers of NT threads, NV vectors each: V <= NT NV kE.
 template <typename T, int NT, int NV>
-__device__ inline float policy_slot(const TokenArgs& a, const PolicyArgs& p, uint32_t slot, Shared& sh) {
-  constexpr int E = kE<T>;
-  const float c = a.scale * kLog2e;
-  const int32_t V = a.V;
-  const Slot sl = slot_of(a, slot);
-  const bool first = thread<NT>() == 0;
-  if (!sl.counts) {
-    skip_slot<T, NT>(a, sl);
-    return 0.f;
-  }
-  const PolicyToken in = policy_inputs(p, a, slot, sl);
-  const T* z = (const T*)a.logits + sl.row * a.ldl;
-  const float zy = (float)z[sl.target];
-  const Cut cut = cut_row<T, NT>(z, V);
-  const T rest = cut.at < V ? z[cut.at] : (T)-INFINITY;
+struct RowRegs {
+  static constexpr int E = kE<T>;
+  const T* z;
+  Cut cut;
+  T rest;
   i32x4 v[NV];
+
+  __device__ inline void load(const T* row, int32_t V) {
+    z = row;
+    cut = cut_row<T, NT>(z, V);
+    rest = cut.at < V ? z[cut.at] : (T)-INFINITY;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int32_t j = (k * NT + thread<NT>()) * E;
-    v[k] = j < cut.whole ? load_vec(z + cut.head + j) : no_vec(T{});
+    for (int k = 0; k < NV; ++k) {
+      const int32_t j = (k * NT + thread<NT>()) * E;
+      v[k] = j < cut.whole ? load_vec(z + cut.head + j) : no_vec(T{});
+    }
   }
-  float top = fmaxf(zy, (float)rest);  // zy, an element of the row, is read before anything of it is written
+  // The row's maximum; `also` is an element of it, read before anything is written.
+  __device__ inline float top(float also, Shared& sh) {
+    float m = fmaxf(also, (float)rest);
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    float x[E];
-    unpack(v[k], T{}, x);
+    for (int k = 0; k < NV; ++k) {
+      float x[E];
+      unpack(v[k], T{}, x);
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = fmaxf(top, x[e]);
+      for (int e = 0; e < E; ++e) m = fmaxf(m, x[e]);
+    }
+    return block_max<NT>(m, sh.max);
   }
-  const float m = block_max<NT>(top, sh.max), mc = m * c;
-  if (!(fabsf(mc) <= kMostMc)) {
-    const RowSum r = row_sum_apart<T, NT>(z, V, c, m, sh.slow);
+  // Its sum in the fused form.
+  __device__ inline RowSum sum(float m, float c, Shared& sh) {
+    const float mc = m * c;
+    forget(v);
+    float s = __builtin_amdgcn_exp2f(fmaf((float)rest, c, -mc));
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float x[E];
+      unpack(v[k], T{}, x);
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
+    }
+    return {mc, block_add<NT>(s, sh.sum), m, false};
+  }
+  // g ([j = y] - p_j) into out
+  __device__ inline void grad(T* out, int32_t V, int32_t y, float c, const RowSum& r, float g) {
+    const float ce = -g / r.sum;
+    if (cut.at < V) out[cut.at] = grad_one(rest, c, r.offset, g, ce, cut.at == y);
+    out += cut.head;
+    forget(v);
+    int32_t j0 = thread<NT>() * E;
+    forget(j0);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int32_t j = j0 + k * NT * E;
+      if (j < cut.whole) store_vec(out + j, grad_vec<T>(v[k], c, r.offset, g, ce, y - cut.head - j));
+    }
+  }
+};
+// One slot of the policy loss, its row in registers.
+template <typename T, int NT, int NV>
+struct PolicySlot {
+  Slot sl;
+  PolicyToken in;
+  float zy;
+  RowRegs<T, NT, NV> row;
+
+  __device__ inline void load(const TokenArgs& a, const PolicyArgs& p, uint32_t slot) {
+    sl = slot_of(a, slot);
+    if (!sl.counts) return;
+    in = policy_inputs(p, a, slot, sl);
+    const T* z = (const T*)a.logits + sl.row * a.ldl;
+    zy = (float)z[sl.target];
+    row.load(z, a.V);
+  }
+  // Writes the row's outputs; returns the token's loss.
+  __device__ inline float finish(const TokenArgs& a, const PolicyArgs& p, Shared& sh) {
+    if (!sl.counts) {
+      skip_slot<T, NT>(a, sl);
+      return 0.f;
+    }
+    const float c = a.scale * kLog2e;
+    T* out = (T*)a.dlogits + sl.row * a.ldd;
+    const float m = row.top(zy, sh);
+    if (!fused(m, c)) {  // a path of its own, which needs no registers
+      const RowSum r = row_sum_apart<T, NT>(row.z, a.V, c, m, sh.slow);
+      const float logp = row_logp(zy, c, r);
+      const TokenLoss l = policy_token(p, in, logp);
+      if (thread<NT>() == 0 && a.logp) a.logp[sl.row] = logp;
+      if (a.dlogits) row_grad_apart<T, NT>(row.z, out, a.V, sl.target, c, r, l.c * a.scale, -l.c * a.scale / r.sum);
+      return l.loss;
+    }
+    const RowSum r = row.sum(m, c, sh);
     const float logp = row_logp(zy, c, r);
     const TokenLoss l = policy_token(p, in, logp);
-    if (first && a.logp) a.logp[sl.row] = logp;
-    const float g = l.c * a.scale;
-    if (a.dlogits) row_grad_apart<T, NT>(z, (T*)a.dlogits + sl.row * a.ldd, V, sl.target, c, r, g, -g / r.sum);
+    if (thread<NT>() == 0 && a.logp) a.logp[sl.row] = logp;
+    if (a.dlogits) row.grad(out, a.V, sl.target, c, r, l.c * a.scale);
     return l.loss;
   }
-  forget(v);
-  float s = __builtin_amdgcn_exp2f(fmaf((float)rest, c, -mc));
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    float x[E];
-    unpack(v[k], T{}, x);
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
-  }
-  const RowSum r{mc, block_add<NT>(s, sh.sum), m, false};
-  const float logp = row_logp(zy, c, r);
-  const TokenLoss l = policy_token(p, in, logp);
-  if (first && a.logp) a.logp[sl.row] = logp;
-  if (!a.dlogits) return l.loss;
-  T* out = (T*)a.dlogits + sl.row * a.ldd;
-  const float g = l.c * a.scale, ce = -g / r.sum;
-  if (cut.at < V) out[cut.at] = grad_one(rest, c, mc, g, ce, cut.at == sl.target);
-  out += cut.head;
-  forget(v);
-  int32_t j0 = thread<NT>() * E;
-  forget(j0);
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int32_t j = j0 + k * NT * E;
-    if (j < cut.whole) store_vec(out + j, grad_vec<T>(v[k], c, mc, g, ce, sl.target - cut.head - j));
-  }
-  return l.loss;
-}
+};
 
 template <typename T, int NT, int NV>
 __global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
   __shared__ Shared sh;
   const uint32_t slot = a.slot0 + first_slot<NT>();
   if (slot >= a.n_slots) return;
-  const float loss = policy_slot<T, NT, NV>(a, p, slot, sh);
+  PolicySlot<T, NT, NV> k;
+  k.load(a, p, slot);
+  const float loss = k.finish(a, p, sh);
   if (thread<NT>() == 0) p.token_loss[slot] = loss;
 }
 
-// Examples of up to 16 short rows in one launch: a workgroup an example, a wave a
-// token; the first adds the losses up, in fp64 in the order of the tokens.  256
-// examples of 16 rows of 4 KB take 7.4 us so, 11.9 with sums of their own; with two
-// tokens a wave (8 examples of 32) the sums' launch is the cheaper (5.3 against 8.3).
-template <typename T, int NV>
-__global__ __launch_bounds__(64 * kPolicyExampleMost) void policy_example_kernel(TokenArgs a, PolicyArgs p, float* loss) {
+// Examples of few short rows in one launch: a workgroup an example, K tokens a wave
+// with all of their rows in flight; the first wave adds the losses up, in fp64 in the
+// order of the tokens.
+template <typename T, int NV, int K>
+__global__ __launch_bounds__(1024) void policy_example_kernel(TokenArgs a, PolicyArgs p, float* loss) {
   __shared__ Shared sh;
   __shared__ float token[kPolicyExampleMost];
-  const uint32_t t = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const float l = policy_slot<T, 64, NV>(a, p, blockIdx.x * a.T + t, sh);
-  if ((threadIdx.x & 63) == 0) token[t] = l;
+  const uint32_t t0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), step = blockDim.x >> 6;
+  PolicySlot<T, 64, NV> k[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i)
+    if (t0 + i * step < a.T) k[i].load(a, p, blockIdx.x * a.T + t0 + i * step);
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const uint32_t t = t0 + i * step;
+    if (t >= a.T) continue;
+    const float l = k[i].finish(a, p, sh);
+    if ((threadIdx.x & 63) == 0) token[t] = l;
+  }
   __syncthreads();
   if (threadIdx.x >= 64) return;
   const double v = wave_sum(threadIdx.x < a.T ? (double)token[threadIdx.x] : 0.0);
@@ -572,7 +622,7 @@ __device__ inline RowSum join_parts(const float2* part, int32_t n, float c) {
   const float2 k = lane < n ? part[lane] : float2{-INFINITY, 0.f};
   const float m = wave_max_dpp(k.x), mc = m * c;
   const float s = wave_sum_dpp(k.y == 0.f ? 0.f : k.y * __builtin_amdgcn_exp2f((k.x - m) * c));
-  if (fabsf(mc) <= kMostMc) return {mc, s * __builtin_amdgcn_exp2f(fmaf(m, c, -mc)), m, false};
+  if (fused(m, c)) return {mc, s * __builtin_amdgcn_exp2f(fmaf(m, c, -mc)), m, false};
   return {m, s, m, true};
 }
 
@@ -681,9 +731,22 @@ __device__ inline double threads_sum(double v, double* sh) {
   return v;
 }
 
-// h of a pair from its tokens' parts; one call writes its loss and log ratios.
-// Returns the derivative of its loss by the log-probability of a chosen token of
-// weight 1.
+// A pair's loss from its log ratios (written where `outputs`); returns the derivative
+// by the log-probability of a chosen token of weight 1.
+__device__ inline float pair_loss(const PrefArgs& p, uint32_t pair, const double (&ratio)[2], bool outputs) {
+  const double h = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin;
+  const float pw = p.pair_weight ? p.pair_weight[pair] : 1.f, e = p.smoothing;
+  if (outputs) {
+    p.loss[pair] = (float)((double)pw * ((1.0 - (double)e) * softplus(-h) + (double)e * softplus(h)));
+    if (p.log_ratio) {
+      p.log_ratio[pair] = (float)ratio[0];
+      p.log_ratio[pair + p.n_pairs] = (float)ratio[1];
+    }
+  }
+  return pw * p.beta * (e / (1.f + expf((float)-h)) - (1.f - e) / (1.f + expf((float)h)));
+}
+
+// The same from the parts of its tokens, summed by NT threads.
 template <int NT>
 __device__ inline float pair_coefficient(const TokenArgs& a, const PrefArgs& p, uint32_t pair, bool outputs, double* sh) {
   double ratio[2];
@@ -694,16 +757,7 @@ __device__ inline float pair_coefficient(const TokenArgs& a, const PrefArgs& p, 
     for (uint32_t t = thread<NT>(); t < a.T; t += NT) v += part[t];
     ratio[side] = threads_sum<NT>(v, sh);
   }
-  const double h = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin;
-  const float pw = p.pair_weight ? p.pair_weight[pair] : 1.f, e = p.smoothing;
-  if (outputs && thread<NT>() == 0) {
-    p.loss[pair] = (float)((double)pw * ((1.0 - (double)e) * softplus(-h) + (double)e * softplus(h)));
-    if (p.log_ratio) {
-      p.log_ratio[pair] = (float)ratio[0];
-      p.log_ratio[pair + p.n_pairs] = (float)ratio[1];
-    }
-  }
-  return pw * p.beta * (e / (1.f + expf((float)-h)) - (1.f - e) / (1.f + expf((float)h)));
+  return pair_loss(p, pair, ratio, outputs && thread<NT>() == 0);
 }
 
 __global__ __launch_bounds__(256) void pair_kernel(TokenArgs a, PrefArgs p) {
@@ -711,6 +765,55 @@ __global__ __launch_bounds__(256) void pair_kernel(TokenArgs a, PrefArgs p) {
   for (uint32_t pair = blockIdx.x; pair < p.n_pairs; pair += gridDim.x) {
     const float g = pair_coefficient<256>(a, p, pair, true, sh);
     if (threadIdx.x == 0) p.coef[pair] = g;
+  }
+}
+
+// Short pairs of short rows in one launch: a workgroup a pair, a wave a chosen token and
+// the rejected one beside it, both rows in registers between the sums and the gradient.
+template <typename T, int NV>
+__global__ __launch_bounds__(1024) void pref_pair_kernel(TokenArgs a, PrefArgs p) {
+  __shared__ Shared sh;
+  __shared__ double parts[2][kPrefPairMost];
+  const uint32_t t = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pair = blockIdx.x;
+  const float c = a.scale * kLog2e;
+  Slot sl[2];
+  float zy[2];
+  RowRegs<T, 64, NV> row[2];
+  RowSum r[2];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    sl[side] = slot_of(a, (pair + side * p.n_pairs) * a.T + t);
+    if (!sl[side].counts) continue;
+    const T* z = (const T*)a.logits + sl[side].row * a.ldl;
+    zy[side] = (float)z[sl[side].target];
+    row[side].load(z, a.V);
+  }
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    double part = 0.0;
+    if (sl[side].counts) {
+      const float m = row[side].top(zy[side], sh);
+      r[side] = fused(m, c) ? row[side].sum(m, c, sh) : row_sum_apart<T, 64>(row[side].z, a.V, c, m, sh.slow);
+      part = token_part(a, sl[side], zy[side], c, r[side], p.logp_ref);
+    } else if (thread<64>() == 0 && sl[side].write && a.logp) {
+      a.logp[sl[side].row] = 0.f;
+    }
+    if (thread<64>() == 0) parts[side][t] = part;
+  }
+  __syncthreads();
+  double ratio[2];
+#pragma unroll
+  for (int side = 0; side < 2; ++side)
+    ratio[side] = wave_sum((uint32_t)thread<64>() < a.T ? parts[side][thread<64>()] : 0.0);
+  const float g = pair_loss(p, pair, ratio, threadIdx.x == 0);
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    if (!a.dlogits || !sl[side].write) continue;
+    T* out = (T*)a.dlogits + sl[side].row * a.ldd;
+    const float cs = (side == 0 ? g : -g) * sl[side].weight * a.scale;
+    if (!sl[side].counts) row_zero<T, 64>(out, a.V);
+    else if (r[side].apart) row_grad_apart<T, 64>(row[side].z, out, a.V, sl[side].target, c, r[side], cs, -cs / r[side].sum);
+    else row[side].grad(out, a.V, sl[side].target, c, r[side], cs);
   }
 }
 
@@ -791,10 +894,12 @@ void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
 
 template <typename T>
 void launch_examples(const TokenArgs& a, const PolicyArgs& p, uint32_t n, float* loss, hipStream_t s) {
-  if ((int64_t)a.V * (int64_t)sizeof(T) <= 2048)
-    hipLaunchKernelGGL((policy_example_kernel<T, 2>), dim3(n), dim3(64 * a.T), 0, s, a, p, loss);
+  if ((int64_t)a.V * (int64_t)sizeof(T) > 4096)
+    hipLaunchKernelGGL((policy_example_kernel<T, 8, 1>), dim3(n), dim3(64 * a.T), 0, s, a, p, loss);
+  else if (a.T <= 16)
+    hipLaunchKernelGGL((policy_example_kernel<T, 4, 1>), dim3(n), dim3(64 * a.T), 0, s, a, p, loss);
   else
-    hipLaunchKernelGGL((policy_example_kernel<T, 8>), dim3(n), dim3(64 * a.T), 0, s, a, p, loss);
+    hipLaunchKernelGGL((policy_example_kernel<T, 4, 2>), dim3(n), dim3(64 * ((a.T + 1) / 2)), 0, s, a, p, loss);
 }
 
 template <typename T, bool PAIR>
@@ -831,8 +936,12 @@ int token_parts(int64_t n_slots, int64_t row_bytes) {
   return (int)(by_size < by_count ? (by_size < 64 ? by_size : 64) : (by_count < 64 ? by_count : 64));
 }
 
+// A second launch costs the host 3 us, what a call this small waits for: 8 examples of
+// 32 rows of 4 KB take 7.2 us in one launch, 5.3 in two (and 9 of the host); 256 of 16
+// rows 6.5 against 11.5.  Longer rows take too long in one wave: 16 rows of 16 KB,
+// 15.2 against 6.6.
 bool policy_by_example(int64_t row_bytes, int64_t T, int64_t n) {
-  return row_bytes <= 8192 && T <= kPolicyExampleMost && n <= 4096;
+  return n <= 4096 && T > 1 && (row_bytes <= 4096 ? T <= kPolicyExampleMost : row_bytes <= 8192 && T <= 16);
 }
 
 hipError_t launch_policy_examples(int dtype, const TokenArgs& a, const PolicyArgs& p, uint32_t n, float* loss,
@@ -852,6 +961,18 @@ hipError_t launch_policy_rows(int dtype, const TokenArgs& a, const PolicyArgs& p
 
 hipError_t launch_example_sum(const float* token_loss, uint32_t T, uint32_t n, float* loss, hipStream_t s) {
   hipLaunchKernelGGL(example_sum_kernel, dim3(blocks_for(n)), dim3(256), 0, s, token_loss, T, n, loss);
+  return hipGetLastError();
+}
+
+bool pref_by_pair(int64_t row_bytes, int64_t T, int64_t n_pairs) {
+  return row_bytes <= 8192 && T <= kPrefPairMost && n_pairs <= 4096;
+}
+
+hipError_t launch_pref_pairs(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s) {
+  const dim3 grid(p.n_pairs), block(64 * a.T);
+  if (dtype == 0) hipLaunchKernelGGL((pref_pair_kernel<float, 8>), grid, block, 0, s, a, p);
+  else if (dtype == 1) hipLaunchKernelGGL((pref_pair_kernel<__bf16, 8>), grid, block, 0, s, a, p);
+  else hipLaunchKernelGGL((pref_pair_kernel<_Float16, 8>), grid, block, 0, s, a, p);
   return hipGetLastError();
 }
 
