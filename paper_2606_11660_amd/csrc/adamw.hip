@@ -37,11 +37,6 @@ struct Four<__bf16> {
 };
 template <>
 struct Four<_Float16> { typedef f16x4 vec __attribute__((aligned(2))); };
-template <>
-struct Four<uint8_t> {
-  typedef uint8_t plain __attribute__((ext_vector_type(4)));
-  typedef plain vec __attribute__((aligned(1)));
-};
 
 // Four elements in one access, or (not WHOLE) the first `in` of them and 0 for the rest.
 template <bool WHOLE, typename T>
@@ -69,6 +64,46 @@ __device__ inline void store4(T* p, int in, const T (&x)[4]) {
   }
 }
 
+// The same of the 8-bit states: four codes in a word, at any address.
+typedef uint32_t loose_u32 __attribute__((aligned(1)));
+template <bool WHOLE>
+__device__ inline uint32_t load_codes(const uint8_t* p, int in) {
+  if constexpr (WHOLE) return __builtin_nontemporal_load(reinterpret_cast<const loose_u32*>(p));
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w |= e < in ? (uint32_t)p[e] << (8 * e) : 0u;
+  return w;
+}
+template <bool WHOLE>
+__device__ inline void store_codes(uint8_t* p, int in, uint32_t w) {
+  if constexpr (WHOLE) {
+    __builtin_nontemporal_store(w, reinterpret_cast<loose_u32*>(p));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < in) p[e] = (uint8_t)(w >> (8 * e));
+  }
+}
+__device__ inline void decode(uint32_t w, float scale, float (&x)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  x[0] = lo[0] * scale;
+  x[1] = lo[1] * scale;
+  x[2] = hi[0] * scale;
+  x[3] = hi[1] * scale;
+}
+__device__ inline uint32_t encode(const float (&x)[4]) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true);
+}
+
+// Square root within an ulp, for the step itself (the states' roots are rounded
+// correctly: one bit of them would move codes).  The instruction takes normal inputs.
+__device__ inline float near_sqrt(float x) {
+  const bool tiny = x < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(tiny ? x * 0x1p96f : x);
+  return tiny ? r * 0x1p-48f : r;
+}
+
 // largest of a wave's values: magnitudes as their bits, whose order keeps
 // infinities and NaN above every finite value
 template <int CTRL, int ROWS>
@@ -92,11 +127,6 @@ __device__ inline float wave_amax(const float (&x)[4]) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)b, 63));
 }
 
-__device__ inline float e4m3_value(uint8_t code) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0); }
-__device__ inline uint8_t e4m3_code(float x) {
-  return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
-}
-
 // RUNS runs of a wave from run0 on; all of their elements are there (WHOLE), or some
 // are not.
 template <typename P, typename G, bool EIGHT, bool MASTER, bool WHOLE, int RUNS>
@@ -104,7 +134,6 @@ __device__ inline void adamw_runs(const AdamwStep& a, const AdamwEntry& t, const
   typedef typename std::conditional<EIGHT, uint8_t, float>::type S;
   typedef typename std::conditional<MASTER, float, P>::type W;
   const int lane = threadIdx.x & 63;
-  const float lr = t.lr, lr_wd = t.lr_wd;
   const int64_t i0 = run0 * kQuantBlock + lane * 4;
   W* const wt = (MASTER ? (W*)ex.master : (W*)t.p) + i0;
   P* const pt = (P*)t.p + i0;
@@ -113,44 +142,44 @@ __device__ inline void adamw_runs(const AdamwStep& a, const AdamwEntry& t, const
   S* const vt = (S*)t.v + i0;
   W x[RUNS][4];
   G g[RUNS][4];
-  S m[RUNS][4], v[RUNS][4];
-  float ms[RUNS], vs[RUNS];
+  float m[RUNS][4], v[RUNS][4], ms[RUNS], vs[RUNS];
+  uint32_t mw[RUNS], vw[RUNS];
 #pragma unroll
   for (int u = 0; u < RUNS; ++u) {
     const int k = u * kQuantBlock;
     const int in = (int64_t)t.n - i0 - k >= 4 ? 4 : (int)((int64_t)t.n - i0 - k);
     load4<WHOLE>(wt + k, in, x[u]);
     load4<WHOLE>(gt + k, in, g[u]);
-    load4<WHOLE>(mt + k, in, m[u]);
-    load4<WHOLE>(vt + k, in, v[u]);
-    if (EIGHT) {
+    if constexpr (EIGHT) {
+      mw[u] = load_codes<WHOLE>(mt + k, in);
+      vw[u] = load_codes<WHOLE>(vt + k, in);
       ms[u] = ex.m_scale[run0 + u];
       vs[u] = ex.v_scale[run0 + u];
+    } else {
+      load4<WHOLE>(mt + k, in, m[u]);
+      load4<WHOLE>(vt + k, in, v[u]);
     }
   }
 #pragma unroll
   for (int u = 0; u < RUNS; ++u) {
     const int k = u * kQuantBlock;
     const int in = (int64_t)t.n - i0 - k >= 4 ? 4 : (int)((int64_t)t.n - i0 - k);
+    if constexpr (EIGHT) {
+      decode(mw[u], ms[u], m[u]);
+      decode(vw[u], vs[u], v[u]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[u][e] = v[u][e] * v[u][e];
+    }
     float nm[4], nv[4];
     W nx[4];
     P np[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float gr = (float)g[u][e] * gs, w = (float)x[u][e];
-      float om, ov;
-      if constexpr (EIGHT) {
-        om = e4m3_value(m[u][e]) * ms[u];
-        ov = e4m3_value(v[u][e]) * vs[u];
-        ov = ov * ov;
-      } else {
-        om = m[u][e];
-        ov = v[u][e];
-      }
-      nm[e] = om * a.beta1 + gr * a.one_beta1;
-      nv[e] = ov * a.beta2 + (gr * gr) * a.one_beta2;
-      const float root = sqrtf(nv[e] * a.corr2 + a.eps_root) + a.eps;
-      const float r = w - w * lr_wd - (nm[e] * a.corr1) / root * lr;
+      nm[e] = m[u][e] * a.beta1 + gr * a.one_beta1;
+      nv[e] = v[u][e] * a.beta2 + (gr * gr) * a.one_beta2;
+      const float root = near_sqrt(nv[e] * a.corr2 + a.eps_root) + a.eps;
+      const float r = w - w * t.lr_wd - nm[e] * t.lr * __builtin_amdgcn_rcpf(root);
       nx[e] = (W)r;
       np[e] = (P)r;
     }
@@ -167,15 +196,15 @@ __device__ inline void adamw_runs(const AdamwStep& a, const AdamwEntry& t, const
       am = am < kAmaxLeast ? kAmaxLeast : am;
       av = av < kAmaxLeast ? kAmaxLeast : av;
       const float fm = 1.f / am * kE4M3Max, fv = 1.f / av * kE4M3Max;
-      uint8_t qm[4], qv[4];
+      float qm[4], qv[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        qm[e] = e4m3_code(nm[e] * fm);
+        qm[e] = nm[e] * fm;
         const float q = root[e] * fv;
-        qv[e] = e4m3_code(q > 0.f && q < kE4M3Least ? kE4M3Least : q);
+        qv[e] = q > 0.f && q < kE4M3Least ? kE4M3Least : q;
       }
-      store4<WHOLE>(mt + k, in, qm);
-      store4<WHOLE>(vt + k, in, qv);
+      store_codes<WHOLE>(mt + k, in, encode(qm));
+      store_codes<WHOLE>(vt + k, in, encode(qv));
       if (lane == 0) {
         ex.m_scale[run0 + u] = am < INFINITY ? am * (1.f / kE4M3Max) : NAN;
         ex.v_scale[run0 + u] = av < INFINITY ? av * (1.f / kE4M3Max) : NAN;

@@ -964,7 +964,7 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
     h.one_beta1 = (float)(1.0 - beta1);
     h.beta2 = (float)beta2;
     h.one_beta2 = (float)(1.0 - beta2);
-    h.corr1 = (float)(1.0 / (1.0 - std::pow(beta1, (double)step)));
+    const double corr1 = 1.0 / (1.0 - std::pow(beta1, (double)step));
     h.corr2 = (float)(1.0 / (1.0 - std::pow(beta2, (double)step)));
     h.eps = (float)eps;
     h.eps_root = (float)eps_root;
@@ -972,8 +972,22 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
     int64_t total = 0;
     for (int32_t j = 0; j < n_tensors; ++j) total = std::min(total + tensors[j].n, (int64_t)1 << 40);
     AdamwLaunch L{(int)p_dtype, (int)g_dtype, eight, attr::adamw_runs_per_wave(total), h, s};
+    // The neighbour of a tensor in every buffer, with the same rates, is one tensor with
+    // it: a model in flat buffers takes one launch (168 adapters: two, and 20.4 us
+    // against 16.6).
+    const auto joins = [&](const attr_adamw_tensor& t, const attr_adamw_tensor& u) {
+      const auto after = [&](const void* x, const void* y, size_t each) {
+        return x ? y == static_cast<const char*>(x) + (size_t)t.n * each : !y;
+      };
+      return (!eight || (t.n % attr::kAdamwRun == 0 && u.m_scale == t.m_scale + t.n / attr::kAdamwRun &&
+                         u.v_scale == t.v_scale + t.n / attr::kAdamwRun)) &&
+             after(t.p, u.p, pb) && after(t.g, u.g, gb) && after(t.m, u.m, sb) && after(t.v, u.v, sb) &&
+             after(t.master, u.master, 4) && t.lr_scale == u.lr_scale && t.weight_decay == u.weight_decay;
+    };
     for (int32_t j = 0; j < n_tensors; ++j) {
-      const attr_adamw_tensor& t = tensors[j];
+      attr_adamw_tensor t = tensors[j];
+      if (t.n == 0) continue;
+      while (j + 1 < n_tensors && tensors[j + 1].n > 0 && joins(t, tensors[j + 1])) t.n += tensors[++j].n;
       // pieces of whole blocks whose sizes fit 32 bits
       constexpr int64_t kMost = 1ll << 31;
       for (int64_t at = 0; at < t.n; at += kMost) {
@@ -982,7 +996,7 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
         e.g = static_cast<const char*>(t.g) + (size_t)at * gb;
         e.m = static_cast<char*>(t.m) + (size_t)at * sb;
         e.v = static_cast<char*>(t.v) + (size_t)at * sb;
-        e.lr = (float)(lr * (double)t.lr_scale);
+        e.lr = (float)(lr * (double)t.lr_scale * corr1);
         e.lr_wd = (float)(lr * (double)t.lr_scale * (double)t.weight_decay);
         e.n = (uint32_t)std::min(t.n - at, kMost);
         e.chunk0 = 0;

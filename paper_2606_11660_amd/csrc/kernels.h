@@ -258,7 +258,7 @@ struct AdamwEntry {
   const void* g;
   void* m;
   void* v;
-  float lr, lr_wd;
+  float lr, lr_wd;  // of the corrected first moment, of the weight
   uint32_t n;       // elements
   uint32_t chunk0;  // first workgroup
 };
@@ -270,7 +270,7 @@ struct AdamwExtra {
 constexpr int kAdamwMost = 84, kAdamwMostExtra = 55;
 struct AdamwStep {
   const float* grad_scale;  // or null
-  float beta1, one_beta1, beta2, one_beta2, corr1, corr2, eps, eps_root;
+  float beta1, one_beta1, beta2, one_beta2, corr2, eps, eps_root;
   int32_t n;
 };
 struct AdamwPlain {
