@@ -142,23 +142,23 @@ def lib() -> ctypes.CDLL:
 
 
 _native_modules = None
-_native_rows = None
+_native_call = None
 
 
-def _native_token_rows():
-    """The native gatherer of a token call's rows, loaded once, as _native()."""
-    global _native_rows
-    if _native_rows is None:
+def _native_token_call():
+    """The native checks and calls of the token losses, loaded once, as _native()."""
+    global _native_call
+    if _native_call is None:
         try:
-            from ._marshal import token_rows
+            from ._marshal import token_call
         except ImportError as e:
             warnings.warn(f"_marshal is not available ({e}): token calls check their tensors in Python "
                           "(build it with `python -m paper_2606_11660_amd.build`)", RuntimeWarning, stacklevel=2)
 
-            def token_rows(*args):
+            def token_call(*args):
                 return None
-        _native_rows = token_rows
-    return _native_rows
+        _native_call = token_call
+    return _native_call
 
 
 def _native():
@@ -589,13 +589,30 @@ def attr_preference_loss_workspace_size(rows: TokenRows) -> int:
     return int(lib().attr_preference_loss_workspace_size(rows.c()))
 
 
-def _token_call(rows: TokenRows, per_row: tuple, per_example: tuple = (), per_pair: tuple = (),
-                dlogits: Optional[torch.Tensor] = None) -> Tuple[_CTokenRows, int]:
-    """(checked descriptor, row stride of dlogits) of a token call with these fp32 vectors
-    (or None), by the number of elements that each needs."""
-    got = _native_token_rows()(rows, TokenRows, per_row, per_example, per_pair, dlogits)
-    if got is not None:
-        return _CTokenRows.from_buffer(got[0]), got[1]
+_LOGP, _POLICY, _POLICY_PER_TOKEN, _PREFERENCE = range(4)
+_TOKEN_ENTRY = ("attr_token_logp", "attr_policy_loss", "attr_policy_loss", "attr_preference_loss")
+_token_address: Dict[int, int] = {}
+
+
+def _token_call(op: int, rows: TokenRows, per_row: tuple, per_example: tuple, per_pair: tuple, scalars: tuple,
+                dlogits: Optional[torch.Tensor], ws: Optional[Workspace], stream) -> None:
+    """One call of a token loss.  The tuples hold its fp32 vectors (or None) by the number of
+    elements that each needs, in the order of csrc/marshal.cpp's token_call()."""
+    L = lib()
+    raw = _raw_stream(stream)
+    w = _ws(ws, rows.logits.device, raw)
+    buf = w.buf
+    if op not in _token_address:
+        _token_address[op] = ctypes.cast(getattr(L, _TOKEN_ENTRY[op]), ctypes.c_void_p).value
+    ready = buf is not None and raw in w._streams
+    status = _native_token_call()(op, _token_address[op], rows, TokenRows, per_row, per_example, per_pair, dlogits,
+                                  scalars, buf.data_ptr() if ready else 0, buf.numel() if ready else 0, raw)
+    if status == 0:
+        return
+    if status is not None and status != 4:
+        _check(status)
+    # the Python checks, or (ATTR_ERR_WORKSPACE) a workspace that has to grow or that
+    # this stream has not used yet
     c = rows.c()
     for ts, n, what in ((per_row, c.n_rows, "row"), (per_example, c.n_examples, "example"),
                         (per_pair, c.n_examples // 2, "pair")):
@@ -607,17 +624,23 @@ def _token_call(rows: TokenRows, per_row: tuple, per_example: tuple = (), per_pa
         if dlogits.dtype != rows.logits.dtype or (n, V) != (c.n_rows, c.V):
             raise ValueError("dlogits must have the logits' shape and type")
     _same_gpu(rows.logits, dlogits, *per_row, *per_example, *per_pair)
-    return c, ldd
+    wsp, wsn = w.get(getattr(L, _TOKEN_ENTRY[op] + "_workspace_size")(c), raw)
+    if op == _LOGP:
+        args = (_ptr(per_row[0]),)
+    elif op == _PREFERENCE:
+        args = (_ptr(per_row[1]), _ptr(per_pair[1]), *scalars, _ptr(per_pair[0]), _ptr(per_example[0]),
+                _ptr(per_row[0]), _ptr(dlogits), ldd)
+    else:
+        advantage = per_row[3] if op == _POLICY_PER_TOKEN else per_example[1]
+        args = (_ptr(advantage), int(op == _POLICY_PER_TOKEN), _ptr(per_row[1]), _ptr(per_row[2]), *scalars,
+                _ptr(per_example[0]), _ptr(per_row[0]), _ptr(dlogits), ldd)
+    _check(getattr(L, _TOKEN_ENTRY[op])(c, *args, wsp, wsn, raw))
 
 
 def attr_token_logp(rows: TokenRows, logp: torch.Tensor, ws: Optional[Workspace] = None,
                     stream=None) -> torch.Tensor:
     """Log-probability of every row's target into logp (fp32 [n_rows]; 0 for tokens that do not count)."""
-    c, _ = _token_call(rows, (logp,))
-    L = lib()
-    raw = _raw_stream(stream)
-    wsp, wsn = _ws(ws, logp.device, raw).get(L.attr_token_logp_workspace_size(c), raw)
-    _check(L.attr_token_logp(c, logp.data_ptr(), wsp, wsn, raw))
+    _token_call(_LOGP, rows, (logp,), (), (), (), None, ws, stream)
     return logp
 
 
@@ -633,15 +656,11 @@ def attr_policy_loss(rows: TokenRows, advantage: torch.Tensor, loss: torch.Tenso
     and type, may be the logits themselves) takes the gradient of loss.sum(); rows'
     weights carry the mask and the normalisation."""
     if per_token:
-        c, ldd = _token_call(rows, (advantage, logp, logp_old, logp_ref), (loss,), (), dlogits)
+        _token_call(_POLICY_PER_TOKEN, rows, (logp, logp_old, logp_ref, advantage), (loss,), (),
+                    (clip_low, clip_high, beta), dlogits, ws, stream)
     else:
-        c, ldd = _token_call(rows, (logp, logp_old, logp_ref), (loss, advantage), (), dlogits)
-    L = lib()
-    raw = _raw_stream(stream)
-    wsp, wsn = _ws(ws, loss.device, raw).get(L.attr_policy_loss_workspace_size(c), raw)
-    _check(L.attr_policy_loss(c, advantage.data_ptr(), 1 if per_token else 0, _ptr(logp_old), _ptr(logp_ref),
-                              clip_low, clip_high, beta, loss.data_ptr(), _ptr(logp), _ptr(dlogits), ldd,
-                              wsp, wsn, raw))
+        _token_call(_POLICY, rows, (logp, logp_old, logp_ref), (loss, advantage), (), (clip_low, clip_high, beta),
+                    dlogits, ws, stream)
     return loss
 
 
@@ -655,12 +674,8 @@ def attr_preference_loss(rows: TokenRows, loss: torch.Tensor, log_ratio: Optiona
     Pair p: example p was chosen, example n_pairs + p rejected.  log_ratio: fp32
     [n_examples], the weighted sums of logp - logp_ref; dlogits takes the gradient
     of loss.sum(); pair_weight (fp32 [n_pairs]) scales each pair's loss."""
-    c, ldd = _token_call(rows, (logp, logp_ref), (log_ratio,), (loss, pair_weight), dlogits)
-    L = lib()
-    raw = _raw_stream(stream)
-    wsp, wsn = _ws(ws, loss.device, raw).get(L.attr_preference_loss_workspace_size(c), raw)
-    _check(L.attr_preference_loss(c, _ptr(logp_ref), _ptr(pair_weight), beta, margin, label_smoothing,
-                                  loss.data_ptr(), _ptr(log_ratio), _ptr(logp), _ptr(dlogits), ldd, wsp, wsn, raw))
+    _token_call(_PREFERENCE, rows, (logp, logp_ref), (log_ratio,), (loss, pair_weight),
+                (beta, margin, label_smoothing), dlogits, ws, stream)
     return loss
 
 

@@ -7,9 +7,9 @@
 // take (here: 15 us).  modules() makes the binding's checks on exact torch
 // tensors and returns None as soon as one does not hold or anything is of
 // another kind (a subclass, a wrapper without storage, a CPU tensor): the
-// binding's own Python checks then run, and raise or accept.  token_rows() does the
-// same for a batch of token rows and the fp32 vectors of its call (1 us of the 7 that
-// the Python checks take, where a small call's kernels take 4).
+// binding's own Python checks then run, and raise or accept.  token_call() makes the
+// checks of a token loss on its rows and vectors, and the library's call too (the
+// checks in Python take 7 us, where a small call's kernel takes 4).
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -210,35 +210,86 @@ bool gather_rows(PyObject* rows, PyObject* rows_type, PyObject* const* vecs, PyO
   return true;
 }
 
-// token_rows(rows, TokenRows, per_row, per_example, per_pair, dlogits)
-// -> (bytearray of attr_token_rows, row stride of dlogits) or None; the three tuples:
-// the call's fp32 vectors by the number of their elements
-PyObject* py_token_rows(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  if (nargs != 6) {
-    PyErr_SetString(PyExc_TypeError, "token_rows() takes 6 arguments");
+float* floats(PyObject* tuple, Py_ssize_t j) {
+  PyObject* o = PyTuple_GET_ITEM(tuple, j);
+  return o == Py_None ? nullptr : static_cast<float*>(THPVariable_Unpack(o).mutable_data_ptr());
+}
+
+// The library's entry points, by the numbers that token_call() takes.
+typedef attr_status (*LogpFn)(const attr_token_rows*, float*, void*, size_t, void*);
+typedef attr_status (*PolicyFn)(const attr_token_rows*, const float*, int32_t, const float*, const float*, float, float,
+                                float, float*, float*, void*, int64_t, void*, size_t, void*);
+typedef attr_status (*PreferenceFn)(const attr_token_rows*, const float*, const float*, float, float, float, float*,
+                                    float*, float*, void*, int64_t, void*, size_t, void*);
+constexpr int kLogp = 0, kPolicy = 1, kPolicyPerToken = 2, kPreference = 3;
+
+// token_call(op, address, rows, TokenRows, per_row, per_example, per_pair, dlogits,
+//            scalars, workspace, workspace_bytes, stream) -> status, or None
+// The three tuples hold the call's fp32 vectors by the number of their elements:
+//   attr_token_logp       (logp), (), ()
+//   attr_policy_loss      (logp, logp_old, logp_ref), (loss, advantage), ()
+//    with per_token       (logp, logp_old, logp_ref, advantage), (loss), ()
+//   attr_preference_loss  (logp, logp_ref), (log_ratio), (loss, pair_weight)
+// scalars: three numbers (clip_low, clip_high, beta; beta, margin, label_smoothing).
+PyObject* py_token_call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  if (nargs != 12) {
+    PyErr_SetString(PyExc_TypeError, "token_call() takes 12 arguments");
     return nullptr;
   }
   attr_token_rows c;
   std::memset(&c, 0, sizeof(c));
   int64_t ldd = 0;
   bool ok = false;
+  double x[3] = {0, 0, 0};
+  void* d = nullptr;
+  const long op = PyLong_AsLong(args[0]);
+  void* fn = PyLong_AsVoidPtr(args[1]);
+  void* ws = PyLong_AsVoidPtr(args[9]);
+  const size_t ws_bytes = PyLong_AsSize_t(args[10]);
+  void* stream = PyLong_AsVoidPtr(args[11]);
+  PyObject* const* v = args + 4;
   try {
-    ok = gather_rows(args[0], args[1], args + 2, args[5], c, ldd);
+    ok = !PyErr_Occurred() && fn && gather_rows(args[2], args[3], v, args[7], c, ldd) && PyTuple_CheckExact(args[8]) &&
+         PyTuple_GET_SIZE(args[8]) == (op == kLogp ? 0 : 3);
+    if (ok && args[7] != Py_None) d = THPVariable_Unpack(args[7]).mutable_data_ptr();
   } catch (...) {  // a tensor without storage, for one
     ok = false;
   }
+  for (int k = 0; ok && op != kLogp && k < 3; ++k) x[k] = PyFloat_AsDouble(PyTuple_GET_ITEM(args[8], k));
+  const int sizes[4][3] = {{1, 0, 0}, {3, 2, 0}, {4, 1, 0}, {2, 1, 2}};
+  ok = ok && !PyErr_Occurred() && op >= 0 && op <= 3;
+  for (int k = 0; ok && k < 3; ++k) ok = PyTuple_GET_SIZE(v[k]) == sizes[op][k];
   if (!ok) {
     PyErr_Clear();
     Py_RETURN_NONE;
   }
-  PyObject* buf = PyByteArray_FromStringAndSize(reinterpret_cast<const char*>(&c), (Py_ssize_t)sizeof(c));
-  return buf ? Py_BuildValue("NL", buf, (long long)ldd) : nullptr;
+  attr_status st;
+  try {
+    float *r0 = floats(v[0], 0), *r1 = op == kLogp ? nullptr : floats(v[0], 1),
+          *r2 = op == kPolicy || op == kPolicyPerToken ? floats(v[0], 2) : nullptr,
+          *e0 = op == kLogp ? nullptr : floats(v[1], 0);
+    float *a = op == kPolicy ? floats(v[1], 1) : op == kPolicyPerToken ? floats(v[0], 3) : nullptr,
+          *p0 = op == kPreference ? floats(v[2], 0) : nullptr, *p1 = op == kPreference ? floats(v[2], 1) : nullptr;
+    Py_BEGIN_ALLOW_THREADS;
+    if (op == kLogp)
+      st = reinterpret_cast<LogpFn>(fn)(&c, r0, ws, ws_bytes, stream);
+    else if (op == kPreference)
+      st = reinterpret_cast<PreferenceFn>(fn)(&c, r1, p1, (float)x[0], (float)x[1], (float)x[2], p0, e0, r0, d, ldd, ws,
+                                              ws_bytes, stream);
+    else
+      st = reinterpret_cast<PolicyFn>(fn)(&c, a, op == kPolicyPerToken, r1, r2, (float)x[0], (float)x[1], (float)x[2], e0,
+                                          r0, d, ldd, ws, ws_bytes, stream);
+    Py_END_ALLOW_THREADS;
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+  return PyLong_FromLong((long)st);
 }
 
 PyMethodDef methods[] = {{"modules", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_modules)),
                           METH_FASTCALL, "module descriptors of a projection call, or None"},
-                         {"token_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_token_rows)),
-                          METH_FASTCALL, "descriptor of a token call's rows, or None"},
+                         {"token_call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_token_call)),
+                          METH_FASTCALL, "status of a token loss's call, or None"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
