@@ -432,10 +432,13 @@ __global__ __launch_bounds__(group_of(NT)) void token_logp_kernel(TokenArgs a, c
   if (thread<NT>() == 0) write_logp<PREF>(a, slot, sl, zy, c, r, logp_ref);
 }
 
-// A row in the registers of NT threads, NV vectors each: V <= NT NV kE.
+// A row in the registers of NT threads, NV vectors each: V <= NT NV kE.  16-bit rows of
+// more than 128 KB, one to a CU, are read through the caches after all (8192 bf16 rows
+// of 131072: 841 us, 868 past them; fp32 rows of 200 KB: 310 and 305).
 template <typename T, int NT, int NV>
 struct RowRegs {
   static constexpr int E = kE<T>;
+  static constexpr bool KEEP = sizeof(T) == 2 && NT * NV > 8192;
   const T* z;
   Cut cut;
   T rest;
@@ -448,7 +451,7 @@ struct RowRegs {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int32_t j = (k * NT + thread<NT>()) * E;
-      v[k] = j < cut.whole ? load_vec(z + cut.head + j) : no_vec(T{});
+      v[k] = j < cut.whole ? load_vec<KEEP>(z + cut.head + j) : no_vec(T{});
     }
   }
   // The row's maximum; `also` is an element of it, read before anything is written.
@@ -456,6 +459,7 @@ struct RowRegs {
     float m = fmaxf(also, (float)rest);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
+      if (k * NT * E >= cut.whole) break;  // nothing but -inf from here on
       float x[E];
       unpack(v[k], T{}, x);
 #pragma unroll
@@ -470,6 +474,7 @@ struct RowRegs {
     float s = __builtin_amdgcn_exp2f(fmaf((float)rest, c, -mc));
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
+      if (k * NT * E >= cut.whole) break;  // nothing but -inf from here on
       float x[E];
       unpack(v[k], T{}, x);
 #pragma unroll
@@ -883,10 +888,16 @@ void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((split_policy_kernel<T, 512, 4>), dim3(a.n_slots, a.n_parts), dim3(512), 0, s, a, p);
     return;
   }
-  if (bytes <= 2048) launch_slots<64>(policy_kernel<T, 64, 2>, a, s, p);
+  // Threads and vectors by the row's bytes; us of 16384, 8192 or 6400 rows at the
+  // neighbouring choices: bf16 2048 wide 28 (256 x 2: 34), 4000 wide 51 (256 x 8: 55),
+  // 10000 wide 59 (256 x 8: 64), 32003 wide 145 (512 x 8: 154, 1024 x 4: 164), 65536 wide
+  // 286 (512 x 16: 291).  50257 wide 244 (512 x 16: 233), but 244 against 253 with half
+  // of the rows masked.
+  if (bytes <= 4096) launch_slots<64>(policy_kernel<T, 64, 4>, a, s, p);
   else if (bytes <= 8192) launch_slots<256>(policy_kernel<T, 256, 2>, a, s, p);
-  else if (bytes <= 32768) launch_slots<256>(policy_kernel<T, 256, 8>, a, s, p);
-  else if (bytes <= 65536) launch_slots<1024>(policy_kernel<T, 1024, 4>, a, s, p);
+  else if (bytes <= 16384) launch_slots<256>(policy_kernel<T, 256, 8>, a, s, p);
+  else if (bytes <= 49152) launch_slots<512>(policy_kernel<T, 512, 8>, a, s, p);
+  else if (bytes <= 65536) launch_slots<512>(policy_kernel<T, 512, 16>, a, s, p);
   else if (bytes <= 131072) launch_slots<1024>(policy_kernel<T, 1024, 8>, a, s, p);
   else if (bytes <= 262144) launch_slots<1024>(policy_kernel<T, 1024, 16>, a, s, p);
   else launch_slots<1024>(policy_stream_kernel<T, 1024>, a, s, p);
