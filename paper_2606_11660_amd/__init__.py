@@ -719,23 +719,22 @@ class AdamTensors:
         self.p_dtype, self.g_dtype = _dtype(p[0]), _dtype(g[0])
         self.state_dtype = ATTR_E4M3 if eight else ATTR_F32
         self.tensors = {k: list(x[0]) for k, x in kinds.items()}
-        self.device = p[0].device
-        self.array = (_CAdamTensor * n)()
-        spans = []
-        for j in range(n):
-            size = p[j].numel()
-            for name, (ts, dtype) in kinds.items():
-                t = ts[j]
-                want = -(-size // 256) if name.endswith("_scale") else size
-                if t.dtype != dtype or not t.is_contiguous() or t.numel() != want:
-                    raise ValueError(f"tensor {j}: {name} must be a contiguous {dtype} tensor of {want} elements")
-                if not t.is_cuda or t.device != self.device:
+        self.device = device = p[0].device
+        if device.type != "cuda":
+            raise ValueError("every tensor must live on the same GPU device")
+        sizes, address, spans = [t.numel() for t in p], {}, []
+        for name, (ts, dtype) in kinds.items():
+            want = [-(-x // 256) for x in sizes] if name.endswith("_scale") else sizes
+            each, address[name] = dtype.itemsize, [t.data_ptr() for t in ts]
+            for j, t in enumerate(ts):
+                if t.dtype != dtype or not t.is_contiguous() or t.numel() != want[j]:
+                    raise ValueError(f"tensor {j}: {name} must be a contiguous {dtype} tensor of {want[j]} elements")
+                if t.device != device:
                     raise ValueError("every tensor must live on the same GPU device")
-                if want:
-                    spans.append((t.data_ptr(), t.data_ptr() + want * t.element_size(), name, j))
-            of = {k: x[0][j].data_ptr() for k, x in kinds.items()}
-            self.array[j] = _CAdamTensor(of["p"], of["g"], of["m"], of["v"], of.get("master"), of.get("m_scale"),
-                                         of.get("v_scale"), size, scale[j], decay[j])
+            spans += [(a, a + x * each, name, j) for j, (a, x) in enumerate(zip(address[name], want)) if x]
+        none = [None] * n
+        self.array = (_CAdamTensor * n)(*zip(*(address.get(k, none) for k in ("p", "g", "m", "v", "master", "m_scale",
+                                                                              "v_scale")), sizes, scale, decay))
         spans.sort()
         for a, b in zip(spans, spans[1:]):
             if b[0] < a[1] and not (a[2] == b[2] == "g"):
