@@ -599,6 +599,8 @@ def _token_call(op: int, rows: TokenRows, per_row: tuple, per_example: tuple, pe
     """One call of a token loss.  The tuples hold its fp32 vectors (or None) by the number of
     elements that each needs, in the order of csrc/marshal.cpp's token_call()."""
     L = lib()
+    if not rows.logits.is_cuda:
+        rows.c()  # raises
     raw = _raw_stream(stream)
     w = _ws(ws, rows.logits.device, raw)
     buf = w.buf

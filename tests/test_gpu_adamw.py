@@ -217,3 +217,61 @@ def test_plan_refusals():
         with pytest.raises(P.AttrError, match=text):
             P.attr_adamw_step(plan, **kw)
     assert (p == 0).all()
+
+
+def test_neighbouring_tensors_are_one():
+    """Tensors side by side in flat buffers give the bits of separate ones, whatever their sizes and rates."""
+    for eight, sizes in ((False, [100, 7, 256, 1000, 31, 5000]), (True, [256, 512, 100, 256, 768, 300])):
+        pads = [-(-n // 256) * 256 if eight else n for n in sizes]
+        total, at = sum(pads), np.concatenate([[0], np.cumsum(pads)[:-1]])
+        A = Model(5, [total], eight=eight)
+        flat = lambda t: [t[a:a + n] for a, n in zip(at, sizes)]  # noqa: E731
+        scales = (lambda t: [t[a // 256:a // 256 + -(-n // 256)] for a, n in zip(at, sizes)]) if eight else (lambda t: None)
+        decay, rate = [0.1, 0.1, 0.0, 0.0, 0.0, 0.1], [1.0, 1.0, 1.0, 1.0, 0.5, 0.5]
+        own = [[t.clone() for t in flat(x[0])] for x in (A.p, A.gd, A.m, A.v)]
+        own_s = [[t.clone() for t in scales(x[0])] if eight else None for x in (A.ms or [None], A.vs or [None])]
+        plan = P.AdamTensors(*own, m_scale=own_s[0], v_scale=own_s[1], weight_decay=decay, lr_scale=rate)
+        P.attr_adamw_step(plan, 3, **HYPER)
+        plan = P.AdamTensors(flat(A.p[0]), flat(A.gd[0]), flat(A.m[0]), flat(A.v[0]), m_scale=scales(A.ms[0] if eight else None),
+                             v_scale=scales(A.vs[0] if eight else None), weight_decay=decay, lr_scale=rate)
+        P.attr_adamw_step(plan, 3, **HYPER)
+        for got, want in zip((flat(A.p[0]), flat(A.m[0]), flat(A.v[0])), (own[0], own[2], own[3])):
+            for x, y in zip(got, want):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+        if eight:
+            for got, want in zip((scales(A.ms[0]), scales(A.vs[0])), own_s):
+                assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_step_under_graph_capture():
+    """A captured step replays on the gradients that are there."""
+    M, N = Model(8, [3000, 77], g=torch.bfloat16), Model(8, [3000, 77], g=torch.bfloat16)
+    plan, other = M.tensors(), N.tensors()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.attr_adamw_step(plan, 5, **HYPER)
+    for k in range(3):
+        for a, b in zip(M.gd, N.gd):
+            a.mul_(0.5)
+            b.mul_(0.5)
+        graph.replay()
+        P.attr_adamw_step(other, 5, **HYPER)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(M.p + M.m + M.v, N.p + N.m + N.v)), k
+
+
+def test_tiny_second_moments():
+    """Gradients whose squares are subnormal or zero in fp32, with and without eps: finite where the formula is."""
+    n = 1024
+    g = torch.logspace(-24, -14, n, device="cuda")
+    for eps in (0.0, 1e-8):
+        p, m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+        P.attr_adamw_step(P.AdamTensors([p], [g], [m], [v]), 1, 1.0, 0.9, 0.95, eps)
+        got, gv = host(p).astype(np.float64), host(v).astype(np.float64)
+        gm = host(m).astype(np.float64)
+        want = -(gm / (1 - 0.9)) / (np.sqrt(gv / (1 - 0.95)) + eps) if eps else np.where(gv > 0, -(gm / 0.1) / np.sqrt(np.where(gv > 0, gv, 1) / 0.05), 0)
+        live = gv > 0 if not eps else np.ones(n, bool)
+        # roundings of m's and v's factors, and of a subnormal v itself: 2^-149 of it
+        tol = np.abs(want) * (32 * U + (2.0 ** -149 / np.where(gv > 0, gv, 1) if not eps else 0)) + 1e-37
+        assert (np.abs(got - want) <= tol)[live].all()
+        assert eps or not np.isfinite(got[~live]).any() or (~live).sum() == 0

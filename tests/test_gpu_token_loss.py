@@ -488,3 +488,121 @@ def test_long_rows(V, rows, dtype):
         w[2] = 1.0
     P.attr_policy_loss(tok, adv, loss, dlogits=z)  # in place
     assert torch.equal(z[live], dl[live])
+
+
+@pytest.mark.parametrize("n,T,V,dtype", [(4, 700, 64, torch.float32), (2, 1500, 33, torch.bfloat16), (6, 40, 1500, torch.float16),
+                                         (3, 33, 2050, torch.float32), (40, 16, 1999, torch.bfloat16), (2, 17, 4100, torch.bfloat16),
+                                         (10, 300, 9, torch.float32), (64, 32, 1024, torch.float32)])
+def test_long_and_short_examples(n, T, V, dtype):
+    """Lengths on both sides of every rule: sums in the rows' launch, in one of their own, pairs formed by
+    each row or beforehand."""
+    say(f"case: examples n={n} T={T} V={V} {NAMES[dtype]}")
+    b = Batch(n * T, dtype, V, n, T, ragged=True, weighted=True)
+    old, ref = b.old_ref((0.8, 1.28))
+    adv = b.r.standard_normal(n).astype(np.float32)
+    up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    loss, logp, (dl, _) = torch.full((n,), 7.0, device="cuda"), torch.full((b.rows,), 7.0, device="cuda"), b.dbuf()
+    P.attr_policy_loss(b.tokens(), up(adv), loss, logp=logp, dlogits=dl, logp_old=up(old), logp_ref=up(ref), clip_high=0.28, beta=0.04)
+    wl, wlp, wg = O.policy_loss(b.numpy(), b.target, n, T, adv, logp_old=old, logp_ref=ref, clip_high=0.28, beta=0.04, **b.where())
+    check_logp(b, host(logp), 7.0)
+    c_abs, tol = policy_tols(b, old, adv, ref, 0.04, False)
+    assert (np.abs(host(loss) - wl) <= tol + U * np.abs(wl)).all()
+    check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 0.0, c_abs)
+    if n % 2:
+        return
+    for gradient in (True, False):
+        pl, ratio, (pd, _) = torch.full((n // 2,), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda"), b.dbuf()
+        logp.fill_(7.0)
+        P.attr_preference_loss(b.tokens(), pl, log_ratio=ratio, logp=logp, dlogits=pd if gradient else None, logp_ref=up(ref), beta=0.02)
+        wl, wr, wlp, wg = O.preference_loss(b.numpy(), b.target, n, T, logp_ref=ref, beta=0.02, **b.where())
+        check_logp(b, host(logp), 7.0)
+        r_tol, c_abs = np.zeros(n), np.zeros(b.rows)
+        for i, _, row, counts in b.slots():
+            if counts:
+                r_tol[i] += b.weight[row] * logp_tol(wlp[row], V)
+        h_tol = 0.02 * (r_tol[:n // 2] + r_tol[n // 2:])
+        assert (np.abs(host(ratio) - wr) <= r_tol + 2 * U * np.abs(wr)).all()
+        assert (np.abs(host(pl) - wl) <= h_tol + 2 * U * np.abs(wl)).all()
+        for i, _, row, counts in b.slots():
+            if counts:
+                c_abs[row] = b.weight[row] * 0.02 * h_tol[i % (n // 2)] / 4
+        if gradient:
+            check_dlogits(b, pd.double().cpu().numpy(), wg, wlp, 8 * U, c_abs)
+
+
+def test_repeated_calls_are_equal():
+    """The same call gives the same bits: no sum depends on the order in which workgroups end."""
+    for V, n, T in ((513, 6, 50), (50257, 4, 60), (262144, 2, 3)):
+        b = Batch(V, torch.bfloat16, V, n, T, ragged=True)
+        up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+        ref = up(b.r.standard_normal(b.rows).astype(np.float32) - 5)
+        adv = up(b.r.standard_normal(n).astype(np.float32))
+        tok, got = b.tokens(), []
+        for _ in range(3):
+            loss, pl, (d1, _), (d2, _) = torch.zeros(n, device="cuda"), torch.zeros(n // 2, device="cuda"), b.dbuf(), b.dbuf()
+            P.attr_policy_loss(tok, adv, loss, dlogits=d1, logp_ref=ref, beta=0.1)
+            P.attr_preference_loss(tok, pl, dlogits=d2, logp_ref=ref)
+            got.append((loss, pl, d1, d2))
+        for other in got[1:]:
+            assert all(torch.equal(x, y) for x, y in zip(got[0], other))
+
+
+def test_under_graph_capture():
+    """Captured calls replay like eager ones, other work between the replays."""
+    b = Batch(31, torch.bfloat16, 3001, 8, 40, ragged=True, weighted=True)
+    adv = torch.randn(8, device="cuda")
+    ws, tok = P.Workspace(), b.tokens()
+    loss, pl, logp, (d1, _), (d2, _) = (torch.zeros(8, device="cuda"), torch.zeros(4, device="cuda"),
+                                        torch.zeros(b.rows, device="cuda"), b.dbuf(), b.dbuf())
+
+    def calls():
+        P.attr_token_logp(tok, logp, ws=ws)
+        P.attr_policy_loss(tok, adv, loss, dlogits=d1, logp_old=logp, ws=ws)
+        P.attr_preference_loss(tok, pl, dlogits=d2, ws=ws)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for k in range(4):
+        b.logits.copy_((b.z.float() * (1 + 0.1 * k)).to(b.z.dtype))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (loss, pl, logp, d1, d2)]
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, (loss, pl, logp, d1, d2))), k
+        torch.randn(1000, device="cuda").sum().item()
+
+
+def test_python_checks_make_the_same_call(monkeypatch):
+    """Without the native part of the binding: the same outputs, and the refusals of Python."""
+    b = Batch(37, torch.float16, 777, 4, 9, packed=True, ragged=True, weighted=True)
+    adv, per = torch.randn(4, device="cuda"), torch.randn(b.rows, device="cuda")
+    ref = torch.randn(b.rows, device="cuda") - 4
+    outs = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(P, "_native_call", lambda *args: None)
+        tok, ws = b.tokens(), P.Workspace()
+        logp, loss, l2, pl, ratio = (torch.zeros(k, device="cuda") for k in (b.rows, 4, 4, 2, 4))
+        (d1, _), (d2, _), (d3, _) = b.dbuf(), b.dbuf(), b.dbuf()
+        P.attr_token_logp(tok, logp, ws=ws)
+        P.attr_policy_loss(tok, adv, loss, dlogits=d1, logp_old=logp, logp_ref=ref, beta=0.1, clip_low=0.1, ws=ws)
+        P.attr_policy_loss(tok, per, l2, dlogits=d2, per_token=True, ws=ws)
+        P.attr_preference_loss(tok, pl, log_ratio=ratio, dlogits=d3, logp_ref=ref, pair_weight=adv, beta=0.2, margin=0.1,
+                               label_smoothing=0.2, ws=ws)
+        outs.append([logp, loss, l2, pl, ratio, d1, d2, d3])
+        assert P.attr_policy_loss_workspace_size(tok) > 0 and P.attr_preference_loss_workspace_size(tok) > 0
+        assert P.attr_token_logp_workspace_size(tok) == 0
+        for bad, text in ((lambda: P.attr_token_logp(tok, logp[:3]), "one value for each row"),
+                          (lambda: P.attr_policy_loss(tok, adv[:3], loss), "one value for each example"),
+                          (lambda: P.attr_preference_loss(tok, pl[:1]), "one value for each pair"),
+                          (lambda: P.attr_policy_loss(tok, adv, loss, dlogits=d1.float()), "shape and type"),
+                          (lambda: P.attr_policy_loss(tok, adv.cpu(), loss), "same GPU"),
+                          (lambda: P.attr_policy_loss(tok, adv.double(), loss), "float32")):
+            with pytest.raises(ValueError, match=text):
+                bad()
+    assert all(torch.equal(x, y) for x, y in zip(*outs))

@@ -183,3 +183,35 @@ def test_binding_refusals():
     with pytest.raises(ValueError, match="same GPU"):
         P.AdamTensors([x], [x], [x], [x])
     assert ctypes.sizeof(P._CTokenRows) == 96 and ctypes.sizeof(P._CAdamTensor) == 72
+
+
+def test_token_calls_refuse_host_tensors():
+    """Before anything of the GPU is touched."""
+    rows = P.TokenRows(torch.zeros((8, 100)), torch.zeros(8, dtype=torch.int64), 4, 2)
+    x = torch.zeros(8)
+    for call in (lambda: P.attr_token_logp(rows, x), lambda: P.attr_policy_loss(rows, x, x),
+                 lambda: P.attr_preference_loss(rows, x)):
+        with pytest.raises(ValueError, match="same GPU"):
+            call()
+
+
+def test_native_calls_are_optional(monkeypatch):
+    """Without the native part the binding warns once and checks in Python."""
+    import sys
+    monkeypatch.setattr(P, "_native_call", None)
+    monkeypatch.setitem(sys.modules, "paper_2606_11660_amd._marshal", None)  # the import fails
+    with pytest.warns(RuntimeWarning, match="check their tensors in Python"):
+        assert P._native_token_call()(1, 2, 3) is None
+
+
+def test_native_call_refuses_what_it_does_not_know():
+    """Anything but the exact kinds of arguments goes to the Python checks: None, and no error."""
+    from paper_2606_11660_amd import _marshal
+    rows = P.TokenRows(torch.zeros((8, 100)), torch.zeros(8, dtype=torch.int64), 4, 2)
+    x = torch.zeros(8)
+    for args in ((0, 1, rows, P.TokenRows, (x,), (), (), None, (), 0, 0, 0), (9, 1, rows, P.TokenRows, (x,), (), (), None, (), 0, 0, 0),
+                 ("a", 1, rows, P.TokenRows, (x,), (), (), None, (), 0, 0, 0), (0, 0, rows, P.TokenRows, (x,), (), (), None, (), 0, 0, 0),
+                 (0, 1, object(), P.TokenRows, (x,), (), (), None, (), 0, 0, 0), (1, 1, rows, P.TokenRows, [x], (), (), x, ("a",) * 3, 0, 0, 0)):
+        assert _marshal.token_call(*args) is None
+    with pytest.raises(TypeError, match="12 arguments"):
+        _marshal.token_call(1)
