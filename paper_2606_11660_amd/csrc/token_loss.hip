@@ -34,17 +34,27 @@ struct Slot {
   bool counts;      // its logits are read
 };
 
-// Token slot of a batch: example slot / T, token slot % T (attr_token_rows).  Loads
+// A value that is the same in a wave's lanes, into a scalar register: a slot's row, its
+// addresses and its loss's inputs then take none of the registers that hold the row.
+__device__ inline float uniform(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+__device__ inline int64_t uniform(int64_t x) {
+  return ((int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) |
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// Token slot (the same for a wave's lanes) of a batch: example slot / T, token slot % T (attr_token_rows).  Loads
 // that do not depend on each other are issued together: their latency is what a call
 // of few rows consists of.
 __device__ inline Slot slot_of(const TokenArgs& a, uint32_t slot) {
   const uint32_t i = slot / a.T, t = slot - i * a.T;
   Slot r;
   const int32_t len = a.length ? a.length[i] : (int32_t)a.T;
-  r.row = a.row_offset ? a.row_offset[i] + t : (int64_t)slot;
-  const bool inside = r.row >= 0 && r.row < a.n_rows, in = (int32_t)t < len;
-  const int64_t y = inside ? a.target[r.row] : -1;
-  r.weight = inside && a.weight ? a.weight[r.row] : 1.f;
+  r.row = a.row_offset ? uniform(a.row_offset[i]) + t : (int64_t)slot;
+  const bool inside = r.row >= 0 && r.row < a.n_rows, in = (int32_t)t < __builtin_amdgcn_readfirstlane(len);
+  const int64_t y = uniform(inside ? a.target[r.row] : -1);
+  r.weight = uniform(inside && a.weight ? a.weight[r.row] : 1.f);
   r.write = inside && (in || !a.row_offset);
   r.counts = inside && in && y >= 0 && y < a.V && r.weight != 0.f;
   r.target = (int32_t)y;
@@ -226,8 +236,13 @@ struct RowSum {
 __device__ inline float exponent(float z, float c, const RowSum& r) {
   return r.apart ? (z - r.offset) * c : fmaf(z, c, -r.offset);
 }
+// The offset need not be the row's maximum, so the sum's binary exponent is taken out
+// and joined with the linear part, whose terms may be large, in fp64.
 __device__ inline float row_logp(float zy, float c, const RowSum& r) {
-  return (exponent(zy, c, r) - log2f(r.sum)) * kLn2;
+  const float f = __builtin_amdgcn_frexp_mantf(r.sum);
+  const int n = __builtin_amdgcn_frexp_expf(r.sum);
+  const double x = r.apart ? ((double)zy - (double)r.offset) * (double)c : (double)zy * (double)c - (double)r.offset;
+  return ((float)(x - (double)n) - log2f(f)) * kLn2;
 }
 
 // Whether the fused form takes a row (part) with maximum m; not if it is NaN.
@@ -241,6 +256,13 @@ __device__ RowSum row_sum_apart(const T* z, int32_t V, float c, float m, float* 
 #pragma unroll 1
   for (int32_t j = thread<NT>(); j < V; j += NT) s += __builtin_amdgcn_exp2f(((float)z[j] - m) * c);
   return {m, block_add<NT>(s, sh), m, true};
+}
+template <typename T, int NT>
+__device__ RowSum row_sum_apart(const T* z, int32_t V, float c, Shared& sh) {
+  float m = -INFINITY;
+#pragma unroll 1
+  for (int32_t j = thread<NT>(); j < V; j += NT) m = fmaxf(m, (float)z[j]);
+  return row_sum_apart<T, NT>(z, V, c, block_max<NT>(m, sh.max), sh.slow);
 }
 template <typename T, int NT>
 __device__ void row_grad_apart(const T* z, T* out, int32_t V, int32_t y, float c, const RowSum& r, float cs,
@@ -351,8 +373,11 @@ struct PolicyToken {
   float weight, advantage, old, ref;
 };
 __device__ inline PolicyToken policy_inputs(const PolicyArgs& p, const TokenArgs& a, uint32_t slot, const Slot& sl) {
-  return {sl.weight, p.advantage[p.per_token ? sl.row : (int64_t)(slot / a.T)],
-          p.logp_old ? p.logp_old[sl.row] : 0.f, p.beta != 0.f ? p.logp_ref[sl.row] : 0.f};
+  // what there is not is read elsewhere, without a branch (and its wait), and not used
+  const float* advantage = p.advantage + (p.per_token ? sl.row : (int64_t)(slot / a.T));
+  const float* old = p.logp_old ? p.logp_old + sl.row : advantage;
+  const float* ref = p.beta != 0.f ? p.logp_ref + sl.row : advantage;
+  return {sl.weight, *advantage, *old, *ref};
 }
 
 // Loss and derivative by logp of one token of the policy loss, weights included.
@@ -448,39 +473,47 @@ struct RowRegs {
     z = row;
     cut = cut_row<T, NT>(z, V);
     rest = cut.at < V ? z[cut.at] : (T)-INFINITY;
+    // range-checked, so that no branch is around them: the sums wait for each vector
+    // alone.  Lanes past the row's end read nothing and hold zeros.
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(z + cut.head, (uint32_t)cut.whole * (uint32_t)sizeof(T));
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int32_t j = (k * NT + thread<NT>()) * E;
-      v[k] = j < cut.whole ? load_vec<KEEP>(z + cut.head + j) : no_vec(T{});
+      const uint32_t off = (uint32_t)(k * NT + thread<NT>()) * 16u;
+      v[k] = KEEP ? load16_cached(r, off) : load16_stream(r, off);
     }
   }
-  // The row's maximum; `also` is an element of it, read before anything is written.
-  __device__ inline float top(float also, Shared& sh) {
-    float m = fmaxf(also, (float)rest);
+  __device__ inline float vec_sum(int k, float mc, float c) {
+    float x[E], s = 0.f;
+    unpack(v[k], T{}, x);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      if (k * NT * E >= cut.whole) break;  // nothing but -inf from here on
+    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
+    return s;
+  }
+  // The row's sum relative to the largest of its first vectors, which is known while the
+  // others are still on their way; `also`, an element of the row, is read before anything
+  // is written.  Not ok: an entry so far above them (2^100), or a row that the fused form
+  // does not take.
+  __device__ inline RowSum sum(float also, float c, Shared& sh, bool& ok) {
+    const int32_t at = thread<NT>() * E;
+    float m = fmaxf(also, (float)rest);
+    if (at < cut.whole) {
       float x[E];
-      unpack(v[k], T{}, x);
+      unpack(v[0], T{}, x);
 #pragma unroll
       for (int e = 0; e < E; ++e) m = fmaxf(m, x[e]);
     }
-    return block_max<NT>(m, sh.max);
-  }
-  // Its sum in the fused form.
-  __device__ inline RowSum sum(float m, float c, Shared& sh) {
+    m = block_max<NT>(m, sh.max);
     const float mc = m * c;
-    forget(v);
     float s = __builtin_amdgcn_exp2f(fmaf((float)rest, c, -mc));
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      if (k * NT * E >= cut.whole) break;  // nothing but -inf from here on
-      float x[E];
-      unpack(v[k], T{}, x);
-#pragma unroll
-      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
+      forget(v[k]);
+      if ((k + 1) * NT * E <= cut.whole) s += vec_sum(k, mc, c);
+      else if (at + k * NT * E < cut.whole) s += vec_sum(k, mc, c);
     }
-    return {mc, block_add<NT>(s, sh.sum), m, false};
+    s = block_add<NT>(s, sh.sum);
+    ok = fused(m, c) && s < 0x1p100f;
+    return {mc, s, m, false};
   }
   // g ([j = y] - p_j) into out
   __device__ inline void grad(T* out, int32_t V, int32_t y, float c, const RowSum& r, float g) {
@@ -505,9 +538,8 @@ struct PolicySlot {
   float zy;
   RowRegs<T, NT, NV> row;
 
+  // sl is set, and counts
   __device__ inline void load(const TokenArgs& a, const PolicyArgs& p, uint32_t slot) {
-    sl = slot_of(a, slot);
-    if (!sl.counts) return;
     in = policy_inputs(p, a, slot, sl);
     const T* z = (const T*)a.logits + sl.row * a.ldl;
     zy = (float)z[sl.target];
@@ -515,22 +547,18 @@ struct PolicySlot {
   }
   // Writes the row's outputs; returns the token's loss.
   __device__ inline float finish(const TokenArgs& a, const PolicyArgs& p, Shared& sh) {
-    if (!sl.counts) {
-      skip_slot<T, NT>(a, sl);
-      return 0.f;
-    }
     const float c = a.scale * kLog2e;
     T* out = (T*)a.dlogits + sl.row * a.ldd;
-    const float m = row.top(zy, sh);
-    if (!fused(m, c)) {  // a path of its own, which needs no registers
-      const RowSum r = row_sum_apart<T, NT>(row.z, a.V, c, m, sh.slow);
+    bool ok;
+    const RowSum r = row.sum(zy, c, sh, ok);
+    if (!ok) {  // a path of its own, which needs no registers
+      const RowSum r = row_sum_apart<T, NT>(row.z, a.V, c, sh);
       const float logp = row_logp(zy, c, r);
       const TokenLoss l = policy_token(p, in, logp);
       if (thread<NT>() == 0 && a.logp) a.logp[sl.row] = logp;
       if (a.dlogits) row_grad_apart<T, NT>(row.z, out, a.V, sl.target, c, r, l.c * a.scale, -l.c * a.scale / r.sum);
       return l.loss;
     }
-    const RowSum r = row.sum(m, c, sh);
     const float logp = row_logp(zy, c, r);
     const TokenLoss l = policy_token(p, in, logp);
     if (thread<NT>() == 0 && a.logp) a.logp[sl.row] = logp;
@@ -545,6 +573,12 @@ __global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void po
   const uint32_t slot = a.slot0 + first_slot<NT>();
   if (slot >= a.n_slots) return;
   PolicySlot<T, NT, NV> k;
+  k.sl = slot_of(a, slot);
+  if (!k.sl.counts) {
+    skip_slot<T, NT>(a, k.sl);
+    if (thread<NT>() == 0) p.token_loss[slot] = 0.f;
+    return;
+  }
   k.load(a, p, slot);
   const float loss = k.finish(a, p, sh);
   if (thread<NT>() == 0) p.token_loss[slot] = loss;
@@ -560,13 +594,19 @@ __global__ __launch_bounds__(1024) void policy_example_kernel(TokenArgs a, Polic
   const uint32_t t0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), step = blockDim.x >> 6;
   PolicySlot<T, 64, NV> k[K];
 #pragma unroll
-  for (int i = 0; i < K; ++i)
-    if (t0 + i * step < a.T) k[i].load(a, p, blockIdx.x * a.T + t0 + i * step);
+  for (int i = 0; i < K; ++i) {
+    const uint32_t t = t0 + i * step;
+    k[i].sl.counts = false;
+    if (t >= a.T) continue;
+    k[i].sl = slot_of(a, blockIdx.x * a.T + t);
+    if (k[i].sl.counts) k[i].load(a, p, blockIdx.x * a.T + t);
+    else skip_slot<T, 64>(a, k[i].sl);
+  }
 #pragma unroll
   for (int i = 0; i < K; ++i) {
     const uint32_t t = t0 + i * step;
     if (t >= a.T) continue;
-    const float l = k[i].finish(a, p, sh);
+    const float l = k[i].sl.counts ? k[i].finish(a, p, sh) : 0.f;
     if ((threadIdx.x & 63) == 0) token[t] = l;
   }
   __syncthreads();
@@ -797,8 +837,9 @@ __global__ __launch_bounds__(1024) void pref_pair_kernel(TokenArgs a, PrefArgs p
   for (int side = 0; side < 2; ++side) {
     double part = 0.0;
     if (sl[side].counts) {
-      const float m = row[side].top(zy[side], sh);
-      r[side] = fused(m, c) ? row[side].sum(m, c, sh) : row_sum_apart<T, 64>(row[side].z, a.V, c, m, sh.slow);
+      bool ok;
+      r[side] = row[side].sum(zy[side], c, sh, ok);
+      if (!ok) r[side] = row_sum_apart<T, 64>(row[side].z, a.V, c, sh);
       part = token_part(a, sl[side], zy[side], c, r[side], p.logp_ref);
     } else if (thread<64>() == 0 && sl[side].write && a.logp) {
       a.logp[sl[side].row] = 0.f;
