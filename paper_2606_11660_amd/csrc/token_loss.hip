@@ -12,9 +12,9 @@
 // trees.
 //
 // All of it is bound by HBM: rows are read with 16-byte loads.  An odd vocabulary's
-// rows start anywhere; the elements before a row's first 16-byte boundary and those
-// after its last whole vector go one a thread (vectors across the boundaries cost a
-// fifth of the rate).  Stores follow the loads' cut, wherever that falls in dlogits.
+// rows start anywhere; the elements before a row's first line or 16-byte boundary and
+// those after its last whole vector go one a thread (vectors across the boundaries cost
+// a fifth of the rate).  Stores follow the loads' cut, wherever that falls in dlogits.
 #include "common.h"
 #include "kernels.h"
 
@@ -204,16 +204,17 @@ __device__ inline uint32_t first_slot() {
   return NT == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
 }
 
-// A row of V elements: `head` before the first 16-byte boundary, `whole` in vectors
-// from there on, fewer than a vector's after them; `at`: this thread's element of the
-// first and last (V or more: none).
+// A row of V elements: `head` before the first boundary, `whole` in vectors from there
+// on, fewer than a vector's after them; `at`: this thread's element of the first and
+// last (V or more: none).  Boundaries are those of 128-byte lines where there are
+// threads for the head, so that a wave's stores fill whole lines.
 struct Cut {
   int32_t head, whole, at;
 };
 template <typename T, int NT>
 __device__ inline Cut cut_row(const T* z, int32_t V) {
-  constexpr int E = kE<T>;
-  const int32_t off = (int32_t)(-(reinterpret_cast<intptr_t>(z) / (int)sizeof(T)) & (E - 1));
+  constexpr int E = kE<T>, A = NT > 64 ? 128 / (int)sizeof(T) : E;
+  const int32_t off = (int32_t)(-(reinterpret_cast<intptr_t>(z) / (int)sizeof(T)) & (A - 1));
   Cut k;
   k.head = off < V ? off : V;
   k.whole = (V - k.head) / E * E;
