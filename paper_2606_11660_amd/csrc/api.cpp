@@ -886,7 +886,8 @@ struct AdamwLaunch {
   attr::AdamwFull full = {};
 
   hipError_t add(attr::AdamwEntry e, const attr::AdamwExtra& x) {
-    const uint32_t chunk = 4 * (uint32_t)runs * attr::kAdamwRun, need = (uint32_t)(((uint64_t)e.n + chunk - 1) / chunk);
+    const uint32_t chunk = 4 * (uint32_t)runs * attr::kAdamwRun, lead = eight ? 0 : attr::adamw_lead(e.m),
+                   need = (uint32_t)(((uint64_t)e.n + lead + chunk - 1) / chunk);
     const int most = eight || x.master ? attr::kAdamwMostExtra : attr::kAdamwMost;
     // below 2^32 threads a launch
     if (step.n >= most || blocks + need > (1u << 23) || master != (x.master != nullptr)) {

@@ -287,6 +287,12 @@ static_assert(sizeof(AdamwPlain) <= 4096 && sizeof(AdamwFull) <= 4096, "kernel a
 // waves' chunk of them.
 constexpr int kAdamwRun = 256;
 int adamw_runs_per_wave(int64_t elements);
+// 32-bit states: elements of the first run that would be before the tensor's start, so
+// that every run starts at a 128-byte line of the first moment.
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline int adamw_lead(const void* m) { return (int)(reinterpret_cast<uintptr_t>(m) & 127) >> 2; }
 // Every tensor of a launch has a master, or none has.  AdamwPlain: no masters, 32-bit
 // states.
 hipError_t launch_adamw(int p_dtype, int g_dtype, int runs, uint32_t blocks, const AdamwPlain& a, hipStream_t s);
