@@ -295,9 +295,10 @@ attr_status attr_score_topk(const void* Q, int64_t n_q, int64_t ldq, const void*
  * tokens that do not count are never read (padding may hold any bits).
  * With a row's largest logit z_max and s = logit_scale,
  *     logp = s (z_target - z_max) - log sum_j exp(s (z_j - z_max)),
- * differences, products and sums in fp32.  Logits of -inf are vocabulary
- * entries of probability 0; a row that holds a NaN or +inf, or -inf only, has
- * logp NaN.
+ * exponentials and their sum in fp32 (the order of the sum, and so the last
+ * bits, follow the call's sizes and the rows' alignment).  Logits of -inf are
+ * vocabulary entries of probability 0; a row that holds a NaN or +inf, or -inf
+ * only, has logp NaN.
  * Outputs of rows that do not count: without row_offset every row i * T + t,
  * t < T, is written (logp 0, dlogits zeros); with row_offset the rows of
  * tokens t < length[i] (clamped to [0, T]), and no others, are written.  The
@@ -335,7 +336,9 @@ attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, 
  * The weights carry the mask and the normalisation (1 / tokens for a mean over
  * each example, one constant for a sum, a loss scale).  Each row of logits is
  * read once and each row of dlogits written once where a row fits a
- * workgroup's registers (256 KB); loss sums are formed in fp64 in a fixed order.
+ * workgroup's registers (256 KB; longer rows, and few long rows, which are
+ * spread over many CUs, are read twice); loss sums are formed in fp64 in a
+ * fixed order.
  *   advantage  device fp32 [n_examples], or [n_rows] with per_token != 0
  *   logp_old   device fp32 [n_rows], or NULL: the logits' own (ratio 1)
  *   logp_ref   device fp32 [n_rows]; may be NULL if beta is 0
@@ -406,10 +409,11 @@ typedef struct {
  *     x = x - lr' wd x - lr' (m / (1 - beta1^step))
  *                        / (sqrt(v / (1 - beta2^step) + eps_root) + eps)
  * with lr' = lr lr_scale, x the weight (its master where there is one).  All
- * in fp32 without contraction, so the result does not depend on how the work
- * is split.  8-bit states are encoded after the update: m to the nearest E4M3
- * value (ties to even), the root of v likewise but never to zero while v is
- * positive (a second moment rounded to zero would make the next step huge).
+ * in fp32 without contraction (the quotient and its root within an ulp each),
+ * so the result does not depend on how the work is split.  8-bit states are
+ * encoded after the update: m to the nearest E4M3 value (ties to even), the
+ * root of v likewise but never to zero while v is positive (a second moment
+ * rounded to zero would make the next step huge).
  * E4M3 keeps a root within 6.25%: between steps a stored second moment follows
  * its block's scale exactly, and its place in the block only by changes of
  * that size.  A NaN or infinity in a block's new states makes the block's

@@ -286,7 +286,7 @@ static_assert(sizeof(AdamwPlain) <= 4096 && sizeof(AdamwFull) <= 4096, "kernel a
 // A wave takes runs of 256 elements (a block of the 8-bit states), a workgroup four
 // waves' chunk of them.
 constexpr int kAdamwRun = 256;
-int adamw_runs_per_wave(int64_t elements);
+int adamw_runs_per_wave(int64_t elements, bool eight);
 // 32-bit states: elements of the first run that would be before the tensor's start, so
 // that every run starts at a 128-byte line of the first moment.
 #ifdef __HIPCC__
