@@ -2,19 +2,28 @@
 // the paired log-ratio preference loss, with their gradients with respect to
 // the logits.
 //
-// With c = s log2 e, a row's largest m and e_j = exp2(c z_j - c m), S = sum e_j:
+// With c = s log2 e, an offset m and e_j = exp2(c z_j - c m), S = sum e_j:
 //     logp = (c z_y - c m - log2 S) ln 2,   p_j = e_j / S,
-// and the gradient of a loss with derivative g by logp is s g ([j = y] - p_j).
-// c z_j - c m is one fused multiply-add with the rounded c m: its rounding is the
-// same factor in every e_j and cancels (up to |c m| = 2^20, see kMostMc; other
-// rows, those of infinities and of nothing but a mask's lowest value among them,
-// form the differences z_j - m first).  Sums are fp32 chains per thread, then
-// trees.
+// and the gradient of a loss with derivative g by logp is s g ([j = y] - p_j).  m is
+// the row's largest element, or the largest of its first ones.  c z_j - c m is one fused
+// multiply-add with the rounded c m: its rounding is the same factor in every e_j and
+// cancels (up to |c m| = 2^20, see kMostMc; other rows, those of infinities and of
+// nothing but a mask's lowest value among them, form the differences z_j - m first).
+// Sums are fp32 chains per thread, then trees; the losses' sums over tokens are fp64.
 //
 // All of it is bound by HBM: rows are read with 16-byte loads.  An odd vocabulary's
 // rows start anywhere; the elements before a row's first line or 16-byte boundary and
 // those after its last whole vector go one a thread (vectors across the boundaries cost
 // a fifth of the rate).  Stores follow the loads' cut, wherever that falls in dlogits.
+// An element takes one exponential for the sum and one for the gradient (a quarter of
+// the other instructions' rate): at 16-bit types half of the time that its bytes take.
+//
+// Measured on one MI355X (large copies: 5.2 TB/s; one read stream: 7.1):
+//   log-probabilities of 3984 bf16 rows of 65536: 81 us, 6.5 TB/s
+//   policy loss and gradient of 11008 bf16 rows of 131072, an eighth of them masked:
+//     994 us, 5.4 TB/s; 8192 rows of 65536: 355 us, 6.0 TB/s
+//   preference loss and gradient of 5312 fp16 rows of 50257, a quarter of them masked:
+//     212 us (rows read twice: 1.33 GB, 6.3 TB/s)
 #include "common.h"
 #include "kernels.h"
 
@@ -44,9 +53,9 @@ __device__ inline int64_t uniform(int64_t x) {
          (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 
-// Token slot (the same for a wave's lanes) of a batch: example slot / T, token slot % T (attr_token_rows).  Loads
-// that do not depend on each other are issued together: their latency is what a call
-// of few rows consists of.
+// Token slot (the same for a wave's lanes) of a batch: example slot / T, token slot % T
+// (attr_token_rows).  Loads that do not depend on each other are issued together: their
+// latency is what a call of few rows consists of.
 __device__ inline Slot slot_of(const TokenArgs& a, uint32_t slot) {
   const uint32_t i = slot / a.T, t = slot - i * a.T;
   Slot r;
@@ -460,11 +469,11 @@ __global__ __launch_bounds__(group_of(NT)) void token_logp_kernel(TokenArgs a, c
 
 // A row in the registers of NT threads, NV vectors each: V <= NT NV kE.  16-bit rows of
 // more than 128 KB, one to a CU, are read through the caches after all (8192 bf16 rows
-// of 131072: 841 us, 868 past them; fp32 rows of 200 KB: 310 and 305).
+// of 131072: 804 us, 829 past them; fp32 rows of 256 KB: 393 and 387).
 template <typename T, int NT, int NV>
 struct RowRegs {
   static constexpr int E = kE<T>;
-  static constexpr bool KEEP = sizeof(T) == 2 && NT * NV > 8192;
+  static constexpr bool KEEP = sizeof(T) == 2 && NT * NV > 8192;  // vectors
   const T* z;
   Cut cut;
   T rest;
@@ -934,16 +943,15 @@ void launch_policy(const TokenArgs& a, const PolicyArgs& p, hipStream_t s) {
     hipLaunchKernelGGL((split_policy_kernel<T, 512, 4>), dim3(a.n_slots, a.n_parts), dim3(512), 0, s, a, p);
     return;
   }
-  // Threads and vectors by the row's bytes; us of 16384, 8192 or 6400 rows at the
-  // neighbouring choices: bf16 2048 wide 28 (256 x 2: 34), 4000 wide 51 (256 x 8: 55),
-  // 10000 wide 59 (256 x 8: 64), 32003 wide 145 (512 x 8: 154, 1024 x 4: 164), 65536 wide
-  // 286 (512 x 16: 291).  50257 wide 244 (512 x 16: 233), but 244 against 253 with half
-  // of the rows masked.
+  // Threads and vectors by the row's bytes; us of 32768, 16384, 8192 or 6400 rows at the
+  // neighbouring choices: bf16 1000 wide 29 (256 x 2: 62), 4000 wide 50 (256 x 8: 57),
+  // 10000 wide 58 (512 x 8: 61), 16000 wide 89 (256 x 8: 94), 24000 wide 104 (1024 x 8:
+  // 112), 32003 wide 140 (1024 x 8: 140), 65536 wide 282 (512 x 16: 283).  50257 wide 232
+  // (512 x 16: 219), but 226 against 237 with half of the rows masked.
   if (bytes <= 4096) launch_slots<64>(policy_kernel<T, 64, 4>, a, s, p);
   else if (bytes <= 8192) launch_slots<256>(policy_kernel<T, 256, 2>, a, s, p);
-  else if (bytes <= 16384) launch_slots<256>(policy_kernel<T, 256, 8>, a, s, p);
-  else if (bytes <= 49152) launch_slots<512>(policy_kernel<T, 512, 8>, a, s, p);
-  else if (bytes <= 65536) launch_slots<512>(policy_kernel<T, 512, 16>, a, s, p);
+  else if (bytes <= 24576) launch_slots<256>(policy_kernel<T, 256, 8>, a, s, p);
+  else if (bytes <= 65536) launch_slots<512>(policy_kernel<T, 512, 8>, a, s, p);
   else if (bytes <= 131072) launch_slots<1024>(policy_kernel<T, 1024, 8>, a, s, p);
   else if (bytes <= 262144) launch_slots<1024>(policy_kernel<T, 1024, 16>, a, s, p);
   else launch_slots<1024>(policy_stream_kernel<T, 1024>, a, s, p);

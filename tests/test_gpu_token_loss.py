@@ -606,3 +606,31 @@ def test_python_checks_make_the_same_call(monkeypatch):
             with pytest.raises(ValueError, match=text):
                 bad()
     assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+def test_largest_entries_late_in_the_row():
+    """Rows whose first elements say nothing of their maximum: hundreds below it, or masked."""
+    for dtype in NAMES:
+        for V in (3000, 9000, 20000, 50000):
+            say(f"case: late maximum {NAMES[dtype]} V={V}")
+            b = Batch(V, dtype, V, 300, 1)
+            first = 3 * V // 4
+            for row in range(300):
+                kind = row % 6
+                if kind == 1:
+                    b.z[row, :first] -= 60.0        # within the range of one exponential
+                elif kind == 2:
+                    b.z[row, :first] -= 2000.0      # past it
+                elif kind == 3:
+                    b.z[row, :first] = -math.inf
+                elif kind == 4:
+                    b.z[row, :first] = torch.finfo(dtype).min
+                elif kind == 5:
+                    b.z[row, V - 1] = 300.0
+                b.target[row] = [5, first + 7, 5, first + 9, V - 1, 5][kind]
+            b.sync()
+            logp, loss, (dl, _) = torch.zeros(300, device="cuda"), torch.zeros(300, device="cuda"), b.dbuf()
+            P.attr_policy_loss(b.tokens(), torch.ones(300, device="cuda"), loss, logp=logp, dlogits=dl)
+            _, wlp, wg = O.policy_loss(b.numpy(), b.target, 300, 1, np.ones(300))
+            check_logp(b, host(logp), None)
+            check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 2 * U, np.zeros(300))
