@@ -308,7 +308,7 @@ typedef struct {
   const void* logits;    /* [n_rows, V], row stride ldl >= V; any V, stride and element alignment */
   attr_dtype dtype;      /* ATTR_F32, ATTR_BF16 or ATTR_F16 */
   int64_t n_rows, V, ldl;  /* 1 <= V <= 2^28 */
-  float logit_scale;     /* s: one over the sampling temperature; > 0 */
+  float logit_scale;     /* s: one over the sampling temperature; > 0, at most 2e38 */
   const int64_t* target;   /* device [n_rows] */
   const float* weight;     /* device [n_rows] or NULL (1 for every token) */
   int64_t n_examples, T;   /* n_examples * T < 2^31; without row_offset n_rows >= n_examples * T */
@@ -360,6 +360,7 @@ attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage
  *     log_ratio[i] = sum_t w (logp - logp_ref)      (over tokens that count)
  *     h = beta (log_ratio[p] - log_ratio[n_pairs + p]) - margin
  *     loss[p] = pw ((1 - e) softplus(-h) + e softplus(h)),  e = label_smoothing
+ *                                  (a term of factor 0 is 0, also at infinite h)
  *     c = dloss/dlogp = +-w pw beta (e sigma(h) - (1 - e) sigma(-h))
  *                                  (+: chosen, -: rejected)
  *     dlogits[row, j] = s c ([j = target] - exp(logp_j))

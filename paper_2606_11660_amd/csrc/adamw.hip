@@ -15,8 +15,8 @@
 //
 // Measured on one MI355X (large copies: 5.2 TB/s): 268M elements with bf16 weights,
 // fp32 masters and 32-bit states 1.26 to 1.29 ms (5.9 TB/s); 134M fp32 weights with 8-bit
-// states 314 us (6.0 TB/s, 67 vector instructions an element: 86% of what the rate
-// allows); 168 adapter tensors side by side, 3.1M elements, 15 us.
+// states 310 us (6.1 TB/s, 67 vector instructions an element: 86% of what the rate
+// allows); 168 adapter tensors side by side, 2.9M elements, 13 us.
 #include "common.h"
 #include "kernels.h"
 
@@ -144,8 +144,8 @@ __device__ inline float wave_amax(const float (&x)[4]) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)b, 63));
 }
 
-// RUNS runs of a wave from run0 on, of `lead` elements fewer in the first; all of their elements are there (WHOLE), or some
-// are not.
+// RUNS runs of a wave from run0 on, of `lead` elements fewer in the first; all of their
+// elements are there (WHOLE), or some are not.
 template <typename P, typename G, bool EIGHT, bool MASTER, bool WHOLE, int RUNS>
 __device__ inline void adamw_runs(const AdamwStep& a, const AdamwEntry& t, const AdamwExtra& ex, float gs, int64_t run0,
                                   int lead) {

@@ -632,8 +632,8 @@ attr_status token_validate(const attr_token_rows* r, const char* who) {
     return fail(ATTR_ERR_INVALID_ARG, "%s: ldl=%lld must be in [V, 2^40]", who, (long long)r->ldl);
   if (r->n_rows > (1ll << 40) / r->ldl * (1ll << 20))
     return fail(ATTR_ERR_INVALID_ARG, "%s: n_rows=%lld is too large", who, (long long)r->n_rows);
-  if (!(r->logit_scale > 0.f) || r->logit_scale > 3.0e38f)
-    return fail(ATTR_ERR_INVALID_ARG, "%s: logit_scale must be positive and finite", who);
+  if (!(r->logit_scale > 0.f) || r->logit_scale > 2.0e38f)  // times log2 e it is finite
+    return fail(ATTR_ERR_INVALID_ARG, "%s: logit_scale must be positive and at most 2e38", who);
   if (!r->row_offset && r->n_rows < r->n_examples * r->T)
     return fail(ATTR_ERR_INVALID_ARG, "%s: %lld rows, %lld examples of %lld tokens need more", who,
                 (long long)r->n_rows, (long long)r->n_examples, (long long)r->T);
@@ -678,7 +678,7 @@ TokenLayout token_layout(const attr_token_rows* r, int mode) {
     L.off_coef = L.off_part + align_up(8 * slots);
     L.total = L.off_coef + align_up(4 * (size_t)(r->n_examples / 2));
   }
-  L.n_parts = attr::token_parts(n, r->V * dtype_bytes(r->dtype));
+  L.n_parts = attr::token_parts(mode, n, r->V * dtype_bytes(r->dtype));
   if (L.n_parts > 1) {
     L.off_parts = L.total;
     L.off_zy = L.off_parts + align_up(8 * slots * (size_t)L.n_parts);
@@ -725,8 +725,8 @@ attr_status token_workspace(const TokenLayout& L, void* ws, size_t ws_bytes, con
 }
 
 size_t token_query(const attr_token_rows* r, int mode) {
-  if (!r || !valid_dtype(r->dtype) || r->V < 1 || r->V > (1ll << 28) || r->n_examples < 0 || r->T < 1 || r->T >= (1ll << 31) || r->n_examples >= (1ll << 31) ||
-      r->n_examples * r->T >= (1ll << 31))
+  if (!r || !valid_dtype(r->dtype) || r->V < 1 || r->V > (1ll << 28) || r->n_examples < 0 || r->T < 1 ||
+      r->T >= (1ll << 31) || r->n_examples >= (1ll << 31) || r->n_examples * r->T >= (1ll << 31))
     return 0;
   return token_layout(r, mode).total;
 }
@@ -857,7 +857,7 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
     }
     hipError_t e = attr::launch_pref_stats((int)rows->dtype, a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_preference_loss launch");
-    const bool pair = dlogits && rows->T <= 1024 && a.n_slots <= 2048;
+    const bool pair = dlogits && attr::pref_pairs_within(rows->V * dtype_bytes(rows->dtype), rows->T, a.n_slots);
     if (!pair) e = attr::launch_pairs(a, p, s);
     if (e != hipSuccess) return device_fail(e, "attr_preference_loss pair launch");
     if (!dlogits) return ATTR_OK;

@@ -229,7 +229,7 @@ struct PrefArgs {
   uint32_t n_pairs;
   float beta, margin, smoothing;
 };
-int token_parts(int64_t n_slots, int64_t row_bytes);
+int token_parts(int mode, int64_t n_slots, int64_t row_bytes);
 hipError_t launch_token_logp(int dtype, const TokenArgs& a, hipStream_t s);
 // Policy loss: token losses of every slot, then their sums; or both at once.
 hipError_t launch_policy_rows(int dtype, const TokenArgs& a, const PolicyArgs& p, hipStream_t s);
@@ -242,6 +242,7 @@ hipError_t launch_policy_examples(int dtype, const TokenArgs& a, const PolicyArg
 // the pairs, and the gradient, with the pairs (pair) or after them.
 constexpr uint32_t kPrefPairMost = 16;  // tokens of a sequence
 bool pref_by_pair(int64_t row_bytes, int64_t T, int64_t n_pairs);
+bool pref_pairs_within(int64_t row_bytes, int64_t T, int64_t n_slots);
 hipError_t launch_pref_pairs(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 hipError_t launch_pref_stats(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s);
 hipError_t launch_pairs(const TokenArgs& a, const PrefArgs& p, hipStream_t s);

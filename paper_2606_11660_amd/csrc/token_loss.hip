@@ -246,13 +246,20 @@ struct RowSum {
 __device__ inline float exponent(float z, float c, const RowSum& r) {
   return r.apart ? (z - r.offset) * c : fmaf(z, c, -r.offset);
 }
-// The offset need not be the row's maximum, so the sum's binary exponent is taken out
-// and joined with the linear part, whose terms may be large, in fp64.
-__device__ inline float row_logp(float zy, float c, const RowSum& r) {
-  const float f = __builtin_amdgcn_frexp_mantf(r.sum);
-  const int n = __builtin_amdgcn_frexp_expf(r.sum);
+// logp / ln 2 = x - n - log2 f with the linear part x, and the sum's binary exponent n and
+// mantissa f: the offset need not be the row's maximum, so x and n may be large and are
+// joined in fp64; log2 f is in [-1, 0].
+struct LogParts {
+  double whole;
+  float rest;
+};
+__device__ inline LogParts log_parts(float zy, float c, const RowSum& r) {
   const double x = r.apart ? ((double)zy - (double)r.offset) * (double)c : (double)zy * (double)c - (double)r.offset;
-  return ((float)(x - (double)n) - log2f(f)) * kLn2;
+  return {x - (double)__builtin_amdgcn_frexp_expf(r.sum), log2f(__builtin_amdgcn_frexp_mantf(r.sum))};
+}
+__device__ inline float row_logp(float zy, float c, const RowSum& r) {
+  const LogParts l = log_parts(zy, c, r);
+  return ((float)l.whole - l.rest) * kLn2;
 }
 
 // Whether the fused form takes a row (part) with maximum m; not if it is NaN.
@@ -420,12 +427,11 @@ __device__ inline void skip_slot(const TokenArgs& a, const Slot& sl) {
 constexpr int group_of(int nt) { return nt == 64 ? 256 : nt; }
 
 // A counting token's share of its log ratio; one thread writes its log-probability.  The
-// ratios are small differences of sums: here the logarithm and its differences are in
-// fp64.
+// ratios are small differences of sums: here the difference is in fp64.
 __device__ inline double token_part(const TokenArgs& a, const Slot& sl, float zy, float c, const RowSum& r,
                                     const float* logp_ref) {
-  const double x = r.apart ? ((double)zy - (double)r.offset) * (double)c : (double)zy * (double)c - (double)r.offset;
-  const double logp = (x - log2((double)r.sum)) * 0.6931471805599453;
+  const LogParts l = log_parts(zy, c, r);
+  const double logp = (l.whole - (double)l.rest) * 0.6931471805599453;
   if (thread<64>() == 0 && a.logp) a.logp[sl.row] = (float)logp;
   return (double)sl.weight * (logp - (logp_ref ? (double)logp_ref[sl.row] : 0.0));
 }
@@ -501,8 +507,9 @@ struct RowRegs {
   }
   // The row's sum relative to the largest of its first vectors, which is known while the
   // others are still on their way; `also`, an element of the row, is read before anything
-  // is written.  Not ok: an entry so far above them (2^100), or a row that the fused form
-  // does not take.
+  // is written.  Not ok: a sum past 2^60, from entries far above them (a gradient is
+  // divided by it: 2^100 would leave one of 1e-15 to subnormal numbers), or a row that
+  // the fused form does not take.
   __device__ inline RowSum sum(float also, float c, Shared& sh, bool& ok) {
     const int32_t at = thread<NT>() * E;
     float m = fmaxf(also, (float)rest);
@@ -522,7 +529,7 @@ struct RowRegs {
       else if (at + k * NT * E < cut.whole) s += vec_sum(k, mc, c);
     }
     s = block_add<NT>(s, sh.sum);
-    ok = fused(m, c) && s < 0x1p100f;
+    ok = fused(m, c) && s < 0x1p60f;
     return {mc, s, m, false};
   }
   // g ([j = y] - p_j) into out
@@ -578,7 +585,7 @@ struct PolicySlot {
 };
 
 template <typename T, int NT, int NV>
-__global__ __launch_bounds__(group_of(NT), NV > 16 ? 2 : NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
+__global__ __launch_bounds__(group_of(NT), NV > 8 ? 4 : 8) void policy_kernel(TokenArgs a, PolicyArgs p) {
   __shared__ Shared sh;
   const uint32_t slot = a.slot0 + first_slot<NT>();
   if (slot >= a.n_slots) return;
@@ -792,7 +799,9 @@ __device__ inline float pair_loss(const PrefArgs& p, uint32_t pair, const double
   const double h = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin;
   const float pw = p.pair_weight ? p.pair_weight[pair] : 1.f, e = p.smoothing;
   if (outputs) {
-    p.loss[pair] = (float)((double)pw * ((1.0 - (double)e) * softplus(-h) + (double)e * softplus(h)));
+    // a share of nothing is not taken of an infinite ratio's loss
+    const double won = e < 1.f ? (1.0 - (double)e) * softplus(-h) : 0.0, lost = e > 0.f ? (double)e * softplus(h) : 0.0;
+    p.loss[pair] = (float)((double)pw * (won + lost));
     if (p.log_ratio) {
       p.log_ratio[pair] = (float)ratio[0];
       p.log_ratio[pair + p.n_pairs] = (float)ratio[1];
@@ -994,19 +1003,29 @@ hipError_t launch_pref_stats(int dtype, const TokenArgs& a, const PrefArgs& p, h
 
 // Parts of a row where there are fewer rows than CUs: of 32 KB or more, a thousand in
 // all, from rows of more than 128 KB on (below, the launch that joins them takes as
-// long as it saves).
-int token_parts(int64_t n_slots, int64_t row_bytes) {
-  if (n_slots < 1 || n_slots >= 256 || row_bytes <= 131072) return 1;
+// long as it saves: log-probabilities of one row of 100 KB 6.1 us whole, 8.4 in parts; of
+// 64 bf16 rows of 100000 9.2 and 7.8, of 200 fp32 rows of 131072 26 and 21).  Where the
+// gradient is read again in parts though a whole row's would be in registers, up to half
+// as many rows (one bf16 row of 131072: 14.7 us whole, 7.8 in parts; 64: 15.4 and 10.4;
+// 128 fp32 rows of 80000: 21.4 and 21.2; 200: 28.3 and 30.7).
+int token_parts(int mode, int64_t n_slots, int64_t row_bytes) {
+  const int64_t most = mode == kTokenPolicy ? 128 : 256;
+  if (n_slots < 1 || n_slots >= most || row_bytes <= 131072) return 1;
   const int64_t by_size = (row_bytes + 32767) / 32768, by_count = (1024 + n_slots - 1) / n_slots;
   return (int)(by_size < by_count ? (by_size < 64 ? by_size : 64) : (by_count < 64 ? by_count : 64));
 }
 
+// Threads of a launch stay below 2^32.
+constexpr int64_t kGroupsMost = 1 << 20;
+
 // A second launch costs the host 3 us, what a call this small waits for: 8 examples of
-// 32 rows of 4 KB take 7.2 us in one launch, 5.3 in two (and 9 of the host); 256 of 16
-// rows 6.5 against 11.5.  Longer rows take too long in one wave: 16 rows of 16 KB,
+// 32 rows of 4 KB take 7.6 us in one launch, 8.5 in two; 512 of 16 rows of 8 KB 23.8 and
+// 24.7; 16384 of 4 of 4 KB 86 and 97.  Many long ones fill the card either way: 2048 of
+// 32 rows of 4 KB 95 and 89.  Longer rows take too long in one wave: 16 rows of 16 KB,
 // 15.2 against 6.6.
 bool policy_by_example(int64_t row_bytes, int64_t T, int64_t n) {
-  return n <= 4096 && T > 1 && (row_bytes <= 4096 ? T <= kPolicyExampleMost : row_bytes <= 8192 && T <= 16);
+  if (T < 2 || n > kGroupsMost || (T > 8 && n * T > 16384)) return false;
+  return row_bytes <= 4096 ? T <= kPolicyExampleMost : row_bytes <= 8192 && T <= 16;
 }
 
 hipError_t launch_policy_examples(int dtype, const TokenArgs& a, const PolicyArgs& p, uint32_t n, float* loss,
@@ -1029,8 +1048,18 @@ hipError_t launch_example_sum(const float* token_loss, uint32_t T, uint32_t n, f
   return hipGetLastError();
 }
 
+// Pairs of short rows at once: 32 pairs of 16 tokens and rows of 4 KB 9.3 us, 13.1 in
+// two launches; 2048 of 8 tokens 48 and 68 (4 of 16 tokens of 8 KB: 10.5 and 8.8).
 bool pref_by_pair(int64_t row_bytes, int64_t T, int64_t n_pairs) {
-  return row_bytes <= 8192 && T <= kPrefPairMost && n_pairs <= 4096;
+  return row_bytes <= 8192 && T <= kPrefPairMost && n_pairs <= kGroupsMost;
+}
+
+// Every row adds up its pair's tokens itself instead of a launch between the two: 192
+// tokens of 32 KB take 10.5 us, 13.7 with it; 2048 of 16 KB 16.2 and 17.9; 4096 of 4 KB in
+// sequences of 512 16.4 and 14.8.  Of long rows, whose workgroups are large, fewer: 800 of
+// 100 KB take 49.2 and 46.4.
+bool pref_pairs_within(int64_t row_bytes, int64_t T, int64_t n_slots) {
+  return T <= 1024 && n_slots <= (row_bytes <= 65536 ? 2048 : 512);
 }
 
 hipError_t launch_pref_pairs(int dtype, const TokenArgs& a, const PrefArgs& p, hipStream_t s) {

@@ -634,3 +634,58 @@ def test_largest_entries_late_in_the_row():
             _, wlp, wg = O.policy_loss(b.numpy(), b.target, 300, 1, np.ones(300))
             check_logp(b, host(logp), None)
             check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 2 * U, np.zeros(300))
+
+
+def test_gradients_of_tiny_weights():
+    """Weights of 1e-15 on rows whose maximum is 60 above their first elements: nothing of
+    the gradient, near fp32's least normal number as an exponential's factor, is lost."""
+    for V in (3000, 9000, 50000):
+        say(f"case: tiny weights V={V}")
+        b = Batch(V + 1, torch.float32, V, 300, 1)
+        b.z[:, :3 * V // 4] -= 60.0
+        b.target[:] = 5
+        b.weight = np.full(300, 1e-15, np.float32)
+        b.sync()
+        loss, (dl, _) = torch.zeros(300, device="cuda"), b.dbuf()
+        P.attr_policy_loss(b.tokens(), torch.ones(300, device="cuda"), loss, dlogits=dl)
+        _, wlp, wg = O.policy_loss(b.numpy(), b.target, 300, 1, np.ones(300), weight=b.weight)
+        check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 3 * U, np.zeros(300))
+
+
+@pytest.mark.parametrize("V,T", [(500, 4), (5000, 4), (40000, 20)])
+def test_pairs_with_an_impossible_token(V, T):
+    """A rejected token of probability 0: nothing is left to learn; a chosen one: the loss is infinite."""
+    say(f"case: impossible token V={V} T={T}")
+    b = Batch(V, torch.float32, V, 4, T)
+    at = lambda i: (i * T + 1, int(b.target[i * T + 1]))
+    b.z[at(2)] = -math.inf  # rejected, of pair 0
+    b.z[at(1)] = -math.inf  # chosen, of pair 1
+    b.sync()
+    for smoothing, want in ((0.0, [0.0, math.inf]), (1.0, [math.inf, 0.0]), (0.25, [math.inf, math.inf])):
+        loss, (dl, _) = torch.zeros(2, device="cuda"), b.dbuf()
+        P.attr_preference_loss(b.tokens(), loss, dlogits=dl, label_smoothing=smoothing)
+        assert loss.tolist() == want, (smoothing, loss)
+        _, _, wlp, wg = O.preference_loss(b.numpy(), b.target, 4, T, label_smoothing=smoothing)
+        check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 4 * U, np.zeros(4 * T))
+
+
+@pytest.mark.parametrize("n,T,V", [(6000, 2, 64), (9000, 3, 40), (600, 30, 40)])
+def test_many_short_examples(n, T, V):
+    """Thousands of examples of few short rows, both losses."""
+    say(f"case: many examples n={n} T={T} V={V}")
+    b = Batch(n, torch.float32, V, n, T, weighted=True)
+    adv = torch.from_numpy(b.r.uniform(-1, 1, n).astype(np.float32))
+    loss, (dl, _) = torch.zeros(n, device="cuda"), b.dbuf()
+    P.attr_policy_loss(b.tokens(), adv.cuda(), loss, dlogits=dl)
+    wl, wlp, wg = O.policy_loss(b.numpy(), b.target, n, T, adv.numpy(), weight=b.weight)
+    # on policy: a token's loss is -w A, its sums' rounding apart
+    assert (np.abs(host(loss) - wl) <= 2 * U * T * 1.5).all()
+    check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 2 * U, np.zeros(b.rows))
+    pl, (dl, _) = torch.zeros(n // 2, device="cuda"), b.dbuf()
+    P.attr_preference_loss(b.tokens(), pl, dlogits=dl)
+    wl, _, wlp, wg = O.preference_loss(b.numpy(), b.target, n, T, weight=b.weight)
+    tol = sum(1.5 * 0.1 * logp_tol(np.array([wlp[i * T + t] for i in range(n)]), V) for t in range(T))
+    h_tol = tol[:n // 2] + tol[n // 2:]
+    assert (np.abs(host(pl) - wl) <= h_tol + 2 * U * (1 + np.abs(wl))).all()
+    c_abs = np.repeat(np.concatenate([h_tol, h_tol]) * 1.5 * 0.1 / 4, T)
+    check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 4 * U, c_abs)

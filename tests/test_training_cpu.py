@@ -215,3 +215,9 @@ def test_native_call_refuses_what_it_does_not_know():
         assert _marshal.token_call(*args) is None
     with pytest.raises(TypeError, match="12 arguments"):
         _marshal.token_call(1)
+
+
+@pytest.mark.parametrize("scale,status", [(2.5e38, INVALID), (2.0e38, 0)])
+def test_logit_scale_stays_finite(scale, status):
+    """The scale times log2 e is what multiplies a logit: past 2e38 it is infinite."""
+    assert _calls(_rows(logit_scale=scale, n_examples=0)) == [status] * 3
