@@ -302,7 +302,8 @@ attr_status attr_score_topk(const void* Q, int64_t n_q, int64_t ldq, const void*
  * Outputs of rows that do not count: without row_offset every row i * T + t,
  * t < T, is written (logp 0, dlogits zeros); with row_offset the rows of
  * tokens t < length[i] (clamped to [0, T]), and no others, are written.  The
- * ranges of two examples must not overlap.
+ * ranges of two examples must not overlap, nor may a call's outputs overlap each
+ * other or its inputs (but for dlogits over the logits, see below).
  * Read only during the call (host struct with device pointers). */
 typedef struct {
   const void* logits;    /* [n_rows, V], row stride ldl >= V; any V, stride and element alignment */

@@ -662,6 +662,47 @@ attr_status dlogits_validate(const attr_token_rows* r, void* dlogits, int64_t ld
   return ATTR_OK;
 }
 
+// Outputs overlap neither each other nor an input: workgroups of one row read its loss's
+// inputs while another of them writes (dlogits and the logits: dlogits_validate).
+class TokenSpans {
+ public:
+  explicit TokenSpans(const attr_token_rows* r) : n_rows_(r->n_rows) {
+    input(r->target, r->n_rows, 8);
+    input(r->weight, r->n_rows, 4);
+    input(r->row_offset, r->n_examples, 8);
+    input(r->length, r->n_examples, 4);
+  }
+  void input(const void* p, int64_t n, int eb) {
+    if (p && n > 0) in_[n_in_++] = span_of(p, 1, n, n, eb);
+  }
+  void output(const void* p, int64_t n, int eb = 4) {
+    if (p && n > 0) out_[n_out_++] = span_of(p, 1, n, n, eb);
+  }
+  // `r`'s logits are an input of every output but dlogits.
+  attr_status check(const attr_token_rows* r, const void* dlogits, int64_t ldd, const char* who) {
+    const int eb = dtype_bytes(r->dtype);
+    const Span logits = span_of(r->logits, n_rows_, r->V, r->ldl, eb);
+    bool bad = false;
+    for (int i = 0; i < n_out_; ++i) {
+      bad |= n_rows_ > 0 && overlap(out_[i], logits);
+      for (int j = 0; j < i; ++j) bad |= overlap(out_[i], out_[j]);
+    }
+    if (dlogits && n_rows_ > 0) {
+      const Span d = span_of(dlogits, n_rows_, r->V, ldd, eb);
+      for (int i = 0; i < n_out_; ++i) bad |= overlap(d, out_[i]);
+      out_[n_out_++] = d;
+    }
+    for (int i = 0; i < n_out_; ++i)
+      for (int j = 0; j < n_in_; ++j) bad |= overlap(out_[i], in_[j]);
+    return bad ? fail(ATTR_ERR_INVALID_ARG, "%s: outputs overlap each other or the inputs", who) : ATTR_OK;
+  }
+
+ private:
+  Span in_[8], out_[4];  // four of the rows and up to three of the loss; three vectors and dlogits
+  int n_in_ = 0, n_out_ = 0;
+  int64_t n_rows_;
+};
+
 // Workspace of the three calls: what each keeps per token slot, per pair and per part
 // of a row.
 struct TokenLayout {
@@ -747,6 +788,10 @@ attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, 
     if (rows->n_examples == 0 || rows->n_rows == 0) return ATTR_OK;
     if (!logp) return fail(ATTR_ERR_INVALID_ARG, "%s: logp is NULL", who);
     if (!aligned_to(logp, 4)) return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    TokenSpans spans(rows);
+    spans.output(logp, rows->n_rows);
+    st = spans.check(rows, nullptr, 0, who);
+    if (st != ATTR_OK) return st;
     const TokenLayout L = token_layout(rows, attr::kTokenLogp);
     st = token_workspace(L, ws, ws_bytes, who);
     if (st != ATTR_OK) return st;
@@ -779,6 +824,14 @@ attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage
     if (!aligned_to(advantage, 4) || !aligned_to(logp_old, 4) || !aligned_to(logp_ref, 4) || !aligned_to(loss, 4) ||
         !aligned_to(logp, 4))
       return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    TokenSpans spans(rows);
+    spans.input(advantage, per_token ? rows->n_rows : rows->n_examples, 4);
+    spans.input(logp_old, rows->n_rows, 4);
+    spans.input(beta != 0.f ? logp_ref : nullptr, rows->n_rows, 4);
+    spans.output(loss, rows->n_examples);
+    spans.output(logp, rows->n_rows);
+    st = spans.check(rows, dlogits, ldd, who);
+    if (st != ATTR_OK) return st;
     const TokenLayout L = token_layout(rows, attr::kTokenPolicy);
     st = token_workspace(L, ws, ws_bytes, who);
     if (st != ATTR_OK) return st;
@@ -832,6 +885,14 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
     if (!aligned_to(logp_ref, 4) || !aligned_to(pair_weight, 4) || !aligned_to(loss, 4) ||
         !aligned_to(log_ratio, 4) || !aligned_to(logp, 4))
       return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    TokenSpans spans(rows);
+    spans.input(logp_ref, rows->n_rows, 4);
+    spans.input(pair_weight, rows->n_examples / 2, 4);
+    spans.output(loss, rows->n_examples / 2);
+    spans.output(log_ratio, rows->n_examples);
+    spans.output(logp, rows->n_rows);
+    st = spans.check(rows, dlogits, ldd, who);
+    if (st != ATTR_OK) return st;
     const TokenLayout L = token_layout(rows, attr::kTokenPref);
     st = token_workspace(L, ws, ws_bytes, who);
     if (st != ATTR_OK) return st;

@@ -221,3 +221,35 @@ def test_native_call_refuses_what_it_does_not_know():
 def test_logit_scale_stays_finite(scale, status):
     """The scale times log2 e is what multiplies a logit: past 2e38 it is infinite."""
     assert _calls(_rows(logit_scale=scale, n_examples=0)) == [status] * 3
+
+
+def test_outputs_stay_apart():
+    """Outputs over inputs or each other are refused: rows are taken by several workgroups."""
+    L, z = P.lib(), 0x100000   # 8 rows of 100 fp32 logits: 3200 bytes
+    apart = dict(target=0x110000, weight=0x120000, row_offset=0x130000, length=0x140000)
+    rows = _rows(**apart)
+    old, ref, adv, loss, logp, ratio, d = (0x200000 + 0x10000 * i for i in range(7))
+    no_ws = (None, 0, None)
+
+    def logp_call(out):
+        return L.attr_token_logp(rows, out, *no_ws)
+
+    def policy(per=0, old=old, ref=ref, adv=adv, loss=loss, logp=logp, d=d):
+        return L.attr_policy_loss(rows, adv, per, old, ref, 0.2, 0.2, 0.1, loss, logp, d, 100, *no_ws)
+
+    def pref(ref=ref, pw=adv, loss=loss, ratio=ratio, logp=logp, d=d):
+        return L.attr_preference_loss(rows, ref, pw, 0.1, 0.0, 0.0, loss, ratio, logp, d, 100, *no_ws)
+    assert policy() == policy(per=1) == pref() == WORKSPACE   # apart: only the workspace is missing
+    assert policy(d=z) == pref(d=z) == WORKSPACE              # dlogits over the logits
+    assert policy(logp=adv + 16) == WORKSPACE                 # after the last example's advantage
+    ends = (z, z + 3196, 0x110000, 0x110000 + 60, 0x120000 + 28, 0x130000 + 28, 0x140000 + 12)
+    for at in ends:
+        assert logp_call(at) == policy(logp=at) == policy(loss=at) == pref(logp=at) == pref(loss=at) == INVALID, hex(at)
+        assert pref(ratio=at) == INVALID and b"overlap" in L.attr_last_error()
+    for at in ends[2:]:
+        assert policy(d=at) == pref(d=at) == INVALID, hex(at)
+    for kw in (dict(logp=old), dict(logp=ref + 28), dict(logp=adv), dict(per=1, logp=adv + 16), dict(loss=adv),
+               dict(loss=logp), dict(logp=d + 3196), dict(d=old), dict(d=loss)):
+        assert policy(**kw) == INVALID, kw
+    for kw in (dict(logp=ref), dict(loss=adv), dict(loss=ratio + 12), dict(ratio=logp), dict(ratio=d), dict(d=ref)):
+        assert pref(**kw) == INVALID, kw
