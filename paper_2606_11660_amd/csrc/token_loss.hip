@@ -262,6 +262,14 @@ __device__ inline float row_logp(float zy, float c, const RowSum& r) {
   return ((float)l.whole - l.rest) * kLn2;
 }
 
+// c m as the fused form's offset: the rounded product itself, and never the exact one within
+// a difference of two offsets (contracted, a sum would be rescaled to another offset than its
+// next terms are relative to: at logits near 1e5 logp lost 1e-4).
+__device__ inline float offset_at(float m, float c) {
+#pragma clang fp contract(off)
+  return m * c;
+}
+
 // Whether the fused form takes a row (part) with maximum m; not if it is NaN.
 __device__ inline bool fused(float m, float c) { return fabsf(m * c) <= kMostMc; }
 
@@ -332,7 +340,7 @@ __device__ inline RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& 
   const Cut k = cut_row<T, NT>(z, V);
   const T* zv = z + k.head;
   float top = k.at < V ? (float)z[k.at] : -INFINITY;
-  float mc = fmaxf(top * c, -kMostMc), s = __builtin_amdgcn_exp2f(fmaf(top, c, -mc));
+  float mc = fmaxf(offset_at(top, c), -kMostMc), s = __builtin_amdgcn_exp2f(fmaf(top, c, -mc));
   for (int32_t j0 = thread<NT>() * E; j0 < k.whole; j0 += NT * E * U) {
     i32x4 v[U];
 #pragma unroll
@@ -345,9 +353,10 @@ __device__ inline RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& 
 #pragma unroll
       for (int e = 1; e < E; ++e) m = fmaxf(m, x[e]);
       top = fmaxf(top, m);
-      if (m * c > mc) {
-        s *= __builtin_amdgcn_exp2f(mc - m * c);
-        mc = m * c;
+      const float up = offset_at(m, c);
+      if (up > mc) {
+        s *= __builtin_amdgcn_exp2f(mc - up);
+        mc = up;
       }
 #pragma unroll
       for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
@@ -355,7 +364,7 @@ __device__ inline RowSum row_sum_stream(const T* z, int32_t V, float c, Shared& 
   }
   const float m = block_max<NT>(top, sh.max);
   if (!fused(m, c)) return row_sum_apart<T, NT>(z, V, c, m, sh.slow);
-  const float most = m * c;
+  const float most = offset_at(m, c);
   s *= __builtin_amdgcn_exp2f(mc - most);
   return {most, block_add<NT>(s, sh.sum), m, false};
 }
@@ -523,7 +532,7 @@ struct RowRegs {
       for (int e = 0; e < E; ++e) m = fmaxf(m, x[e]);
     }
     m = block_max<NT>(m, sh.max);
-    const float mc = m * c;
+    const float mc = offset_at(m, c);
     float s = __builtin_amdgcn_exp2f(fmaf((float)rest, c, -mc));
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -685,7 +694,7 @@ __device__ inline float2 part_sum(const T* z, int32_t n, float c, Shared& sh) {
 __device__ inline RowSum join_parts(const float2* part, int32_t n, float c) {
   const int lane = threadIdx.x & 63;
   const float2 k = lane < n ? part[lane] : float2{-INFINITY, 0.f};
-  const float m = wave_max_dpp(k.x), mc = m * c;
+  const float m = wave_max_dpp(k.x), mc = offset_at(m, c);
   const float s = wave_sum_dpp(k.y == 0.f ? 0.f : k.y * __builtin_amdgcn_exp2f((k.x - m) * c));
   if (fused(m, c)) return {mc, s * __builtin_amdgcn_exp2f(fmaf(m, c, -mc)), m, false};
   return {m, s, m, true};

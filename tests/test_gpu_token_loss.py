@@ -689,3 +689,38 @@ def test_many_short_examples(n, T, V):
     assert (np.abs(host(pl) - wl) <= h_tol + 2 * U * (1 + np.abs(wl))).all()
     c_abs = np.repeat(np.concatenate([h_tol, h_tol]) * 1.5 * 0.1 / 4, T)
     check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 4 * U, c_abs)
+
+
+def offset_tol(lps, lp):
+    """Error of a log-probability into which no offset of the logits enters, in units of u.  An exponential's
+    argument and its factor log2 e are rounded once each (2 |x|, weighted by the probabilities, and 2 |lp| for
+    the target), an exponential is within an ulp (2), a thread's largest element grows a dozen times by far at
+    most (an exponential and a product each: 36), the roundings of n additions add up like sqrt(n) (8 of them;
+    a thread takes 64 elements of rows up to 128 KB, V / 512 of longer ones, the trees 16), logp has 4 |lp|."""
+    far = (lps.exp() * (lps.max(1, keepdim=True)[0] - lps)).sum(1)
+    return U * (8 * math.sqrt(max(64, lps.shape[1] / 512) + 16) + 38 + 2 * far + 6 * lp.abs())
+
+
+@pytest.mark.parametrize("V,rows", [(1000, 90), (8193, 40), (20011, 300), (50257, 24), (70001, 300), (300007, 6)])
+@pytest.mark.parametrize("dtype", list(NAMES), ids=NAMES.get)
+def test_offset_logits(dtype, V, rows):
+    """A constant beside every logit costs a log-probability no more than the logits' own rounding."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    base = torch.randn((rows, V), generator=gen, device="cuda") * 2.5
+    y = torch.randint(0, V, (rows,), generator=gen, device="cuda")
+    for offset in (0.0, 3e3, -3e3, 5e4, 1e5, -1e5, 5e5, -5e5):
+        if dtype == torch.float16 and abs(offset) > 6e4:
+            continue
+        say(f"case: offset logits {NAMES[dtype]} V={V} rows={rows} offset={offset}")
+        z = (base + offset).to(dtype)
+        lps = torch.log_softmax(z.double(), 1)
+        lp = lps[torch.arange(rows, device="cuda"), y]
+        tol = offset_tol(lps, lp)
+        tok = P.TokenRows(z, y, rows, 1)
+        logp, pref, policy = (torch.full((rows,), 7.0, device="cuda") for _ in range(3))
+        P.attr_token_logp(tok, logp)
+        P.attr_preference_loss(tok, torch.empty(rows // 2, device="cuda"), logp=pref)
+        P.attr_policy_loss(tok, torch.ones(rows, device="cuda"), torch.empty(rows, device="cuda"), logp=policy,
+                           dlogits=torch.empty_like(z))
+        for got in (logp, pref, policy):
+            assert ((got.double() - lp).abs() <= tol).all(), (offset, (got.double() - lp).abs().max())
