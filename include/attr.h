@@ -42,7 +42,9 @@
  *   checked on the host; their documented clamping applies instead.
  * - Calls that share a workspace or an output must be ordered by the
  *   caller (same stream, or events); concurrent calls on different
- *   workspaces are independent.
+ *   workspaces are independent.  A call may be several launches: one stream
+ *   orders the calls of one host thread, while those that several threads make
+ *   on it at the same time may interleave and must not share a workspace.
  */
 #ifndef ATTR_H_
 #define ATTR_H_

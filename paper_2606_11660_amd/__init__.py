@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 import warnings
 from typing import Dict, Iterable, List, Optional, Sequence, Tuple
 
@@ -256,9 +257,11 @@ def _torch_stream(stream):
 class Workspace:
     """Grow-only device scratch buffer handed to the library calls.
 
-    A workspace serves one stream at a time: calls that may overlap on
-    different streams need workspaces of their own (the default workspace is
-    kept per device and stream).  Every stream of use is recorded on the
+    A workspace serves one stream and one host thread at a time: calls that may
+    overlap on different streams need workspaces of their own, and so do calls
+    that several threads make on one stream, since a call is several launches
+    and another thread's may come between them (the default workspace is kept
+    per device, stream and thread).  Every stream of use is recorded on the
     buffer (once: torch's allocator keeps a buffer's streams until it is
     freed), so a buffer replaced by a larger one is not handed out again
     before the work queued on those streams has finished.
@@ -289,13 +292,14 @@ class Workspace:
         return self._buf.data_ptr(), self._buf.numel()
 
 
-_default_ws: Dict[Tuple[torch.device, int], Workspace] = {}
+_default_ws: Dict[Tuple[torch.device, int, int], Workspace] = {}
 
 
 def _ws(ws: Optional[Workspace], device, stream=None) -> Workspace:
     if ws is not None:
         return ws
-    key = (device, _stream(stream))
+    # a thread that has ended leaves its identity, and so its workspaces, to a later one
+    key = (device, _stream(stream), threading.get_ident())
     if key not in _default_ws:
         _default_ws[key] = Workspace(device)
     return _default_ws[key]

@@ -724,3 +724,32 @@ def test_offset_logits(dtype, V, rows):
                            dlogits=torch.empty_like(z))
         for got in (logp, pref, policy):
             assert ((got.double() - lp).abs() <= tol).all(), (offset, (got.double() - lp).abs().max())
+
+
+def test_two_threads_on_one_stream():
+    """Losses that two host threads compute at once, with the default workspace, are those of one thread."""
+    import threading
+    jobs, wrong = [], []
+    for k, (V, n, T) in enumerate(((5003, 4, 30), (4201, 6, 24))):
+        b = Batch(100 + k, torch.float32, V, n, T, weighted=True)
+        tok, adv = b.tokens(), torch.from_numpy(b.r.standard_normal(n).astype(np.float32)).cuda()
+        want, pair = torch.empty(n, device="cuda"), torch.empty(n // 2, device="cuda")
+        P.attr_policy_loss(tok, adv, want)
+        P.attr_preference_loss(tok, pair)
+        jobs.append((b, tok, adv, want, pair))
+    torch.cuda.synchronize()
+
+    def work(b, tok, adv, want, pair):
+        got = [(torch.empty_like(want), torch.empty_like(pair)) for _ in range(200)]
+        for loss, pl in got:
+            P.attr_policy_loss(tok, adv, loss)
+            P.attr_preference_loss(tok, pl)
+        torch.cuda.synchronize()
+        wrong.extend(i for i, (loss, pl) in enumerate(got) if not torch.equal(loss, want) or not torch.equal(pl, pair))
+    say("case: two threads on one stream")
+    threads = [threading.Thread(target=work, args=job) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong

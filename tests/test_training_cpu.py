@@ -253,3 +253,25 @@ def test_outputs_stay_apart():
         assert policy(**kw) == INVALID, kw
     for kw in (dict(logp=ref), dict(loss=adv), dict(loss=ratio + 12), dict(ratio=logp), dict(ratio=d), dict(d=ref)):
         assert pref(**kw) == INVALID, kw
+
+
+def test_default_workspaces_are_a_threads_own():
+    """Calls of several launches that two threads make on one stream may interleave: no scratch is shared."""
+    import threading
+    device, seen = torch.device("cuda", 0), {}
+    together = threading.Barrier(2)
+
+    def look(k):
+        first = P._ws(None, device, 0)
+        together.wait()
+        seen[k] = (first, P._ws(None, device, 0), P._ws(None, device, 64))
+        together.wait()
+    threads = [threading.Thread(target=look, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    (a, b, c), (d, e, f) = seen[0], seen[1]
+    assert a is b and d is e and len({id(x) for x in (a, c, d, f)}) == 4
+    own = P.Workspace("cuda")
+    assert P._ws(own, device, 0) is own
