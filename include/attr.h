@@ -336,6 +336,8 @@ attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, 
  *     c = dloss/dlogp = w ((-A ratio if that is the maximum, else 0)
  *                          - beta (exp(logp_ref - logp) - 1))
  *     dlogits[row, j] = s c ([j = target] - exp(logp_j))
+ * Beside a finite logp_ref a target of probability 0 (logit -inf) makes the KL
+ * term, and so a loss with beta > 0, +inf; its row of dlogits is then not finite.
  * The weights carry the mask and the normalisation (1 / tokens for a mean over
  * each example, one constant for a sum, a loss scale).  Each row of logits is
  * read once and each row of dlogits written once where a row fits a

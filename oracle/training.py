@@ -61,7 +61,7 @@ def policy_loss(logits, target, n_examples, T, advantage, scale=1.0, weight=None
         value, c = max(free, held), free if free >= held else 0.0
         if beta != 0:
             d = float(logp_ref[row]) - lp
-            value += beta * (np.expm1(d) - d)
+            value += beta * (np.inf if d == np.inf else np.expm1(d) - d)
             c -= beta * np.expm1(d)
         loss[i] += w * value
         grad[row] = _d_row(lps, target[row], w * c, scale)

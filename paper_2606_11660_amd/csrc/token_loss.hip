@@ -421,7 +421,7 @@ __device__ inline TokenLoss policy_token(const PolicyArgs& p, const PolicyToken&
   if (ratio != ratio) loss = c = ratio;  // a NaN stays
   if (p.beta != 0.f) {
     const float d = k.ref - logp, less = expm1f(d);
-    loss += p.beta * (less - d);
+    loss += p.beta * (less == INFINITY ? less : less - d);  // a token of probability 0: d is infinite too
     c -= p.beta * less;
   }
   return {k.weight * loss, k.weight * c};

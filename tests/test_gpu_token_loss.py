@@ -753,3 +753,22 @@ def test_two_threads_on_one_stream():
     for t in threads:
         t.join()
     assert not wrong
+
+
+@pytest.mark.parametrize("V,n,T", [(300, 3, 4), (5000, 3, 2), (40000, 3, 2), (70001, 3, 50), (140000, 3, 2)])
+def test_infinite_kl(V, n, T):
+    """A counting token of probability 0 beside a reference that allows it: the KL term is infinite, not NaN."""
+    say(f"case: infinite KL V={V} n={n} T={T}")
+    b = Batch(V, torch.float32, V, n, T)
+    at = T + 1                                       # of the second example
+    b.z[at, int(b.target[at])] = -math.inf
+    b.sync()
+    old, ref = np.full(b.rows, -3.0, np.float32), np.full(b.rows, -2.5, np.float32)
+    adv = np.array([0.5, -1.0, 1.0], np.float32)
+    up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    loss = torch.zeros(n, device="cuda")
+    P.attr_policy_loss(b.tokens(), up(adv), loss, logp_old=up(old), logp_ref=up(ref), beta=0.1)
+    want = O.policy_loss(b.numpy(), b.target, n, T, adv, logp_old=old, logp_ref=ref, beta=0.1)[0]
+    assert want[1] == math.inf and host(loss)[1] == math.inf
+    got = host(loss)[[0, 2]]
+    assert np.isfinite(got).all() and np.isfinite(want[[0, 2]]).all()
