@@ -415,8 +415,9 @@ struct TokenLoss {
 };
 __device__ inline TokenLoss policy_token(const PolicyArgs& p, const PolicyToken& k, float logp) {
   const float ratio = p.logp_old ? expf(logp - k.old) : logp == logp ? 1.f : logp;
-  const float free_ = -k.advantage * ratio;
-  const float held = -k.advantage * fminf(fmaxf(ratio, p.lo), p.hi);
+  const float taken = k.advantage == 0.f ? 1.f : ratio;  // an advantage of 0 takes 0 of a ratio past fp32 too
+  const float free_ = -k.advantage * taken;
+  const float held = -k.advantage * fminf(fmaxf(taken, p.lo), p.hi);
   float loss = free_ >= held ? free_ : held, c = free_ >= held ? free_ : 0.f;
   if (ratio != ratio) loss = c = ratio;  // a NaN stays
   if (p.beta != 0.f) {

@@ -772,3 +772,15 @@ def test_infinite_kl(V, n, T):
     assert want[1] == math.inf and host(loss)[1] == math.inf
     got = host(loss)[[0, 2]]
     assert np.isfinite(got).all() and np.isfinite(want[[0, 2]]).all()
+
+
+@pytest.mark.parametrize("V,n,T", [(300, 3, 4), (5000, 3, 2), (140000, 3, 2)])
+def test_advantages_of_zero_beside_large_ratios(V, n, T):
+    """A ratio of e^193, past fp32, times an advantage of 0 is 0, clipped from above or not."""
+    say(f"case: advantages of zero V={V} n={n} T={T}")
+    b = Batch(V, torch.float32, V, n, T)
+    old = torch.full((b.rows,), -200.0, device="cuda")
+    for high in (0.2, math.inf):
+        loss, (dl, _) = torch.full((n,), 7.0, device="cuda"), b.dbuf()
+        P.attr_policy_loss(b.tokens(), torch.zeros(n, device="cuda"), loss, dlogits=dl, logp_old=old, clip_high=high)
+        assert (loss == 0).all() and (dl == 0).all(), high
