@@ -365,7 +365,9 @@ attr_status attr_policy_loss(const attr_token_rows* rows, const float* advantage
  *     log_ratio[i] = sum_t w (logp - logp_ref)      (over tokens that count)
  *     h = beta (log_ratio[p] - log_ratio[n_pairs + p]) - margin
  *     loss[p] = pw ((1 - e) softplus(-h) + e softplus(h)),  e = label_smoothing
- *                                  (a term of factor 0 is 0, also at infinite h)
+ *                                  (a term of factor 0 is 0, also at infinite h;
+ *                                  so are the loss and the rows of dlogits of a
+ *                                  pair of weight 0, whatever its logits hold)
  *     c = dloss/dlogp = +-w pw beta (e sigma(h) - (1 - e) sigma(-h))
  *                                  (+: chosen, -: rejected)
  *     dlogits[row, j] = s c ([j = target] - exp(logp_j))

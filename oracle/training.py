@@ -84,12 +84,12 @@ def preference_loss(logits, target, n_examples, T, scale=1.0, weight=None, row_o
             rows[row] = (i, lps, w)
     h = beta * (ratio[:n_pairs] - ratio[n_pairs:]) - margin
     pw = np.ones(n_pairs) if pair_weight is None else np.asarray(pair_weight, np.float64)[:n_pairs]
-    loss = pw * ((1 - e) * np.logaddexp(0, -h) + e * np.logaddexp(0, h))
-    dh = pw * beta * (e / (1 + np.exp(-h)) - (1 - e) / (1 + np.exp(h)))
+    loss = np.where(pw == 0, 0.0, pw * ((1 - e) * np.logaddexp(0, -h) + e * np.logaddexp(0, h)))
+    dh = np.where(pw == 0, 0.0, pw * beta * (e / (1 + np.exp(-h)) - (1 - e) / (1 + np.exp(h))))
     grad = {}
     for row, (i, lps, w) in rows.items():
         c = w * (dh[i] if i < n_pairs else -dh[i - n_pairs])
-        grad[row] = np.zeros(logits.shape[1]) if lps is None else _d_row(lps, target[row], c, scale)
+        grad[row] = np.zeros(logits.shape[1]) if lps is None or c == 0 else _d_row(lps, target[row], c, scale)
     return loss, ratio, logp, grad
 
 

@@ -807,20 +807,21 @@ __device__ inline double threads_sum(double v, double* sh) {
 }
 
 // A pair's loss from its log ratios (written where `outputs`); returns the derivative
-// by the log-probability of a chosen token of weight 1.
+// by the log-probability of a chosen token of weight 1.  A pair of weight 0 has 0 of both,
+// whatever its log ratios.
 __device__ inline float pair_loss(const PrefArgs& p, uint32_t pair, const double (&ratio)[2], bool outputs) {
   const double h = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin;
   const float pw = p.pair_weight ? p.pair_weight[pair] : 1.f, e = p.smoothing;
   if (outputs) {
     // a share of nothing is not taken of an infinite ratio's loss
     const double won = e < 1.f ? (1.0 - (double)e) * softplus(-h) : 0.0, lost = e > 0.f ? (double)e * softplus(h) : 0.0;
-    p.loss[pair] = (float)((double)pw * (won + lost));
+    p.loss[pair] = pw != 0.f ? (float)((double)pw * (won + lost)) : 0.f;
     if (p.log_ratio) {
       p.log_ratio[pair] = (float)ratio[0];
       p.log_ratio[pair + p.n_pairs] = (float)ratio[1];
     }
   }
-  return pw * p.beta * (e / (1.f + expf((float)-h)) - (1.f - e) / (1.f + expf((float)h)));
+  return pw != 0.f ? pw * p.beta * (e / (1.f + expf((float)-h)) - (1.f - e) / (1.f + expf((float)h))) : 0.f;
 }
 
 // The same from the parts of its tokens, summed by NT threads.
@@ -889,7 +890,7 @@ __global__ __launch_bounds__(1024) void pref_pair_kernel(TokenArgs a, PrefArgs p
     if (!a.dlogits || !sl[side].write) continue;
     T* out = (T*)a.dlogits + sl[side].row * a.ldd;
     const float cs = (side == 0 ? g : -g) * sl[side].weight * a.scale;
-    if (!sl[side].counts) row_zero<T, 64>(out, a.V);
+    if (!sl[side].counts || cs == 0.f) row_zero<T, 64>(out, a.V);
     else if (r[side].apart) row_grad_apart<T, 64>(row[side].z, out, a.V, sl[side].target, c, r[side], cs, -cs / r[side].sum);
     else row[side].grad(out, a.V, sl[side].target, c, r[side], cs);
   }
@@ -918,6 +919,7 @@ __global__ __launch_bounds__(group_of(NT)) void pref_grad_kernel(TokenArgs a, Pr
   const float2 st = a.stats[slot];
   const RowSum r{st.x, fabsf(st.y), 0.f, st.y < 0.f};
   const float cs = (i < p.n_pairs ? g : -g) * sl.weight * a.scale, ce = -cs / r.sum;
+  if (cs == 0.f) return row_zero<T, NT>(out, part.n);  // also of a row that holds NaN, in a pair of weight 0
   row_grad_stream<T, NT, U>((const T*)a.logits + sl.row * a.ldl + part.from, out, part.n, sl.target - part.from, c, r,
                             cs, ce);
 }

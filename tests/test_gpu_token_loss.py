@@ -784,3 +784,23 @@ def test_advantages_of_zero_beside_large_ratios(V, n, T):
         loss, (dl, _) = torch.full((n,), 7.0, device="cuda"), b.dbuf()
         P.attr_policy_loss(b.tokens(), torch.zeros(n, device="cuda"), loss, dlogits=dl, logp_old=old, clip_high=high)
         assert (loss == 0).all() and (dl == 0).all(), high
+
+
+@pytest.mark.parametrize("V,T", [(500, 4), (5000, 4), (700, 30), (40000, 300), (3000, 1200), (140000, 4)])
+def test_pairs_of_weight_zero(V, T):
+    """A pair of weight 0 adds nothing to the losses and gradients, though its tokens be impossible or its logits NaN."""
+    say(f"case: pairs of weight 0 V={V} T={T}")
+    b = Batch(V + T, torch.float32, V, 6, T)
+    b.z[T + 1, int(b.target[T + 1])] = -math.inf     # pair 1: a chosen token of probability 0
+    b.z[5 * T] = math.nan                            # pair 2: a rejected row of NaN
+    b.sync()
+    pw = np.array([0.75, 0.0, 0.0], np.float32)
+    for smoothing in (0.0, 0.25):
+        loss, (dl, _) = torch.full((3,), 7.0, device="cuda"), b.dbuf()
+        P.attr_preference_loss(b.tokens(), loss, dlogits=dl, pair_weight=torch.from_numpy(pw).cuda(), label_smoothing=smoothing)
+        got, rows = host(loss), dl.view(6, T, V)
+        assert got[0] > 0 and np.isfinite(got[0]) and (got[1:] == 0).all(), got
+        assert (rows[[1, 2, 4, 5]] == 0).all() and torch.isfinite(rows[[0, 3]]).all() and (rows[[0, 3]] != 0).any()
+        alone = torch.full((3,), 7.0, device="cuda")
+        P.attr_preference_loss(b.tokens(), alone, pair_weight=torch.from_numpy(pw).cuda(), label_smoothing=smoothing)
+        assert (alone[1:] == 0).all()

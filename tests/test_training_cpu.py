@@ -275,3 +275,11 @@ def test_default_workspaces_are_a_threads_own():
     assert a is b and d is e and len({id(x) for x in (a, c, d, f)}) == 4
     own = P.Workspace("cuda")
     assert P._ws(own, device, 0) is own
+
+
+def test_oracle_pairs_of_weight_zero():
+    """Loss and gradients of 0 in 64 bits too, beside infinities and NaN."""
+    z = np.random.default_rng(4).standard_normal((4, 9))
+    z[0, 2], z[3] = -np.inf, np.nan
+    loss, _, _, grad = O.preference_loss(z, [2, 1, 3, 4], 4, 1, pair_weight=[0.0, 0.0])
+    assert (loss == 0).all() and all((g == 0).all() for g in grad.values())
