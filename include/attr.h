@@ -432,7 +432,10 @@ typedef struct {
  *              masters); g_dtype the same three; state_dtype ATTR_F32 or
  *              ATTR_E4M3
  *   step       >= 1 (the first step is 1)
- *   beta1, beta2 in [0, 1);  eps, eps_root >= 0;  lr finite */
+ *   beta1, beta2 in [0, 1);  lr finite
+ *   eps        0 or in [2^-126, 3e38];  eps_root 0 or in [2^-149, 3e38] (fp32
+ *              divides by their sums; with both 0 a weight whose second moment
+ *              is 0 becomes NaN, as in the formula) */
 attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors, attr_dtype p_dtype,
                             attr_dtype g_dtype, attr_dtype state_dtype, int64_t step, double lr,
                             double beta1, double beta2, double eps, double eps_root,

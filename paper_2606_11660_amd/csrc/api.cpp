@@ -1003,6 +1003,11 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
       return fail(ATTR_ERR_INVALID_ARG, "%s: beta1 and beta2 must be in [0, 1)", who);
     if (!(eps >= 0.0 && eps <= 3.0e38) || !(eps_root >= 0.0 && eps_root <= 3.0e38) || !(std::fabs(lr) <= 3.0e38))
       return fail(ATTR_ERR_INVALID_ARG, "%s: lr, eps and eps_root must be finite, eps and eps_root >= 0", who);
+    // The step divides by sqrt(v + eps_root) + eps through fp32 reciprocals: an eps that fp32
+    // holds as a subnormal number or as 0 would make 0 / eps of an untouched weight NaN, and
+    // so would an eps_root that it holds as 0.
+    if ((eps > 0.0 && eps < 0x1p-126) || (eps_root > 0.0 && eps_root < 0x1p-149))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: eps must be 0 or at least 2^-126, eps_root 0 or at least 2^-149", who);
     if (!aligned_to(grad_scale, 4)) return fail(ATTR_ERR_ALIGNMENT, "%s: grad_scale must be 4-byte aligned", who);
     const bool eight = state_dtype == ATTR_E4M3;
     const size_t pb = (size_t)dtype_bytes(p_dtype), gb = (size_t)dtype_bytes(g_dtype), sb = eight ? 1 : 4;

@@ -275,3 +275,18 @@ def test_tiny_second_moments():
         tol = np.abs(want) * (32 * U + (2.0 ** -149 / np.where(gv > 0, gv, 1) if not eps else 0)) + 1e-37
         assert (np.abs(got - want) <= tol)[live].all()
         assert eps or not np.isfinite(got[~live]).any() or (~live).sum() == 0
+
+
+@pytest.mark.parametrize("eps,root", [(2.0 ** -126, 0.0), (1e-30, 0.0), (0.0, 1e-40), (0.0, 2.0 ** -149)])
+def test_least_eps_leaves_untouched_weights(eps, root):
+    """Zero gradients and moments: no step, down to the least eps that is taken."""
+    say(f"case: least eps {eps} {root}")
+    for eight in (False, True):
+        kind = torch.float8_e4m3fn if eight else torch.float32
+        p, g = torch.ones(512, device="cuda"), torch.zeros(512, device="cuda")
+        m, v = (torch.zeros(512, dtype=kind, device="cuda") for _ in range(2))
+        scales = dict(m_scale=[torch.zeros(2, device="cuda")], v_scale=[torch.zeros(2, device="cuda")]) if eight else {}
+        plan = P.AdamTensors([p], [g], [m], [v], **scales)
+        for step in (1, 2):
+            P.attr_adamw_step(plan, step, 1e-3, eps=eps, eps_root=root)
+        assert (p == 1).all()

@@ -283,3 +283,16 @@ def test_oracle_pairs_of_weight_zero():
     z[0, 2], z[3] = -np.inf, np.nan
     loss, _, _, grad = O.preference_loss(z, [2, 1, 3, 4], 4, 1, pair_weight=[0.0, 0.0])
     assert (loss == 0).all() and all((g == 0).all() for g in grad.values())
+
+
+def test_adamw_refuses_what_fp32_does_not_divide_by():
+    """An eps that the reciprocal of fp32 does not take would turn weights that no gradient touched into NaN."""
+    L, none = P.lib(), (P._CAdamTensor * 1)(P._CAdamTensor(n=0))
+
+    def call(eps, root):
+        return L.attr_adamw_step(none, 1, 0, 0, 0, 1, 1e-3, 0.9, 0.95, eps, root, None, None)
+    least = 2.0 ** -126
+    for eps, root in ((1e-40, 0.0), (least * 0.999, 1e-6), (5e-324, 0.0), (0.0, 1e-46), (1e-8, 5e-324)):
+        assert call(eps, root) == INVALID and b"at least 2^-126" in L.attr_last_error(), (eps, root)
+    for eps, root in ((0.0, 0.0), (least, 0.0), (1e-30, 0.0), (0.0, 2.0 ** -149), (0.0, 1e-40)):
+        assert call(eps, root) == 0, (eps, root)
