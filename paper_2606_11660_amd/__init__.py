@@ -688,6 +688,20 @@ def attr_preference_loss(rows: TokenRows, loss: torch.Tensor, log_ratio: Optiona
 # ----------------------------------------------------------------------------
 # (5) AdamW
 # ----------------------------------------------------------------------------
+def _refuse_overlaps(spans: List[Tuple[int, int, str, int]]) -> None:
+    """spans: (from, to, buffer's name, tensor).  Gradients ("g") are only read and may overlap
+    each other; every other buffer stands alone."""
+    read = written = (0, 0, "", 0)  # of either kind, the span that reaches furthest so far
+    for s in sorted(spans):
+        other = read if s[2] != "g" and s[0] < read[1] else written
+        if s[0] < other[1]:
+            raise ValueError(f"tensor {other[3]}'s {other[2]} and tensor {s[3]}'s {s[2]} overlap")
+        if s[2] != "g":
+            written = s
+        elif s[1] > read[1]:
+            read = s
+
+
 class AdamTensors:
     """A model's tensors for ``attr_adamw_step``, checked once.
 
@@ -741,10 +755,7 @@ class AdamTensors:
         none = [None] * n
         self.array = (_CAdamTensor * n)(*zip(*(address.get(k, none) for k in ("p", "g", "m", "v", "master", "m_scale",
                                                                               "v_scale")), sizes, scale, decay))
-        spans.sort()
-        for a, b in zip(spans, spans[1:]):
-            if b[0] < a[1] and not (a[2] == b[2] == "g"):
-                raise ValueError(f"tensor {a[3]}'s {a[2]} and tensor {b[3]}'s {b[2]} overlap")
+        _refuse_overlaps(spans)
 
 
 def attr_adamw_step(tensors: AdamTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,

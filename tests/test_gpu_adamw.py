@@ -290,3 +290,13 @@ def test_least_eps_leaves_untouched_weights(eps, root):
         for step in (1, 2):
             P.attr_adamw_step(plan, step, 1e-3, eps=eps, eps_root=root)
         assert (p == 1).all()
+
+
+def test_overlaps_behind_other_gradients():
+    """Weights inside a long gradient that a shorter one starts in."""
+    buf = torch.zeros(1000, device="cuda")
+    m, v = ([torch.zeros(n, device="cuda") for n in (1000, 90)] for _ in range(2))
+    p = torch.zeros(1000, device="cuda")
+    with pytest.raises(ValueError, match="tensor 0's g and tensor 1's p overlap"):
+        P.AdamTensors([p, buf[500:590]], [buf, buf[10:100]], m, v)
+    P.AdamTensors([p, torch.zeros(90, device="cuda")], [buf, buf[10:100]], m, v)

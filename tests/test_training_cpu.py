@@ -296,3 +296,19 @@ def test_adamw_refuses_what_fp32_does_not_divide_by():
         assert call(eps, root) == INVALID and b"at least 2^-126" in L.attr_last_error(), (eps, root)
     for eps, root in ((0.0, 0.0), (least, 0.0), (1e-30, 0.0), (0.0, 2.0 ** -149), (0.0, 1e-40)):
         assert call(eps, root) == 0, (eps, root)
+
+
+def test_overlaps_of_an_adamw_plan():
+    """A buffer that the step writes overlaps nothing, also where gradients that overlap each other lie between."""
+    long, short = (0, 1000, "g", 0), (10, 100, "g", 1)
+    for spans in ([long, short, (2000, 2100, "p", 0), (2100, 2200, "m", 0)], [(0, 10, "p", 0), (10, 20, "p", 1)],
+                  [(5, 9, "g", 0), (5, 9, "g", 1), (9, 12, "v", 0)], []):
+        P._refuse_overlaps(spans)
+    for spans, text in (([long, short, (500, 600, "p", 1)], "tensor 0's g and tensor 1's p overlap"),
+                        ([(500, 600, "p", 1), short, long], "tensor 0's g and tensor 1's p"),
+                        ([(0, 50, "p", 0), (49, 60, "g", 3)], "tensor 0's p and tensor 3's g"),
+                        ([(0, 50, "p", 0), (10, 20, "p", 1)], "tensor 0's p and tensor 1's p"),
+                        ([(0, 50, "m", 0), (0, 50, "v", 0)], "tensor 0's m and tensor 0's v"),
+                        ([long, (990, 1200, "g", 1), (1199, 1300, "master", 0)], "tensor 1's g and tensor 0's master")):
+        with pytest.raises(ValueError, match=text):
+            P._refuse_overlaps(spans)
