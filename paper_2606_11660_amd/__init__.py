@@ -144,6 +144,19 @@ def lib() -> ctypes.CDLL:
 
 _native_modules = None
 _native_call = None
+_native_written = None
+
+
+def _written(tensors: Sequence[torch.Tensor]) -> None:
+    """Counts a change in place of tensors that a call wrote through their pointers, so that a
+    backward pass that saved their earlier values raises."""
+    global _native_written
+    if _native_written is None:
+        try:
+            from ._marshal import written as _native_written
+        except ImportError:  # the calls that need it warn
+            _native_written = torch.autograd.graph.increment_version
+    _native_written(tensors)
 
 
 def _native_token_call():
@@ -641,6 +654,8 @@ def _token_call(op: int, rows: TokenRows, per_row: tuple, per_example: tuple, pe
         args = (_ptr(advantage), int(op == _POLICY_PER_TOKEN), _ptr(per_row[1]), _ptr(per_row[2]), *scalars,
                 _ptr(per_example[0]), _ptr(per_row[0]), _ptr(dlogits), ldd)
     _check(getattr(L, _TOKEN_ENTRY[op])(c, *args, wsp, wsn, raw))
+    # what it wrote stands first in each tuple
+    _written([t for t in (dlogits, *per_row[:1], *per_example[:1], *per_pair[:1]) if t is not None])
 
 
 def attr_token_logp(rows: TokenRows, logp: torch.Tensor, ws: Optional[Workspace] = None,
@@ -659,8 +674,8 @@ def attr_policy_loss(rows: TokenRows, advantage: torch.Tensor, loss: torch.Tenso
 
     advantage: fp32 [n_examples], or [n_rows] with per_token; logp_old, logp_ref:
     fp32 [n_rows] (logp_old None: on policy, ratio 1).  dlogits (the logits' shape
-    and type, may be the logits themselves) takes the gradient of loss.sum(); rows'
-    weights carry the mask and the normalisation."""
+    and type, may be the logits themselves: a change in place to autograd) takes the
+    gradient of loss.sum(); rows' weights carry the mask and the normalisation."""
     if per_token:
         _token_call(_POLICY_PER_TOKEN, rows, (logp, logp_old, logp_ref, advantage), (loss,), (),
                     (clip_low, clip_high, beta), dlogits, ws, stream)
@@ -739,6 +754,7 @@ class AdamTensors:
         self.p_dtype, self.g_dtype = _dtype(p[0]), _dtype(g[0])
         self.state_dtype = ATTR_E4M3 if eight else ATTR_F32
         self.tensors = {k: list(x[0]) for k, x in kinds.items()}
+        self.weights = self.tensors["p"] + self.tensors.get("master", [])  # what autograd may have saved
         self.device = device = p[0].device
         if device.type != "cuda":
             raise ValueError("every tensor must live on the same GPU device")
@@ -762,7 +778,8 @@ def attr_adamw_step(tensors: AdamTensors, step: int, lr: float, beta1: float = 0
                     eps: float = 1e-8, eps_root: float = 0.0, grad_scale: Optional[torch.Tensor] = None,
                     stream=None) -> None:
     """AdamW step number `step` (from 1) over every tensor: updates p, m, v (and
-    master, scales) in place.  grad_scale: fp32 device scalar that multiplies the gradients."""
+    master, scales) in place, which autograd counts as a change of p and master.
+    grad_scale: fp32 device scalar that multiplies the gradients."""
     if grad_scale is not None:
         _vector(grad_scale, 1, torch.float32, "grad_scale")
         if grad_scale.device != tensors.device:
@@ -770,6 +787,7 @@ def attr_adamw_step(tensors: AdamTensors, step: int, lr: float, beta1: float = 0
     _check(lib().attr_adamw_step(tensors.array, len(tensors.array), tensors.p_dtype, tensors.g_dtype,
                                  tensors.state_dtype, step, lr, beta1, beta2, eps, eps_root, _ptr(grad_scale),
                                  _raw_stream(stream)))
+    _written(tensors.weights)
 
 
 # ----------------------------------------------------------------------------

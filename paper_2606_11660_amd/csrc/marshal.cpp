@@ -9,7 +9,10 @@
 // another kind (a subclass, a wrapper without storage, a CPU tensor): the
 // binding's own Python checks then run, and raise or accept.  token_call() makes the
 // checks of a token loss on its rows and vectors, and the library's call too (the
-// checks in Python take 7 us, where a small call's kernel takes 4).
+// checks in Python take 7 us, where a small call's kernel takes 4).  written() tells autograd
+// of tensors that a call wrote through their pointers (168 weights: under 2 us, 8 us in
+// Python): a backward pass that saved their earlier values then raises, as after any change
+// in place.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -215,6 +218,23 @@ float* floats(PyObject* tuple, Py_ssize_t j) {
   return o == Py_None ? nullptr : static_cast<float*>(THPVariable_Unpack(o).mutable_data_ptr());
 }
 
+void bump(PyObject* o) {
+  if (!o || !THPVariable_Check(o)) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();  // inference tensors count no versions
+}
+
+// written(list or tuple of tensors) -> True, or None where it is neither
+PyObject* py_written(PyObject*, PyObject* seq) {
+  if (!PyList_CheckExact(seq) && !PyTuple_CheckExact(seq)) Py_RETURN_NONE;
+  try {
+    for (Py_ssize_t j = 0; j < PySequence_Fast_GET_SIZE(seq); ++j) bump(PySequence_Fast_GET_ITEM(seq, j));
+  } catch (...) {
+    Py_RETURN_NONE;
+  }
+  Py_RETURN_TRUE;
+}
+
 // The library's entry points, by the numbers that token_call() takes.
 typedef attr_status (*LogpFn)(const attr_token_rows*, float*, void*, size_t, void*);
 typedef attr_status (*PolicyFn)(const attr_token_rows*, const float*, int32_t, const float*, const float*, float, float,
@@ -280,6 +300,12 @@ PyObject* py_token_call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       st = reinterpret_cast<PolicyFn>(fn)(&c, a, op == kPolicyPerToken, r1, r2, (float)x[0], (float)x[1], (float)x[2], e0,
                                           r0, d, ldd, ws, ws_bytes, stream);
     Py_END_ALLOW_THREADS;
+    if (st == ATTR_OK) {
+      bump(args[7]);
+      bump(PyTuple_GET_ITEM(v[0], 0));
+      if (op != kLogp) bump(PyTuple_GET_ITEM(v[1], 0));
+      if (op == kPreference) bump(PyTuple_GET_ITEM(v[2], 0));
+    }
   } catch (...) {
     Py_RETURN_NONE;
   }
@@ -290,6 +316,7 @@ PyMethodDef methods[] = {{"modules", reinterpret_cast<PyCFunction>(reinterpret_c
                           METH_FASTCALL, "module descriptors of a projection call, or None"},
                          {"token_call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_token_call)),
                           METH_FASTCALL, "status of a token loss's call, or None"},
+                         {"written", py_written, METH_O, "counts a change in place of every tensor"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -300,3 +300,21 @@ def test_overlaps_behind_other_gradients():
     with pytest.raises(ValueError, match="tensor 0's g and tensor 1's p overlap"):
         P.AdamTensors([p, buf[500:590]], [buf, buf[10:100]], m, v)
     P.AdamTensors([p, torch.zeros(90, device="cuda")], [buf, buf[10:100]], m, v)
+
+
+def test_autograd_sees_the_step(monkeypatch):
+    """A backward pass that saved the weights raises after a step on them."""
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(P, "_native_written", torch.autograd.graph.increment_version)
+        w = torch.nn.Parameter(torch.randn(64, 32, device="cuda"))
+        x = torch.randn(8, 64, device="cuda", requires_grad=True)
+        y = x @ w
+        g, m, v = (torch.zeros(64, 32, device="cuda") for _ in range(3))
+        P.attr_adamw_step(P.AdamTensors([w], [g], [m], [v]), 1, 1e-3)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+        master = torch.randn(64, 32, device="cuda")
+        p16, before = master.bfloat16(), master._version
+        P.attr_adamw_step(P.AdamTensors([p16], [g], [m], [v], master=[master]), 1, 1e-3)
+        assert master._version > before and p16._version > 0

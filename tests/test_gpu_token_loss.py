@@ -804,3 +804,33 @@ def test_pairs_of_weight_zero(V, T):
         alone = torch.full((3,), 7.0, device="cuda")
         P.attr_preference_loss(b.tokens(), alone, pair_weight=torch.from_numpy(pw).cuda(), label_smoothing=smoothing)
         assert (alone[1:] == 0).all()
+
+
+def test_autograd_sees_what_the_losses_write(monkeypatch):
+    """A backward pass through an operation that saved the logits raises once gradients stand in their place."""
+    b = Batch(41, torch.float32, 300, 4, 5)
+    tok, ones = b.tokens(), torch.ones(4, device="cuda")
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(P, "_native_call", lambda *args: None)
+        for loss_of in (lambda r, into: P.attr_policy_loss(r, ones, torch.empty(4, device="cuda"), dlogits=into),
+                        lambda r, into: P.attr_preference_loss(r, torch.empty(2, device="cuda"), dlogits=into)):
+            x = b.logits.clone().requires_grad_()
+            y = torch.tanh(x)  # saves its result
+            logits = y.detach()
+            rows = P.TokenRows(logits, tok.target, 4, 5)
+            apart = torch.empty_like(logits)
+            loss_of(rows, apart)
+            torch.autograd.grad(y, x, apart, retain_graph=True)     # the logits are whole
+            loss_of(rows, logits)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                torch.autograd.grad(y, x, apart)
+        outs = [torch.empty(k, device="cuda") for k in (b.rows, 4, 2, 4)]
+        before = [t._version for t in outs]
+        P.attr_token_logp(tok, outs[0])
+        P.attr_policy_loss(tok, ones, outs[1], logp=outs[0])
+        P.attr_preference_loss(tok, outs[2], log_ratio=outs[3])
+        assert all(t._version > v for t, v in zip(outs, before))
+    with torch.inference_mode():  # counts no versions
+        logp = torch.empty(b.rows, device="cuda")
+        P.attr_token_logp(tok, logp)

@@ -312,3 +312,19 @@ def test_overlaps_of_an_adamw_plan():
                         ([long, (990, 1200, "g", 1), (1199, 1300, "master", 0)], "tensor 1's g and tensor 0's master")):
         with pytest.raises(ValueError, match=text):
             P._refuse_overlaps(spans)
+
+
+def test_written_counts_versions():
+    """Of every tensor, with and without the native part; tensors of inference mode count none."""
+    from paper_2606_11660_amd import _marshal
+    x, w = torch.zeros(3), torch.nn.Parameter(torch.zeros(2))
+    with torch.inference_mode():
+        y = torch.zeros(3)
+    for seq in ([x, w, y], (x, y, w)):
+        before = x._version, w._version
+        assert _marshal.written(seq) is True
+        assert (x._version, w._version) == (before[0] + 1, before[1] + 1)
+    assert _marshal.written(x) is None and _marshal.written([3, None]) is True
+    before = x._version
+    P._written([x, y])
+    assert x._version == before + 1
