@@ -31,7 +31,7 @@ namespace attr {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
+constexpr double kLn2 = 0.69314718055994530942;
 constexpr float kMostMc = 1048576.f;  // 2^20: the residual of the fused form stays below 2^-4
 
 // What a workgroup does with one token's slot.
@@ -257,9 +257,9 @@ __device__ inline LogParts log_parts(float zy, float c, const RowSum& r) {
   const double x = r.apart ? ((double)zy - (double)r.offset) * (double)c : (double)zy * (double)c - (double)r.offset;
   return {x - (double)__builtin_amdgcn_frexp_expf(r.sum), log2f(__builtin_amdgcn_frexp_mantf(r.sum))};
 }
-__device__ inline float row_logp(float zy, float c, const RowSum& r) {
+__device__ inline double row_logp(float zy, float c, const RowSum& r) {
   const LogParts l = log_parts(zy, c, r);
-  return ((float)l.whole - l.rest) * kLn2;
+  return (l.whole - (double)l.rest) * kLn2;
 }
 
 // c m as the fused form's offset: the rounded product itself, and never the exact one within
@@ -443,8 +443,7 @@ constexpr int group_of(int nt) { return nt == 64 ? 256 : nt; }
 // ratios are small differences of sums: here the difference is in fp64.
 __device__ inline double token_part(const TokenArgs& a, const Slot& sl, float zy, float c, const RowSum& r,
                                     const float* logp_ref) {
-  const LogParts l = log_parts(zy, c, r);
-  const double logp = (l.whole - (double)l.rest) * 0.6931471805599453;
+  const double logp = row_logp(zy, c, r);
   if (thread<64>() == 0 && a.logp) a.logp[sl.row] = (float)logp;
   return (double)sl.weight * (logp - (logp_ref ? (double)logp_ref[sl.row] : 0.0));
 }
@@ -454,7 +453,7 @@ template <bool PREF>
 __device__ inline void write_logp(const TokenArgs& a, uint32_t slot, const Slot& sl, float zy, float c,
                                   const RowSum& r, const float* logp_ref) {
   if (!PREF) {
-    a.logp[sl.row] = row_logp(zy, c, r);
+    a.logp[sl.row] = (float)row_logp(zy, c, r);
     return;
   }
   a.part[slot] = token_part(a, sl, zy, c, r, logp_ref);
@@ -583,13 +582,13 @@ struct PolicySlot {
     const RowSum r = row.sum(zy, c, sh, ok);
     if (!ok) {  // a path of its own, which needs no registers
       const RowSum r = row_sum_apart<T, NT>(row.z, a.V, c, sh);
-      const float logp = row_logp(zy, c, r);
+      const float logp = (float)row_logp(zy, c, r);
       const TokenLoss l = policy_token(p, in, logp);
       if (thread<NT>() == 0 && a.logp) a.logp[sl.row] = logp;
       if (a.dlogits) row_grad_apart<T, NT>(row.z, out, a.V, sl.target, c, r, l.c * a.scale, -l.c * a.scale / r.sum);
       return l.loss;
     }
-    const float logp = row_logp(zy, c, r);
+    const float logp = (float)row_logp(zy, c, r);
     const TokenLoss l = policy_token(p, in, logp);
     if (thread<NT>() == 0 && a.logp) a.logp[sl.row] = logp;
     if (a.dlogits) row.grad(out, a.V, sl.target, c, r, l.c * a.scale);
@@ -662,7 +661,7 @@ __global__ __launch_bounds__(NT) void policy_stream_kernel(TokenArgs a, PolicyAr
   const T* z = (const T*)a.logits + sl.row * a.ldl;
   if (first) sh.zy = (float)z[sl.target];  // read before anything of the row is written
   const RowSum r = row_sum_stream<T, NT, 4, true>(z, a.V, c, sh);
-  const float logp = row_logp(sh.zy, c, r);
+  const float logp = (float)row_logp(sh.zy, c, r);
   const TokenLoss l = policy_token(p, in, logp);
   if (first) p.token_loss[slot] = l.loss;
   if (first && a.logp) a.logp[sl.row] = logp;
@@ -757,7 +756,7 @@ __global__ __launch_bounds__(NT) void split_policy_kernel(TokenArgs a, PolicyArg
   const PolicyToken in = policy_inputs(p, a, slot, sl);
   const float c = a.scale * kLog2e;
   const RowSum r = join_parts(a.parts + (size_t)slot * gridDim.y, gridDim.y, c);
-  const float logp = row_logp(a.zy[slot], c, r);
+  const float logp = (float)row_logp(a.zy[slot], c, r);
   const TokenLoss l = policy_token(p, in, logp);
   if (first) {
     p.token_loss[slot] = l.loss;

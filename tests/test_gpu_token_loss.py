@@ -834,3 +834,15 @@ def test_autograd_sees_what_the_losses_write(monkeypatch):
     with torch.inference_mode():  # counts no versions
         logp = torch.empty(b.rows, device="cuda")
         P.attr_token_logp(tok, logp)
+
+
+@pytest.mark.parametrize("V,rows", [(1000, 90), (5003, 40), (9001, 300), (50257, 24), (70001, 300), (300007, 6)])
+def test_calls_agree_on_log_probabilities(V, rows):
+    """Log-probabilities are rounded once: the two calls that sum a row alike give the same bits."""
+    for dtype in NAMES:
+        say(f"case: agreeing calls {NAMES[dtype]} V={V} rows={rows}")
+        b = Batch(V + 7, dtype, V, 2, rows // 2, weighted=True, scale=1.25)
+        logp, pref = (torch.full((b.rows,), 7.0, device="cuda") for _ in range(2))
+        P.attr_token_logp(b.tokens(), logp)
+        P.attr_preference_loss(b.tokens(), torch.empty(1, device="cuda"), logp=pref)
+        assert torch.equal(logp, pref), (logp - pref).abs().max()
