@@ -846,3 +846,57 @@ def test_calls_agree_on_log_probabilities(V, rows):
         P.attr_token_logp(b.tokens(), logp)
         P.attr_preference_loss(b.tokens(), torch.empty(1, device="cuda"), logp=pref)
         assert torch.equal(logp, pref), (logp - pref).abs().max()
+
+
+@pytest.mark.parametrize("dtype", list(NAMES), ids=NAMES.get)
+@pytest.mark.parametrize("n,T,row_bytes,packed", [(4, 530, 10012, False), (2, 1100, 6002, True), (4, 520, 36004, True),
+                                                  (2, 270, 80044, True), (4, 131, 100516, False)])
+def test_preference_of_many_rows(n, T, row_bytes, packed, dtype):
+    """More rows than add up their pairs themselves: the pairs in a launch between the sums and the
+    gradient, for rows of 8 to 64 KB and past them; in place too."""
+    V = row_bytes // torch.empty(0, dtype=dtype).element_size()
+    say(f"case: preference of many rows n={n} T={T} V={V} {NAMES[dtype]}")
+    b = Batch(n * T + V, dtype, V, n, T, ragged=True, weighted=True, packed=packed)
+    _, ref = b.old_ref()
+    up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    loss, ratio, logp = (torch.full((k,), 7.0, device="cuda") for k in (n // 2, n, b.rows))
+    dl, _ = b.dbuf()
+    P.attr_preference_loss(b.tokens(), loss, log_ratio=ratio, logp=logp, dlogits=dl, logp_ref=up(ref), beta=0.02)
+    wl, wr, wlp, wg = O.preference_loss(b.numpy(), b.target, n, T, logp_ref=ref, beta=0.02, **b.where())
+    check_logp(b, host(logp), 7.0)
+    r_tol, c_abs = np.zeros(n), np.zeros(b.rows)
+    for i, _, row, counts in b.slots():
+        if counts:
+            r_tol[i] += b.weight[row] * logp_tol(wlp[row], V)
+    h_tol = 0.02 * (r_tol[:n // 2] + r_tol[n // 2:])
+    assert (np.abs(host(ratio) - wr) <= r_tol + 2 * U * np.abs(wr)).all()
+    assert (np.abs(host(loss) - wl) <= h_tol + 2 * U * np.abs(wl)).all()
+    for i, _, row, counts in b.slots():
+        if counts:
+            c_abs[row] = b.weight[row] * 0.02 * h_tol[i % (n // 2)] / 4
+    check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 8 * U, c_abs)
+    again = torch.full((n // 2,), 7.0, device="cuda")
+    P.attr_preference_loss(b.tokens(), again, dlogits=b.logits, logp_ref=up(ref), beta=0.02)  # over the logits
+    assert torch.equal(again, loss)
+    for _, _, row, _ in b.slots():
+        assert torch.equal(b.logits[row], dl[row]), row
+
+
+@pytest.mark.parametrize("n,T,V", [(5, 17, 700), (7, 23, 1000), (3, 31, 64), (2, 32, 1)])
+def test_short_examples_of_odd_lengths(n, T, V):
+    """Two tokens a wave, the last wave's second one past the example's end."""
+    for dtype in NAMES:
+        say(f"case: odd lengths n={n} T={T} V={V} {NAMES[dtype]}")
+        b = Batch(n * T + V, dtype, V, n, T, ragged=True, weighted=True, packed=T % 2 == 1, extra_ld=3)
+        old, ref = b.old_ref((0.8, 1.28))
+        adv = b.r.standard_normal(n).astype(np.float32)
+        up = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+        loss, logp, (dl, _) = torch.full((n,), 7.0, device="cuda"), torch.full((b.rows,), 7.0, device="cuda"), b.dbuf()
+        P.attr_policy_loss(b.tokens(), up(adv), loss, logp=logp, dlogits=dl, logp_old=up(old), logp_ref=up(ref), clip_high=0.28,
+                           beta=0.04)
+        wl, wlp, wg = O.policy_loss(b.numpy(), b.target, n, T, adv, logp_old=old, logp_ref=ref, clip_high=0.28, beta=0.04,
+                                    **b.where())
+        check_logp(b, host(logp), 7.0)
+        c_abs, tol = policy_tols(b, old, adv, ref, 0.04, False)
+        assert (np.abs(host(loss) - wl) <= tol + U * np.abs(wl)).all()
+        check_dlogits(b, dl.double().cpu().numpy(), wg, wlp, 0.0, c_abs)
