@@ -396,8 +396,8 @@ attr_status attr_preference_loss(const attr_token_rows* rows, const float* logp_
  * element alignment).  With 8-bit states m and v hold E4M3 values in blocks of
  * 256 elements, the last one as long as what is left: m_e = m_scale[b] m[e],
  * and v holds the root of the second moment, v_e = (v_scale[b] v[e])^2; a
- * block's scale is its largest magnitude over 448.  Zeroed states and scales
- * are those of step 0. */
+ * block's scale is its largest magnitude, or 2^-100 where that is less, over
+ * 448.  Zeroed states and scales are those of step 0. */
 typedef struct {
   void* p;          /* weights, p_dtype; with a master: its rounding, written and never read */
   const void* g;    /* gradients, g_dtype */
@@ -417,15 +417,22 @@ typedef struct {
  *     x = x - lr' wd x - lr' (m / (1 - beta1^step))
  *                        / (sqrt(v / (1 - beta2^step) + eps_root) + eps)
  * with lr' = lr lr_scale, x the weight (its master where there is one).  All
- * in fp32 without contraction (the quotient and its root within an ulp each),
- * so the result does not depend on how the work is split.  8-bit states are
+ * in fp32 without contraction, so the result does not depend on how the work is
+ * split; the step is (m lr'/(1 - beta1^step)) times the reciprocal of the root,
+ * both products rounded, the root and the reciprocal within an ulp each.
+ * step, lr and the other numbers enter the launch as they are: a graph that
+ * captured this call repeats that one step, with its rate and its corrections.
+ * 8-bit states are
  * encoded after the update: m to the nearest E4M3 value (ties to even), the
  * root of v likewise but never to zero while v is positive (a second moment
  * rounded to zero would make the next step huge).
  * E4M3 keeps a root within 6.25%: between steps a stored second moment follows
  * its block's scale exactly, and its place in the block only by changes of
- * that size.  A NaN or infinity in a block's new states makes the block's
- * scale NaN.
+ * that size.  A root that is too small for its gradients thus grows only while
+ * (1 - beta2) (g'^2 / v - 1) is more than about 0.13: it may stay at half of a
+ * steady |g'| with beta2 = 0.95, at a twelfth with 0.999 (steps up to 12 times as
+ * long as those of 32-bit states).  A NaN or infinity in a block's new states
+ * makes the block's scale NaN.
  *   tensors    (host) [n_tensors], 0 <= n_tensors; their buffers must not
  *              overlap
  *   p_dtype    ATTR_F32, ATTR_BF16 or ATTR_F16 (the last two with or without
