@@ -789,8 +789,6 @@ __global__ __launch_bounds__(256) void example_sum_kernel(const float* __restric
   }
 }
 
-__device__ inline double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
-
 // Sum over NT threads, the result in all of them.
 template <int NT>
 __device__ inline double threads_sum(double v, double* sh) {
@@ -812,8 +810,11 @@ __device__ inline float pair_loss(const PrefArgs& p, uint32_t pair, const double
   const double h = (double)p.beta * (ratio[0] - ratio[1]) - (double)p.margin;
   const float pw = p.pair_weight ? p.pair_weight[pair] : 1.f, e = p.smoothing;
   if (outputs) {
-    // a share of nothing is not taken of an infinite ratio's loss
-    const double won = e < 1.f ? (1.0 - (double)e) * softplus(-h) : 0.0, lost = e > 0.f ? (double)e * softplus(h) : 0.0;
+    // softplus(x) = max(x, 0) + log1p(exp(-|x|)); a share of nothing is not taken of an
+    // infinite ratio's loss
+    const double tail = log1p(exp(-fabs(h)));
+    const double won = e < 1.f ? (1.0 - (double)e) * (fmax(-h, 0.0) + tail) : 0.0;
+    const double lost = e > 0.f ? (double)e * (fmax(h, 0.0) + tail) : 0.0;
     p.loss[pair] = pw != 0.f ? (float)((double)pw * (won + lost)) : 0.f;
     if (p.log_ratio) {
       p.log_ratio[pair] = (float)ratio[0];
