@@ -341,8 +341,9 @@ attr_status attr_token_logp(const attr_token_rows* rows, float* logp, void* ws, 
  * The weights carry the mask and the normalisation (1 / tokens for a mean over
  * each example, one constant for a sum, a loss scale).  Each row of logits is
  * read once and each row of dlogits written once where a row fits a
- * workgroup's registers (256 KB; longer rows, and few long rows, which are
- * spread over many CUs, are read twice); loss sums are formed in fp64 in a
+ * workgroup's registers (256 KB; longer rows, few long rows, which are spread
+ * over many CUs, and rows whose largest logit is some 41 / s above the first ones
+ * are read again); loss sums are formed in fp64 in a
  * fixed order.
  *   advantage  device fp32 [n_examples], or [n_rows] with per_token != 0
  *   logp_old   device fp32 [n_rows], or NULL: the logits' own (ratio 1)

@@ -728,7 +728,8 @@ class AdamTensors:
     and lr_scale: one number, or one for each tensor.
 
     The object keeps the tensors and their addresses: give their storage new
-    contents, not a new place (a step with gradients elsewhere needs a new object).
+    contents, not a new place (a step with gradients elsewhere needs a new object,
+    2 us of host time a tensor: keep the gradients' storage between steps).
     """
 
     def __init__(self, p: Sequence[torch.Tensor], g: Sequence[torch.Tensor], m: Sequence[torch.Tensor],
@@ -779,7 +780,8 @@ def attr_adamw_step(tensors: AdamTensors, step: int, lr: float, beta1: float = 0
                     stream=None) -> None:
     """AdamW step number `step` (from 1) over every tensor: updates p, m, v (and
     master, scales) in place, which autograd counts as a change of p and master.
-    grad_scale: fp32 device scalar that multiplies the gradients."""
+    grad_scale: fp32 device scalar that multiplies the gradients.  A graph that
+    captured the call repeats this step, with its number and its lr."""
     if grad_scale is not None:
         _vector(grad_scale, 1, torch.float32, "grad_scale")
         if grad_scale.device != tensors.device:

@@ -1,7 +1,8 @@
 // One AdamW step over many tensors (attr_adamw_step).
 //
-// Every element is read once and written once: HBM-bound (26 to 28 bytes an
-// element with 32-bit states, 12 to 16 with 8-bit ones).  The descriptors travel in
+// Every element is read once and written once: HBM-bound (with 32-bit
+// states 26 or 28 bytes an element of fp32 weights, 22 or 24 of 16-bit ones, 28 or 30 with
+// masters; with 8-bit states 12 fewer and 1/16 for the scales).  The descriptors travel in
 // kernel arguments; a workgroup finds its tensor by its first chunk and takes one
 // chunk of it, a wave U runs of 256 elements, four elements a lane, all loads in
 // flight before the first is used.  A run is a block of the 8-bit states: its
@@ -15,8 +16,8 @@
 //
 // Measured on one MI355X (large copies: 5.2 TB/s): 268M elements with bf16 weights,
 // fp32 masters and 32-bit states 1.26 to 1.29 ms (5.9 TB/s); 134M fp32 weights with 8-bit
-// states 310 us (6.1 TB/s, 67 vector instructions an element: 86% of what the rate
-// allows); 168 adapter tensors side by side, 2.9M elements, 13 us.
+// states 310 us (6.1 TB/s, 69 vector instructions an element: 82 to 93% of what the
+// rate allows, by the clock); 168 adapter tensors side by side, 2.9M elements, 15 us.
 #include "common.h"
 #include "kernels.h"
 

@@ -1040,8 +1040,8 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
     for (int32_t j = 0; j < n_tensors; ++j) total = std::min(total + tensors[j].n, (int64_t)1 << 40);
     AdamwLaunch L{(int)p_dtype, (int)g_dtype, eight, attr::adamw_runs_per_wave(total, eight), h, s};
     // The neighbour of a tensor in every buffer, with the same rates, is one tensor with
-    // it: a model in flat buffers takes one launch (168 adapters: two, and 19.4 us
-    // against 13.0).
+    // it: a model in flat buffers takes one launch (168 adapters: two, and 20.7 us
+    // against 15.6).
     const auto joins = [&](const attr_adamw_tensor& t, const attr_adamw_tensor& u) {
       const auto after = [&](const void* x, const void* y, size_t each) {
         return x ? y == static_cast<const char*>(x) + (size_t)t.n * each : !y;
