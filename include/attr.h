@@ -18,7 +18,10 @@
  *       respect to the logits (the gradients whose per-example products (1)
  *       projects);
  *   (5) the AdamW step over a model's tensors, whose second moments are the
- *       optimizer states that (1) divides gradients by.
+ *       optimizer states that (1) divides gradients by, and the Muon step over
+ *       the modules' matrices;
+ *   (6) embedding and layer norm of token rows, what the rows that (1) reads
+ *       come from, with their gradients (the norm's for each example, too).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -448,6 +451,138 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
                             attr_dtype g_dtype, attr_dtype state_dtype, int64_t step, double lr,
                             double beta1, double beta2, double eps, double eps_root,
                             const float* grad_scale, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* (5b) attr_muon_step: one Muon step over many matrices.                    */
+/* ------------------------------------------------------------------------ */
+
+/* One weight matrix of rows x cols contiguous elements, row-major, with its
+ * gradient and momentum laid out the same (host struct with device pointers; any
+ * element alignment).  A zeroed momentum is that of step 0. */
+typedef struct {
+  void* p;          /* weights, p_dtype; with a master: its rounding, written and never read */
+  const void* g;    /* gradients, g_dtype */
+  float* m;         /* momentum */
+  float* master;    /* fp32 weights that the step updates, or NULL: p itself */
+  int64_t rows, cols;  /* 0 <= rows, cols <= 2^20; see below for their product */
+  float lr_scale;   /* times lr for this matrix */
+  float weight_decay;
+} attr_muon_matrix;
+
+/* For every matrix, with g' = grad_scale g (a device scalar, or NULL: 1):
+ *     m = momentum m + (1 - momentum) g'
+ *     u = momentum m + (1 - momentum) g'   (nesterov; with the new m), else m
+ *     X = u / |u|_F, then `steps` times, with A = X X^T:
+ *     X = a X + (b A + c A A) X,   a = 3.4445, b = -4.7750, c = 2.0315
+ *     x = x - lr' wd x - lr' X,    lr' = lr lr_scale
+ * The polynomial takes singular values in (0, 1] towards 1 (after five steps those from
+ * 0.01 on lie in [0.68, 1.21]), so X approaches the orthogonal factor of u.
+ * Where a matrix is not square its longer side is multiplied last.  A matrix
+ * whose u is zero has X = 0; one with a NaN or an infinity in u becomes NaN.
+ * m is fp32 without contraction, the norm fp64; the iteration runs on the matrix
+ * cores with fp32 sums and its operands (X, A, b A + c A A) rounded
+ *   pairs = 0  to fp16, 11 bits: X is off by some 1e-3 of its norm, less than half
+ *              a step of a 16-bit weight's update;
+ *   pairs = 1  to pairs of fp16, 22 bits: three times the products, X off by some 1e-6.
+ * The numbers enter the launches as they are: a graph that captured this call
+ * repeats the step with its rate.
+ *   mats       (host) [n_mats], 0 <= n_mats; their buffers must not overlap (gradients
+ *              may overlap gradients).  With t the longer side and s' the shorter one
+ *              rounded up to a multiple of 64, t s' < 2^30
+ *   p_dtype, g_dtype  ATTR_F32, ATTR_BF16 or ATTR_F16
+ *   momentum   in [0, 1);  steps 1 to 16;  lr finite
+ *   ws         attr_muon_step_workspace_size(mats, n_mats, pairs) bytes, 256-byte
+ *              aligned: some 8 bytes (pairs: 16) for each element of the matrices that
+ *              are worked on together, which are taken in turn where they are many */
+size_t attr_muon_step_workspace_size(const attr_muon_matrix* mats, int32_t n_mats, int32_t pairs);
+attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dtype p_dtype,
+                           attr_dtype g_dtype, double lr, double momentum, int32_t nesterov,
+                           int32_t steps, int32_t pairs, const float* grad_scale, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* (6) Embedding and layer norm of token rows, and their gradients.          */
+/* ------------------------------------------------------------------------ */
+
+/* The rows of a batch: token t of example i is row (row_offset ? row_offset[i] :
+ * i * T) + t, as in attr_project.  Rows of tokens t < length[i] that lie in
+ * [0, n_rows) are INSIDE; nothing else is read.  Of the outputs the rows inside are
+ * written, and without row_offset the padding rows i * T + t, t < T, too (as
+ * zeros); no others.  The ranges of two examples must not overlap.
+ * Read only during the call (host struct with device pointers). */
+typedef struct {
+  int64_t n_rows;          /* rows of every token tensor of the call */
+  int64_t n_examples, T;   /* n_examples * T < 2^31; without row_offset n_rows >= n_examples * T */
+  const int64_t* row_offset;  /* device [n_examples] or NULL (then i * T) */
+  const int32_t* length;      /* device [n_examples] or NULL (then T); clamped to [0, T] */
+} attr_rows;
+
+/* out[row] = scale * table[token[row]] for the rows inside; a row whose token is
+ * outside [0, V) is zeros.  The product is fp32, rounded once.
+ *   token       device int64 [n_rows]
+ *   table       device [V, d], row stride ldt >= d, any type, stride and element
+ *               alignment; 1 <= V <= 2^28, 1 <= d <= 65536
+ *   out         device [n_rows, d], row stride ldo >= d; overlaps no input */
+attr_status attr_embed(const attr_rows* rows, const int64_t* token, const void* table,
+                       attr_dtype table_dtype, int64_t V, int64_t d, int64_t ldt, float scale,
+                       void* out, attr_dtype out_dtype, int64_t ldo, void* stream);
+
+/* The table's gradient:
+ *     dtable[v] = scale * sum of dout[row] over the rows inside whose token is v
+ * for every v in [0, V) (zeros where there is none), or with accumulate added to
+ * the rows of dtable whose tokens the batch holds, the others left alone.  The rows are
+ * sorted by token first, and a token's are added up in fp32 in the order of their
+ * slots (32 neighbours of that sorted order at a time, these sums in fp64): no
+ * atomic additions, the same bits for the same call.
+ *   dout        device [n_rows, d], row stride ldd >= d; n_rows below 2^32
+ *   dtable      device [V, d], row stride ldt >= d; overlaps no input
+ *   ws          attr_embed_backward_workspace_size(rows, V, d) bytes, 256-byte aligned */
+size_t attr_embed_backward_workspace_size(const attr_rows* rows, int64_t V, int64_t d);
+attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, const void* dout,
+                                attr_dtype dout_dtype, int64_t ldd, int64_t V, int64_t d,
+                                float scale, void* dtable, attr_dtype dtable_dtype, int64_t ldt,
+                                int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Layer norm of every row x inside:
+ *     mean = sum_j x_j / d,   rstd = 1 / sqrt(sum_j (x_j - mean)^2 / d + eps)
+ *     y_j = (x_j - mean) rstd w_j + b_j
+ * in fp32 (the sums over a row too), y rounded once.  A row whose squares pass
+ * fp32's range has rstd 0.
+ *   x, y        device [n_rows, d], any types, strides >= d and element alignment;
+ *               1 <= d <= 32768.  y may be x itself with the same type and stride; any
+ *               other overlap is ATTR_ERR_INVALID_ARG
+ *   weight, bias  device [d] of w_dtype, or NULL (1 and 0)
+ *   eps         finite, >= 0
+ *   mean, rstd  device fp32 [n_rows] or NULL: what the backward pass takes (padding
+ *               rows: 0) */
+attr_status attr_layer_norm(const attr_rows* rows, const void* x, attr_dtype x_dtype, int64_t d,
+                            int64_t ldx, const void* weight, const void* bias, attr_dtype w_dtype,
+                            float eps, void* y, attr_dtype y_dtype, int64_t ldy, float* mean,
+                            float* rstd, void* stream);
+
+/* Its gradient.  With u = (x - mean) rstd and e = dy w for every row inside:
+ *     dx_j = rstd (e_j - sum_k e_k / d - u_j sum_k e_k u_k / d)
+ *     dweight_j = sum of dy_j u_j,   dbias_j = sum of dy_j
+ * summed over all rows inside, or with per_example over those of each example: the
+ * gradients that attribution compresses and stores are per example.  accumulate adds
+ * to what dweight and dbias hold.  Sums over a workgroup's rows are fp32, those of
+ * workgroups fp64, in a fixed order.
+ *   dy          device [n_rows, d] of dy_dtype, stride lddy >= d
+ *   x, mean, rstd  what the forward pass took and gave
+ *   dx          device [n_rows, d] of x's type, stride lddx, or NULL; may be x or dy
+ *               itself with the same type and stride
+ *   dweight     device fp32 [d], or with per_example [n_examples, d] of row stride
+ *               ldw >= d (the columns of a wider row of gradients); or NULL
+ *   dbias       likewise with ldb
+ *   ws          attr_layer_norm_backward_workspace_size(rows, d, per_example) bytes */
+size_t attr_layer_norm_backward_workspace_size(const attr_rows* rows, int64_t d, int32_t per_example);
+attr_status attr_layer_norm_backward(const attr_rows* rows, const void* dy, attr_dtype dy_dtype,
+                                     int64_t lddy, const void* x, attr_dtype x_dtype, int64_t d,
+                                     int64_t ldx, const float* mean, const float* rstd,
+                                     const void* weight, attr_dtype w_dtype, void* dx, int64_t lddx,
+                                     float* dweight, int64_t ldw, float* dbias, int64_t ldb,
+                                     int32_t per_example, int32_t accumulate, void* ws,
+                                     size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Calibration (not part of the method): the rates this GPU sustains, used  */

@@ -133,3 +133,82 @@ def adamw(x, g, m, v, step, lr, beta1, beta2, eps, eps_root=0.0, weight_decay=0.
     new = x - lr * weight_decay * x - lr * (m / (1 - beta1 ** step)) / (
         np.sqrt(v / (1 - beta2 ** step) + eps_root) + eps)
     return new, m, v
+
+
+# ----------------------------------------------------------------------------
+# token rows: embedding and layer norm, and their gradients
+# ----------------------------------------------------------------------------
+def row_slots(n_examples, T, n_rows, row_offset=None, length=None):
+    """(example, row, inside) of every slot whose outputs are written."""
+    got = []
+    for i in range(n_examples):
+        n = T if length is None else min(max(int(length[i]), 0), T)
+        for t in range(T):
+            row = i * T + t if row_offset is None else int(row_offset[i]) + t
+            if 0 <= row < n_rows and (row_offset is None or t < n):
+                got.append((i, row, t < n))
+    return got
+
+
+def embed(table, token, scale, slots):
+    """{row: out[row]}"""
+    table = np.asarray(table, np.float64)
+    zero = np.zeros(table.shape[1])
+    return {row: scale * table[token[row]] if inside and 0 <= token[row] < len(table) else zero
+            for _, row, inside in slots}
+
+
+def embed_backward(dout, token, V, scale, slots):
+    """(gradient [V, d], what its magnitudes sum to, rows of each token)"""
+    dout = np.asarray(dout, np.float64)
+    grad, size, count = np.zeros((V, dout.shape[1])), np.zeros((V, dout.shape[1])), np.zeros(V, int)
+    for _, row, inside in slots:
+        v = int(token[row])
+        if inside and 0 <= v < V:
+            grad[v] += scale * dout[row]
+            size[v] += np.abs(scale * dout[row])
+            count[v] += 1
+    return grad, size, count
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """(y, mean, rstd) of one row."""
+    x = np.asarray(x, np.float64)
+    mean = x.mean()
+    rstd = 1 / np.sqrt(np.square(x - mean).mean() + eps)
+    y = (x - mean) * rstd
+    return y * (1 if weight is None else weight) + (0 if bias is None else bias), mean, rstd
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None):
+    """(dx, dweight's term, dbias's term) of one row."""
+    u = (np.asarray(x, np.float64) - mean) * rstd
+    e = dy * (1.0 if weight is None else weight)
+    return rstd * (e - e.mean() - u * (e * u).mean()), dy * u, np.asarray(dy, np.float64)
+
+
+# ----------------------------------------------------------------------------
+# Muon
+# ----------------------------------------------------------------------------
+NS = (3.4445, -4.7750, 2.0315)
+
+
+def newton_schulz(u, steps=5):
+    """u / |u| after the steps (zeros for zeros)."""
+    a, b, c = NS
+    x = np.asarray(u, np.float64)
+    norm = np.linalg.norm(x)
+    x = x / norm if norm else x
+    for _ in range(steps):
+        gram = x @ x.T if x.shape[0] <= x.shape[1] else x.T @ x
+        poly = b * gram + c * gram @ gram
+        x = a * x + (poly @ x if x.shape[0] <= x.shape[1] else x @ poly)
+    return x
+
+
+def muon(w, g, m, lr, momentum=0.95, nesterov=True, steps=5, weight_decay=0.0, grad_scale=1.0):
+    """(w, m, X) after the step."""
+    g = np.asarray(g, np.float64) * grad_scale
+    m = momentum * np.asarray(m, np.float64) + (1 - momentum) * g
+    x = newton_schulz(momentum * m + (1 - momentum) * g if nesterov else m, steps)
+    return w - lr * weight_decay * w - lr * x, m, x

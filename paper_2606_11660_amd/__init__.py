@@ -34,6 +34,9 @@ __all__ = [
     "ATTR_E4M3", "TokenRows", "attr_token_logp", "attr_policy_loss", "attr_preference_loss",
     "attr_token_logp_workspace_size", "attr_policy_loss_workspace_size",
     "attr_preference_loss_workspace_size", "AdamTensors", "attr_adamw_step",
+    "MuonTensors", "attr_muon_step", "attr_muon_step_workspace_size", "ExampleRows", "attr_embed", "attr_embed_backward",
+    "attr_embed_backward_workspace_size", "attr_layer_norm", "attr_layer_norm_backward",
+    "attr_layer_norm_backward_workspace_size",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -74,6 +77,17 @@ class _CAdamTensor(ctypes.Structure):
                 ("v", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64), ("lr_scale", ctypes.c_float),
                 ("weight_decay", ctypes.c_float)]
+
+
+class _CMuonMatrix(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("lr_scale", ctypes.c_float),
+                ("weight_decay", ctypes.c_float)]
+
+
+class _CRows(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_examples", ctypes.c_int64), ("T", ctypes.c_int64),
+                ("row_offset", ctypes.c_void_p), ("length", ctypes.c_void_p)]
 
 
 _lib = None
@@ -138,6 +152,24 @@ def lib() -> ctypes.CDLL:
     L.attr_adamw_step.restype = ctypes.c_int
     L.attr_adamw_step.argtypes = [ctypes.POINTER(_CAdamTensor), i32, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                   i64, f64, f64, f64, f64, f64, vp, vp]
+    mats, code, batch = ctypes.POINTER(_CMuonMatrix), ctypes.c_int, ctypes.POINTER(_CRows)
+    L.attr_muon_step_workspace_size.restype = sz
+    L.attr_muon_step_workspace_size.argtypes = [mats, i32, i32]
+    L.attr_muon_step.restype = code
+    L.attr_muon_step.argtypes = [mats, i32, code, code, f64, f64, i32, i32, i32, vp, vp, sz, vp]
+    L.attr_embed.restype = code
+    L.attr_embed.argtypes = [batch, vp, vp, code, i64, i64, i64, f32, vp, code, i64, vp]
+    L.attr_embed_backward_workspace_size.restype = sz
+    L.attr_embed_backward_workspace_size.argtypes = [batch, i64, i64]
+    L.attr_embed_backward.restype = code
+    L.attr_embed_backward.argtypes = [batch, vp, vp, code, i64, i64, i64, f32, vp, code, i64, i32, vp, sz, vp]
+    L.attr_layer_norm.restype = code
+    L.attr_layer_norm.argtypes = [batch, vp, code, i64, i64, vp, vp, code, f32, vp, code, i64, vp, vp, vp]
+    L.attr_layer_norm_backward_workspace_size.restype = sz
+    L.attr_layer_norm_backward_workspace_size.argtypes = [batch, i64, i32]
+    L.attr_layer_norm_backward.restype = code
+    L.attr_layer_norm_backward.argtypes = [batch, vp, code, i64, vp, code, i64, i64, vp, vp, vp, code, vp, i64, vp, i64,
+                                           vp, i64, i32, i32, vp, sz, vp]
     _lib = L
     return L
 
@@ -790,6 +822,263 @@ def attr_adamw_step(tensors: AdamTensors, step: int, lr: float, beta1: float = 0
                                  tensors.state_dtype, step, lr, beta1, beta2, eps, eps_root, _ptr(grad_scale),
                                  _raw_stream(stream)))
     _written(tensors.weights)
+
+
+# ----------------------------------------------------------------------------
+# (5b) Muon
+# ----------------------------------------------------------------------------
+class MuonTensors:
+    """A model's matrices for ``attr_muon_step``, checked once.
+
+    p, g, m: lists of contiguous 2-D tensors, one of each per weight matrix, of the
+    same shape; p and g fp32, bf16 or fp16, all of one type each; m (the momentum)
+    fp32.  master: fp32 weights that the step updates, p taking their rounded values.
+    weight_decay and lr_scale: one number, or one for each matrix (a common choice of
+    lr_scale is sqrt(max(1, rows / cols)); 0.2 sqrt(max(rows, cols)) makes steps as long
+    as AdamW's).
+
+    The object keeps the tensors and their addresses: give their storage new
+    contents, not a new place.
+    """
+
+    def __init__(self, p: Sequence[torch.Tensor], g: Sequence[torch.Tensor], m: Sequence[torch.Tensor],
+                 master: Optional[Sequence[torch.Tensor]] = None, weight_decay=0.0, lr_scale=1.0):
+        n = len(p)
+        if n == 0:
+            raise ValueError("need at least one matrix")
+        kinds = {"p": (p, p[0].dtype), "g": (g, g[0].dtype if len(g) else None), "m": (m, torch.float32),
+                 "master": (master, torch.float32)}
+        kinds = {k: x for k, x in kinds.items() if x[0] is not None}
+        decay, scale = ([float(x)] * n if isinstance(x, (int, float)) else [float(y) for y in x]
+                        for x in (weight_decay, lr_scale))
+        for name, ts in [(k, x[0]) for k, x in kinds.items()] + [("weight_decay", decay), ("lr_scale", scale)]:
+            if len(ts) != n:
+                raise ValueError(f"{name} has {len(ts)} entries, p has {n}")
+        self.p_dtype, self.g_dtype = _dtype(p[0]), _dtype(g[0])
+        self.tensors = {k: list(x[0]) for k, x in kinds.items()}
+        self.weights = self.tensors["p"] + self.tensors.get("master", [])  # what autograd may have saved
+        self.device = device = p[0].device
+        if device.type != "cuda":
+            raise ValueError("every tensor must live on the same GPU device")
+        address, spans = {}, []
+        for name, (ts, dtype) in kinds.items():
+            address[name] = [t.data_ptr() for t in ts]
+            for j, t in enumerate(ts):
+                if t.dim() != 2 or t.dtype != dtype or not t.is_contiguous() or t.shape != p[j].shape:
+                    raise ValueError(f"matrix {j}: {name} must be a contiguous {dtype} tensor of shape {list(p[j].shape)}")
+                if t.device != device:
+                    raise ValueError("every tensor must live on the same GPU device")
+                if t.numel():
+                    spans.append((address[name][j], address[name][j] + t.numel() * dtype.itemsize, name, j))
+        none = [None] * n
+        self.array = (_CMuonMatrix * n)(*zip(*(address.get(k, none) for k in ("p", "g", "m", "master")),
+                                             [t.shape[0] for t in p], [t.shape[1] for t in p], scale, decay))
+        _refuse_overlaps(spans)
+        self._need: Dict[int, int] = {}
+
+    def workspace_size(self, pairs: bool) -> int:
+        k = int(pairs)
+        if k not in self._need:
+            self._need[k] = int(lib().attr_muon_step_workspace_size(self.array, len(self.array), k))
+        return self._need[k]
+
+    def default_pairs(self) -> bool:
+        return self.p_dtype == ATTR_F32 or "master" in self.tensors
+
+
+def attr_muon_step_workspace_size(tensors: MuonTensors, pairs: Optional[bool] = None) -> int:
+    return tensors.workspace_size(tensors.default_pairs() if pairs is None else pairs)
+
+
+def attr_muon_step(tensors: MuonTensors, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
+                   pairs: Optional[bool] = None, grad_scale: Optional[torch.Tensor] = None,
+                   ws: Optional[Workspace] = None, stream=None) -> None:
+    """One Muon step over every matrix: updates p and m (and master) in place, which autograd
+    counts as a change of p and master.
+
+    pairs: whether the orthogonalisation holds its operands as pairs of fp16 (three
+    times the products, an update good to some 1e-6 of its norm) or as fp16 (1e-3).  None: pairs
+    where the step updates 32-bit weights (p or masters), fp16 where it updates 16-bit ones,
+    whose own rounding is coarser.  grad_scale: fp32 device scalar that multiplies the
+    gradients.  A graph that captured the call repeats this step with its lr."""
+    if grad_scale is not None:
+        _vector(grad_scale, 1, torch.float32, "grad_scale")
+        if grad_scale.device != tensors.device:
+            raise ValueError("every tensor must live on the same GPU device")
+    pairs = tensors.default_pairs() if pairs is None else bool(pairs)
+    raw = _raw_stream(stream)
+    wsp, wsn = _ws(ws, tensors.device, raw).get(tensors.workspace_size(pairs), raw)
+    _check(lib().attr_muon_step(tensors.array, len(tensors.array), tensors.p_dtype, tensors.g_dtype, lr, momentum,
+                                int(bool(nesterov)), steps, int(pairs), _ptr(grad_scale), wsp, wsn, raw))
+    _written(tensors.weights)
+
+
+# ----------------------------------------------------------------------------
+# (6) embedding and layer norm over token rows
+# ----------------------------------------------------------------------------
+class ExampleRows:
+    """The rows of a batch: token t of example i is row i*T + t, or row_offset[i] + t (int64
+    [n_examples]); tokens from length[i] on (int32 [n_examples]) are padding, never read, and
+    written as zeros without row_offset, not at all with it."""
+
+    def __init__(self, n_examples: int, T: int, row_offset: Optional[torch.Tensor] = None,
+                 length: Optional[torch.Tensor] = None):
+        self.n_examples, self.T = int(n_examples), int(T)
+        self.row_offset, self.length = row_offset, length
+
+    def c(self, n_rows: int) -> _CRows:
+        """The checked descriptor of a call over tensors of n_rows rows."""
+        if self.n_examples < 0 or self.T < 1:
+            raise ValueError("n_examples must be >= 0 and T >= 1")
+        if self.row_offset is None and n_rows < self.n_examples * self.T:
+            raise ValueError(f"{n_rows} rows, {self.n_examples} examples of {self.T} tokens need "
+                             f"{self.n_examples * self.T}")
+        _vector(self.row_offset, self.n_examples, torch.int64, "row_offset")
+        _vector(self.length, self.n_examples, torch.int32, "length")
+        return _CRows(n_rows, self.n_examples, self.T, _ptr(self.row_offset), _ptr(self.length))
+
+
+_ALL_ROWS = ExampleRows(0, 1)
+
+
+def _batch(rows: Optional[ExampleRows], n_rows: int) -> Tuple[_CRows, ExampleRows]:
+    """The call's rows; without `rows` every row is a token of one example."""
+    if rows is None:
+        return _CRows(n_rows, 1 if n_rows else 0, max(n_rows, 1), None, None), _ALL_ROWS
+    return rows.c(n_rows), rows
+
+
+def _matrix(t: torch.Tensor, rows: Optional[int], width: int, name: str) -> int:
+    """Row stride of a tensor of `rows` (None: any number of) rows of `width` elements."""
+    n, w, ld = _rows(t)
+    if (rows is not None and n != rows) or w != width:
+        raise ValueError(f"{name} must have {rows} rows of {width} elements, it has {n} of {w}")
+    return ld if n > 1 else max(ld, w)
+
+
+def _tokens(token: torch.Tensor, n_rows: int) -> None:
+    _vector(token, n_rows, torch.int64, "token")
+
+
+def attr_embed(table: torch.Tensor, token: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+               rows: Optional[ExampleRows] = None, stream=None) -> torch.Tensor:
+    """out[row] = scale * table[token[row]] (table [V, d], token int64 [n_rows], out [n_rows, d], any
+    types); rows of tokens outside [0, V) are zeros."""
+    n, d, ldo = _rows(out)
+    V = table.shape[0]
+    ldt = _matrix(table, V, d, "table")
+    _tokens(token, n)
+    batch, where = _batch(rows, n)
+    _same_gpu(table, token, out, where.row_offset, where.length)
+    _check(lib().attr_embed(batch, token.data_ptr(), table.data_ptr(), _dtype(table), V, d, ldt, scale, out.data_ptr(),
+                            _dtype(out), max(ldo, d), _raw_stream(stream)))
+    _written((out,))
+    return out
+
+
+def attr_embed_backward_workspace_size(n_rows: int, V: int, d: int, rows: Optional[ExampleRows] = None) -> int:
+    return int(lib().attr_embed_backward_workspace_size(_batch(rows, n_rows)[0], V, d))
+
+
+def attr_embed_backward(dout: torch.Tensor, token: torch.Tensor, dtable: torch.Tensor, scale: float = 1.0,
+                        accumulate: bool = False, rows: Optional[ExampleRows] = None, ws: Optional[Workspace] = None,
+                        stream=None) -> torch.Tensor:
+    """dtable[v] = scale * sum of dout's rows whose token is v (zeros where there is none), or with
+    accumulate added to what dtable holds.  The same bits for the same call: tokens are sorted,
+    and their rows added up in order."""
+    n, d, ldd = _rows(dout)
+    V = dtable.shape[0]
+    ldt = _matrix(dtable, V, d, "dtable")
+    _tokens(token, n)
+    batch, where = _batch(rows, n)
+    _same_gpu(dout, token, dtable, where.row_offset, where.length)
+    raw = _raw_stream(stream)
+    need = lib().attr_embed_backward_workspace_size(batch, V, d)
+    wsp, wsn = _ws(ws, dout.device, raw).get(need, raw)
+    _check(lib().attr_embed_backward(batch, token.data_ptr(), dout.data_ptr(), _dtype(dout), max(ldd, d), V, d, scale,
+                                     dtable.data_ptr(), _dtype(dtable), ldt, int(bool(accumulate)), wsp, wsn, raw))
+    _written((dtable,))
+    return dtable
+
+
+def _norm_weights(d: int, *weights: Optional[torch.Tensor]) -> int:
+    """The one type of a norm's weights (fp32 without any)."""
+    kinds = {w.dtype for w in weights if w is not None}
+    if len(kinds) > 1:
+        raise ValueError("weight and bias must have one type")
+    for w in weights:
+        if w is not None and (w.dim() != 1 or w.numel() != d or not w.is_contiguous()):
+            raise ValueError(f"weight and bias must be contiguous vectors of {d} elements")
+    for w in weights:
+        if w is not None:
+            return _dtype(w)
+    return ATTR_F32
+
+
+def attr_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                    bias: Optional[torch.Tensor] = None, eps: float = 1e-5, mean: Optional[torch.Tensor] = None,
+                    rstd: Optional[torch.Tensor] = None, rows: Optional[ExampleRows] = None, stream=None) -> torch.Tensor:
+    """y = (x - mean) rstd weight + bias over the last dimension (x, y [n_rows, d], any types; weight
+    and bias [d] of one type).  mean, rstd: fp32 [n_rows], what the backward pass takes.  y may be x."""
+    n, d, ldx = _rows(x)
+    ldy = _matrix(y, n, d, "y")
+    w_dtype = _norm_weights(d, weight, bias)
+    _vector(mean, n, torch.float32, "mean")
+    _vector(rstd, n, torch.float32, "rstd")
+    batch, where = _batch(rows, n)
+    _same_gpu(x, y, weight, bias, mean, rstd, where.row_offset, where.length)
+    _check(lib().attr_layer_norm(batch, x.data_ptr(), _dtype(x), d, max(ldx, d), _ptr(weight), _ptr(bias), w_dtype, eps,
+                                 y.data_ptr(), _dtype(y), ldy, _ptr(mean), _ptr(rstd), _raw_stream(stream)))
+    _written([t for t in (y, mean, rstd) if t is not None])
+    return y
+
+
+def attr_layer_norm_backward_workspace_size(n_rows: int, d: int, per_example: bool = False,
+                                            rows: Optional[ExampleRows] = None) -> int:
+    return int(lib().attr_layer_norm_backward_workspace_size(_batch(rows, n_rows)[0], d, int(bool(per_example))))
+
+
+def attr_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                             weight: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                             dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                             per_example: bool = False, accumulate: bool = False, rows: Optional[ExampleRows] = None,
+                             ws: Optional[Workspace] = None, stream=None) -> None:
+    """Gradients of attr_layer_norm into those of dx (x's shape and type; may be x or dy), dweight and
+    dbias that are given.  dweight, dbias: fp32 [d], or with per_example [n_examples, d] (rows may be
+    columns of wider ones): every example's own.  accumulate adds to what they hold."""
+    n, d, ldx = _rows(x)
+    ldy = _matrix(dy, n, d, "dy")
+    w_dtype = _norm_weights(d, weight)
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd are what the forward pass gave")
+    _vector(mean, n, torch.float32, "mean")
+    _vector(rstd, n, torch.float32, "rstd")
+    batch, where = _batch(rows, n)
+    lddx, lds = 0, []
+    if dx is not None:
+        lddx = _matrix(dx, n, d, "dx")
+        if dx.dtype != x.dtype:
+            raise ValueError("dx must have x's type")
+    for name, t in (("dweight", dweight), ("dbias", dbias)):
+        if t is None:
+            lds.append(d)
+        elif t.dtype != torch.float32:
+            raise ValueError(f"{name} must be fp32")
+        elif per_example:
+            lds.append(_matrix(t, batch.n_examples, d, name))
+        else:
+            if t.dim() != 1 or t.numel() != d or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous vector of {d} elements")
+            lds.append(d)
+    _same_gpu(dy, x, mean, rstd, weight, dx, dweight, dbias, where.row_offset, where.length)
+    raw = _raw_stream(stream)
+    need = lib().attr_layer_norm_backward_workspace_size(batch, d, int(bool(per_example)))
+    wsp, wsn = _ws(ws, x.device, raw).get(need, raw)
+    _check(lib().attr_layer_norm_backward(batch, dy.data_ptr(), _dtype(dy), ldy, x.data_ptr(), _dtype(x), d, max(ldx, d),
+                                          mean.data_ptr(), rstd.data_ptr(), _ptr(weight), w_dtype, _ptr(dx), lddx,
+                                          _ptr(dweight), lds[0], _ptr(dbias), lds[1], int(bool(per_example)),
+                                          int(bool(accumulate)), wsp, wsn, raw))
+    _written([t for t in (dx, dweight, dbias) if t is not None])
 
 
 # ----------------------------------------------------------------------------

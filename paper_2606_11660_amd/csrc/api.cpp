@@ -1081,6 +1081,572 @@ attr_status attr_adamw_step(const attr_adamw_tensor* tensors, int32_t n_tensors,
 }
 
 // ---------------------------------------------------------------------------
+// Muon
+// ---------------------------------------------------------------------------
+namespace {
+
+static_assert(sizeof(attr_muon_matrix) == 56 && sizeof(attr_rows) == 40, "layouts that the binding mirrors");
+
+// Matrices that are worked on together: those of one shape side by side.
+struct MuonRound {
+  std::vector<int32_t> order;  // the matrices, group by group
+  attr::MuonArgs args;         // but for the table and the workspace's address
+  uint32_t sym, full, flat, turn;  // workgroups
+  size_t bytes;                // of workspace behind the table
+};
+struct MuonPlan {
+  std::vector<MuonRound> rounds;
+  size_t table, total;  // bytes
+};
+
+bool muon_fits(const attr_muon_matrix& t) {
+  if (t.rows < 0 || t.cols < 0 || t.rows > (1ll << 20) || t.cols > (1ll << 20)) return false;
+  return std::max(t.rows, t.cols) * ((std::min(t.rows, t.cols) + 63) / 64 * 64) < (1ll << 30);
+}
+
+// Workspace of one matrix, and the workgroups that its launches take.
+attr::MuonGroup muon_group(int64_t rows, int64_t cols, bool pairs) {
+  attr::MuonGroup q;
+  std::memset(&q, 0, sizeof(q));
+  q.rows = (int32_t)rows;
+  q.cols = (int32_t)cols;
+  q.L = (int32_t)std::max(rows, cols);
+  q.S = (int32_t)std::min(rows, cols);
+  q.ld = (q.S + 63) / 64 * 64;
+  const int64_t y = (int64_t)align_up((size_t)q.L * q.ld * 2), s = (int64_t)align_up((size_t)q.S * q.ld * 2);
+  const int64_t many = pairs ? 2 : 1;
+  q.lo_y = y;
+  q.lo_s = s;
+  q.y[0] = 0;
+  q.y[1] = many * y;
+  q.gram = 2 * many * y;
+  q.poly = q.gram + many * s;
+  q.norm = q.poly + many * s;
+  q.stride = q.norm + (int64_t)align_up(8 * attr::kMuonFlatMost);
+  const uint32_t ts = (uint32_t)(q.S + attr::kMuonTile - 1) / attr::kMuonTile,
+                 tl = (uint32_t)(q.L + attr::kMuonTile - 1) / attr::kMuonTile;
+  q.n_sym = ts * (ts + 1) / 2;
+  q.n_full = ts * tl;
+  q.n_flat = (uint32_t)std::min<int64_t>((rows * cols + attr::kMuonFlat - 1) / attr::kMuonFlat, attr::kMuonFlatMost);
+  q.n_turn = (uint32_t)((q.L + 63) / 64) * (uint32_t)(q.ld / 64);
+  return q;
+}
+
+// A round ends where its launches fill the GPU some times over: its buffers then stay
+// small, and nearer to the caches.
+constexpr uint32_t kMuonRoundTiles = 4096;
+constexpr size_t kMuonRoundBytes = (size_t)1 << 30;
+
+MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
+  MuonPlan P;
+  std::map<std::pair<int64_t, int64_t>, std::vector<int32_t>> shapes;
+  for (int32_t j = 0; j < n; ++j)
+    if (mats[j].rows > 0 && mats[j].cols > 0) shapes[{mats[j].rows, mats[j].cols}].push_back(j);
+  MuonRound R;
+  const auto clear = [&] {
+    R.order.clear();
+    std::memset(&R.args, 0, sizeof(R.args));
+    R.sym = R.full = R.flat = R.turn = 0;
+    R.bytes = 0;
+  };
+  size_t most = 0, matrices = 0;
+  const auto end = [&] {
+    if (R.order.empty()) return;
+    most = std::max(most, R.bytes);
+    matrices = std::max(matrices, R.order.size());
+    P.rounds.push_back(R);
+    clear();
+  };
+  clear();
+  for (const auto& sh : shapes) {
+    attr::MuonGroup q = muon_group(sh.first.first, sh.first.second, pairs);
+    bool open = false;
+    for (int32_t j : sh.second) {
+      if (!R.order.empty() && (R.full + q.n_full > kMuonRoundTiles || R.bytes + (size_t)q.stride > kMuonRoundBytes ||
+                               (!open && R.args.n_groups == attr::kMuonGroups))) {
+        end();
+        open = false;
+      }
+      if (!open) {
+        q.base = reinterpret_cast<char*>(R.bytes);  // behind the table
+        q.tile_sym = R.sym;
+        q.tile_full = R.full;
+        q.tile_flat = R.flat;
+        q.tile_turn = R.turn;
+        q.entry = (uint32_t)R.order.size();
+        R.args.g[R.args.n_groups++] = q;
+        open = true;
+      }
+      R.order.push_back(j);
+      R.sym += q.n_sym;
+      R.full += q.n_full;
+      R.flat += q.n_flat;
+      R.turn += q.n_turn;
+      R.bytes += (size_t)q.stride;
+    }
+  }
+  end();
+  P.table = align_up(matrices * sizeof(attr::MuonEntry));
+  P.total = P.rounds.empty() ? 0 : P.table + most;
+  return P;
+}
+
+}  // namespace
+
+size_t attr_muon_step_workspace_size(const attr_muon_matrix* mats, int32_t n_mats, int32_t pairs) {
+  try {
+    if (n_mats <= 0 || !mats || (pairs != 0 && pairs != 1)) return 0;
+    for (int32_t j = 0; j < n_mats; ++j)
+      if (!muon_fits(mats[j])) return 0;
+    return muon_plan(mats, n_mats, pairs != 0).total;
+  } catch (...) {
+    return 0;
+  }
+}
+
+attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dtype p_dtype, attr_dtype g_dtype,
+                           double lr, double momentum, int32_t nesterov, int32_t steps, int32_t pairs,
+                           const float* grad_scale, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_muon_step";
+    if (n_mats < 0 || (n_mats > 0 && !mats))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: n_mats is negative or mats NULL", who);
+    if (!valid_dtype(p_dtype) || !valid_dtype(g_dtype))
+      return fail(ATTR_ERR_UNSUPPORTED, "%s: weights and gradients must be ATTR_F32, ATTR_BF16 or ATTR_F16", who);
+    if (!(std::fabs(lr) <= 3.0e38)) return fail(ATTR_ERR_INVALID_ARG, "%s: lr must be finite", who);
+    if (!(momentum >= 0.0 && momentum < 1.0)) return fail(ATTR_ERR_INVALID_ARG, "%s: momentum must be in [0, 1)", who);
+    if ((nesterov != 0 && nesterov != 1) || (pairs != 0 && pairs != 1))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: nesterov and pairs must be 0 or 1", who);
+    if (steps < 1 || steps > 16) return fail(ATTR_ERR_INVALID_ARG, "%s: steps=%d must be in [1, 16]", who, (int)steps);
+    if (!aligned_to(grad_scale, 4)) return fail(ATTR_ERR_ALIGNMENT, "%s: grad_scale must be 4-byte aligned", who);
+    const size_t pb = (size_t)dtype_bytes(p_dtype), gb = (size_t)dtype_bytes(g_dtype);
+    bool master = false, plain = false;
+    for (int32_t j = 0; j < n_mats; ++j) {
+      const attr_muon_matrix& t = mats[j];
+      if (t.rows < 0 || t.cols < 0)
+        return fail(ATTR_ERR_INVALID_ARG, "%s: matrix %d: %lld x %lld", who, j, (long long)t.rows, (long long)t.cols);
+      if (!muon_fits(t))
+        return fail(ATTR_ERR_UNSUPPORTED, "%s: matrix %d: %lld x %lld is too large", who, j, (long long)t.rows,
+                    (long long)t.cols);
+      if (!(std::fabs(t.lr_scale) <= 3.0e38f) || !(std::fabs(t.weight_decay) <= 3.0e38f))
+        return fail(ATTR_ERR_INVALID_ARG, "%s: matrix %d: lr_scale and weight_decay must be finite", who, j);
+      if (t.rows == 0 || t.cols == 0) continue;
+      if (!t.p || !t.g || !t.m) return fail(ATTR_ERR_INVALID_ARG, "%s: matrix %d: NULL pointer", who, j);
+      if (!aligned_to(t.p, pb) || !aligned_to(t.g, gb) || !aligned_to(t.m, 4) || !aligned_to(t.master, 4))
+        return fail(ATTR_ERR_ALIGNMENT, "%s: matrix %d: pointers must be aligned to their elements", who, j);
+      (t.master ? master : plain) = true;
+    }
+    if (master && plain)
+      return fail(ATTR_ERR_INVALID_ARG, "%s: either every matrix has a master, or none has", who);
+    const MuonPlan P = muon_plan(mats, n_mats, pairs != 0);
+    if (P.rounds.empty()) return ATTR_OK;
+    if (!ws || ws_bytes < P.total)
+      return fail(ATTR_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", who, P.total, ws ? ws_bytes : (size_t)0);
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ATTR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* const base = static_cast<char*>(ws);
+    const auto launch = [&](const MuonRound& R) -> hipError_t {
+      attr::MuonTable T;
+      for (size_t at = 0; at < R.order.size(); at += attr::kMuonTable) {
+        std::memset(&T, 0, sizeof(T));
+        T.n = (int32_t)std::min<size_t>(attr::kMuonTable, R.order.size() - at);
+        T.to = reinterpret_cast<attr::MuonEntry*>(base) + at;
+        for (int32_t k = 0; k < T.n; ++k) {
+          const attr_muon_matrix& t = mats[R.order[at + (size_t)k]];
+          const double rate = lr * (double)t.lr_scale;
+          T.e[k] = {t.p, t.g, t.m, t.master, (float)rate, (float)(rate * (double)t.weight_decay)};
+        }
+        const hipError_t e = attr::launch_muon_table(T, s);
+        if (e != hipSuccess) return e;
+      }
+      attr::MuonArgs a = R.args;
+      for (int k = 0; k < a.n_groups; ++k) a.g[k].base = base + P.table + reinterpret_cast<uintptr_t>(a.g[k].base);
+      a.table = reinterpret_cast<const attr::MuonEntry*>(base);
+      a.grad_scale = grad_scale;
+      a.momentum = (float)momentum;
+      a.one_momentum = (float)(1.0 - momentum);
+      a.nesterov = nesterov;
+      hipError_t e = attr::launch_muon_momentum((int)g_dtype, a, R.flat, s);
+      if (e == hipSuccess) e = attr::launch_muon_split((int)g_dtype, pairs != 0, a, R.turn, s);
+      for (int32_t k = 0; k < steps && e == hipSuccess; ++k) {
+        const int from = k & 1;
+        e = attr::launch_muon_gram(pairs != 0, from, a, R.sym, s);
+        if (e == hipSuccess) e = attr::launch_muon_poly(pairs != 0, a, R.sym, s);
+        if (e != hipSuccess) break;
+        e = k + 1 < steps ? attr::launch_muon_apply(pairs != 0, from, a, R.full, s)
+                          : attr::launch_muon_last(pairs != 0, (int)p_dtype, master, from, a, R.full, s);
+      }
+      return e;
+    };
+    for (const MuonRound& R : P.rounds) {
+      const hipError_t e = launch(R);
+      if (e != hipSuccess) return device_fail(e, "attr_muon_step launch");
+    }
+    return ATTR_OK;
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_muon_step: host exception");
+  }
+}
+
+// ---------------------------------------------------------------------------
+// embedding and layer norm over token rows
+// ---------------------------------------------------------------------------
+namespace {
+
+bool rows_sizes_ok(const attr_rows* r) {
+  return r && r->n_rows >= 0 && r->n_examples >= 0 && r->T >= 1 && r->T < (1ll << 31) &&
+         r->n_examples < (1ll << 31) && r->n_examples * r->T < (1ll << 31);
+}
+
+attr_status rows_validate(const attr_rows* r, const char* who) {
+  if (!r) return fail(ATTR_ERR_INVALID_ARG, "%s: rows is NULL", who);
+  if (r->n_rows < 0 || r->n_examples < 0 || r->T < 1)
+    return fail(ATTR_ERR_INVALID_ARG, "%s: n_rows and n_examples must be >= 0, T >= 1", who);
+  if (!rows_sizes_ok(r)) return fail(ATTR_ERR_UNSUPPORTED, "%s: n_examples * T must be below 2^31; split the batch", who);
+  if (!r->row_offset && r->n_rows < r->n_examples * r->T)
+    return fail(ATTR_ERR_INVALID_ARG, "%s: %lld rows, %lld examples of %lld tokens need more", who, (long long)r->n_rows,
+                (long long)r->n_examples, (long long)r->T);
+  if (!aligned_to(r->row_offset, 8) || !aligned_to(r->length, 4))
+    return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+  return ATTR_OK;
+}
+
+// A matrix of a call: its type, stride, size and alignment.
+attr_status matrix_validate(const void* p, attr_dtype t, int64_t rows, int64_t d, int64_t ld, const char* name,
+                            const char* who) {
+  if (!valid_dtype(t)) return fail(ATTR_ERR_UNSUPPORTED, "%s: %s must be ATTR_F32, ATTR_BF16 or ATTR_F16", who, name);
+  if (ld < d || ld > (1ll << 40)) return fail(ATTR_ERR_INVALID_ARG, "%s: %s's row stride %lld must be in [d, 2^40]", who, name, (long long)ld);
+  if (rows > (1ll << 40) / ld * (1ll << 20)) return fail(ATTR_ERR_INVALID_ARG, "%s: %s has too many rows", who, name);
+  if (!p) return fail(ATTR_ERR_INVALID_ARG, "%s: %s is NULL", who, name);
+  if (!aligned_to(p, (size_t)dtype_bytes(t))) return fail(ATTR_ERR_ALIGNMENT, "%s: %s must be aligned to its elements", who, name);
+  return ATTR_OK;
+}
+
+attr::RowsArgs rows_args(const attr_rows* r) {
+  attr::RowsArgs a;
+  a.row_offset = r->row_offset;
+  a.length = r->length;
+  a.n_rows = r->n_rows;
+  a.n_slots = (uint32_t)(r->n_examples * r->T);
+  a.T = (uint32_t)r->T;
+  return a;
+}
+
+// Spans of a call's buffers: no output overlaps an input or another output.
+class RowSpans {
+ public:
+  explicit RowSpans(const attr_rows* r) {
+    input(span_of(r->row_offset, 1, r->row_offset ? r->n_examples : 0, r->n_examples, 8));
+    input(span_of(r->length, 1, r->length ? r->n_examples : 0, r->n_examples, 4));
+  }
+  void input(Span x) { in_.push_back(x); }
+  // between: its rows lie between those of the output before it, and are known not to touch them
+  void output(Span x, bool between = false) {
+    for (size_t j = 0; j + (between ? 1 : 0) < out_.size(); ++j) clash_ |= touches(x, out_[j]);
+    out_.push_back(x);
+  }
+  bool clash() const {
+    bool bad = clash_;
+    for (const Span& o : out_)
+      for (const Span& x : in_) bad |= touches(o, x);
+    return bad;
+  }
+
+ private:
+  static bool touches(Span a, Span b) { return a.lo < a.hi && b.lo < b.hi && overlap(a, b); }
+  std::vector<Span> in_, out_;
+  bool clash_ = false;
+};
+Span vector_span(const void* p, int64_t n, int eb) { return span_of(p, 1, p ? n : 0, n, eb); }
+attr_status overlap_fail(const char* who) {
+  return fail(ATTR_ERR_INVALID_ARG, "%s: outputs overlap each other or the inputs", who);
+}
+
+attr_status table_validate(int64_t V, int64_t d, const char* who) {
+  if (V < 1 || V > (1ll << 28)) return fail(ATTR_ERR_INVALID_ARG, "%s: V=%lld must be in [1, 2^28]", who, (long long)V);
+  if (d < 1 || d > 65536) return fail(ATTR_ERR_INVALID_ARG, "%s: d=%lld must be in [1, 65536]", who, (long long)d);
+  return ATTR_OK;
+}
+
+struct EmbedLayout {
+  size_t key[2], row[2], count, part, total;
+};
+EmbedLayout embed_layout(const attr_rows* r, int64_t V, int64_t d) {
+  EmbedLayout L;
+  const size_t n = (size_t)(r->n_examples * r->T), each = align_up(4 * n);
+  L.key[0] = 0;
+  L.key[1] = each;
+  L.row[0] = 2 * each;
+  L.row[1] = 3 * each;
+  L.count = 4 * each;
+  const size_t blocks = (n + attr::kSortKeys - 1) / attr::kSortKeys;
+  L.part = L.count + (n > attr::kSortOneMost ? align_up((blocks << attr::sort_bits(V)) * 4) : 0);
+  const size_t parts = (n + attr::kEmbedPart - 1) / attr::kEmbedPart;
+  L.total = L.part + align_up(parts * 2 * (size_t)d * 4);
+  return L;
+}
+
+}  // namespace
+
+attr_status attr_embed(const attr_rows* rows, const int64_t* token, const void* table, attr_dtype table_dtype, int64_t V,
+                       int64_t d, int64_t ldt, float scale, void* out, attr_dtype out_dtype, int64_t ldo, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_embed";
+    attr_status st = rows_validate(rows, who);
+    if (st == ATTR_OK) st = table_validate(V, d, who);
+    if (st != ATTR_OK) return st;
+    if (!(std::fabs(scale) <= 3.0e38f)) return fail(ATTR_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    if (rows->n_examples == 0 || rows->n_rows == 0) return ATTR_OK;
+    st = matrix_validate(table, table_dtype, V, d, ldt, "table", who);
+    if (st == ATTR_OK) st = matrix_validate(out, out_dtype, rows->n_rows, d, ldo, "out", who);
+    if (st != ATTR_OK) return st;
+    if (!token) return fail(ATTR_ERR_INVALID_ARG, "%s: token is NULL", who);
+    if (!aligned_to(token, 8)) return fail(ATTR_ERR_ALIGNMENT, "%s: token must be aligned to its elements", who);
+    RowSpans spans(rows);
+    spans.input(vector_span(token, rows->n_rows, 8));
+    spans.input(span_of(table, V, d, ldt, dtype_bytes(table_dtype)));
+    spans.output(span_of(out, rows->n_rows, d, ldo, dtype_bytes(out_dtype)));
+    if (spans.clash()) return overlap_fail(who);
+    const attr::EmbedArgs a{token, table, out, V, ldt, ldo, (int32_t)d, scale};
+    const hipError_t e = attr::launch_embed((int)table_dtype, (int)out_dtype, rows_args(rows), a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_embed launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_embed: host exception");
+  }
+}
+
+size_t attr_embed_backward_workspace_size(const attr_rows* rows, int64_t V, int64_t d) {
+  if (!rows_sizes_ok(rows) || V < 1 || V > (1ll << 28) || d < 1 || d > 65536) return 0;
+  return embed_layout(rows, V, d).total;
+}
+
+attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, const void* dout, attr_dtype dout_dtype,
+                                int64_t ldd, int64_t V, int64_t d, float scale, void* dtable, attr_dtype dtable_dtype,
+                                int64_t ldt, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_embed_backward";
+    attr_status st = rows_validate(rows, who);
+    if (st == ATTR_OK) st = table_validate(V, d, who);
+    if (st != ATTR_OK) return st;
+    if (!(std::fabs(scale) <= 3.0e38f)) return fail(ATTR_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    if (accumulate != 0 && accumulate != 1) return fail(ATTR_ERR_INVALID_ARG, "%s: accumulate must be 0 or 1", who);
+    if (rows->n_rows >= (1ll << 32)) return fail(ATTR_ERR_UNSUPPORTED, "%s: n_rows must be below 2^32; split the batch", who);
+    const bool none = rows->n_examples == 0 || rows->n_rows == 0;
+    if (none && accumulate) return ATTR_OK;
+    st = matrix_validate(dtable, dtable_dtype, V, d, ldt, "dtable", who);
+    if (st == ATTR_OK && !none) st = matrix_validate(dout, dout_dtype, rows->n_rows, d, ldd, "dout", who);
+    if (st != ATTR_OK) return st;
+    if (!valid_dtype(dout_dtype)) return fail(ATTR_ERR_UNSUPPORTED, "%s: dout must be ATTR_F32, ATTR_BF16 or ATTR_F16", who);
+    if (!none && !token) return fail(ATTR_ERR_INVALID_ARG, "%s: token is NULL", who);
+    if (!aligned_to(token, 8)) return fail(ATTR_ERR_ALIGNMENT, "%s: token must be aligned to its elements", who);
+    RowSpans spans(rows);
+    spans.input(vector_span(token, rows->n_rows, 8));
+    if (!none) spans.input(span_of(dout, rows->n_rows, d, ldd, dtype_bytes(dout_dtype)));
+    spans.output(span_of(dtable, V, d, ldt, dtype_bytes(dtable_dtype)));
+    if (spans.clash()) return overlap_fail(who);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    attr::EmbedGradArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.dout = dout;
+    a.dtable = dtable;
+    a.V = V;
+    a.ldd = ldd;
+    a.ldt = ldt;
+    a.d = (int32_t)d;
+    a.accumulate = accumulate;
+    a.scale = scale;
+    if (!none) {
+      const EmbedLayout L = embed_layout(rows, V, d);
+      if (!ws || ws_bytes < L.total)
+        return fail(ATTR_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", who, L.total, ws ? ws_bytes : (size_t)0);
+      if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ATTR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+      char* const base = static_cast<char*>(ws);
+      const attr::RowsArgs r = rows_args(rows);
+      attr::EmbedSort e;
+      for (int k = 0; k < 2; ++k) {
+        e.key[k] = reinterpret_cast<uint32_t*>(base + L.key[k]);
+        e.row[k] = reinterpret_cast<uint32_t*>(base + L.row[k]);
+      }
+      e.count = reinterpret_cast<uint32_t*>(base + L.count);
+      e.passes = attr::sort_passes(V);
+      e.bits = attr::sort_bits(V);
+      e.blocks = (r.n_slots + attr::kSortKeys - 1) / attr::kSortKeys;
+      const hipError_t st2 = attr::launch_embed_sort(r, token, V, e, s);
+      if (st2 != hipSuccess) return device_fail(st2, "attr_embed_backward sort launch");
+      a.key = e.key[e.passes & 1];
+      a.row = e.row[e.passes & 1];
+      a.part = reinterpret_cast<float*>(base + L.part);
+      a.n = r.n_slots;
+    }
+    const hipError_t e = attr::launch_embed_grad((int)dout_dtype, (int)dtable_dtype, a, s);
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_embed_backward launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_embed_backward: host exception");
+  }
+}
+
+namespace {
+
+attr_status norm_validate(const attr_rows* r, int64_t d, const void* weight, const void* bias, attr_dtype w_dtype,
+                          const char* who) {
+  const attr_status st = rows_validate(r, who);
+  if (st != ATTR_OK) return st;
+  if (d < 1 || d > attr::kNormWidest)
+    return fail(ATTR_ERR_INVALID_ARG, "%s: d=%lld must be in [1, %d]", who, (long long)d, (int)attr::kNormWidest);
+  if ((weight || bias) && !valid_dtype(w_dtype))
+    return fail(ATTR_ERR_UNSUPPORTED, "%s: weights must be ATTR_F32, ATTR_BF16 or ATTR_F16", who);
+  const size_t wb = weight || bias ? (size_t)dtype_bytes(w_dtype) : 1;
+  if (!aligned_to(weight, wb) || !aligned_to(bias, wb))
+    return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+  return ATTR_OK;
+}
+
+// Whether d columns from p and d from q of matrices with row stride ld are columns of one matrix
+// that do not touch.
+bool columns_apart(const float* p, const float* q, int64_t d, int64_t ld) {
+  const int64_t at = (int64_t)(reinterpret_cast<uintptr_t>(q) / 4) - (int64_t)(reinterpret_cast<uintptr_t>(p) / 4);
+  const int64_t c = (at % ld + ld) % ld;
+  return c >= d && c + d <= ld;
+}
+
+// (unit, units, chunk, chunks) of a gradient call.
+void norm_split(const attr_rows* r, int64_t d, int32_t per_example, attr::NormGradArgs& a) {
+  a.unit = (uint32_t)(per_example ? r->T : r->n_examples * r->T);
+  a.units = (uint32_t)(per_example ? r->n_examples : 1);
+  a.chunk = attr::norm_chunk(a.unit, a.units, (int32_t)d);
+  a.chunks = (a.unit + a.chunk - 1) / a.chunk;
+}
+size_t norm_bytes(const attr::NormGradArgs& a, int64_t d) {
+  return a.chunks > 1 ? align_up((size_t)a.units * a.chunks * 2 * (size_t)d * 4) : 0;
+}
+
+}  // namespace
+
+attr_status attr_layer_norm(const attr_rows* rows, const void* x, attr_dtype x_dtype, int64_t d, int64_t ldx,
+                            const void* weight, const void* bias, attr_dtype w_dtype, float eps, void* y,
+                            attr_dtype y_dtype, int64_t ldy, float* mean, float* rstd, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_layer_norm";
+    attr_status st = norm_validate(rows, d, weight, bias, w_dtype, who);
+    if (st != ATTR_OK) return st;
+    if (!(eps >= 0.f && eps <= 3.0e38f)) return fail(ATTR_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", who);
+    if (rows->n_examples == 0 || rows->n_rows == 0) return ATTR_OK;
+    st = matrix_validate(x, x_dtype, rows->n_rows, d, ldx, "x", who);
+    if (st == ATTR_OK) st = matrix_validate(y, y_dtype, rows->n_rows, d, ldy, "y", who);
+    if (st != ATTR_OK) return st;
+    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4))
+      return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    RowSpans spans(rows);
+    if (!(y == x && y_dtype == x_dtype && ldy == ldx)) spans.input(span_of(x, rows->n_rows, d, ldx, dtype_bytes(x_dtype)));
+    if (weight) spans.input(vector_span(weight, d, dtype_bytes(w_dtype)));
+    if (bias) spans.input(vector_span(bias, d, dtype_bytes(w_dtype)));
+    spans.output(span_of(y, rows->n_rows, d, ldy, dtype_bytes(y_dtype)));
+    spans.output(vector_span(mean, rows->n_rows, 4));
+    spans.output(vector_span(rstd, rows->n_rows, 4));
+    if (spans.clash()) return overlap_fail(who);
+    const attr::NormArgs a{x, weight, bias, y, mean, rstd, ldx, ldy, (int32_t)d, (int32_t)w_dtype, eps};
+    const hipError_t e = attr::launch_layer_norm((int)x_dtype, (int)y_dtype, rows_args(rows), a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_layer_norm launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_layer_norm: host exception");
+  }
+}
+
+size_t attr_layer_norm_backward_workspace_size(const attr_rows* rows, int64_t d, int32_t per_example) {
+  if (!rows_sizes_ok(rows) || d < 1 || d > attr::kNormWidest || (per_example != 0 && per_example != 1) ||
+      rows->n_examples == 0)
+    return 0;
+  attr::NormGradArgs a;
+  norm_split(rows, d, per_example, a);
+  return norm_bytes(a, d);
+}
+
+attr_status attr_layer_norm_backward(const attr_rows* rows, const void* dy, attr_dtype dy_dtype, int64_t lddy,
+                                     const void* x, attr_dtype x_dtype, int64_t d, int64_t ldx, const float* mean,
+                                     const float* rstd, const void* weight, attr_dtype w_dtype, void* dx, int64_t lddx,
+                                     float* dweight, int64_t ldw, float* dbias, int64_t ldb, int32_t per_example,
+                                     int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    g_err.clear();
+    const char* who = "attr_layer_norm_backward";
+    attr_status st = norm_validate(rows, d, weight, nullptr, w_dtype, who);
+    if (st != ATTR_OK) return st;
+    if ((per_example != 0 && per_example != 1) || (accumulate != 0 && accumulate != 1))
+      return fail(ATTR_ERR_INVALID_ARG, "%s: per_example and accumulate must be 0 or 1", who);
+    const int64_t units = per_example ? rows->n_examples : 1;
+    if (dweight && (st = matrix_validate(dweight, ATTR_F32, units, d, per_example ? ldw : d, "dweight", who)) != ATTR_OK) return st;
+    if (dbias && (st = matrix_validate(dbias, ATTR_F32, units, d, per_example ? ldb : d, "dbias", who)) != ATTR_OK) return st;
+    if (rows->n_examples == 0 && (per_example || accumulate)) return ATTR_OK;
+    const bool none = rows->n_examples == 0 || rows->n_rows == 0;
+    if (!none) {
+      st = matrix_validate(x, x_dtype, rows->n_rows, d, ldx, "x", who);
+      if (st == ATTR_OK) st = matrix_validate(dy, dy_dtype, rows->n_rows, d, lddy, "dy", who);
+      if (st == ATTR_OK && dx) st = matrix_validate(dx, x_dtype, rows->n_rows, d, lddx, "dx", who);
+      if (st != ATTR_OK) return st;
+      if (!mean || !rstd) return fail(ATTR_ERR_INVALID_ARG, "%s: mean or rstd is NULL", who);
+      if (!aligned_to(mean, 4) || !aligned_to(rstd, 4))
+        return fail(ATTR_ERR_ALIGNMENT, "%s: pointers must be aligned to their elements", who);
+    }
+    if (!valid_dtype(x_dtype) || !valid_dtype(dy_dtype))
+      return fail(ATTR_ERR_UNSUPPORTED, "%s: x and dy must be ATTR_F32, ATTR_BF16 or ATTR_F16", who);
+    RowSpans spans(rows);
+    if (!none) {
+      if (!(dx == x && lddx == ldx)) spans.input(span_of(x, rows->n_rows, d, ldx, dtype_bytes(x_dtype)));
+      if (!(dx == dy && dy_dtype == x_dtype && lddx == lddy)) spans.input(span_of(dy, rows->n_rows, d, lddy, dtype_bytes(dy_dtype)));
+      if (weight) spans.input(vector_span(weight, d, dtype_bytes(w_dtype)));
+      spans.input(vector_span(mean, rows->n_rows, 4));
+      spans.input(vector_span(rstd, rows->n_rows, 4));
+      if (dx) spans.output(span_of(dx, rows->n_rows, d, lddx, dtype_bytes(x_dtype)));
+    }
+    if (dweight) spans.output(span_of(dweight, units, d, per_example ? ldw : d, 4));
+    if (dbias)
+      spans.output(span_of(dbias, units, d, per_example ? ldb : d, 4),
+                   dweight && per_example && ldw == ldb && columns_apart(dweight, dbias, d, ldw));
+    if (spans.clash()) return overlap_fail(who);
+    if (!dx && !dweight && !dbias) return ATTR_OK;
+    attr::NormGradArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.x = x;
+    a.dy = dy;
+    a.weight = weight;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.dx = dx;
+    a.dweight = dweight;
+    a.dbias = dbias;
+    a.ldx = ldx;
+    a.lddy = lddy;
+    a.lddx = lddx;
+    a.ldw = ldw;
+    a.ldb = ldb;
+    a.d = (int32_t)d;
+    a.w_dtype = (int32_t)w_dtype;
+    a.accumulate = accumulate;
+    attr::RowsArgs r = rows_args(rows);
+    if (none) {  // sums of no rows: one empty unit, or one for each example
+      a.unit = a.chunk = a.chunks = 1;
+      a.units = (uint32_t)units;
+      r = attr::RowsArgs{nullptr, nullptr, 0, (uint32_t)units, 1};
+    } else {
+      norm_split(rows, d, per_example, a);
+      const size_t need = norm_bytes(a, d);
+      if (need && (!ws || ws_bytes < need))
+        return fail(ATTR_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", who, need, ws ? ws_bytes : (size_t)0);
+      if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ATTR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+      a.part = need ? static_cast<float*>(ws) : nullptr;
+    }
+    const hipError_t e = attr::launch_layer_norm_grad((int)x_dtype, (int)dy_dtype, r, a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_layer_norm_backward launch");
+  } catch (...) {
+    return fail(ATTR_ERR_INVALID_ARG, "attr_layer_norm_backward: host exception");
+  }
+}
+
+// ---------------------------------------------------------------------------
 attr_status attr_probe_read(const void* x, size_t bytes, void* sink, void* stream) {
   g_err.clear();
   if (bytes == 0) return ATTR_OK;

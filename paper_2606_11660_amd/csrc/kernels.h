@@ -301,6 +301,152 @@ hipError_t launch_adamw(int p_dtype, int g_dtype, bool eight, bool master, int r
                         const AdamwFull& a, hipStream_t s);
 
 // ---------------------------------------------------------------------------
+// embedding and layer norm over token rows
+// ---------------------------------------------------------------------------
+struct RowsArgs {
+  const int64_t* row_offset;  // or null
+  const int32_t* length;      // or null
+  int64_t n_rows;
+  uint32_t n_slots, T;
+};
+struct EmbedArgs {
+  const int64_t* token;
+  const void* table;
+  void* out;
+  int64_t V, ldt, ldo;
+  int32_t d;
+  float scale;
+};
+hipError_t launch_embed(int table_dtype, int out_dtype, const RowsArgs& r, const EmbedArgs& a, hipStream_t s);
+
+// The gradient of a table: the batch's (token, row) pairs in the order of their tokens,
+// rows of one token in the order of their slots; slots without a token have the key V.
+struct EmbedSort {
+  uint32_t* key[2];   // [n_slots] each; the sorted pairs are in [passes & 1]
+  uint32_t* row[2];
+  uint32_t* count;    // [bins * blocks], one workgroup's sort needs none
+  int passes, bits;   // bits of a pass's digit
+  uint32_t blocks;
+};
+constexpr uint32_t kSortKeys = 4096;        // keys of a workgroup
+constexpr uint32_t kSortOneMost = 16384;    // keys that one workgroup sorts alone
+constexpr int kSortBits = 10;               // of a digit, at most
+inline int sort_passes(int64_t V) {
+  int bits = 1;
+  while ((V >> bits) != 0) ++bits;  // of the key V
+  return (bits + kSortBits - 1) / kSortBits;
+}
+inline int sort_bits(int64_t V) {
+  int bits = 1;
+  while ((V >> bits) != 0) ++bits;
+  const int passes = sort_passes(V);
+  return (bits + passes - 1) / passes;
+}
+hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, hipStream_t s);
+// A wave adds up the rows of kEmbedPart neighbours in that order; a token whose rows
+// reach past a part leaves sums to be joined.
+constexpr uint32_t kEmbedPart = 32;
+struct EmbedGradArgs {
+  const uint32_t* key;
+  const uint32_t* row;
+  const void* dout;
+  void* dtable;
+  float* part;        // [parts][2][d]: of the token that began before, of the one that goes on
+  int64_t V, ldd, ldt;
+  uint32_t n;         // pairs, those without a token last
+  int32_t d, accumulate;
+  float scale;
+};
+hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArgs& a, hipStream_t s);
+
+struct NormArgs {
+  const void* x;
+  const void* weight;  // or null: 1
+  const void* bias;    // or null: 0
+  void* y;
+  float* mean;         // or null
+  float* rstd;         // or null
+  int64_t ldx, ldy;
+  int32_t d, w_dtype;
+  float eps;
+};
+hipError_t launch_layer_norm(int x_dtype, int y_dtype, const RowsArgs& r, const NormArgs& a, hipStream_t s);
+
+// A unit is what the weights' gradients are summed over: an example's slots, or all of
+// them; a workgroup sums a chunk of a unit's slots.
+struct NormGradArgs {
+  const void* x;
+  const void* dy;
+  const void* weight;  // or null: 1
+  const float* mean;
+  const float* rstd;
+  void* dx;            // or null
+  float* dweight;      // or null
+  float* dbias;        // or null
+  float* part;         // [chunks][2][d], or null: a unit is one chunk
+  int64_t ldx, lddy, lddx, ldw, ldb;
+  int32_t d, w_dtype, accumulate;
+  uint32_t unit;       // slots of a unit
+  uint32_t chunk;      // slots of a chunk
+  uint32_t chunks;     // of a unit
+  uint32_t units;
+};
+uint32_t norm_chunk(uint32_t unit, uint32_t units, int32_t d);
+hipError_t launch_layer_norm_grad(int x_dtype, int dy_dtype, const RowsArgs& r, const NormGradArgs& a, hipStream_t s);
+constexpr int32_t kNormWidest = 32768;
+
+// ---------------------------------------------------------------------------
+// Muon
+// ---------------------------------------------------------------------------
+struct MuonEntry {
+  void* p;
+  const void* g;
+  float* m;
+  float* master;
+  float lr, lr_wd;
+};
+constexpr int kMuonTable = 96;  // entries that travel in one launch's arguments
+struct MuonTable {
+  MuonEntry* to;
+  int32_t n, pad;
+  MuonEntry e[kMuonTable];
+};
+static_assert(sizeof(MuonTable) <= 4096, "kernel arguments");
+// Matrices of one shape.  Y is the update with its longer side first, [L][S] with rows of ld
+// halves; each is held as 16-bit values, and with pairs as two (the second `lo` bytes after the
+// first).
+struct MuonGroup {
+  char* base;             // of the first matrix's buffers
+  int64_t stride;         // bytes from a matrix's to the next one's
+  int64_t y[2], gram, poly, norm;  // byte offsets in a matrix's buffers
+  int64_t lo_y, lo_s;     // from the first halves to the second: of Y; of gram and poly
+  uint32_t tile_sym, tile_full, tile_flat, tile_turn;  // first workgroup of the group in each launch
+  uint32_t n_sym, n_full, n_flat, n_turn;              // workgroups of a matrix
+  uint32_t entry;         // first matrix in the table
+  int32_t rows, cols, L, S, ld;
+};
+constexpr int kMuonGroups = 16;
+struct MuonArgs {
+  const MuonEntry* table;
+  const float* grad_scale;
+  float momentum, one_momentum;
+  int32_t nesterov, n_groups;
+  MuonGroup g[kMuonGroups];
+};
+static_assert(sizeof(MuonArgs) <= 4096, "kernel arguments");
+constexpr int kMuonTile = 128;
+constexpr int64_t kMuonFlat = 16384;   // elements of a workgroup of the momentum's launch, at least
+constexpr uint32_t kMuonFlatMost = 256;  // such workgroups of a matrix
+hipError_t launch_muon_table(const MuonTable& t, hipStream_t s);
+hipError_t launch_muon_momentum(int g_dtype, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_split(int g_dtype, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_gram(bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_poly(bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_apply(bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_last(bool pairs, int p_dtype, bool master, int from, const MuonArgs& a, uint32_t blocks,
+                            hipStream_t s);
+
+// ---------------------------------------------------------------------------
 // calibration
 // ---------------------------------------------------------------------------
 hipError_t launch_probe_read(const void* x, size_t bytes, void* sink, hipStream_t s);

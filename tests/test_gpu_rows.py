@@ -1,0 +1,466 @@
+"""Embedding and layer norm of token rows, and their gradients, against the 64-bit oracle.
+
+Tolerances, u = 2^-24.  A sum of n fp32 terms in any order is off by less than n u of their
+magnitudes' sum; a row's sum over its threads has at most 8 NV + 22 additions after one another
+(NV <= 4 vectors of 8 a thread, 6 across a wave, 16 waves): 64.  Rounding to a 16-bit type adds half a step.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_11660_amd as P
+from oracle import training as O
+from tests._util import host, say
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+K = 64
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+HALF = {F32: 0.0, BF16: 2.0 ** -8, F16: 2.0 ** -11}   # half a step of 8 and 11 significant bits, relative
+LEAST = {F32: 2.0 ** -149, BF16: 2.0 ** -133, F16: 2.0 ** -25}  # and of subnormal values
+
+
+def near(got, want, tol, dtype):
+    got = host(got.double()) if isinstance(got, torch.Tensor) else got
+    tol = tol + HALF[dtype] * (np.abs(want) + tol) + LEAST[dtype]
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], want[bad][:3], np.broadcast_to(tol, want.shape)[bad][:3])
+
+
+class Batch:
+    """Rows of n examples: slots, or packed with gaps; `shift` elements into wider rows."""
+
+    def __init__(self, n, T, packed, seed, ragged=True):
+        r = self.r = np.random.default_rng(seed)
+        self.n, self.T = n, T
+        self.length = r.integers(0, T + 1, n) if ragged else np.full(n, T)
+        if ragged:
+            self.length[0] = T
+            self.length[-1] = 0 if n > 1 else T
+        self.offset = None
+        self.rows = n * T
+        if packed:
+            order = r.permutation(n)   # examples in another order than their rows, a row between them
+            self.offset = np.zeros(n, np.int64)
+            at = 1
+            for i in order:
+                self.offset[i] = at
+                at += self.length[i] + 1
+            self.rows = at
+        self.slots = O.row_slots(n, T, self.rows, self.offset, self.length)
+
+    def c(self):
+        return P.ExampleRows(self.n, self.T, None if self.offset is None else torch.from_numpy(self.offset).cuda(),
+                             torch.from_numpy(self.length.astype(np.int32)).cuda())
+
+    def put(self, x, dtype, pad=0, shift=0):
+        """x's rows on the device, NaN in the padding rows and in `pad` columns behind each row."""
+        x = np.array(x, np.float64)
+        inside = np.zeros(len(x), bool)
+        inside[[row for _, row, ok in self.slots if ok]] = True
+        x[~inside] = np.nan
+        wide = torch.full((x.shape[0] * (x.shape[1] + pad) + shift,), float("nan"), dtype=dtype, device="cuda")
+        v = wide[shift:].view(x.shape[0], x.shape[1] + pad)[:, :x.shape[1]]
+        v.copy_(torch.from_numpy(x).cuda())
+        return v
+
+    def empty(self, d, dtype, pad=0, shift=0):
+        wide = torch.full((self.rows * (d + pad) + shift,), 77.0, dtype=dtype, device="cuda")
+        return wide[shift:].view(self.rows, d + pad)[:, :d], wide
+
+    def untouched(self, out, d, pad):
+        """Rows that are not written, and the columns behind each row."""
+        v, wide = out
+        shift = wide.numel() - self.rows * (d + pad)
+        whole = host(wide.float())[shift:].reshape(self.rows, d + pad)
+        assert (host(wide.float())[:shift] == 77).all() and (whole[:, d:] == 77).all()
+        written = {row for _, row, _ in self.slots}
+        rest = [i for i in range(self.rows) if i not in written]
+        assert (whole[rest] == 77).all()
+
+
+# ----------------------------------------------------------------------------
+# embedding
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("d", [1, 2, 63, 130, 512, 513, 769, 2048, 4100])
+@pytest.mark.parametrize("table,out", [(F32, BF16), (BF16, BF16), (F16, F32), (BF16, F16)])
+def test_embed(d, table, out):
+    for packed, scale, pad, shift in ((False, 1.0, 0, 0), (True, 1.7, 3, 1)):
+        say(f"case: embed d={d} {table}->{out} packed={packed}")
+        V = 37
+        B = Batch(5, 7, packed, d)
+        tab = torch.randn(V, d + pad, device="cuda").to(table)[:, :d]
+        token = B.r.integers(0, V, B.rows)
+        token[B.r.random(B.rows) < 0.2] = -1
+        token[B.slots[0][1]] = V
+        token[B.slots[1][1]] = 2 ** 40
+        o = B.empty(d, out, pad, shift)
+        P.attr_embed(tab, torch.from_numpy(token).cuda(), o[0], scale=scale, rows=B.c())
+        want = O.embed(host(tab.double()), token, scale, B.slots)
+        rows = sorted(want)
+        w = np.stack([want[i] for i in rows])
+        near(o[0][rows], w, 2 * U * np.abs(w), out)   # the scale's fp32 value, the product
+        B.untouched(o, d, pad)
+
+
+def test_embed_without_rows():
+    tab, token = torch.randn(11, 40, device="cuda"), torch.tensor([[3, 10], [0, 11]], device="cuda")
+    out = torch.full((2, 2, 40), 5.0, device="cuda")
+    P.attr_embed(tab, token, out)
+    assert torch.equal(out[0], tab[[3, 10]]) and torch.equal(out[1, 0], tab[0]) and (out[1, 1] == 0).all()
+
+
+def back_case(V, d, dout, table, B, token, accumulate, scale, pad=0, shift=0):
+    g = B.put(B.r.standard_normal((B.rows, d)), dout, pad, shift)
+    wide = torch.full((V * (d + pad) + shift,), 77.0, dtype=table, device="cuda")
+    dt = wide[shift:].view(V, d + pad)[:, :d]
+    was = np.zeros((V, d))
+    if accumulate:
+        dt.copy_(torch.from_numpy(B.r.standard_normal((V, d))).cuda())
+        was = host(dt.double())
+    tok = torch.from_numpy(token).cuda()
+    P.attr_embed_backward(g, tok, dt, scale=scale, accumulate=accumulate, rows=B.c())
+    want, size, count = O.embed_backward(host(g.double()), token, V, scale, B.slots)
+    tol = (count[:, None] + 3) * U * size + 2 * U * np.abs(was)
+    if accumulate:
+        assert np.array_equal(host(dt.double())[count == 0], was[count == 0])
+    near(dt, want + was, tol, table)
+    assert (wide[:shift] == 77).all()
+    if pad:
+        assert (wide[shift:].view(V, d + pad)[:, d:] == 77).all()
+    return dt
+
+
+@pytest.mark.parametrize("d", [1, 64, 65, 256, 257, 769, 1500])
+@pytest.mark.parametrize("dout,table", [(BF16, F32), (F32, F32), (F16, F16), (BF16, BF16)])
+def test_embed_backward(d, dout, table):
+    for V, n, T, packed, accumulate in ((1, 3, 9, False, False), (5, 9, 40, True, False), (300, 6, 50, False, True),
+                                        (2000, 7, 33, True, True)):
+        say(f"case: embed backward d={d} {dout}->{table} V={V} packed={packed} accumulate={accumulate}")
+        B = Batch(n, T, packed, d + V)
+        token = B.r.integers(-1, V + 1, B.rows)
+        back_case(V, d, dout, table, B, token, accumulate and table == F32, 1.0 if packed else 1.3, 3 if packed else 0,
+                  1 if packed else 0)
+
+
+@pytest.mark.parametrize("V", [1, 1023, 1024, 40000, 2 ** 20 + 5])
+def test_embed_backward_long(V):
+    """More tokens than one workgroup sorts: one token's rows past many parts, every digit's pass."""
+    d = 8
+    for n, T in ((1, 16384), (1, 16385), (7, 4099)):
+        say(f"case: embed backward long V={V} n={n} T={T}")
+        B = Batch(n, T, False, V, ragged=n > 1)
+        token = np.where(B.r.random(B.rows) < 0.4, V // 2, B.r.integers(0, V, B.rows))
+        first = back_case(V, d, F32, F32, B, token, False, 1.0)
+        B.r = np.random.default_rng(5)
+        a = back_case(V, d, F32, F32, B, token, False, 1.0).clone()
+        B.r = np.random.default_rng(5)
+        assert torch.equal(a, back_case(V, d, F32, F32, B, token, False, 1.0)) and first.shape == a.shape
+
+
+def test_embed_backward_order():
+    """A token's rows are added in the order of their slots: 1 + 2^-24 + 2^-24 is 1, the other way round 1 + 2^-23."""
+    for rows, want in (([1.0, U, U], 1.0), ([U, U, 1.0], 1.0 + 2 * U)):
+        token = torch.tensor([4, 2, 4, 1, 4], device="cuda")
+        g = torch.tensor([rows[0], 9.0, rows[1], 9.0, rows[2]], device="cuda")[:, None].repeat(1, 3)
+        dt = torch.empty(6, 3, device="cuda")
+        P.attr_embed_backward(g, token, dt)
+        assert (dt[4] == want).all() and (dt[[0, 3, 5]] == 0).all()
+
+
+def test_embed_backward_nothing():
+    dt = torch.full((9, 5), 3.0, device="cuda")
+    none, tok = torch.empty(0, 5, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")
+    P.attr_embed_backward(none, tok, dt, accumulate=True)
+    assert (dt == 3).all()
+    P.attr_embed_backward(none, tok, dt)
+    assert (dt == 0).all()
+    g, tok = torch.full((4, 5), float("nan"), device="cuda"), torch.tensor([0, 1, 2, 3], device="cuda")
+    dt.fill_(3)
+    P.attr_embed_backward(g, tok, dt, rows=P.ExampleRows(2, 2, length=torch.zeros(2, dtype=torch.int32, device="cuda")))
+    assert (dt == 0).all()
+    P.attr_embed_backward(g, torch.full((4,), 9, device="cuda"), dt.fill_(3), accumulate=True)
+    assert (dt == 3).all()
+
+
+# ----------------------------------------------------------------------------
+# layer norm
+# ----------------------------------------------------------------------------
+WIDTHS = [1, 2, 7, 8, 511, 512, 513, 769, 1024, 1500, 2048, 2056, 4096, 5000, 8192, 8199, 16384, 16400, 32768]
+
+
+def stat_tolerances(x, eps):
+    """How far the mean may be, and (relative) 1/std."""
+    size = np.abs(x).mean(1)
+    dm = (K + 1) * U * size
+    var = x.var(1)
+    off = (dm + U * size) ** 2  # the mean's error and the differences' rounding, squared
+    rel = ((K + 6) * U * var + off + 2 * np.sqrt(var) * U * size) / (var + eps)
+    return dm, rel / 2 + 4 * U
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+def test_layer_norm(d):
+    kinds = [(F32, F32, F32), (BF16, BF16, BF16), (F32, BF16, F32), (F16, F16, F32), (BF16, F32, F16), (F16, BF16, BF16)]
+    for j, (xt, yt, wt) in enumerate(kinds if d < 3000 else kinds[d % 3::3]):
+        packed, pad, shift = bool(j & 1), (0, 3)[j & 1], (0, 1)[j & 1]
+        say(f"case: layer norm d={d} {xt}->{yt} w={wt} packed={packed}")
+        B = Batch(4, 5, packed, d + j)
+        x = B.put(B.r.standard_normal((B.rows, d)) * np.exp(B.r.standard_normal((B.rows, 1))) + 2 * B.r.standard_normal((B.rows, 1)),
+                  xt, pad, shift)
+        w, b = (torch.from_numpy(B.r.standard_normal(d)).cuda().to(wt) for _ in range(2))
+        if j == 4:
+            b = None
+        if j == 5:
+            w = None
+        y = B.empty(d, yt, pad, shift)
+        mean, rstd = (torch.full((B.rows,), 77.0, device="cuda") for _ in range(2))
+        eps = 1e-5 if j < 3 else 1e-2
+        P.attr_layer_norm(x, y[0], w, b, eps, mean, rstd, rows=B.c())
+        inside = [row for _, row, ok in B.slots if ok]
+        pads = [row for _, row, ok in B.slots if not ok]
+        xs = host(x.double())[inside]
+        wn, bn = (1.0 if w is None else host(w.double())), (0.0 if b is None else host(b.double()))
+        got = [O.layer_norm(row, wn, bn, eps) for row in xs]
+        want, m, r = np.stack([g[0] for g in got]), np.array([g[1] for g in got]), np.array([g[2] for g in got])
+        dm, dr = stat_tolerances(xs, eps)
+        near(mean[inside], m, dm, F32)
+        near(rstd[inside], r, dr * r, F32)
+        unit = np.abs((xs - m[:, None]) * r[:, None])
+        tol = np.abs(wn) * (r[:, None] * (dm[:, None] + U * np.abs(xs)) + unit * (dr[:, None] + 4 * U)) + 2 * U * (np.abs(want) + np.abs(bn))
+        near(y[0][inside], want, tol, yt)
+        assert (y[0][pads] == 0).all() and (mean[pads] == 0).all() and (rstd[pads] == 0).all()
+        B.untouched(y, d, pad)
+
+
+def test_layer_norm_rows_at_their_edges():
+    """One value, equal values, large means, infinities and NaN: a row's own only; in place."""
+    d = 600
+    x = torch.randn(8, d, device="cuda")
+    x[1] = 3.0
+    x[2] += 1e4
+    x[3, 5], x[4, 7] = float("inf"), float("nan")
+    x[5] *= 1e25     # squares pass fp32's range
+    x[6] = 0
+    x[7] *= 1e-25
+    keep = x.clone()
+    mean, rstd = torch.empty(8, device="cuda"), torch.empty(8, device="cuda")
+    P.attr_layer_norm(x, x, eps=1e-5, mean=mean, rstd=rstd)
+    assert torch.isnan(x[3]).all() and torch.isnan(x[4]).all()
+    fine = [0, 2]
+    want = np.stack([O.layer_norm(host(keep[i].double()))[0] for i in fine])
+    size = np.array([np.abs(host(keep[i])).mean() for i in fine])[:, None]
+    near(x[fine], want, (K + 8) * U * (size / host(keep[fine].double()).std(1)[:, None] + np.abs(want)) * 2, F32)
+    assert (x[1] == 0).all() and (x[6] == 0).all() and (x[5] == 0).all() and (rstd[5] == 0).all()
+    assert torch.isfinite(x[7]).all() and abs(float(rstd[6]) - 1e-5 ** -0.5) < 1e-4 * 1e-5 ** -0.5
+    one = torch.tensor([[5.0], [-2.0]], device="cuda", dtype=BF16)
+    P.attr_layer_norm(one, one, bias=torch.ones(1, device="cuda"))
+    assert (one == 1).all()
+
+
+def backward_case(B, d, xt, yt, wt, per_example, accumulate, pad=0, shift=0, in_place=None, joined=False):
+    x = B.put(B.r.standard_normal((B.rows, d)) + B.r.standard_normal((B.rows, 1)), xt, pad, shift)
+    dy = B.put(B.r.standard_normal((B.rows, d)), yt, pad, shift)
+    w = None if wt is None else torch.from_numpy(1 + 0.3 * B.r.standard_normal(d)).cuda().to(wt)
+    inside = [(i, row) for i, row, ok in B.slots if ok]
+    rows = [row for _, row in inside]
+    xs, ds = host(x.double()), host(dy.double())
+    mean, rstd = (torch.full((B.rows,), float("nan"), device="cuda") for _ in range(2))
+    if rows:
+        mean[rows] = torch.from_numpy(xs[rows].mean(1)).float().cuda()
+        rstd[rows] = torch.from_numpy(1 / np.sqrt(xs[rows].var(1) + 1e-5)).float().cuda()
+    units = B.n if per_example else 1
+    grads = torch.full((units, 2 * d + 5), 0.5 if accumulate else 77.0, device="cuda")
+    if joined:
+        dw, db = grads[:, 2:2 + d], grads[:, 3 + d:3 + 2 * d]
+    else:
+        dw, db = (torch.full((units, d), 0.5 if accumulate else 77.0, device="cuda") for _ in range(2))
+    dx = B.empty(d, xt, pad, shift)
+    out = {None: dx[0], "x": x, "dy": dy}[in_place]
+    P.attr_layer_norm_backward(dy, x, mean, rstd, w, out, dw if per_example else dw[0], db if per_example else db[0],
+                               per_example=per_example, accumulate=accumulate, rows=B.c())
+    m, r, wn = host(mean.double()), host(rstd.double()), 1.0 if w is None else host(w.double())
+    sums = np.zeros((4, units, d))
+    for i, row in inside:
+        want, tw, tb = O.layer_norm_backward(ds[row], xs[row], m[row], r[row], wn)
+        j = i if per_example else 0
+        sums[:, j] += tw, tb, np.abs(tw), np.abs(tb)
+        unit, e = np.abs((xs[row] - m[row]) * r[row]), np.abs(ds[row] * wn)
+        tol = r[row] * ((K + 4) * U * e.mean() + 4 * U * e + unit * ((K + 10) * U * (e * unit).mean()))
+        near(out[row], want, tol, xt)
+    n = max(1, len(rows)) + 6
+    base = 0.5 if accumulate else 0.0
+    near(dw, sums[0] + base, n * U * sums[2] + U, F32)
+    near(db, sums[1] + base, n * U * sums[3] + U, F32)
+    if in_place is None:
+        B.untouched(dx, d, pad)
+        pads = [row for _, row, ok in B.slots if not ok]
+        assert (dx[0][pads] == 0).all()
+    if joined:
+        rest = torch.cat([grads[:, :2], grads[:, 2 + d:3 + d], grads[:, 3 + 2 * d:]], 1)
+        assert (rest == (0.5 if accumulate else 77)).all()
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+def test_layer_norm_backward(d):
+    kinds = [(F32, F32, F32), (BF16, BF16, BF16), (F32, BF16, F32), (F16, F16, None), (BF16, F32, F16)]
+    for j, (xt, yt, wt) in enumerate(kinds if d < 3000 else kinds[d % 2::2]):
+        say(f"case: layer norm backward d={d} x={xt} dy={yt} w={wt}")
+        backward_case(Batch(4, 5, bool(j & 1), d + j), d, xt, yt, wt, j % 3 == 1, j > 2, (0, 3)[j & 1], (0, 1)[j & 1])
+
+
+@pytest.mark.parametrize("d", [40, 769, 2304])
+def test_layer_norm_backward_many_rows(d):
+    """Many chunks, joined; examples of one and of many chunks; gradients that are columns of wider rows."""
+    for n, T, packed, per_example in ((3, 300, False, True), (40, 3, True, True), (1, 999, False, False), (6, 170, True, False)):
+        say(f"case: layer norm backward d={d} n={n} T={T} per_example={per_example}")
+        backward_case(Batch(n, T, packed, d + n), d, F32, F32, F32, per_example, n == 3, joined=per_example)
+
+
+@pytest.mark.parametrize("d", [100, 3000, 20000])
+def test_layer_norm_backward_in_place(d):
+    for where in ("x", "dy"):
+        backward_case(Batch(3, 4, where == "x", d), d, BF16, BF16, F32, False, False, in_place=where)
+
+
+def test_layer_norm_backward_parts():
+    """Each of its outputs alone gives the same bits."""
+    d, n = 300, 50
+    x, dy = torch.randn(n, d, device="cuda"), torch.randn(n, d, device="cuda")
+    mean, rstd = x.mean(1), 1 / (x.var(1, correction=0) + 1e-5).sqrt()
+    new = lambda: (torch.empty_like(x), torch.empty(d, device="cuda"), torch.empty(d, device="cuda"))  # noqa: E731
+    dx, dw, db = new()
+    P.attr_layer_norm_backward(dy, x, mean, rstd, None, dx, dw, db)
+    for keep in range(8):
+        got = new()
+        give = [t if keep >> k & 1 else None for k, t in enumerate(got)]
+        P.attr_layer_norm_backward(dy, x, mean, rstd, None, *give)
+        for k, (a, b) in enumerate(zip(got, (dx, dw, db))):
+            assert not keep >> k & 1 or torch.equal(a, b)
+
+
+def test_layer_norm_backward_nothing():
+    e = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
+    dw, db = torch.full((7,), 3.0, device="cuda"), torch.full((7,), 3.0, device="cuda")
+    P.attr_layer_norm_backward(e(0, 7), e(0, 7), e(0), e(0), None, e(0, 7), dw, db, accumulate=True)
+    assert (dw == 3).all() and (db == 3).all()
+    P.attr_layer_norm_backward(e(0, 7), e(0, 7), e(0), e(0), None, e(0, 7), dw, db)
+    assert (dw == 0).all() and (db == 0).all()
+    dw = torch.full((2, 7), 3.0, device="cuda")
+    x = torch.full((4, 7), float("nan"), device="cuda")
+    P.attr_layer_norm_backward(x, x.clone(), x[:, 0].contiguous(), x[:, 0].contiguous(), None, None, dw, per_example=True,
+                               rows=P.ExampleRows(2, 2, length=torch.tensor([-3, 0], dtype=torch.int32, device="cuda")))
+    assert (dw == 0).all()
+
+
+def test_gradient_against_differences():
+    """The kernels' own differences in fp32: a step h moves <y, c> by h <dx, v>."""
+    torch.manual_seed(3)
+    n, d, h = 6, 96, 1e-2
+    x, c, v = (torch.randn(n, d, device="cuda") for _ in range(3))
+    w, b, vw, vb = (torch.randn(d, device="cuda") for _ in range(4))
+
+    def f(t):
+        y = torch.empty_like(x)
+        P.attr_layer_norm(x + t * v, y, w + t * vw, b + t * vb)
+        return float((y.double() * c).sum())
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    P.attr_layer_norm(x, y, w, b, mean=mean, rstd=rstd)
+    dx, dw, db = torch.empty_like(x), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    P.attr_layer_norm_backward(c, x, mean, rstd, w, dx, dw, db)
+    want = float((dx.double() * v).sum() + (dw.double() * vw).sum() + (db.double() * vb).sum())
+    got = (8 * (f(h) - f(-h)) - (f(2 * h) - f(-2 * h))) / (12 * h)   # to fourth order
+    # fp32 values of |y c| ~ 1, 600 of them, over 2 h: 600^(1/2) 2^-23 / h ~ 3e-4; the fifth derivative times h^4: 1e-6
+    assert abs(got - want) < 2e-3 * max(1.0, abs(want)), (got, want)
+
+
+def test_offsets_past_32_bits():
+    """Rows whose elements lie past 2^32 bytes and 2^31 elements from the first."""
+    d, far = 512, 2 ** 31 // 512 + 3
+    x = torch.zeros(far + 2, d, dtype=BF16, device="cuda")
+    x[far:] = torch.randn(2, d, device="cuda").to(BF16)
+    B = P.ExampleRows(1, 2, torch.tensor([far], device="cuda"), torch.tensor([2], dtype=torch.int32, device="cuda"))
+    y = torch.zeros(far + 2, d, dtype=BF16, device="cuda")
+    mean, rstd = torch.zeros(far + 2, device="cuda"), torch.zeros(far + 2, device="cuda")
+    P.attr_layer_norm(x, y, mean=mean, rstd=rstd, rows=B)
+    want = np.stack([O.layer_norm(r)[0] for r in host(x[far:].double())])
+    near(y[far:], want, 200 * U * np.ones_like(want), BF16)
+    assert (y[:far] == 0).all()
+    dx = torch.zeros_like(x)
+    P.attr_layer_norm_backward(y, x, mean, rstd, None, dx, rows=B)
+    assert (dx[:far] == 0).all() and torch.isfinite(dx[far:]).all() and (dx[far:] != 0).any()
+    del dx
+    token = torch.zeros(far + 2, dtype=torch.int64, device="cuda")
+    token[far + 1] = far
+    P.attr_embed(x, token, y.zero_(), rows=B)
+    assert torch.equal(y[far + 1], x[far]) and (y[:far + 1] == 0).all()
+    dt = x.zero_()
+    P.attr_embed_backward(y, token, dt, rows=B)
+    assert torch.equal(dt[far], y[far + 1]) and (dt[:far] == 0).all()
+
+
+def test_rows_outside_the_tensors():
+    """Offsets before the first row and past the last: those rows are neither read nor written."""
+    d, n_rows = 24, 10
+    x = torch.randn(n_rows, d, device="cuda")
+    B = P.ExampleRows(4, 4, torch.tensor([-2, 8, 2 ** 62, -2 ** 63], device="cuda"))
+    y = torch.full_like(x, 7.0)
+    mean, rstd = torch.full((n_rows,), 7.0, device="cuda"), torch.full((n_rows,), 7.0, device="cuda")
+    P.attr_layer_norm(x, y, mean=mean, rstd=rstd, rows=B)
+    assert (y[2:8] == 7).all() and (y[:2] != 7).all() and (y[8:] != 7).all()
+    dx, dw = torch.full_like(x, 7.0), torch.empty(4, d, device="cuda")
+    P.attr_layer_norm_backward(x, x.clone(), mean, rstd, None, dx, dw, per_example=True, rows=B)
+    assert (dx[2:8] == 7).all() and (dx[:2] != 7).all() and (dw[2:] == 0).all() and (dw[:2] != 0).any(1).all()
+    dt = torch.empty(3, d, device="cuda")
+    P.attr_embed_backward(x, torch.ones(n_rows, dtype=torch.int64, device="cuda"), dt, rows=B)
+    assert torch.allclose(dt[1], x[[0, 1, 8, 9]].sum(0), atol=1e-5) and (dt[[0, 2]] == 0).all()
+
+
+def test_types_that_are_not_taken():
+    x = torch.zeros(4, 8, dtype=torch.float64, device="cuda")
+    with pytest.raises(TypeError, match="float64"):
+        P.attr_layer_norm(x, x.float())
+    with pytest.raises(TypeError, match="float64"):
+        P.attr_embed(x, torch.zeros(2, dtype=torch.int64, device="cuda"), x[:2].float())
+
+
+def test_captured_and_on_another_stream():
+    """Replays with eager work between them, two graphs on one workspace, another stream."""
+    d, n, V = 700, 300, 50
+    torch.manual_seed(1)
+    x, dy = torch.randn(n, d, device="cuda"), torch.randn(n, d, device="cuda")
+    token = torch.randint(0, V, (n,), device="cuda")
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    y, dx, dw, db = torch.empty_like(x), torch.empty_like(x), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    dt, out = torch.empty(V, d, device="cuda"), torch.empty(n, d, device="cuda")
+    side, ws = torch.cuda.Stream(), P.Workspace()
+
+    def norm():
+        P.attr_layer_norm(x, y, mean=mean, rstd=rstd)
+        P.attr_layer_norm_backward(dy, x, mean, rstd, None, dx, dw, db, ws=ws)
+
+    def emb():
+        P.attr_embed(dt, token, out)
+        P.attr_embed_backward(dy, token, dt, ws=ws)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        norm(), emb()
+    side.synchronize()
+    graphs = []
+    for f in (norm, emb):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            f()
+        graphs.append(g)
+    for k in range(4):
+        x.normal_(), dy.normal_()
+        token.random_(0, V)
+        dt.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, dx, dw, db, dt)]
+        norm(), emb()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (y, dx, dw, db, dt)):
+            assert torch.equal(a, b), k
