@@ -1374,14 +1374,16 @@ struct EmbedLayout {
 };
 EmbedLayout embed_layout(const attr_rows* r, int64_t V, int64_t d) {
   EmbedLayout L;
+  std::memset(&L, 0, sizeof(L));
   const size_t n = (size_t)(r->n_examples * r->T), each = align_up(4 * n);
+  if (n <= attr::kEmbedSmall) return L;
   L.key[0] = 0;
   L.key[1] = each;
   L.row[0] = 2 * each;
   L.row[1] = 3 * each;
   L.count = 4 * each;
   const size_t blocks = (n + attr::kSortKeys - 1) / attr::kSortKeys;
-  L.part = L.count + (n > attr::kSortOneMost ? align_up((blocks << attr::sort_bits(V)) * 4) : 0);
+  L.part = L.count + (blocks > 1 ? align_up((blocks << attr::sort_bits(V)) * 4) : 0);
   const size_t parts = (n + attr::kEmbedPart - 1) / attr::kEmbedPart;
   L.total = L.part + align_up(parts * 2 * (size_t)d * 4);
   return L;
@@ -1458,13 +1460,17 @@ attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, con
     a.d = (int32_t)d;
     a.accumulate = accumulate;
     a.scale = scale;
+    const attr::RowsArgs r = rows_args(rows);
+    if (!none && r.n_slots <= attr::kEmbedSmall) {
+      const hipError_t e = attr::launch_embed_small((int)dout_dtype, (int)dtable_dtype, r, token, a, s);
+      return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_embed_backward launch");
+    }
     if (!none) {
       const EmbedLayout L = embed_layout(rows, V, d);
       if (!ws || ws_bytes < L.total)
         return fail(ATTR_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", who, L.total, ws ? ws_bytes : (size_t)0);
       if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ATTR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
       char* const base = static_cast<char*>(ws);
-      const attr::RowsArgs r = rows_args(rows);
       attr::EmbedSort e;
       for (int k = 0; k < 2; ++k) {
         e.key[k] = reinterpret_cast<uint32_t*>(base + L.key[k]);
@@ -1512,12 +1518,11 @@ bool columns_apart(const float* p, const float* q, int64_t d, int64_t ld) {
   return c >= d && c + d <= ld;
 }
 
-// (unit, units, chunk, chunks) of a gradient call.
+// (unit, units, chunks) of a gradient call.
 void norm_split(const attr_rows* r, int64_t d, int32_t per_example, attr::NormGradArgs& a) {
   a.unit = (uint32_t)(per_example ? r->T : r->n_examples * r->T);
   a.units = (uint32_t)(per_example ? r->n_examples : 1);
-  a.chunk = attr::norm_chunk(a.unit, a.units, (int32_t)d);
-  a.chunks = (a.unit + a.chunk - 1) / a.chunk;
+  a.chunks = attr::norm_chunks(a.unit, a.units, (int32_t)d);
 }
 size_t norm_bytes(const attr::NormGradArgs& a, int64_t d) {
   return a.chunks > 1 ? align_up((size_t)a.units * a.chunks * 2 * (size_t)d * 4) : 0;
@@ -1628,7 +1633,7 @@ attr_status attr_layer_norm_backward(const attr_rows* rows, const void* dy, attr
     a.accumulate = accumulate;
     attr::RowsArgs r = rows_args(rows);
     if (none) {  // sums of no rows: one empty unit, or one for each example
-      a.unit = a.chunk = a.chunks = 1;
+      a.unit = a.chunks = 1;
       a.units = (uint32_t)units;
       r = attr::RowsArgs{nullptr, nullptr, 0, (uint32_t)units, 1};
     } else {

@@ -20,18 +20,18 @@ __device__ inline void embed_row(const RowsArgs& r, const EmbedArgs& a, uint32_t
   O* const out = (O*)a.out + s.row * a.ldo;
   constexpr int U = 4;
   const int c0 = (int)(cut * U * 64 + (threadIdx.x & 63)) * N;
-  float x[U][N];
+  Raw<T, N> in[U];
+  if (there) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int c = c0 + u * 64 * N;
-    load_n<T, N>(from + c, there ? a.d - c : 0, x[u]);
+    for (int u = 0; u < U; ++u) in[u].load(from + Cols<N>(c0 + u * 64 * N, a.d).at);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int c = c0 + u * 64 * N;
+    float x[N];
+    in[u].get(x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[u][e] = there ? x[u][e] * a.scale : 0.f;
-    store_n<O, N>(out + c, a.d - c, x[u]);
+    for (int e = 0; e < N; ++e) x[e] = there ? x[e] * a.scale : 0.f;
+    store_n<O, N>(out, Cols<N>(c0 + u * 64 * N, a.d), x);
   }
 }
 template <typename T, typename O, int N>
@@ -47,14 +47,30 @@ __global__ __launch_bounds__(256) void embed_kernel(RowsArgs r, EmbedArgs a, uin
 struct Pair {
   uint32_t key, row;
 };
-__device__ inline Pair first_pair(const RowsArgs& r, const int64_t* token, int64_t V, uint32_t slot) {
-  const RowSlot s = row_slot(r, slot);
-  const int64_t v = s.inside ? token[s.row] : -1;
-  return {v >= 0 && v < V ? (uint32_t)v : (uint32_t)V, (uint32_t)s.row};
+
+// A lane's pairs of a wave's share: K rounds from `from` on, all loads in flight.
+template <int K>
+__device__ inline void load_pairs(const uint32_t* key, const uint32_t* row, uint32_t from, uint32_t to, Pair (&p)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const uint32_t i = from + k * 64 + (threadIdx.x & 63), j = i < to ? i : from;
+    p[k] = {key[j], row[j]};
+  }
 }
-__device__ inline Pair pair_of(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, int pass, uint32_t i) {
-  if (pass == 0) return first_pair(r, token, V, i);
-  return {e.key[pass & 1][i], e.row[pass & 1][i]};
+// The same of the batch itself: tokens outside [0, V) and slots that are not inside have the key V.
+template <int K>
+__device__ inline void load_tokens(const RowsArgs& r, const int64_t* token, int64_t V, uint32_t from, uint32_t to, Pair (&p)[K]) {
+  RowSlot s[K];
+  int64_t v[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const uint32_t i = from + k * 64 + (threadIdx.x & 63);
+    s[k] = row_slot(r, i < to ? i : from);
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = s[k].inside ? token[s[k].row] : -1;
+#pragma unroll
+  for (int k = 0; k < K; ++k) p[k] = {v[k] >= 0 && v[k] < V ? (uint32_t)v[k] : (uint32_t)V, (uint32_t)s[k].row};
 }
 
 // Where each of a wave's lanes puts its pair: base[digit] and the lanes before it with the
@@ -101,69 +117,112 @@ __device__ inline uint32_t block_before(uint32_t v, uint32_t* sm, uint32_t& tota
 
 constexpr int kBinsMost = 1 << kSortBits;
 
-// Every pass of a short batch in one workgroup; a wave takes a contiguous share of the pairs.
+// Adds a wave's pairs to the counts of their digits; then, the counts turned into first places,
+// puts the pairs there.
+template <int K>
+__device__ inline void count_pairs(uint32_t* count, const Pair (&p)[K], uint32_t from, uint32_t to, int shift, uint32_t bins) {
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (from + k * 64 + (threadIdx.x & 63) < to) atomicAdd(&count[(p[k].key >> shift) & (bins - 1)], 1u);
+}
+template <int K>
+__device__ inline void place_pairs(uint32_t* base, const EmbedSort& e, int pass, const Pair (&p)[K], uint32_t from, uint32_t to) {
+  uint32_t* const key = e.key[(pass + 1) & 1];
+  uint32_t* const row = e.row[(pass + 1) & 1];
+  const uint32_t bins = 1u << e.bits;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (from + k * 64 >= to) break;
+    const bool live = from + k * 64 + (threadIdx.x & 63) < to;
+    const uint32_t at = place(base, (p[k].key >> (pass * e.bits)) & (bins - 1), e.bits, live);
+    if (live) {
+      key[at] = p[k].key;
+      row[at] = p[k].row;
+    }
+  }
+}
+// Counts of 16 waves to the first places of their pairs, over a workgroup's digits.
+__device__ inline void wave_places(uint32_t (&base)[16][kBinsMost], uint32_t bin, uint32_t at) {
+  for (int w = 0; w < 16; ++w) {
+    const uint32_t c = base[w][bin];
+    base[w][bin] = at;
+    at += c;
+  }
+}
+// A wave's share of a workgroup's kSortKeys pairs.
+constexpr int kSortRounds = kSortKeys / 1024;
+struct Share {
+  uint32_t from, to;
+  __device__ inline Share(uint32_t n, uint32_t wave, uint32_t each) {
+    const uint32_t first = blockIdx.x * kSortKeys + wave * each;
+    from = first < n ? first : n;
+    to = n - from < each ? n : from + each;
+  }
+};
+
+// Every pass of a short batch (up to 1024 K pairs) in one workgroup.
+template <int K>
 __global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e) {
   __shared__ uint32_t base[16][kBinsMost];
   __shared__ uint32_t sm[16];
   const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
-  const uint32_t n = r.n_slots, share = ((n + 1023) / 1024) * 64;
-  const uint32_t from = wave * share, to = from + share < n ? from + share : n;
+  const Share w(r.n_slots, wave, ((r.n_slots + 1023) / 1024) * 64);
   const uint32_t bins = 1u << e.bits;
   for (int pass = 0; pass < e.passes; ++pass) {
-    const int shift = pass * e.bits;
+    Pair p[K];
+    if (w.from < w.to) {
+      if (pass == 0) load_tokens<K>(r, token, V, w.from, w.to, p);
+      else load_pairs<K>(e.key[pass & 1], e.row[pass & 1], w.from, w.to, p);
+    }
     for (uint32_t b = lane; b < bins; b += 64) base[wave][b] = 0;
     __syncthreads();
-    for (uint32_t i = from + lane; i < to; i += 64) {
-      const Pair p = pair_of(r, token, V, e, pass, i);
-      atomicAdd(&base[wave][(p.key >> shift) & (bins - 1)], 1u);
-    }
+    count_pairs<K>(base[wave], p, w.from, w.to, pass * e.bits, bins);
     __syncthreads();
-    // counts to first places: over the bins, and over a bin's waves
     uint32_t mine = 0, total;
     const uint32_t b = threadIdx.x;
     if (b < bins)
-      for (int w = 0; w < 16; ++w) mine += base[w][b];
-    uint32_t at = block_before<16>(mine, sm, total);
-    if (b < bins)
-      for (int w = 0; w < 16; ++w) {
-        const uint32_t c = base[w][b];
-        base[w][b] = at;
-        at += c;
-      }
+      for (int k = 0; k < 16; ++k) mine += base[k][b];
+    const uint32_t at = block_before<16>(mine, sm, total);
+    if (b < bins) wave_places(base, b, at);
     __syncthreads();
-    uint32_t* const key = e.key[(pass + 1) & 1];
-    uint32_t* const row = e.row[(pass + 1) & 1];
-    for (uint32_t i0 = from; i0 < to; i0 += 64) {
-      const bool live = i0 + lane < to;
-      Pair p{0, 0};
-      if (live) p = pair_of(r, token, V, e, pass, i0 + lane);
-      const uint32_t at = place(base[wave], (p.key >> shift) & (bins - 1), e.bits, live);
-      if (live) {
-        key[at] = p.key;
-        row[at] = p.row;
-      }
-    }
+    place_pairs<K>(base[wave], e, pass, p, w.from, w.to);
     __threadfence_block();
     __syncthreads();
   }
 }
 
-// Long batches: each workgroup counts its pairs' digits, one adds the counts up, and each
-// puts its pairs in their places.
-__global__ __launch_bounds__(256) void embed_count_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, int pass) {
+// Longer ones, pass by pass: each workgroup counts its pairs' digits (the first pass leaves the
+// pairs themselves behind), the counts are added up, and each workgroup puts its pairs in their places.
+template <bool FIRST>
+__global__ __launch_bounds__(1024) void embed_count_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, int pass) {
   __shared__ uint32_t count[kBinsMost];
   const uint32_t bins = 1u << e.bits;
-  for (uint32_t b = threadIdx.x; b < bins; b += 256) count[b] = 0;
+  for (uint32_t b = threadIdx.x; b < bins; b += 1024) count[b] = 0;
+  const Share w(r.n_slots, wave_uniform(threadIdx.x >> 6), kSortKeys / 16);
+  Pair p[kSortRounds];
+  if (w.from < w.to) {
+    if (FIRST) load_tokens<kSortRounds>(r, token, V, w.from, w.to, p);
+    else load_pairs<kSortRounds>(e.key[pass & 1], e.row[pass & 1], w.from, w.to, p);
+  }
   __syncthreads();
-  const uint32_t from = blockIdx.x * kSortKeys, to = r.n_slots - from < kSortKeys ? r.n_slots : from + kSortKeys;
-  for (uint32_t i = from + threadIdx.x; i < to; i += 256)
-    atomicAdd(&count[(pair_of(r, token, V, e, pass, i).key >> (pass * e.bits)) & (bins - 1)], 1u);
+  count_pairs<kSortRounds>(count, p, w.from, w.to, pass * e.bits, bins);
+  if (FIRST) {
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+      const uint32_t i = w.from + k * 64 + (threadIdx.x & 63);
+      if (i < w.to) {
+        e.key[0][i] = p[k].key;
+        e.row[0][i] = p[k].row;
+      }
+    }
+  }
   __syncthreads();
-  for (uint32_t b = threadIdx.x; b < bins; b += 256) e.count[(uint64_t)b * e.blocks + blockIdx.x] = count[b];
+  for (uint32_t b = threadIdx.x; b < bins; b += 1024) e.count[(uint64_t)b * e.blocks + blockIdx.x] = count[b];
 }
+// Counts of many workgroups to first places, by one.
 __global__ __launch_bounds__(1024) void embed_scan_kernel(EmbedSort e) {
   __shared__ uint32_t sm[16];
-  const uint32_t n = (1u << e.bits) * e.blocks;
+  const uint32_t n = e.blocks << e.bits;
   uint32_t run = 0;
   for (uint32_t i0 = 0; i0 < n; i0 += 4096) {
     uint32_t c[4], sum = 0, total;
@@ -182,133 +241,174 @@ __global__ __launch_bounds__(1024) void embed_scan_kernel(EmbedSort e) {
     run += total;
   }
 }
-__global__ __launch_bounds__(256) void embed_place_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, int pass) {
-  __shared__ uint32_t base[4][kBinsMost];
-  const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6), shift = pass * e.bits;
-  const uint32_t bins = 1u << e.bits;
-  const uint32_t end = r.n_slots, first = blockIdx.x * kSortKeys + wave * (kSortKeys / 4);
-  const uint32_t from = first < end ? first : end, to = end - from < kSortKeys / 4 ? end : from + kSortKeys / 4;
-  for (uint32_t b = lane; b < bins; b += 64) base[wave][b] = 0;
-  __syncthreads();
-  for (uint32_t i = from + lane; i < to; i += 64)
-    atomicAdd(&base[wave][(pair_of(r, token, V, e, pass, i).key >> shift) & (bins - 1)], 1u);
-  __syncthreads();
-  for (uint32_t b = threadIdx.x; b < bins; b += 256) {
-    uint32_t at = e.count[(uint64_t)b * e.blocks + blockIdx.x];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t c = base[w][b];
-      base[w][b] = at;
-      at += c;
-    }
+// SCAN: the counts are those of few workgroups, and each adds them up by itself.
+template <bool SCAN>
+__global__ __launch_bounds__(1024) void embed_place_kernel(EmbedSort e, uint32_t n, int pass) {
+  __shared__ uint32_t base[16][kBinsMost];
+  __shared__ uint32_t sm[16];
+  const int lane = threadIdx.x & 63;
+  const uint32_t wave = wave_uniform(threadIdx.x >> 6), bins = 1u << e.bits, b = threadIdx.x;
+  const Share w(n, wave, kSortKeys / 16);
+  Pair p[kSortRounds];
+  if (w.from < w.to) load_pairs<kSortRounds>(e.key[pass & 1], e.row[pass & 1], w.from, w.to, p);
+  uint32_t at = 0;
+  if (SCAN) {
+    uint32_t mine = 0, before = 0, total;
+    if (b < bins)
+      for (uint32_t k = 0; k < e.blocks; ++k) {
+        const uint32_t c = e.count[(uint64_t)b * e.blocks + k];
+        mine += c;
+        if (k < blockIdx.x) before += c;
+      }
+    at = block_before<16>(mine, sm, total) + before;
+  } else if (b < bins) {
+    at = e.count[(uint64_t)b * e.blocks + blockIdx.x];
   }
+  for (uint32_t k = lane; k < bins; k += 64) base[wave][k] = 0;
   __syncthreads();
-  uint32_t* const key = e.key[(pass + 1) & 1];
-  uint32_t* const row = e.row[(pass + 1) & 1];
-  for (uint32_t i0 = from; i0 < to; i0 += 64) {
-    const bool live = i0 + lane < to;
-    Pair p{0, 0};
-    if (live) p = pair_of(r, token, V, e, pass, i0 + lane);
-    const uint32_t at = place(base[wave], (p.key >> shift) & (bins - 1), e.bits, live);
-    if (live) {
-      key[at] = p.key;
-      row[at] = p.row;
-    }
-  }
+  count_pairs<kSortRounds>(base[wave], p, w.from, w.to, pass * e.bits, bins);
+  __syncthreads();
+  if (b < bins) wave_places(base, b, at);
+  __syncthreads();
+  place_pairs<kSortRounds>(base[wave], e, pass, p, w.from, w.to);
 }
 
 // ----------------------------------------------------------------------------
 // sums of a token's rows
 // ----------------------------------------------------------------------------
-// First of the sorted keys that is not below (or, ABOVE, that is above) `key`.
-template <bool ABOVE>
-__device__ inline uint32_t bound_of(const uint32_t* keys, uint32_t n, uint32_t key) {
+// The first place of the sorted keys whose key is above `key`.
+__device__ inline uint32_t end_of(const uint32_t* keys, uint32_t n, uint32_t key) {
   uint32_t lo = 0, hi = n;
   while (lo < hi) {
     const uint32_t mid = (lo + hi) >> 1;
-    if (ABOVE ? keys[mid] <= key : keys[mid] < key) lo = mid + 1;
+    if (keys[mid] <= key) lo = mid + 1;
     else hi = mid;
   }
   return lo;
 }
 
 template <typename T, int N>
-__device__ inline void put_sum(const EmbedGradArgs& a, uint32_t v, int c, float (&sum)[N]) {
-  T* const out = (T*)a.dtable + (int64_t)v * a.ldt + c;
+__device__ inline void put_sum(const EmbedGradArgs& a, uint32_t v, Cols<N> c, float (&sum)[N]) {
+  T* const out = (T*)a.dtable + (int64_t)v * a.ldt;
   if (a.accumulate) {
     float was[N];
-    load_n<T, N>(out, a.d - c, was);
+    load_n<T, N>(out, c, was);
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = sum[e] * a.scale + was[e];
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] *= a.scale;
   }
-  store_n<T, N>(out, a.d - c, sum);
+  store_n<T, N>(out, c, sum);
+}
+
+// Zeros from p on, by one wave: whole 16-byte pieces, elements before and behind them.
+template <typename T>
+__device__ inline void zero_span(T* p, int64_t n) {
+  const int lane = threadIdx.x & 63;
+  int64_t head = (int64_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int64_t)sizeof(T);
+  head = head < n ? head : n;
+  constexpr int E = 16 / sizeof(T);
+  if (lane < head) p[lane] = (T)0;
+  i32x4* const q = reinterpret_cast<i32x4*>(p + head);
+  const int64_t whole = (n - head) / E;
+#pragma unroll 4
+  for (int64_t k = lane; k < whole; k += 64) q[k] = i32x4{0, 0, 0, 0};
+  if (head + whole * E + lane < n) p[head + whole * E + lane] = (T)0;
+}
+
+constexpr uint32_t kZeroRows = 16;
+// The rows v0 + k whose bits are set; neighbouring rows of a table without gaps are one span.
+template <typename T>
+__device__ inline void zero_rows(const EmbedGradArgs& a, int64_t v0, uint64_t rows) {
+  while (rows) {
+    const int k = __builtin_ctzll(rows), run = a.ldt == a.d ? __builtin_ctzll(~(rows >> k)) : 1;
+    zero_span((T*)a.dtable + (v0 + k) * a.ldt, (int64_t)run * a.d);
+    rows &= ~(((1ull << run) - 1) << k);
+  }
+}
+// Which of v0 .. v0 + kZeroRows - 1 (those below V) the sorted keys do not hold, by one wave: each
+// step of its searches looks at 64 places.
+__device__ inline uint64_t absent_of(const uint32_t* keys, uint32_t n, int64_t v0, int64_t V) {
+  const uint32_t lane = threadIdx.x & 63, first = (uint32_t)v0;
+  uint64_t absent = V - v0 < (int64_t)kZeroRows ? (1ull << (V - v0)) - 1 : (1ull << kZeroRows) - 1;
+  uint32_t lo = 0, hi = n, key = first;  // the first place in [lo, hi] with a key not below `key`
+  for (;;) {
+    while (hi - lo > 64) {
+      const uint32_t step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step - 1;
+      const uint32_t below = (uint32_t)__popcll(__ballot(at < hi && keys[at] < key));
+      lo += below * step;
+      hi = hi - lo < step ? hi : lo + step;
+    }
+    lo += (uint32_t)__popcll(__ballot(lo + lane < hi && keys[lo + lane] < key));
+    if (lo >= n) return absent;
+    const uint32_t mine = lo + lane < n ? keys[lo + lane] : (uint32_t)V;
+    for (uint32_t k = 0; k < kZeroRows; ++k)
+      if (__ballot(mine == first + k)) absent &= ~(1ull << k);
+    const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)mine, 63);
+    if (last >= first + kZeroRows - 1 || lo + 64 >= n) return absent;
+    key = last + 1;
+    lo += 64;
+    hi = n;
+  }
 }
 
 // A wave takes 64 N columns of a part of the sorted pairs, or zeroes rows of tokens that the
 // batch does not hold.
-constexpr uint32_t kZeroRows = 16;
 template <typename G, typename T, int N>
 __device__ inline void embed_sum(const EmbedGradArgs& a, uint32_t parts, uint32_t cuts, uint64_t unit) {
   const int lane = threadIdx.x & 63;
   if (unit >= (uint64_t)parts * cuts) {
     const int64_t v0 = (int64_t)(unit - (uint64_t)parts * cuts) * kZeroRows;
-    bool absent = false;
-    if (lane < (int)kZeroRows && v0 + lane < a.V) {
-      const uint32_t v = (uint32_t)(v0 + lane), at = bound_of<false>(a.key, a.n, v);
-      absent = at == a.n || a.key[at] != v;
-    }
-    const uint64_t rows = __ballot(absent);
-    const float zero[N] = {};
-    for (uint32_t k = 0; k < kZeroRows; ++k) {
-      if (!((rows >> k) & 1)) continue;
-      T* const out = (T*)a.dtable + (v0 + k) * a.ldt;
-      for (int c = lane * N; c < a.d; c += 64 * N) store_n<T, N>(out + c, a.d - c, zero);
-    }
+    zero_rows<T>(a, v0, absent_of(a.key, a.n, v0, a.V));
     return;
   }
   const uint32_t part = (uint32_t)(unit / cuts), cut = (uint32_t)(unit % cuts);
-  const int c = (int)(cut * 64 + lane) * N;
+  const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
   const uint32_t from = part * kEmbedPart, to = a.n - from < kEmbedPart ? a.n : from + kEmbedPart;
   const uint32_t V = (uint32_t)a.V;
-  const int n = a.d - c > 0 ? a.d - c : 0;
   float sum[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) sum[e] = 0.f;
-  uint32_t cur = wave_uniform(a.key[from]);
+  // the part's pairs, and the keys on both sides of it, in the wave's lanes
+  const uint32_t j = from + (lane & (kEmbedPart - 1)), jj = j < to ? j : to - 1;
+  const uint32_t keys = a.key[jj], rows = a.row[jj];
+  const uint32_t sides = a.key[lane ? (to < a.n ? to : a.n - 1) : (from > 0 ? from - 1 : 0)];
+  const auto lane_of = [](uint32_t x, uint32_t k) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)k); };
+  uint32_t cur = lane_of(keys, 0);
   if (cur == V) return;
-  bool before = from > 0 && wave_uniform(a.key[from - 1]) == cur;  // cur's rows began in an earlier part
-  constexpr int U = 4;
-  for (uint32_t i = from; i < to; i += U) {
-    float x[U][N];
-    uint32_t key[U];
+  bool before = from > 0 && lane_of(sides, 0) == cur;  // cur's rows began in an earlier part
+  constexpr int U = N == 1 ? 32 : N == 4 ? 16 : 8;  // rows in flight
+  const uint32_t count = to - from;
+  for (uint32_t i = 0; i < count; i += U) {
+    Raw<G, N> x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t j = i + u < to ? i + u : to - 1;
-      key[u] = i + u < to ? wave_uniform(a.key[j]) : V;
-      const bool there = key[u] != V;
-      load_n<G, N>((const G*)a.dout + (int64_t)(there ? wave_uniform(a.row[j]) : 0u) * a.ldd + c, there ? n : 0, x[u]);
+      const uint32_t k = i + u < count ? i + u : 0;  // the first one is there, and has a row
+      x[u].load((const G*)a.dout + (int64_t)(lane_of(keys, k) != V ? lane_of(rows, k) : lane_of(rows, 0)) * a.ldd + c.at);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i + u < to && key[u] != cur) {
-        if (before) store_n<float, N>(a.part + (int64_t)part * 2 * a.d + c, n, sum);
+      if (i + u >= count) break;
+      const uint32_t key = lane_of(keys, i + u);
+      if (key != cur) {
+        if (before) store_n<float, N>(a.part + (int64_t)part * 2 * a.d, c, sum);
         else put_sum<T, N>(a, cur, c, sum);
         before = false;
-        cur = key[u];
+        cur = key;
         if (cur == V) return;
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] = 0.f;
       }
+      float f[N];
+      x[u].get(f);
 #pragma unroll
-      for (int e = 0; e < N; ++e) sum[e] += x[u][e];
+      for (int e = 0; e < N; ++e) sum[e] += f[e];
     }
   }
-  const bool on = to < a.n && wave_uniform(a.key[to]) == cur;
+  const bool on = to < a.n && lane_of(sides, 1) == cur;
   if (!before && !on) put_sum<T, N>(a, cur, c, sum);
-  else store_n<float, N>(a.part + ((int64_t)part * 2 + (before ? 0 : 1)) * a.d + c, n, sum);
+  else store_n<float, N>(a.part + ((int64_t)part * 2 + (before ? 0 : 1)) * a.d, c, sum);
 }
 template <typename G, typename T, int N>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, uint32_t parts, uint32_t cuts, uint64_t units) {
@@ -329,9 +429,8 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, uint32
   if (cur == (uint32_t)a.V || wave_uniform(a.key[to]) != cur) continue;
   const uint32_t from = part * kEmbedPart;
   if (wave_uniform(a.key[from]) == cur && from > 0 && wave_uniform(a.key[from - 1]) == cur) continue;
-  const uint32_t last = (bound_of<true>(a.key, a.n, cur) - 1) / kEmbedPart;  // the part that holds its last row
-  const int c = (int)(cut * 64 + lane) * N;
-  const int n = a.d - c > 0 ? a.d - c : 0;
+  const uint32_t last = (end_of(a.key, a.n, cur) - 1) / kEmbedPart;  // the part that holds its last row
+  const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
   const uint32_t each = (last - part + 3) / 4;
   const uint32_t k0 = part + 1 + wave * each, k1 = k0 + each < last + 1 ? k0 + each : last + 1;
   double sum[N];
@@ -339,14 +438,14 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, uint32
   for (int e = 0; e < N; ++e) sum[e] = 0;
   if (wave == 0) {
     float x[N];
-    load_n<float, N>(a.part + ((int64_t)part * 2 + 1) * a.d + c, n, x);
+    load_n<float, N>(a.part + ((int64_t)part * 2 + 1) * a.d, c, x);
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] = x[e];
   }
 #pragma unroll 4
   for (uint32_t k = k0; k < k1; ++k) {
     float x[N];
-    load_n<float, N>(a.part + (int64_t)k * 2 * a.d + c, n, x);
+    load_n<float, N>(a.part + (int64_t)k * 2 * a.d, c, x);
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[e] += x[e];
   }
@@ -367,11 +466,78 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, uint32
   }
 }
 
+// A batch of up to kEmbedSmall slots, without a sort: a wave looks through its tokens for those of its
+// two rows of the table, and adds up their rows in the order of their slots.
+constexpr uint32_t kSmallRows = 2;
+template <typename G, typename T, int N>
+__global__ __launch_bounds__(256) void embed_small_kernel(RowsArgs r, const int64_t* token, EmbedGradArgs a, uint32_t cuts,
+                                                          uint64_t units) {
+  constexpr int K = kEmbedSmall / 64, U = N == 1 ? 16 : 8;
+  const uint32_t lane = threadIdx.x & 63;
+  const uint64_t first = (uint64_t)blockIdx.x * 4 + wave_uniform(threadIdx.x >> 6);
+  if (first >= units) return;
+  Pair p[K];
+  load_tokens<K>(r, token, a.V, 0, r.n_slots, p);
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (k * 64 + lane >= r.n_slots) p[k].key = (uint32_t)a.V;
+  for (uint64_t unit = first; unit < units; unit += (uint64_t)gridDim.x * 4) {
+    const int64_t v0 = (int64_t)(unit / cuts) * kSmallRows;
+    const uint32_t cut = (uint32_t)(unit % cuts);
+    const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
+    uint64_t absent = 0;
+    for (uint32_t v = 0; v < kSmallRows && v0 + v < a.V; ++v) {
+      uint64_t has[K], any = 0;
+#pragma unroll
+      for (int k = 0; k < K; ++k) any |= has[k] = __ballot(p[k].key == (uint32_t)v0 + v);
+      if (!any) {
+        absent |= 1ull << v;
+        continue;
+      }
+      float sum[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        while (has[k]) {
+          Raw<G, N> x[U];
+          const int count = __popcll(has[k]) < U ? (int)__popcll(has[k]) : U;
+          uint64_t left = has[k];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int at = __builtin_ctzll(left);
+            if (u + 1 < count) left &= left - 1;  // the last one again behind it
+            x[u].load((const G*)a.dout + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)p[k].row, at) * a.ldd + c.at);
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (u >= count) break;
+            has[k] &= has[k] - 1;
+            float f[N];
+            x[u].get(f);
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[e] += f[e];
+          }
+        }
+      }
+      put_sum<T, N>(a, (uint32_t)v0 + v, c, sum);
+    }
+    if (!a.accumulate && cut == 0) zero_rows<T>(a, v0, absent);
+  }
+}
+
 template <typename T, typename O, int N>
 hipError_t embed_rows(const RowsArgs& r, const EmbedArgs& a, hipStream_t s) {
   const uint32_t cuts = (uint32_t)((a.d + 256 * N - 1) / (256 * N));
   const uint64_t units = (uint64_t)r.n_slots * cuts;
   hipLaunchKernelGGL((embed_kernel<T, O, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, r, a, cuts);
+  return hipGetLastError();
+}
+template <typename G, typename T, int N>
+hipError_t embed_small(const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a, hipStream_t s) {
+  const uint32_t cuts = (uint32_t)((a.d + 64 * N - 1) / (64 * N));
+  const uint64_t units = ((uint64_t)a.V + kSmallRows - 1) / kSmallRows * cuts;
+  hipLaunchKernelGGL((embed_small_kernel<G, T, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, r, token, a, cuts, units);
   return hipGetLastError();
 }
 template <typename G, typename T, int N>
@@ -392,24 +558,32 @@ hipError_t launch_embed(int table_dtype, int out_dtype, const RowsArgs& r, const
   return with_type(table_dtype, [&](auto t) {
     return with_type(out_dtype, [&](auto o) {
       if (a.d > 512) return embed_rows<decltype(t), decltype(o), 8>(r, a, s);
-      return embed_rows<decltype(t), decltype(o), 2>(r, a, s);
+      if (a.d >= 64) return embed_rows<decltype(t), decltype(o), 2>(r, a, s);
+      return embed_rows<decltype(t), decltype(o), 1>(r, a, s);
     });
   });
 }
 
 hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, hipStream_t s) {
-  if (r.n_slots <= kSortOneMost) {
-    hipLaunchKernelGGL(embed_sort_one_kernel, dim3(1), dim3(1024), 0, s, r, token, V, e);
+  if (r.n_slots <= 1024) {
+    hipLaunchKernelGGL(embed_sort_one_kernel<1>, dim3(1), dim3(1024), 0, s, r, token, V, e);
+    return hipGetLastError();
+  }
+  if (r.n_slots <= kSortKeys) {
+    hipLaunchKernelGGL(embed_sort_one_kernel<kSortRounds>, dim3(1), dim3(1024), 0, s, r, token, V, e);
     return hipGetLastError();
   }
   for (int pass = 0; pass < e.passes; ++pass) {
-    hipLaunchKernelGGL(embed_count_kernel, dim3(e.blocks), dim3(256), 0, s, r, token, V, e, pass);
-    hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(1024), 0, s, e);
-    hipLaunchKernelGGL(embed_place_kernel, dim3(e.blocks), dim3(256), 0, s, r, token, V, e, pass);
-    const hipError_t st = hipGetLastError();
-    if (st != hipSuccess) return st;
+    if (pass == 0) hipLaunchKernelGGL(embed_count_kernel<true>, dim3(e.blocks), dim3(1024), 0, s, r, token, V, e, pass);
+    else hipLaunchKernelGGL(embed_count_kernel<false>, dim3(e.blocks), dim3(1024), 0, s, r, token, V, e, pass);
+    if (e.blocks <= 32) {
+      hipLaunchKernelGGL(embed_place_kernel<true>, dim3(e.blocks), dim3(1024), 0, s, e, r.n_slots, pass);
+    } else {
+      hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(1024), 0, s, e);
+      hipLaunchKernelGGL(embed_place_kernel<false>, dim3(e.blocks), dim3(1024), 0, s, e, r.n_slots, pass);
+    }
   }
-  return hipSuccess;
+  return hipGetLastError();
 }
 
 hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArgs& a, hipStream_t s) {
@@ -418,6 +592,17 @@ hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArg
       if (a.d > 256) return embed_sums<decltype(g), decltype(t), 8>(a, s);
       if (a.d > 64) return embed_sums<decltype(g), decltype(t), 4>(a, s);
       return embed_sums<decltype(g), decltype(t), 1>(a, s);
+    });
+  });
+}
+
+hipError_t launch_embed_small(int dout_dtype, int table_dtype, const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a,
+                              hipStream_t s) {
+  return with_type(dout_dtype, [&](auto g) {
+    return with_type(table_dtype, [&](auto t) {
+      if (a.d > 256) return embed_small<decltype(g), decltype(t), 8>(r, token, a, s);
+      if (a.d > 64) return embed_small<decltype(g), decltype(t), 4>(r, token, a, s);
+      return embed_small<decltype(g), decltype(t), 1>(r, token, a, s);
     });
   });
 }

@@ -324,12 +324,11 @@ hipError_t launch_embed(int table_dtype, int out_dtype, const RowsArgs& r, const
 struct EmbedSort {
   uint32_t* key[2];   // [n_slots] each; the sorted pairs are in [passes & 1]
   uint32_t* row[2];
-  uint32_t* count;    // [bins * blocks], one workgroup's sort needs none
+  uint32_t* count;    // [bins][blocks], one workgroup's sort needs none
   int passes, bits;   // bits of a pass's digit
   uint32_t blocks;
 };
-constexpr uint32_t kSortKeys = 4096;        // keys of a workgroup
-constexpr uint32_t kSortOneMost = 16384;    // keys that one workgroup sorts alone
+constexpr uint32_t kSortKeys = 4096;        // keys of a workgroup; one sorts as many alone
 constexpr int kSortBits = 10;               // of a digit, at most
 inline int sort_passes(int64_t V) {
   int bits = 1;
@@ -357,6 +356,9 @@ struct EmbedGradArgs {
   int32_t d, accumulate;
   float scale;
 };
+constexpr uint32_t kEmbedSmall = 256;  // slots of a batch that needs no sort
+hipError_t launch_embed_small(int dout_dtype, int table_dtype, const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a,
+                              hipStream_t s);
 hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArgs& a, hipStream_t s);
 
 struct NormArgs {
@@ -373,7 +375,7 @@ struct NormArgs {
 hipError_t launch_layer_norm(int x_dtype, int y_dtype, const RowsArgs& r, const NormArgs& a, hipStream_t s);
 
 // A unit is what the weights' gradients are summed over: an example's slots, or all of
-// them; a workgroup sums a chunk of a unit's slots.
+// them; a workgroup sums a share of a unit's slots.
 struct NormGradArgs {
   const void* x;
   const void* dy;
@@ -383,15 +385,14 @@ struct NormGradArgs {
   void* dx;            // or null
   float* dweight;      // or null
   float* dbias;        // or null
-  float* part;         // [chunks][2][d], or null: a unit is one chunk
+  float* part;         // [units * chunks][2][d], or null: a unit is one share
   int64_t ldx, lddy, lddx, ldw, ldb;
   int32_t d, w_dtype, accumulate;
   uint32_t unit;       // slots of a unit
-  uint32_t chunk;      // slots of a chunk
-  uint32_t chunks;     // of a unit
+  uint32_t chunks;     // shares of a unit
   uint32_t units;
 };
-uint32_t norm_chunk(uint32_t unit, uint32_t units, int32_t d);
+uint32_t norm_chunks(uint32_t unit, uint32_t units, int32_t d);
 hipError_t launch_layer_norm_grad(int x_dtype, int dy_dtype, const RowsArgs& r, const NormGradArgs& a, hipStream_t s);
 constexpr int32_t kNormWidest = 32768;
 

@@ -47,6 +47,32 @@ __device__ inline double block_sum(double v, double* sm) {
   return sm[0] + sm[1] + sm[2] + sm[3];
 }
 
+// Four elements at any element's address, n of them there (the others are 0).
+template <typename T>
+__device__ inline void load4(const T* p, int n, float (&x)[4]) {
+  if (n >= 4) {
+    Raw<T, 4> r;
+    r.load(p);
+    r.get(x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = e < n ? (float)p[e] : 0.f;
+  }
+}
+template <typename T>
+__device__ inline void store4(T* p, int n, const float (&x)[4]) {
+  if (n >= 4) {
+    Raw<T, 4> r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.set(e, (T)x[e]);
+    *reinterpret_cast<typename Raw<T, 4>::vec*>(p) = r.v[0];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = (T)x[e];
+  }
+}
+
 __device__ inline float momentum_of(const MuonArgs& a, float m, float g) {
   return m * a.momentum + g * a.one_momentum;
 }
@@ -71,8 +97,8 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
   for (int64_t k = from + threadIdx.x * 4; k < to; k += 1024) {
     float m[4], g[4];
     const int c = to - k < 4 ? (int)(to - k) : 4;
-    load_n<float, 4>(mt + k, c, m);
-    load_n<G, 4>(gt + k, c, g);
+    load4(mt + k, c, m);
+    load4(gt + k, c, g);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       g[e] *= gs;
@@ -80,7 +106,7 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
       const float u = update_of(a, m[e], g[e]);
       if (e < c) sq += (double)u * (double)u;
     }
-    store_n<float, 4>(mt + k, c, m);
+    store4(mt + k, c, m);
   }
   sq = block_sum(sq, sm);
   if (threadIdx.x == 0) reinterpret_cast<double*>(q.base + i * q.stride + q.norm)[part] = sq;

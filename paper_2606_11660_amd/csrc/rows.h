@@ -36,7 +36,8 @@ __device__ inline RowSlot row_slot(const RowsArgs& a, uint32_t slot) {
   return r;
 }
 
-// N elements of type T at any element's address, in accesses of up to 16 bytes.
+// N elements of type T at any element's address, as they come from memory: accesses of up to 16
+// bytes, converted where they are used, so that the loads of several vectors are in flight together.
 template <typename T, int N>
 struct Vec {
   typedef T plain __attribute__((ext_vector_type(N)));
@@ -47,52 +48,57 @@ struct Vec<T, 1> {
   typedef T loose;
 };
 template <typename T, int N>
-__device__ inline void load_n(const T* p, int n, float (&x)[N]) {  // n of them are there; the others are 0
-  if (n >= N) {
-    if constexpr (N == 1) {
-      x[0] = (float)p[0];
-    } else if constexpr (N * sizeof(T) > 16) {
-      constexpr int H = 16 / sizeof(T);
-#pragma unroll
-      for (int h = 0; h < N / H; ++h) {
-        const auto v = *reinterpret_cast<const typename Vec<T, H>::loose*>(p + h * H);
-#pragma unroll
-        for (int e = 0; e < H; ++e) x[h * H + e] = (float)v[e];
-      }
-    } else {
-      const auto v = *reinterpret_cast<const typename Vec<T, N>::loose*>(p);
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = (float)v[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = e < n ? (float)p[e] : 0.f;
+struct Raw {
+  static constexpr int W = N * sizeof(T) > 16 ? 16 / sizeof(T) : N;  // elements of an access
+  typedef typename Vec<T, W>::loose vec;
+  vec v[N / W];
+  __device__ inline T at(int e) const {
+    if constexpr (W == 1) return v[e];
+    else return v[e / W][e % W];
   }
+  __device__ inline void set(int e, T x) {
+    if constexpr (W == 1) v[e] = x;
+    else v[e / W][e % W] = x;
+  }
+  __device__ inline void load(const T* p) {
+#pragma unroll
+    for (int k = 0; k < N / W; ++k) v[k] = *reinterpret_cast<const vec*>(p + k * W);
+  }
+  __device__ inline void get(float (&x)[N]) const {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = (float)at(e);
+  }
+};
+// A lane's N columns of rows of d >= N: from c on, or, where fewer are left, the row's last N, of
+// which the first `skip` belong to the lane before (skip >= N: none is the lane's own).  So every
+// lane loads whole vectors inside the row, without a branch.
+template <int N>
+struct Cols {
+  int at, skip;
+  __device__ inline Cols(int c, int d) {
+    at = c < d - N ? c : d - N;
+    skip = c - at;
+  }
+  __device__ inline bool own(int e) const { return e >= skip; }
+};
+template <typename T, int N>
+__device__ inline void load_n(const T* row, Cols<N> c, float (&x)[N]) {
+  Raw<T, N> r;
+  r.load(row + c.at);
+  r.get(x);
 }
 template <typename T, int N>
-__device__ inline void store_n(T* p, int n, const float (&x)[N]) {
-  if (n >= N) {
-    if constexpr (N == 1) {
-      p[0] = (T)x[0];
-    } else if constexpr (N * sizeof(T) > 16) {
-      constexpr int H = 16 / sizeof(T);
+__device__ inline void store_n(T* row, Cols<N> c, const float (&x)[N]) {
+  Raw<T, N> r;
 #pragma unroll
-      for (int h = 0; h < N / H; ++h) {
-        typename Vec<T, H>::loose v;
+  for (int e = 0; e < N; ++e) r.set(e, (T)x[e]);
+  if (c.skip == 0) {
 #pragma unroll
-        for (int e = 0; e < H; ++e) v[e] = (T)x[h * H + e];
-        *reinterpret_cast<typename Vec<T, H>::loose*>(p + h * H) = v;
-      }
-    } else {
-      typename Vec<T, N>::loose v;
+    for (int k = 0; k < N / Raw<T, N>::W; ++k) *reinterpret_cast<typename Raw<T, N>::vec*>(row + c.at + k * Raw<T, N>::W) = r.v[k];
+  } else if (c.skip < N) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = (T)x[e];
-      *reinterpret_cast<typename Vec<T, N>::loose*>(p) = v;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (e < n) p[e] = (T)x[e];
+    for (int e = 1; e < N; ++e)
+      if (c.own(e)) row[c.at + e] = r.at(e);
   }
 }
 

@@ -95,8 +95,9 @@ def test_embed_refusals():
 
 def test_embed_backward_refusals():
     L = P.lib()
-    need = L.attr_embed_backward_workspace_size(_r(), 10, 8)
-    assert need >= 4 * 8 * 4 and L.attr_embed_backward_workspace_size(_r(T=0), 10, 8) == 0
+    big = _r(n_rows=8000, n_examples=4, T=2000)
+    need = L.attr_embed_backward_workspace_size(big, 10, 8)
+    assert need >= 4 * 4 * 8000 and L.attr_embed_backward_workspace_size(_r(T=0), 10, 8) == 0
 
     def call(rows=None, tok=FAKE, g=MORE, gt=0, ldd=8, V=10, d=8, s=1.0, out=OUT, ot=0, ldt=8, acc=0, ws=WS, n=need):
         return L.attr_embed_backward(rows or _r(), tok, g, gt, ldd, V, d, s, out, ot, ldt, acc, ws, n, None)
@@ -105,8 +106,8 @@ def test_embed_backward_refusals():
         assert call(**kw) == INVALID, (kw, L.attr_last_error())
     assert call(gt=3) == UNSUPPORTED and call(ot=3) == UNSUPPORTED
     assert call(_r(n_rows=2 ** 32)) == UNSUPPORTED
-    assert call(tok=FAKE + 4) == ALIGN and call(g=MORE + 2) == ALIGN and call(out=OUT + 2) == ALIGN and call(ws=WS + 16) == ALIGN
-    assert call(ws=None) == WORKSPACE and call(n=need - 1) == WORKSPACE
+    assert call(tok=FAKE + 4) == ALIGN and call(g=MORE + 2) == ALIGN and call(out=OUT + 2) == ALIGN and call(big, g=0x1000000, ws=WS + 16) == ALIGN
+    assert call(big, g=0x1000000, ws=None) == WORKSPACE and call(big, g=0x1000000, n=need - 1) == WORKSPACE
     assert call(_r(n_examples=0, n_rows=0), acc=1, tok=None, g=None, out=None, ws=None) == 0
 
 
