@@ -1089,6 +1089,7 @@ static_assert(sizeof(attr_muon_matrix) == 56 && sizeof(attr_rows) == 40, "layout
 
 // Matrices that are worked on together: those of one shape side by side.
 struct MuonRound {
+  int thin;                    // sixteens of the shorter sides, all at most kThinMost; or 0
   std::vector<int32_t> order;  // the matrices, group by group
   attr::MuonArgs args;         // but for the table and the workspace's address
   uint32_t sym, full, flat, turn;  // workgroups
@@ -1132,16 +1133,35 @@ attr::MuonGroup muon_group(int64_t rows, int64_t cols, bool pairs) {
   return q;
 }
 
+// The same of a thin one.
+attr::MuonGroup thin_group(int64_t rows, int64_t cols) {
+  attr::MuonGroup q;
+  std::memset(&q, 0, sizeof(q));
+  q.rows = (int32_t)rows;
+  q.cols = (int32_t)cols;
+  q.L = (int32_t)std::max(rows, cols);
+  q.S = (int32_t)std::min(rows, cols);
+  const int64_t t = (q.S + 15) / 16;
+  q.n_flat = (uint32_t)((q.L + attr::kThinRows - 1) / attr::kThinRows);
+  q.poly = (int64_t)q.n_flat * (t * (t + 1) / 2 * 256 * 8);
+  q.stride = q.poly + t * t * 256 * 8;
+  return q;
+}
+
 // A round ends where its launches fill the GPU some times over: its buffers then stay
 // small, and nearer to the caches.
 constexpr uint32_t kMuonRoundTiles = 4096;
+constexpr uint32_t kMuonRoundFlat = 1u << 20;
 constexpr size_t kMuonRoundBytes = (size_t)1 << 30;
 
 MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
   MuonPlan P;
-  std::map<std::pair<int64_t, int64_t>, std::vector<int32_t>> shapes;
-  for (int32_t j = 0; j < n; ++j)
-    if (mats[j].rows > 0 && mats[j].cols > 0) shapes[{mats[j].rows, mats[j].cols}].push_back(j);
+  // by the sixteens of a thin shape (0: none), and by shape
+  std::map<std::tuple<int, int64_t, int64_t>, std::vector<int32_t>> shapes;
+  for (int32_t j = 0; j < n; ++j) {
+    const int64_t s = std::min(mats[j].rows, mats[j].cols);
+    if (s > 0) shapes[{s <= attr::kThinMost ? (int)((s + 15) / 16) : 0, mats[j].rows, mats[j].cols}].push_back(j);
+  }
   MuonRound R;
   const auto clear = [&] {
     R.order.clear();
@@ -1159,14 +1179,18 @@ MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
   };
   clear();
   for (const auto& sh : shapes) {
-    attr::MuonGroup q = muon_group(sh.first.first, sh.first.second, pairs);
+    const int thin = std::get<0>(sh.first);
+    attr::MuonGroup q = thin ? thin_group(std::get<1>(sh.first), std::get<2>(sh.first))
+                             : muon_group(std::get<1>(sh.first), std::get<2>(sh.first), pairs);
+    if (!R.order.empty() && R.thin != thin) end();
     bool open = false;
     for (int32_t j : sh.second) {
-      if (!R.order.empty() && (R.full + q.n_full > kMuonRoundTiles || R.bytes + (size_t)q.stride > kMuonRoundBytes ||
+      if (!R.order.empty() && (R.full + q.n_full > kMuonRoundTiles || R.flat + q.n_flat > kMuonRoundFlat || R.bytes + (size_t)q.stride > kMuonRoundBytes ||
                                (!open && R.args.n_groups == attr::kMuonGroups))) {
         end();
         open = false;
       }
+      R.thin = thin;
       if (!open) {
         q.base = reinterpret_cast<char*>(R.bytes);  // behind the table
         q.tile_sym = R.sym;
@@ -1267,6 +1291,12 @@ attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dt
       a.momentum = (float)momentum;
       a.one_momentum = (float)(1.0 - momentum);
       a.nesterov = nesterov;
+      if (R.thin) {
+        hipError_t e = attr::launch_muon_thin_gram((int)g_dtype, R.thin, a, R.flat, s);
+        if (e == hipSuccess) e = attr::launch_muon_thin_poly(R.thin, steps, a, (uint32_t)R.order.size(), s);
+        if (e == hipSuccess) e = attr::launch_muon_thin_apply((int)p_dtype, (int)g_dtype, master, R.thin, a, R.flat, s);
+        return e;
+      }
       hipError_t e = attr::launch_muon_momentum((int)g_dtype, a, R.flat, s);
       if (e == hipSuccess) e = attr::launch_muon_split((int)g_dtype, pairs != 0, a, R.turn, s);
       for (int32_t k = 0; k < steps && e == hipSuccess; ++k) {

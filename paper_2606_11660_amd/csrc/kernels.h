@@ -435,6 +435,13 @@ struct MuonArgs {
   MuonGroup g[kMuonGroups];
 };
 static_assert(sizeof(MuonArgs) <= 4096, "kernel arguments");
+// Shorter sides up to kThinMost: the iteration on their products (t: their sixteens); a workgroup takes
+// kThinRows of the longer side.  A group's workgroups are its tile_flat and n_flat; gram is its parts'
+// place, poly that of what u is multiplied by.
+constexpr int kThinMost = 64, kThinRows = 256;
+hipError_t launch_muon_thin_gram(int g_dtype, int t, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_thin_poly(int t, int steps, const MuonArgs& a, uint32_t matrices, hipStream_t s);
+hipError_t launch_muon_thin_apply(int p_dtype, int g_dtype, bool master, int t, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 constexpr int kMuonTile = 128;
 constexpr int64_t kMuonFlat = 16384;   // elements of a workgroup of the momentum's launch, at least
 constexpr uint32_t kMuonFlatMost = 256;  // such workgroups of a matrix

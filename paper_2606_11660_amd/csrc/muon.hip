@@ -15,25 +15,12 @@
 // 2^14 B fit, and what is below 2^-24 of the largest entry is still held.  fp16 keeps 11 bits where
 // bf16 keeps 8, at the same rate.  With pairs every operand is two fp16 values (22 bits) and a
 // product three: hi hi + hi lo + lo hi.  Sums are fp32, the norm's fp64.
-#include "common.h"
-#include "kernels.h"
-#include "rows.h"
-
-#pragma clang fp contract(off)
+#include "muon.h"
 
 namespace attr {
 namespace {
 
-constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kScale = 32768.f, kScalePoly = 16384.f;  // of X and A; of B
-
-// The group of a launch that holds this workgroup, and the workgroup within it.
-template <typename First>
-__device__ inline const MuonGroup& group_of(const MuonArgs& a, uint32_t block, First first) {
-  int k = 0;
-  while (k + 1 < a.n_groups && first(a.g[k + 1]) <= block) ++k;
-  return a.g[k];
-}
 
 __global__ __launch_bounds__(64) void muon_table_kernel(MuonTable t) {
   for (int j = threadIdx.x; j < t.n; j += 64) t.to[j] = t.e[j];
@@ -71,13 +58,6 @@ __device__ inline void store4(T* p, int n, const float (&x)[4]) {
     for (int e = 0; e < 3; ++e)
       if (e < n) p[e] = (T)x[e];
   }
-}
-
-__device__ inline float momentum_of(const MuonArgs& a, float m, float g) {
-  return m * a.momentum + g * a.one_momentum;
-}
-__device__ inline float update_of(const MuonArgs& a, float m, float g) {  // m after its step
-  return a.nesterov ? m * a.momentum + g * a.one_momentum : m;
 }
 
 // The momentum's step, and a workgroup's share of |u|^2.
@@ -154,7 +134,7 @@ __global__ __launch_bounds__(256) void muon_split_kernel(MuonArgs a) {
   char* const base = q.base + i * q.stride;
   const double* const norm = reinterpret_cast<const double*>(base + q.norm);
   const double total = block_sum(threadIdx.x < q.n_flat ? norm[threadIdx.x] : 0.0, sm);
-  const double inv = total > 0 ? (total < INFINITY ? (double)kScale / sqrt(total) : NAN) : total == 0 ? 0 : NAN;
+  const double inv = (double)kScale * inverse_norm(total);
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const uint32_t across = (uint32_t)q.ld / 64;  // Y's tiles in a row
   const int l0 = (int)(t / across) * 64, s0 = (int)(t - t / across * across) * 64;
@@ -473,7 +453,7 @@ __global__ __launch_bounds__(256, 2) void muon_last_kernel(MuonArgs a, int from)
         if (s + e >= q.S) continue;
         const int64_t at = turned ? (int64_t)(s + e) * q.cols + l : (int64_t)l * q.cols + s + e;
         const float w = MASTER ? en.master[at] : (float)p[at];
-        const float nw = w - w * lr_wd - x[e] * (1.f / kScale) * lr;
+        const float nw = stepped(w, x[e] * (1.f / kScale), lr, lr_wd);
         if (MASTER) en.master[at] = nw;
         p[at] = (P)nw;
       }

@@ -1,0 +1,273 @@
+// The Muon step of thin matrices, whose shorter side s is at most 64 (adapters, small heads).
+//
+// X^T X has only s x s entries, so the iteration runs on them: with G = u^T u (u's longer side
+// first, [t][s]), A = G / trace G and P = a I + b A + c A^2, a step X = X P turns A into P A P, and
+// after all of them X = u Q / |u|_F with Q the product of the P's.  All symmetric, all
+// polynomials of A.  A holds the squares of the singular values, so this needs twice the
+// digits, and has them: G, the iteration and the last product are in fp64 on the matrix cores
+// (16 x 16 x 4).  u is computed twice and nothing of its size is stored: bound by memory, the
+// gradient and the momentum read twice, the momentum and the weights written once.
+//
+// Lanes of the 16 x 16 x 4 product: A's row and B's column are lane % 16, the fourth of K is
+// lane / 16, and D's column is lane % 16, its rows lane / 16 + 4 r.
+#include "muon.h"
+
+namespace attr {
+namespace {
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+__device__ inline f64x4 mma(double a, double b, f64x4 c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0); }
+
+// Element (l, s) of a matrix whose longer side is l: its place.
+__device__ inline int64_t place_of(const MuonGroup& q, int l, int s) {
+  return q.rows >= q.cols ? (int64_t)l * q.cols + s : (int64_t)s * q.cols + l;
+}
+
+// The momentum's step, and G's upper tiles over kThinRows of the longer side: a wave adds up every
+// fourth 16 of them, the four waves' sums in the order of the waves.
+template <typename G, int T>
+__global__ __launch_bounds__(256) void muon_thin_gram_kernel(MuonArgs a) {
+  constexpr int TILES = T * (T + 1) / 2;
+  __shared__ double sm[3][TILES * 256];
+  const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_flat; });
+  const uint32_t at = blockIdx.x - q.tile_flat, i = at / q.n_flat, part = at - i * q.n_flat;
+  const MuonEntry& en = a.table[q.entry + i];
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
+  const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6));
+  const int l0 = (int)part * kThinRows, l1 = q.L - l0 < kThinRows ? q.L : l0 + kThinRows;
+  f64x4 acc[TILES];
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) acc[k] = f64x4{0, 0, 0, 0};
+  for (int l = l0 + wave * 16; l < l1; l += 64) {
+    // K in fours: step e takes the rows l + 4 (lane / 16) + e
+    float m[T][4], g[T][4];
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = l + 4 * (lane >> 4) + e, s = 16 * t + (lane & 15);
+        m[t][e] = g[t][e] = 0.f;
+        if (r < l1 && s < q.S) {
+          const int64_t p = place_of(q, r, s);
+          m[t][e] = en.m[p];
+          g[t][e] = (float)((const G*)en.g)[p];
+        }
+      }
+    double u[T][4];
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = l + 4 * (lane >> 4) + e, s = 16 * t + (lane & 15);
+        const float gr = g[t][e] * gs, mo = momentum_of(a, m[t][e], gr);
+        const bool there = r < l1 && s < q.S;
+        u[t][e] = there ? (double)update_of(a, mo, gr) : 0.0;
+        if (there) en.m[place_of(q, r, s)] = mo;
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int tj = 0, k = 0; tj < T; ++tj)
+#pragma unroll
+        for (int ti = 0; ti <= tj; ++ti, ++k) acc[k] = mma(u[ti][e], u[tj][e], acc[k]);
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int k = 0; k < TILES; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sm[wave - 1][k * 256 + e * 64 + lane] = acc[k][e];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  double* const out = reinterpret_cast<double*>(q.base + i * q.stride + q.gram) + (int64_t)part * TILES * 256;
+#pragma unroll
+  for (int k = 0; k < TILES; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      double x = acc[k][e];
+#pragma unroll
+      for (int w = 0; w < 3; ++w) x += sm[w][k * 256 + e * 64 + lane];
+      out[k * 256 + e * 64 + lane] = x;  // row 16 ti + lane / 16 + 4 e, column 16 tj + lane % 16
+    }
+}
+
+// Q / |u| of one matrix from its parts of G: a wave for each 16 x 16 tile.
+template <int T>
+__global__ __launch_bounds__(64 * T * T) void muon_thin_poly_kernel(MuonArgs a, int steps) {
+  constexpr int W = 16 * T, TILES = T * (T + 1) / 2;
+  __shared__ double A[W][W], P[W][W], Q[W][W];
+  __shared__ double trace;
+  int k = 0;
+  while (k + 1 < a.n_groups && a.g[k + 1].entry <= blockIdx.x) ++k;
+  const MuonGroup& q = a.g[k];
+  char* const base = q.base + (int64_t)(blockIdx.x - q.entry) * q.stride;
+  const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6));
+  const int ti = wave / T, tj = wave - ti * T;
+  const int c = 16 * tj + (lane & 15), r0 = 16 * ti + (lane >> 4);  // this lane's column, first of its rows
+  const double* const parts = reinterpret_cast<const double*>(base + q.gram);
+  if (ti <= tj) {
+    const int tile = tj * (tj + 1) / 2 + ti;
+    double x[4] = {0, 0, 0, 0};
+#pragma unroll 2
+    for (uint32_t p = 0; p < q.n_flat; ++p)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += parts[(int64_t)p * TILES * 256 + tile * 256 + e * 64 + lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      A[r0 + 4 * e][c] = x[e];
+      if (ti != tj) A[c][r0 + 4 * e] = x[e];
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    double x = (int)threadIdx.x < W ? A[threadIdx.x][threadIdx.x] : 0.0;
+    x = wave_sum(x);
+    if (threadIdx.x == 0) trace = x;
+  }
+  __syncthreads();
+  const double inv = inverse_norm(trace);
+  double own[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    own[e] = A[r0 + 4 * e][c] * inv * inv;
+    Q[r0 + 4 * e][c] = r0 + 4 * e == c ? inv : 0.0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 4; ++e) A[r0 + 4 * e][c] = own[e];
+  __syncthreads();
+  // this wave's tile of x y, both symmetric
+  const auto product = [&](const double(&x)[W][W], const double(&y)[W][W]) {
+    f64x4 d = {0, 0, 0, 0};
+#pragma unroll
+    for (int n = 0; n < W / 4; ++n) {
+      const int kk = 4 * n + (lane >> 4);
+      d = mma(x[kk][16 * ti + (lane & 15)], y[kk][c], d);
+    }
+    return d;
+  };
+  for (int step = 0; step < steps; ++step) {
+    const f64x4 sq = product(A, A);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = r0 + 4 * e;
+      P[r][c] = (r == c ? (double)kNsA : 0.0) + (double)kNsB * A[r][c] + (double)kNsC * sq[e];
+    }
+    __syncthreads();
+    const f64x4 nq = product(P, Q), pa = product(P, A);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      Q[r0 + 4 * e][c] = nq[e];
+      A[r0 + 4 * e][c] = pa[e];
+    }
+    __syncthreads();
+    const f64x4 pap = product(P, A);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) A[r0 + 4 * e][c] = pap[e];
+    __syncthreads();
+  }
+  double* const out = reinterpret_cast<double*>(base + q.poly);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[(r0 + 4 * e) * W + c] = Q[r0 + 4 * e][c];
+}
+
+// X = u Q and the weights' step: a wave takes 16 of the longer side at a time.
+template <typename P, typename G, bool MASTER, int T>
+__global__ __launch_bounds__(256) void muon_thin_apply_kernel(MuonArgs a) {
+  constexpr int W = 16 * T;
+  const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_flat; });
+  const uint32_t at = blockIdx.x - q.tile_flat, i = at / q.n_flat, part = at - i * q.n_flat;
+  const MuonEntry& en = a.table[q.entry + i];
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
+  const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6));
+  const int low = lane & 15, high = lane >> 4;
+  const int l0 = (int)part * kThinRows, l1 = q.L - l0 < kThinRows ? q.L : l0 + kThinRows;
+  const double* const Q = reinterpret_cast<const double*>(q.base + i * q.stride + q.poly);
+  const bool turned = q.rows < q.cols;
+  P* const pt = (P*)en.p;
+  for (int l = l0 + wave * 16; l < l1; l += 64) {
+    // K step (t, e) takes the columns 16 t + 4 (lane / 16) + e
+    float m[T][4], g[T][4];
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = l + low, s = 16 * t + 4 * high + e;
+        m[t][e] = g[t][e] = 0.f;
+        if (r < l1 && s < q.S) {
+          const int64_t p = place_of(q, r, s);
+          m[t][e] = en.m[p];
+          g[t][e] = (float)((const G*)en.g)[p];
+        }
+      }
+    f64x4 acc[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) acc[t] = f64x4{0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const double u = (double)update_of(a, m[t][e], g[t][e] * gs);
+#pragma unroll
+        for (int o = 0; o < T; ++o) {
+          const double x = Q[(16 * t + 4 * high + e) * W + 16 * o + low];
+          acc[o] = turned ? mma(x, u, acc[o]) : mma(u, x, acc[o]);  // D's column, its lanes' neighbours, is the weights'
+        }
+      }
+#pragma unroll
+    for (int o = 0; o < T; ++o)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = l + (turned ? low : high + 4 * e), s = 16 * o + (turned ? high + 4 * e : low);
+        if (r >= l1 || s >= q.S) continue;
+        const int64_t p = place_of(q, r, s);
+        const float w = MASTER ? en.master[p] : (float)pt[p];
+        const float nw = stepped(w, (float)acc[o][e], en.lr, en.lr_wd);
+        if (MASTER) en.master[p] = nw;
+        pt[p] = (P)nw;
+      }
+  }
+}
+
+// Calls f with T, the 16s of a shorter side.
+template <typename F>
+hipError_t with_sixteens(int t, F f) {
+  if (t == 1) f(std::integral_constant<int, 1>{});
+  else if (t == 2) f(std::integral_constant<int, 2>{});
+  else if (t == 3) f(std::integral_constant<int, 3>{});
+  else f(std::integral_constant<int, 4>{});
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_muon_thin_gram(int g_dtype, int t, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
+  return with_type(g_dtype, [&](auto g) {
+    return with_sixteens(t, [&](auto n) {
+      hipLaunchKernelGGL((muon_thin_gram_kernel<decltype(g), decltype(n)::value>), dim3(blocks), dim3(256), 0, s, a);
+    });
+  });
+}
+hipError_t launch_muon_thin_poly(int t, int steps, const MuonArgs& a, uint32_t matrices, hipStream_t s) {
+  return with_sixteens(t, [&](auto n) {
+    constexpr int T = decltype(n)::value;
+    hipLaunchKernelGGL((muon_thin_poly_kernel<T>), dim3(matrices), dim3(64 * T * T), 0, s, a, steps);
+  });
+}
+hipError_t launch_muon_thin_apply(int p_dtype, int g_dtype, bool master, int t, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
+  return with_type(p_dtype, [&](auto p) {
+    return with_type(g_dtype, [&](auto g) {
+      return with_sixteens(t, [&](auto n) {
+        typedef decltype(p) P;
+        typedef decltype(g) G;
+        constexpr int T = decltype(n)::value;
+        if (master) hipLaunchKernelGGL((muon_thin_apply_kernel<P, G, true, T>), dim3(blocks), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((muon_thin_apply_kernel<P, G, false, T>), dim3(blocks), dim3(256), 0, s, a);
+      });
+    });
+  });
+}
+
+}  // namespace attr

@@ -178,10 +178,11 @@ def test_muon_refusals():
     for kw in (dict(mats=[_m(p=FAKE + 2)]), dict(mats=[_m(g=OUT + 2)]), dict(mats=[_m(m=MORE + 2)]), dict(gs=FAKE + 2),
                dict(mats=[_m(master=0xd00002)], p=1), dict(ws=WS + 16)):
         assert call(**kw) == ALIGN, (kw, L.attr_last_error())
-    arr = (P._CMuonMatrix * 1)(_m())
+    wide = _m(rows=100, cols=80)
+    arr = (P._CMuonMatrix * 1)(wide)
     need = L.attr_muon_step_workspace_size(arr, 1, 0)
     assert need > 0 and L.attr_muon_step_workspace_size(arr, 1, 1) > need and L.attr_muon_step_workspace_size(arr, 1, 2) == 0
-    assert call(n=need - 1) == WORKSPACE and call(ws=None) == WORKSPACE
+    assert call(mats=[wide], n=need - 1) == WORKSPACE and call(ws=None) == WORKSPACE
     assert call(mats=[]) == 0 and call(mats=[_m(rows=0, p=None, g=None, m=None)], ws=None) == 0
 
 
