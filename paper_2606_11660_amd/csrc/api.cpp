@@ -1089,7 +1089,7 @@ static_assert(sizeof(attr_muon_matrix) == 56 && sizeof(attr_rows) == 40, "layout
 
 // Matrices that are worked on together: those of one shape side by side.
 struct MuonRound {
-  int thin;                    // sixteens of the shorter sides, all at most kThinMost; or 0
+  int kind;                    // sixteens of the shorter sides, all at most kThinMost; or kTiles, kBigTiles
   std::vector<int32_t> order;  // the matrices, group by group
   attr::MuonArgs args;         // but for the table and the workspace's address
   uint32_t sym, full, flat, turn;  // workgroups
@@ -1106,7 +1106,7 @@ bool muon_fits(const attr_muon_matrix& t) {
 }
 
 // Workspace of one matrix, and the workgroups that its launches take.
-attr::MuonGroup muon_group(int64_t rows, int64_t cols, bool pairs) {
+attr::MuonGroup muon_group(int64_t rows, int64_t cols, bool pairs, bool big) {
   attr::MuonGroup q;
   std::memset(&q, 0, sizeof(q));
   q.rows = (int32_t)rows;
@@ -1124,8 +1124,8 @@ attr::MuonGroup muon_group(int64_t rows, int64_t cols, bool pairs) {
   q.poly = q.gram + many * s;
   q.norm = q.poly + many * s;
   q.stride = q.norm + (int64_t)align_up(8 * attr::kMuonFlatMost);
-  const uint32_t ts = (uint32_t)(q.S + attr::kMuonTile - 1) / attr::kMuonTile,
-                 tl = (uint32_t)(q.L + attr::kMuonTile - 1) / attr::kMuonTile;
+  const int32_t tile = big ? 2 * attr::kMuonTile : attr::kMuonTile;
+  const uint32_t ts = (uint32_t)((q.S + tile - 1) / tile), tl = (uint32_t)((q.L + tile - 1) / tile);
   q.n_sym = ts * (ts + 1) / 2;
   q.n_full = ts * tl;
   q.n_flat = (uint32_t)std::min<int64_t>((rows * cols + attr::kMuonFlat - 1) / attr::kMuonFlat, attr::kMuonFlatMost);
@@ -1148,6 +1148,13 @@ attr::MuonGroup thin_group(int64_t rows, int64_t cols) {
   return q;
 }
 
+constexpr int kTiles = 8, kBigTiles = 9;
+int muon_kind(const attr_muon_matrix& t) {
+  const int64_t s = std::min(t.rows, t.cols);
+  if (s <= attr::kThinMost) return (int)((s + 15) / 16);
+  return s >= 1024 ? kBigTiles : kTiles;
+}
+
 // A round ends where its launches fill the GPU some times over: its buffers then stay
 // small, and nearer to the caches.
 constexpr uint32_t kMuonRoundTiles = 4096;
@@ -1156,11 +1163,10 @@ constexpr size_t kMuonRoundBytes = (size_t)1 << 30;
 
 MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
   MuonPlan P;
-  // by the sixteens of a thin shape (0: none), and by shape
+  // by kind, and by shape
   std::map<std::tuple<int, int64_t, int64_t>, std::vector<int32_t>> shapes;
   for (int32_t j = 0; j < n; ++j) {
-    const int64_t s = std::min(mats[j].rows, mats[j].cols);
-    if (s > 0) shapes[{s <= attr::kThinMost ? (int)((s + 15) / 16) : 0, mats[j].rows, mats[j].cols}].push_back(j);
+    if (mats[j].rows > 0 && mats[j].cols > 0) shapes[{muon_kind(mats[j]), mats[j].rows, mats[j].cols}].push_back(j);
   }
   MuonRound R;
   const auto clear = [&] {
@@ -1179,10 +1185,10 @@ MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
   };
   clear();
   for (const auto& sh : shapes) {
-    const int thin = std::get<0>(sh.first);
-    attr::MuonGroup q = thin ? thin_group(std::get<1>(sh.first), std::get<2>(sh.first))
-                             : muon_group(std::get<1>(sh.first), std::get<2>(sh.first), pairs);
-    if (!R.order.empty() && R.thin != thin) end();
+    const int kind = std::get<0>(sh.first);
+    attr::MuonGroup q = kind < kTiles ? thin_group(std::get<1>(sh.first), std::get<2>(sh.first))
+                                      : muon_group(std::get<1>(sh.first), std::get<2>(sh.first), pairs, kind == kBigTiles);
+    if (!R.order.empty() && R.kind != kind) end();
     bool open = false;
     for (int32_t j : sh.second) {
       if (!R.order.empty() && (R.full + q.n_full > kMuonRoundTiles || R.flat + q.n_flat > kMuonRoundFlat || R.bytes + (size_t)q.stride > kMuonRoundBytes ||
@@ -1190,7 +1196,7 @@ MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
         end();
         open = false;
       }
-      R.thin = thin;
+      R.kind = kind;
       if (!open) {
         q.base = reinterpret_cast<char*>(R.bytes);  // behind the table
         q.tile_sym = R.sym;
@@ -1291,21 +1297,22 @@ attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dt
       a.momentum = (float)momentum;
       a.one_momentum = (float)(1.0 - momentum);
       a.nesterov = nesterov;
-      if (R.thin) {
-        hipError_t e = attr::launch_muon_thin_gram((int)g_dtype, R.thin, a, R.flat, s);
-        if (e == hipSuccess) e = attr::launch_muon_thin_poly(R.thin, steps, a, (uint32_t)R.order.size(), s);
-        if (e == hipSuccess) e = attr::launch_muon_thin_apply((int)p_dtype, (int)g_dtype, master, R.thin, a, R.flat, s);
+      if (R.kind < kTiles) {
+        hipError_t e = attr::launch_muon_thin_gram((int)g_dtype, R.kind, a, R.flat, s);
+        if (e == hipSuccess) e = attr::launch_muon_thin_poly(R.kind, steps, a, (uint32_t)R.order.size(), s);
+        if (e == hipSuccess) e = attr::launch_muon_thin_apply((int)p_dtype, (int)g_dtype, master, R.kind, a, R.flat, s);
         return e;
       }
+      const bool big = R.kind == kBigTiles;
       hipError_t e = attr::launch_muon_momentum((int)g_dtype, a, R.flat, s);
       if (e == hipSuccess) e = attr::launch_muon_split((int)g_dtype, pairs != 0, a, R.turn, s);
       for (int32_t k = 0; k < steps && e == hipSuccess; ++k) {
         const int from = k & 1;
-        e = attr::launch_muon_gram(pairs != 0, from, a, R.sym, s);
-        if (e == hipSuccess) e = attr::launch_muon_poly(pairs != 0, a, R.sym, s);
+        e = attr::launch_muon_gram(big, pairs != 0, from, a, R.sym, s);
+        if (e == hipSuccess) e = attr::launch_muon_poly(big, pairs != 0, a, R.sym, s);
         if (e != hipSuccess) break;
-        e = k + 1 < steps ? attr::launch_muon_apply(pairs != 0, from, a, R.full, s)
-                          : attr::launch_muon_last(pairs != 0, (int)p_dtype, master, from, a, R.full, s);
+        e = k + 1 < steps ? attr::launch_muon_apply(big, pairs != 0, from, a, R.full, s)
+                          : attr::launch_muon_last(big, pairs != 0, (int)p_dtype, master, from, a, R.full, s);
       }
       return e;
     };

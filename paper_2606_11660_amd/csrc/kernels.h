@@ -448,10 +448,11 @@ constexpr uint32_t kMuonFlatMost = 256;  // such workgroups of a matrix
 hipError_t launch_muon_table(const MuonTable& t, hipStream_t s);
 hipError_t launch_muon_momentum(int g_dtype, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 hipError_t launch_muon_split(int g_dtype, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
-hipError_t launch_muon_gram(bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
-hipError_t launch_muon_poly(bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
-hipError_t launch_muon_apply(bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
-hipError_t launch_muon_last(bool pairs, int p_dtype, bool master, int from, const MuonArgs& a, uint32_t blocks,
+// big: tiles of 256 x 256, whose numbers the groups then hold
+hipError_t launch_muon_gram(bool big, bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_poly(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_apply(bool big, bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_last(bool big, bool pairs, int p_dtype, bool master, int from, const MuonArgs& a, uint32_t blocks,
                             hipStream_t s);
 
 // ---------------------------------------------------------------------------

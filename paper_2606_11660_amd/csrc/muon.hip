@@ -15,6 +15,7 @@
 // 2^14 B fit, and what is below 2^-24 of the largest entry is still held.  fp16 keeps 11 bits where
 // bf16 keeps 8, at the same rate.  With pairs every operand is two fp16 values (22 bits) and a
 // product three: hi hi + hi lo + lo hi.  Sums are fp32, the norm's fp64.
+#include "gemm.h"
 #include "muon.h"
 
 namespace attr {
@@ -92,12 +93,6 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
   if (threadIdx.x == 0) reinterpret_cast<double*>(q.base + i * q.stride + q.norm)[part] = sq;
 }
 
-template <bool PAIRS>
-__device__ inline void put_halves(_Float16* hi, int64_t lo, float x) {  // lo: bytes
-  const _Float16 h = (_Float16)x;
-  *hi = h;
-  if (PAIRS) *reinterpret_cast<_Float16*>(reinterpret_cast<char*>(hi) + lo) = (_Float16)(x - (float)h);
-}
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 template <bool PAIRS>
 __device__ inline void put_halves4(_Float16* hi, int64_t lo, const float (&x)[4]) {
@@ -110,18 +105,6 @@ __device__ inline void put_halves4(_Float16* hi, int64_t lo, const float (&x)[4]
   *reinterpret_cast<half4*>(hi) = h;
   if (PAIRS) *reinterpret_cast<half4*>(reinterpret_cast<char*>(hi) + lo) = l;
 }
-template <bool PAIRS>
-__device__ inline void get_halves4(const _Float16* hi, int64_t lo, float (&x)[4]) {
-  const half4 h = *reinterpret_cast<const half4*>(hi);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = (float)h[e];
-  if (PAIRS) {
-    const half4 l = *reinterpret_cast<const half4*>(reinterpret_cast<const char*>(hi) + lo);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] += (float)l[e];
-  }
-}
-
 // u / |u| as halves, its longer side first: 64 x 64 elements of the matrix a workgroup, turned
 // in LDS where the columns are the longer side.  Columns from S to ld are zeros.
 template <typename G, bool PAIRS>
@@ -164,7 +147,7 @@ __global__ __launch_bounds__(256) void muon_split_kernel(MuonArgs a) {
 }
 
 // ----------------------------------------------------------------------------
-// 128 x 128 tiles of a product, K in stages of 64
+// 128 x 128 tiles of a product
 // ----------------------------------------------------------------------------
 constexpr int MT = kMuonTile;
 constexpr uint32_t M_SLOT = MT * 128;  // bytes of an operand's stage
@@ -173,120 +156,179 @@ struct MuonSmem {
   i32x4 b[2][MT * 8];
 };
 
-template <int N>
-__device__ inline void wait_vm() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
 // Four waves (2 x 2) hold 64 x 64 each, as 4 x 4 accumulators.  C[m][n] += sum_k A[m][k] B[n][k];
-// KMAJOR: of operands stored [k][m] and [k][n].  Stages go straight to LDS, one ahead.
-template <bool KMAJOR>
+// KMAJOR: of operands stored [k][m] and [k][n].  Stages (K = 64, or with PAIRS 32 of both halves)
+// go straight to LDS, one ahead, two workgroups a CU.  With PAIRS the three products of a stage
+// share their fragments: 16 reads for 48 products, where three passes took 24.
+template <bool KMAJOR, bool PAIRS>
 struct MuonCore {
-  f32x4 acc[4][4];
+  static constexpr int F = 4;  // 16 x 16 accumulators of a wave each way
+  typedef MuonSmem Smem;
+  f32x4 acc[F][F];
 
-  __device__ inline void zero() {
+  // K in n_k rows (KMAJOR) or values; ao and bo: the operands' first halves from the tile's first
+  // row (KMAJOR: column), ld both operands' row stride, a_lo and b_lo the second halves'
+  // descriptors.  What is past a descriptor's range reads as zeros.
+  __device__ inline void product(MuonSmem& sm, const i32x4& a_hi_, const i32x4& a_lo_, const i32x4& b_hi_, const i32x4& b_lo_,
+                                 int32_t ld, int n_k) {
+    const i32x4 a_hi = uniform_desc(a_hi_), a_lo = uniform_desc(a_lo_), b_hi = uniform_desc(b_hi_), b_lo = uniform_desc(b_lo_);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < F; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  // n_st stages; da and db start at the tile's first row (KMAJOR: column), ld is both
-  // operands' row stride.  What is past a descriptor's range reads as zeros.
-  __device__ inline void run(MuonSmem& sm, const i32x4& da_, const i32x4& db_, int32_t ld, int n_st) {
-    const i32x4 da = uniform_desc(da_), db = uniform_desc(db_);
+      for (int j = 0; j < F; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int KS = PAIRS ? 32 : 64;
+    const int n_st = (n_k + KS - 1) / KS;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int lane = threadIdx.x & 63;
     const int wm = wave >> 1, wn = wave & 1;
-    // loads: instruction h (0..3) of a wave fills 1 KB of the operand's stage: eight rows of 64
-    // values, or (KMAJOR) four K-rows of 128
+    // loads: an instruction fills 1 KB of a stage, four of them an operand's share of a wave:
+    //   rows of K            eight rows of 64 values; PAIRS: 16 rows of 32, of each half
+    //   KMAJOR               four K-rows of 128 values
+    // The 16-byte pieces of a row (KMAJOR: 32-byte pieces) change places by row, so that the
+    // fragment reads of 16 lanes meet distinct banks.
     uint32_t off[4];
-    if constexpr (KMAJOR) {
-      const int lr = lane >> 4, s = lane & 15;
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int row = 16 * wave + 4 * h + lr;
-        const int c = (((s >> 1) ^ swz(row)) << 1) | (s & 1);
-        off[h] = (uint32_t)(row * ld * 2 + c * 16) - 1024u * (uint32_t)h;
+    for (int h = 0; h < 4; ++h) {
+      const int part = PAIRS ? h & 1 : h, first = PAIRS ? 2 * wave + part : 4 * wave + part;  // of the KBs of a half
+      if constexpr (KMAJOR) {
+        const int row = 4 * first + (lane >> 4), s = lane & 15;
+        off[h] = (uint32_t)(row * ld * 2 + (((((s >> 1) ^ swz(row)) << 1) | (s & 1)) * 16));
+      } else if constexpr (PAIRS) {
+        const int row = 16 * first + (lane >> 2);
+        off[h] = (uint32_t)(row * ld * 2 + (((lane & 3) ^ ((row >> 2) & 3)) * 16));
+      } else {
+        const int row = 8 * first + (lane >> 3);
+        off[h] = (uint32_t)(row * ld * 2 + (((lane & 7) ^ (row & 7)) * 16));
       }
-    } else {
-      const int lr = lane >> 3, c = (lane & 7) ^ lr;
-#pragma unroll
-      for (int h = 0; h < 4; ++h)
-        off[h] = (uint32_t)((32 * wave + 8 * h + lr) * ld * 2 + c * 16) - 1024u * (uint32_t)h;
+      off[h] -= 1024u * (uint32_t)part;
     }
-    const uint32_t step = KMAJOR ? (uint32_t)(64 * ld * 2) : 128u;
+    const uint32_t step = KMAJOR ? (uint32_t)(KS * ld * 2) : 2u * KS;
     const uint32_t sa = (uint32_t)(uintptr_t)&sm.a[0][0], sb = (uint32_t)(uintptr_t)&sm.b[0][0];
-    const uint32_t lds_a = sa + (uint32_t)wave * 4096u, lds_b = sb + (uint32_t)wave * 4096u;
-    auto issue = [&](int st) {
+    const auto issue = [&](int st) {
       const bool live = st < n_st;
-      const uint32_t slot = (uint32_t)(st & 1) * M_SLOT;
-      const i32x4 xa = desc_at(da, (uint32_t)st * step, live), xb = desc_at(db, (uint32_t)st * step, live);
-      set_m0(lds_a + slot);
-      lds_dma16_m0<0>(xa, off[0]);
-      lds_dma16_m0<1024>(xa, off[1]);
-      lds_dma16_m0<2048>(xa, off[2]);
-      lds_dma16_m0<3072>(xa, off[3]);
-      set_m0(lds_b + slot);
-      lds_dma16_m0<0>(xb, off[0]);
-      lds_dma16_m0<1024>(xb, off[1]);
-      lds_dma16_m0<2048>(xb, off[2]);
-      lds_dma16_m0<3072>(xb, off[3]);
+      const uint32_t slot = (uint32_t)(st & 1) * M_SLOT, ko = (uint32_t)st * step;
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const uint32_t lds = (o ? sb : sa) + slot;
+        const i32x4 hi = desc_at(o ? b_hi : a_hi, ko, live);
+        if constexpr (PAIRS) {
+          const i32x4 lo = desc_at(o ? b_lo : a_lo, ko, live);
+          set_m0(lds + (uint32_t)wave * 2048u);
+          lds_dma16_m0<0>(hi, off[0]);
+          lds_dma16_m0<1024>(hi, off[1]);
+          set_m0(lds + M_SLOT / 2 + (uint32_t)wave * 2048u);
+          lds_dma16_m0<0>(lo, off[2]);
+          lds_dma16_m0<1024>(lo, off[3]);
+        } else {
+          set_m0(lds + (uint32_t)wave * 4096u);
+          lds_dma16_m0<0>(hi, off[0]);
+          lds_dma16_m0<1024>(hi, off[1]);
+          lds_dma16_m0<2048>(hi, off[2]);
+          lds_dma16_m0<3072>(hi, off[3]);
+        }
+      }
     };
     const int ri = lane & 15, rg = lane >> 4;
-    auto frag = [&](uint32_t base, int half, int t, int hk) -> i32x4 {  // block t of the operand's half, K-half hk
+    const auto frag = [&](uint32_t base, int half, int t, int hk) -> i32x4 {  // block t of the operand's half, K-half hk
       if constexpr (KMAJOR) {
         const int gl = (ri >> 2) | ((rg & 1) << 2);
         const uint32_t at = base + (uint32_t)(32 * hk + 8 * rg + (ri >> 2)) * 256u + 32u * (uint32_t)((4 * half + t) ^ gl) +
                             8u * (uint32_t)(ri & 3);
-        const i32x2 lo = read_tr(at), hi = read_tr(at + 4u * 256u);
+        const i32x2 lo = lds_read_tr16(at), hi = lds_read_tr16(at + 4u * 256u);
         return i32x4{lo.x, lo.y, hi.x, hi.y};
       } else {
-        const uint32_t at = base + (uint32_t)(64 * half + 16 * t + ri) * 128u + 16u * (uint32_t)((4 * hk + rg) ^ (ri & 7));
+        const uint32_t row = (uint32_t)(64 * half + 16 * t + ri);
+        const uint32_t at = PAIRS ? base + row * 64u + 16u * (uint32_t)(rg ^ ((ri >> 2) & 3))
+                                  : base + row * 128u + 16u * (uint32_t)((4 * hk + rg) ^ (ri & 7));
         return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>((uintptr_t)at);
       }
     };
     issue(0);
     for (int st = 0; st < n_st; ++st) {
-      wait_vm<0>();   // stage st has landed
-      wait_lgkm0();   // this wave has read stage st - 1
+      gemm_wait_vm<0>();  // stage st has landed
+      wait_lgkm0();       // this wave has read stage st - 1
       __builtin_amdgcn_s_barrier();
-      issue(st + 1);  // past the end nothing is fetched
+      issue(st + 1);      // past the end nothing is fetched
       const uint32_t slot = (uint32_t)(st & 1) * M_SLOT;
+      i32x4 fa[F], fb[F], ga[F], gb[F];
+      if constexpr (PAIRS) {
 #pragma unroll
-      for (int hk = 0; hk < 2; ++hk) {
-        i32x4 fa[4], fb[4];
+        for (int t = 0; t < F; ++t) {
+          fb[t] = frag(sb + slot, wn, t, 0);
+          fa[t] = frag(sa + slot, wm, t, 0);
+        }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) fb[t] = frag(sb + slot, wn, t, hk);
+        for (int t = 0; t < F; ++t) {
+          gb[t] = frag(sb + slot + M_SLOT / 2, wn, t, 0);
+          ga[t] = frag(sa + slot + M_SLOT / 2, wm, t, 0);
+        }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) fa[t] = frag(sa + slot, wm, t, hk);
+        for (int i = 0; i < F; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, fa[i], fb[j], acc[i][j]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] = mma16(F16Tag{}, fa[i], fb[j], acc[i][j]);
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+          for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, fa[i], gb[j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+          for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, ga[i], fb[j], acc[i][j]);
+      } else {
+#pragma unroll
+        for (int hk = 0; hk < 2; ++hk) {
+#pragma unroll
+          for (int t = 0; t < F; ++t) {
+            fb[t] = frag(sb + slot, wn, t, hk);
+            fa[t] = frag(sa + slot, wm, t, hk);
+          }
+#pragma unroll
+          for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, fa[i], fb[j], acc[i][j]);
+        }
       }
     }
-    wait_vm<0>();
+    gemm_wait_vm<0>();
     wait_lgkm0();
     __builtin_amdgcn_s_barrier();
   }
-
   __device__ static inline int swz(int r) { return (r & 3) | (((r >> 3) & 1) << 2); }
-  __device__ static inline i32x2 read_tr(uint32_t at) {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at);
-    return __builtin_bit_cast(i32x2, v);
-  }
-  // First row (of four) and column of accumulator (i, j).
-  __device__ static inline int row_of(int i) {
-    return 64 * (int)(threadIdx.x >> 7) + 16 * i + 4 * (int)((threadIdx.x & 63) >> 4);
-  }
-  __device__ static inline int col_of(int j) { return 64 * (int)((threadIdx.x >> 6) & 1) + 16 * j + (int)(threadIdx.x & 15); }
 };
 
-// Descriptor of rows [r0, rows) of a matrix with row stride ld halves.
+// The same of 256 x 256 tiles, through the block-tile cores: one workgroup a CU, 128 x 128 a wave,
+// which halves the LDS reads of a product.  PAIRS: the three products one after another.
+template <bool KMAJOR, bool PAIRS>
+struct MuonCoreBig : std::conditional<KMAJOR, GemmCoreT<F16Tag>, GemmCore<F16Tag>>::type {
+  static constexpr int F = 8;
+  typedef GemmSmem Smem;
+
+  __device__ inline void product(GemmSmem& sm, const i32x4& a_hi, const i32x4& a_lo, const i32x4& b_hi, const i32x4& b_lo,
+                                 int32_t ld, int n_k) {
+    const int n_st = (n_k + 63) / 64;
+    this->zero();
+    i32x4 da = uniform_desc(a_hi), db = uniform_desc(b_hi);
+#pragma unroll 1
+    for (int k = 0;; ++k) {
+      if constexpr (KMAJOR) this->run(sm, da, db, ld, n_st);
+      else this->run(sm, da, ld, db, ld, n_st);
+      if (!PAIRS || k == 2) break;
+      da = uniform_desc(k == 1 ? a_lo : a_hi);
+      db = uniform_desc(k == 0 ? b_lo : b_hi);
+    }
+  }
+};
+
+template <bool BIG, bool KMAJOR, bool PAIRS>
+struct CoreOf {
+  typedef typename std::conditional<BIG, MuonCoreBig<KMAJOR, PAIRS>, MuonCore<KMAJOR, PAIRS>>::type type;
+  static constexpr int tile = BIG ? 256 : 128;
+};
+
+// Descriptor of rows [r0, rows) of a matrix with row stride ld halves, of a tile.
+template <int TILE>
 __device__ inline i32x4 rows_desc(const char* p, int32_t ld, int32_t r0, int32_t rows) {
-  const int32_t n = rows - r0 < MT ? rows - r0 : MT;
+  const int32_t n = rows - r0 < TILE ? rows - r0 : TILE;
   return make_desc(p + (int64_t)r0 * ld * 2, (uint32_t)n * (uint32_t)ld * 2u);
 }
 // Descriptor of a matrix of `rows` K-rows from column c0.
@@ -303,159 +345,292 @@ __device__ inline void upper_tile(uint32_t t, int& ti, int& tj) {
   ti = wave_uniform((int)(t - (uint32_t)j * (uint32_t)(j + 1) / 2));
 }
 
-// Writes a symmetric matrix's tile and its mirror image; columns from S to ld are zeros.
-// value(row, col, sum): what is stored.
-template <bool PAIRS, typename F>
-__device__ inline void put_symmetric(const MuonGroup& q, char* to, int ti, int tj, const f32x4 (&acc)[4][4], F value) {
-  _Float16* const o = reinterpret_cast<_Float16*>(to);
+// ----------------------------------------------------------------------------
+// a tile's way out
+// ----------------------------------------------------------------------------
+// A wave's 16F x 16F sums go through its own part of LDS, 32 of C's columns at a time, so that
+// memory is read and written in runs of rows: eight neighbouring rows m of one column n in a
+// lane, or eight columns n of one row m.
+template <int F>
+struct Stage {
+  static constexpr int W = 16 * F, PITCH = W + 4, LANES = W / 8, PER = 64 / LANES;
+  float* st;
+  int lane;
+  __device__ inline Stage(void* smem) {
+    st = reinterpret_cast<float*>(smem) + wave_uniform((int)(threadIdx.x >> 6)) * 32 * PITCH;
+    lane = threadIdx.x & 63;
+  }
+  // Columns 32 jp .. 32 jp + 31 of the wave's sums.
+  __device__ inline void put(const f32x4 (&acc)[F][F], int jp) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = ti * MT + MuonCore<false>::row_of(i), c = tj * MT + MuonCore<false>::col_of(j);
-      float x[4];
+      for (int i = 0; i < F; ++i)
+        *reinterpret_cast<f32x4*>(st + (16 * jj + (lane & 15)) * PITCH + 16 * i + 4 * (lane >> 4)) = acc[i][2 * jp + jj];
+  }
+  // Eight rows from m() of column n(k), k below 32 / PER.
+  __device__ inline int n(int k) const { return k * PER + lane / LANES; }
+  __device__ inline int m() const { return lane % LANES * 8; }
+  __device__ inline void get(int k, float (&x)[8]) const {
+    const f32x4* p = reinterpret_cast<const f32x4*>(st + n(k) * PITCH + m());
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = r + e < q.S && c < q.S ? value(r + e, c, acc[i][j][e]) : 0.f;
-      if (c < q.S && r < q.ld) put_halves4<PAIRS>(o + (int64_t)c * q.ld + r, q.lo_s, x);
-      if (ti == tj) continue;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (r + e < q.S && c < q.ld) put_halves<PAIRS>(o + (int64_t)(r + e) * q.ld + c, q.lo_s, x[e]);
-    }
+      for (int e = 0; e < 4; ++e) x[4 * h + e] = p[h][e];
+  }
+  __device__ inline void keep(int k, const float (&x)[8]) {
+    f32x4* p = reinterpret_cast<f32x4*>(st + n(k) * PITCH + m());
+#pragma unroll
+    for (int h = 0; h < 2; ++h) p[h] = f32x4{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+  }
+  // Eight columns from tn() of row tm(k), k below F.
+  __device__ inline int tn() const { return lane % 4 * 8; }
+  __device__ inline int tm(int k) const { return k * 16 + lane / 4; }
+  __device__ inline void turned(int k, float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = st[(tn() + e) * PITCH + tm(k)];
+  }
+};
+// First row and column of a wave's sums within its tile.
+template <int F>
+__device__ inline int wave_row() { return 16 * F * (int)wave_uniform(threadIdx.x >> 7); }
+template <int F>
+__device__ inline int wave_col() { return 16 * F * (int)wave_uniform((threadIdx.x >> 6) & 1); }
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+template <bool PAIRS>
+__device__ inline void put_halves8(_Float16* hi, int64_t lo, const float (&x)[8]) {
+  half8 h, l;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    h[e] = (_Float16)x[e];
+    l[e] = (_Float16)(x[e] - (float)h[e]);
+  }
+  *reinterpret_cast<half8*>(hi) = h;
+  if (PAIRS) *reinterpret_cast<half8*>(reinterpret_cast<char*>(hi) + lo) = l;
+}
+template <bool PAIRS>
+__device__ inline void get_halves8(const _Float16* hi, int64_t lo, float (&x)[8]) {
+  const half8 h = *reinterpret_cast<const half8*>(hi);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
+  if (PAIRS) {
+    const half8 l = *reinterpret_cast<const half8*>(reinterpret_cast<const char*>(hi) + lo);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] += (float)l[e];
+  }
 }
 
-template <bool PAIRS, bool KMAJOR, typename Desc>
-__device__ inline void products(MuonCore<KMAJOR>& core, MuonSmem& sm, int32_t ld, int n_st, int64_t lo_a, int64_t lo_b, Desc desc) {
-  core.zero();
-  core.run(sm, desc(0, (int64_t)0), desc(1, (int64_t)0), ld, n_st);
-  if (PAIRS) {
-    core.run(sm, desc(0, (int64_t)0), desc(1, lo_b), ld, n_st);
-    core.run(sm, desc(0, lo_a), desc(1, (int64_t)0), ld, n_st);
+// A symmetric matrix's tile and its mirror image; columns from S to ld are zeros.  value(r, c, x)
+// turns the sums of eight rows from r of column c into what is stored.
+template <bool PAIRS, int F, typename V>
+__device__ inline void put_symmetric(const MuonGroup& q, char* to, void* smem, int ti, int tj, const f32x4 (&acc)[F][F], V value) {
+  _Float16* const o = reinterpret_cast<_Float16*>(to);
+  Stage<F> st(smem);
+  const int r0 = ti * 32 * F + wave_row<F>(), c0 = tj * 32 * F + wave_col<F>();
+#pragma unroll
+  for (int jp = 0; jp < F / 2; ++jp) {
+    st.put(acc, jp);
+#pragma unroll 2
+    for (int k = 0; k < 32 / Stage<F>::PER; ++k) {
+      const int r = r0 + st.m(), c = c0 + 32 * jp + st.n(k);
+      float x[8];
+      st.get(k, x);
+      if (c < q.S && r < q.ld) value(r, c, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = c < q.S && r + e < q.S ? x[e] : 0.f;
+      if (c < q.S && r < q.ld) put_halves8<PAIRS>(o + (int64_t)c * q.ld + r, q.lo_s, x);
+      if (ti != tj) st.keep(k, x);
+    }
+    if (ti != tj) {
+#pragma unroll 2
+      for (int k = 0; k < F; ++k) {
+        const int r = r0 + st.tm(k), c = c0 + 32 * jp + st.tn();
+        float x[8];
+        st.turned(k, x);
+        if (r < q.S && c < q.ld) put_halves8<PAIRS>(o + (int64_t)r * q.ld + c, q.lo_s, x);
+      }
+    }
   }
 }
 
 // A = Y^T Y
-template <bool PAIRS>
-__global__ __launch_bounds__(256, 2) void muon_gram_kernel(MuonArgs a, int from) {
-  __shared__ MuonSmem sm;
+template <bool BIG, bool PAIRS>
+__global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_gram_kernel(MuonArgs a, int from) {
+  typedef CoreOf<BIG, true, PAIRS> C;
+  __shared__ typename C::type::Smem sm;
   const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_sym; });
   const uint32_t at = blockIdx.x - q.tile_sym, i = wave_uniform(at / q.n_sym);
   char* const base = q.base + i * q.stride;
   int ti, tj;
   upper_tile(at - i * q.n_sym, ti, tj);
-  MuonCore<true> core;
-  products<PAIRS>(core, sm, q.ld, (q.L + 63) / 64, q.lo_y, q.lo_y, [&](int b, int64_t lo) {
-    return cols_desc(base + q.y[from] + lo, q.ld, (b ? tj : ti) * MT, q.L);
+  const char* const y = base + q.y[from];
+  typename C::type core;
+  core.product(sm, cols_desc(y, q.ld, ti * C::tile, q.L), cols_desc(y + q.lo_y, q.ld, ti * C::tile, q.L),
+           cols_desc(y, q.ld, tj * C::tile, q.L), cols_desc(y + q.lo_y, q.ld, tj * C::tile, q.L), q.ld, q.L);
+  put_symmetric<PAIRS>(q, base + q.gram, &sm, ti, tj, core.acc, [](int, int, float(&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= 1.f / kScale;
   });
-  put_symmetric<PAIRS>(q, base + q.gram, ti, tj, core.acc,
-                       [](int, int, float v) { return v * (1.f / kScale); });
 }
 
 // B = b A + c A A
-template <bool PAIRS>
-__global__ __launch_bounds__(256, 2) void muon_poly_kernel(MuonArgs a) {
-  __shared__ MuonSmem sm;
+template <bool BIG, bool PAIRS>
+__global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_poly_kernel(MuonArgs a) {
+  typedef CoreOf<BIG, false, PAIRS> C;
+  __shared__ typename C::type::Smem sm;
   const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_sym; });
   const uint32_t at = blockIdx.x - q.tile_sym, i = wave_uniform(at / q.n_sym);
   char* const base = q.base + i * q.stride;
   int ti, tj;
   upper_tile(at - i * q.n_sym, ti, tj);
-  MuonCore<false> core;
-  products<PAIRS>(core, sm, q.ld, q.ld / 64, q.lo_s, q.lo_s, [&](int b, int64_t lo) {
-    return rows_desc(base + q.gram + lo, q.ld, (b ? tj : ti) * MT, q.S);
-  });
-  const _Float16* const g = reinterpret_cast<const _Float16*>(base + q.gram);
-  put_symmetric<PAIRS>(q, base + q.poly, ti, tj, core.acc, [&](int r, int c, float v) {
-    const _Float16* const p = g + (int64_t)c * q.ld + r;  // A is symmetric
-    float x = (float)*p;
-    if (PAIRS) x += (float)*reinterpret_cast<const _Float16*>(reinterpret_cast<const char*>(p) + q.lo_s);
-    return x * (kNsB * kScalePoly / kScale) + v * (kNsC * kScalePoly / (kScale * kScale));
-  });
-}
-
-// Sums of B Y^T's tile (rows: Y's columns, columns: Y's rows), and Y's new values from them.
-template <bool PAIRS>
-__device__ inline void apply_tile(const MuonGroup& q, char* base, int from, int ts, int tl, MuonCore<false>& core, MuonSmem& sm) {
-  products<PAIRS>(core, sm, q.ld, q.ld / 64, q.lo_s, q.lo_y, [&](int b, int64_t lo) {
-    return b ? rows_desc(base + q.y[from] + lo, q.ld, tl * MT, q.L)
-             : rows_desc(base + q.poly + lo, q.ld, ts * MT, q.S);
-  });
-}
-template <bool PAIRS>
-__device__ inline void new_y(const MuonGroup& q, const _Float16* y, const f32x4& sum, float (&x)[4]) {
-  get_halves4<PAIRS>(y, q.lo_y, x);
+  const char* const g = base + q.gram;
+  typename C::type core;
+  core.product(sm, rows_desc<C::tile>(g, q.ld, ti * C::tile, q.S), rows_desc<C::tile>(g + q.lo_s, q.ld, ti * C::tile, q.S),
+           rows_desc<C::tile>(g, q.ld, tj * C::tile, q.S), rows_desc<C::tile>(g + q.lo_s, q.ld, tj * C::tile, q.S), q.ld, q.ld);
+  put_symmetric<PAIRS>(q, base + q.poly, &sm, ti, tj, core.acc, [&](int r, int c, float(&x)[8]) {
+    float v[8];
+    get_halves8<PAIRS>(reinterpret_cast<const _Float16*>(g) + (int64_t)c * q.ld + r, q.lo_s, v);  // A is symmetric
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = kNsA * x[e] + sum[e] * (1.f / kScalePoly);
-}
-__device__ inline void full_tile(const MuonGroup& q, uint32_t at, uint32_t& i, int& ts, int& tl) {
-  i = wave_uniform(at / q.n_full);
-  const uint32_t t = at - i * q.n_full, across = (uint32_t)(q.S + MT - 1) / MT;
-  tl = wave_uniform((int)(t / across));
-  ts = (int)(t - (uint32_t)tl * across);
+    for (int e = 0; e < 8; ++e) x[e] = v[e] * (kNsB * kScalePoly / kScale) + x[e] * (kNsC * kScalePoly / (kScale * kScale));
+  });
 }
 
-// Y = a Y + Y B, into the other buffer
-template <bool PAIRS>
-__global__ __launch_bounds__(256, 2) void muon_apply_kernel(MuonArgs a, int from) {
-  __shared__ MuonSmem sm;
-  const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_full; });
+// Sums of B Y^T's tile: rows are Y's columns (s), columns its rows (l).
+template <bool BIG, bool PAIRS>
+struct ApplyTile {
+  typedef CoreOf<BIG, false, PAIRS> C;
+  const MuonGroup& q;
   uint32_t i;
   int ts, tl;
-  full_tile(q, blockIdx.x - q.tile_full, i, ts, tl);
-  char* const base = q.base + i * q.stride;
-  MuonCore<false> core;
-  apply_tile<PAIRS>(q, base, from, ts, tl, core, sm);
-  const _Float16* const y = reinterpret_cast<const _Float16*>(base + q.y[from]);
-  _Float16* const o = reinterpret_cast<_Float16*>(base + q.y[1 - from]);
+  char* base;
+  __device__ inline ApplyTile(const MuonArgs& a) : q(group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_full; })) {
+    const uint32_t at = blockIdx.x - q.tile_full;
+    i = wave_uniform(at / q.n_full);
+    const uint32_t t = at - i * q.n_full, across = (uint32_t)(q.S + C::tile - 1) / C::tile;
+    tl = wave_uniform((int)(t / across));
+    ts = wave_uniform((int)(t - (uint32_t)tl * across));
+    base = q.base + i * q.stride;
+  }
+  __device__ inline void run(typename C::type& core, typename C::type::Smem& sm, int from) const {
+    const char *y = base + q.y[from], *b = base + q.poly;
+    core.product(sm, rows_desc<C::tile>(b, q.ld, ts * C::tile, q.S), rows_desc<C::tile>(b + q.lo_s, q.ld, ts * C::tile, q.S),
+             rows_desc<C::tile>(y, q.ld, tl * C::tile, q.L), rows_desc<C::tile>(y + q.lo_y, q.ld, tl * C::tile, q.L), q.ld, q.ld);
+  }
+  // a Y + Y B of eight columns of a row of Y
+  __device__ inline void value(const _Float16* y, float (&x)[8]) const {
+    float v[8];
+    get_halves8<PAIRS>(y, q.lo_y, v);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int l = tl * MT + core.col_of(j);
-    if (l >= q.L) continue;
+    for (int e = 0; e < 8; ++e) x[e] = kNsA * v[e] + x[e] * (1.f / kScalePoly);
+  }
+};
+
+// Y = a Y + Y B, into the other buffer
+template <bool BIG, bool PAIRS>
+__global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_apply_kernel(MuonArgs a, int from) {
+  typedef CoreOf<BIG, false, PAIRS> C;
+  constexpr int F = C::type::F;
+  __shared__ typename C::type::Smem sm;
+  const ApplyTile<BIG, PAIRS> t(a);
+  const MuonGroup& q = t.q;
+  typename C::type core;
+  t.run(core, sm, from);
+  const _Float16* const y = reinterpret_cast<const _Float16*>(t.base + q.y[from]);
+  _Float16* const o = reinterpret_cast<_Float16*>(t.base + q.y[1 - from]);
+  Stage<F> st(&sm);
+  const int s = t.ts * C::tile + wave_row<F>() + st.m(), l0 = t.tl * C::tile + wave_col<F>();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int s = ts * MT + core.row_of(k);
-      if (s >= q.ld) continue;
-      float x[4];
-      new_y<PAIRS>(q, y + (int64_t)l * q.ld + s, core.acc[k][j], x);
-      put_halves4<PAIRS>(o + (int64_t)l * q.ld + s, q.lo_y, x);
+  for (int jp = 0; jp < F / 2; ++jp) {
+    st.put(core.acc, jp);
+#pragma unroll 2
+    for (int k = 0; k < 32 / Stage<F>::PER; ++k) {
+      const int l = l0 + 32 * jp + st.n(k);
+      if (l >= q.L || s >= q.ld) continue;
+      float x[8];
+      st.get(k, x);
+      t.value(y + (int64_t)l * q.ld + s, x);
+      put_halves8<PAIRS>(o + (int64_t)l * q.ld + s, q.lo_y, x);
+    }
+  }
+}
+
+// The step of n of eight neighbouring weights from p on.
+template <typename P, bool MASTER>
+__device__ inline void step8(P* p, float* master, const float (&x)[8], int n, float lr, float lr_wd) {
+  if (n >= 8) {
+    float w[8];
+    if constexpr (MASTER) {
+      Raw<float, 8> in;
+      in.load(master);
+      in.get(w);
+    } else {
+      Raw<P, 8> in;
+      in.load(p);
+      in.get(w);
+    }
+    Raw<P, 8> out;
+    Raw<float, 8> wide;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = stepped(w[e], x[e] * (1.f / kScale), lr, lr_wd);
+      out.set(e, (P)w[e]);
+      if (MASTER) wide.set(e, w[e]);
+    }
+    if constexpr (MASTER) wide.store(master);
+    out.store(p);
+  } else {
+    for (int e = 0; e < n; ++e) {
+      const float w = stepped(MASTER ? master[e] : (float)p[e], x[e] * (1.f / kScale), lr, lr_wd);
+      if (MASTER) master[e] = w;
+      p[e] = (P)w;
     }
   }
 }
 
 // The last product and the weights' step.
-template <bool PAIRS, typename P, bool MASTER>
-__global__ __launch_bounds__(256, 2) void muon_last_kernel(MuonArgs a, int from) {
-  __shared__ MuonSmem sm;
-  const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_full; });
-  uint32_t i;
-  int ts, tl;
-  full_tile(q, blockIdx.x - q.tile_full, i, ts, tl);
-  char* const base = q.base + i * q.stride;
-  MuonCore<false> core;
-  apply_tile<PAIRS>(q, base, from, ts, tl, core, sm);
-  const _Float16* const y = reinterpret_cast<const _Float16*>(base + q.y[from]);
-  const MuonEntry& en = a.table[q.entry + i];
+template <bool BIG, bool PAIRS, typename P, bool MASTER>
+__global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_last_kernel(MuonArgs a, int from) {
+  typedef CoreOf<BIG, false, PAIRS> C;
+  constexpr int F = C::type::F;
+  __shared__ typename C::type::Smem sm;
+  const ApplyTile<BIG, PAIRS> t(a);
+  const MuonGroup& q = t.q;
+  typename C::type core;
+  t.run(core, sm, from);
+  const _Float16* const y = reinterpret_cast<const _Float16*>(t.base + q.y[from]);
+  const MuonEntry& en = a.table[q.entry + t.i];
   P* const p = (P*)en.p;
   const float lr = en.lr, lr_wd = en.lr_wd;
   const bool turned = q.rows < q.cols;
+  Stage<F> st(&sm);
+  const int s0 = t.ts * C::tile + wave_row<F>(), l0 = t.tl * C::tile + wave_col<F>(), s = s0 + st.m();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int l = tl * MT + core.col_of(j);
-    if (l >= q.L) continue;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int s = ts * MT + core.row_of(k);
-      if (s >= q.S) continue;
-      float x[4];
-      new_y<PAIRS>(q, y + (int64_t)l * q.ld + s, core.acc[k][j], x);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (s + e >= q.S) continue;
-        const int64_t at = turned ? (int64_t)(s + e) * q.cols + l : (int64_t)l * q.cols + s + e;
-        const float w = MASTER ? en.master[at] : (float)p[at];
-        const float nw = stepped(w, x[e] * (1.f / kScale), lr, lr_wd);
-        if (MASTER) en.master[at] = nw;
-        p[at] = (P)nw;
+  for (int jp = 0; jp < F / 2; ++jp) {
+    st.put(core.acc, jp);
+#pragma unroll 2
+    for (int k = 0; k < 32 / Stage<F>::PER; ++k) {
+      const int l = l0 + 32 * jp + st.n(k);
+      if (l >= q.L || s >= q.S) continue;
+      float x[8];
+      st.get(k, x);
+      t.value(y + (int64_t)l * q.ld + s, x);
+      if (turned) {
+        st.keep(k, x);
+      } else {
+        const int64_t at = (int64_t)l * q.cols + s;
+        step8<P, MASTER>(p + at, MASTER ? en.master + at : nullptr, x, q.S - s, lr, lr_wd);
+      }
+    }
+    if (turned) {
+#pragma unroll 2
+      for (int k = 0; k < F; ++k) {
+        const int r = s0 + st.tm(k), l = l0 + 32 * jp + st.tn();
+        if (r >= q.S || l >= q.L) continue;
+        float x[8];
+        st.turned(k, x);
+        const int64_t at = (int64_t)r * q.cols + l;
+        step8<P, MASTER>(p + at, MASTER ? en.master + at : nullptr, x, q.L - l, lr, lr_wd);
       }
     }
   }
@@ -466,6 +641,14 @@ hipError_t with_pairs(bool pairs, F f) {
   if (pairs) f(std::true_type{});
   else f(std::false_type{});
   return hipGetLastError();
+}
+
+template <typename F>
+hipError_t with_both(bool big, bool pairs, F f) {
+  return with_pairs(pairs, [&](auto pr) {
+    if (big) f(std::true_type{}, pr);
+    else f(std::false_type{}, pr);
+  });
 }
 
 }  // namespace
@@ -487,27 +670,29 @@ hipError_t launch_muon_split(int g_dtype, bool pairs, const MuonArgs& a, uint32_
     });
   });
 }
-hipError_t launch_muon_gram(bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
-  return with_pairs(pairs, [&](auto pr) {
-    hipLaunchKernelGGL((muon_gram_kernel<decltype(pr)::value>), dim3(blocks), dim3(256), 0, s, a, from);
+hipError_t launch_muon_gram(bool big, bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
+  return with_both(big, pairs, [&](auto b, auto pr) {
+    hipLaunchKernelGGL((muon_gram_kernel<decltype(b)::value, decltype(pr)::value>), dim3(blocks), dim3(256), 0, s, a, from);
   });
 }
-hipError_t launch_muon_poly(bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
-  return with_pairs(pairs, [&](auto pr) {
-    hipLaunchKernelGGL((muon_poly_kernel<decltype(pr)::value>), dim3(blocks), dim3(256), 0, s, a);
+hipError_t launch_muon_poly(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
+  return with_both(big, pairs, [&](auto b, auto pr) {
+    hipLaunchKernelGGL((muon_poly_kernel<decltype(b)::value, decltype(pr)::value>), dim3(blocks), dim3(256), 0, s, a);
   });
 }
-hipError_t launch_muon_apply(bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
-  return with_pairs(pairs, [&](auto pr) {
-    hipLaunchKernelGGL((muon_apply_kernel<decltype(pr)::value>), dim3(blocks), dim3(256), 0, s, a, from);
+hipError_t launch_muon_apply(bool big, bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
+  return with_both(big, pairs, [&](auto b, auto pr) {
+    hipLaunchKernelGGL((muon_apply_kernel<decltype(b)::value, decltype(pr)::value>), dim3(blocks), dim3(256), 0, s, a, from);
   });
 }
-hipError_t launch_muon_last(bool pairs, int p_dtype, bool master, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
+hipError_t launch_muon_last(bool big, bool pairs, int p_dtype, bool master, int from, const MuonArgs& a, uint32_t blocks,
+                            hipStream_t s) {
   return with_type(p_dtype, [&](auto p) {
     typedef decltype(p) T;
-    return with_pairs(pairs, [&](auto pr) {
-      if (master) hipLaunchKernelGGL((muon_last_kernel<decltype(pr)::value, T, true>), dim3(blocks), dim3(256), 0, s, a, from);
-      else hipLaunchKernelGGL((muon_last_kernel<decltype(pr)::value, T, false>), dim3(blocks), dim3(256), 0, s, a, from);
+    return with_both(big, pairs, [&](auto b, auto pr) {
+      constexpr bool B = decltype(b)::value, R = decltype(pr)::value;
+      if (master) hipLaunchKernelGGL((muon_last_kernel<B, R, T, true>), dim3(blocks), dim3(256), 0, s, a, from);
+      else hipLaunchKernelGGL((muon_last_kernel<B, R, T, false>), dim3(blocks), dim3(256), 0, s, a, from);
     });
   });
 }

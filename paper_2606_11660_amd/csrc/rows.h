@@ -64,6 +64,10 @@ struct Raw {
 #pragma unroll
     for (int k = 0; k < N / W; ++k) v[k] = *reinterpret_cast<const vec*>(p + k * W);
   }
+  __device__ inline void store(T* p) const {
+#pragma unroll
+    for (int k = 0; k < N / W; ++k) *reinterpret_cast<vec*>(p + k * W) = v[k];
+  }
   __device__ inline void get(float (&x)[N]) const {
 #pragma unroll
     for (int e = 0; e < N; ++e) x[e] = (float)at(e);
@@ -93,8 +97,7 @@ __device__ inline void store_n(T* row, Cols<N> c, const float (&x)[N]) {
 #pragma unroll
   for (int e = 0; e < N; ++e) r.set(e, (T)x[e]);
   if (c.skip == 0) {
-#pragma unroll
-    for (int k = 0; k < N / Raw<T, N>::W; ++k) *reinterpret_cast<typename Raw<T, N>::vec*>(row + c.at + k * Raw<T, N>::W) = r.v[k];
+    r.store(row + c.at);
   } else if (c.skip < N) {
 #pragma unroll
     for (int e = 1; e < N; ++e)

@@ -136,7 +136,7 @@ def test_steps(steps):
 
 def test_larger_matrices():
     """Several tiles each way, and their products' longer sums; singular values near one."""
-    for shape in ((1030, 520), (640, 1537)):
+    for shape in ((1030, 520), (640, 1537), (1100, 1030), (1025, 1800)):
         M = Model(8, [shape], zero=True)
         N = Model(8, [shape], zero=True)
         P.attr_muon_step(M.plan(), -1.0)
