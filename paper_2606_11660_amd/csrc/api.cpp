@@ -1178,20 +1178,41 @@ MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
   size_t most = 0, matrices = 0;
   const auto end = [&] {
     if (R.order.empty()) return;
+    for (int k = 0; k < R.args.n_groups; ++k) {
+      attr::MuonGroup& q = R.args.g[k];
+      q.tile_sym = R.sym;
+      q.tile_full = R.full;
+      R.sym += attr::muon_tiles(q.n_sym * q.count);
+      R.full += attr::muon_tiles(q.n_full * q.count);
+    }
     most = std::max(most, R.bytes);
     matrices = std::max(matrices, R.order.size());
     P.rounds.push_back(R);
     clear();
   };
   clear();
-  for (const auto& sh : shapes) {
-    const int kind = std::get<0>(sh.first);
-    attr::MuonGroup q = kind < kTiles ? thin_group(std::get<1>(sh.first), std::get<2>(sh.first))
-                                      : muon_group(std::get<1>(sh.first), std::get<2>(sh.first), pairs, kind == kBigTiles);
+  // the workgroups of the tile kinds' launches, from their groups' numbers of matrices
+  const auto tiles = [](const MuonRound& r, uint32_t attr::MuonGroup::*each) {
+    uint32_t n = 0;
+    for (int k = 0; k < r.args.n_groups; ++k) n += attr::muon_tiles(r.args.g[k].*each * r.args.g[k].count);
+    return n;
+  };
+  // long products first: what is left at a launch's end is short
+  std::vector<const std::pair<const std::tuple<int, int64_t, int64_t>, std::vector<int32_t>>*> order;
+  for (const auto& sh : shapes) order.push_back(&sh);
+  std::stable_sort(order.begin(), order.end(), [](const auto* x, const auto* y) {
+    const auto side = [](const auto* s) { return std::max(std::get<1>(s->first), std::get<2>(s->first)); };
+    return std::make_tuple(std::get<0>(x->first), -side(x)) < std::make_tuple(std::get<0>(y->first), -side(y));
+  });
+  for (const auto* sh : order) {
+    const int kind = std::get<0>(sh->first);
+    attr::MuonGroup q = kind < kTiles ? thin_group(std::get<1>(sh->first), std::get<2>(sh->first))
+                                      : muon_group(std::get<1>(sh->first), std::get<2>(sh->first), pairs, kind == kBigTiles);
     if (!R.order.empty() && R.kind != kind) end();
     bool open = false;
-    for (int32_t j : sh.second) {
-      if (!R.order.empty() && (R.full + q.n_full > kMuonRoundTiles || R.flat + q.n_flat > kMuonRoundFlat || R.bytes + (size_t)q.stride > kMuonRoundBytes ||
+    for (int32_t j : sh->second) {
+      if (!R.order.empty() && (tiles(R, &attr::MuonGroup::n_full) > kMuonRoundTiles || R.flat + q.n_flat > kMuonRoundFlat ||
+                               R.bytes + (size_t)q.stride > kMuonRoundBytes ||
                                (!open && R.args.n_groups == attr::kMuonGroups))) {
         end();
         open = false;
@@ -1199,17 +1220,14 @@ MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
       R.kind = kind;
       if (!open) {
         q.base = reinterpret_cast<char*>(R.bytes);  // behind the table
-        q.tile_sym = R.sym;
-        q.tile_full = R.full;
         q.tile_flat = R.flat;
         q.tile_turn = R.turn;
         q.entry = (uint32_t)R.order.size();
         R.args.g[R.args.n_groups++] = q;
         open = true;
       }
+      ++R.args.g[R.args.n_groups - 1].count;
       R.order.push_back(j);
-      R.sym += q.n_sym;
-      R.full += q.n_full;
       R.flat += q.n_flat;
       R.turn += q.n_turn;
       R.bytes += (size_t)q.stride;

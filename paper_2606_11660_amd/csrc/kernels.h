@@ -423,9 +423,11 @@ struct MuonGroup {
   int64_t lo_y, lo_s;     // from the first halves to the second: of Y; of gram and poly
   uint32_t tile_sym, tile_full, tile_flat, tile_turn;  // first workgroup of the group in each launch
   uint32_t n_sym, n_full, n_flat, n_turn;              // workgroups of a matrix
-  uint32_t entry;         // first matrix in the table
+  uint32_t entry, count;  // first matrix in the table, matrices
   int32_t rows, cols, L, S, ld;
 };
+// Workgroups of a group's n tiles: an eighth for each die.
+inline uint32_t muon_tiles(uint32_t n) { return (n + 7) / 8 * 8; }
 constexpr int kMuonGroups = 16;
 struct MuonArgs {
   const MuonEntry* table;

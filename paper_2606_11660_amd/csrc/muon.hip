@@ -1,17 +1,17 @@
 // One Muon step over many matrices (attr_muon_step).
 //
 //     m = mu m + (1 - mu) g',   u = mu m + (1 - mu) g' (nesterov) or m
-//     X = u / |u|_F;  five times:  A = X X^T,  B = b A + c A^2,  X = a X + B X
+//     X = u / |u|_F;  five times:  A = X X^T,  B = a I + b A + c A^2,  X = B X
 //     w = w - lr wd w - lr X
 //
 // Bound by the matrix cores: with s and t a matrix's shorter and longer side, s^2 t + s^3 +
 // 2 s^2 t flops a step of the iteration, since A and B are symmetric and only their upper
 // triangles of tiles are computed.  The iteration holds Y, the update with its longer side
-// first ([t][s]; A = Y^T Y, Y = a Y + Y B), so that Y is stored once and in one order: A reads
+// first ([t][s]; A = Y^T Y, Y = Y B), so that Y is stored once and in one order: A reads
 // it along its columns (transposing LDS reads), Y B along its rows.
 //
 // Operands are fp16 with powers of two before them: no entry of X passes 1.21, of A 1.45 or of
-// B 2.9 (|p(x)| <= 1.2025 on [0, 1.2025] for p = a x + b x^3 + c x^5), so 2^15 X, 2^15 A and
+// B 3.45 (|p(x)| <= 1.2025 on [0, 1.2025] for p = a x + b x^3 + c x^5), so 2^15 X, 2^15 A and
 // 2^14 B fit, and what is below 2^-24 of the largest entry is still held.  fp16 keeps 11 bits where
 // bf16 keeps 8, at the same rate.  With pairs every operand is two fp16 values (22 bits) and a
 // product three: hi hi + hi lo + lo hi.  Sums are fp32, the norm's fp64.
@@ -124,17 +124,25 @@ __global__ __launch_bounds__(256) void muon_split_kernel(MuonArgs a) {
   const bool turned = q.rows < q.cols;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   _Float16* const y = reinterpret_cast<_Float16*>(base + q.y[0]);
-#pragma unroll 4
-  for (int k = wave; k < 64; k += 4) {
-    const int r = turned ? s0 + k : l0 + k, c = turned ? l0 + lane : s0 + lane;
-    float x = 0.f;
-    if (r < q.rows && c < q.cols) {
+  // four neighbouring elements of the matrix a lane
+  const int r0 = turned ? s0 : l0, c = (turned ? l0 : s0) + lane % 16 * 4;
+  const int n = q.cols - c;
+#pragma unroll
+  for (int k = wave * 4 + lane / 16; k < 64; k += 16) {
+    const int r = r0 + k;
+    float m[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f};
+    if (r < q.rows && n > 0) {
       const int64_t e = (int64_t)r * q.cols + c;
-      const float g = (float)((const G*)en.g)[e] * gs;
-      x = (float)((double)update_of(a, en.m[e], g) * inv);
+      load4(en.m + e, n, m);
+      load4((const G*)en.g + e, n, g);
     }
-    if (turned) tile[lane][k] = x;
-    else tile[k][lane] = x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = (float)((double)update_of(a, m[e], g[e] * gs) * inv);
+      const float there = r < q.rows && e < n ? x : 0.f;
+      if (turned) tile[lane % 16 * 4 + e][k] = there;
+      else tile[k][lane % 16 * 4 + e] = there;
+    }
   }
   __syncthreads();
 #pragma unroll 4
@@ -345,6 +353,14 @@ __device__ inline void upper_tile(uint32_t t, int& ti, int& tj) {
   ti = wave_uniform((int)(t - (uint32_t)j * (uint32_t)(j + 1) / 2));
 }
 
+// A workgroup's tile of a group of n: workgroups go to the eight dies in turn, and each die takes
+// an eighth of the tiles, one after another, so that the operands' panels that neighbouring tiles
+// share are in its own L2.  False: the group has no such tile (its workgroups are rounded up).
+__device__ inline bool tile_of(uint32_t block, uint32_t n, uint32_t& tile) {
+  tile = (block & 7) * ((n + 7) / 8) + block / 8;
+  return block / 8 < (n + 7) / 8 && tile < n;
+}
+
 // ----------------------------------------------------------------------------
 // a tile's way out
 // ----------------------------------------------------------------------------
@@ -460,7 +476,9 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_gram_kernel(MuonArgs a,
   typedef CoreOf<BIG, true, PAIRS> C;
   __shared__ typename C::type::Smem sm;
   const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_sym; });
-  const uint32_t at = blockIdx.x - q.tile_sym, i = wave_uniform(at / q.n_sym);
+  uint32_t at;
+  if (!tile_of(blockIdx.x - q.tile_sym, q.n_sym * q.count, at)) return;
+  const uint32_t i = wave_uniform(at / q.n_sym);
   char* const base = q.base + i * q.stride;
   int ti, tj;
   upper_tile(at - i * q.n_sym, ti, tj);
@@ -474,13 +492,15 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_gram_kernel(MuonArgs a,
   });
 }
 
-// B = b A + c A A
+// B = a I + b A + c A A
 template <bool BIG, bool PAIRS>
 __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_poly_kernel(MuonArgs a) {
   typedef CoreOf<BIG, false, PAIRS> C;
   __shared__ typename C::type::Smem sm;
   const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_sym; });
-  const uint32_t at = blockIdx.x - q.tile_sym, i = wave_uniform(at / q.n_sym);
+  uint32_t at;
+  if (!tile_of(blockIdx.x - q.tile_sym, q.n_sym * q.count, at)) return;
+  const uint32_t i = wave_uniform(at / q.n_sym);
   char* const base = q.base + i * q.stride;
   int ti, tj;
   upper_tile(at - i * q.n_sym, ti, tj);
@@ -492,7 +512,10 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_poly_kernel(MuonArgs a)
     float v[8];
     get_halves8<PAIRS>(reinterpret_cast<const _Float16*>(g) + (int64_t)c * q.ld + r, q.lo_s, v);  // A is symmetric
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = v[e] * (kNsB * kScalePoly / kScale) + x[e] * (kNsC * kScalePoly / (kScale * kScale));
+    for (int e = 0; e < 8; ++e) {
+      x[e] = v[e] * (kNsB * kScalePoly / kScale) + x[e] * (kNsC * kScalePoly / (kScale * kScale));
+      if (r + e == c) x[e] += kNsA * kScalePoly;
+    }
   });
 }
 
@@ -504,8 +527,10 @@ struct ApplyTile {
   uint32_t i;
   int ts, tl;
   char* base;
+  bool there;
   __device__ inline ApplyTile(const MuonArgs& a) : q(group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_full; })) {
-    const uint32_t at = blockIdx.x - q.tile_full;
+    uint32_t at;
+    there = tile_of(blockIdx.x - q.tile_full, q.n_full * q.count, at);
     i = wave_uniform(at / q.n_full);
     const uint32_t t = at - i * q.n_full, across = (uint32_t)(q.S + C::tile - 1) / C::tile;
     tl = wave_uniform((int)(t / across));
@@ -517,26 +542,19 @@ struct ApplyTile {
     core.product(sm, rows_desc<C::tile>(b, q.ld, ts * C::tile, q.S), rows_desc<C::tile>(b + q.lo_s, q.ld, ts * C::tile, q.S),
              rows_desc<C::tile>(y, q.ld, tl * C::tile, q.L), rows_desc<C::tile>(y + q.lo_y, q.ld, tl * C::tile, q.L), q.ld, q.ld);
   }
-  // a Y + Y B of eight columns of a row of Y
-  __device__ inline void value(const _Float16* y, float (&x)[8]) const {
-    float v[8];
-    get_halves8<PAIRS>(y, q.lo_y, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = kNsA * v[e] + x[e] * (1.f / kScalePoly);
-  }
 };
 
-// Y = a Y + Y B, into the other buffer
+// Y = Y B, into the other buffer
 template <bool BIG, bool PAIRS>
 __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_apply_kernel(MuonArgs a, int from) {
   typedef CoreOf<BIG, false, PAIRS> C;
   constexpr int F = C::type::F;
   __shared__ typename C::type::Smem sm;
   const ApplyTile<BIG, PAIRS> t(a);
+  if (!t.there) return;
   const MuonGroup& q = t.q;
   typename C::type core;
   t.run(core, sm, from);
-  const _Float16* const y = reinterpret_cast<const _Float16*>(t.base + q.y[from]);
   _Float16* const o = reinterpret_cast<_Float16*>(t.base + q.y[1 - from]);
   Stage<F> st(&sm);
   const int s = t.ts * C::tile + wave_row<F>() + st.m(), l0 = t.tl * C::tile + wave_col<F>();
@@ -549,7 +567,8 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_apply_kernel(MuonArgs a
       if (l >= q.L || s >= q.ld) continue;
       float x[8];
       st.get(k, x);
-      t.value(y + (int64_t)l * q.ld + s, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= 1.f / kScalePoly;
       put_halves8<PAIRS>(o + (int64_t)l * q.ld + s, q.lo_y, x);
     }
   }
@@ -573,7 +592,7 @@ __device__ inline void step8(P* p, float* master, const float (&x)[8], int n, fl
     Raw<float, 8> wide;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      w[e] = stepped(w[e], x[e] * (1.f / kScale), lr, lr_wd);
+      w[e] = stepped(w[e], x[e] * (1.f / (kScale * kScalePoly)), lr, lr_wd);
       out.set(e, (P)w[e]);
       if (MASTER) wide.set(e, w[e]);
     }
@@ -581,7 +600,7 @@ __device__ inline void step8(P* p, float* master, const float (&x)[8], int n, fl
     out.store(p);
   } else {
     for (int e = 0; e < n; ++e) {
-      const float w = stepped(MASTER ? master[e] : (float)p[e], x[e] * (1.f / kScale), lr, lr_wd);
+      const float w = stepped(MASTER ? master[e] : (float)p[e], x[e] * (1.f / (kScale * kScalePoly)), lr, lr_wd);
       if (MASTER) master[e] = w;
       p[e] = (P)w;
     }
@@ -595,10 +614,10 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_last_kernel(MuonArgs a,
   constexpr int F = C::type::F;
   __shared__ typename C::type::Smem sm;
   const ApplyTile<BIG, PAIRS> t(a);
+  if (!t.there) return;
   const MuonGroup& q = t.q;
   typename C::type core;
   t.run(core, sm, from);
-  const _Float16* const y = reinterpret_cast<const _Float16*>(t.base + q.y[from]);
   const MuonEntry& en = a.table[q.entry + t.i];
   P* const p = (P*)en.p;
   const float lr = en.lr, lr_wd = en.lr_wd;
@@ -611,16 +630,11 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_last_kernel(MuonArgs a,
 #pragma unroll 2
     for (int k = 0; k < 32 / Stage<F>::PER; ++k) {
       const int l = l0 + 32 * jp + st.n(k);
-      if (l >= q.L || s >= q.S) continue;
+      if (turned || l >= q.L || s >= q.S) continue;
       float x[8];
       st.get(k, x);
-      t.value(y + (int64_t)l * q.ld + s, x);
-      if (turned) {
-        st.keep(k, x);
-      } else {
-        const int64_t at = (int64_t)l * q.cols + s;
-        step8<P, MASTER>(p + at, MASTER ? en.master + at : nullptr, x, q.S - s, lr, lr_wd);
-      }
+      const int64_t at = (int64_t)l * q.cols + s;
+      step8<P, MASTER>(p + at, MASTER ? en.master + at : nullptr, x, q.S - s, lr, lr_wd);
     }
     if (turned) {
 #pragma unroll 2

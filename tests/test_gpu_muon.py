@@ -8,7 +8,7 @@ carried, spread evenly over the entries where they arise:
     X rounded:  (h / 3^(1/2) |X|)^2,  h = 2^-11 or, with pairs, 2^-22
     A, B:       likewise, and fp32 sums of K products, whose roundings on the matrix cores may all
                 point one way: K / 16 2^-24 |A| (twice that with pairs, which add three products)
-    into X:     dX_ij = dB_ij s_j,  dB_ij = (b + c (s_i^2 + s_j^2)) dA_ij + B's own
+    into X:     dX_ij = dB_ij s_j,  dB_ij = (b + c (s_i^2 + s_j^2)) dA_ij + that of B = a + b A + c A^2
 The test allows four times the root of that energy.
 """
 import numpy as np
@@ -45,7 +45,7 @@ def tolerance(u, pairs, steps=5):
         gs = a + b * (x * x + x * y + y * y) + c * (x ** 4 + x ** 3 * y + x * x * y * y + x * y ** 3 + y ** 4)
         ga = a + b * (x * x - x * y + y * y) + c * (x ** 4 - x ** 3 * y + x * x * y * y - x * y ** 3 + y ** 4)
         dA = (h ** 2 + kl ** 2) * (lam ** 2).sum() / S ** 2
-        dB = (b + c * (x * x + y * y)) ** 2 * dA + (h ** 2 * (poly ** 2).sum() + (ks * c) ** 2 * (lam ** 4).sum()) / S ** 2
+        dB = (b + c * (x * x + y * y)) ** 2 * dA + (h ** 2 * ((a + poly) ** 2).sum() + (ks * c) ** 2 * (lam ** 4).sum()) / S ** 2
         into = dB * y * y
         new = (h ** 2 + ks ** 2) * (p(s) ** 2).sum()
         sym, anti = (e * g * g + into / 2 + even(new) / 2 for e, g in ((sym, gs), (anti, ga)))
