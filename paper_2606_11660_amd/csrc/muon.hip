@@ -159,9 +159,10 @@ __global__ __launch_bounds__(256) void muon_split_kernel(MuonArgs a) {
 // ----------------------------------------------------------------------------
 constexpr int MT = kMuonTile;
 constexpr uint32_t M_SLOT = MT * 128;  // bytes of an operand's stage
+constexpr int M_SLOTS = 2;  // stages of a workgroup's LDS
 struct MuonSmem {
-  i32x4 a[2][MT * 8];
-  i32x4 b[2][MT * 8];
+  i32x4 a[M_SLOTS][MT * 8];
+  i32x4 b[M_SLOTS][MT * 8];
 };
 
 // Four waves (2 x 2) hold 64 x 64 each, as 4 x 4 accumulators.  C[m][n] += sum_k A[m][k] B[n][k];
@@ -203,7 +204,7 @@ struct MuonCore {
         off[h] = (uint32_t)(row * ld * 2 + (((((s >> 1) ^ swz(row)) << 1) | (s & 1)) * 16));
       } else if constexpr (PAIRS) {
         const int row = 16 * first + (lane >> 2);
-        off[h] = (uint32_t)(row * ld * 2 + (((lane & 3) ^ ((row >> 2) & 3)) * 16));
+        off[h] = (uint32_t)(row * ld * 2 + (((lane & 3) ^ ((row >> 1) & 3)) * 16));
       } else {
         const int row = 8 * first + (lane >> 3);
         off[h] = (uint32_t)(row * ld * 2 + (((lane & 7) ^ (row & 7)) * 16));
@@ -214,7 +215,7 @@ struct MuonCore {
     const uint32_t sa = (uint32_t)(uintptr_t)&sm.a[0][0], sb = (uint32_t)(uintptr_t)&sm.b[0][0];
     const auto issue = [&](int st) {
       const bool live = st < n_st;
-      const uint32_t slot = (uint32_t)(st & 1) * M_SLOT, ko = (uint32_t)st * step;
+      const uint32_t slot = (uint32_t)(st % M_SLOTS) * M_SLOT, ko = (uint32_t)st * step;
 #pragma unroll
       for (int o = 0; o < 2; ++o) {
         const uint32_t lds = (o ? sb : sa) + slot;
@@ -246,18 +247,19 @@ struct MuonCore {
         return i32x4{lo.x, lo.y, hi.x, hi.y};
       } else {
         const uint32_t row = (uint32_t)(64 * half + 16 * t + ri);
-        const uint32_t at = PAIRS ? base + row * 64u + 16u * (uint32_t)(rg ^ ((ri >> 2) & 3))
+        const uint32_t at = PAIRS ? base + row * 64u + 16u * (uint32_t)(rg ^ ((ri >> 1) & 3))
                                   : base + row * 128u + 16u * (uint32_t)((4 * hk + rg) ^ (ri & 7));
         return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>((uintptr_t)at);
       }
     };
-    issue(0);
+#pragma unroll
+    for (int st = 0; st < M_SLOTS - 1; ++st) issue(st);
     for (int st = 0; st < n_st; ++st) {
-      gemm_wait_vm<0>();  // stage st has landed
-      wait_lgkm0();       // this wave has read stage st - 1
+      gemm_wait_vm<8 * (M_SLOTS - 2)>();  // stage st has landed: eight loads of a wave are a stage
+      wait_lgkm0();                       // this wave has read stage st - 1
       __builtin_amdgcn_s_barrier();
-      issue(st + 1);      // past the end nothing is fetched
-      const uint32_t slot = (uint32_t)(st & 1) * M_SLOT;
+      issue(st + M_SLOTS - 1);            // past the end nothing is fetched
+      const uint32_t slot = (uint32_t)(st % M_SLOTS) * M_SLOT;
       i32x4 fa[F], fb[F], ga[F], gb[F];
       if constexpr (PAIRS) {
 #pragma unroll
