@@ -159,15 +159,17 @@ __global__ __launch_bounds__(256) void muon_split_kernel(MuonArgs a) {
 // ----------------------------------------------------------------------------
 constexpr int MT = kMuonTile;
 constexpr uint32_t M_SLOT = MT * 128;  // bytes of an operand's stage
-constexpr int M_SLOTS = 2;  // stages of a workgroup's LDS
 struct MuonSmem {
-  i32x4 a[M_SLOTS][MT * 8];
-  i32x4 b[M_SLOTS][MT * 8];
+  i32x4 a[2][MT * 8];
+  i32x4 b[2][MT * 8];
 };
 
 // Four waves (2 x 2) hold 64 x 64 each, as 4 x 4 accumulators.  C[m][n] += sum_k A[m][k] B[n][k];
 // KMAJOR: of operands stored [k][m] and [k][n].  Stages (K = 64, or with PAIRS 32 of both halves)
-// go straight to LDS, one ahead, two workgroups a CU.  With PAIRS the three products of a stage
+// go straight to LDS, one ahead of the one whose fragments are read, which is one ahead of the
+// products; two workgroups a CU fill each other's waits (four slots and one workgroup: the products
+// A of 14 matrices in 75 us, so in 66).  A wave whose rows or columns are past the matrix (rows,
+// cols: what is left of it from the tile on) only loads.  With PAIRS the three products of a stage
 // share their fragments: 16 reads for 48 products, where three passes took 24.
 template <bool KMAJOR, bool PAIRS>
 struct MuonCore {
@@ -178,8 +180,8 @@ struct MuonCore {
   // K in n_k rows (KMAJOR) or values; ao and bo: the operands' first halves from the tile's first
   // row (KMAJOR: column), ld both operands' row stride, a_lo and b_lo the second halves'
   // descriptors.  What is past a descriptor's range reads as zeros.
-  __device__ inline void product(MuonSmem& sm, const i32x4& a_hi_, const i32x4& a_lo_, const i32x4& b_hi_, const i32x4& b_lo_,
-                                 int32_t ld, int n_k) {
+  __device__ inline void product(Smem& sm, const i32x4& a_hi_, const i32x4& a_lo_, const i32x4& b_hi_, const i32x4& b_lo_,
+                                 int32_t ld, int n_k, int rows, int cols) {
     const i32x4 a_hi = uniform_desc(a_hi_), a_lo = uniform_desc(a_lo_), b_hi = uniform_desc(b_hi_), b_lo = uniform_desc(b_lo_);
 #pragma unroll
     for (int i = 0; i < F; ++i)
@@ -209,32 +211,24 @@ struct MuonCore {
         const int row = 8 * first + (lane >> 3);
         off[h] = (uint32_t)(row * ld * 2 + (((lane & 7) ^ (row & 7)) * 16));
       }
-      off[h] -= 1024u * (uint32_t)part;
+      off[h] -= 1024u * (uint32_t)(h & 1);
     }
     const uint32_t step = KMAJOR ? (uint32_t)(KS * ld * 2) : 2u * KS;
     const uint32_t sa = (uint32_t)(uintptr_t)&sm.a[0][0], sb = (uint32_t)(uintptr_t)&sm.b[0][0];
-    const auto issue = [&](int st) {
-      const bool live = st < n_st;
-      const uint32_t slot = (uint32_t)(st % M_SLOTS) * M_SLOT, ko = (uint32_t)st * step;
-#pragma unroll
-      for (int o = 0; o < 2; ++o) {
-        const uint32_t lds = (o ? sb : sa) + slot;
-        const i32x4 hi = desc_at(o ? b_hi : a_hi, ko, live);
-        if constexpr (PAIRS) {
-          const i32x4 lo = desc_at(o ? b_lo : a_lo, ko, live);
-          set_m0(lds + (uint32_t)wave * 2048u);
-          lds_dma16_m0<0>(hi, off[0]);
-          lds_dma16_m0<1024>(hi, off[1]);
-          set_m0(lds + M_SLOT / 2 + (uint32_t)wave * 2048u);
-          lds_dma16_m0<0>(lo, off[2]);
-          lds_dma16_m0<1024>(lo, off[3]);
-        } else {
-          set_m0(lds + (uint32_t)wave * 4096u);
-          lds_dma16_m0<0>(hi, off[0]);
-          lds_dma16_m0<1024>(hi, off[1]);
-          lds_dma16_m0<2048>(hi, off[2]);
-          lds_dma16_m0<3072>(hi, off[3]);
-        }
+    // group g (0..3) of stage st's loads: A's and B's, two KB of the wave's four at a time
+    const auto issue = [&](int st, int g) {
+      const bool live = st < n_st;  // past the end nothing is fetched
+      const uint32_t lds = (g < 2 ? sa : sb) + (uint32_t)(st & 1) * M_SLOT, ko = (uint32_t)st * step;
+      const int h = g & 1;
+      const i32x4 d = desc_at(PAIRS && h ? (g < 2 ? a_lo : b_lo) : (g < 2 ? a_hi : b_hi), ko, live);
+      if constexpr (PAIRS) {
+        set_m0(lds + (uint32_t)h * (M_SLOT / 2) + (uint32_t)wave * 2048u);
+        lds_dma16_m0<0>(d, off[2 * h]);
+        lds_dma16_m0<1024>(d, off[2 * h + 1]);
+      } else {
+        set_m0(lds + (uint32_t)wave * 4096u + (uint32_t)h * 2048u);
+        lds_dma16_m0<0>(d, off[2 * h]);
+        lds_dma16_m0<1024>(d, off[2 * h + 1]);
       }
     };
     const int ri = lane & 15, rg = lane >> 4;
@@ -252,52 +246,51 @@ struct MuonCore {
         return *reinterpret_cast<const __attribute__((address_space(3))) i32x4*>((uintptr_t)at);
       }
     };
+    // A stage's fragments: the two K-halves, or with PAIRS the two halves of the values.  While one
+    // stage's are multiplied the next one's are read.
+    struct Frags {
+      i32x4 a[2][F], b[2][F];
+    } even, odd;
+    const auto read = [&](int st, int n, Frags& f) {  // n (0..7): two fragments, B's before A's
+      const uint32_t base = (n & 2 ? sa : sb) + (uint32_t)(st & 1) * M_SLOT + (PAIRS ? (uint32_t)(n >> 2) * (M_SLOT / 2) : 0u);
+      const int h = n >> 2, t = 2 * (n & 1);
+      i32x4(&to)[F] = n & 2 ? f.a[h] : f.b[h];
 #pragma unroll
-    for (int st = 0; st < M_SLOTS - 1; ++st) issue(st);
-    for (int st = 0; st < n_st; ++st) {
-      gemm_wait_vm<8 * (M_SLOTS - 2)>();  // stage st has landed: eight loads of a wave are a stage
-      wait_lgkm0();                       // this wave has read stage st - 1
+      for (int k = 0; k < 2; ++k) to[t + k] = frag(base, n & 2 ? wm : wn, t + k, PAIRS ? 0 : h);
+    };
+    const bool there = rows > 64 * wm && cols > 64 * wn;  // something of the wave's
+    constexpr int PRODUCTS = PAIRS ? 3 : 2;
+    const auto stage = [&](int st, const Frags& cur, Frags& next) {
+      gemm_wait_vm<0>();  // stage st + 1 has landed
+      wait_lgkm0();       // this wave has read stage st, whose slot is free behind the barrier
       __builtin_amdgcn_s_barrier();
-      issue(st + M_SLOTS - 1);            // past the end nothing is fetched
-      const uint32_t slot = (uint32_t)(st % M_SLOTS) * M_SLOT;
-      i32x4 fa[F], fb[F], ga[F], gb[F];
-      if constexpr (PAIRS) {
+      if (there) {
 #pragma unroll
-        for (int t = 0; t < F; ++t) {
-          fb[t] = frag(sb + slot, wn, t, 0);
-          fa[t] = frag(sa + slot, wm, t, 0);
+        for (int r = 0; r < PRODUCTS * F; ++r) {  // a row of four products, two reads and two loads at a time
+          const int p = r / F, i = r % F;
+          if (r < 8) read(st + 1, r, next);
+          if (r < 4) issue(st + 2, r);
+          __builtin_amdgcn_sched_barrier(0);
+          const i32x4(&x)[F] = cur.a[PAIRS ? p == 2 : p];
+          const i32x4(&y)[F] = cur.b[PAIRS ? p == 1 : p];
+#pragma unroll
+          for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, x[i], y[j], acc[i][j]);
+          __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int t = 0; t < F; ++t) {
-          gb[t] = frag(sb + slot + M_SLOT / 2, wn, t, 0);
-          ga[t] = frag(sa + slot + M_SLOT / 2, wm, t, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-          for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, fa[i], fb[j], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-          for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, fa[i], gb[j], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-          for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, ga[i], fb[j], acc[i][j]);
       } else {
 #pragma unroll
-        for (int hk = 0; hk < 2; ++hk) {
-#pragma unroll
-          for (int t = 0; t < F; ++t) {
-            fb[t] = frag(sb + slot, wn, t, hk);
-            fa[t] = frag(sa + slot, wm, t, hk);
-          }
-#pragma unroll
-          for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j) acc[i][j] = mma16(F16Tag{}, fa[i], fb[j], acc[i][j]);
-        }
+        for (int g = 0; g < 4; ++g) issue(st + 2, g);
       }
+    };
+#pragma unroll
+    for (int k = 0; k < 8; ++k) issue(k / 4, k % 4);
+    gemm_wait_vm<8>();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int n = 0; n < 8; ++n) read(0, n, even);
+    for (int st = 0; st < n_st; st += 2) {
+      stage(st, even, odd);
+      if (st + 1 < n_st) stage(st + 1, odd, even);
     }
     gemm_wait_vm<0>();
     wait_lgkm0();
@@ -314,7 +307,7 @@ struct MuonCoreBig : std::conditional<KMAJOR, GemmCoreT<F16Tag>, GemmCore<F16Tag
   typedef GemmSmem Smem;
 
   __device__ inline void product(GemmSmem& sm, const i32x4& a_hi, const i32x4& a_lo, const i32x4& b_hi, const i32x4& b_lo,
-                                 int32_t ld, int n_k) {
+                                 int32_t ld, int n_k, int, int) {
     const int n_st = (n_k + 63) / 64;
     this->zero();
     i32x4 da = uniform_desc(a_hi), db = uniform_desc(b_hi);
@@ -487,7 +480,8 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_gram_kernel(MuonArgs a,
   const char* const y = base + q.y[from];
   typename C::type core;
   core.product(sm, cols_desc(y, q.ld, ti * C::tile, q.L), cols_desc(y + q.lo_y, q.ld, ti * C::tile, q.L),
-           cols_desc(y, q.ld, tj * C::tile, q.L), cols_desc(y + q.lo_y, q.ld, tj * C::tile, q.L), q.ld, q.L);
+           cols_desc(y, q.ld, tj * C::tile, q.L), cols_desc(y + q.lo_y, q.ld, tj * C::tile, q.L), q.ld, q.L,
+               q.S - ti * C::tile, q.S - tj * C::tile);
   put_symmetric<PAIRS>(q, base + q.gram, &sm, ti, tj, core.acc, [](int, int, float(&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= 1.f / kScale;
@@ -509,7 +503,8 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_poly_kernel(MuonArgs a)
   const char* const g = base + q.gram;
   typename C::type core;
   core.product(sm, rows_desc<C::tile>(g, q.ld, ti * C::tile, q.S), rows_desc<C::tile>(g + q.lo_s, q.ld, ti * C::tile, q.S),
-           rows_desc<C::tile>(g, q.ld, tj * C::tile, q.S), rows_desc<C::tile>(g + q.lo_s, q.ld, tj * C::tile, q.S), q.ld, q.ld);
+           rows_desc<C::tile>(g, q.ld, tj * C::tile, q.S), rows_desc<C::tile>(g + q.lo_s, q.ld, tj * C::tile, q.S), q.ld, q.ld,
+               q.S - ti * C::tile, q.S - tj * C::tile);
   put_symmetric<PAIRS>(q, base + q.poly, &sm, ti, tj, core.acc, [&](int r, int c, float(&x)[8]) {
     float v[8];
     get_halves8<PAIRS>(reinterpret_cast<const _Float16*>(g) + (int64_t)c * q.ld + r, q.lo_s, v);  // A is symmetric
@@ -542,7 +537,8 @@ struct ApplyTile {
   __device__ inline void run(typename C::type& core, typename C::type::Smem& sm, int from) const {
     const char *y = base + q.y[from], *b = base + q.poly;
     core.product(sm, rows_desc<C::tile>(b, q.ld, ts * C::tile, q.S), rows_desc<C::tile>(b + q.lo_s, q.ld, ts * C::tile, q.S),
-             rows_desc<C::tile>(y, q.ld, tl * C::tile, q.L), rows_desc<C::tile>(y + q.lo_y, q.ld, tl * C::tile, q.L), q.ld, q.ld);
+             rows_desc<C::tile>(y, q.ld, tl * C::tile, q.L), rows_desc<C::tile>(y + q.lo_y, q.ld, tl * C::tile, q.L), q.ld, q.ld,
+             q.S - ts * C::tile, q.L - tl * C::tile);
   }
 };
 
@@ -659,6 +655,7 @@ hipError_t with_pairs(bool pairs, F f) {
   return hipGetLastError();
 }
 
+// Calls f with big and pairs as types.
 template <typename F>
 hipError_t with_both(bool big, bool pairs, F f) {
   return with_pairs(pairs, [&](auto pr) {
