@@ -176,6 +176,7 @@ def lib() -> ctypes.CDLL:
 
 _native_modules = None
 _native_call = None
+_native_rows = None
 _native_written = None
 
 
@@ -205,6 +206,22 @@ def _native_token_call():
                 return None
         _native_call = token_call
     return _native_call
+
+
+def _native_rows_call():
+    """The native checks and calls of embedding and layer norm, loaded once, as _native()."""
+    global _native_rows
+    if _native_rows is None:
+        try:
+            from ._marshal import rows_call
+        except ImportError as e:
+            warnings.warn(f"_marshal is not available ({e}): calls over token rows check their tensors in Python "
+                          "(build it with `python -m paper_2606_11660_amd.build`)", RuntimeWarning, stacklevel=2)
+
+            def rows_call(*args):
+                return None
+        _native_rows = rows_call
+    return _native_rows
 
 
 def _native():
@@ -956,6 +973,27 @@ def _matrix(t: torch.Tensor, rows: Optional[int], width: int, name: str) -> int:
     return ld if n > 1 else max(ld, w)
 
 
+_EMBED, _EMBED_BACK, _NORM, _NORM_BACK = range(4)
+_ROWS_ENTRY = ("attr_embed", "attr_embed_backward", "attr_layer_norm", "attr_layer_norm_backward")
+_rows_address: Dict[int, int] = {}
+
+
+def _rows_call(op: int, rows: Optional[ExampleRows], tensors: tuple, numbers: tuple, raw: int,
+               w: Optional[Workspace] = None) -> bool:
+    """One call through csrc/marshal.cpp's rows_call(), the tensors in its order.  False: the Python
+    checks decide, or (ATTR_ERR_WORKSPACE) the workspace has to grow or this stream has not used it yet."""
+    if op not in _rows_address:
+        _rows_address[op] = ctypes.cast(getattr(lib(), _ROWS_ENTRY[op]), ctypes.c_void_p).value
+    buf = w.buf if w is not None and raw in w._streams else None
+    status = _native_rows_call()(op, _rows_address[op], rows, ExampleRows, tensors, numbers,
+                                 0 if buf is None else buf.data_ptr(), 0 if buf is None else buf.numel(), raw)
+    if status == 0:
+        return True
+    if status is not None and status != 4:
+        _check(status)
+    return False
+
+
 def _tokens(token: torch.Tensor, n_rows: int) -> None:
     _vector(token, n_rows, torch.int64, "token")
 
@@ -964,6 +1002,9 @@ def attr_embed(table: torch.Tensor, token: torch.Tensor, out: torch.Tensor, scal
                rows: Optional[ExampleRows] = None, stream=None) -> torch.Tensor:
     """out[row] = scale * table[token[row]] (table [V, d], token int64 [n_rows], out [n_rows, d], any
     types); rows of tokens outside [0, V) are zeros."""
+    raw = _raw_stream(stream) if out.is_cuda else 0
+    if _rows_call(_EMBED, rows, (table, token, out), (scale,), raw):
+        return out
     n, d, ldo = _rows(out)
     V = table.shape[0]
     ldt = _matrix(table, V, d, "table")
@@ -971,7 +1012,7 @@ def attr_embed(table: torch.Tensor, token: torch.Tensor, out: torch.Tensor, scal
     batch, where = _batch(rows, n)
     _same_gpu(table, token, out, where.row_offset, where.length)
     _check(lib().attr_embed(batch, token.data_ptr(), table.data_ptr(), _dtype(table), V, d, ldt, scale, out.data_ptr(),
-                            _dtype(out), max(ldo, d), _raw_stream(stream)))
+                            _dtype(out), max(ldo, d), raw))
     _written((out,))
     return out
 
@@ -986,15 +1027,17 @@ def attr_embed_backward(dout: torch.Tensor, token: torch.Tensor, dtable: torch.T
     """dtable[v] = scale * sum of dout's rows whose token is v (zeros where there is none), or with
     accumulate added to what dtable holds.  The same bits for the same call: tokens are sorted,
     and their rows added up in order."""
+    raw = _raw_stream(stream) if dout.is_cuda else 0
+    w = _ws(ws, dout.device, raw) if dout.is_cuda else None
+    if _rows_call(_EMBED_BACK, rows, (dtable, token, dout), (scale, accumulate), raw, w):
+        return dtable
     n, d, ldd = _rows(dout)
     V = dtable.shape[0]
     ldt = _matrix(dtable, V, d, "dtable")
     _tokens(token, n)
     batch, where = _batch(rows, n)
     _same_gpu(dout, token, dtable, where.row_offset, where.length)
-    raw = _raw_stream(stream)
-    need = lib().attr_embed_backward_workspace_size(batch, V, d)
-    wsp, wsn = _ws(ws, dout.device, raw).get(need, raw)
+    wsp, wsn = w.get(lib().attr_embed_backward_workspace_size(batch, V, d), raw)
     _check(lib().attr_embed_backward(batch, token.data_ptr(), dout.data_ptr(), _dtype(dout), max(ldd, d), V, d, scale,
                                      dtable.data_ptr(), _dtype(dtable), ldt, int(bool(accumulate)), wsp, wsn, raw))
     _written((dtable,))
@@ -1020,6 +1063,9 @@ def attr_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Ten
                     rstd: Optional[torch.Tensor] = None, rows: Optional[ExampleRows] = None, stream=None) -> torch.Tensor:
     """y = (x - mean) rstd weight + bias over the last dimension (x, y [n_rows, d], any types; weight
     and bias [d] of one type).  mean, rstd: fp32 [n_rows], what the backward pass takes.  y may be x."""
+    raw = _raw_stream(stream) if x.is_cuda else 0
+    if _rows_call(_NORM, rows, (x, y, weight, bias, mean, rstd), (eps,), raw):
+        return y
     n, d, ldx = _rows(x)
     ldy = _matrix(y, n, d, "y")
     w_dtype = _norm_weights(d, weight, bias)
@@ -1028,7 +1074,7 @@ def attr_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Ten
     batch, where = _batch(rows, n)
     _same_gpu(x, y, weight, bias, mean, rstd, where.row_offset, where.length)
     _check(lib().attr_layer_norm(batch, x.data_ptr(), _dtype(x), d, max(ldx, d), _ptr(weight), _ptr(bias), w_dtype, eps,
-                                 y.data_ptr(), _dtype(y), ldy, _ptr(mean), _ptr(rstd), _raw_stream(stream)))
+                                 y.data_ptr(), _dtype(y), ldy, _ptr(mean), _ptr(rstd), raw))
     _written([t for t in (y, mean, rstd) if t is not None])
     return y
 
@@ -1046,6 +1092,10 @@ def attr_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tens
     """Gradients of attr_layer_norm into those of dx (x's shape and type; may be x or dy), dweight and
     dbias that are given.  dweight, dbias: fp32 [d], or with per_example [n_examples, d] (rows may be
     columns of wider ones): every example's own.  accumulate adds to what they hold."""
+    raw = _raw_stream(stream) if x.is_cuda else 0
+    w = _ws(ws, x.device, raw) if x.is_cuda else None
+    if _rows_call(_NORM_BACK, rows, (x, dy, weight, dx, mean, rstd, dweight, dbias), (per_example, accumulate), raw, w):
+        return
     n, d, ldx = _rows(x)
     ldy = _matrix(dy, n, d, "dy")
     w_dtype = _norm_weights(d, weight)
@@ -1071,9 +1121,7 @@ def attr_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tens
                 raise ValueError(f"{name} must be a contiguous vector of {d} elements")
             lds.append(d)
     _same_gpu(dy, x, mean, rstd, weight, dx, dweight, dbias, where.row_offset, where.length)
-    raw = _raw_stream(stream)
-    need = lib().attr_layer_norm_backward_workspace_size(batch, d, int(bool(per_example)))
-    wsp, wsn = _ws(ws, x.device, raw).get(need, raw)
+    wsp, wsn = w.get(lib().attr_layer_norm_backward_workspace_size(batch, d, int(bool(per_example))), raw)
     _check(lib().attr_layer_norm_backward(batch, dy.data_ptr(), _dtype(dy), ldy, x.data_ptr(), _dtype(x), d, max(ldx, d),
                                           mean.data_ptr(), rstd.data_ptr(), _ptr(weight), w_dtype, _ptr(dx), lddx,
                                           _ptr(dweight), lds[0], _ptr(dbias), lds[1], int(bool(per_example)),

@@ -9,7 +9,8 @@
 // another kind (a subclass, a wrapper without storage, a CPU tensor): the
 // binding's own Python checks then run, and raise or accept.  token_call() makes the
 // checks of a token loss on its rows and vectors, and the library's call too (the
-// checks in Python take 7 us, where a small call's kernel takes 4).  written() tells autograd
+// checks in Python take 7 us, where a small call's kernel takes 4); rows_call() does the same
+// for embedding and layer norm over token rows.  written() tells autograd
 // of tensors that a call wrote through their pointers (168 weights: under 2 us, 8 us in
 // Python): a backward pass that saved their earlier values then raises, as after any change
 // in place.
@@ -312,10 +313,199 @@ PyObject* py_token_call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return PyLong_FromLong((long)st);
 }
 
+// ----------------------------------------------------------------------------
+// embedding and layer norm over token rows
+// ----------------------------------------------------------------------------
+typedef attr_status (*EmbedFn)(const attr_rows*, const int64_t*, const void*, attr_dtype, int64_t, int64_t, int64_t, float,
+                               void*, attr_dtype, int64_t, void*);
+typedef attr_status (*EmbedBackFn)(const attr_rows*, const int64_t*, const void*, attr_dtype, int64_t, int64_t, int64_t,
+                                   float, void*, attr_dtype, int64_t, int32_t, void*, size_t, void*);
+typedef attr_status (*NormFn)(const attr_rows*, const void*, attr_dtype, int64_t, int64_t, const void*, const void*,
+                              attr_dtype, float, void*, attr_dtype, int64_t, float*, float*, void*);
+typedef attr_status (*NormBackFn)(const attr_rows*, const void*, attr_dtype, int64_t, const void*, attr_dtype, int64_t,
+                                  int64_t, const float*, const float*, const void*, attr_dtype, void*, int64_t, float*,
+                                  int64_t, float*, int64_t, int32_t, int32_t, void*, size_t, void*);
+constexpr int kEmbed = 0, kEmbedBack = 1, kNorm = 2, kNormBack = 3;
+
+// A matrix of a call: its rows, type and stride, as the binding's _matrix() has them.
+struct Mat {
+  void* p = nullptr;
+  int64_t n = 0, w = 0, ld = 0;
+  attr_dtype type = ATTR_F32;
+  // `o` on dev (or, first of a call, on any GPU) with w columns (0: any number) and n rows (-1: any)
+  bool take(PyObject* o, const at::Device* dev, int64_t rows, int64_t width) {
+    const at::Tensor* t = tensor_of(o);
+    if (!t || !t->is_cuda() || (dev && t->device() != *dev) || !rows_of(*t, n, w, ld)) return false;
+    if ((rows >= 0 && n != rows) || (width > 0 && w != width)) return false;
+    const at::ScalarType k = t->scalar_type();
+    if (k != at::kFloat && k != at::kBFloat16 && k != at::kHalf) return false;
+    type = k == at::kFloat ? ATTR_F32 : k == at::kBFloat16 ? ATTR_BF16 : ATTR_F16;
+    if (n <= 1 && ld < w) ld = w;
+    p = t->mutable_data_ptr();
+    return true;
+  }
+};
+// None, or a contiguous vector of exactly d elements of a norm's weights' one type
+bool weight_ok(PyObject* o, int64_t d, const at::Device& dev, bool& any, attr_dtype& type, void** p) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = tensor_of(o);
+  if (!t || !on(*t, dev) || t->dim() != 1 || t->numel() != d || !t->is_contiguous()) return false;
+  const at::ScalarType k = t->scalar_type();
+  if (k != at::kFloat && k != at::kBFloat16 && k != at::kHalf) return false;
+  const attr_dtype mine = k == at::kFloat ? ATTR_F32 : k == at::kBFloat16 ? ATTR_BF16 : ATTR_F16;
+  if (any && type != mine) return false;
+  any = true;
+  type = mine;
+  *p = t->mutable_data_ptr();
+  return true;
+}
+void* data_of(PyObject* o) { return o == Py_None ? nullptr : THPVariable_Unpack(o).mutable_data_ptr(); }
+
+// The call's rows: None (every row is a token of one example) or an ExampleRows.
+bool batch_ok(PyObject* rows, PyObject* rows_type, int64_t n_rows, const at::Device& dev, attr_rows& c) {
+  c.n_rows = n_rows;
+  c.row_offset = nullptr;
+  c.length = nullptr;
+  if (rows == Py_None) {
+    c.n_examples = n_rows ? 1 : 0;
+    c.T = n_rows ? n_rows : 1;
+    return true;
+  }
+  if ((PyObject*)Py_TYPE(rows) != rows_type) return false;
+  const Ref n_ex(PyObject_GetAttr(rows, names.n_examples)), T(PyObject_GetAttr(rows, names.T)),
+      off(PyObject_GetAttr(rows, names.row_offset)), len(PyObject_GetAttr(rows, names.length));
+  if (!off.p || !len.p || !size_of(n_ex.p, c.n_examples) || !size_of(T.p, c.T) || c.T < 1) return false;
+  if (off.p == Py_None && n_rows < c.n_examples * c.T) return false;
+  if (!vector_ok(off.p, at::kLong, c.n_examples, dev) || !vector_ok(len.p, at::kInt, c.n_examples, dev)) return false;
+  c.row_offset = static_cast<const int64_t*>(data_of(off.p));
+  c.length = static_cast<const int32_t*>(data_of(len.p));
+  return true;
+}
+
+// What a call's tensors and numbers are, once checked; run() makes it.
+struct RowsCall {
+  attr_rows rows;
+  Mat a, b, c;
+  attr_dtype w_type = ATTR_F32;
+  void *v[4] = {nullptr, nullptr, nullptr, nullptr};
+  int64_t ldw = 0, ldb = 0;
+  double x = 0;
+  int flag[2] = {0, 0};
+
+  bool gather(int op, PyObject* where, PyObject* rows_type, PyObject* const* t, PyObject* const* num) {
+    const auto truth = [](PyObject* o, int& f) { return (f = PyObject_IsTrue(o)) >= 0; };
+    if (op == kEmbed || op == kEmbedBack) {  // (table or dtable, token, out or dout), (scale[, accumulate])
+      if (!b.take(t[2], nullptr, -1, 0)) return false;
+      const at::Device dev = THPVariable_Unpack(t[2]).device();
+      const at::Tensor* table = tensor_of(t[0]);
+      if (!table || table->dim() < 1 || !a.take(t[0], &dev, table->size(0), b.w)) return false;
+      if (t[1] == Py_None || !vector_ok(t[1], at::kLong, b.n, dev) || !batch_ok(where, rows_type, b.n, dev, rows)) return false;
+      v[0] = data_of(t[1]);
+      x = PyFloat_AsDouble(num[0]);
+      return !PyErr_Occurred() && (op == kEmbed || truth(num[1], flag[0]));
+    }
+    // (x, y or dy, weight, bias or dx, mean, rstd[, dweight, dbias]), (eps) or (per_example, accumulate)
+    if (!a.take(t[0], nullptr, -1, 0)) return false;
+    const at::Device dev = THPVariable_Unpack(t[0]).device();
+    bool any = false;
+    if (!b.take(t[1], &dev, a.n, a.w) || !weight_ok(t[2], a.w, dev, any, w_type, &v[0]) ||
+        !vector_ok(t[4], at::kFloat, a.n, dev) || !vector_ok(t[5], at::kFloat, a.n, dev) ||
+        !batch_ok(where, rows_type, a.n, dev, rows))
+      return false;
+    v[2] = data_of(t[4]);
+    v[3] = data_of(t[5]);
+    if (op == kNorm) {
+      x = PyFloat_AsDouble(num[0]);
+      return !PyErr_Occurred() && weight_ok(t[3], a.w, dev, any, w_type, &v[1]);
+    }
+    if (t[4] == Py_None || t[5] == Py_None || !truth(num[0], flag[0]) || !truth(num[1], flag[1])) return false;
+    if (t[3] != Py_None && (!c.take(t[3], &dev, a.n, a.w) || c.type != a.type)) return false;
+    int64_t* const lds[2] = {&ldw, &ldb};
+    for (int k = 0; k < 2; ++k) {
+      *lds[k] = a.w;
+      PyObject* o = t[6 + k];
+      if (o == Py_None) continue;
+      Mat m;
+      const at::Tensor* g = tensor_of(o);
+      if (!g || g->scalar_type() != at::kFloat || !on(*g, dev)) return false;
+      if (flag[0] ? !m.take(o, &dev, rows.n_examples, a.w) : g->dim() != 1 || g->numel() != a.w || !g->is_contiguous()) return false;
+      if (flag[0]) *lds[k] = m.ld;
+    }
+    return true;
+  }
+  attr_status run(int op, void* fn, float* dweight, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+    const int64_t* token = static_cast<const int64_t*>(v[0]);
+    switch (op) {
+      case kEmbed:
+        return reinterpret_cast<EmbedFn>(fn)(&rows, token, a.p, a.type, a.n, a.w, a.ld, (float)x, b.p, b.type, b.ld, stream);
+      case kEmbedBack:
+        return reinterpret_cast<EmbedBackFn>(fn)(&rows, token, b.p, b.type, b.ld, a.n, a.w, (float)x, a.p, a.type, a.ld,
+                                                 flag[0], ws, ws_bytes, stream);
+      case kNorm:
+        return reinterpret_cast<NormFn>(fn)(&rows, a.p, a.type, a.w, a.ld, v[0], v[1], w_type, (float)x, b.p, b.type, b.ld,
+                                            static_cast<float*>(v[2]), static_cast<float*>(v[3]), stream);
+      default:
+        return reinterpret_cast<NormBackFn>(fn)(&rows, b.p, b.type, b.ld, a.p, a.type, a.w, a.ld,
+                                                static_cast<float*>(v[2]), static_cast<float*>(v[3]), v[0], w_type, c.p, c.ld,
+                                                dweight, ldw, dbias, ldb, flag[0], flag[1], ws, ws_bytes, stream);
+    }
+  }
+};
+
+// rows_call(op, address, rows, ExampleRows, tensors, numbers, workspace, workspace_bytes, stream)
+// -> status, or None
+PyObject* py_rows_call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  if (nargs != 9) {
+    PyErr_SetString(PyExc_TypeError, "rows_call() takes 9 arguments");
+    return nullptr;
+  }
+  const long op = PyLong_AsLong(args[0]);
+  void* fn = PyLong_AsVoidPtr(args[1]);
+  void* ws = PyLong_AsVoidPtr(args[6]);
+  const size_t ws_bytes = PyLong_AsSize_t(args[7]);
+  void* stream = PyLong_AsVoidPtr(args[8]);
+  const Py_ssize_t sizes[4] = {3, 3, 6, 8}, numbers[4] = {1, 2, 1, 2};
+  RowsCall c;
+  float *dweight = nullptr, *dbias = nullptr;
+  bool ok = false;
+  try {
+    ok = !PyErr_Occurred() && fn && op >= 0 && op <= 3 && PyTuple_CheckExact(args[4]) && PyTuple_CheckExact(args[5]) &&
+         PyTuple_GET_SIZE(args[4]) == sizes[op] && PyTuple_GET_SIZE(args[5]) == numbers[op] &&
+         c.gather((int)op, args[2], args[3], reinterpret_cast<PyTupleObject*>(args[4])->ob_item, reinterpret_cast<PyTupleObject*>(args[5])->ob_item);
+    if (ok && op == kNormBack) {
+      dweight = static_cast<float*>(data_of(PyTuple_GET_ITEM(args[4], 6)));
+      dbias = static_cast<float*>(data_of(PyTuple_GET_ITEM(args[4], 7)));
+    }
+  } catch (...) {  // a tensor without storage, for one
+    ok = false;
+  }
+  if (!ok || PyErr_Occurred()) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  attr_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = c.run((int)op, fn, dweight, dbias, ws, ws_bytes, stream);
+  Py_END_ALLOW_THREADS;
+  if (st == ATTR_OK) {  // what it wrote
+    const int written[4][4] = {{2, -1, -1, -1}, {0, -1, -1, -1}, {1, 4, 5, -1}, {3, 6, 7, -1}};
+    try {
+      for (int k = 0; k < 4; ++k)
+        if (written[op][k] >= 0) bump(PyTuple_GET_ITEM(args[4], written[op][k]));
+    } catch (...) {
+      Py_RETURN_NONE;
+    }
+  }
+  return PyLong_FromLong((long)st);
+}
+
 PyMethodDef methods[] = {{"modules", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_modules)),
                           METH_FASTCALL, "module descriptors of a projection call, or None"},
                          {"token_call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_token_call)),
                           METH_FASTCALL, "status of a token loss's call, or None"},
+                         {"rows_call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_rows_call)),
+                          METH_FASTCALL, "status of an embedding's or a layer norm's call, or None"},
                          {"written", py_written, METH_O, "counts a change in place of every tensor"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -464,3 +464,82 @@ def test_captured_and_on_another_stream():
         torch.cuda.synchronize()
         for a, b in zip(got, (y, dx, dw, db, dt)):
             assert torch.equal(a, b), k
+
+
+def _each_call(wide):
+    """Every call once, with all that it may be given; wide: rows that are columns of wider ones."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    n, T, d, V = 5, 9, 40, 23
+    pad = 3 if wide else 0
+
+    def rand(*s, dtype=F32):
+        return torch.randn(*s[:-1], s[-1] + pad, generator=gen, device="cuda").to(dtype)[..., :s[-1]]
+    where = P.ExampleRows(n, T, length=torch.tensor([9, 3, 0, 9, 1], dtype=torch.int32, device="cuda"))
+    token = torch.randint(-1, V + 1, (n * T,), generator=gen, device="cuda")
+    x, dy, w, b = rand(n * T, d, dtype=BF16), rand(n * T, d), rand(d, dtype=F16).contiguous(), rand(d, dtype=F16).contiguous()
+    out, y, dx = rand(n, T, d) if not wide else rand(n * T, d), rand(n * T, d), rand(n * T, d, dtype=BF16)
+    dt, dw, db = rand(V, d), rand(n, d), rand(n, d)
+    mean, rstd = torch.zeros(n * T, device="cuda"), torch.zeros(n * T, device="cuda")
+    P.attr_embed(rand(V, d, dtype=F16), token, out, scale=1.5, rows=where)
+    P.attr_embed_backward(dy, token, dt, scale=0.7, accumulate=True, rows=where)
+    P.attr_layer_norm(x, y, w, b, 1e-3, mean, rstd, rows=where)
+    P.attr_layer_norm_backward(dy, x, mean, rstd, w, dx, dw, db, per_example=True, accumulate=True, rows=where)
+    e = torch.empty(n * T, d, device="cuda")
+    P.attr_layer_norm(x, e)
+    return out, dt, y, mean, rstd, dx, dw, db, e
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_native_checks_and_python_ones_make_the_same_calls(monkeypatch, wide):
+    taken = []
+    native = P._native_rows_call()
+    monkeypatch.setattr(P, "_native_rows", lambda *a: taken.append(native(*a)) or taken[-1])
+    a = _each_call(wide)
+    assert taken.count(0) >= 4 and None not in taken    # 4: a workspace that had to grow
+    monkeypatch.setattr(P, "_native_rows", lambda *a: None)
+    for s, t in zip(a, _each_call(wide)):
+        assert torch.equal(s, t)
+
+
+def test_refusals_on_the_gpu():
+    t = lambda *s, d=F32: torch.zeros(s, dtype=d, device="cuda")  # noqa: E731
+    x, m, tok = t(4, 8), t(4), t(4, d=torch.int64)
+    calls = [(lambda: P.attr_layer_norm(x, t(5, 8)), "y must"), (lambda: P.attr_layer_norm(x, t(4, 8), t(7)), "8 elements"),
+             (lambda: P.attr_layer_norm(x, t(4, 8), t(8), t(8, d=BF16)), "one type"),
+             (lambda: P.attr_layer_norm(x, t(4, 8), mean=t(3)), "mean"), (lambda: P.attr_layer_norm(x, t(4, 8).cpu()), "GPU"),
+             (lambda: P.attr_layer_norm(x.t(), x.t()), "contiguous last"),
+             (lambda: P.attr_layer_norm(x, t(4, 8), rows=P.ExampleRows(3, 2)), "need"),
+             (lambda: P.attr_layer_norm(x, t(4, 8), rows=P.ExampleRows(2, 2, length=t(2))), "length"),
+             (lambda: P.attr_embed(t(5, 9), tok, x), "table"), (lambda: P.attr_embed(t(5, 8), tok[:3], x), "token"),
+             (lambda: P.attr_embed(t(5, 8), tok.int(), x), "token"), (lambda: P.attr_embed(t(5, 8), tok.cpu(), x), "GPU"),
+             (lambda: P.attr_embed_backward(x, tok, t(5, 7)), "dtable"),
+             (lambda: P.attr_layer_norm_backward(x, x, m, None), "forward"),
+             (lambda: P.attr_layer_norm_backward(x, x, m, m, dx=t(4, 8, d=BF16)), "type"),
+             (lambda: P.attr_layer_norm_backward(x, x, m, m, dweight=t(1, 8)), "dweight"),
+             (lambda: P.attr_layer_norm_backward(x, x, m, m, dbias=t(8, d=BF16)), "dbias"),
+             (lambda: P.attr_layer_norm_backward(x, x, m, m, dbias=t(3, 8), per_example=True, rows=P.ExampleRows(2, 2)), "dbias")]
+    for f, match in calls:
+        with pytest.raises(ValueError, match=match):
+            f()
+    for f, match in [(lambda: P.attr_layer_norm(x, t(4, 8), eps=-1.0), "eps"), (lambda: P.attr_embed(t(5, 8), tok, x, scale=float("inf")), "scale"),
+                     (lambda: P.attr_embed(x[:, :8], tok, x), "overlap")]:
+        with pytest.raises(P.AttrError, match=match):
+            f()
+
+
+def test_autograd_sees_what_the_calls_write():
+    for k in range(4):
+        w = [torch.randn(4, 8, device="cuda", requires_grad=True) for _ in range(4)]
+        z = sum((v * v).sum() for v in w)
+        d = [v.detach() for v in w]
+        tok, m = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+        if k == 0:
+            P.attr_embed(torch.zeros(5, 8, device="cuda"), tok, d[0])
+        elif k == 1:
+            P.attr_embed_backward(torch.zeros(4, 8, device="cuda"), tok, d[1])
+        elif k == 2:
+            P.attr_layer_norm(torch.zeros(4, 8, device="cuda"), d[2])
+        else:
+            P.attr_layer_norm_backward(torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda"), m, m, dx=d[3])
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            z.backward()
