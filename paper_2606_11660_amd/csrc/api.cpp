@@ -1515,34 +1515,34 @@ attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, con
     a.d = (int32_t)d;
     a.accumulate = accumulate;
     a.scale = scale;
-    const attr::RowsArgs r = rows_args(rows);
-    if (!none && r.n_slots <= attr::kEmbedSmall) {
+    const attr::RowsArgs r = none ? attr::RowsArgs{nullptr, nullptr, 0, 0, 1} : rows_args(rows);
+    if (r.n_slots <= attr::kEmbedSmall) {
       const hipError_t e = attr::launch_embed_small((int)dout_dtype, (int)dtable_dtype, r, token, a, s);
       return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_embed_backward launch");
     }
-    if (!none) {
-      const EmbedLayout L = embed_layout(rows, V, d);
-      if (!ws || ws_bytes < L.total)
-        return fail(ATTR_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", who, L.total, ws ? ws_bytes : (size_t)0);
-      if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ATTR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
-      char* const base = static_cast<char*>(ws);
-      attr::EmbedSort e;
-      for (int k = 0; k < 2; ++k) {
-        e.key[k] = reinterpret_cast<uint32_t*>(base + L.key[k]);
-        e.row[k] = reinterpret_cast<uint32_t*>(base + L.row[k]);
-      }
-      e.count = reinterpret_cast<uint32_t*>(base + L.count);
-      e.passes = attr::sort_passes(V);
-      e.bits = attr::sort_bits(V);
-      e.blocks = (r.n_slots + attr::kSortKeys - 1) / attr::kSortKeys;
-      const hipError_t st2 = attr::launch_embed_sort(r, token, V, e, s);
-      if (st2 != hipSuccess) return device_fail(st2, "attr_embed_backward sort launch");
-      a.key = e.key[e.passes & 1];
-      a.row = e.row[e.passes & 1];
-      a.part = reinterpret_cast<float*>(base + L.part);
-      a.n = r.n_slots;
+    const EmbedLayout L = embed_layout(rows, V, d);
+    if (!ws || ws_bytes < L.total)
+      return fail(ATTR_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", who, L.total, ws ? ws_bytes : (size_t)0);
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(ATTR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+    char* const base = static_cast<char*>(ws);
+    attr::EmbedSort sort;
+    for (int k = 0; k < 2; ++k) {
+      sort.key[k] = reinterpret_cast<uint32_t*>(base + L.key[k]);
+      sort.row[k] = reinterpret_cast<uint32_t*>(base + L.row[k]);
     }
-    const hipError_t e = attr::launch_embed_grad((int)dout_dtype, (int)dtable_dtype, a, s);
+    sort.count = reinterpret_cast<uint32_t*>(base + L.count);
+    sort.passes = attr::sort_passes(V);
+    sort.bits = attr::sort_bits(V);
+    sort.blocks = (r.n_slots + attr::kSortKeys - 1) / attr::kSortKeys;
+    const int eb = dtype_bytes(dtable_dtype);
+    const attr::EmbedZero z{static_cast<char*>(dtable), accumulate ? 0 : V, d * eb, ldt * eb, 0, 0};
+    hipError_t e = attr::launch_embed_sort(r, token, V, sort, z, s);
+    if (e != hipSuccess) return device_fail(e, "attr_embed_backward sort launch");
+    a.key = sort.key[sort.passes & 1];
+    a.row = sort.row[sort.passes & 1];
+    a.part = reinterpret_cast<float*>(base + L.part);
+    a.n = r.n_slots;
+    e = attr::launch_embed_grad((int)dout_dtype, (int)dtable_dtype, a, s);
     return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_embed_backward launch");
   } catch (...) {
     return fail(ATTR_ERR_INVALID_ARG, "attr_embed_backward: host exception");

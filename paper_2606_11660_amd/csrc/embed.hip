@@ -42,6 +42,31 @@ __global__ __launch_bounds__(256) void embed_kernel(RowsArgs r, EmbedArgs a, uin
 }
 
 // ----------------------------------------------------------------------------
+// zeros of a gradient
+// ----------------------------------------------------------------------------
+// n bytes from p on, by `threads` threads: whole 16-byte pieces, bytes before and behind them.
+__device__ inline void zero_span(char* p, int64_t n, int thread, int threads) {
+  const int64_t lead = (int64_t)(-reinterpret_cast<uintptr_t>(p) & 15), head = lead < n ? lead : n;
+  if (thread < head) p[thread] = 0;
+  i32x4* const q = reinterpret_cast<i32x4*>(p + head);
+  const int64_t whole = (n - head) / 16;
+#pragma unroll 4
+  for (int64_t k = thread; k < whole; k += threads) q[k] = i32x4{0, 0, 0, 0};
+  if (head + whole * 16 + thread < n) p[head + whole * 16 + thread] = 0;
+}
+// Share `share` of the table's rows, by a workgroup of the sort's launches.
+__device__ inline void zero_share(const EmbedZero& z, uint32_t share) {
+  const int64_t each = (z.rows + z.shares - 1) / z.shares, from = share * each, to = from + each < z.rows ? from + each : z.rows;
+  if (from >= to) return;
+  if (z.row == z.ld) {  // rows without gaps are one span
+    zero_span(z.to + from * z.ld, (to - from) * z.row, threadIdx.x, blockDim.x);
+    return;
+  }
+  const int wave = (int)(threadIdx.x >> 6), waves = (int)(blockDim.x >> 6);
+  for (int64_t r = from + wave; r < to; r += waves) zero_span(z.to + r * z.ld, z.row, threadIdx.x & 63, 64);
+}
+
+// ----------------------------------------------------------------------------
 // the sort: least significant digits first, each pass stable
 // ----------------------------------------------------------------------------
 struct Pair {
@@ -160,11 +185,13 @@ struct Share {
   }
 };
 
-// Every pass of a short batch (up to 1024 K pairs) in one workgroup.
+// Every pass of a short batch (up to 1024 K pairs) in one workgroup; the others of this launch, and
+// of those below, write the gradient's zeros meanwhile.
 template <int K>
-__global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e) {
+__global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, EmbedZero z) {
   __shared__ uint32_t base[16][kBinsMost];
   __shared__ uint32_t sm[16];
+  if (blockIdx.x > 0) return zero_share(z, blockIdx.x - 1);
   const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
   const Share w(r.n_slots, wave, ((r.n_slots + 1023) / 1024) * 64);
   const uint32_t bins = 1u << e.bits;
@@ -194,8 +221,9 @@ __global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const 
 // Longer ones, pass by pass: each workgroup counts its pairs' digits (the first pass leaves the
 // pairs themselves behind), the counts are added up, and each workgroup puts its pairs in their places.
 template <bool FIRST>
-__global__ __launch_bounds__(1024) void embed_count_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, int pass) {
+__global__ __launch_bounds__(1024) void embed_count_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, EmbedZero z, int pass) {
   __shared__ uint32_t count[kBinsMost];
+  if (blockIdx.x >= e.blocks) return zero_share(z, 2 * pass * z.blocks + blockIdx.x - e.blocks);
   const uint32_t bins = 1u << e.bits;
   for (uint32_t b = threadIdx.x; b < bins; b += 1024) count[b] = 0;
   const Share w(r.n_slots, wave_uniform(threadIdx.x >> 6), kSortKeys / 16);
@@ -243,9 +271,10 @@ __global__ __launch_bounds__(1024) void embed_scan_kernel(EmbedSort e) {
 }
 // SCAN: the counts are those of few workgroups, and each adds them up by itself.
 template <bool SCAN>
-__global__ __launch_bounds__(1024) void embed_place_kernel(EmbedSort e, uint32_t n, int pass) {
+__global__ __launch_bounds__(1024) void embed_place_kernel(EmbedSort e, EmbedZero z, uint32_t n, int pass) {
   __shared__ uint32_t base[16][kBinsMost];
   __shared__ uint32_t sm[16];
+  if (blockIdx.x >= e.blocks) return zero_share(z, (2 * pass + 1) * z.blocks + blockIdx.x - e.blocks);
   const int lane = threadIdx.x & 63;
   const uint32_t wave = wave_uniform(threadIdx.x >> 6), bins = 1u << e.bits, b = threadIdx.x;
   const Share w(n, wave, kSortKeys / 16);
@@ -302,67 +331,10 @@ __device__ inline void put_sum(const EmbedGradArgs& a, uint32_t v, Cols<N> c, fl
   store_n<T, N>(out, c, sum);
 }
 
-// Zeros from p on, by one wave: whole 16-byte pieces, elements before and behind them.
-template <typename T>
-__device__ inline void zero_span(T* p, int64_t n) {
-  const int lane = threadIdx.x & 63;
-  int64_t head = (int64_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int64_t)sizeof(T);
-  head = head < n ? head : n;
-  constexpr int E = 16 / sizeof(T);
-  if (lane < head) p[lane] = (T)0;
-  i32x4* const q = reinterpret_cast<i32x4*>(p + head);
-  const int64_t whole = (n - head) / E;
-#pragma unroll 4
-  for (int64_t k = lane; k < whole; k += 64) q[k] = i32x4{0, 0, 0, 0};
-  if (head + whole * E + lane < n) p[head + whole * E + lane] = (T)0;
-}
-
-constexpr uint32_t kZeroRows = 16;
-// The rows v0 + k whose bits are set; neighbouring rows of a table without gaps are one span.
-template <typename T>
-__device__ inline void zero_rows(const EmbedGradArgs& a, int64_t v0, uint64_t rows) {
-  while (rows) {
-    const int k = __builtin_ctzll(rows), run = a.ldt == a.d ? __builtin_ctzll(~(rows >> k)) : 1;
-    zero_span((T*)a.dtable + (v0 + k) * a.ldt, (int64_t)run * a.d);
-    rows &= ~(((1ull << run) - 1) << k);
-  }
-}
-// Which of v0 .. v0 + kZeroRows - 1 (those below V) the sorted keys do not hold, by one wave: each
-// step of its searches looks at 64 places.
-__device__ inline uint64_t absent_of(const uint32_t* keys, uint32_t n, int64_t v0, int64_t V) {
-  const uint32_t lane = threadIdx.x & 63, first = (uint32_t)v0;
-  uint64_t absent = V - v0 < (int64_t)kZeroRows ? (1ull << (V - v0)) - 1 : (1ull << kZeroRows) - 1;
-  uint32_t lo = 0, hi = n, key = first;  // the first place in [lo, hi] with a key not below `key`
-  for (;;) {
-    while (hi - lo > 64) {
-      const uint32_t step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step - 1;
-      const uint32_t below = (uint32_t)__popcll(__ballot(at < hi && keys[at] < key));
-      lo += below * step;
-      hi = hi - lo < step ? hi : lo + step;
-    }
-    lo += (uint32_t)__popcll(__ballot(lo + lane < hi && keys[lo + lane] < key));
-    if (lo >= n) return absent;
-    const uint32_t mine = lo + lane < n ? keys[lo + lane] : (uint32_t)V;
-    for (uint32_t k = 0; k < kZeroRows; ++k)
-      if (__ballot(mine == first + k)) absent &= ~(1ull << k);
-    const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)mine, 63);
-    if (last >= first + kZeroRows - 1 || lo + 64 >= n) return absent;
-    key = last + 1;
-    lo += 64;
-    hi = n;
-  }
-}
-
-// A wave takes 64 N columns of a part of the sorted pairs, or zeroes rows of tokens that the
-// batch does not hold.
+// A wave takes 64 N columns of a part of the sorted pairs.
 template <typename G, typename T, int N>
-__device__ inline void embed_sum(const EmbedGradArgs& a, uint32_t parts, uint32_t cuts, uint64_t unit) {
+__device__ inline void embed_sum(const EmbedGradArgs& a, uint32_t cuts, uint64_t unit) {
   const int lane = threadIdx.x & 63;
-  if (unit >= (uint64_t)parts * cuts) {
-    const int64_t v0 = (int64_t)(unit - (uint64_t)parts * cuts) * kZeroRows;
-    zero_rows<T>(a, v0, absent_of(a.key, a.n, v0, a.V));
-    return;
-  }
   const uint32_t part = (uint32_t)(unit / cuts), cut = (uint32_t)(unit % cuts);
   const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
   const uint32_t from = part * kEmbedPart, to = a.n - from < kEmbedPart ? a.n : from + kEmbedPart;
@@ -411,9 +383,9 @@ __device__ inline void embed_sum(const EmbedGradArgs& a, uint32_t parts, uint32_
   else store_n<float, N>(a.part + ((int64_t)part * 2 + (before ? 0 : 1)) * a.d, c, sum);
 }
 template <typename G, typename T, int N>
-__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, uint32_t parts, uint32_t cuts, uint64_t units) {
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, uint32_t cuts, uint64_t units) {
   for (uint64_t unit = (uint64_t)blockIdx.x * 4 + wave_uniform(threadIdx.x >> 6); unit < units; unit += (uint64_t)gridDim.x * 4)
-    embed_sum<G, T, N>(a, parts, cuts, unit);
+    embed_sum<G, T, N>(a, cuts, unit);
 }
 
 // Joins the sums of a token that begins in a part and goes on behind it: each of the four
@@ -466,13 +438,14 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, uint32
   }
 }
 
-// A batch of up to kEmbedSmall slots, without a sort: a wave looks through its tokens for those of its
-// two rows of the table, and adds up their rows in the order of their slots.
-constexpr uint32_t kSmallRows = 2;
+// A batch of up to kEmbedSmall slots, without a sort: a wave looks through its tokens for those of
+// `each` rows of the table, and adds up their rows in the order of their slots.
 template <typename G, typename T, int N>
-__global__ __launch_bounds__(256) void embed_small_kernel(RowsArgs r, const int64_t* token, EmbedGradArgs a, uint32_t cuts,
-                                                          uint64_t units) {
-  constexpr int K = kEmbedSmall / 64, U = N == 1 ? 16 : 8;
+__global__ __launch_bounds__(256) void embed_small_kernel(RowsArgs r, const int64_t* token, EmbedGradArgs a, uint32_t each,
+                                                          uint32_t cuts, uint64_t units) {
+  constexpr int K = kEmbedSmall / 64, U = 8;
+  __shared__ uint32_t lists[4][kEmbedSmall];
+  uint32_t* const list = lists[threadIdx.x >> 6];
   const uint32_t lane = threadIdx.x & 63;
   const uint64_t first = (uint64_t)blockIdx.x * 4 + wave_uniform(threadIdx.x >> 6);
   if (first >= units) return;
@@ -482,47 +455,39 @@ __global__ __launch_bounds__(256) void embed_small_kernel(RowsArgs r, const int6
   for (int k = 0; k < K; ++k)
     if (k * 64 + lane >= r.n_slots) p[k].key = (uint32_t)a.V;
   for (uint64_t unit = first; unit < units; unit += (uint64_t)gridDim.x * 4) {
-    const int64_t v0 = (int64_t)(unit / cuts) * kSmallRows;
-    const uint32_t cut = (uint32_t)(unit % cuts);
-    const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
-    uint64_t absent = 0;
-    for (uint32_t v = 0; v < kSmallRows && v0 + v < a.V; ++v) {
-      uint64_t has[K], any = 0;
+    const int64_t v0 = (int64_t)(unit / cuts) * each, v1 = v0 + each < a.V ? v0 + each : a.V;
+    const Cols<N> c((int)(((uint32_t)(unit % cuts)) * 64 + lane) * N, a.d);
+    for (int64_t v = v0; v < v1; ++v) {
+      int count = 0;
 #pragma unroll
-      for (int k = 0; k < K; ++k) any |= has[k] = __ballot(p[k].key == (uint32_t)v0 + v);
-      if (!any) {
-        absent |= 1ull << v;
-        continue;
+      for (int k = 0; k < K; ++k) {  // the rows of the slots that have the token, in their order
+        const bool mine = p[k].key == (uint32_t)v;
+        const uint64_t has = __ballot(mine);
+        if (mine) list[count + __popcll(has & ((1ull << lane) - 1))] = p[k].row;
+        count += (int)__popcll(has);
       }
+      if (a.accumulate && count == 0) continue;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       float sum[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) sum[e] = 0.f;
+      for (int i0 = 0; i0 < count; i0 += U) {
+        const uint32_t rows = list[i0 + (lane & (U - 1)) < (uint32_t)count ? i0 + (lane & (U - 1)) : i0];
+        Raw<G, N> x[U];
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        while (has[k]) {
-          Raw<G, N> x[U];
-          const int count = __popcll(has[k]) < U ? (int)__popcll(has[k]) : U;
-          uint64_t left = has[k];
+        for (int u = 0; u < U; ++u)
+          x[u].load((const G*)a.dout + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)rows, u) * a.ldd + c.at);
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int at = __builtin_ctzll(left);
-            if (u + 1 < count) left &= left - 1;  // the last one again behind it
-            x[u].load((const G*)a.dout + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)p[k].row, at) * a.ldd + c.at);
-          }
+        for (int u = 0; u < U; ++u) {
+          if (i0 + u >= count) break;
+          float f[N];
+          x[u].get(f);
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            if (u >= count) break;
-            has[k] &= has[k] - 1;
-            float f[N];
-            x[u].get(f);
-#pragma unroll
-            for (int e = 0; e < N; ++e) sum[e] += f[e];
-          }
+          for (int e = 0; e < N; ++e) sum[e] += f[e];
         }
       }
-      put_sum<T, N>(a, (uint32_t)v0 + v, c, sum);
+      put_sum<T, N>(a, (uint32_t)v, c, sum);
     }
-    if (!a.accumulate && cut == 0) zero_rows<T>(a, v0, absent);
   }
 }
 
@@ -536,16 +501,17 @@ hipError_t embed_rows(const RowsArgs& r, const EmbedArgs& a, hipStream_t s) {
 template <typename G, typename T, int N>
 hipError_t embed_small(const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a, hipStream_t s) {
   const uint32_t cuts = (uint32_t)((a.d + 64 * N - 1) / (64 * N));
-  const uint64_t units = ((uint64_t)a.V + kSmallRows - 1) / kSmallRows * cuts;
-  hipLaunchKernelGGL((embed_small_kernel<G, T, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, r, token, a, cuts, units);
+  const uint32_t each = a.V <= 8192 ? 1 : 8;  // few rows: a wave for each
+  const uint64_t units = ((uint64_t)a.V + each - 1) / each * cuts;
+  hipLaunchKernelGGL((embed_small_kernel<G, T, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, r, token, a, each, cuts,
+                     units);
   return hipGetLastError();
 }
 template <typename G, typename T, int N>
 hipError_t embed_sums(const EmbedGradArgs& a, hipStream_t s) {
   const uint32_t parts = (a.n + kEmbedPart - 1) / kEmbedPart, cuts = (uint32_t)((a.d + 64 * N - 1) / (64 * N));
-  const uint64_t zero = a.accumulate ? 0 : ((uint64_t)a.V + kZeroRows - 1) / kZeroRows;
-  const uint64_t units = (uint64_t)parts * cuts + zero;
-  hipLaunchKernelGGL((embed_sum_kernel<G, T, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, a, parts, cuts, units);
+  const uint64_t units = (uint64_t)parts * cuts;
+  hipLaunchKernelGGL((embed_sum_kernel<G, T, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, a, cuts, units);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts < 2) return e;
   hipLaunchKernelGGL((embed_join_kernel<T, N>), dim3(grid_of((uint64_t)(parts - 1) * cuts)), dim3(256), 0, s, a, parts, cuts);
@@ -564,23 +530,29 @@ hipError_t launch_embed(int table_dtype, int out_dtype, const RowsArgs& r, const
   });
 }
 
-hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, hipStream_t s) {
+hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, EmbedZero z, hipStream_t s) {
+  // 64 KB and more of zeros a workgroup, spread over the launches
+  const uint32_t launches = r.n_slots <= kSortKeys ? 1 : 2 * (uint32_t)e.passes;
+  const uint64_t bytes = (uint64_t)z.rows * (uint64_t)z.row, want = (bytes + 65535) / 65536;
+  z.blocks = (uint32_t)((want + launches - 1) / launches < 512 ? (want + launches - 1) / launches : 512);
+  z.shares = z.blocks * launches;
   if (r.n_slots <= 1024) {
-    hipLaunchKernelGGL(embed_sort_one_kernel<1>, dim3(1), dim3(1024), 0, s, r, token, V, e);
+    hipLaunchKernelGGL(embed_sort_one_kernel<1>, dim3(1 + z.blocks), dim3(1024), 0, s, r, token, V, e, z);
     return hipGetLastError();
   }
   if (r.n_slots <= kSortKeys) {
-    hipLaunchKernelGGL(embed_sort_one_kernel<kSortRounds>, dim3(1), dim3(1024), 0, s, r, token, V, e);
+    hipLaunchKernelGGL(embed_sort_one_kernel<kSortRounds>, dim3(1 + z.blocks), dim3(1024), 0, s, r, token, V, e, z);
     return hipGetLastError();
   }
+  const dim3 grid(e.blocks + z.blocks);
   for (int pass = 0; pass < e.passes; ++pass) {
-    if (pass == 0) hipLaunchKernelGGL(embed_count_kernel<true>, dim3(e.blocks), dim3(1024), 0, s, r, token, V, e, pass);
-    else hipLaunchKernelGGL(embed_count_kernel<false>, dim3(e.blocks), dim3(1024), 0, s, r, token, V, e, pass);
+    if (pass == 0) hipLaunchKernelGGL(embed_count_kernel<true>, grid, dim3(1024), 0, s, r, token, V, e, z, pass);
+    else hipLaunchKernelGGL(embed_count_kernel<false>, grid, dim3(1024), 0, s, r, token, V, e, z, pass);
     if (e.blocks <= 32) {
-      hipLaunchKernelGGL(embed_place_kernel<true>, dim3(e.blocks), dim3(1024), 0, s, e, r.n_slots, pass);
+      hipLaunchKernelGGL(embed_place_kernel<true>, grid, dim3(1024), 0, s, e, z, r.n_slots, pass);
     } else {
       hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(1024), 0, s, e);
-      hipLaunchKernelGGL(embed_place_kernel<false>, dim3(e.blocks), dim3(1024), 0, s, e, r.n_slots, pass);
+      hipLaunchKernelGGL(embed_place_kernel<false>, grid, dim3(1024), 0, s, e, z, r.n_slots, pass);
     }
   }
   return hipGetLastError();

@@ -341,7 +341,13 @@ inline int sort_bits(int64_t V) {
   const int passes = sort_passes(V);
   return (bits + passes - 1) / passes;
 }
-hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, hipStream_t s);
+// The rows of a gradient that the sort's launches write zeros to, beside the sort (0 rows: none).
+struct EmbedZero {
+  char* to;
+  int64_t rows, row, ld;    // row and stride in bytes
+  uint32_t blocks, shares;  // workgroups of a launch, and of all; set by the launch
+};
+hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, EmbedZero z, hipStream_t s);
 // A wave adds up the rows of kEmbedPart neighbours in that order; a token whose rows
 // reach past a part leaves sums to be joined.
 constexpr uint32_t kEmbedPart = 32;
