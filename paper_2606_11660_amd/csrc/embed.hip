@@ -166,16 +166,21 @@ __device__ inline void place_pairs(uint32_t* base, const EmbedSort& e, int pass,
     }
   }
 }
-// Counts of 16 waves to the first places of their pairs, over a workgroup's digits.
-__device__ inline void wave_places(uint32_t (&base)[16][kBinsMost], uint32_t bin, uint32_t at) {
-  for (int w = 0; w < 16; ++w) {
-    const uint32_t c = base[w][bin];
+// Counts of a workgroup's waves to the first places of their pairs of one digit.
+template <int NW>
+__device__ inline void wave_places(uint32_t (&base)[NW][kBinsMost], uint32_t bin, uint32_t at) {
+  uint32_t c[NW];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) c[w] = base[w][bin];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
     base[w][bin] = at;
-    at += c;
+    at += c[w];
   }
 }
 // A wave's share of a workgroup's kSortKeys pairs.
-constexpr int kSortRounds = kSortKeys / 1024;
+constexpr int kSortWaves = 8, kSortThreads = 64 * kSortWaves, kSortRounds = kSortKeys / kSortThreads;
+static_assert(kBinsMost <= kSortThreads, "a thread for each digit");
 struct Share {
   uint32_t from, to;
   __device__ inline Share(uint32_t n, uint32_t wave, uint32_t each) {
@@ -207,8 +212,10 @@ __global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const 
     __syncthreads();
     uint32_t mine = 0, total;
     const uint32_t b = threadIdx.x;
-    if (b < bins)
+    if (b < bins) {
+#pragma unroll
       for (int k = 0; k < 16; ++k) mine += base[k][b];
+    }
     const uint32_t at = block_before<16>(mine, sm, total);
     if (b < bins) wave_places(base, b, at);
     __syncthreads();
@@ -221,12 +228,12 @@ __global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const 
 // Longer ones, pass by pass: each workgroup counts its pairs' digits (the first pass leaves the
 // pairs themselves behind), the counts are added up, and each workgroup puts its pairs in their places.
 template <bool FIRST>
-__global__ __launch_bounds__(1024) void embed_count_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, EmbedZero z, int pass) {
+__global__ __launch_bounds__(kSortThreads) void embed_count_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, EmbedZero z, int pass) {
   __shared__ uint32_t count[kBinsMost];
   if (blockIdx.x >= e.blocks) return zero_share(z, 2 * pass * z.blocks + blockIdx.x - e.blocks);
   const uint32_t bins = 1u << e.bits;
-  for (uint32_t b = threadIdx.x; b < bins; b += 1024) count[b] = 0;
-  const Share w(r.n_slots, wave_uniform(threadIdx.x >> 6), kSortKeys / 16);
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) count[b] = 0;
+  const Share w(r.n_slots, wave_uniform(threadIdx.x >> 6), kSortKeys / kSortWaves);
   Pair p[kSortRounds];
   if (w.from < w.to) {
     if (FIRST) load_tokens<kSortRounds>(r, token, V, w.from, w.to, p);
@@ -245,7 +252,7 @@ __global__ __launch_bounds__(1024) void embed_count_kernel(RowsArgs r, const int
     }
   }
   __syncthreads();
-  for (uint32_t b = threadIdx.x; b < bins; b += 1024) e.count[(uint64_t)b * e.blocks + blockIdx.x] = count[b];
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) e.count[(uint64_t)b * e.blocks + blockIdx.x] = count[b];
 }
 // Counts of many workgroups to first places, by one.
 __global__ __launch_bounds__(1024) void embed_scan_kernel(EmbedSort e) {
@@ -271,25 +278,31 @@ __global__ __launch_bounds__(1024) void embed_scan_kernel(EmbedSort e) {
 }
 // SCAN: the counts are those of few workgroups, and each adds them up by itself.
 template <bool SCAN>
-__global__ __launch_bounds__(1024) void embed_place_kernel(EmbedSort e, EmbedZero z, uint32_t n, int pass) {
-  __shared__ uint32_t base[16][kBinsMost];
+__global__ __launch_bounds__(kSortThreads) void embed_place_kernel(EmbedSort e, EmbedZero z, uint32_t n, int pass) {
+  __shared__ uint32_t base[kSortWaves][kBinsMost];
   __shared__ uint32_t sm[16];
   if (blockIdx.x >= e.blocks) return zero_share(z, (2 * pass + 1) * z.blocks + blockIdx.x - e.blocks);
   const int lane = threadIdx.x & 63;
   const uint32_t wave = wave_uniform(threadIdx.x >> 6), bins = 1u << e.bits, b = threadIdx.x;
-  const Share w(n, wave, kSortKeys / 16);
+  const Share w(n, wave, kSortKeys / kSortWaves);
   Pair p[kSortRounds];
   if (w.from < w.to) load_pairs<kSortRounds>(e.key[pass & 1], e.row[pass & 1], w.from, w.to, p);
   uint32_t at = 0;
   if (SCAN) {
     uint32_t mine = 0, before = 0, total;
     if (b < bins)
-      for (uint32_t k = 0; k < e.blocks; ++k) {
-        const uint32_t c = e.count[(uint64_t)b * e.blocks + k];
-        mine += c;
-        if (k < blockIdx.x) before += c;
+      for (uint32_t k0 = 0; k0 < e.blocks; k0 += 8) {
+        uint32_t c[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) c[k] = e.count[(uint64_t)b * e.blocks + (k0 + k < e.blocks ? k0 + k : k0)];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+          if (k0 + k >= e.blocks) c[k] = 0;
+          mine += c[k];
+          if (k0 + k < blockIdx.x) before += c[k];
+        }
       }
-    at = block_before<16>(mine, sm, total) + before;
+    at = block_before<kSortWaves>(mine, sm, total) + before;
   } else if (b < bins) {
     at = e.count[(uint64_t)b * e.blocks + blockIdx.x];
   }
@@ -532,7 +545,7 @@ hipError_t launch_embed(int table_dtype, int out_dtype, const RowsArgs& r, const
 
 hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, EmbedZero z, hipStream_t s) {
   // 64 KB and more of zeros a workgroup, spread over the launches
-  const uint32_t launches = r.n_slots <= kSortKeys ? 1 : 2 * (uint32_t)e.passes;
+  const uint32_t launches = r.n_slots <= kSortOne ? 1 : 2 * (uint32_t)e.passes;
   const uint64_t bytes = (uint64_t)z.rows * (uint64_t)z.row, want = (bytes + 65535) / 65536;
   z.blocks = (uint32_t)((want + launches - 1) / launches < 512 ? (want + launches - 1) / launches : 512);
   z.shares = z.blocks * launches;
@@ -540,19 +553,19 @@ hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V,
     hipLaunchKernelGGL(embed_sort_one_kernel<1>, dim3(1 + z.blocks), dim3(1024), 0, s, r, token, V, e, z);
     return hipGetLastError();
   }
-  if (r.n_slots <= kSortKeys) {
-    hipLaunchKernelGGL(embed_sort_one_kernel<kSortRounds>, dim3(1 + z.blocks), dim3(1024), 0, s, r, token, V, e, z);
+  if (r.n_slots <= kSortOne) {
+    hipLaunchKernelGGL(embed_sort_one_kernel<kSortOne / 1024>, dim3(1 + z.blocks), dim3(1024), 0, s, r, token, V, e, z);
     return hipGetLastError();
   }
   const dim3 grid(e.blocks + z.blocks);
   for (int pass = 0; pass < e.passes; ++pass) {
-    if (pass == 0) hipLaunchKernelGGL(embed_count_kernel<true>, grid, dim3(1024), 0, s, r, token, V, e, z, pass);
-    else hipLaunchKernelGGL(embed_count_kernel<false>, grid, dim3(1024), 0, s, r, token, V, e, z, pass);
+    if (pass == 0) hipLaunchKernelGGL(embed_count_kernel<true>, grid, dim3(kSortThreads), 0, s, r, token, V, e, z, pass);
+    else hipLaunchKernelGGL(embed_count_kernel<false>, grid, dim3(kSortThreads), 0, s, r, token, V, e, z, pass);
     if (e.blocks <= 32) {
-      hipLaunchKernelGGL(embed_place_kernel<true>, grid, dim3(1024), 0, s, e, z, r.n_slots, pass);
+      hipLaunchKernelGGL(embed_place_kernel<true>, grid, dim3(kSortThreads), 0, s, e, z, r.n_slots, pass);
     } else {
       hipLaunchKernelGGL(embed_scan_kernel, dim3(1), dim3(1024), 0, s, e);
-      hipLaunchKernelGGL(embed_place_kernel<false>, grid, dim3(1024), 0, s, e, z, r.n_slots, pass);
+      hipLaunchKernelGGL(embed_place_kernel<false>, grid, dim3(kSortThreads), 0, s, e, z, r.n_slots, pass);
     }
   }
   return hipGetLastError();
@@ -561,7 +574,7 @@ hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V,
 hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArgs& a, hipStream_t s) {
   return with_type(dout_dtype, [&](auto g) {
     return with_type(table_dtype, [&](auto t) {
-      if (a.d > 256) return embed_sums<decltype(g), decltype(t), 8>(a, s);
+      if (a.d > 1024) return embed_sums<decltype(g), decltype(t), 8>(a, s);
       if (a.d > 64) return embed_sums<decltype(g), decltype(t), 4>(a, s);
       return embed_sums<decltype(g), decltype(t), 1>(a, s);
     });

@@ -328,8 +328,9 @@ struct EmbedSort {
   int passes, bits;   // bits of a pass's digit
   uint32_t blocks;
 };
-constexpr uint32_t kSortKeys = 4096;        // keys of a workgroup; one sorts as many alone
-constexpr int kSortBits = 10;               // of a digit, at most
+constexpr uint32_t kSortOne = 4096;   // keys that one workgroup sorts alone
+constexpr uint32_t kSortKeys = 2048;  // keys of each of several
+constexpr int kSortBits = 9;          // of a digit, at most
 inline int sort_passes(int64_t V) {
   int bits = 1;
   while ((V >> bits) != 0) ++bits;  // of the key V
