@@ -28,6 +28,32 @@ __device__ inline float update_of(const MuonArgs& a, float m, float g) {  // m a
   return a.nesterov ? m * a.momentum + g * a.one_momentum : m;
 }
 
+// Four elements at any element's address, n of them there (the others are 0).
+template <typename T>
+__device__ inline void load4(const T* p, int n, float (&x)[4]) {
+  if (n >= 4) {
+    Raw<T, 4> r;
+    r.load(p);
+    r.get(x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = e < n ? (float)p[e] : 0.f;
+  }
+}
+template <typename T>
+__device__ inline void store4(T* p, int n, const float (&x)[4]) {
+  if (n >= 4) {
+    Raw<T, 4> r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.set(e, (T)x[e]);
+    *reinterpret_cast<typename Raw<T, 4>::vec*>(p) = r.v[0];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = (T)x[e];
+  }
+}
+
 // What u is multiplied by to have the norm 1, from |u|^2: 0 for zeros, NaN past all numbers.
 __device__ inline double inverse_norm(double square) {
   return square > 0 ? (square < INFINITY ? 1.0 / sqrt(square) : NAN) : square == 0 ? 0.0 : NAN;

@@ -35,32 +35,6 @@ __device__ inline double block_sum(double v, double* sm) {
   return sm[0] + sm[1] + sm[2] + sm[3];
 }
 
-// Four elements at any element's address, n of them there (the others are 0).
-template <typename T>
-__device__ inline void load4(const T* p, int n, float (&x)[4]) {
-  if (n >= 4) {
-    Raw<T, 4> r;
-    r.load(p);
-    r.get(x);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = e < n ? (float)p[e] : 0.f;
-  }
-}
-template <typename T>
-__device__ inline void store4(T* p, int n, const float (&x)[4]) {
-  if (n >= 4) {
-    Raw<T, 4> r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r.set(e, (T)x[e]);
-    *reinterpret_cast<typename Raw<T, 4>::vec*>(p) = r.v[0];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (e < n) p[e] = (T)x[e];
-  }
-}
-
 // The momentum's step, and a workgroup's share of |u|^2.
 template <typename G>
 __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {

@@ -18,9 +18,32 @@ namespace {
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 __device__ inline f64x4 mma(double a, double b, f64x4 c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0); }
 
+// Times 16 rows of a wave whose loads are in flight together.
+template <int T>
+constexpr int rounds_of() { return T == 1 ? 4 : T == 2 ? 2 : 1; }
+
 // Element (l, s) of a matrix whose longer side is l: its place.
 __device__ inline int64_t place_of(const MuonGroup& q, int l, int s) {
   return q.rows >= q.cols ? (int64_t)l * q.cols + s : (int64_t)s * q.cols + l;
+}
+
+// Momentum and gradient of four of the longer side from r on at s of the shorter one, below l1.
+template <typename G>
+__device__ inline void load_run(const MuonGroup& q, const MuonEntry& en, bool turned, int r, int s, int l1, const G* gt,
+                                float (&m)[4], float (&g)[4]) {
+  const int n = s < q.S ? l1 - r : 0;
+  if (turned) {
+    const int64_t p = n > 0 ? (int64_t)s * q.cols + r : 0;
+    load4(en.m + p, n, m);
+    load4(gt + p, n, g);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t p = e < n ? (int64_t)(r + e) * q.cols + s : 0;
+      m[e] = e < n ? en.m[p] : 0.f;
+      g[e] = e < n ? (float)gt[p] : 0.f;
+    }
+  }
 }
 
 // The momentum's step, and G's upper tiles over kThinRows of the longer side: a wave adds up every
@@ -30,46 +53,51 @@ __global__ __launch_bounds__(256) void muon_thin_gram_kernel(MuonArgs a) {
   constexpr int TILES = T * (T + 1) / 2;
   __shared__ double sm[3][TILES * 256];
   const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_flat; });
-  const uint32_t at = blockIdx.x - q.tile_flat, i = at / q.n_flat, part = at - i * q.n_flat;
-  const MuonEntry& en = a.table[q.entry + i];
+  const uint32_t at = blockIdx.x - q.tile_flat, mat = at / q.n_flat, part = at - mat * q.n_flat;
+  const MuonEntry& en = a.table[q.entry + mat];
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6));
   const int l0 = (int)part * kThinRows, l1 = q.L - l0 < kThinRows ? q.L : l0 + kThinRows;
+  const bool turned = q.rows < q.cols;
   f64x4 acc[TILES];
 #pragma unroll
   for (int k = 0; k < TILES; ++k) acc[k] = f64x4{0, 0, 0, 0};
-  for (int l = l0 + wave * 16; l < l1; l += 64) {
+  constexpr int R = rounds_of<T>();
+  for (int l = l0 + wave * 16; l < l1; l += 64 * R) {
     // K in fours: step e takes the rows l + 4 (lane / 16) + e
-    float m[T][4], g[T][4];
+    float m[R][T][4], g[R][T][4];
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = l + 4 * (lane >> 4) + e, s = 16 * t + (lane & 15);
-        m[t][e] = g[t][e] = 0.f;
-        if (r < l1 && s < q.S) {
-          const int64_t p = place_of(q, r, s);
-          m[t][e] = en.m[p];
-          g[t][e] = (float)((const G*)en.g)[p];
+      for (int t = 0; t < T; ++t)
+        load_run(q, en, turned, l + 64 * i + 4 * (lane >> 4), 16 * t + (lane & 15), l1, (const G*)en.g, m[i][t], g[i][t]);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      double u[T][4];
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const int r = l + 64 * i + 4 * (lane >> 4), s = 16 * t + (lane & 15), n = s < q.S ? l1 - r : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float gr = g[i][t][e] * gs;
+          m[i][t][e] = momentum_of(a, m[i][t][e], gr);
+          u[t][e] = e < n ? (double)update_of(a, m[i][t][e], gr) : 0.0;
+        }
+        if (turned) {
+          if (n > 0) store4(en.m + (int64_t)s * q.cols + r, n, m[i][t]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < n) en.m[(int64_t)(r + e) * q.cols + s] = m[i][t][e];
         }
       }
-    double u[T][4];
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = l + 4 * (lane >> 4) + e, s = 16 * t + (lane & 15);
-        const float gr = g[t][e] * gs, mo = momentum_of(a, m[t][e], gr);
-        const bool there = r < l1 && s < q.S;
-        u[t][e] = there ? (double)update_of(a, mo, gr) : 0.0;
-        if (there) en.m[place_of(q, r, s)] = mo;
-      }
+        for (int tj = 0, k = 0; tj < T; ++tj)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int tj = 0, k = 0; tj < T; ++tj)
-#pragma unroll
-        for (int ti = 0; ti <= tj; ++ti, ++k) acc[k] = mma(u[ti][e], u[tj][e], acc[k]);
+          for (int ti = 0; ti <= tj; ++ti, ++k) acc[k] = mma(u[ti][e], u[tj][e], acc[k]);
+    }
   }
   if (wave > 0) {
 #pragma unroll
@@ -79,7 +107,7 @@ __global__ __launch_bounds__(256) void muon_thin_gram_kernel(MuonArgs a) {
   }
   __syncthreads();
   if (wave > 0) return;
-  double* const out = reinterpret_cast<double*>(q.base + i * q.stride + q.gram) + (int64_t)part * TILES * 256;
+  double* const out = reinterpret_cast<double*>(q.base + mat * q.stride + q.gram) + (int64_t)part * TILES * 256;
 #pragma unroll
   for (int k = 0; k < TILES; ++k)
 #pragma unroll
@@ -178,55 +206,79 @@ template <typename P, typename G, bool MASTER, int T>
 __global__ __launch_bounds__(256) void muon_thin_apply_kernel(MuonArgs a) {
   constexpr int W = 16 * T;
   const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_flat; });
-  const uint32_t at = blockIdx.x - q.tile_flat, i = at / q.n_flat, part = at - i * q.n_flat;
-  const MuonEntry& en = a.table[q.entry + i];
+  const uint32_t at = blockIdx.x - q.tile_flat, mat = at / q.n_flat, part = at - mat * q.n_flat;
+  const MuonEntry& en = a.table[q.entry + mat];
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6));
   const int low = lane & 15, high = lane >> 4;
   const int l0 = (int)part * kThinRows, l1 = q.L - l0 < kThinRows ? q.L : l0 + kThinRows;
-  const double* const Q = reinterpret_cast<const double*>(q.base + i * q.stride + q.poly);
+  const double* const Q = reinterpret_cast<const double*>(q.base + mat * q.stride + q.poly);
   const bool turned = q.rows < q.cols;
+  typedef typename std::conditional<MASTER, float, P>::type W_;
   P* const pt = (P*)en.p;
-  for (int l = l0 + wave * 16; l < l1; l += 64) {
+  const W_* const weights = MASTER ? (const W_*)en.master : (const W_*)en.p;
+  constexpr int R = rounds_of<T>();
+  for (int l = l0 + wave * 16; l < l1; l += 64 * R) {
     // K step (t, e) takes the columns 16 t + 4 (lane / 16) + e
-    float m[T][4], g[T][4];
+    float m[R][T][4], g[R][T][4];
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = l + low, s = 16 * t + 4 * high + e;
-        m[t][e] = g[t][e] = 0.f;
-        if (r < l1 && s < q.S) {
-          const int64_t p = place_of(q, r, s);
-          m[t][e] = en.m[p];
-          g[t][e] = (float)((const G*)en.g)[p];
+      for (int t = 0; t < T; ++t)
+      {
+        const int r = l + 64 * i + low, s = 16 * t + 4 * high, n = r < l1 ? q.S - s : 0;
+        if (turned) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int64_t p = e < n ? (int64_t)(s + e) * q.cols + r : 0;
+            m[i][t][e] = e < n ? en.m[p] : 0.f;
+            g[i][t][e] = e < n ? (float)((const G*)en.g)[p] : 0.f;
+          }
+        } else {
+          const int64_t p = n > 0 ? (int64_t)r * q.cols + s : 0;
+          load4(en.m + p, n, m[i][t]);
+          load4((const G*)en.g + p, n, g[i][t]);
         }
       }
-    f64x4 acc[T];
+    f64x4 acc[R][T];
 #pragma unroll
-    for (int t = 0; t < T; ++t) acc[t] = f64x4{0, 0, 0, 0};
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int t = 0; t < T; ++t) acc[i][t] = f64x4{0, 0, 0, 0};
 #pragma unroll
     for (int t = 0; t < T; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const double u = (double)update_of(a, m[t][e], g[t][e] * gs);
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int o = 0; o < T; ++o) {
           const double x = Q[(16 * t + 4 * high + e) * W + 16 * o + low];
-          acc[o] = turned ? mma(x, u, acc[o]) : mma(u, x, acc[o]);  // D's column, its lanes' neighbours, is the weights'
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const double u = (double)update_of(a, m[i][t][e], g[i][t][e] * gs);
+            acc[i][o] = turned ? mma(x, u, acc[i][o]) : mma(u, x, acc[i][o]);  // D's column, its lanes' neighbours, is the weights'
+          }
         }
-      }
 #pragma unroll
-    for (int o = 0; o < T; ++o)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = l + (turned ? low : high + 4 * e), s = 16 * o + (turned ? high + 4 * e : low);
-        if (r >= l1 || s >= q.S) continue;
-        const int64_t p = place_of(q, r, s);
-        const float w = MASTER ? en.master[p] : (float)pt[p];
-        const float nw = stepped(w, (float)acc[o][e], en.lr, en.lr_wd);
-        if (MASTER) en.master[p] = nw;
-        pt[p] = (P)nw;
+      for (int o = 0; o < T; ++o) {
+        W_ w[4];
+        int64_t p[4];
+        bool there[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = l + 64 * i + (turned ? low : high + 4 * e), s = 16 * o + (turned ? high + 4 * e : low);
+          there[e] = r < l1 && s < q.S;
+          p[e] = there[e] ? place_of(q, r, s) : 0;
+          w[e] = weights[p[e]];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!there[e]) continue;
+          const float nw = stepped((float)w[e], (float)acc[i][o][e], en.lr, en.lr_wd);
+          if (MASTER) en.master[p[e]] = nw;
+          pt[p[e]] = (P)nw;
+        }
       }
   }
 }
