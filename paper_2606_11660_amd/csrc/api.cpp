@@ -1438,7 +1438,7 @@ EmbedLayout embed_layout(const attr_rows* r, int64_t V, int64_t d) {
   L.row[1] = 3 * each;
   L.count = 4 * each;
   const size_t blocks = (n + attr::kSortKeys - 1) / attr::kSortKeys;
-  L.part = L.count + (n > attr::kSortOne ? align_up((blocks << attr::sort_bits(V)) * 4) : 0);
+  L.part = L.count + (n > attr::kSortOne ? align_up((blocks << attr::sort_bits(V)) * 8) : 0);
   const size_t parts = (n + attr::kEmbedPart - 1) / attr::kEmbedPart;
   L.total = L.part + align_up(parts * 2 * (size_t)d * 4);
   return L;

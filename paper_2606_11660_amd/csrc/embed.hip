@@ -150,8 +150,9 @@ __device__ inline void count_pairs(uint32_t* count, const Pair (&p)[K], uint32_t
   for (int k = 0; k < K; ++k)
     if (from + k * 64 + (threadIdx.x & 63) < to) atomicAdd(&count[(p[k].key >> shift) & (bins - 1)], 1u);
 }
-template <int K>
-__device__ inline void place_pairs(uint32_t* base, const EmbedSort& e, int pass, const Pair (&p)[K], uint32_t from, uint32_t to) {
+template <int K, typename F>
+__device__ inline void place_pairs(uint32_t* base, const EmbedSort& e, int pass, const Pair (&p)[K], uint32_t from, uint32_t to,
+                                   F placed) {
   uint32_t* const key = e.key[(pass + 1) & 1];
   uint32_t* const row = e.row[(pass + 1) & 1];
   const uint32_t bins = 1u << e.bits;
@@ -163,6 +164,7 @@ __device__ inline void place_pairs(uint32_t* base, const EmbedSort& e, int pass,
     if (live) {
       key[at] = p[k].key;
       row[at] = p[k].row;
+      placed(p[k].key, at);
     }
   }
 }
@@ -219,7 +221,7 @@ __global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const 
     const uint32_t at = block_before<16>(mine, sm, total);
     if (b < bins) wave_places(base, b, at);
     __syncthreads();
-    place_pairs<K>(base[wave], e, pass, p, w.from, w.to);
+    place_pairs<K>(base[wave], e, pass, p, w.from, w.to, [](uint32_t, uint32_t) {});
     __threadfence_block();
     __syncthreads();
   }
@@ -227,6 +229,15 @@ __global__ __launch_bounds__(1024) void embed_sort_one_kernel(RowsArgs r, const 
 
 // Longer ones, pass by pass: each workgroup counts its pairs' digits (the first pass leaves the
 // pairs themselves behind), the counts are added up, and each workgroup puts its pairs in their places.
+// Two passes over few workgroups (kNextMost counts) take three launches: the first placing counts the
+// second pass's digits where the pairs went, in LDS first.
+constexpr uint32_t kNextMost = 8192;
+__host__ __device__ inline bool counts_next(const EmbedSort& e) {
+  return e.passes == 2 && e.blocks <= 32 && (e.blocks << e.bits) <= kNextMost;
+}
+__device__ inline uint32_t* counts_of(const EmbedSort& e, int pass) {
+  return e.count + (pass && counts_next(e) ? e.blocks << e.bits : 0u);
+}
 template <bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void embed_count_kernel(RowsArgs r, const int64_t* token, int64_t V, EmbedSort e, EmbedZero z, int pass) {
   __shared__ uint32_t count[kBinsMost];
@@ -252,7 +263,10 @@ __global__ __launch_bounds__(kSortThreads) void embed_count_kernel(RowsArgs r, c
     }
   }
   __syncthreads();
-  for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) e.count[(uint64_t)b * e.blocks + blockIdx.x] = count[b];
+  for (uint32_t b = threadIdx.x; b < bins; b += kSortThreads) {
+    counts_of(e, pass)[(uint64_t)b * e.blocks + blockIdx.x] = count[b];
+    if (FIRST && counts_next(e)) counts_of(e, 1)[(uint64_t)b * e.blocks + blockIdx.x] = 0;
+  }
 }
 // Counts of many workgroups to first places, by one.
 __global__ __launch_bounds__(1024) void embed_scan_kernel(EmbedSort e) {
@@ -281,7 +295,11 @@ template <bool SCAN>
 __global__ __launch_bounds__(kSortThreads) void embed_place_kernel(EmbedSort e, EmbedZero z, uint32_t n, int pass) {
   __shared__ uint32_t base[kSortWaves][kBinsMost];
   __shared__ uint32_t sm[16];
-  if (blockIdx.x >= e.blocks) return zero_share(z, (2 * pass + 1) * z.blocks + blockIdx.x - e.blocks);
+  __shared__ uint32_t next[SCAN ? kNextMost : 1];  // counts of the next pass, as its table has them
+  if (blockIdx.x >= e.blocks) return zero_share(z, (2 * pass + 1 - (pass && counts_next(e) ? 1 : 0)) * z.blocks + blockIdx.x - e.blocks);
+  const bool ahead = SCAN && pass == 0 && counts_next(e);
+  if (ahead)
+    for (uint32_t k = threadIdx.x; k < e.blocks << e.bits; k += kSortThreads) next[k] = 0;
   const int lane = threadIdx.x & 63;
   const uint32_t wave = wave_uniform(threadIdx.x >> 6), bins = 1u << e.bits, b = threadIdx.x;
   const Share w(n, wave, kSortKeys / kSortWaves);
@@ -294,7 +312,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_place_kernel(EmbedSort e, 
       for (uint32_t k0 = 0; k0 < e.blocks; k0 += 8) {
         uint32_t c[8];
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) c[k] = e.count[(uint64_t)b * e.blocks + (k0 + k < e.blocks ? k0 + k : k0)];
+        for (uint32_t k = 0; k < 8; ++k) c[k] = counts_of(e, pass)[(uint64_t)b * e.blocks + (k0 + k < e.blocks ? k0 + k : k0)];
 #pragma unroll
         for (uint32_t k = 0; k < 8; ++k) {
           if (k0 + k >= e.blocks) c[k] = 0;
@@ -304,7 +322,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_place_kernel(EmbedSort e, 
       }
     at = block_before<kSortWaves>(mine, sm, total) + before;
   } else if (b < bins) {
-    at = e.count[(uint64_t)b * e.blocks + blockIdx.x];
+    at = counts_of(e, pass)[(uint64_t)b * e.blocks + blockIdx.x];
   }
   for (uint32_t k = lane; k < bins; k += 64) base[wave][k] = 0;
   __syncthreads();
@@ -312,7 +330,13 @@ __global__ __launch_bounds__(kSortThreads) void embed_place_kernel(EmbedSort e, 
   __syncthreads();
   if (b < bins) wave_places(base, b, at);
   __syncthreads();
-  place_pairs<kSortRounds>(base[wave], e, pass, p, w.from, w.to);
+  place_pairs<kSortRounds>(base[wave], e, pass, p, w.from, w.to, [&](uint32_t key, uint32_t to) {
+    if (ahead) atomicAdd(&next[((key >> e.bits) & (bins - 1)) * e.blocks + to / kSortKeys], 1u);
+  });
+  if (!ahead) return;
+  __syncthreads();
+  for (uint32_t k = threadIdx.x; k < e.blocks << e.bits; k += kSortThreads)
+    if (next[k]) atomicAdd(&counts_of(e, 1)[k], next[k]);
 }
 
 // ----------------------------------------------------------------------------
@@ -545,7 +569,8 @@ hipError_t launch_embed(int table_dtype, int out_dtype, const RowsArgs& r, const
 
 hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, EmbedZero z, hipStream_t s) {
   // 64 KB and more of zeros a workgroup, spread over the launches
-  const uint32_t launches = r.n_slots <= kSortOne ? 1 : 2 * (uint32_t)e.passes;
+  const bool skip = counts_next(e);  // the second pass's count
+  const uint32_t launches = r.n_slots <= kSortOne ? 1 : 2 * (uint32_t)e.passes - (skip ? 1 : 0);
   const uint64_t bytes = (uint64_t)z.rows * (uint64_t)z.row, want = (bytes + 65535) / 65536;
   z.blocks = (uint32_t)((want + launches - 1) / launches < 512 ? (want + launches - 1) / launches : 512);
   z.shares = z.blocks * launches;
@@ -560,7 +585,7 @@ hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V,
   const dim3 grid(e.blocks + z.blocks);
   for (int pass = 0; pass < e.passes; ++pass) {
     if (pass == 0) hipLaunchKernelGGL(embed_count_kernel<true>, grid, dim3(kSortThreads), 0, s, r, token, V, e, z, pass);
-    else hipLaunchKernelGGL(embed_count_kernel<false>, grid, dim3(kSortThreads), 0, s, r, token, V, e, z, pass);
+    else if (!skip) hipLaunchKernelGGL(embed_count_kernel<false>, grid, dim3(kSortThreads), 0, s, r, token, V, e, z, pass);
     if (e.blocks <= 32) {
       hipLaunchKernelGGL(embed_place_kernel<true>, grid, dim3(kSortThreads), 0, s, e, z, r.n_slots, pass);
     } else {

@@ -324,7 +324,7 @@ hipError_t launch_embed(int table_dtype, int out_dtype, const RowsArgs& r, const
 struct EmbedSort {
   uint32_t* key[2];   // [n_slots] each; the sorted pairs are in [passes & 1]
   uint32_t* row[2];
-  uint32_t* count;    // [bins][blocks], one workgroup's sort needs none
+  uint32_t* count;    // two of [bins][blocks], one workgroup's sort needs none
   int passes, bits;   // bits of a pass's digit
   uint32_t blocks;
 };
