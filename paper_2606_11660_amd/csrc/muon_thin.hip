@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * T * T) void muon_thin_poly_kernel(MuonArgs a, 
   if (ti <= tj) {
     const int tile = tj * (tj + 1) / 2 + ti;
     double x[4] = {0, 0, 0, 0};
-#pragma unroll 2
+#pragma unroll 8
     for (uint32_t p = 0; p < q.n_flat; ++p)
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] += parts[(int64_t)p * TILES * 256 + tile * 256 + e * 64 + lane];
@@ -182,7 +182,14 @@ __global__ __launch_bounds__(64 * T * T) void muon_thin_poly_kernel(MuonArgs a, 
       P[r][c] = (r == c ? (double)kNsA : 0.0) + (double)kNsB * A[r][c] + (double)kNsC * sq[e];
     }
     __syncthreads();
-    const f64x4 nq = product(P, Q), pa = product(P, A);
+    const f64x4 nq = product(P, Q);
+    if (step + 1 == steps) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 4; ++e) Q[r0 + 4 * e][c] = nq[e];
+      break;  // what is written below is this lane's own
+    }
+    const f64x4 pa = product(P, A);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
