@@ -923,7 +923,7 @@ def attr_muon_step(tensors: MuonTensors, lr: float, momentum: float = 0.95, nest
         if grad_scale.device != tensors.device:
             raise ValueError("every tensor must live on the same GPU device")
     pairs = tensors.default_pairs() if pairs is None else bool(pairs)
-    raw = _raw_stream(stream)
+    raw = _here(tensors.weights[0], stream)
     wsp, wsn = _ws(ws, tensors.device, raw).get(tensors.workspace_size(pairs), raw)
     _check(lib().attr_muon_step(tensors.array, len(tensors.array), tensors.p_dtype, tensors.g_dtype, lr, momentum,
                                 int(bool(nesterov)), steps, int(pairs), _ptr(grad_scale), wsp, wsn, raw))
@@ -994,6 +994,16 @@ def _rows_call(op: int, rows: Optional[ExampleRows], tensors: tuple, numbers: tu
     return False
 
 
+def _here(t: torch.Tensor, stream) -> int:
+    """The call's stream as a handle (0 for a CPU tensor, whose checks raise); the call's tensors live
+    on the current device, whose stream it is."""
+    if not t.is_cuda:
+        return 0
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("the call's tensors must live on the current GPU device")
+    return _raw_stream(stream)
+
+
 def _tokens(token: torch.Tensor, n_rows: int) -> None:
     _vector(token, n_rows, torch.int64, "token")
 
@@ -1002,7 +1012,7 @@ def attr_embed(table: torch.Tensor, token: torch.Tensor, out: torch.Tensor, scal
                rows: Optional[ExampleRows] = None, stream=None) -> torch.Tensor:
     """out[row] = scale * table[token[row]] (table [V, d], token int64 [n_rows], out [n_rows, d], any
     types); rows of tokens outside [0, V) are zeros."""
-    raw = _raw_stream(stream) if out.is_cuda else 0
+    raw = _here(out, stream)
     if _rows_call(_EMBED, rows, (table, token, out), (scale,), raw):
         return out
     n, d, ldo = _rows(out)
@@ -1027,7 +1037,7 @@ def attr_embed_backward(dout: torch.Tensor, token: torch.Tensor, dtable: torch.T
     """dtable[v] = scale * sum of dout's rows whose token is v (zeros where there is none), or with
     accumulate added to what dtable holds.  The same bits for the same call: tokens are sorted,
     and their rows added up in order."""
-    raw = _raw_stream(stream) if dout.is_cuda else 0
+    raw = _here(dout, stream)
     w = _ws(ws, dout.device, raw) if dout.is_cuda else None
     if _rows_call(_EMBED_BACK, rows, (dtable, token, dout), (scale, accumulate), raw, w):
         return dtable
@@ -1063,7 +1073,7 @@ def attr_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Ten
                     rstd: Optional[torch.Tensor] = None, rows: Optional[ExampleRows] = None, stream=None) -> torch.Tensor:
     """y = (x - mean) rstd weight + bias over the last dimension (x, y [n_rows, d], any types; weight
     and bias [d] of one type).  mean, rstd: fp32 [n_rows], what the backward pass takes.  y may be x."""
-    raw = _raw_stream(stream) if x.is_cuda else 0
+    raw = _here(x, stream)
     if _rows_call(_NORM, rows, (x, y, weight, bias, mean, rstd), (eps,), raw):
         return y
     n, d, ldx = _rows(x)
@@ -1092,7 +1102,7 @@ def attr_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tens
     """Gradients of attr_layer_norm into those of dx (x's shape and type; may be x or dy), dweight and
     dbias that are given.  dweight, dbias: fp32 [d], or with per_example [n_examples, d] (rows may be
     columns of wider ones): every example's own.  accumulate adds to what they hold."""
-    raw = _raw_stream(stream) if x.is_cuda else 0
+    raw = _here(x, stream)
     w = _ws(ws, x.device, raw) if x.is_cuda else None
     if _rows_call(_NORM_BACK, rows, (x, dy, weight, dx, mean, rstd, dweight, dbias), (per_example, accumulate), raw, w):
         return

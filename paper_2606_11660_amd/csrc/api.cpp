@@ -1092,7 +1092,8 @@ struct MuonRound {
   int kind;                    // sixteens of the shorter sides, all at most kThinMost; or kTiles, kBigTiles
   std::vector<int32_t> order;  // the matrices, group by group
   attr::MuonArgs args;         // but for the table and the workspace's address
-  uint32_t sym, full, flat, turn;  // workgroups
+  uint32_t sym, full, flat, turn, gram;  // workgroups
+  bool split;                  // some group's rows are divided
   size_t bytes;                // of workspace behind the table
 };
 struct MuonPlan {
@@ -1172,18 +1173,39 @@ MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
   const auto clear = [&] {
     R.order.clear();
     std::memset(&R.args, 0, sizeof(R.args));
-    R.sym = R.full = R.flat = R.turn = 0;
+    R.sym = R.full = R.flat = R.turn = R.gram = 0;
+    R.split = false;
     R.bytes = 0;
   };
   size_t most = 0, matrices = 0;
   const auto end = [&] {
     if (R.order.empty()) return;
+    uint32_t tiles = 0;
+    for (int k = 0; k < R.args.n_groups; ++k) tiles += R.args.g[k].n_sym * R.args.g[k].count;
+    const uint32_t slots = R.kind == kBigTiles ? 256 : 512;  // workgroups that the GPU holds at once
     for (int k = 0; k < R.args.n_groups; ++k) {
       attr::MuonGroup& q = R.args.g[k];
       q.tile_sym = R.sym;
       q.tile_full = R.full;
       R.sym += attr::muon_tiles(q.n_sym * q.count);
       R.full += attr::muon_tiles(q.n_full * q.count);
+      q.splits = 1;
+      if (q.n_sym == 0) continue;
+      const int32_t want = std::min({(int32_t)(slots / tiles), q.L / attr::kMuonSplitRows, attr::kMuonSplits});
+      if (want > 1) {
+        q.split_rows = ((q.L + want - 1) / want + 63) / 64 * 64;
+        q.splits = (uint32_t)((q.L + q.split_rows - 1) / q.split_rows);
+      } else {
+        q.split_rows = q.L;
+      }
+      q.tile_gram = R.gram;
+      R.gram += attr::muon_tiles(q.n_sym * q.count * q.splits);
+      if (q.splits > 1) {
+        const size_t side = R.kind == kBigTiles ? 2 * attr::kMuonTile : attr::kMuonTile;
+        q.part = reinterpret_cast<char*>(R.bytes);
+        R.bytes += (size_t)q.n_sym * q.count * q.splits * side * side * 4;
+        R.split = true;
+      }
     }
     most = std::max(most, R.bytes);
     matrices = std::max(matrices, R.order.size());
@@ -1309,7 +1331,10 @@ attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dt
         if (e != hipSuccess) return e;
       }
       attr::MuonArgs a = R.args;
-      for (int k = 0; k < a.n_groups; ++k) a.g[k].base = base + P.table + reinterpret_cast<uintptr_t>(a.g[k].base);
+      for (int k = 0; k < a.n_groups; ++k) {
+        a.g[k].base = base + P.table + reinterpret_cast<uintptr_t>(a.g[k].base);
+        a.g[k].part = base + P.table + reinterpret_cast<uintptr_t>(a.g[k].part);
+      }
       a.table = reinterpret_cast<const attr::MuonEntry*>(base);
       a.grad_scale = grad_scale;
       a.momentum = (float)momentum;
@@ -1326,7 +1351,8 @@ attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dt
       if (e == hipSuccess) e = attr::launch_muon_split((int)g_dtype, pairs != 0, a, R.turn, s);
       for (int32_t k = 0; k < steps && e == hipSuccess; ++k) {
         const int from = k & 1;
-        e = attr::launch_muon_gram(big, pairs != 0, from, a, R.sym, s);
+        e = attr::launch_muon_gram(big, pairs != 0, from, a, R.gram, s);
+        if (e == hipSuccess && R.split) e = attr::launch_muon_join(big, pairs != 0, a, R.sym, s);
         if (e == hipSuccess) e = attr::launch_muon_poly(big, pairs != 0, a, R.sym, s);
         if (e != hipSuccess) break;
         e = k + 1 < steps ? attr::launch_muon_apply(big, pairs != 0, from, a, R.full, s)

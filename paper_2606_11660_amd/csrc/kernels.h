@@ -431,6 +431,9 @@ struct MuonGroup {
   uint32_t tile_sym, tile_full, tile_flat, tile_turn;  // first workgroup of the group in each launch
   uint32_t n_sym, n_full, n_flat, n_turn;              // workgroups of a matrix
   uint32_t entry, count;  // first matrix in the table, matrices
+  char* part;             // the partial sums of A's tiles, [count][splits][n_sym] tiles of fp32; with one split none
+  uint32_t tile_gram, splits;  // first workgroup of A's launch; parts of Y's rows (of split_rows), one a workgroup
+  int32_t split_rows, pad;
   int32_t rows, cols, L, S, ld;
 };
 // Workgroups of a group's n tiles: an eighth for each die.
@@ -452,6 +455,9 @@ hipError_t launch_muon_thin_gram(int g_dtype, int t, const MuonArgs& a, uint32_t
 hipError_t launch_muon_thin_poly(int t, int steps, const MuonArgs& a, uint32_t matrices, hipStream_t s);
 hipError_t launch_muon_thin_apply(int p_dtype, int g_dtype, bool master, int t, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 constexpr int kMuonTile = 128;
+// A launch of few of A's tiles divides Y's rows: into parts of kMuonSplitRows rows or more, kMuonSplits
+// at most, one workgroup for each slot of the GPU.
+constexpr int kMuonSplitRows = 512, kMuonSplits = 32;
 constexpr int64_t kMuonFlat = 16384;   // elements of a workgroup of the momentum's launch, at least
 constexpr uint32_t kMuonFlatMost = 256;  // such workgroups of a matrix
 hipError_t launch_muon_table(const MuonTable& t, hipStream_t s);
@@ -459,6 +465,8 @@ hipError_t launch_muon_momentum(int g_dtype, const MuonArgs& a, uint32_t blocks,
 hipError_t launch_muon_split(int g_dtype, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 // big: tiles of 256 x 256, whose numbers the groups then hold
 hipError_t launch_muon_gram(bool big, bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+// A from the parts' sums, of the groups with more than one; blocks as for the polynomial
+hipError_t launch_muon_join(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 hipError_t launch_muon_poly(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 hipError_t launch_muon_apply(bool big, bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 hipError_t launch_muon_last(bool big, bool pairs, int p_dtype, bool master, int from, const MuonArgs& a, uint32_t blocks,

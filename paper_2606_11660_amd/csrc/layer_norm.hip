@@ -394,7 +394,7 @@ hipError_t launch_layer_norm(int x_dtype, int y_dtype, const RowsArgs& r, const 
 
 // Shares of a unit: workgroups enough to fill the GPU, each with several rows.
 uint32_t norm_chunks(uint32_t unit, uint32_t units, int32_t d) {
-  const uint32_t rows = d <= 1024 ? 16 : 4, most = d <= 2048 ? 1024 : 512;
+  const uint32_t rows = d <= 1024 ? 16 : d <= 16384 ? 4 : 1, most = d <= 2048 ? 1024 : 512;
   const uint32_t by_rows = (unit + rows - 1) / rows, by_units = most / units;
   return by_rows < by_units ? by_rows : by_units > 1 ? by_units : 1;
 }

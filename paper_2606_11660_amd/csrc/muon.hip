@@ -341,8 +341,9 @@ struct Stage {
   static constexpr int W = 16 * F, PITCH = W + 4, LANES = W / 8, PER = 64 / LANES;
   float* st;
   int lane;
+  static constexpr int FLOATS = 32 * PITCH;  // of a wave
   __device__ inline Stage(void* smem) {
-    st = reinterpret_cast<float*>(smem) + wave_uniform((int)(threadIdx.x >> 6)) * 32 * PITCH;
+    st = reinterpret_cast<float*>(smem) + wave_uniform((int)(threadIdx.x >> 6)) * FLOATS;
     lane = threadIdx.x & 63;
   }
   // Columns 32 jp .. 32 jp + 31 of the wave's sums.
@@ -377,10 +378,11 @@ struct Stage {
   }
 };
 // First row and column of a wave's sums within its tile.
+__device__ inline int this_wave() { return (int)wave_uniform(threadIdx.x >> 6); }
 template <int F>
-__device__ inline int wave_row() { return 16 * F * (int)wave_uniform(threadIdx.x >> 7); }
+__device__ inline int wave_row(int wave = this_wave()) { return 16 * F * (wave >> 1); }
 template <int F>
-__device__ inline int wave_col() { return 16 * F * (int)wave_uniform((threadIdx.x >> 6) & 1); }
+__device__ inline int wave_col(int wave = this_wave()) { return 16 * F * (wave & 1); }
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 template <bool PAIRS>
@@ -409,10 +411,11 @@ __device__ inline void get_halves8(const _Float16* hi, int64_t lo, float (&x)[8]
 // A symmetric matrix's tile and its mirror image; columns from S to ld are zeros.  value(r, c, x)
 // turns the sums of eight rows from r of column c into what is stored.
 template <bool PAIRS, int F, typename V>
-__device__ inline void put_symmetric(const MuonGroup& q, char* to, void* smem, int ti, int tj, const f32x4 (&acc)[F][F], V value) {
+__device__ inline void put_symmetric(const MuonGroup& q, char* to, void* smem, int ti, int tj, const f32x4 (&acc)[F][F], V value,
+                                     int wave = this_wave()) {
   _Float16* const o = reinterpret_cast<_Float16*>(to);
   Stage<F> st(smem);
-  const int r0 = ti * 32 * F + wave_row<F>(), c0 = tj * 32 * F + wave_col<F>();
+  const int r0 = ti * 32 * F + wave_row<F>(wave), c0 = tj * 32 * F + wave_col<F>(wave);
 #pragma unroll
   for (int jp = 0; jp < F / 2; ++jp) {
     st.put(acc, jp);
@@ -439,27 +442,66 @@ __device__ inline void put_symmetric(const MuonGroup& q, char* to, void* smem, i
   }
 }
 
-// A = Y^T Y
+struct AsA {  // a product of X's halves to A's
+  __device__ inline void operator()(int, int, float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= 1.f / kScale;
+  }
+};
+
+// A = Y^T Y, or the sums of a part of Y's rows
 template <bool BIG, bool PAIRS>
 __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_gram_kernel(MuonArgs a, int from) {
   typedef CoreOf<BIG, true, PAIRS> C;
+  constexpr int F = C::type::F;
   __shared__ typename C::type::Smem sm;
-  const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_sym; });
+  const MuonGroup& q = group_of(a, blockIdx.x, [](const MuonGroup& x) { return x.tile_gram; });
+  const uint32_t each = q.n_sym * q.splits;
   uint32_t at;
-  if (!tile_of(blockIdx.x - q.tile_sym, q.n_sym * q.count, at)) return;
-  const uint32_t i = wave_uniform(at / q.n_sym);
+  if (!tile_of(blockIdx.x - q.tile_gram, each * q.count, at)) return;
+  const uint32_t i = wave_uniform(at / each), part = wave_uniform((at - i * each) / q.n_sym);
   char* const base = q.base + i * q.stride;
   int ti, tj;
-  upper_tile(at - i * q.n_sym, ti, tj);
-  const char* const y = base + q.y[from];
+  upper_tile(at - i * each - part * q.n_sym, ti, tj);
+  const int k0 = (int)part * q.split_rows, n = q.L - k0 < q.split_rows ? q.L - k0 : q.split_rows;
+  const char* const y = base + q.y[from] + (int64_t)k0 * q.ld * 2;
   typename C::type core;
-  core.product(sm, cols_desc(y, q.ld, ti * C::tile, q.L), cols_desc(y + q.lo_y, q.ld, ti * C::tile, q.L),
-           cols_desc(y, q.ld, tj * C::tile, q.L), cols_desc(y + q.lo_y, q.ld, tj * C::tile, q.L), q.ld, q.L,
+  core.product(sm, cols_desc(y, q.ld, ti * C::tile, n), cols_desc(y + q.lo_y, q.ld, ti * C::tile, n),
+               cols_desc(y, q.ld, tj * C::tile, n), cols_desc(y + q.lo_y, q.ld, tj * C::tile, n), q.ld, n,
                q.S - ti * C::tile, q.S - tj * C::tile);
-  put_symmetric<PAIRS>(q, base + q.gram, &sm, ti, tj, core.acc, [](int, int, float(&x)[8]) {
+  if (q.splits > 1) {
+    f32x4* const out = reinterpret_cast<f32x4*>(q.part) + (int64_t)at * (F * F * 256) + threadIdx.x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= 1.f / kScale;
-  });
+    for (int k = 0; k < F * F; ++k) out[k * 256] = core.acc[k / F][k % F];
+  } else {
+    put_symmetric<PAIRS>(q, base + q.gram, &sm, ti, tj, core.acc, AsA());
+  }
+}
+
+// A from the parts' sums, added up in their order: a wave for each of a tile's four.
+template <bool BIG, bool PAIRS>
+__global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
+  constexpr int F = BIG ? 8 : 4, AHEAD = BIG ? 1 : 2;
+  __shared__ float sm[Stage<F>::FLOATS];
+  const uint32_t block = blockIdx.x / 4, wave = blockIdx.x % 4;
+  const MuonGroup& q = group_of(a, block, [](const MuonGroup& x) { return x.tile_sym; });
+  const uint32_t at = block - q.tile_sym;
+  if (q.splits < 2 || at >= q.n_sym * q.count) return;
+  const uint32_t i = at / q.n_sym, t = at - i * q.n_sym;
+  int ti, tj;
+  upper_tile(t, ti, tj);
+  const f32x4* const from = reinterpret_cast<const f32x4*>(q.part) + ((int64_t)i * q.splits * q.n_sym + t) * (F * F * 256) +
+                            wave * 64 + threadIdx.x;
+  f32x4 acc[F][F];
+#pragma unroll
+  for (int k = 0; k < F * F; ++k) acc[k / F][k % F] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll AHEAD
+  for (uint32_t part = 0; part < q.splits; ++part) {
+    const f32x4* const p = from + (int64_t)part * q.n_sym * (F * F * 256);
+#pragma unroll
+    for (int k = 0; k < F * F; ++k) acc[k / F][k % F] += p[k * 256];
+  }
+  put_symmetric<PAIRS>(q, q.base + i * q.stride + q.gram, sm, ti, tj, acc, AsA(), (int)wave);
 }
 
 // B = a I + b A + c A A
@@ -660,6 +702,11 @@ hipError_t launch_muon_split(int g_dtype, bool pairs, const MuonArgs& a, uint32_
 hipError_t launch_muon_gram(bool big, bool pairs, int from, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
   return with_both(big, pairs, [&](auto b, auto pr) {
     hipLaunchKernelGGL((muon_gram_kernel<decltype(b)::value, decltype(pr)::value>), dim3(blocks), dim3(256), 0, s, a, from);
+  });
+}
+hipError_t launch_muon_join(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
+  return with_both(big, pairs, [&](auto b, auto pr) {
+    hipLaunchKernelGGL((muon_join_kernel<decltype(b)::value, decltype(pr)::value>), dim3(4 * blocks), dim3(64), 0, s, a);
   });
 }
 hipError_t launch_muon_poly(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s) {

@@ -152,6 +152,24 @@ def test_larger_matrices():
         assert s.max() < 1.21 and np.median(s) > 0.68
 
 
+@pytest.mark.parametrize("shape", [(5000, 65), (65, 1024), (130, 4100), (9001, 70), (1024, 5000), (2100, 1100)])
+@pytest.mark.parametrize("pairs", [False, True], ids=["f16", "pairs"])
+def test_long_matrices(shape, pairs):
+    """The products over the longer side, divided among workgroups; the same bits again, and a second
+    matrix of other values beside it."""
+    M = Model(13, [shape, shape], zero=True)
+    P.attr_muon_step(M.plan(), -1.0, pairs=pairs)
+    for j in range(2):
+        w, g, m = M.was[j]
+        _, nm, x = O.muon(w, g, m, -1.0)
+        off, tol = np.linalg.norm(host(M.p[j]) - x), tolerance(0.95 * nm + 0.05 * g, pairs)
+        say(f"case: muon {shape} {j} off by {off / np.linalg.norm(x)} of {tol / np.linalg.norm(x)}")
+        assert off <= tol
+    N = Model(13, [shape, shape], zero=True)
+    P.attr_muon_step(N.plan(), -1.0, pairs=pairs)
+    assert all(torch.equal(a, b) for a, b in zip(M.p, N.p))
+
+
 def test_many_matrices_of_many_shapes():
     """More shapes than a launch takes groups, more matrices than a table's launch; each as alone."""
     r = np.random.default_rng(3)

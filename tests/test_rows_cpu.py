@@ -195,7 +195,8 @@ def test_muon_workspace_is_bounded():
         sizes.append(L.attr_muon_step_workspace_size(arr, n, 0))
     one = 2 * 2048 * 8192 + 2 * 2048 * 2048   # Y twice, A and B
     one *= 2   # bytes
-    assert one <= sizes[0] < one + (1 << 16) and sizes[1] <= sizes[2] <= (1 << 30) + (1 << 20)
+    parts = 256 * 256 * 256 * 4   # few tiles: sums of parts, at most one tile for each CU
+    assert one <= sizes[0] < one + parts + (1 << 16) and sizes[1] <= sizes[2] <= (1 << 30) + (1 << 20)
 
 
 def test_binding_refusals():
