@@ -1190,7 +1190,10 @@ MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
       R.sym += attr::muon_tiles(q.n_sym * q.count);
       R.full += attr::muon_tiles(q.n_full * q.count);
       q.splits = 1;
-      if (q.n_sym == 0) continue;
+      if (R.kind < kTiles) {
+        R.split |= q.n_flat > attr::kThinParts;
+        continue;
+      }
       const int32_t want = std::min({(int32_t)(slots / tiles), q.L / attr::kMuonSplitRows, attr::kMuonSplits});
       if (want > 1) {
         q.split_rows = ((q.L + want - 1) / want + 63) / 64 * 64;
@@ -1342,6 +1345,7 @@ attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dt
       a.nesterov = nesterov;
       if (R.kind < kTiles) {
         hipError_t e = attr::launch_muon_thin_gram((int)g_dtype, R.kind, a, R.flat, s);
+        if (e == hipSuccess && R.split) e = attr::launch_muon_thin_sum(R.kind, a, (uint32_t)R.order.size(), s);
         if (e == hipSuccess) e = attr::launch_muon_thin_poly(R.kind, steps, a, (uint32_t)R.order.size(), s);
         if (e == hipSuccess) e = attr::launch_muon_thin_apply((int)p_dtype, (int)g_dtype, master, R.kind, a, R.flat, s);
         return e;

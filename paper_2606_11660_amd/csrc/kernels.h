@@ -451,7 +451,9 @@ static_assert(sizeof(MuonArgs) <= 4096, "kernel arguments");
 // kThinRows of the longer side.  A group's workgroups are its tile_flat and n_flat; gram is its parts'
 // place, poly that of what u is multiplied by.
 constexpr int kThinMost = 64, kThinRows = 256;
+constexpr uint32_t kThinParts = 32;  // more parts of a matrix are added up by a launch of their own
 hipError_t launch_muon_thin_gram(int g_dtype, int t, const MuonArgs& a, uint32_t blocks, hipStream_t s);
+hipError_t launch_muon_thin_sum(int t, const MuonArgs& a, uint32_t matrices, hipStream_t s);
 hipError_t launch_muon_thin_poly(int t, int steps, const MuonArgs& a, uint32_t matrices, hipStream_t s);
 hipError_t launch_muon_thin_apply(int p_dtype, int g_dtype, bool master, int t, const MuonArgs& a, uint32_t blocks, hipStream_t s);
 constexpr int kMuonTile = 128;

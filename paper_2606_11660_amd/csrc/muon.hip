@@ -478,30 +478,42 @@ __global__ __launch_bounds__(256, BIG ? 1 : 2) void muon_gram_kernel(MuonArgs a,
   }
 }
 
-// A from the parts' sums, added up in their order: a wave for each of a tile's four.
+// A from the parts' sums: a workgroup for each wave's quarter of a tile, whose four waves add up every
+// fourth part, and then those sums in turn (one wave: 60 us for 32 parts of one tile).
 template <bool BIG, bool PAIRS>
-__global__ __launch_bounds__(64) void muon_join_kernel(MuonArgs a) {
-  constexpr int F = BIG ? 8 : 4, AHEAD = BIG ? 1 : 2;
+__global__ __launch_bounds__(256) void muon_join_kernel(MuonArgs a) {
+  constexpr int F = BIG ? 8 : 4;
+  __shared__ f32x4 sums[F * F][64];
   __shared__ float sm[Stage<F>::FLOATS];
-  const uint32_t block = blockIdx.x / 4, wave = blockIdx.x % 4;
+  const uint32_t block = blockIdx.x / 4, quarter = blockIdx.x % 4;
   const MuonGroup& q = group_of(a, block, [](const MuonGroup& x) { return x.tile_sym; });
   const uint32_t at = block - q.tile_sym;
   if (q.splits < 2 || at >= q.n_sym * q.count) return;
   const uint32_t i = at / q.n_sym, t = at - i * q.n_sym;
   int ti, tj;
   upper_tile(t, ti, tj);
+  const int wave = this_wave(), lane = threadIdx.x & 63;
   const f32x4* const from = reinterpret_cast<const f32x4*>(q.part) + ((int64_t)i * q.splits * q.n_sym + t) * (F * F * 256) +
-                            wave * 64 + threadIdx.x;
+                            quarter * 64 + lane;
   f32x4 acc[F][F];
 #pragma unroll
   for (int k = 0; k < F * F; ++k) acc[k / F][k % F] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll AHEAD
-  for (uint32_t part = 0; part < q.splits; ++part) {
+  for (uint32_t part = (uint32_t)wave; part < q.splits; part += 4) {
     const f32x4* const p = from + (int64_t)part * q.n_sym * (F * F * 256);
 #pragma unroll
     for (int k = 0; k < F * F; ++k) acc[k / F][k % F] += p[k * 256];
   }
-  put_symmetric<PAIRS>(q, q.base + i * q.stride + q.gram, sm, ti, tj, acc, AsA(), (int)wave);
+  for (int w = 3; w >= 0; --w) {
+    if (wave == w) {
+#pragma unroll
+      for (int k = 0; k < F * F; ++k) {
+        if (w < 3) acc[k / F][k % F] += sums[k][lane];
+        if (w > 0) sums[k][lane] = acc[k / F][k % F];
+      }
+    }
+    __syncthreads();
+  }
+  if (wave == 0) put_symmetric<PAIRS>(q, q.base + i * q.stride + q.gram, sm, ti, tj, acc, AsA(), (int)quarter);
 }
 
 // B = a I + b A + c A A
@@ -706,7 +718,7 @@ hipError_t launch_muon_gram(bool big, bool pairs, int from, const MuonArgs& a, u
 }
 hipError_t launch_muon_join(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s) {
   return with_both(big, pairs, [&](auto b, auto pr) {
-    hipLaunchKernelGGL((muon_join_kernel<decltype(b)::value, decltype(pr)::value>), dim3(4 * blocks), dim3(64), 0, s, a);
+    hipLaunchKernelGGL((muon_join_kernel<decltype(b)::value, decltype(pr)::value>), dim3(4 * blocks), dim3(256), 0, s, a);
   });
 }
 hipError_t launch_muon_poly(bool big, bool pairs, const MuonArgs& a, uint32_t blocks, hipStream_t s) {

@@ -119,6 +119,27 @@ __global__ __launch_bounds__(256) void muon_thin_gram_kernel(MuonArgs a) {
     }
 }
 
+// The sum of a long matrix's parts of G, in the first one's place: a workgroup for each tile, a quarter of
+// it every fourth part.  (One CU reads some 80 GB/s: 512 parts of 64 x 64 took the next kernel 136 us.)
+template <int T>
+__global__ __launch_bounds__(1024) void muon_thin_sum_kernel(MuonArgs a) {
+  constexpr int TILES = T * (T + 1) / 2;
+  __shared__ double sm[3][256];
+  const uint32_t mat = blockIdx.x / TILES, tile = blockIdx.x % TILES;
+  int k = 0;
+  while (k + 1 < a.n_groups && a.g[k + 1].entry <= mat) ++k;
+  const MuonGroup& q = a.g[k];
+  if (q.n_flat <= kThinParts) return;
+  double* const first = reinterpret_cast<double*>(q.base + (int64_t)(mat - q.entry) * q.stride + q.gram) + tile * 256 + threadIdx.x % 256;
+  const uint32_t w = threadIdx.x / 256;
+  double x = 0;
+#pragma unroll 8
+  for (uint32_t p = w; p < q.n_flat; p += 4) x += first[(int64_t)p * TILES * 256];
+  if (w > 0) sm[w - 1][threadIdx.x % 256] = x;
+  __syncthreads();
+  if (w == 0) *first = x + sm[0][threadIdx.x] + sm[1][threadIdx.x] + sm[2][threadIdx.x];
+}
+
 // Q / |u| of one matrix from its parts of G: a wave for each 16 x 16 tile.
 template <int T>
 __global__ __launch_bounds__(64 * T * T) void muon_thin_poly_kernel(MuonArgs a, int steps) {
@@ -131,13 +152,14 @@ __global__ __launch_bounds__(64 * T * T) void muon_thin_poly_kernel(MuonArgs a, 
   char* const base = q.base + (int64_t)(blockIdx.x - q.entry) * q.stride;
   const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6));
   const int ti = wave / T, tj = wave - ti * T;
+  const uint32_t n_parts = q.n_flat > kThinParts ? 1 : q.n_flat;
   const int c = 16 * tj + (lane & 15), r0 = 16 * ti + (lane >> 4);  // this lane's column, first of its rows
   const double* const parts = reinterpret_cast<const double*>(base + q.gram);
   if (ti <= tj) {
     const int tile = tj * (tj + 1) / 2 + ti;
     double x[4] = {0, 0, 0, 0};
 #pragma unroll 8
-    for (uint32_t p = 0; p < q.n_flat; ++p)
+    for (uint32_t p = 0; p < n_parts; ++p)
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] += parts[(int64_t)p * TILES * 256 + tile * 256 + e * 64 + lane];
 #pragma unroll
@@ -231,8 +253,7 @@ __global__ __launch_bounds__(256) void muon_thin_apply_kernel(MuonArgs a) {
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int t = 0; t < T; ++t)
-      {
+      for (int t = 0; t < T; ++t) {
         const int r = l + 64 * i + low, s = 16 * t + 4 * high, n = r < l1 ? q.S - s : 0;
         if (turned) {
 #pragma unroll
@@ -307,6 +328,12 @@ hipError_t launch_muon_thin_gram(int g_dtype, int t, const MuonArgs& a, uint32_t
     return with_sixteens(t, [&](auto n) {
       hipLaunchKernelGGL((muon_thin_gram_kernel<decltype(g), decltype(n)::value>), dim3(blocks), dim3(256), 0, s, a);
     });
+  });
+}
+hipError_t launch_muon_thin_sum(int t, const MuonArgs& a, uint32_t matrices, hipStream_t s) {
+  return with_sixteens(t, [&](auto n) {
+    constexpr int T = decltype(n)::value;
+    hipLaunchKernelGGL((muon_thin_sum_kernel<T>), dim3(matrices * (T * (T + 1) / 2)), dim3(1024), 0, s, a);
   });
 }
 hipError_t launch_muon_thin_poly(int t, int steps, const MuonArgs& a, uint32_t matrices, hipStream_t s) {

@@ -152,7 +152,8 @@ def test_larger_matrices():
         assert s.max() < 1.21 and np.median(s) > 0.68
 
 
-@pytest.mark.parametrize("shape", [(5000, 65), (65, 1024), (130, 4100), (9001, 70), (1024, 5000), (2100, 1100)])
+@pytest.mark.parametrize("shape", [(5000, 65), (65, 1024), (130, 4100), (9001, 70), (1024, 5000), (2100, 1100), (8193, 64),
+                                   (40, 9000), (20000, 7)])
 @pytest.mark.parametrize("pairs", [False, True], ids=["f16", "pairs"])
 def test_long_matrices(shape, pairs):
     """The products over the longer side, divided among workgroups; the same bits again, and a second
