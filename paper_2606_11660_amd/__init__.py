@@ -997,11 +997,13 @@ def _rows_call(op: int, rows: Optional[ExampleRows], tensors: tuple, numbers: tu
 def _here(t: torch.Tensor, stream) -> int:
     """The call's stream as a handle (0 for a CPU tensor, whose checks raise); the call's tensors live
     on the current device, whose stream it is."""
-    if not t.is_cuda:
+    on = t.get_device()
+    if on < 0:
         return 0
-    if t.device.index != torch.cuda.current_device():
+    here = torch.cuda.current_device()
+    if on != here:
         raise ValueError("the call's tensors must live on the current GPU device")
-    return _raw_stream(stream)
+    return torch._C._cuda_getCurrentRawStream(here) if stream is None else _stream(stream)
 
 
 def _tokens(token: torch.Tensor, n_rows: int) -> None:

@@ -1150,10 +1150,22 @@ attr::MuonGroup thin_group(int64_t rows, int64_t cols) {
 }
 
 constexpr int kTiles = 8, kBigTiles = 9;
-int muon_kind(const attr_muon_matrix& t) {
+// Tiles of 256 x 256 for shorter sides from 1024 on, where the call has enough of them: 128 and more
+// for the products A, which have the fewest (bf16 weights, 128 x 128 in brackets: 4 of 2048 x 8192, 144
+// tiles, 2665 us (2982); 24 of 1024 x 4096, 240 tiles, 2251 (2810); 4 of them, 40 tiles, 844 (540)).
+constexpr int64_t kMuonBigSide = 1024, kMuonBigTiles = 128;
+bool muon_big(const attr_muon_matrix* mats, int32_t n) {
+  int64_t tiles = 0;
+  for (int32_t j = 0; j < n; ++j) {
+    const int64_t s = std::min(mats[j].rows, mats[j].cols), t = (s + 255) / 256;
+    if (s >= kMuonBigSide) tiles += t * (t + 1) / 2;
+  }
+  return tiles >= kMuonBigTiles;
+}
+int muon_kind(const attr_muon_matrix& t, bool big) {
   const int64_t s = std::min(t.rows, t.cols);
   if (s <= attr::kThinMost) return (int)((s + 15) / 16);
-  return s >= 1024 ? kBigTiles : kTiles;
+  return big && s >= kMuonBigSide ? kBigTiles : kTiles;
 }
 
 // A round ends where its launches fill the GPU some times over: its buffers then stay
@@ -1164,10 +1176,11 @@ constexpr size_t kMuonRoundBytes = (size_t)1 << 30;
 
 MuonPlan muon_plan(const attr_muon_matrix* mats, int32_t n, bool pairs) {
   MuonPlan P;
+  const bool big = muon_big(mats, n);
   // by kind, and by shape
   std::map<std::tuple<int, int64_t, int64_t>, std::vector<int32_t>> shapes;
   for (int32_t j = 0; j < n; ++j) {
-    if (mats[j].rows > 0 && mats[j].cols > 0) shapes[{muon_kind(mats[j]), mats[j].rows, mats[j].cols}].push_back(j);
+    if (mats[j].rows > 0 && mats[j].cols > 0) shapes[{muon_kind(mats[j], big), mats[j].rows, mats[j].cols}].push_back(j);
   }
   MuonRound R;
   const auto clear = [&] {
@@ -1469,7 +1482,7 @@ EmbedLayout embed_layout(const attr_rows* r, int64_t V, int64_t d) {
   L.count = 4 * each;
   const size_t blocks = (n + attr::kSortKeys - 1) / attr::kSortKeys;
   L.part = L.count + (n > attr::kSortOne ? align_up((blocks << attr::sort_bits(V)) * 8) : 0);
-  const size_t parts = (n + attr::kEmbedPart - 1) / attr::kEmbedPart;
+  const size_t each_part = attr::embed_part(n, d), parts = (n + each_part - 1) / each_part;
   L.total = L.part + align_up(parts * 2 * (size_t)d * 4);
   return L;
 }
@@ -1572,6 +1585,7 @@ attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, con
     a.row = sort.row[sort.passes & 1];
     a.part = reinterpret_cast<float*>(base + L.part);
     a.n = r.n_slots;
+    a.each = attr::embed_part(a.n, d);
     e = attr::launch_embed_grad((int)dout_dtype, (int)dtable_dtype, a, s);
     return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_embed_backward launch");
   } catch (...) {

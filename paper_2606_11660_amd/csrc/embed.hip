@@ -2,8 +2,11 @@
 //
 //     out[row] = scale table[token]          dtable[v] (+)= scale sum of dout[row], token = v
 //
-// Both are HBM-bound.  The gradient sorts the batch's (token, row) pairs by token, stably, and
-// adds up each token's rows in that order in fp32: no atomic additions, the same bits every time.
+// Both are HBM-bound: a row is read and written once (16384 rows of 1024, fp16: 37.7 us, 34 at the rate of
+// a large copy).  The gradient sorts the batch's (token, row) pairs by token, stably, and
+// adds up each token's rows in that order in fp32: no atomic additions of values, the same bits every
+// time.  The sort is a chain of short launches, which write the gradient's zeros meanwhile; the sums read
+// dout once, a wave a run of neighbours.
 #include "rows.h"
 
 namespace attr {
@@ -374,13 +377,13 @@ __device__ inline void embed_sum(const EmbedGradArgs& a, uint32_t cuts, uint64_t
   const int lane = threadIdx.x & 63;
   const uint32_t part = (uint32_t)(unit / cuts), cut = (uint32_t)(unit % cuts);
   const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
-  const uint32_t from = part * kEmbedPart, to = a.n - from < kEmbedPart ? a.n : from + kEmbedPart;
+  const uint32_t from = part * a.each, to = a.n - from < a.each ? a.n : from + a.each;
   const uint32_t V = (uint32_t)a.V;
   float sum[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) sum[e] = 0.f;
   // the part's pairs, and the keys on both sides of it, in the wave's lanes
-  const uint32_t j = from + (lane & (kEmbedPart - 1)), jj = j < to ? j : to - 1;
+  const uint32_t j = from + (lane & (a.each - 1)), jj = j < to ? j : to - 1;
   const uint32_t keys = a.key[jj], rows = a.row[jj];
   const uint32_t sides = a.key[lane ? (to < a.n ? to : a.n - 1) : (from > 0 ? from - 1 : 0)];
   const auto lane_of = [](uint32_t x, uint32_t k) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)k); };
@@ -426,62 +429,63 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, uint32_
 }
 
 // Joins the sums of a token that begins in a part and goes on behind it: each of the four
-// waves an equal share of the following parts, in fp64.
+// waves an equal share of the following parts, in fp64.  Bound by latency: most workgroups only read the
+// keys at a part's end (65536 slots of 1024: 9 us; of one token, whose parts one workgroup a cut adds up: 45).
 template <typename T, int N>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, uint32_t parts, uint32_t cuts) {
   __shared__ double sm[3][N][64];
   const int lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
   for (uint64_t block = blockIdx.x; block < (uint64_t)(parts - 1) * cuts; block += gridDim.x) {
-  const uint32_t part = (uint32_t)(block / cuts), cut = (uint32_t)(block % cuts);
-  const uint32_t to = (part + 1) * kEmbedPart;  // not the last part: it has nothing behind it
-  const uint32_t cur = wave_uniform(a.key[to - 1]);
-  if (cur == (uint32_t)a.V || wave_uniform(a.key[to]) != cur) continue;
-  const uint32_t from = part * kEmbedPart;
-  if (wave_uniform(a.key[from]) == cur && from > 0 && wave_uniform(a.key[from - 1]) == cur) continue;
-  const uint32_t last = (end_of(a.key, a.n, cur) - 1) / kEmbedPart;  // the part that holds its last row
-  const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
-  const uint32_t each = (last - part + 3) / 4;
-  const uint32_t k0 = part + 1 + wave * each, k1 = k0 + each < last + 1 ? k0 + each : last + 1;
-  double sum[N];
+    const uint32_t part = (uint32_t)(block / cuts), cut = (uint32_t)(block % cuts);
+    const uint32_t to = (part + 1) * a.each;  // not the last part: it has nothing behind it
+    const uint32_t cur = wave_uniform(a.key[to - 1]);
+    if (cur == (uint32_t)a.V || wave_uniform(a.key[to]) != cur) continue;
+    const uint32_t from = part * a.each;
+    if (wave_uniform(a.key[from]) == cur && from > 0 && wave_uniform(a.key[from - 1]) == cur) continue;
+    const uint32_t last = (end_of(a.key, a.n, cur) - 1) / a.each;  // the part that holds its last row
+    const Cols<N> c((int)(cut * 64 + lane) * N, a.d);
+    const uint32_t each = (last - part + 3) / 4;
+    const uint32_t k0 = part + 1 + wave * each, k1 = k0 + each < last + 1 ? k0 + each : last + 1;
+    double sum[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) sum[e] = 0;
-  if (wave == 0) {
-    float x[N];
-    load_n<float, N>(a.part + ((int64_t)part * 2 + 1) * a.d, c, x);
+    for (int e = 0; e < N; ++e) sum[e] = 0;
+    if (wave == 0) {
+      float x[N];
+      load_n<float, N>(a.part + ((int64_t)part * 2 + 1) * a.d, c, x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum[e] = x[e];
-  }
+      for (int e = 0; e < N; ++e) sum[e] = x[e];
+    }
 #pragma unroll 4
-  for (uint32_t k = k0; k < k1; ++k) {
-    float x[N];
-    load_n<float, N>(a.part + (int64_t)k * 2 * a.d, c, x);
+    for (uint32_t k = k0; k < k1; ++k) {
+      float x[N];
+      load_n<float, N>(a.part + (int64_t)k * 2 * a.d, c, x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum[e] += x[e];
-  }
-  __syncthreads();
-  if (wave > 0) {
+      for (int e = 0; e < N; ++e) sum[e] += x[e];
+    }
+    __syncthreads();
+    if (wave > 0) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) sm[wave - 1][e][lane] = sum[e];
-  }
-  __syncthreads();
-  if (wave > 0) continue;
-  float out[N];
+      for (int e = 0; e < N; ++e) sm[wave - 1][e][lane] = sum[e];
+    }
+    __syncthreads();
+    if (wave > 0) continue;
+    float out[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    for (int w = 0; w < 3; ++w) sum[e] += sm[w][e][lane];
-    out[e] = (float)sum[e];
-  }
-  put_sum<T, N>(a, cur, c, out);
+    for (int e = 0; e < N; ++e) {
+      for (int w = 0; w < 3; ++w) sum[e] += sm[w][e][lane];
+      out[e] = (float)sum[e];
+    }
+    put_sum<T, N>(a, cur, c, out);
   }
 }
 
-// A batch of up to kEmbedSmall slots, without a sort: a wave looks through its tokens for those of
+// A batch of up to 64 K slots, without a sort: a wave looks through its tokens for those of
 // `each` rows of the table, and adds up their rows in the order of their slots.
-template <typename G, typename T, int N>
+template <typename G, typename T, int N, int K>
 __global__ __launch_bounds__(256) void embed_small_kernel(RowsArgs r, const int64_t* token, EmbedGradArgs a, uint32_t each,
                                                           uint32_t cuts, uint64_t units) {
-  constexpr int K = kEmbedSmall / 64, U = 8;
-  __shared__ uint32_t lists[4][kEmbedSmall];
+  constexpr int U = 8;
+  __shared__ uint32_t lists[4][64 * K];
   uint32_t* const list = lists[threadIdx.x >> 6];
   const uint32_t lane = threadIdx.x & 63;
   const uint64_t first = (uint64_t)blockIdx.x * 4 + wave_uniform(threadIdx.x >> 6);
@@ -538,15 +542,18 @@ hipError_t embed_rows(const RowsArgs& r, const EmbedArgs& a, hipStream_t s) {
 template <typename G, typename T, int N>
 hipError_t embed_small(const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a, hipStream_t s) {
   const uint32_t cuts = (uint32_t)((a.d + 64 * N - 1) / (64 * N));
-  const uint32_t each = a.V <= 8192 ? 1 : 8;  // few rows: a wave for each
+  // a small table: a wave for each row; a large one: fewer searches of the tokens (256 slots of 1024,
+  // 50257 rows: 36.3 us, a wave for each row 45.0; 2048 rows: 5.2 and 5.5)
+  const uint32_t each = a.V <= 8192 ? 1 : 8;
   const uint64_t units = ((uint64_t)a.V + each - 1) / each * cuts;
-  hipLaunchKernelGGL((embed_small_kernel<G, T, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, r, token, a, each, cuts,
-                     units);
+  const dim3 grid(grid_of((units + 3) / 4));
+  if (r.n_slots <= 256) hipLaunchKernelGGL((embed_small_kernel<G, T, N, 4>), grid, dim3(256), 0, s, r, token, a, each, cuts, units);
+  else hipLaunchKernelGGL((embed_small_kernel<G, T, N, kEmbedSmall / 64>), grid, dim3(256), 0, s, r, token, a, each, cuts, units);
   return hipGetLastError();
 }
 template <typename G, typename T, int N>
 hipError_t embed_sums(const EmbedGradArgs& a, hipStream_t s) {
-  const uint32_t parts = (a.n + kEmbedPart - 1) / kEmbedPart, cuts = (uint32_t)((a.d + 64 * N - 1) / (64 * N));
+  const uint32_t parts = (a.n + a.each - 1) / a.each, cuts = embed_cuts(a.d);
   const uint64_t units = (uint64_t)parts * cuts;
   hipLaunchKernelGGL((embed_sum_kernel<G, T, N>), dim3(grid_of((units + 3) / 4)), dim3(256), 0, s, a, cuts, units);
   const hipError_t e = hipGetLastError();
@@ -599,8 +606,8 @@ hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V,
 hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArgs& a, hipStream_t s) {
   return with_type(dout_dtype, [&](auto g) {
     return with_type(table_dtype, [&](auto t) {
-      if (a.d > 1024) return embed_sums<decltype(g), decltype(t), 8>(a, s);
-      if (a.d > 64) return embed_sums<decltype(g), decltype(t), 4>(a, s);
+      if (embed_lane(a.d) == 8) return embed_sums<decltype(g), decltype(t), 8>(a, s);
+      if (embed_lane(a.d) == 4) return embed_sums<decltype(g), decltype(t), 4>(a, s);
       return embed_sums<decltype(g), decltype(t), 1>(a, s);
     });
   });

@@ -349,9 +349,12 @@ struct EmbedZero {
   uint32_t blocks, shares;  // workgroups of a launch, and of all; set by the launch
 };
 hipError_t launch_embed_sort(const RowsArgs& r, const int64_t* token, int64_t V, const EmbedSort& e, EmbedZero z, hipStream_t s);
-// A wave adds up the rows of kEmbedPart neighbours in that order; a token whose rows
-// reach past a part leaves sums to be joined.
-constexpr uint32_t kEmbedPart = 32;
+// A wave adds up 64 N columns, N = embed_lane(d), of the rows of a part of neighbours in that order: of 32,
+// or of 64 where those leave 16 waves a CU (65536 slots of 1024, 4096 waves: 89.0 us with parts of 32, 82.0 of
+// 64; 32768 of 2048, 2048 waves: 99 and 115).  A token whose rows reach past a part leaves sums to be joined.
+inline int embed_lane(int64_t d) { return d > 1024 ? 8 : d > 64 ? 4 : 1; }
+inline uint32_t embed_cuts(int64_t d) { return (uint32_t)((d + 64 * embed_lane(d) - 1) / (64 * embed_lane(d))); }
+inline uint32_t embed_part(uint64_t n, int64_t d) { return n / 64 * embed_cuts(d) >= 4096 ? 64 : 32; }
 struct EmbedGradArgs {
   const uint32_t* key;
   const uint32_t* row;
@@ -360,10 +363,12 @@ struct EmbedGradArgs {
   float* part;        // [parts][2][d]: of the token that began before, of the one that goes on
   int64_t V, ldd, ldt;
   uint32_t n;         // pairs, those without a token last
+  uint32_t each;      // pairs of a part
   int32_t d, accumulate;
   float scale;
 };
-constexpr uint32_t kEmbedSmall = 256;  // slots of a batch that needs no sort
+// Slots of a batch that needs no sort (400 slots, a table of 8192 x 1024: 11.9 us without, 24.2 with it).
+constexpr uint32_t kEmbedSmall = 512;
 hipError_t launch_embed_small(int dout_dtype, int table_dtype, const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a,
                               hipStream_t s);
 hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArgs& a, hipStream_t s);

@@ -6,7 +6,9 @@
 //
 // HBM-bound: a row is read once (forward: x; backward: x and dy) into the registers of its
 // threads, so that the variance is taken about the mean itself, and written once.  All sums are
-// in fp32 over a row's threads and over a chunk of rows; the chunks are joined in fp64.
+// in fp32 over a row's threads and over a share of rows; the shares are joined in fp64.  The
+// threads of a row are chosen by its width, for 8 to 32 values a thread: one wave up to 1024 columns
+// needs no barrier, more waves keep enough of the registers free for several rows on a CU.
 #include "rows.h"
 
 namespace attr {
@@ -173,9 +175,11 @@ __device__ inline float lane_of(float x, int k) {
 // A share of a unit's slots (every chunks-th of them, so that padding is spread evenly): dx of
 // its rows, and its part of the weights' gradients, each thread its own columns.  The next row
 // is loaded while one is worked on.  RELOAD: a row's registers do not fit beside those sums;
-// it is read twice.
+// it is read twice.  Of 512 threads two workgroups a CU hide each other's waits where both types have
+// 16 bits (8192 rows of 8192, bf16: 90.1 us, one workgroup 99.0); wider rows need the registers (fp32: 131 us,
+// with two workgroups 254).
 template <typename X, typename Y, int NT, int NV, int N, bool RELOAD>
-__global__ __launch_bounds__(block_of<NT>(), NT == 512 ? 4 : 1) void layer_norm_grad_kernel(RowsArgs r, NormGradArgs a) {
+__global__ __launch_bounds__(block_of<NT>(), NT == 512 ? (sizeof(X) + sizeof(Y) == 4 ? 4 : 2) : 1) void layer_norm_grad_kernel(RowsArgs r, NormGradArgs a) {
   constexpr int ROWS = block_of<NT>() / NT, KEPT = RELOAD ? 1 : NV;
   __shared__ float sm[2][2][16];
   __shared__ float join[ROWS == 1 ? 1 : (ROWS - 1) * NV * NT * N];
@@ -205,81 +209,81 @@ __global__ __launch_bounds__(block_of<NT>(), NT == 512 ? 4 : 1) void layer_norm_
       }
     };
     for (uint64_t i0 = (uint64_t)chunk * ROWS + which; i0 < a.unit; i0 += 64 * stride) {
-    const NormRows ahead(r, a, base, i0 + (threadIdx.x & 63) * stride);
-    RowSlot s = ahead.slot(0), next;
-    fetch(s);
-    for (int q = 0; q < 64 && i0 + q * stride < a.unit; ++q, s = next) {
-      next = q < 63 ? ahead.slot(q + 1) : RowSlot{0, false, false};
-      X* const dx = (X*)a.dx + s.row * a.lddx;
-      if (!s.inside) {
-        fetch(next);
-        if (s.written && a.dx) {
-          const float zero[N] = {};
+      const NormRows ahead(r, a, base, i0 + (threadIdx.x & 63) * stride);
+      RowSlot s = ahead.slot(0), next;
+      fetch(s);
+      for (int q = 0; q < 64 && i0 + q * stride < a.unit; ++q, s = next) {
+        next = q < 63 ? ahead.slot(q + 1) : RowSlot{0, false, false};
+        X* const dx = (X*)a.dx + s.row * a.lddx;
+        if (!s.inside) {
+          fetch(next);
+          if (s.written && a.dx) {
+            const float zero[N] = {};
 #pragma unroll
-          for (int v = 0; v < NV; ++v) store_n<X, N>(dx, Cols<N>((v * NT + t) * N, d), zero);
+            for (int v = 0; v < NV; ++v) store_n<X, N>(dx, Cols<N>((v * NT + t) * N, d), zero);
+          }
+          continue;
         }
-        continue;
-      }
-      const float mean = lane_of(ahead.mean, q), rstd = lane_of(ahead.rstd, q);
-      float u[KEPT][N], e1[KEPT][N];
-      float s1 = 0.f, s2 = 0.f;
-      const auto terms = [&](int v) {  // u and dy of vector v
-        const Cols<N> c((v * NT + t) * N, d);
-        const int k = RELOAD ? 0 : v;
-        if constexpr (RELOAD) {
-          cur.x[0].load((const X*)a.x + s.row * a.ldx + c.at);
-          cur.dy[0].load((const Y*)a.dy + s.row * a.lddy + c.at);
-        }
-        cur.x[k].get(u[k]);
-        cur.dy[k].get(e1[k]);
-#pragma unroll
-        for (int e = 0; e < N; ++e) u[k][e] = (u[k][e] - mean) * rstd;
-      };
-      if constexpr (!RELOAD) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) terms(v);
-        fetch(next);
-      }
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const Cols<N> c((v * NT + t) * N, d);
-        const int k = RELOAD ? 0 : v;
-        if constexpr (RELOAD) terms(v);
-        float w[N];
-        load_w<N>(a.weight, a.w_dtype, c, w, 1.f);
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          dw[v][e] += e1[k][e] * u[k][e];
-          db[v][e] += e1[k][e];
-          e1[k][e] *= w[e];
-          s1 += c.own(e) ? e1[k][e] : 0.f;
-          s2 += c.own(e) ? e1[k][e] * u[k][e] : 0.f;
-        }
-        if (RELOAD) __builtin_amdgcn_sched_barrier(0);
-      }
-      if (a.dx) {
-        row_sums<NT>(s1, s2, sm[turn]);
-        s1 /= (float)d;
-        s2 /= (float)d;
-        turn ^= 1;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
+        const float mean = lane_of(ahead.mean, q), rstd = lane_of(ahead.rstd, q);
+        float u[KEPT][N], e1[KEPT][N];
+        float s1 = 0.f, s2 = 0.f;
+        const auto terms = [&](int v) {  // u and dy of vector v
+          const Cols<N> c((v * NT + t) * N, d);
           const int k = RELOAD ? 0 : v;
           if constexpr (RELOAD) {
-            terms(v);
-            float w[N];
-            load_w<N>(a.weight, a.w_dtype, Cols<N>((v * NT + t) * N, d), w, 1.f);
-#pragma unroll
-            for (int e = 0; e < N; ++e) e1[0][e] *= w[e];
+            cur.x[0].load((const X*)a.x + s.row * a.ldx + c.at);
+            cur.dy[0].load((const Y*)a.dy + s.row * a.lddy + c.at);
           }
-          float o[N];
+          cur.x[k].get(u[k]);
+          cur.dy[k].get(e1[k]);
 #pragma unroll
-          for (int e = 0; e < N; ++e) o[e] = (e1[k][e] - s1 - u[k][e] * s2) * rstd;
-          store_n<X, N>(dx, Cols<N>((v * NT + t) * N, d), o);
+          for (int e = 0; e < N; ++e) u[k][e] = (u[k][e] - mean) * rstd;
+        };
+        if constexpr (!RELOAD) {
+#pragma unroll
+          for (int v = 0; v < NV; ++v) terms(v);
+          fetch(next);
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const Cols<N> c((v * NT + t) * N, d);
+          const int k = RELOAD ? 0 : v;
+          if constexpr (RELOAD) terms(v);
+          float w[N];
+          load_w<N>(a.weight, a.w_dtype, c, w, 1.f);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            dw[v][e] += e1[k][e] * u[k][e];
+            db[v][e] += e1[k][e];
+            e1[k][e] *= w[e];
+            s1 += c.own(e) ? e1[k][e] : 0.f;
+            s2 += c.own(e) ? e1[k][e] * u[k][e] : 0.f;
+          }
           if (RELOAD) __builtin_amdgcn_sched_barrier(0);
         }
+        if (a.dx) {
+          row_sums<NT>(s1, s2, sm[turn]);
+          s1 /= (float)d;
+          s2 /= (float)d;
+          turn ^= 1;
+#pragma unroll
+          for (int v = 0; v < NV; ++v) {
+            const int k = RELOAD ? 0 : v;
+            if constexpr (RELOAD) {
+              terms(v);
+              float w[N];
+              load_w<N>(a.weight, a.w_dtype, Cols<N>((v * NT + t) * N, d), w, 1.f);
+#pragma unroll
+              for (int e = 0; e < N; ++e) e1[0][e] *= w[e];
+            }
+            float o[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] = (e1[k][e] - s1 - u[k][e] * s2) * rstd;
+            store_n<X, N>(dx, Cols<N>((v * NT + t) * N, d), o);
+            if (RELOAD) __builtin_amdgcn_sched_barrier(0);
+          }
+        }
       }
-    }
     }
     // the sums of a workgroup's rows, those of its first threads first
 #pragma unroll
@@ -372,8 +376,9 @@ constexpr int elements() { return sizeof(X) == 4 || sizeof(Y) == 4 ? 4 : 8; }
 }  // namespace
 
 hipError_t launch_layer_norm(int x_dtype, int y_dtype, const RowsArgs& r, const NormArgs& a, hipStream_t s) {
-  // few rows: all of a row's threads at once, for the time of one row
-  const bool few = r.n_slots <= 1024;
+  // few rows: more threads for each, for the time of one row (1024 rows of 2048: 4.7 us, with a wave for
+  // each 6.0; 64 of 8192: 4.6 with 1024 threads, 5.2 with 256, but 1024 of them 13.6 and 10.0)
+  const bool few = r.n_slots <= (a.d <= 2048 ? 1024u : 256u);
   return with_type(x_dtype, [&](auto x) {
     return with_type(y_dtype, [&](auto y) {
       typedef decltype(x) X;
@@ -392,7 +397,9 @@ hipError_t launch_layer_norm(int x_dtype, int y_dtype, const RowsArgs& r, const 
   });
 }
 
-// Shares of a unit: workgroups enough to fill the GPU, each with several rows.
+// Shares of a unit: workgroups enough to fill the GPU, each with several rows, since its sums are written
+// and read again; past 16384 columns, where a row takes 40 us, with one at least (64 rows of 32768: 55 us,
+// with four 120).
 uint32_t norm_chunks(uint32_t unit, uint32_t units, int32_t d) {
   const uint32_t rows = d <= 1024 ? 16 : d <= 16384 ? 4 : 1, most = d <= 2048 ? 1024 : 512;
   const uint32_t by_rows = (unit + rows - 1) / rows, by_units = most / units;

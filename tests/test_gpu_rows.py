@@ -543,3 +543,27 @@ def test_autograd_sees_what_the_calls_write():
             P.attr_layer_norm_backward(torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda"), m, m, dx=d[3])
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             z.backward()
+
+
+def test_embed_backward_many_parts():
+    """Parts of 32 neighbours, and of 64 in the longest batches, that begin, end and hold whole tokens; on both sides of
+    the sort's sizes, and of the batches that need none."""
+    for n, V in ((256, 40), (257, 40), (512, 9000), (513, 40), (2049, 600), (32768, 700), (262143, 700), (262144, 700),
+                 (300001, 70000)):
+        say(f"case: embed backward parts n={n} V={V}")
+        B = Batch(1, n, False, n, ragged=False)
+        token = np.where(B.r.random(B.rows) < 0.3, 1, B.r.integers(0, V, B.rows))
+        back_case(V, 12, BF16, F32, B, token, False, 1.0)
+
+
+def test_tensors_of_another_device_than_the_current_one(monkeypatch):
+    """Refused: the current stream is not theirs."""
+    x = torch.zeros(4, 8, device="cuda")
+    tok, v = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    plan = P.MuonTensors([x], [x.clone()], [x.clone()])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: x.device.index + 1)
+    for call in (lambda: P.attr_embed(x, tok, x.clone()), lambda: P.attr_embed_backward(x, tok, x.clone()),
+                 lambda: P.attr_layer_norm(x, x.clone()), lambda: P.attr_layer_norm_backward(x, x, v, v, dx=x.clone()),
+                 lambda: P.attr_muon_step(plan, 0.1)):
+        with pytest.raises(ValueError, match="current GPU device"):
+            call()
