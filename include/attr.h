@@ -476,14 +476,17 @@ typedef struct {
  *     X = a X + (b A + c A A) X,   a = 3.4445, b = -4.7750, c = 2.0315
  *     x = x - lr' wd x - lr' X,    lr' = lr lr_scale
  * The polynomial takes singular values in (0, 1] towards 1 (after five steps those from
- * 0.01 on lie in [0.68, 1.21]), so X approaches the orthogonal factor of u.
+ * 0.002 on lie in [0.68, 1.21]), so X approaches the orthogonal factor of u.
  * Where a matrix is not square its longer side is multiplied last.  A matrix
  * whose u is zero has X = 0; one with a NaN or an infinity in u becomes NaN.
  * m is fp32 without contraction, the norm fp64; the iteration runs on the matrix
- * cores with fp32 sums and its operands (X, A, b A + c A A) rounded
- *   pairs = 0  to fp16, 11 bits: X is off by some 1e-3 of its norm, less than half
- *              a step of a 16-bit weight's update;
- *   pairs = 1  to pairs of fp16, 22 bits: three times the products, X off by some 1e-6.
+ * cores with fp32 sums and its operands (X, A, a I + b A + c A A) rounded
+ *   pairs = 0  to fp16, 11 bits: X is off by 1.2e-3 to 1.5e-3 of its norm (more where a
+ *              few directions carry most of u);
+ *   pairs = 1  to pairs of fp16, 22 bits: three times the products, X off by 1e-6 to 3e-6.
+ * Matrices whose shorter side is at most 64 run in fp64 on their products by themselves,
+ * whatever `pairs`: X off by some 1e-7.  The same call gives the same bits; the order of
+ * a larger matrix's sums depends on the sizes of all matrices of the call.
  * The numbers enter the launches as they are: a graph that captured this call
  * repeats the step with its rate.
  *   mats       (host) [n_mats], 0 <= n_mats; their buffers must not overlap (gradients
@@ -493,7 +496,8 @@ typedef struct {
  *   momentum   in [0, 1);  steps 1 to 16;  lr finite
  *   ws         attr_muon_step_workspace_size(mats, n_mats, pairs) bytes, 256-byte
  *              aligned: some 8 bytes (pairs: 16) for each element of the matrices that
- *              are worked on together, which are taken in turn where they are many */
+ *              are worked on together, which are taken in turn where they are many,
+ *              and up to 64 MB for sums of parts where they are few */
 size_t attr_muon_step_workspace_size(const attr_muon_matrix* mats, int32_t n_mats, int32_t pairs);
 attr_status attr_muon_step(const attr_muon_matrix* mats, int32_t n_mats, attr_dtype p_dtype,
                            attr_dtype g_dtype, double lr, double momentum, int32_t nesterov,
@@ -530,10 +534,10 @@ attr_status attr_embed(const attr_rows* rows, const int64_t* token, const void* 
 /* The table's gradient:
  *     dtable[v] = scale * sum of dout[row] over the rows inside whose token is v
  * for every v in [0, V) (zeros where there is none), or with accumulate added to
- * the rows of dtable whose tokens the batch holds, the others left alone.  The rows are
- * sorted by token first, and a token's are added up in fp32 in the order of their
- * slots (32 neighbours of that sorted order at a time, these sums in fp64): no
- * atomic additions, the same bits for the same call.
+ * the rows of dtable whose tokens the batch holds, the others left alone.  A token's
+ * rows are added up in fp32 in the order of their slots; past 512 slots the rows are
+ * sorted by token, and 32 or 64 neighbours of that order added up at a time, these
+ * sums in fp64.  The same bits for the same call.
  *   dout        device [n_rows, d], row stride ldd >= d; n_rows below 2^32
  *   dtable      device [V, d], row stride ldt >= d; overlaps no input
  *   ws          attr_embed_backward_workspace_size(rows, V, d) bytes, 256-byte aligned */
@@ -547,7 +551,7 @@ attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, con
  *     mean = sum_j x_j / d,   rstd = 1 / sqrt(sum_j (x_j - mean)^2 / d + eps)
  *     y_j = (x_j - mean) rstd w_j + b_j
  * in fp32 (the sums over a row too), y rounded once.  A row whose squares pass
- * fp32's range has rstd 0.
+ * fp32's range has rstd 0; with eps = 0 a row of equal values may be NaN.
  *   x, y        device [n_rows, d], any types, strides >= d and element alignment;
  *               1 <= d <= 32768.  y may be x itself with the same type and stride; any
  *               other overlap is ATTR_ERR_INVALID_ARG
