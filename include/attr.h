@@ -535,9 +535,8 @@ attr_status attr_embed(const attr_rows* rows, const int64_t* token, const void* 
  *     dtable[v] = scale * sum of dout[row] over the rows inside whose token is v
  * for every v in [0, V) (zeros where there is none), or with accumulate added to
  * the rows of dtable whose tokens the batch holds, the others left alone.  A token's
- * rows are added up in fp32 in the order of their slots; past 512 slots the rows are
- * sorted by token, and 32 or 64 neighbours of that order added up at a time, these
- * sums in fp64.  The same bits for the same call.
+ * rows are added up in fp32 in the order of their slots, up to 128 of them at a time
+ * (of a sorted batch: 64), and these sums in fp64.  The same bits for the same call.
  *   dout        device [n_rows, d], row stride ldd >= d; n_rows below 2^32
  *   dtable      device [V, d], row stride ldt >= d; overlaps no input
  *   ws          attr_embed_backward_workspace_size(rows, V, d) bytes, 256-byte aligned */

@@ -1474,7 +1474,7 @@ EmbedLayout embed_layout(const attr_rows* r, int64_t V, int64_t d) {
   EmbedLayout L;
   std::memset(&L, 0, sizeof(L));
   const size_t n = (size_t)(r->n_examples * r->T), each = align_up(4 * n);
-  if (n <= attr::kEmbedSmall) return L;
+  if (attr::embed_searches(n, V, d)) return L;
   L.key[0] = 0;
   L.key[1] = each;
   L.row[0] = 2 * each;
@@ -1559,7 +1559,7 @@ attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, con
     a.accumulate = accumulate;
     a.scale = scale;
     const attr::RowsArgs r = none ? attr::RowsArgs{nullptr, nullptr, 0, 0, 1} : rows_args(rows);
-    if (r.n_slots <= attr::kEmbedSmall) {
+    if (attr::embed_searches(r.n_slots, V, d)) {
       const hipError_t e = attr::launch_embed_small((int)dout_dtype, (int)dtable_dtype, r, token, a, s);
       return e == hipSuccess ? ATTR_OK : device_fail(e, "attr_embed_backward launch");
     }

@@ -479,56 +479,107 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, uint32
   }
 }
 
-// A batch of up to 64 K slots, without a sort: a wave looks through its tokens for those of
-// `each` rows of the table, and adds up their rows in the order of their slots.
+// A batch of up to 64 K slots, without a sort: a wave looks through its tokens for those of `each` rows of
+// the table, and adds up their rows in the order of their slots.  A token of more than kEmbedLong rows
+// takes a workgroup, a quarter of its rows each wave (512 slots of one token: 39.5 us, by one wave 151).
+constexpr int kEmbedLong = 64;
+struct Found {
+  uint32_t count;  // the tokens' slots that have the token
+  template <int K>
+  __device__ inline Found(const Pair (&p)[K], uint32_t v, uint32_t* list) : count(0) {
+    const uint32_t lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {  // their rows, in their order
+      const bool mine = p[k].key == v;
+      const uint64_t has = __ballot(mine);
+      if (mine) list[count + (uint32_t)__popcll(has & ((1ull << lane) - 1))] = p[k].row;
+      count += (uint32_t)__popcll(has);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+};
+// Adds up rows [from, to) of a list, eight of them in flight (16 take the kernel 178 registers: 400 slots of
+// 1024 in 21.5 us, where they take 12).
+template <typename G, int N>
+__device__ inline void sum_list(const EmbedGradArgs& a, const uint32_t* list, uint32_t from, uint32_t to, Cols<N> c, float (&sum)[N]) {
+  constexpr int U = 8;
+  const uint32_t lane = threadIdx.x & 63;
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum[e] = 0.f;
+  for (uint32_t i0 = from; i0 < to; i0 += U) {
+    const uint32_t rows = list[i0 + (lane & (U - 1)) < to ? i0 + (lane & (U - 1)) : i0];
+    Raw<G, N> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      x[u].load((const G*)a.dout + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)rows, u) * a.ldd + c.at);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u < to) {
+        float f[N];
+        x[u].get(f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += f[e];
+      }
+    }
+  }
+}
 template <typename G, typename T, int N, int K>
 __global__ __launch_bounds__(256) void embed_small_kernel(RowsArgs r, const int64_t* token, EmbedGradArgs a, uint32_t each,
                                                           uint32_t cuts, uint64_t units) {
-  constexpr int U = 8;
   __shared__ uint32_t lists[4][64 * K];
-  uint32_t* const list = lists[threadIdx.x >> 6];
-  const uint32_t lane = threadIdx.x & 63;
-  const uint64_t first = (uint64_t)blockIdx.x * 4 + wave_uniform(threadIdx.x >> 6);
-  if (first >= units) return;
+  __shared__ uint32_t longs[4][8], n_long[4];  // each wave's tokens of many rows
+  __shared__ float quarter[3][N][64];
+  const uint32_t lane = threadIdx.x & 63, wave = wave_uniform(threadIdx.x >> 6);
+  uint32_t* const list = lists[wave];
   Pair p[K];
   load_tokens<K>(r, token, a.V, 0, r.n_slots, p);
 #pragma unroll
   for (int k = 0; k < K; ++k)
     if (k * 64 + lane >= r.n_slots) p[k].key = (uint32_t)a.V;
-  for (uint64_t unit = first; unit < units; unit += (uint64_t)gridDim.x * 4) {
-    const int64_t v0 = (int64_t)(unit / cuts) * each, v1 = v0 + each < a.V ? v0 + each : a.V;
-    const Cols<N> c((int)(((uint32_t)(unit % cuts)) * 64 + lane) * N, a.d);
-    for (int64_t v = v0; v < v1; ++v) {
-      int count = 0;
-#pragma unroll
-      for (int k = 0; k < K; ++k) {  // the rows of the slots that have the token, in their order
-        const bool mine = p[k].key == (uint32_t)v;
-        const uint64_t has = __ballot(mine);
-        if (mine) list[count + __popcll(has & ((1ull << lane) - 1))] = p[k].row;
-        count += (int)__popcll(has);
-      }
-      if (a.accumulate && count == 0) continue;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      float sum[N];
-#pragma unroll
-      for (int e = 0; e < N; ++e) sum[e] = 0.f;
-      for (int i0 = 0; i0 < count; i0 += U) {
-        const uint32_t rows = list[i0 + (lane & (U - 1)) < (uint32_t)count ? i0 + (lane & (U - 1)) : i0];
-        Raw<G, N> x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          x[u].load((const G*)a.dout + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)rows, u) * a.ldd + c.at);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (i0 + u >= count) break;
-          float f[N];
-          x[u].get(f);
-#pragma unroll
-          for (int e = 0; e < N; ++e) sum[e] += f[e];
+  for (uint64_t first = (uint64_t)blockIdx.x * 4; first < units; first += (uint64_t)gridDim.x * 4) {
+    const uint64_t unit = first + wave;
+    uint32_t longer = 0;
+    if (unit < units) {
+      const int64_t v0 = (int64_t)(unit / cuts) * each, v1 = v0 + each < a.V ? v0 + each : a.V;
+      const Cols<N> c((int)(((uint32_t)(unit % cuts)) * 64 + lane) * N, a.d);
+      for (int64_t v = v0; v < v1; ++v) {
+        const Found f(p, (uint32_t)v, list);
+        if (a.accumulate && f.count == 0) continue;
+        if (f.count > kEmbedLong) {
+          longs[wave][longer++] = (uint32_t)v;
+          continue;
         }
+        float sum[N];
+        sum_list<G, N>(a, list, 0, f.count, c, sum);
+        put_sum<T, N>(a, (uint32_t)v, c, sum);
       }
-      put_sum<T, N>(a, (uint32_t)v, c, sum);
     }
+    if constexpr (K == 1) continue;
+    if (lane == 0) n_long[wave] = longer;
+    __syncthreads();
+    for (uint32_t w = 0; w < 4; ++w) {
+      const Cols<N> c((int)(((uint32_t)((first + w) % cuts)) * 64 + lane) * N, a.d);
+      for (uint32_t k = 0; k < n_long[w]; ++k) {
+        const uint32_t v = longs[w][k];
+        const Found f(p, v, list);
+        const uint32_t share = (f.count + 3) / 4, from = wave * share, to = from + share < f.count ? from + share : f.count;
+        float sum[N];
+        sum_list<G, N>(a, list, from, to, c, sum);
+        if (wave > 0) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) quarter[wave - 1][e][lane] = sum[e];
+        }
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            sum[e] = (float)((double)sum[e] + quarter[0][e][lane] + quarter[1][e][lane] + quarter[2][e][lane]);
+          put_sum<T, N>(a, v, c, sum);
+        }
+        __syncthreads();
+      }
+    }
+    __syncthreads();  // n_long is read until here
   }
 }
 
@@ -541,13 +592,14 @@ hipError_t embed_rows(const RowsArgs& r, const EmbedArgs& a, hipStream_t s) {
 }
 template <typename G, typename T, int N>
 hipError_t embed_small(const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a, hipStream_t s) {
-  const uint32_t cuts = (uint32_t)((a.d + 64 * N - 1) / (64 * N));
+  const uint32_t cuts = embed_small_cuts(a.d);
   // a small table: a wave for each row; a large one: fewer searches of the tokens (256 slots of 1024,
   // 50257 rows: 36.3 us, a wave for each row 45.0; 2048 rows: 5.2 and 5.5)
   const uint32_t each = a.V <= 8192 ? 1 : 8;
   const uint64_t units = ((uint64_t)a.V + each - 1) / each * cuts;
   const dim3 grid(grid_of((units + 3) / 4));
-  if (r.n_slots <= 256) hipLaunchKernelGGL((embed_small_kernel<G, T, N, 4>), grid, dim3(256), 0, s, r, token, a, each, cuts, units);
+  if (r.n_slots <= 64) hipLaunchKernelGGL((embed_small_kernel<G, T, N, 1>), grid, dim3(256), 0, s, r, token, a, each, cuts, units);
+  else if (r.n_slots <= 256) hipLaunchKernelGGL((embed_small_kernel<G, T, N, 4>), grid, dim3(256), 0, s, r, token, a, each, cuts, units);
   else hipLaunchKernelGGL((embed_small_kernel<G, T, N, kEmbedSmall / 64>), grid, dim3(256), 0, s, r, token, a, each, cuts, units);
   return hipGetLastError();
 }
@@ -617,8 +669,8 @@ hipError_t launch_embed_small(int dout_dtype, int table_dtype, const RowsArgs& r
                               hipStream_t s) {
   return with_type(dout_dtype, [&](auto g) {
     return with_type(table_dtype, [&](auto t) {
-      if (a.d > 256) return embed_small<decltype(g), decltype(t), 8>(r, token, a, s);
-      if (a.d > 64) return embed_small<decltype(g), decltype(t), 4>(r, token, a, s);
+      if (embed_small_lane(a.d) == 8) return embed_small<decltype(g), decltype(t), 8>(r, token, a, s);
+      if (embed_small_lane(a.d) == 4) return embed_small<decltype(g), decltype(t), 4>(r, token, a, s);
       return embed_small<decltype(g), decltype(t), 1>(r, token, a, s);
     });
   });

@@ -367,8 +367,15 @@ struct EmbedGradArgs {
   int32_t d, accumulate;
   float scale;
 };
-// Slots of a batch that needs no sort (400 slots, a table of 8192 x 1024: 11.9 us without, 24.2 with it).
+// Whether a batch needs no sort: up to kEmbedSmall slots, searched for every row of the table (400 slots, a
+// table of 8192 x 1024: 13.3 us without a sort, 24.2 with it), unless these searches are many (256 slots and
+// 128256 x 2048, added to, 2.1M searches of 64 slots: 36.9 us and 25.5).
 constexpr uint32_t kEmbedSmall = 512;
+inline int embed_small_lane(int64_t d) { return d > 256 ? 8 : d > 64 ? 4 : 1; }
+inline uint32_t embed_small_cuts(int64_t d) { return (uint32_t)((d + 64 * embed_small_lane(d) - 1) / (64 * embed_small_lane(d))); }
+inline bool embed_searches(uint64_t n, int64_t V, int64_t d) {
+  return n <= kEmbedSmall && (n + 63) / 64 * (uint64_t)V * embed_small_cuts(d) <= (1u << 20);
+}
 hipError_t launch_embed_small(int dout_dtype, int table_dtype, const RowsArgs& r, const int64_t* token, const EmbedGradArgs& a,
                               hipStream_t s);
 hipError_t launch_embed_grad(int dout_dtype, int table_dtype, const EmbedGradArgs& a, hipStream_t s);

@@ -554,6 +554,9 @@ def test_embed_backward_many_parts():
         B = Batch(1, n, False, n, ragged=False)
         token = np.where(B.r.random(B.rows) < 0.3, 1, B.r.integers(0, V, B.rows))
         back_case(V, 12, BF16, F32, B, token, False, 1.0)
+    for n, V, d in ((400, 3, 700), (64, 1, 300), (65, 1, 300), (300, 100000, 2100)):   # tokens of many rows; a search too long
+        B = Batch(n, 1, True, n)
+        back_case(V, d, F16, F32, B, B.r.integers(0, V, B.rows), True, 0.7)
 
 
 def test_tensors_of_another_device_than_the_current_one(monkeypatch):
