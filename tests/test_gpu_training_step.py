@@ -5,6 +5,7 @@ import os
 import pytest
 import torch
 
+import paper_2606_11660_amd as P
 from tests._util import say
 
 pytestmark = pytest.mark.gpu
@@ -104,3 +105,57 @@ def test_a_captured_step(ex):
         torch.cuda.synchronize()
         for name in m.names:
             assert torch.equal(getattr(m, name), getattr(w, name)), (k, name)
+
+
+def test_captured_calls_of_every_plan():
+    """The embedding's gradient without a sort, sorted by one workgroup and by several, the norm's with
+    shares, Muon on thin, long and square matrices: one graph, replayed over new values beside eager work."""
+    n_slots, V, d = (300, 3000, 9000), 5000, 72
+    dout = [torch.empty(n, d, device="cuda") for n in n_slots]
+    token = [torch.empty(n, dtype=torch.int64, device="cuda") for n in n_slots]
+    table = [torch.empty(V, d, device="cuda") for _ in n_slots]
+    x = torch.empty(3000, d, device="cuda")
+    mean, rstd, dw = (torch.empty(n, device="cuda") for n in (3000, 3000, d))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    shapes = [(9000, 16), (2500, 70), (200, 200)]
+    w, g, m = ([torch.zeros(s, device="cuda") for s in shapes] for _ in range(3))
+    plan = P.MuonTensors(w, g, m)
+    ws = P.Workspace()
+
+    def fill(seed):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        for t in dout + [x] + w + g + m:
+            t.normal_(generator=gen)
+        for t in token:
+            t.random_(0, V, generator=gen)
+            t[::3] = seed
+
+    def calls():
+        for a, b, c in zip(dout, token, table):
+            P.attr_embed_backward(a, b, c, ws=ws)
+        P.attr_layer_norm(x, y, mean=mean, rstd=rstd)
+        P.attr_layer_norm_backward(y, x, mean, rstd, dx=dx, dweight=dw, ws=ws)
+        P.attr_muon_step(plan, 0.02, ws=ws)
+
+    outs = table + [y, mean, rstd, dx, dw] + w + m
+    side = torch.cuda.Stream()
+    fill(0)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        calls()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for k in range(1, 4):
+        fill(k)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        fill(k)
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.current_stream())
+            calls()
+        side.synchronize()
+        for j, (a, b) in enumerate(zip(got, outs)):
+            assert torch.equal(a, b) and torch.isfinite(a).all(), (k, j)
