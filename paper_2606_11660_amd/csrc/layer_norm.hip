@@ -400,8 +400,11 @@ hipError_t launch_layer_norm(int x_dtype, int y_dtype, const RowsArgs& r, const 
 // Shares of a unit: workgroups enough to fill the GPU, each with several rows, since its sums are written
 // and read again; past 16384 columns, where a row takes 40 us, with one at least (64 rows of 32768: 55 us,
 // with four 120).
+// As many as the GPU holds at once: 1024 workgroups of a few registers a thread, 512 of many (32768 rows, us,
+// with 512 / 1024: of 512 bf16 37.2 / 31.0, of 1024 fp32 81.4 / 86.5, of 2048 bf16 128 / 97.6; 16384 of 4096
+// bf16 93.0 / 110).
 uint32_t norm_chunks(uint32_t unit, uint32_t units, int32_t d) {
-  const uint32_t rows = d <= 1024 ? 16 : d <= 16384 ? 4 : 1, most = d <= 2048 ? 1024 : 512;
+  const uint32_t rows = d <= 1024 ? 16 : d <= 16384 ? 4 : 1, most = d <= 512 || (d > 1024 && d <= 2048) ? 1024 : 512;
   const uint32_t by_rows = (unit + rows - 1) / rows, by_units = most / units;
   return by_rows < by_units ? by_rows : by_units > 1 ? by_units : 1;
 }
