@@ -493,8 +493,7 @@ PyObject* py_rows_call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     try {
       for (int k = 0; k < 4; ++k)
         if (written[op][k] >= 0) bump(PyTuple_GET_ITEM(args[4], written[op][k]));
-    } catch (...) {
-      Py_RETURN_NONE;
+    } catch (...) {  // the call is made: None would make it again
     }
   }
   return PyLong_FromLong((long)st);
