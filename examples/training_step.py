@@ -39,7 +39,7 @@ class Model:
         self.adam = P.AdamTensors([getattr(self, k) for k in vectors], [self.grad[k] for k in vectors], zeros(vectors),
                                   zeros(vectors))
         self.muon = P.MuonTensors([self.head], [self.grad["head"]], zeros(["head"]), weight_decay=0.01,
-                                  lr_scale=max(1.0, V / D) ** 0.5)
+                                  update_scale=max(1.0, V / D) ** 0.5)
 
 
 class Batch:

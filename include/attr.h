@@ -465,8 +465,8 @@ typedef struct {
   float* m;         /* momentum */
   float* master;    /* fp32 weights that the step updates, or NULL: p itself */
   int64_t rows, cols;  /* 0 <= rows, cols <= 2^20; see below for their product */
-  float lr_scale;   /* times lr for this matrix */
-  float weight_decay;
+  float lr_scale;   /* times lr for this matrix: of its update and of its decay */
+  float weight_decay;  /* to scale the update alone by f: lr_scale f and weight_decay / f */
 } attr_muon_matrix;
 
 /* For every matrix, with g' = grad_scale g (a device scalar, or NULL: 1):

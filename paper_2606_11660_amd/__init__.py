@@ -850,27 +850,35 @@ class MuonTensors:
     p, g, m: lists of contiguous 2-D tensors, one of each per weight matrix, of the
     same shape; p and g fp32, bf16 or fp16, all of one type each; m (the momentum)
     fp32.  master: fp32 weights that the step updates, p taking their rounded values.
-    weight_decay and lr_scale: one number, or one for each matrix (a common choice of
-    lr_scale is sqrt(max(1, rows / cols)); 0.2 sqrt(max(rows, cols)) makes steps as long
-    as AdamW's).
+    weight_decay, lr_scale and update_scale: one number, or one for each matrix.
+    lr_scale is of the matrix's rate, so of its decay too, as in ``AdamTensors``;
+    update_scale (positive) is of the orthogonal update alone:
+        w - lr lr_scale (weight_decay w + update_scale X).
+    What a published recipe scales by a matrix's shape is the update: sqrt(max(1, rows / cols)), or
+    0.2 sqrt(max(rows, cols)), which makes steps as long as AdamW's and goes with its rate and decay.
 
     The object keeps the tensors and their addresses: give their storage new
     contents, not a new place.
     """
 
     def __init__(self, p: Sequence[torch.Tensor], g: Sequence[torch.Tensor], m: Sequence[torch.Tensor],
-                 master: Optional[Sequence[torch.Tensor]] = None, weight_decay=0.0, lr_scale=1.0):
+                 master: Optional[Sequence[torch.Tensor]] = None, weight_decay=0.0, lr_scale=1.0, update_scale=1.0):
         n = len(p)
         if n == 0:
             raise ValueError("need at least one matrix")
         kinds = {"p": (p, p[0].dtype), "g": (g, g[0].dtype if len(g) else None), "m": (m, torch.float32),
                  "master": (master, torch.float32)}
         kinds = {k: x for k, x in kinds.items() if x[0] is not None}
-        decay, scale = ([float(x)] * n if isinstance(x, (int, float)) else [float(y) for y in x]
-                        for x in (weight_decay, lr_scale))
-        for name, ts in [(k, x[0]) for k, x in kinds.items()] + [("weight_decay", decay), ("lr_scale", scale)]:
+        decay, scale, update = ([float(x)] * n if isinstance(x, (int, float)) else [float(y) for y in x]
+                                for x in (weight_decay, lr_scale, update_scale))
+        for name, ts in [(k, x[0]) for k, x in kinds.items()] + [("weight_decay", decay), ("lr_scale", scale),
+                                                                 ("update_scale", update)]:
             if len(ts) != n:
                 raise ValueError(f"{name} has {len(ts)} entries, p has {n}")
+        if not all(0.0 < x < float("inf") for x in update):
+            raise ValueError("update_scale must be positive and finite")
+        # the entry point's rate is of the decay too
+        decay, scale = [x / u for x, u in zip(decay, update)], [x * u for x, u in zip(scale, update)]
         self.p_dtype, self.g_dtype = _dtype(p[0]), _dtype(g[0])
         self.tensors = {k: list(x[0]) for k, x in kinds.items()}
         self.weights = self.tensors["p"] + self.tensors.get("master", [])  # what autograd may have saved

@@ -264,3 +264,31 @@ def test_autograd_sees_the_step():
         P.attr_muon_step(P.MuonTensors([w.detach()], [torch.randn(6, 6, device="cuda")], [torch.zeros(6, 6, device="cuda")]), 0.1)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+@pytest.mark.parametrize("p,master", [(F32, False), (BF16, True), (F16, False)])
+def test_a_factor_of_the_update_alone(p, master):
+    """x (1 - lr wd) - lr f X: the decay is the rate's, whatever the matrix's shape scales the update by.
+    Roundings, in half steps of 2^-24: lr f and wd / f one each, lr wd one, then two products and two
+    differences; of the weight once more where it has 16 bits."""
+    shapes, f, lr, wd, rate = [(70, 30), (30, 70), (200, 90)], [12.8, 0.3, (200 / 90) ** 0.5], 0.02, 0.5, [1.0, 2.0, 0.7]
+    M, Z = Model(4, shapes, p, F32, master), Model(4, shapes, F32, F32, zero=True)
+    P.attr_muon_step(M.plan(weight_decay=wd, lr_scale=rate, update_scale=f), lr)
+    P.attr_muon_step(Z.plan(), -1.0, pairs=p == F32 or master)
+    for j, s in enumerate(shapes):
+        w, x, r = M.was[j][0], host(Z.p[j].double()), lr * rate[j]
+        want = w * (1 - r * wd) - r * f[j] * x
+        tol = V * (5 * np.abs(w) * r * wd + 4 * np.abs(r * f[j] * x) + 2 * (np.abs(w) + np.abs(want)))
+        got = M.master[j] if master else M.p[j]
+        tol = tol + {F32: 0.0, F16: 2.0 ** -11}[got.dtype] * (np.abs(want) + tol) + (2.0 ** -25 if got.dtype == F16 else 0.0)
+        assert (np.abs(host(got.double()) - want) <= tol).all(), s
+        assert not master or torch.equal(M.p[j], got.to(p))
+
+
+def test_factors_that_are_refused():
+    t = [torch.zeros(4, 5, device="cuda") for _ in range(3)]
+    for bad in (0.0, -1.0, float("inf"), float("nan")):
+        with pytest.raises(ValueError, match="update_scale"):
+            P.MuonTensors([t[0]], [t[1]], [t[2]], update_scale=bad)
+    with pytest.raises(ValueError, match="entries"):
+        P.MuonTensors([t[0]], [t[1]], [t[2]], update_scale=[1.0, 2.0])
