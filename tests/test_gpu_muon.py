@@ -292,3 +292,92 @@ def test_factors_that_are_refused():
             P.MuonTensors([t[0]], [t[1]], [t[2]], update_scale=bad)
     with pytest.raises(ValueError, match="entries"):
         P.MuonTensors([t[0]], [t[1]], [t[2]], update_scale=[1.0, 2.0])
+
+
+# ----------------------------------------------------------------------------
+# 256 x 256 tiles (shorter sides from 1024, 128 such tiles of A's in a call), rounds, special values
+# ----------------------------------------------------------------------------
+LARGE = [(1025, 1100), (1100, 1025)] * 5      # 15 tiles of A's each: 150
+
+
+@pytest.mark.parametrize("pairs", [False, True], ids=["f16", "pairs"])
+def test_large_tiles(pairs):
+    """Sides that end inside a tile, both ways round; the same bits again."""
+    say(f"case: muon tiles of 256, pairs={pairs}")
+    M, N = Model(15, LARGE, zero=True), Model(15, LARGE, zero=True)
+    P.attr_muon_step(M.plan(), -1.0, pairs=pairs)
+    P.attr_muon_step(N.plan(), -1.0, pairs=pairs)
+    for j in (0, 1, 2, 9):
+        w, g, m = M.was[j]
+        _, nm, x = O.muon(w, g, m, -1.0)
+        off, tol = np.linalg.norm(host(M.p[j]) - x), tolerance(0.95 * nm + 0.05 * g, pairs)
+        say(f"case: muon {LARGE[j]} {j} off by {off / np.linalg.norm(x)} of {tol / np.linalg.norm(x)}")
+        assert off <= tol
+    for a, b in zip(M.p + M.m, N.p + N.m):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("p,g,master", [(F32, F32, False), (BF16, BF16, True), (BF16, BF16, False), (F16, F32, False)])
+def test_large_tiles_weights(p, g, master):
+    """The step of the weights from that update, rounded once, between aligned places too."""
+    for shift in (0, 1):
+        say(f"case: muon tiles of 256, weights {p} shift={shift}")
+        M, Z = Model(16, LARGE, p, g, master, shift=shift), Model(16, LARGE, F32, g, zero=True)
+        pairs = p == F32 or master
+        P.attr_muon_step(M.plan(weight_decay=0.1), 0.02)
+        P.attr_muon_step(Z.plan(), -1.0, pairs=pairs)
+        lr, lr_wd = np.float32(0.02), np.float32(0.02 * np.float64(np.float32(0.1)))
+        for j in (0, 1, 9):
+            w = M.was[j][0].astype(np.float32)
+            want = w - w * lr_wd - host(Z.p[j]) * lr
+            got = M.master[j] if master else M.p[j]
+            assert torch.equal(got, torch.from_numpy(want).cuda().to(got.dtype)), j
+            assert not master or torch.equal(M.p[j], got.to(p))
+            assert torch.equal(M.m[j], Z.m[j])
+
+
+class Many:
+    """n matrices of one shape and zero weights, gradients of normal values in one buffer."""
+
+    def __init__(self, n, shape, seed=21):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.g = torch.empty((n,) + shape, device="cuda", dtype=BF16).normal_(generator=gen)
+        self.p, self.m = (torch.zeros((n,) + shape, device="cuda") for _ in range(2))
+
+    def plan(self, n=None):
+        return P.MuonTensors(list(self.p[:n]), list(self.g[:n]), list(self.m[:n]))
+
+    def check(self, j, pairs):
+        g = host(self.g[j].double()) * (1.0 - 0.5)
+        x = O.newton_schulz(g)
+        off, tol = np.linalg.norm(host(self.p[j]) - x), tolerance(g, pairs)
+        say(f"case: muon matrix {j} off by {off / np.linalg.norm(x)} of {tol / np.linalg.norm(x)}")
+        assert off <= tol, j
+
+
+@pytest.mark.parametrize("n,last,shape,pairs", [(48, 1, (1030, 4200), False), (24, 1, (4200, 1030), True),
+                                                (460, 4, (70, 1100), False), (460, 4, (1100, 70), True)])
+def test_rounds(n, last, shape, pairs):
+    """More matrices than are worked on together: the last round has one of 256-tiles, or four of one
+    128-tile each, which share out their rows; the same bits again."""
+    say(f"case: muon {n} of {shape} pairs={pairs}")
+    M, N = Many(n, shape), Many(n, shape)
+    size = [P.attr_muon_step_workspace_size(M.plan(k), pairs) for k in (n - last - 1, n - last, n)]
+    assert size[0] < size[1] == size[2]    # the last ones take a round of their own
+    for t in (M, N):
+        P.attr_muon_step(t.plan(), -1.0, momentum=0.5, nesterov=False, pairs=pairs)
+    assert torch.equal(M.p, N.p) and torch.equal(M.m, M.g.float() * 0.5)
+    for j in (0, n - 2, n - 1):
+        M.check(j, pairs)
+
+
+def test_many_shapes_of_tiles():
+    """More shapes than a launch takes groups, matrices of one and of several tiles: each as alone."""
+    shapes = [(66 + 5 * j, 70 + 17 * (j * 7 % 23)) for j in range(22)] * 2
+    for pairs in (False, True):
+        M = Model(17, shapes, zero=True)
+        P.attr_muon_step(M.plan(), -1.0, pairs=pairs)
+        for j in range(0, 44, 5):
+            A = Model(17, shapes, zero=True)
+            P.attr_muon_step(P.MuonTensors([A.p[j]], [A.g[j]], [A.m[j]]), -1.0, pairs=pairs)
+            assert torch.equal(A.p[j], M.p[j]) and torch.equal(A.m[j], M.m[j]), shapes[j]
