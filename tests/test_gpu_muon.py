@@ -381,3 +381,35 @@ def test_many_shapes_of_tiles():
             A = Model(17, shapes, zero=True)
             P.attr_muon_step(P.MuonTensors([A.p[j]], [A.g[j]], [A.m[j]]), -1.0, pairs=pairs)
             assert torch.equal(A.p[j], M.p[j]) and torch.equal(A.m[j], M.m[j]), shapes[j]
+
+
+@pytest.mark.parametrize("pairs", [False, True], ids=["f16", "pairs"])
+@pytest.mark.parametrize("shape", [(130, 200), (300, 70), (1030, 1100)])
+def test_special_values_on_tiles(shape, pairs):
+    """A zero update, NaN and infinities, huge and tiny gradients, one entry, one direction: each
+    matrix on its own, on tiles of 128 and of 256."""
+    say(f"case: muon special values {shape} pairs={pairs}")
+    r = np.random.default_rng(5)
+    g = [matrix(r, *shape) * 1e3 for _ in range(9)]
+    g[0][:] = 0
+    g[1][-1, -1], g[2][0, 3], g[3][7, 0] = np.nan, np.inf, -np.inf
+    g[4] *= 1e34
+    g[5] *= 1e-34
+    g[6][:] = 0
+    g[6][shape[0] - 2, shape[1] - 1] = 3.0
+    g[7] = np.outer(g[7][:, 0], g[7][0])
+    gt = [torch.from_numpy(x).float().cuda() for x in g]
+    for w in (0.0, 1.0):
+        p, m = [torch.full(shape, w, device="cuda") for _ in g], [torch.zeros(shape, device="cuda") for _ in g]
+        P.attr_muon_step(P.MuonTensors(p, gt, m, weight_decay=0.5 * w), -1.0 + 1.1 * w, momentum=0.5, pairs=pairs)
+        assert torch.equal(p[0], torch.full_like(p[0], float(w - w * np.float32(0.05)) if w else 0.0))
+        assert all(torch.isnan(p[j]).all() for j in (1, 2, 3))
+        if w:
+            assert all(torch.isfinite(p[j]).all() for j in (4, 5, 6, 7, 8))
+            continue
+        for j in (4, 5, 6, 7, 8):
+            u = host(gt[j].double())    # X does not depend on its length
+            # an update near the end of fp32's range: 2^-149 / 1e-34 = 1.4e-11 of it
+            off, tol = np.linalg.norm(host(p[j]) - O.newton_schulz(u)), tolerance(u, pairs)
+            say(j, "off by", off, "of", tol)
+            assert off <= tol, j
