@@ -570,3 +570,17 @@ def test_tensors_of_another_device_than_the_current_one(monkeypatch):
                  lambda: P.attr_muon_step(plan, 0.1)):
         with pytest.raises(ValueError, match="current GPU device"):
             call()
+
+
+@pytest.mark.parametrize("d", [65, 769, 1025, 2100])
+@pytest.mark.parametrize("dout,table", [(BF16, F32), (F16, F16), (F32, BF16)])
+def test_embed_backward_sorted(d, dout, table):
+    """Batches that are sorted, by one workgroup and by several: four and eight columns a lane, a token whose
+    rows cross many parts, tables between aligned places and with gaps, written whole and added to."""
+    for n, T, V, packed, accumulate, pad, shift in ((6, 500, 700, False, False, 3, 1), (6, 500, 700, True, True, 0, 1),
+                                                    (9, 1000, 700, True, False, 0, 1), (9, 1000, 20011, False, True, 3, 0),
+                                                    (9, 1000, 20011, True, False, 3, 1)):
+        say(f"case: embed backward sorted d={d} {dout}->{table} n={n * T} V={V} packed={packed} accumulate={accumulate}")
+        B = Batch(n, T, packed, d + V + pad)
+        token = np.where(B.r.random(B.rows) < 0.3, V // 2, B.r.integers(-1, V + 1, B.rows))
+        back_case(V, d, dout, table, B, token, accumulate, 0.7, pad, shift)
