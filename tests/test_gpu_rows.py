@@ -584,3 +584,41 @@ def test_embed_backward_sorted(d, dout, table):
         B = Batch(n, T, packed, d + V + pad)
         token = np.where(B.r.random(B.rows) < 0.3, V // 2, B.r.integers(-1, V + 1, B.rows))
         back_case(V, d, dout, table, B, token, accumulate, 0.7, pad, shift)
+
+
+def forward_case(B, d, xt, yt, wt, pad, shift, eps=1e-5):
+    """Layer norm of a batch against the oracle; y is x itself where pad and shift are 0 and the types are one."""
+    x = B.put(B.r.standard_normal((B.rows, d)) * np.exp(B.r.standard_normal((B.rows, 1))) + 2 * B.r.standard_normal((B.rows, 1)),
+              xt, pad, shift)
+    xs = host(x.double())
+    w, b = (torch.from_numpy(B.r.standard_normal(d)).cuda().to(wt) for _ in range(2))
+    in_place = xt == yt and not pad and not shift
+    y = (x, None) if in_place else B.empty(d, yt, pad, shift)
+    mean, rstd = (torch.full((B.rows,), 77.0, device="cuda") for _ in range(2))
+    P.attr_layer_norm(x, y[0], w, b, eps, mean, rstd, rows=B.c())
+    inside, pads = ([row for _, row, ok in B.slots if ok == want] for want in (True, False))
+    xs, wn, bn = xs[inside], host(w.double()), host(b.double())
+    m = xs.mean(1)
+    r = 1 / np.sqrt(np.square(xs - m[:, None]).mean(1) + eps)
+    want = (xs - m[:, None]) * r[:, None] * wn + bn
+    assert np.allclose(want[0], O.layer_norm(xs[0], wn, bn, eps)[0], rtol=1e-12, atol=1e-12)
+    dm, dr = stat_tolerances(xs, eps)
+    near(mean[inside], m, dm, F32)
+    near(rstd[inside], r, dr * r, F32)
+    unit = np.abs((xs - m[:, None]) * r[:, None])
+    tol = np.abs(wn) * (r[:, None] * (dm[:, None] + U * np.abs(xs)) + unit * (dr[:, None] + 4 * U)) + 2 * U * (np.abs(want) + np.abs(bn))
+    near(y[0][inside], want, tol, yt)
+    assert (y[0][pads] == 0).all() and (mean[pads] == 0).all() and (rstd[pads] == 0).all()
+    if not in_place:
+        B.untouched(y, d, pad)
+
+
+@pytest.mark.parametrize("n,T,d", [(10, 103, d) for d in (8, 512, 513, 769, 1023, 1024, 1025, 1500, 2048)]
+                         + [(10, 26, d) for d in (2049, 3001, 4096, 4100, 5000, 8191, 8192, 8199)])
+def test_layer_norm_of_many_rows(n, T, d):
+    """Batches past the sizes at which a row takes more threads (1024 slots to 2048 columns, 256 beyond):
+    packed, padded, with gaps and in place, widths that end inside a lane's vector."""
+    for xt, yt, wt, packed, pad, shift in ((F32, BF16, F32, True, 3, 1), (BF16, BF16, BF16, False, 0, 0),
+                                           (F32, F32, F16, True, 0, 0), (F16, F32, F32, False, 0, 1)):
+        say(f"case: layer norm of many rows d={d} n={n * T} {xt}->{yt} w={wt} packed={packed}")
+        forward_case(Batch(n, T, packed, d + 1), d, xt, yt, wt, pad, shift)
