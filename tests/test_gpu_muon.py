@@ -413,3 +413,13 @@ def test_special_values_on_tiles(shape, pairs):
             off, tol = np.linalg.norm(host(p[j]) - O.newton_schulz(u)), tolerance(u, pairs)
             say(j, "off by", off, "of", tol)
             assert off <= tol, j
+
+
+@pytest.mark.parametrize("pairs", [False, True], ids=["f16", "pairs"])
+@pytest.mark.parametrize("shape", [(1 << 20, 64), (65, 1 << 20), (1, 1 << 20)])
+def test_longest_sides(shape, pairs):
+    """The longest sides that are taken, of a thin matrix and of one tile's."""
+    say(f"case: muon {shape} pairs={pairs}")
+    M = Many(1, shape)
+    P.attr_muon_step(M.plan(), -1.0, momentum=0.5, nesterov=False, pairs=pairs)
+    M.check(0, pairs)

@@ -622,3 +622,88 @@ def test_layer_norm_of_many_rows(n, T, d):
                                            (F32, F32, F16, True, 0, 0), (F16, F32, F32, False, 0, 1)):
         say(f"case: layer norm of many rows d={d} n={n * T} {xt}->{yt} w={wt} packed={packed}")
         forward_case(Batch(n, T, packed, d + 1), d, xt, yt, wt, pad, shift)
+
+
+# ----------------------------------------------------------------------------
+# the largest sizes, compared on the GPU in 64 bits
+# ----------------------------------------------------------------------------
+@pytest.mark.parametrize("n,accumulate", [(40, True), (700, False)])
+def test_embed_widest(n, accumulate):
+    V, d = 30, 65536
+    B = Batch(n, 1, True, n)
+    say(f"case: embed d={d} n={n}")
+    token = B.r.integers(-1, V + 1, B.rows)
+    dt = back_case(V, d, BF16, F32, B, token, accumulate, 0.7)
+    o = B.empty(d, BF16)
+    P.attr_embed(dt, torch.from_numpy(token).cuda(), o[0], rows=B.c())
+    inside = [row for _, row, ok in B.slots if ok]
+    there = torch.from_numpy((token[inside] >= 0) & (token[inside] < V)).cuda()
+    want = dt[torch.from_numpy(token[inside].clip(0, V - 1)).cuda()].to(BF16)
+    assert torch.equal(o[0][inside], torch.where(there[:, None], want, 0))
+
+
+def test_embed_of_the_largest_table():
+    """2^28 rows: digits of four passes, zeros written beside them."""
+    V, n = 2 ** 28, 5000
+    say(f"case: embed backward V={V}")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    token = torch.randint(0, V, (n,), generator=gen, device="cuda")
+    token[::3], token[-1], token[7] = V - 1, V, 0
+    g = torch.randint(-8, 9, (n, 1), generator=gen, device="cuda").to(F32)   # sums are whole numbers below 2^14: exact
+    dt = torch.full((V, 1), 9.0, device="cuda")
+    P.attr_embed_backward(g, token, dt)
+    ok = token < V
+    want = torch.zeros(V, device="cuda", dtype=torch.float64).index_add_(0, token[ok], g[ok, 0].double())
+    assert torch.equal(dt[:, 0].double(), want)
+    out = torch.full((n, 1), 9.0, device="cuda")
+    P.attr_embed(dt, token, out)
+    assert torch.equal(out[ok], dt[token[ok]]) and (out[~ok] == 0).all()
+
+
+def test_more_rows_than_a_launch_has_waves():
+    """2^21 workgroups of four rows each, and some more: they stride over what is left."""
+    n, V = 2 ** 23 + 1001, 91
+    say(f"case: embed and layer norm n={n}")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    token = torch.randint(0, V, (n,), generator=gen, device="cuda")
+    table, out = torch.randn(V, 3, generator=gen, device="cuda"), torch.empty(n, 3, device="cuda")
+    P.attr_embed(table, token, out)
+    assert torch.equal(out, table[token])
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    y = torch.empty_like(out)
+    P.attr_layer_norm(out, y, mean=mean, rstd=rstd)
+    one, m1, r1 = torch.empty_like(table), torch.empty(V, device="cuda"), torch.empty(V, device="cuda")
+    P.attr_layer_norm(table, one, mean=m1, rstd=r1)
+    assert torch.equal(y, one[token]) and torch.equal(mean, m1[token]) and torch.equal(rstd, r1[token])
+
+
+@pytest.mark.parametrize("n,T,d,per_example", [(520, 270, 40, True), (520, 90, 1030, True), (520, 70, 2100, True),
+                                               (1, 300001, 40, False)])
+def test_layer_norm_backward_long_shares(n, T, d, per_example):
+    """Shares of more rows than a wave knows the places of at once (64).  dx as of few rows; sums: n u of the
+    magnitudes' sum."""
+    say(f"case: layer norm backward long shares n={n} T={T} d={d}")
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    x, dy = (torch.randn(n * T, d, generator=gen, device="cuda") for _ in range(2))
+    w = 1 + 0.3 * torch.randn(d, generator=gen, device="cuda")
+    length = torch.randint(0, T + 1, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    length[0] = T
+    inside = (torch.arange(T, device="cuda") < length[:, None]).view(-1)
+    mean, rstd = x.double().mean(1).float(), (1 / (x.double().var(1, correction=0) + 1e-5).sqrt()).float()
+    x[~inside], dy[~inside] = float("nan"), float("nan")
+    units = n if per_example else 1
+    dx = torch.full_like(x, 77.0)
+    dw, db = (torch.full((units, d), 0.5, device="cuda") for _ in range(2))
+    P.attr_layer_norm_backward(dy, x, mean, rstd, w, dx, dw if per_example else dw[0], db if per_example else db[0],
+                               per_example=per_example, accumulate=True, rows=P.ExampleRows(n, T, length=length))
+    u = torch.where(inside[:, None], (x.double() - mean[:, None]) * rstd[:, None], 0.0)
+    g = torch.where(inside[:, None], dy.double(), 0.0)
+    e = g * w
+    want = (e - e.mean(1, keepdim=True) - u * (e * u).mean(1, keepdim=True)) * rstd[:, None]
+    r, a = rstd[:, None].double(), e.abs()
+    tol = r * ((K + 4) * U * a.mean(1, keepdim=True) + 4 * U * a + u.abs() * ((K + 10) * U * (a * u.abs()).mean(1, keepdim=True)))
+    assert ((dx.double() - want).abs() <= tol + 2.0 ** -149).all()
+    terms = (T if per_example else n * T) + 6
+    for got, term in ((dw, g * u), (db, g)):
+        total, size = term.view(units, -1, d).sum(1), term.abs().view(units, -1, d).sum(1)
+        assert ((got.double() - total - 0.5).abs() <= terms * U * size + U).all()
