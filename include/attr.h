@@ -474,6 +474,7 @@ typedef struct {
  *     u = momentum m + (1 - momentum) g'   (nesterov; with the new m), else m
  *     X = u / |u|_F, then `steps` times, with A = X X^T:
  *     X = a X + (b A + c A A) X,   a = 3.4445, b = -4.7750, c = 2.0315
+ * (the coefficients published with the method; K. Jordan and others, 2024)
  *     x = x - lr' wd x - lr' X,    lr' = lr lr_scale
  * The polynomial takes singular values in (0, 1] towards 1 (after five steps those from
  * 0.002 on lie in [0.68, 1.21]), so X approaches the orthogonal factor of u.
@@ -481,9 +482,11 @@ typedef struct {
  * whose u is zero has X = 0; one with a NaN or an infinity in u becomes NaN.
  * m is fp32 without contraction, the norm fp64; the iteration runs on the matrix
  * cores with fp32 sums and its operands (X, A, a I + b A + c A A) rounded
- *   pairs = 0  to fp16, 11 bits: X is off by 1.2e-3 to 1.5e-3 of its norm (more where a
- *              few directions carry most of u);
- *   pairs = 1  to pairs of fp16, 22 bits: three times the products, X off by 1e-6 to 3e-6.
+ *   pairs = 0  to fp16, 11 bits: X is off by 1.2e-3 to 1.5e-3 of its norm, where a few
+ *              directions carry most of u by more (four of 512 with 10 times the rest's
+ *              norm: 3e-3 to 5e-3, with 100 times 2e-2 to 4e-2);
+ *   pairs = 1  to pairs of fp16, 22 bits: three times the products, X off by 1e-6 to 4e-6
+ *              (such directions with 100 times the rest: 7e-6).
  * Matrices whose shorter side is at most 64 run in fp64 on their products by themselves,
  * whatever `pairs`: X off by some 1e-7.  The same call gives the same bits; the order of
  * a larger matrix's sums depends on the sizes of all matrices of the call.
@@ -550,7 +553,8 @@ attr_status attr_embed_backward(const attr_rows* rows, const int64_t* token, con
  *     mean = sum_j x_j / d,   rstd = 1 / sqrt(sum_j (x_j - mean)^2 / d + eps)
  *     y_j = (x_j - mean) rstd w_j + b_j
  * in fp32 (the sums over a row too), y rounded once.  A row whose squares pass
- * fp32's range has rstd 0; with eps = 0 a row of equal values may be NaN.
+ * fp32's range has rstd 0, one whose sum does becomes NaN; with eps = 0 a row of equal
+ * values may be NaN.
  *   x, y        device [n_rows, d], any types, strides >= d and element alignment;
  *               1 <= d <= 32768.  y may be x itself with the same type and stride; any
  *               other overlap is ATTR_ERR_INVALID_ARG

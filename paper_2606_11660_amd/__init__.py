@@ -921,10 +921,10 @@ def attr_muon_step(tensors: MuonTensors, lr: float, momentum: float = 0.95, nest
     """One Muon step over every matrix: updates p and m (and master) in place, which autograd
     counts as a change of p and master.
 
-    pairs: whether the orthogonalisation holds its operands as pairs of fp16 (three
-    times the products, an update good to some 1e-6 of its norm) or as fp16 (1e-3).  None: pairs
-    where the step updates 32-bit weights (p or masters), fp16 where it updates 16-bit ones,
-    whose own rounding is coarser.  grad_scale: fp32 device scalar that multiplies the
+    pairs: whether the orthogonalisation holds its operands as pairs of fp16 (three times the
+    products, an update good to 1e-6 to 4e-6 of its norm) or as fp16 (1.2e-3 to 1.5e-3, and up to some 4e-2 where a
+    few directions carry nearly all of it).  None: pairs where the step updates 32-bit weights (p or
+    masters), fp16 where it updates 16-bit ones.  grad_scale: fp32 device scalar that multiplies the
     gradients.  A graph that captured the call repeats this step with its lr."""
     if grad_scale is not None:
         _vector(grad_scale, 1, torch.float32, "grad_scale")

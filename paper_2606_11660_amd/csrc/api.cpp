@@ -1151,8 +1151,12 @@ attr::MuonGroup thin_group(int64_t rows, int64_t cols) {
 
 constexpr int kTiles = 8, kBigTiles = 9;
 // Tiles of 256 x 256 for shorter sides from 1024 on, where the call has enough of them: 128 and more
-// for the products A, which have the fewest (bf16 weights, 128 x 128 in brackets: 4 of 2048 x 8192, 144
-// tiles, 2665 us (2982); 24 of 1024 x 4096, 240 tiles, 2251 (2810); 4 of them, 40 tiles, 844 (540)).
+// for the products A, which have the fewest (us, 128 x 128 in brackets; bf16 weights: 4 of 2048 x 8192, 144
+// tiles, 2665 (2982); 24 of 1024 x 4096, 240 tiles, 2251 (2810); 4 of them, 40 tiles, 844 (540)).  The line is a
+// middle one: fp32 weights, fp16 operands, 3 of 4096 x 4096, 408 tiles, 3930 (4971), but 14 of 1024 x 4096, 140
+// tiles, 1665 (1457).  With pairs, whose three products share no fragments there, it lies further up:
+// 4 of 2048 x 8192 6681 (7331), 3 of 4096 x 4096 11217 (13184), but 16 of 2048 x 2048, 576 tiles, 10396 (9217) and
+// 28 of 1024 x 4096, 280 tiles, 7605 (7070).
 constexpr int64_t kMuonBigSide = 1024, kMuonBigTiles = 128;
 bool muon_big(const attr_muon_matrix* mats, int32_t n) {
   int64_t tiles = 0;

@@ -10,7 +10,7 @@
 
 namespace attr {
 
-// p(x) = a x + b x^3 + c x^5
+// p(x) = a x + b x^3 + c x^5, the coefficients published with the method (K. Jordan and others, 2024)
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 
 // The group of a launch that holds this workgroup: the last whose first workgroup is not past it.

@@ -7,9 +7,10 @@
 // digits, and has them: G, the iteration and the last product are in fp64 on the matrix cores
 // (16 x 16 x 4).  u is computed twice and nothing of its size is stored: bound by memory, the
 // gradient and the momentum read twice, the momentum and the weights written once.  168 matrices of rank 16
-// (59 MB): 14 us for G, 8.5 for the steps, whose 20 dependent products are one workgroup's, and 13 for X,
-// of 38.7 in all; as 128 x 128 tiles with pairs 209 where this takes 27 (56 of 16 x 1024), and for
-// 8 of 4096 x 64 473 where this takes 112.
+// (59 MB): 14 us for G, 8.5 for the steps, whose 18 products, 14 of them one after another, are one
+// workgroup's, 13 for X and 6.6 for the two launches that copy the matrices' table, of 38.7 in all; as
+// 128 x 128 tiles with pairs 209 where this takes 27 (56 of 16 x 1024), and for 8 of 4096 x 64 473 where
+// this takes 112.
 //
 // Lanes of the 16 x 16 x 4 product: A's row and B's column are lane % 16, the fourth of K is
 // lane / 16, and D's column is lane % 16, its rows lane / 16 + 4 r.

@@ -707,3 +707,13 @@ def test_layer_norm_backward_long_shares(n, T, d, per_example):
     for got, term in ((dw, g * u), (db, g)):
         total, size = term.view(units, -1, d).sum(1), term.abs().view(units, -1, d).sum(1)
         assert ((got.double() - total - 0.5).abs() <= terms * U * size + U).all()
+
+
+def test_layer_norm_past_fp32s_range():
+    """A row whose sum passes fp32's range is NaN, one whose squares do has 1/std 0; their neighbours are their own."""
+    x = torch.ones(4, 600, device="cuda")
+    x[0], x[1, ::2], x[1, 1::2], x[2, 0] = 3e38, 3e38, -3e38, 2.0
+    y, rstd = torch.empty_like(x), torch.empty(4, device="cuda")
+    P.attr_layer_norm(x, y, rstd=rstd)
+    assert torch.isnan(y[0]).all() and (y[1] == 0).all() and rstd[1] == 0
+    assert torch.isfinite(y[2:]).all() and (y[3] == 0).all()
